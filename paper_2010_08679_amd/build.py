@@ -5,7 +5,10 @@ from __future__ import annotations
 import glob
 import hashlib
 import os
+import shutil
 import subprocess
+import tempfile
+from concurrent.futures import ThreadPoolExecutor
 
 PKG = os.path.dirname(os.path.abspath(__file__))
 ROOT = os.path.dirname(PKG)
@@ -26,18 +29,25 @@ HIPCC_FLAGS = [
     "-Wall", "-Wno-unused-function",
 ]
 
+# The operators for language models (csrc/lm_*.hip) take infinities and NaN: comparisons with them count there.
+NANS_COUNT = [f for f in HIPCC_FLAGS if f not in ("-fno-honor-nans", "-mno-amdgpu-ieee")]
+
+
+def flags_of(source: str):
+    return NANS_COUNT if os.path.basename(source).startswith("lm_") else HIPCC_FLAGS
+
 
 def sources():
     return sorted(glob.glob(os.path.join(CSRC, "*.hip")))
 
 
 def dependencies():
-    return sources() + sorted(glob.glob(os.path.join(CSRC, "*.h"))) + [os.path.join(ROOT, "include", "cnr.h")]
+    return sources() + sorted(glob.glob(os.path.join(CSRC, "*.h"))) + [os.path.join(ROOT, "include", h) for h in ("cnr.h", "cnr_lm.h")]
 
 
 def source_hash() -> str:
     """Hash of the compiler flags and of every file the library is built from."""
-    h = hashlib.sha256(" ".join(HIPCC_FLAGS).encode())
+    h = hashlib.sha256(" ".join(HIPCC_FLAGS + NANS_COUNT).encode())
     for path in dependencies():
         h.update(os.path.basename(path).encode())
         with open(path, "rb") as f:
@@ -58,16 +68,28 @@ def is_stale() -> bool:
 
 
 def build_lib(force: bool = True, verbose: bool = False) -> str:
-    """Runs hipcc over every .hip file under csrc/ and links them into libcnr.so."""
+    """Runs hipcc over every .hip file under csrc/, each with its flags, and links them into libcnr.so."""
     if not force and not is_stale():
         return LIB
     hipcc = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
     tmp = LIB + ".tmp.%d" % os.getpid()
-    cmd = [hipcc, *HIPCC_FLAGS, "-I", os.path.join(ROOT, "include"), "-I", CSRC, "-o", tmp, *sources()]
-    if verbose:
-        print(" ".join(cmd), flush=True)
     built_from = source_hash()
-    subprocess.check_call(cmd)
+    objects = tempfile.mkdtemp(prefix="cnr_build_")
+
+    def compiled(source):
+        to = os.path.join(objects, os.path.basename(source) + ".o")
+        cmd = [hipcc, *(f for f in flags_of(source) if f != "-shared"), "-I", os.path.join(ROOT, "include"), "-I", CSRC, "-c", source, "-o", to]
+        if verbose:
+            print(" ".join(cmd), flush=True)
+        subprocess.check_call(cmd)
+        return to
+
+    try:
+        with ThreadPoolExecutor(4) as pool:
+            parts = list(pool.map(compiled, sources()))
+        subprocess.check_call([hipcc, "--offload-arch=gfx950", "-fPIC", "-shared", "-o", tmp, *parts])
+    finally:
+        shutil.rmtree(objects, ignore_errors=True)
     os.replace(tmp, LIB)
     with open(STAMP, "w") as f:
         f.write(built_from + "\n")

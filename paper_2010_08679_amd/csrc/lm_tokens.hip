@@ -1,0 +1,283 @@
+// Tokens that sequences hold, and what follows from them for their logits.
+//
+// A sequence's state is a slot: a bitmap of the vocabulary (laid out as a table's tracking bitmap) and a counter for each token.
+// The bitmap is what makes the adjustment cheap: of a row's 4 bytes a token of counters only those of seen
+// tokens are read, so that beside the logits a row costs its two bitmaps, 1/16 byte a token each way.
+#include "lm_common.h"
+
+namespace {
+
+// ---- counts ---------------------------------------------------------------------------------------------------
+
+struct CountArgs {
+    uint32_t *seen, *counts;
+    uint64_t n_slots, vocab, words;
+    const void *tokens;
+    uint64_t n_tokens;
+    const uint64_t *offsets;
+    const int32_t *slots;
+    uint64_t n;
+    cnr_dev_errors *err;
+};
+
+// Slot of sequence i, or n_slots where it has none.
+__device__ __forceinline__ uint64_t slot_of(const int32_t *slots, uint64_t n_slots, uint64_t i) {
+    const int64_t s = slots ? (int64_t)slots[i] : (int64_t)i;
+    return s >= 0 && (uint64_t)s < n_slots ? (uint64_t)s : n_slots;
+}
+
+// Empties the slots of the call: grid.y a sequence, grid.x shares of its state.
+__global__ void __launch_bounds__(kBlock) restart_kernel(const CountArgs a, uint32_t shares) {
+    for (uint64_t i = wg_y(); i < a.n; i += 32768) {
+        const uint64_t slot = slot_of(a.slots, a.n_slots, i);
+        if (slot == a.n_slots) continue;
+        uint32_t *seen = a.seen + slot * a.words;
+        for (uint64_t at = (uint64_t)wg_x() * kBlock + tid_x(); at < a.words; at += (uint64_t)shares * kBlock) seen[at] = 0u;
+        if (!a.counts) continue;
+        uint32_t *counts = a.counts + slot * a.vocab;
+        for (uint64_t at = (uint64_t)wg_x() * kBlock + tid_x(); at < a.vocab; at += (uint64_t)shares * kBlock) counts[at] = 0u;
+    }
+}
+
+// The sequence that token p belongs to: the last one that begins at or before p; n where p lies in none.
+__device__ __forceinline__ uint64_t sequence_of(const uint64_t *offsets, uint64_t n, uint64_t p) {
+    uint64_t lo = 0, hi = n;  // offsets[lo] <= p, if any is
+    while (hi - lo > 1) {
+        const uint64_t mid = (lo + hi) / 2;
+        if (offsets[mid] <= p)
+            lo = mid;
+        else
+            hi = mid;
+    }
+    return offsets[lo] <= p && p < offsets[lo + 1] ? lo : n;
+}
+
+// A thread for each token.
+template <typename Index>
+__global__ void __launch_bounds__(kBlock) count_kernel(const CountArgs a) {
+    const uint64_t p = (uint64_t)wg_x() * kBlock + tid_x();
+    if (p >= a.n_tokens) return;
+    const int64_t token = (int64_t)reinterpret_cast<const Index *>(a.tokens)[p];
+    const uint64_t i = a.offsets ? sequence_of(a.offsets, a.n, p) : p;
+    if (i >= a.n) return;
+    const uint64_t slot = slot_of(a.slots, a.n_slots, i);
+    if (slot == a.n_slots) {
+        raise_flag(a.err, CNR_FLAG_ROW_ID);
+        return;
+    }
+    if (token < 0 || (uint64_t)token >= a.vocab) {
+        atomicAdd(&a.err->n_bad_indices, 1ull);
+        return;
+    }
+    uint32_t *word = a.seen + slot * a.words + ((uint64_t)token >> 5);
+    const uint32_t bit = 1u << ((uint32_t)token & 31u);
+    if (!(*word & bit)) atomicOr(word, bit);
+    if (a.counts) atomicAdd(a.counts + slot * a.vocab + (uint64_t)token, 1u);
+}
+
+// ---- logits -----------------------------------------------------------------------------------------------------
+
+constexpr uint32_t kTokensPerThread = 8;
+constexpr uint32_t kChunk = kBlock * kTokensPerThread;  // tokens of a workgroup
+
+struct AdjustArgs {
+    const void *logits;
+    void *out;
+    uint64_t stride, out_stride;
+    uint64_t n, vocab, words;
+    cnr_adjustments with;
+    cnr_dev_errors *err;
+};
+
+// First entry of bias_tokens[lo, hi) that is not below `token`.
+__device__ __forceinline__ uint64_t bias_from(const int32_t *tokens, uint64_t lo, uint64_t hi, int64_t token) {
+    while (lo < hi) {
+        const uint64_t mid = (lo + hi) / 2;
+        if ((int64_t)tokens[mid] < token)
+            lo = mid + 1;
+        else
+            hi = mid;
+    }
+    return lo;
+}
+
+// grid.x: chunks of the vocabulary, grid.y: rows.
+template <int TYPE>
+__global__ void __launch_bounds__(kBlock) adjust_kernel(const AdjustArgs a) {
+    typedef typename Element<TYPE>::type T;
+    __shared__ float bias[kChunk];
+    const cnr_adjustments &w = a.with;
+    const uint32_t begin = wg_x() * kChunk, first = begin + tid_x() * kTokensPerThread;
+    for (uint64_t row = wg_y(); row < a.n; row += 32768) {
+        // 8 tokens' bits lie in one byte of a bitmap, since `first` is a multiple of 8
+        uint32_t allowed = 0xffu, seen = 0u;
+        const bool inside = first < a.vocab;
+        uint64_t slot = 0;
+        if (w.masks) {
+            const int64_t m = w.mask_of ? (int64_t)w.mask_of[row] : (int64_t)row;
+            if (m >= 0 && (uint64_t)m < w.n_masks) {
+                if (inside) allowed = w.masks[(uint64_t)m * a.words + first / 32] >> (first % 32) & 0xffu;
+            } else if (m >= 0 && begin == 0 && tid_x() == 0) {
+                raise_flag(a.err, CNR_FLAG_ROW_ID);
+            }
+        }
+        if (w.seen) {
+            const int64_t s = w.slots ? (int64_t)w.slots[row] : (int64_t)row;
+            if (s >= 0 && (uint64_t)s < w.n_slots) {
+                slot = (uint64_t)s;
+                if (inside) seen = w.seen[slot * a.words + first / 32] >> (first % 32) & 0xffu;
+            } else if (s >= 0 && begin == 0 && tid_x() == 0) {
+                raise_flag(a.err, CNR_FLAG_ROW_ID);
+            }
+        }
+        bool biased = false;
+        if (w.bias_offsets) {
+            uint64_t lo = w.bias_offsets[row], hi = w.bias_offsets[row + 1];
+            hi = hi < w.n_bias ? hi : w.n_bias;
+            if (lo < hi) {
+                lo = bias_from(w.bias_tokens, lo, hi, (int64_t)begin);
+                hi = bias_from(w.bias_tokens, lo, hi, (int64_t)begin + kChunk);
+            }
+            if (lo < hi) {  // the same for the whole workgroup
+                biased = true;
+                __syncthreads();
+#pragma unroll
+                for (uint32_t j = 0; j < kTokensPerThread; ++j) bias[j * kBlock + tid_x()] = 0.0f;
+                __syncthreads();
+                for (uint64_t e = lo + tid_x(); e < hi; e += kBlock) {
+                    const int64_t at = (int64_t)w.bias_tokens[e] - (int64_t)begin;
+                    if (at >= 0 && at < (int64_t)kChunk) bias[at] = w.bias_values[e];
+                }
+                __syncthreads();
+            }
+        }
+        if (!inside) continue;
+        const T *from = reinterpret_cast<const T *>(a.logits) + row * a.stride + first;
+        T *to = reinterpret_cast<T *>(a.out) + row * a.out_stride + first;
+        const bool whole = first + kTokensPerThread <= a.vocab;
+        Pack<T, kTokensPerThread> got;
+        if (whole)
+            got = *reinterpret_cast<const Pack<T, kTokensPerThread> *>(from);
+        else
+#pragma unroll
+            for (uint32_t j = 0; j < kTokensPerThread; ++j) got.v[j] = first + j < a.vocab ? from[j] : (T)0.0f;
+        float v[kTokensPerThread];
+#pragma unroll
+        for (uint32_t j = 0; j < kTokensPerThread; ++j) v[j] = Element<TYPE>::wide(got.v[j]);
+        if (seen) {
+            const float repetition = w.repetition ? w.repetition[row] : 1.0f;
+            const float frequency = w.frequency ? w.frequency[row] : 0.0f, presence = w.presence ? w.presence[row] : 0.0f;
+            const uint32_t *counts = w.counts ? w.counts + slot * a.vocab + first : nullptr;
+#pragma unroll
+            for (uint32_t j = 0; j < kTokensPerThread; ++j) {
+                if (!(seen >> j & 1u) || first + j >= a.vocab) continue;
+                v[j] = v[j] > 0.0f ? v[j] / repetition : v[j] * repetition;
+                if (counts) {
+                    const uint32_t count = counts[j];
+                    v[j] -= frequency * (float)count;
+                    if (count) v[j] -= presence;
+                }
+            }
+        }
+        if (biased) {
+#pragma unroll
+            for (uint32_t j = 0; j < kTokensPerThread; ++j) v[j] += bias[tid_x() * kTokensPerThread + j];
+        }
+        Pack<T, kTokensPerThread> put;
+#pragma unroll
+        for (uint32_t j = 0; j < kTokensPerThread; ++j)
+            put.v[j] = Element<TYPE>::narrow(allowed >> j & 1u ? v[j] : -__builtin_inff());
+        if (whole)
+            *reinterpret_cast<Pack<T, kTokensPerThread> *>(to) = put;
+        else
+#pragma unroll
+            for (uint32_t j = 0; j < kTokensPerThread; ++j)
+                if (first + j < a.vocab) to[j] = put.v[j];
+    }
+}
+
+}  // namespace
+
+extern "C" {
+
+cnr_status cnr_count_tokens(cnr_ctx *ctx, uint32_t *seen, uint32_t *counts, uint64_t n_slots, uint64_t vocab,
+                            const void *tokens, uint64_t n_tokens, cnr_index_type type, const uint64_t *offsets,
+                            const int32_t *slots, uint64_t n, int prompt, int restart, void *stream) {
+    if (!ctx || (type != CNR_IDX_I32 && type != CNR_IDX_I64)) return CNR_E_INVALID;
+    if (!offsets && n_tokens != n) return CNR_E_INVALID;
+    if (vocab > CNR_LM_MAX_SIZE || n > CNR_LM_MAX_SIZE || n_slots > CNR_LM_MAX_SIZE || n_tokens > CNR_LM_MAX_SIZE) return CNR_E_TOO_LARGE;
+    if (n == 0) return CNR_OK;
+    if (!seen && n_slots && vocab) return CNR_E_INVALID;
+    if (!tokens && n_tokens) return CNR_E_INVALID;
+    if (!cnr_aligned(seen, 4) || !cnr_aligned(counts, 4) || !cnr_aligned(tokens, type == CNR_IDX_I64 ? 8 : 4) || !cnr_aligned(offsets, 8) ||
+        !cnr_aligned(slots, 4))
+        return CNR_E_ALIGN;
+    cnr_status st = cnr_enter(ctx);
+    if (st != CNR_OK) return st;
+    CountArgs a;
+    a.seen = seen;
+    a.counts = counts;
+    a.n_slots = n_slots;
+    a.vocab = vocab;
+    a.words = cnr_bitmap_words(vocab);
+    a.tokens = tokens;
+    a.n_tokens = n_tokens;
+    a.offsets = offsets;
+    a.slots = slots;
+    a.n = n;
+    a.err = ctx->dev_err;
+    hipStream_t s = as_stream(stream);
+    if (restart && vocab && n_slots) {
+        const uint32_t shares = (uint32_t)cnr_ceil_div(counts ? vocab : a.words, 16 * kBlock);
+        hipLaunchKernelGGL(restart_kernel, dim3(shares, (unsigned)(n < 32768 ? n : 32768)), dim3(kBlock), 0, s, a, shares);
+        st = cnr_launch_status(ctx);
+        if (st != CNR_OK) return st;
+    }
+    if (n_tokens == 0) return CNR_OK;
+    if (prompt) a.counts = nullptr;
+    const unsigned grid = (unsigned)cnr_ceil_div(n_tokens, kBlock);
+    if (type == CNR_IDX_I64)
+        hipLaunchKernelGGL((count_kernel<int64_t>), dim3(grid), dim3(kBlock), 0, s, a);
+    else
+        hipLaunchKernelGGL((count_kernel<int32_t>), dim3(grid), dim3(kBlock), 0, s, a);
+    return cnr_launch_status(ctx);
+}
+
+cnr_status cnr_adjust_logits(cnr_ctx *ctx, const void *logits, uint64_t stride, void *out, uint64_t out_stride,
+                             cnr_float_type type, uint64_t n, uint64_t vocab, const cnr_adjustments *adjustments,
+                             void *stream) {
+    if (!ctx || !adjustments || !cnr_valid_float_type(type) || stride < vocab || out_stride < vocab) return CNR_E_INVALID;
+    const cnr_adjustments &w = *adjustments;
+    if (vocab > CNR_LM_MAX_SIZE || n > CNR_LM_MAX_SIZE) return CNR_E_TOO_LARGE;
+    if (n == 0 || vocab == 0) return CNR_OK;
+    if (!logits || !out || (logits == out && stride != out_stride)) return CNR_E_INVALID;
+    if (w.bias_offsets && w.n_bias && (!w.bias_tokens || !w.bias_values)) return CNR_E_INVALID;
+    const size_t element = cnr_float_bytes(type);
+    if (!cnr_aligned(logits, element) || !cnr_aligned(out, element) || !cnr_aligned(w.seen, 4) || !cnr_aligned(w.counts, 4) ||
+        !cnr_aligned(w.slots, 4) || !cnr_aligned(w.repetition, 4) || !cnr_aligned(w.frequency, 4) || !cnr_aligned(w.presence, 4) ||
+        !cnr_aligned(w.bias_offsets, 8) || !cnr_aligned(w.bias_tokens, 4) || !cnr_aligned(w.bias_values, 4) || !cnr_aligned(w.masks, 4) ||
+        !cnr_aligned(w.mask_of, 4))
+        return CNR_E_ALIGN;
+    cnr_status st = cnr_enter(ctx);
+    if (st != CNR_OK) return st;
+    AdjustArgs a;
+    a.logits = logits;
+    a.out = out;
+    a.stride = stride;
+    a.out_stride = out_stride;
+    a.n = n;
+    a.vocab = vocab;
+    a.words = cnr_bitmap_words(vocab);
+    a.with = w;
+    a.err = ctx->dev_err;
+    const dim3 grid((unsigned)cnr_ceil_div(vocab, kChunk), (unsigned)(n < 32768 ? n : 32768));
+    if (type == CNR_FLOAT_F32)
+        hipLaunchKernelGGL((adjust_kernel<CNR_FLOAT_F32>), grid, dim3(kBlock), 0, as_stream(stream), a);
+    else if (type == CNR_FLOAT_BF16)
+        hipLaunchKernelGGL((adjust_kernel<CNR_FLOAT_BF16>), grid, dim3(kBlock), 0, as_stream(stream), a);
+    else
+        hipLaunchKernelGGL((adjust_kernel<CNR_FLOAT_F16>), grid, dim3(kBlock), 0, as_stream(stream), a);
+    return cnr_launch_status(ctx);
+}
+
+}  // extern "C"

@@ -1,0 +1,169 @@
+"""Operators for language models over the library's calls (``include/cnr_lm.h``): matrices in 8-bit floating point with
+a scale for each block of 128, a linear layer trained and served in them, and the tokens that sequences hold with
+what follows from them for their logits.
+
+Plumbing only, as in :mod:`checkpoint`: torch allocates the memory and provides the stream, every step runs in libcnr's
+kernels.
+"""
+from __future__ import annotations
+
+from dataclasses import dataclass
+
+import torch
+
+from . import lm_binding as L
+
+
+@dataclass
+class BlockMatrix:
+    """A matrix of n_rows x dim as e4m3 codes and the scales of its blocks (layout in ``include/cnr_lm.h``)."""
+    codes: torch.Tensor   # uint8 [n_rows, dim rounded up to a multiple of 128]
+    scale: torch.Tensor   # uint8 (powers of two, e8m0) or float32 [ceil(dim / 128), cnr_block_scale_stride(n_rows, kind)]
+    n_rows: int
+    dim: int
+    kind: int = L.CNR_BLOCK_ROW
+
+    @property
+    def scale_type(self) -> int:
+        return L._kind(L._SCALES, self.scale, "scale", "uint8 or float32")
+
+    @staticmethod
+    def empty(n_rows: int, dim: int, kind: int = L.CNR_BLOCK_ROW, scale_type: int = L.CNR_SCALE_E8M0, device="cuda:0") -> "BlockMatrix":
+        across, down = -(-dim // L.CNR_BLOCK), -(-n_rows // L.CNR_BLOCK)
+        return BlockMatrix(torch.empty(n_rows, across * L.CNR_BLOCK, dtype=torch.uint8, device=device),
+                           torch.empty(across, down if kind == L.CNR_BLOCK_TILE else down * L.CNR_BLOCK,
+                                       dtype=torch.uint8 if scale_type == L.CNR_SCALE_E8M0 else torch.float32, device=device),
+                           n_rows, dim, kind)
+
+
+def quantize_blocks(ctx, x: torch.Tensor, out: BlockMatrix | None = None, out_t: BlockMatrix | None = None, stream=None) -> BlockMatrix | None:
+    """Quantizes the matrix ``x`` into ``out`` and its transpose into ``out_t`` (either may be None; a new matrix of rows' blocks
+    with scales of powers of two where both are)."""
+    if out is None and out_t is None:
+        out = BlockMatrix.empty(*x.shape, device=x.device)
+    like = out if out is not None else out_t
+    for m, shape in ((out, tuple(x.shape)), (out_t, tuple(x.shape)[::-1])):
+        if m is not None and ((m.n_rows, m.dim) != shape or m.kind != like.kind or m.scale_type != like.scale_type):
+            raise ValueError("a blocked matrix of another size, kind or scale type")
+    L.cnr_quantize_blocks(ctx, x, like.kind, like.scale_type, *((out.codes, out.scale) if out is not None else (None, None)),
+                          *((out_t.codes, out_t.scale) if out_t is not None else (None, None)), stream)
+    return out
+
+
+def block_workspace(ctx, m: int, n: int, k: int, device="cuda:0") -> torch.Tensor | None:
+    """What :func:`block_product` may use for a product of these sizes; None where it has no use for any."""
+    size = L.cnr_block_product_workspace_bytes(ctx, m, n, k)
+    return torch.empty(size, dtype=torch.uint8, device=device) if size else None
+
+
+def block_product(ctx, a: BlockMatrix, b: BlockMatrix, out: torch.Tensor | None = None, accumulate: bool = False,
+                  workspace: torch.Tensor | None = None, stream=None) -> torch.Tensor:
+    """``a`` times the transpose of ``b``, written to or added to ``out`` (a new bfloat16 matrix when None)."""
+    if a.dim != b.dim:
+        raise ValueError("rows of %d and of %d columns" % (a.dim, b.dim))
+    if out is None:
+        if accumulate:
+            raise ValueError("nothing to add to")
+        out = torch.empty(a.n_rows, b.n_rows, dtype=torch.bfloat16, device=a.codes.device)
+    elif tuple(out.shape) != (a.n_rows, b.n_rows):
+        raise ValueError("out must be %d x %d" % (a.n_rows, b.n_rows))
+    L.cnr_block_product(ctx, a.codes, a.scale, a.kind, a.n_rows, b.codes, b.scale, b.kind, b.n_rows, a.dim, out, accumulate, workspace, stream)
+    return out
+
+
+class BlockLinear:
+    """y = x W^T in 8 bits, forward and backward, for up to max_tokens rows of x at a time.
+
+    The layer keeps the weight in tiles in both directions (:meth:`load`, after every change of the weight) and, from :meth:`forward` to
+    :meth:`backward`, the transpose of its input.  Calls of one layer belong on one stream."""
+
+    def __init__(self, ctx, n_out: int, n_in: int, max_tokens: int, scale_type: int = L.CNR_SCALE_E8M0, device="cuda:0"):
+        self.ctx, self.n_out, self.n_in, self.max_tokens, self.scale_type = ctx, int(n_out), int(n_in), int(max_tokens), scale_type
+        self.device = torch.device(device)
+        self.weight = BlockMatrix.empty(n_out, n_in, L.CNR_BLOCK_TILE, scale_type, device)
+        self.weight_t = BlockMatrix.empty(n_in, n_out, L.CNR_BLOCK_TILE, scale_type, device)
+        self._x, self._x_t = self._buffers(max_tokens, n_in), self._buffers(n_in, max_tokens)
+        self._dy, self._dy_t = self._buffers(max_tokens, n_out), self._buffers(n_out, max_tokens)
+        self._input_t = None
+        self._sized = {}
+
+    def _buffers(self, n_rows: int, dim: int):
+        m = BlockMatrix.empty(n_rows, dim, L.CNR_BLOCK_ROW, self.scale_type, self.device)
+        return m.codes.view(-1), m.scale.view(-1)
+
+    def _of(self, buffers, n_rows: int, dim: int) -> BlockMatrix:
+        across, stride = -(-dim // L.CNR_BLOCK), -(-n_rows // L.CNR_BLOCK) * L.CNR_BLOCK
+        codes, scale = buffers
+        return BlockMatrix(codes[: n_rows * across * L.CNR_BLOCK].view(n_rows, across * L.CNR_BLOCK), scale[: across * stride].view(across, stride),
+                           n_rows, dim, L.CNR_BLOCK_ROW)
+
+    def _for(self, tokens: int):
+        """Input and output gradient of that many tokens within the layer's buffers, and a workspace for their products."""
+        if tokens > self.max_tokens:
+            raise ValueError("%d tokens, the layer was made for %d" % (tokens, self.max_tokens))
+        if tokens not in self._sized:
+            space = max(L.cnr_block_product_workspace_bytes(self.ctx, *s) for s in (
+                (tokens, self.n_out, self.n_in), (tokens, self.n_in, self.n_out), (self.n_out, self.n_in, tokens)))
+            self._sized = {tokens: (self._of(self._x, tokens, self.n_in), self._of(self._x_t, self.n_in, tokens),
+                                    self._of(self._dy, tokens, self.n_out), self._of(self._dy_t, self.n_out, tokens),
+                                    torch.empty(space, dtype=torch.uint8, device=self.device) if space else None)}
+        return self._sized[tokens]
+
+    def load(self, weight: torch.Tensor, stream=None) -> None:
+        """Takes the weight [n_out, n_in] as it is now."""
+        quantize_blocks(self.ctx, weight, self.weight, self.weight_t, stream)
+
+    def forward(self, x: torch.Tensor, out: torch.Tensor | None = None, training: bool = True, stream=None) -> torch.Tensor:
+        """x [tokens, n_in] -> [tokens, n_out], of x's type when ``out`` is None; ``training``: :meth:`backward` follows."""
+        qx, qx_t, _, _, space = self._for(x.shape[0])
+        quantize_blocks(self.ctx, x, qx, qx_t if training else None, stream)
+        self._input_t = qx_t if training else None
+        if out is None:
+            out = torch.empty(x.shape[0], self.n_out, dtype=x.dtype, device=self.device)
+        return block_product(self.ctx, qx, self.weight, out, workspace=space, stream=stream)
+
+    def backward(self, dy: torch.Tensor, dx: torch.Tensor | None = None, dw: torch.Tensor | None = None, accumulate: bool = False, stream=None):
+        """The gradients (dx of dy's type, dw in float32 unless given) of the last :meth:`forward`'s input and of the weight, the latter
+        added to ``dw`` where ``accumulate`` is set."""
+        if self._input_t is None or self._input_t.dim != dy.shape[0]:
+            raise ValueError("no forward pass of %d tokens in training precedes" % dy.shape[0])
+        _, _, qdy, qdy_t, space = self._for(dy.shape[0])
+        quantize_blocks(self.ctx, dy, qdy, qdy_t, stream)
+        if dx is None:
+            dx = torch.empty(dy.shape[0], self.n_in, dtype=dy.dtype, device=self.device)
+        if dw is None:
+            if accumulate:
+                raise ValueError("nothing to add to")
+            dw = torch.empty(self.n_out, self.n_in, dtype=torch.float32, device=self.device)
+        block_product(self.ctx, qdy, self.weight_t, dx, workspace=space, stream=stream)
+        block_product(self.ctx, qdy_t, self._input_t, dw, accumulate, space, stream)
+        return dx, dw
+
+
+class TokenLedger:
+    """The tokens of up to n_slots sequences: which of the vocabulary each has seen (a bitmap, as a table's tracking bitmap) and
+    how often the model wrote each."""
+
+    def __init__(self, ctx, n_slots: int, vocab: int, seen: torch.Tensor | None = None, counts: torch.Tensor | None = None, device="cuda:0"):
+        self.ctx, self.n_slots, self.vocab = ctx, int(n_slots), int(vocab)
+        words = (self.vocab + 31) // 32
+        self.seen = torch.zeros(n_slots, words, dtype=torch.int32, device=device) if seen is None else seen
+        self.counts = torch.zeros(n_slots, vocab, dtype=torch.int32, device=device) if counts is None and seen is None else counts
+
+    def count(self, tokens: torch.Tensor, offsets: torch.Tensor | None = None, slots: torch.Tensor | None = None, prompt: bool = False,
+              restart: bool = False, stream=None) -> None:
+        """Enters one token of each sequence, or those that ``offsets`` gives each; ``restart`` empties the slots first."""
+        L.cnr_count_tokens(self.ctx, self.seen, self.counts, self.n_slots, self.vocab, tokens, offsets, slots, prompt, restart, stream)
+
+    def adjust(self, logits: torch.Tensor, out: torch.Tensor | None = None, slots: torch.Tensor | None = None, repetition=None, frequency=None,
+               presence=None, bias=None, masks: torch.Tensor | None = None, mask_of: torch.Tensor | None = None, stream=None) -> torch.Tensor:
+        """Applies penalties (float32 [n] each), biases (offsets, tokens, values) and masks to ``logits`` [n, vocab], in place when ``out``
+        is None."""
+        if logits.shape[1] != self.vocab:
+            raise ValueError("logits of %d tokens, a vocabulary of %d" % (logits.shape[1], self.vocab))
+        out = logits if out is None else out
+        penalties = repetition is not None or frequency is not None or presence is not None
+        seen, counts = (self.seen, self.counts) if penalties else (None, None)
+        L.cnr_adjust_logits(self.ctx, logits, out, seen, counts, self.n_slots if penalties else 0, slots, repetition, frequency, presence,
+                            *(bias if bias is not None else (None, None, None)), masks, 0 if masks is None else masks.shape[0], mask_of, stream)
+        return out

@@ -104,7 +104,8 @@ _call.ctx = ctypes.create_string_buffer(4096)
     ("cnr_block_product", ALIGN, dict(a_codes=A + 8)), ("cnr_block_product", ALIGN, dict(b_codes=A + 1)), ("cnr_block_product", ALIGN, dict(a_scale=A + 2)),
     ("cnr_block_product", ALIGN, dict(b_scale=A + 8)), ("cnr_block_product", ALIGN, dict(out=A + 2)), ("cnr_block_product", ALIGN, dict(workspace=A + 8)),
     ("cnr_block_product", TOO_LARGE, dict(m=1 << 31)), ("cnr_block_product", TOO_LARGE, dict(n=1 << 31, out_stride=1 << 31)),
-    ("cnr_block_product", TOO_LARGE, dict(k=1 << 31)),
+    ("cnr_block_product", TOO_LARGE, dict(k=1 << 31)), ("cnr_block_product", TOO_LARGE, dict(m=1 << 20, n=1 << 20, out_stride=1 << 20)),
+    ("cnr_block_product", TOO_LARGE, dict(m=1 << 20, k=1 << 24)),
     ("cnr_block_product", OK, dict(m=0)), ("cnr_block_product", OK, dict(n=0)), ("cnr_block_product", OK, dict(k=0, accumulate=1)),
     ("cnr_count_tokens", INVALID, dict(ctx=None)), ("cnr_count_tokens", INVALID, dict(type=2)), ("cnr_count_tokens", INVALID, dict(seen=None)),
     ("cnr_count_tokens", INVALID, dict(tokens=None)), ("cnr_count_tokens", INVALID, dict(offsets=None, n=3)),

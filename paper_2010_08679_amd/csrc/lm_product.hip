@@ -2,7 +2,8 @@
 //
 // Both operands have k along their rows, so a matrix instruction's operand is 32 bytes in a row of codes for each lane,
 // whichever way a block is held.  Which of the block's 128 columns a lane's bytes are does not matter as long as
-// both operands agree: a lane takes the 32 bytes from 32 * (lane / 16) of row lane % 16.
+// both operands agree: a lane takes 16 bytes from 16 * (lane / 16) of row lane % 16 and 16 from 64 bytes further on, so
+// that a load of all lanes reads 64 bytes in a row.
 //
 // Two ways to add up a block's 16 x 16 x 128 products:
 //   8-bit instructions, scales of powers of two applied by them.  Exact products; of each eight that are added in one
@@ -32,6 +33,9 @@ struct ProductArgs {
     void *out;
     uint64_t out_stride;
     int out_type, accumulate;
+    uint32_t splits;                // parts of the sum, each in its own workgroups
+    float *partial;                 // [splits][m][partial_stride]
+    uint64_t partial_stride;
 };
 
 template <int SCALE>
@@ -65,7 +69,7 @@ __device__ __forceinline__ Wide widen(const i32x8 &codes, uint32_t scale) {
 }
 
 __device__ __forceinline__ i32x8 load_codes(const uint8_t *p) {
-    const i32x4 lo = *reinterpret_cast<const i32x4 *>(p), hi = *reinterpret_cast<const i32x4 *>(p + 16);
+    const i32x4 lo = *reinterpret_cast<const i32x4 *>(p), hi = *reinterpret_cast<const i32x4 *>(p + 64);
     return __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7);
 }
 
@@ -83,37 +87,39 @@ __device__ __forceinline__ void store_out(const ProductArgs &p, uint32_t m, uint
     }
 }
 
-// Few rows of A: the codes of B are read once, straight into the matrix instructions' registers.  A workgroup has 16 MF x 16 NF
-// outputs; its waves take every fourth block of columns and add up their sums in LDS at the end.
-template <int SCALE, bool FULL, int MF, int NF>
+// A scale's exponent goes into the matrix instruction and its fraction, from 1 to 2, multiplies the sum: neither leaves fp32's range
+// unless the result does.  (A scale below 2^-126 counts as 0.)
+__device__ __forceinline__ float fraction_of(float s) {
+    const uint32_t b = __float_as_uint(s);
+    return b & 0x7f800000u ? __uint_as_float((b & 0x807fffffu) | 0x3f800000u) : 0.0f;
+}
+__device__ __forceinline__ uint32_t exponent_of(float s) { return __float_as_uint(s) >> 23 & 255u; }
+
+// ---- few rows or few tiles: operands straight from memory ---------------------------------------------------------
+//
+// A workgroup has 16 MF x 16 NF outputs; its waves take every fourth block of columns, U of them at a time so that enough loads are
+// under way, straight into the matrix instructions' registers, and add up their sums in LDS at the end.
+template <int SCALE, bool FULL, int MF, int NF, int U>
 __global__ void __launch_bounds__(kBlock) narrow_kernel(const ProductArgs p) {
     typedef typename ScaleOf<SCALE>::type S;
     __shared__ f32x4 sums[kWavesPerBlock][MF * NF][kWave];
     const uint32_t lane = tid_x() % kWave, wave = (uint32_t)__builtin_amdgcn_readfirstlane((int)(tid_x() / kWave));
-    const uint32_t m0 = wg_y() * 16 * MF, n0 = wg_x() * 16 * NF;
+    const uint32_t quarter = lane / 16, m0 = wg_y() * 16 * MF, n0 = wg_x() * 16 * NF;
+    // Rows beyond the matrix read its last one again.
     const uint8_t *a[MF], *b[NF];
     const S *sa[MF], *sb[NF];
-    uint32_t sa_at[MF][4];  // scales of the rows of A that a lane's four sums belong to
 #pragma unroll
     for (int f = 0; f < MF; ++f) {
         uint32_t r = m0 + 16 * f + lane % 16;
         r = r < p.m ? r : p.m - 1;
-        a[f] = p.a + (uint64_t)r * p.row_bytes + lane / 16 * 32;
+        a[f] = p.a + (uint64_t)r * p.row_bytes + quarter * 16;
         sa[f] = reinterpret_cast<const S *>(p.a_scale) + (r >> p.a_shift);
-        if (SCALE == CNR_SCALE_F32) {
-            sa[f] = reinterpret_cast<const S *>(p.a_scale);
-#pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                const uint32_t q = m0 + 16 * f + lane / 16 * 4 + i;
-                sa_at[f][i] = (q < p.m ? q : p.m - 1) >> p.a_shift;
-            }
-        }
     }
 #pragma unroll
     for (int f = 0; f < NF; ++f) {
         uint32_t r = n0 + 16 * f + lane % 16;
         r = r < p.n ? r : p.n - 1;
-        b[f] = p.b + (uint64_t)r * p.row_bytes + lane / 16 * 32;
+        b[f] = p.b + (uint64_t)r * p.row_bytes + quarter * 16;
         sb[f] = reinterpret_cast<const S *>(p.b_scale) + (r >> p.b_shift);
     }
     f32x4 acc[MF][NF];
@@ -122,58 +128,72 @@ __global__ void __launch_bounds__(kBlock) narrow_kernel(const ProductArgs p) {
 #pragma unroll
         for (int g = 0; g < NF; ++g) acc[f][g] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
 
-    for (uint32_t kb = wave; kb < p.blocks; kb += kWavesPerBlock) {
-        i32x8 x[MF], y[NF];
+    for (uint32_t first = wave; first < p.blocks; first += U * kWavesPerBlock) {
+        i32x8 x[U][MF], y[U][NF];
+        S s[U][MF], t[U][NF];
 #pragma unroll
-        for (int f = 0; f < NF; ++f) y[f] = load_codes(b[f] + (uint64_t)kb * CNR_BLOCK);
+        for (int u = 0; u < U; ++u) {
+            const uint32_t kb = first + u * kWavesPerBlock;
+            if (u && kb >= p.blocks) break;
 #pragma unroll
-        for (int f = 0; f < MF; ++f) x[f] = load_codes(a[f] + (uint64_t)kb * CNR_BLOCK);
-        S t[NF];
-#pragma unroll
-        for (int f = 0; f < NF; ++f) t[f] = sb[f][kb * p.b_stride];
-        if (SCALE == CNR_SCALE_E8M0) {
-            uint32_t s[MF];
-#pragma unroll
-            for (int f = 0; f < MF; ++f) s[f] = (uint32_t)sa[f][kb * p.a_stride];
-            if (FULL) {
-                Wide wx[MF];
-#pragma unroll
-                for (int f = 0; f < MF; ++f) wx[f] = widen(x[f], s[f]);
-#pragma unroll
-                for (int g = 0; g < NF; ++g) {
-                    const Wide wy = widen(y[g], (uint32_t)t[g]);
-#pragma unroll
-                    for (int f = 0; f < MF; ++f)
-#pragma unroll
-                        for (int i = 0; i < 4; ++i) acc[f][g] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(wx[f].part[i], wy.part[i], acc[f][g], 0, 0, 0);
-                }
-            } else {
-#pragma unroll
-                for (int f = 0; f < MF; ++f)
-#pragma unroll
-                    for (int g = 0; g < NF; ++g)
-                        acc[f][g] = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(x[f], y[g], acc[f][g], 0, 0, 0, (int)s[f], 0, (int)t[g]);
+            for (int f = 0; f < NF; ++f) {
+                y[u][f] = load_codes(b[f] + (uint64_t)kb * CNR_BLOCK);
+                t[u][f] = sb[f][kb * p.b_stride];
             }
-        } else {
-            const f32x4 zero = {0.0f, 0.0f, 0.0f, 0.0f};
 #pragma unroll
             for (int f = 0; f < MF; ++f) {
-                const S *from = sa[f] + kb * p.a_stride;
-                const f32x4 s = {(float)from[sa_at[f][0]], (float)from[sa_at[f][1]], (float)from[sa_at[f][2]], (float)from[sa_at[f][3]]};
-                Wide wx;
-                if (FULL) wx = widen(x[f], 127);
+                x[u][f] = load_codes(a[f] + (uint64_t)kb * CNR_BLOCK);
+                s[u][f] = sa[f][kb * p.a_stride];
+            }
+        }
 #pragma unroll
-                for (int g = 0; g < NF; ++g) {
-                    f32x4 d = zero;
-                    if (FULL) {
-                        const Wide wy = widen(y[g], 127);
+        for (int u = 0; u < U; ++u) {
+            if (u && first + u * kWavesPerBlock >= p.blocks) break;
+            uint32_t ex[MF], ey[NF];
+            float fy[NF], rows[MF][4];  // fractions; of A's those of the rows of the lane's sums
 #pragma unroll
-                        for (int i = 0; i < 4; ++i) d = __builtin_amdgcn_mfma_f32_16x16x32_bf16(wx.part[i], wy.part[i], d, 0, 0, 0);
+            for (int f = 0; f < MF; ++f) {
+                if constexpr (SCALE == CNR_SCALE_E8M0) {
+                    ex[f] = s[u][f];
+                } else {
+                    ex[f] = exponent_of(s[u][f]);
+                    const float fx = fraction_of(s[u][f]);
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) rows[f][i] = __shfl(fx, (int)(quarter * 4 + i));
+                }
+            }
+#pragma unroll
+            for (int g = 0; g < NF; ++g) {
+                if constexpr (SCALE == CNR_SCALE_E8M0) {
+                    ey[g] = t[u][g];
+                } else {
+                    ey[g] = exponent_of(t[u][g]);
+                    fy[g] = fraction_of(t[u][g]);
+                }
+            }
+            Wide wx[MF];
+            if constexpr (FULL)
+#pragma unroll
+                for (int f = 0; f < MF; ++f) wx[f] = widen(x[u][f], ex[f]);
+#pragma unroll
+            for (int g = 0; g < NF; ++g) {
+                Wide wy;
+                if constexpr (FULL) wy = widen(y[u][g], ey[g]);
+#pragma unroll
+                for (int f = 0; f < MF; ++f) {
+                    f32x4 d = SCALE == CNR_SCALE_F32 ? f32x4{0.0f, 0.0f, 0.0f, 0.0f} : acc[f][g];
+                    if constexpr (FULL) {
+#pragma unroll
+                        for (int i = 0; i < 4; ++i) d = __builtin_amdgcn_mfma_f32_16x16x32_bf16(wx[f].part[i], wy.part[i], d, 0, 0, 0);
                     } else {
-                        d = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(x[f], y[g], zero, 0, 0, 0, 127, 0, 127);
+                        d = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(x[u][f], y[u][g], d, 0, 0, 0, (int)ex[f], 0, (int)ey[g]);
                     }
+                    if constexpr (SCALE == CNR_SCALE_F32) {
 #pragma unroll
-                    for (int i = 0; i < 4; ++i) acc[f][g][i] = __builtin_fmaf(d[i] * s[i], (float)t[g], acc[f][g][i]);
+                        for (int i = 0; i < 4; ++i) acc[f][g][i] = __builtin_fmaf(d[i], rows[f][i] * fy[g], acc[f][g][i]);
+                    } else {
+                        acc[f][g] = d;
+                    }
                 }
             }
         }
@@ -183,8 +203,9 @@ __global__ void __launch_bounds__(kBlock) narrow_kernel(const ProductArgs p) {
 #pragma unroll
         for (int g = 0; g < NF; ++g) sums[wave][f * NF + g][lane] = acc[f][g];
     __syncthreads();
-    for (uint32_t e = tid_x(); e < 16 * MF * 16 * NF; e += kBlock) {
-        const uint32_t m = e / (16 * NF), n = e % (16 * NF);
+#pragma unroll
+    for (uint32_t i = 0; i < MF * NF; ++i) {
+        const uint32_t e = i * kBlock + tid_x(), m = e / (16 * NF), n = e % (16 * NF);
         if (m0 + m >= p.m || n0 + n >= p.n) continue;
         const uint32_t from = m % 16 / 4 * 16 + n % 16;
         float v = 0.0f;
@@ -194,30 +215,30 @@ __global__ void __launch_bounds__(kBlock) narrow_kernel(const ProductArgs p) {
     }
 }
 
-template <int MF, int NF>
+template <int MF, int NF, int U>
 void narrow(const ProductArgs &p, cnr_scale_type scale, hipStream_t s) {
     const dim3 grid((unsigned)cnr_ceil_div(p.n, 16 * NF), (unsigned)cnr_ceil_div(p.m, 16 * MF));
     const bool full = p.out_type == CNR_FLOAT_F32;
     if (scale == CNR_SCALE_E8M0) {
         if (full)
-            hipLaunchKernelGGL((narrow_kernel<CNR_SCALE_E8M0, true, MF, NF>), grid, dim3(kBlock), 0, s, p);
+            hipLaunchKernelGGL((narrow_kernel<CNR_SCALE_E8M0, true, MF, NF, U>), grid, dim3(kBlock), 0, s, p);
         else
-            hipLaunchKernelGGL((narrow_kernel<CNR_SCALE_E8M0, false, MF, NF>), grid, dim3(kBlock), 0, s, p);
+            hipLaunchKernelGGL((narrow_kernel<CNR_SCALE_E8M0, false, MF, NF, U>), grid, dim3(kBlock), 0, s, p);
     } else {
         if (full)
-            hipLaunchKernelGGL((narrow_kernel<CNR_SCALE_F32, true, MF, NF>), grid, dim3(kBlock), 0, s, p);
+            hipLaunchKernelGGL((narrow_kernel<CNR_SCALE_F32, true, MF, NF, U>), grid, dim3(kBlock), 0, s, p);
         else
-            hipLaunchKernelGGL((narrow_kernel<CNR_SCALE_F32, false, MF, NF>), grid, dim3(kBlock), 0, s, p);
+            hipLaunchKernelGGL((narrow_kernel<CNR_SCALE_F32, false, MF, NF, U>), grid, dim3(kBlock), 0, s, p);
     }
 }
 
 // ---- many rows: tiles staged in LDS -----------------------------------------------------------------------------
 //
-// A workgroup of four waves has 32 MF x 32 NF outputs, each wave 16 MF x 16 NF, and walks along k a block of 128 at a time; the next
-// block's codes travel from memory into LDS while this one's are multiplied.
+// A workgroup of four waves has 32 MF x 32 NF outputs, each wave 16 MF x 16 NF, and walks along k a block of 128 at a time; the codes
+// and scales of the next STAGES - 1 blocks travel from memory into LDS while this one's are multiplied.
 //
 // Fragment f of a wave holds rows MF * r + f of its part of A (r = lane % 16), and likewise of B: a lane's fragments are rows side by
-// side, so that it reads their scales in one load (a byte of which each matrix instruction picks), and holds
+// side, so that it finds their scales in one or two words (a byte of which each matrix instruction picks), and holds
 // NF outputs side by side, which it stores in one go.
 //
 // LDS holds two rows of 128 codes to a line of 256 bytes, its sixteen pieces of 16 bytes permuted by r: sixteen lanes that
@@ -234,13 +255,20 @@ __device__ __forceinline__ i32x4 buffer_of(const void *base, uint64_t bytes) {
     return r;
 }
 
-// 64 pieces of 16 bytes, one for each lane, from memory to `lds` and on in lane order.  Written as an instruction because the
-// compiler, which cannot tell the halves of the LDS apart, would wait for it before every read of the other half;
+// 64 pieces of 16 (or 4) bytes, one for each lane, from memory to `lds` and on in lane order.  Written as instructions because the
+// compiler, which cannot tell the stages of the LDS apart, would wait for them before every read of another;
 // wait_for_loads() below does, once a block.  (Nothing else here uses M0.)
 __device__ __forceinline__ void load_to_lds(const i32x4 &buffer, uint32_t lds, uint32_t offset, uint32_t all) {
     asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dwordx4 %1, %2, %3 offen lds" ::"s"(lds), "v"(offset), "s"(buffer), "s"(all));
 }
-__device__ __forceinline__ void wait_for_loads() { asm volatile("s_waitcnt vmcnt(0)" ::: "memory"); }
+__device__ __forceinline__ void load_words_to_lds(const i32x4 &buffer, uint32_t lds, uint32_t offset) {
+    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dword %1, %2, 0 offen lds" ::"s"(lds), "v"(offset), "s"(buffer));
+}
+template <int LEFT>  // loads that need not have arrived
+__device__ __forceinline__ void wait_for_loads() {
+    static_assert(LEFT < 64, "the counter's range");
+    asm volatile("s_waitcnt vmcnt(%0)" ::"n"(LEFT) : "memory");
+}
 __device__ __forceinline__ void barrier() {
     asm volatile("" ::: "memory");
     __builtin_amdgcn_s_barrier();
@@ -253,44 +281,56 @@ struct Scales {
     uint32_t exponent[(F + 3) / 4];
     float fraction[SCALE == CNR_SCALE_F32 ? F : 1];
 };
-// A scale's exponent goes into the matrix instruction and its fraction, from 1 to 2, multiplies the sum: neither leaves fp32's range
-// unless the result does.  (A scale below 2^-126 counts as 0.)
-__device__ __forceinline__ float fraction_of(float s) {
-    const uint32_t b = __float_as_uint(s);
-    return b & 0x7f800000u ? __uint_as_float((b & 0x807fffffu) | 0x3f800000u) : 0.0f;
-}
-__device__ __forceinline__ uint32_t exponent_of(float s) { return __float_as_uint(s) >> 23 & 255u; }
 
-// In two parts, so that the loads are waited for where they are used.  Without a branch, which would end the compiler's sight of the
-// block: a tile's one scale is taken from the aligned word (or four) that it lies in, of which rows' scales fill one and the next.
-template <int SCALE, int F>
-struct LoadedScales {
-    typedef typename std::conditional<SCALE == CNR_SCALE_E8M0, uint32_t, f32x4>::type Word;
-    static_assert(F % 4 == 0, "whole words of scales");
-    Word word[F / 4];
-    uint32_t pick;
-    bool tile;
-    __device__ __forceinline__ void load(const typename ScaleOf<SCALE>::type *p, bool of_tile) {
-        const uintptr_t at = reinterpret_cast<uintptr_t>(p);
-        const Word *from = reinterpret_cast<const Word *>(at & ~(uintptr_t)(sizeof(Word) - 1));
-#pragma unroll
-        for (int i = 0; i < F / 4; ++i) word[i] = from[of_tile ? 0 : i];
-        tile = of_tile;
-        pick = SCALE == CNR_SCALE_F32 ? (uint32_t)at / 4 % 4 : of_tile ? ((uint32_t)at & 3u) * 0x01010101u : 0x03020100u;
+// One operand's scales on their way through LDS: a word (E8M0), or four (F32), for each four rows of the tile.  Rows' scales fill
+// them; where 128 rows share one, each word is the aligned one that it lies in.
+template <int SCALE>
+struct ScaleStream {
+    static constexpr uint32_t kGroup = SCALE == CNR_SCALE_E8M0 ? 4 : 16;  // bytes
+    static constexpr uint32_t kBytes = kWave * kGroup;                    // in LDS
+    const uint8_t *base;
+    uint64_t stride;
+    uint32_t row0, step, count, group;  // step: rows to a scale; count: scales of a block; group: the lane's four rows
+    __device__ __forceinline__ ScaleStream(const void *p, uint64_t stride_, uint32_t shift, uint32_t row0_, uint32_t rows, uint32_t lane)
+        : base(reinterpret_cast<const uint8_t *>(p)), stride(stride_), row0(row0_), step(1u << shift), count((uint32_t)stride_) {
+        group = lane < rows / 4 ? lane : rows / 4 - 1;
     }
-    __device__ __forceinline__ Scales<SCALE, F> scales() const {
+    static constexpr uint32_t kSize = kGroup / 4;
+    // Index of the scale of a row (the first of four); rows beyond the matrix take the last ones that there are.
+    __device__ __forceinline__ uint32_t entry(uint32_t row) const {
+        const uint32_t at = step == 1 ? row : row / CNR_BLOCK, last = count - (step == 1 ? 4 : 1);
+        return at < last ? at : last;
+    }
+    // `wanted` false: asks for nothing, but counts as a load.
+    __device__ __forceinline__ void fetch(uint32_t kb, uint32_t lds, bool wanted) const {
+        const bool rows = step == 1;
+        // the lowest row's offset and, where blocks' scales begin at whole words, the block's go into the base, so that offsets stay small
+        const uint32_t low = rows ? entry(row0) * kSize : 0, in_row = entry(row0 + group * 4) * kSize - low;
+        const uint32_t offset = rows ? in_row : ((uint32_t)(kb * stride) * kSize + in_row) & ~(kGroup - 1);
+        const i32x4 buffer = buffer_of(base + (rows ? kb * stride * kSize + low : 0), wanted ? 0xffffffffull : 0);
+        if (SCALE == CNR_SCALE_E8M0)
+            load_words_to_lds(buffer, lds, offset);
+        else
+            load_to_lds(buffer, lds, offset, 0);
+    }
+    // The scales of rows [row, row + F) of the tile, from where fetch(kb) has put them.
+    template <int F>
+    __device__ __forceinline__ Scales<SCALE, F> read(const uint8_t *lds, uint32_t row, uint32_t kb) const {
         Scales<SCALE, F> s;
+        const uint32_t within = row % 4;  // 0, or 2 where F is 2
+        const uint32_t which = ((uint32_t)(kb * stride) + entry(row0 + row)) % 4;
 #pragma unroll
-        for (int i = 0; i < F / 4; ++i) {
+        for (int i = 0; i < (F + 3) / 4; ++i) {
+            const uint8_t *from = lds + (row / 4 + i) * kGroup;
             if constexpr (SCALE == CNR_SCALE_E8M0) {
-                s.exponent[i] = __builtin_amdgcn_perm(0u, word[i], pick);
+                s.exponent[i] = __builtin_amdgcn_perm(0u, *reinterpret_cast<const uint32_t *>(from), step == 1 ? 0x03020100u + within * 0x0101u : which * 0x01010101u);
             } else {
-                const f32x4 w = word[i];
-                const float one = pick & 2 ? (pick & 1 ? w[3] : w[2]) : (pick & 1 ? w[1] : w[0]);
+                const f32x4 w = *reinterpret_cast<const f32x4 *>(from);
+                const float one = which & 2 ? (which & 1 ? w[3] : w[2]) : (which & 1 ? w[1] : w[0]);
                 s.exponent[i] = 0;
 #pragma unroll
-                for (int j = 0; j < 4; ++j) {
-                    const float v = tile ? one : w[j];
+                for (int j = 0; j < 4 && 4 * i + j < F; ++j) {
+                    const float v = step != 1 ? one : F == 2 && within ? w[(j + 2) % 4] : w[j];
                     s.exponent[i] |= exponent_of(v) << (8 * j);
                     s.fraction[4 * i + j] = fraction_of(v);
                 }
@@ -299,6 +339,7 @@ struct LoadedScales {
         return s;
     }
 };
+
 template <int I>
 struct Index {
     static constexpr int value = I;
@@ -311,27 +352,11 @@ __device__ __forceinline__ void unrolled(const Body &body) {
     }
 }
 
-// acc += A B, written as instructions for the sake of their registers: 128 x 128 sums fill all accumulation registers of a lane
-// and the operands lie in the others, which the compiler does not find by itself (it moves sums to and fro and
-// spills).  The idle states in front are what an operand needs that an ordinary instruction has just written.  Sums are not touched in any other way between settle() before the first and settle() after the last of these.
-template <int BYTE_A, int BYTE_B>
-__device__ __forceinline__ void multiply_add(f32x4 &acc, const i32x8 &x, const i32x8 &y, uint32_t sx, uint32_t sy) {
-    asm("s_nop 1\n\tv_mfma_scale_f32_16x16x128_f8f6f4 %0, %1, %2, %0, %3, %4 op_sel:[%5,%6,0] op_sel_hi:[%7,%8,0]"
-        : "+a"(acc)
-        : "v"(x), "v"(y), "v"(sx), "v"(sy), "n"(BYTE_A % 2), "n"(BYTE_B % 2), "n"(BYTE_A / 2), "n"(BYTE_B / 2));
-}
-__device__ __forceinline__ void multiply_add(f32x4 &acc, const bf16x8 &x, const bf16x8 &y) {
-    asm("s_nop 1\n\tv_mfma_f32_16x16x32_bf16 %0, %1, %2, %0" : "+a"(acc) : "v"(x), "v"(y));
-}
-// Longer than any matrix instruction takes to write its sums, or a move to become visible to one.
-__device__ __forceinline__ void settle() { asm volatile("s_nop 15\n\ts_nop 15\n\ts_nop 15" ::: "memory"); }
-
 template <typename T, int NF>
-__device__ __forceinline__ void store_row(const ProductArgs &p, uint32_t m, uint32_t n, const float *v) {
-    T *o = reinterpret_cast<T *>(p.out) + (uint64_t)m * p.out_stride + n;
-    if (n + NF <= p.n) {
+__device__ __forceinline__ void store_row(T *o, uint32_t n, uint32_t n_end, const float *v, bool accumulate) {
+    if (n + NF <= n_end) {
         Pack<T, NF> w;
-        if (p.accumulate) {
+        if (accumulate) {
             const Pack<T, NF> old = *reinterpret_cast<const Pack<T, NF> *>(o);
 #pragma unroll
             for (int j = 0; j < NF; ++j) w.v[j] = (T)((float)old.v[j] + v[j]);
@@ -343,27 +368,32 @@ __device__ __forceinline__ void store_row(const ProductArgs &p, uint32_t m, uint
     } else {
 #pragma unroll
         for (int j = 0; j < NF; ++j)
-            if (n + j < p.n) o[j] = (T)(p.accumulate ? (float)o[j] + v[j] : v[j]);
+            if (n + j < n_end) o[j] = (T)(accumulate ? (float)o[j] + v[j] : v[j]);
     }
 }
 
-template <int SCALE, bool FULL, int MF, int NF>
+template <int SCALE, bool FULL, int MF, int NF, int STAGES>
 __global__ void __launch_bounds__(kBlock, 1) tile_kernel(const ProductArgs p) {
-    typedef typename ScaleOf<SCALE>::type S;
-    constexpr uint32_t TM = 32 * MF, TN = 32 * NF, kStage = (TM + TN) * CNR_BLOCK;
-    __shared__ __align__(256) uint8_t lds[2 * kStage];
+    constexpr uint32_t TM = 32 * MF, TN = 32 * NF;
+    typedef ScaleStream<SCALE> Stream;
+    constexpr uint32_t kB = TM * CNR_BLOCK, kScaleA = kB + TN * CNR_BLOCK, kScaleB = kScaleA + Stream::kBytes, kStage = kScaleB + Stream::kBytes;
+    constexpr int kLoads = MF + NF + 1;  // of a wave for one block
+    __shared__ __align__(256) uint8_t lds[STAGES * kStage];
     const uint32_t lane = tid_x() % kWave, wave = (uint32_t)__builtin_amdgcn_readfirstlane((int)(tid_x() / kWave));
     const uint32_t r = lane % 16, quarter = lane / 16;
     const uint32_t wave_m = wave / 2 * 16 * MF, wave_n = wave % 2 * 16 * NF;
 
     // Workgroups go to the eight XCDs in turn: each XCD gets tiles that lie together, in bands of kBand rows of tiles, for its L2.
     constexpr uint32_t kBand = 4;
-    const uint32_t tiles_m = (p.m + TM - 1) / TM, tiles_n = (p.n + TN - 1) / TN, tiles = tiles_m * tiles_n;
-    const uint32_t xcd = wg_x() % 8, each = tiles / 8, more = tiles % 8;
-    const uint32_t at = xcd * each + (xcd < more ? xcd : more) + wg_x() / 8;
+    const uint32_t tiles_m = (p.m + TM - 1) / TM, tiles_n = (p.n + TN - 1) / TN, tiles = tiles_m * tiles_n, all = tiles * p.splits;
+    const uint32_t xcd = wg_x() % 8, each = all / 8, more = all % 8;
+    const uint32_t id = xcd * each + (xcd < more ? xcd : more) + wg_x() / 8;
+    const uint32_t split = id / tiles, at = id % tiles;
     const uint32_t band = at / (kBand * tiles_n), band_rows = tiles_m - band * kBand < kBand ? tiles_m - band * kBand : kBand;
     const uint32_t in_band = at - band * kBand * tiles_n;
     const uint32_t m0 = (band * kBand + in_band % band_rows) * TM, n0 = in_band / band_rows * TN;
+    // Blocks of this part of the sum.
+    const uint32_t begin = (uint32_t)((uint64_t)p.blocks * split / p.splits), end = (uint32_t)((uint64_t)p.blocks * (split + 1) / p.splits);
 
     // Rows beyond the matrix read its last one again.
     const uint32_t rows_a = p.m - m0 < TM ? p.m - m0 : TM, rows_b = p.n - n0 < TN ? p.n - n0 : TN;
@@ -382,21 +412,26 @@ __global__ void __launch_bounds__(kBlock, 1) tile_kernel(const ProductArgs p) {
         const uint32_t row = 2 * line + logical / 8;
         from_b[j] = (row < rows_b ? row : rows_b - 1) * (uint32_t)p.row_bytes + logical % 8 * 16;
     }
+    const Stream stream_a(p.a_scale, p.a_stride, p.a_shift, m0, TM, lane), stream_b(p.b_scale, p.b_stride, p.b_shift, n0, TN, lane);
+    // Two waves bring the scales of A, two those of B, so that all have as many loads under way.
+    const bool brings_a = wave % 2 == 0;
+    const Stream mine(brings_a ? p.a_scale : p.b_scale, brings_a ? p.a_stride : p.b_stride, brings_a ? p.a_shift : p.b_shift, brings_a ? m0 : n0,
+                      brings_a ? TM : TN, lane);
     const uint32_t lds_at = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) uint8_t *)lds;
+    // Block kb of this part of the sum into a stage; beyond its end buffers of no size are asked, so that the count of loads stays
+    // the same without a branch, which would end the compiler's sight of the loop.
     auto fetch = [&](uint32_t kb, uint32_t stage) {
+        const uint32_t to = lds_at + stage * kStage;
+        const bool wanted = kb < end;
+        i32x4 a = buffer_a, b = buffer_b;
+        a[2] = wanted ? a[2] : 0;
+        b[2] = wanted ? b[2] : 0;
 #pragma unroll
-        for (int j = 0; j < MF; ++j) load_to_lds(buffer_a, lds_at + stage * kStage + (wave * MF + j) * 1024, from_a[j], kb * CNR_BLOCK);
+        for (int j = 0; j < MF; ++j) load_to_lds(a, to + (wave * MF + j) * 1024, from_a[j], kb * CNR_BLOCK);
 #pragma unroll
-        for (int j = 0; j < NF; ++j) load_to_lds(buffer_b, lds_at + stage * kStage + TM * CNR_BLOCK + (wave * NF + j) * 1024, from_b[j], kb * CNR_BLOCK);
+        for (int j = 0; j < NF; ++j) load_to_lds(b, to + kB + (wave * NF + j) * 1024, from_b[j], kb * CNR_BLOCK);
+        mine.fetch(kb, to + (brings_a ? kScaleA : kScaleB), wanted);
     };
-    // Row of each kind's scales that a lane starts at; rows beyond the matrix take ones that are there.
-    const bool tile_a = p.a_shift != 0, tile_b = p.b_shift != 0;
-    auto scale_row = [&](uint32_t row, uint64_t stride, bool tile, uint32_t per) {
-        const uint64_t at = tile ? row / CNR_BLOCK : row, last = stride - (tile ? 1 : per);
-        return at < last ? at : last;
-    };
-    const S *scale_a = reinterpret_cast<const S *>(p.a_scale) + scale_row(m0 + wave_m + r * MF, p.a_stride, tile_a, MF);
-    const S *scale_b = reinterpret_cast<const S *>(p.b_scale) + scale_row(n0 + wave_n + r * NF, p.b_stride, tile_b, NF);
 
     f32x4 acc[MF][NF];
 #pragma unroll
@@ -409,30 +444,26 @@ __global__ void __launch_bounds__(kBlock, 1) tile_kernel(const ProductArgs p) {
     uint32_t piece_a[2], piece_b[2];
 #pragma unroll
     for (int h = 0; h < 2; ++h) {
-        piece_a[h] = (wave_m + r * MF) * CNR_BLOCK + ((2 * quarter + h) ^ r) * 16;
-        piece_b[h] = TM * CNR_BLOCK + (wave_n + r * NF) * CNR_BLOCK + ((2 * quarter + h) ^ r) * 16;
+        piece_a[h] = (wave_m + r * MF) * CNR_BLOCK + ((quarter + 4 * h) ^ r) * 16;
+        piece_b[h] = kB + (wave_n + r * NF) * CNR_BLOCK + ((quarter + 4 * h) ^ r) * 16;
     }
-    auto fragment = [&](const uint32_t (&piece)[2], uint32_t f) {
+    auto fragment = [&](const uint8_t *base, const uint32_t (&piece)[2], uint32_t f) {
         i32x4 part[2];
 #pragma unroll
-        for (int h = 0; h < 2; ++h) part[h] = *reinterpret_cast<const i32x4 *>(lds + (piece[h] ^ (f % 2 * 128)) + f / 2 * 256);
+        for (int h = 0; h < 2; ++h) part[h] = *reinterpret_cast<const i32x4 *>(base + (piece[h] ^ (f % 2 * 128)) + f / 2 * 256);
         return __builtin_shufflevector(part[0], part[1], 0, 1, 2, 3, 4, 5, 6, 7);
     };
-    fetch(0, 0);
-    LoadedScales<SCALE, MF> next_a;
-    LoadedScales<SCALE, NF> next_b;
-    next_a.load(scale_a, tile_a);
-    next_b.load(scale_b, tile_b);
-    wait_for_loads();
+
+#pragma unroll
+    for (int i = 0; i < STAGES - 1; ++i) fetch(begin + i, i);
+    wait_for_loads<(STAGES - 2) * kLoads>();
     barrier();
-    Scales<SCALE, MF> sa = next_a.scales();
-    Scales<SCALE, NF> sb = next_b.scales();
-    settle();
-    for (uint32_t kb = 0; kb < p.blocks; ++kb) {
-        const uint32_t next = kb + 1 < p.blocks ? kb + 1 : kb;  // at the end once more what nobody reads
-        fetch(next, (kb + 1) % 2);
-        next_a.load(scale_a + (uint64_t)next * p.a_stride, tile_a);
-        next_b.load(scale_b + (uint64_t)next * p.b_stride, tile_b);
+    uint32_t stage = 0;
+    for (uint32_t kb = begin; kb < end; ++kb) {
+        fetch(kb + STAGES - 1, stage ? stage - 1 : STAGES - 1);
+        const uint8_t *base = lds + stage * kStage;
+        const Scales<SCALE, MF> sa = stream_a.template read<MF>(base + kScaleA, wave_m + r * MF, kb);
+        const Scales<SCALE, NF> sb = stream_b.template read<NF>(base + kScaleB, wave_n + r * NF, kb);
         float rows[SCALE == CNR_SCALE_F32 ? MF : 1][4];  // fractions of the rows of the lane's sums
         if (SCALE == CNR_SCALE_F32) {
 #pragma unroll
@@ -444,27 +475,27 @@ __global__ void __launch_bounds__(kBlock, 1) tile_kernel(const ProductArgs p) {
 #pragma unroll
         for (int f = 0; f < MF; ++f) {
             if constexpr (FULL)
-                x[f] = widen(fragment(piece_a, f), sa.exponent[f / 4] >> (8 * (f % 4)) & 255u);
+                x[f] = widen(fragment(base, piece_a, f), sa.exponent[f / 4] >> (8 * (f % 4)) & 255u);
             else
-                x[f] = fragment(piece_a, f);
+                x[f] = fragment(base, piece_a, f);
         }
-        i32x8 ahead = fragment(piece_b, 0);
+        i32x8 ahead = fragment(base, piece_b, 0);
         unrolled<NF>([&](auto g) {
             constexpr int G = decltype(g)::value;
             const i32x8 y = ahead;
-            if constexpr (G + 1 < NF) ahead = fragment(piece_b, G + 1);
+            if constexpr (G + 1 < NF) ahead = fragment(base, piece_b, G + 1);
             Wide wy;
             if constexpr (FULL) wy = widen(y, sb.exponent[G / 4] >> (8 * (G % 4)) & 255u);
             if constexpr (SCALE == CNR_SCALE_E8M0 && FULL) {
 #pragma unroll
                 for (int i = 0; i < 4; ++i)
 #pragma unroll
-                    for (int f = 0; f < MF; ++f) multiply_add(acc[f][G], x[f].part[i], wy.part[i]);
+                    for (int f = 0; f < MF; ++f) acc[f][G] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(x[f].part[i], wy.part[i], acc[f][G], 0, 0, 0);
             } else {
                 unrolled<MF>([&](auto f) {
                     constexpr int F = decltype(f)::value;
                     if constexpr (SCALE == CNR_SCALE_E8M0) {
-                        multiply_add<F % 4, G % 4>(acc[F][G], x[F], y, sa.exponent[F / 4], sb.exponent[G / 4]);
+                        acc[F][G] = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(x[F], y, acc[F][G], 0, 0, F % 4, (int)sa.exponent[F / 4], G % 4, (int)sb.exponent[G / 4]);
                     } else {
                         f32x4 d = {0.0f, 0.0f, 0.0f, 0.0f};
                         if constexpr (FULL) {
@@ -480,51 +511,70 @@ __global__ void __launch_bounds__(kBlock, 1) tile_kernel(const ProductArgs p) {
             }
             __builtin_amdgcn_sched_barrier(0);
         });
-#pragma unroll
-        for (int h = 0; h < 2; ++h) {
-            const uint32_t other = kb % 2 ? 0u - kStage : kStage;
-            piece_a[h] += other;
-            piece_b[h] += other;
-        }
-        wait_for_loads();
+        stage = stage + 1 < STAGES ? stage + 1 : 0;
+        wait_for_loads<(STAGES - 2) * kLoads>();
         barrier();
-        sa = next_a.scales();
-        sb = next_b.scales();
     }
-    settle();
+    wait_for_loads<0>();
 
+    const uint32_t n = n0 + wave_n + r * NF;
 #pragma unroll
     for (int f = 0; f < MF; ++f)
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
-            const uint32_t m = m0 + wave_m + (quarter * 4 + i) * MF + f, n = n0 + wave_n + r * NF;
+            const uint32_t m = m0 + wave_m + (quarter * 4 + i) * MF + f;
             if (m >= p.m || n >= p.n) continue;
             float v[NF];
 #pragma unroll
             for (int g = 0; g < NF; ++g) v[g] = acc[f][g][i];
-            if (FULL)
-                store_row<float, NF>(p, m, n, v);
+            if (p.splits > 1)
+                store_row<float, NF>(p.partial + ((uint64_t)split * p.m + m) * p.partial_stride + n, n, p.n, v, false);
+            else if (FULL)
+                store_row<float, NF>(reinterpret_cast<float *>(p.out) + m * p.out_stride + n, n, p.n, v, p.accumulate);
             else if (p.out_type == CNR_FLOAT_BF16)
-                store_row<__bf16, NF>(p, m, n, v);
+                store_row<__bf16, NF>(reinterpret_cast<__bf16 *>(p.out) + m * p.out_stride + n, n, p.n, v, p.accumulate);
             else
-                store_row<_Float16, NF>(p, m, n, v);
+                store_row<_Float16, NF>(reinterpret_cast<_Float16 *>(p.out) + m * p.out_stride + n, n, p.n, v, p.accumulate);
         }
 }
 
-template <int MF, int NF>
+// The parts of sums that were split, added up in order: four outputs of a row to a thread.
+template <typename T>
+__global__ void __launch_bounds__(kBlock) join_kernel(const ProductArgs p) {
+    const uint32_t across = (uint32_t)(p.partial_stride / 4);
+    const uint64_t at = (uint64_t)wg_x() * kBlock + tid_x();
+    if (at >= (uint64_t)p.m * across) return;
+    const uint32_t m = (uint32_t)(at / across), n = (uint32_t)(at % across) * 4;
+    const float *from = p.partial + (uint64_t)m * p.partial_stride + n;
+    f32x4 sum = *reinterpret_cast<const f32x4 *>(from);
+    for (uint32_t s = 1; s < p.splits; ++s) sum += *reinterpret_cast<const f32x4 *>(from + (uint64_t)s * p.m * p.partial_stride);
+    const float v[4] = {sum[0], sum[1], sum[2], sum[3]};
+    store_row<T, 4>(reinterpret_cast<T *>(p.out) + m * p.out_stride + n, n, p.n, v, p.accumulate);
+}
+
+template <int MF, int NF, int STAGES>
 void tiled(const ProductArgs &p, cnr_scale_type scale, hipStream_t s) {
-    const dim3 grid((unsigned)(cnr_ceil_div(p.m, 32 * MF) * cnr_ceil_div(p.n, 32 * NF)));
+    const dim3 grid((unsigned)(cnr_ceil_div(p.m, 32 * MF) * cnr_ceil_div(p.n, 32 * NF) * p.splits));
     const bool full = p.out_type == CNR_FLOAT_F32;
-    if constexpr (MF * NF > 32) {
+    if (scale == CNR_SCALE_E8M0) {
         if (full)
-            hipLaunchKernelGGL((tile_kernel<CNR_SCALE_E8M0, true, MF, NF>), grid, dim3(kBlock), 0, s, p);
+            hipLaunchKernelGGL((tile_kernel<CNR_SCALE_E8M0, true, MF, NF, STAGES>), grid, dim3(kBlock), 0, s, p);
         else
-            hipLaunchKernelGGL((tile_kernel<CNR_SCALE_E8M0, false, MF, NF>), grid, dim3(kBlock), 0, s, p);
-    } else {
+            hipLaunchKernelGGL((tile_kernel<CNR_SCALE_E8M0, false, MF, NF, STAGES>), grid, dim3(kBlock), 0, s, p);
+    } else if constexpr (MF * NF <= 32) {
         if (full)
-            hipLaunchKernelGGL((tile_kernel<CNR_SCALE_F32, true, MF, NF>), grid, dim3(kBlock), 0, s, p);
+            hipLaunchKernelGGL((tile_kernel<CNR_SCALE_F32, true, MF, NF, STAGES>), grid, dim3(kBlock), 0, s, p);
         else
-            hipLaunchKernelGGL((tile_kernel<CNR_SCALE_F32, false, MF, NF>), grid, dim3(kBlock), 0, s, p);
+            hipLaunchKernelGGL((tile_kernel<CNR_SCALE_F32, false, MF, NF, STAGES>), grid, dim3(kBlock), 0, s, p);
+    }
+    if (p.splits > 1) {
+        const dim3 join((unsigned)cnr_ceil_div((uint64_t)p.m * (p.partial_stride / 4), kBlock));
+        if (full)
+            hipLaunchKernelGGL((join_kernel<float>), join, dim3(kBlock), 0, s, p);
+        else if (p.out_type == CNR_FLOAT_BF16)
+            hipLaunchKernelGGL((join_kernel<__bf16>), join, dim3(kBlock), 0, s, p);
+        else
+            hipLaunchKernelGGL((join_kernel<_Float16>), join, dim3(kBlock), 0, s, p);
     }
 }
 
@@ -568,11 +618,14 @@ cnr_status cnr_block_product(cnr_ctx *ctx, const uint8_t *a_codes, const void *a
     p.out_stride = out_stride;
     p.out_type = out_type;
     p.accumulate = accumulate ? 1 : 0;
+    p.splits = 1;
+    p.partial = reinterpret_cast<float *>(workspace);
+    p.partial_stride = cnr_ceil_div(n, 4) * 4;
     // A tile's offsets are 32 bits: 256 rows of less than 2^24 codes.
     if (m > 64 && p.row_bytes < 1u << 24)
-        scale_type == CNR_SCALE_E8M0 ? tiled<8, 8>(p, scale_type, as_stream(stream)) : tiled<4, 8>(p, scale_type, as_stream(stream));
+        scale_type == CNR_SCALE_E8M0 ? tiled<8, 8, 2>(p, scale_type, as_stream(stream)) : tiled<4, 4, 2>(p, scale_type, as_stream(stream));
     else
-        narrow<1, 1>(p, scale_type, as_stream(stream));
+        narrow<1, 1, 2>(p, scale_type, as_stream(stream));
     return cnr_launch_status(ctx);
 }
 

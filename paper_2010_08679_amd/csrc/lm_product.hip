@@ -257,9 +257,14 @@ __device__ __forceinline__ i32x4 buffer_of(const void *base, uint64_t bytes) {
 
 // 64 pieces of 16 (or 4) bytes, one for each lane, from memory to `lds` and on in lane order.  Written as instructions because the
 // compiler, which cannot tell the stages of the LDS apart, would wait for them before every read of another;
-// wait_for_loads() below does, once a block.  (Nothing else here uses M0.)
+// wait_for_loads() below does, once a block.  (Nothing else here uses M0, which holds the place in LDS.)  The instruction's own offset
+// OFFSET counts for both addresses, so that four loads in a row need one M0; the buffer and `offset` make up for it.
+template <int OFFSET>
 __device__ __forceinline__ void load_to_lds(const i32x4 &buffer, uint32_t lds, uint32_t offset, uint32_t all) {
-    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dwordx4 %1, %2, %3 offen lds" ::"s"(lds), "v"(offset), "s"(buffer), "s"(all));
+    if constexpr (OFFSET == 0)
+        asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dwordx4 %1, %2, %3 offen lds" ::"s"(lds), "v"(offset), "s"(buffer), "s"(all));
+    else
+        asm volatile("buffer_load_dwordx4 %0, %1, %2 offen offset:%3 lds" ::"v"(offset), "s"(buffer), "s"(all), "n"(OFFSET));
 }
 __device__ __forceinline__ void load_words_to_lds(const i32x4 &buffer, uint32_t lds, uint32_t offset) {
     asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dword %1, %2, 0 offen lds" ::"s"(lds), "v"(offset), "s"(buffer));
@@ -286,51 +291,63 @@ struct Scales {
 // them; where 128 rows share one, each word is the aligned one that it lies in.
 template <int SCALE>
 struct ScaleStream {
-    static constexpr uint32_t kGroup = SCALE == CNR_SCALE_E8M0 ? 4 : 16;  // bytes
-    static constexpr uint32_t kBytes = kWave * kGroup;                    // in LDS
-    const uint8_t *base;
-    uint64_t stride;
-    uint32_t row0, step, count, group;  // step: rows to a scale; count: scales of a block; group: the lane's four rows
-    __device__ __forceinline__ ScaleStream(const void *p, uint64_t stride_, uint32_t shift, uint32_t row0_, uint32_t rows, uint32_t lane)
-        : base(reinterpret_cast<const uint8_t *>(p)), stride(stride_), row0(row0_), step(1u << shift), count((uint32_t)stride_) {
-        group = lane < rows / 4 ? lane : rows / 4 - 1;
-    }
-    static constexpr uint32_t kSize = kGroup / 4;
-    // Index of the scale of a row (the first of four); rows beyond the matrix take the last ones that there are.
-    __device__ __forceinline__ uint32_t entry(uint32_t row) const {
-        const uint32_t at = step == 1 ? row : row / CNR_BLOCK, last = count - (step == 1 ? 4 : 1);
-        return at < last ? at : last;
+    static constexpr uint32_t kSize = SCALE == CNR_SCALE_E8M0 ? 1 : 4;  // bytes of a scale
+    static constexpr uint32_t kGroup = 4 * kSize, kBytes = kWave * kGroup;  // of four, and of all in LDS
+    bool rows;       // a scale for each row
+    uint64_t base;   // address of the block to fetch next
+    uint64_t step;   // bytes from a block to the next
+    uint32_t block;  // the same within an array of tiles' scales, whose words are not aligned with its blocks
+    uint32_t block_step, in_block;
+    // `row0`: first row of the tile; four rows to a lane, as far as `n` of them go; rows beyond the matrix take the last scales that there are.
+    __device__ __forceinline__ ScaleStream(const void *p, uint64_t stride, uint32_t shift, uint32_t row0, uint32_t n, uint32_t lane, uint32_t kb) {
+        rows = shift == 0;
+        const uint32_t row = row0 + 4 * (lane < n / 4 ? lane : n / 4 - 1);
+        const uint32_t last = (uint32_t)stride - (rows ? 4 : 1), entry = rows ? row : row / CNR_BLOCK;
+        const uint32_t low = rows ? row0 : 0;  // goes into the base, so that offsets stay small
+        in_block = ((entry < last ? entry : last) - low) * kSize;
+        base = reinterpret_cast<uint64_t>(p) + (rows ? ((uint64_t)kb * stride + low) * kSize : 0);
+        step = rows ? stride * kSize : 0;
+        block = rows ? 0 : (uint32_t)(kb * stride) * kSize;
+        block_step = rows ? 0 : (uint32_t)stride * kSize;
     }
     // `wanted` false: asks for nothing, but counts as a load.
-    __device__ __forceinline__ void fetch(uint32_t kb, uint32_t lds, bool wanted) const {
-        const bool rows = step == 1;
-        // the lowest row's offset and, where blocks' scales begin at whole words, the block's go into the base, so that offsets stay small
-        const uint32_t low = rows ? entry(row0) * kSize : 0, in_row = entry(row0 + group * 4) * kSize - low;
-        const uint32_t offset = rows ? in_row : ((uint32_t)(kb * stride) * kSize + in_row) & ~(kGroup - 1);
-        const i32x4 buffer = buffer_of(base + (rows ? kb * stride * kSize + low : 0), wanted ? 0xffffffffull : 0);
-        if (SCALE == CNR_SCALE_E8M0)
+    __device__ __forceinline__ void fetch_next(uint32_t lds, bool wanted) {
+        const i32x4 buffer = buffer_of(reinterpret_cast<const void *>(base), wanted ? 0xffffffffull : 0);
+        const uint32_t offset = (block + in_block) & ~(kGroup - 1);
+        if constexpr (SCALE == CNR_SCALE_E8M0)
             load_words_to_lds(buffer, lds, offset);
         else
-            load_to_lds(buffer, lds, offset, 0);
+            load_to_lds<0>(buffer, lds, offset, 0);
+        base += step;
+        block += block_step;
     }
-    // The scales of rows [row, row + F) of the tile, from where fetch(kb) has put them.
-    template <int F>
-    __device__ __forceinline__ Scales<SCALE, F> read(const uint8_t *lds, uint32_t row, uint32_t kb) const {
+};
+// The scales of rows [row, row + F) of the tile, in two parts: the words from where they were put, and what they say.  `pick`: which of
+// its word's four is the tile's (the wave's rows lie within one); 4: rows have their own.
+template <int SCALE, int F>
+struct ScaleWords {
+    typedef typename std::conditional<SCALE == CNR_SCALE_E8M0, uint32_t, f32x4>::type Word;
+    Word word[(F + 3) / 4];
+    uint32_t within;  // first row of the word's four: 0, or 2 where F is 2
+    __device__ __forceinline__ ScaleWords(const uint8_t *lds, uint32_t row) : within(row % 4) {
+#pragma unroll
+        for (int i = 0; i < (F + 3) / 4; ++i) word[i] = *reinterpret_cast<const Word *>(lds + (row / 4 + i) * sizeof(Word));
+    }
+    __device__ __forceinline__ Scales<SCALE, F> scales(uint32_t pick) const {
         Scales<SCALE, F> s;
-        const uint32_t within = row % 4;  // 0, or 2 where F is 2
-        const uint32_t which = ((uint32_t)(kb * stride) + entry(row0 + row)) % 4;
 #pragma unroll
         for (int i = 0; i < (F + 3) / 4; ++i) {
-            const uint8_t *from = lds + (row / 4 + i) * kGroup;
             if constexpr (SCALE == CNR_SCALE_E8M0) {
-                s.exponent[i] = __builtin_amdgcn_perm(0u, *reinterpret_cast<const uint32_t *>(from), step == 1 ? 0x03020100u + within * 0x0101u : which * 0x01010101u);
+                const uint32_t own = 0u - pick / 4;
+                const uint32_t order = (pick * 0x01010101u & ~own) | (0x03020100u + (F == 2 ? within * 0x0101u : 0u) & own);
+                s.exponent[i] = __builtin_amdgcn_perm(0u, word[i], order);
             } else {
-                const f32x4 w = *reinterpret_cast<const f32x4 *>(from);
-                const float one = which & 2 ? (which & 1 ? w[3] : w[2]) : (which & 1 ? w[1] : w[0]);
+                const f32x4 w = word[i];
+                const float one = pick & 2 ? (pick & 1 ? w[3] : w[2]) : (pick & 1 ? w[1] : w[0]);
                 s.exponent[i] = 0;
 #pragma unroll
                 for (int j = 0; j < 4 && 4 * i + j < F; ++j) {
-                    const float v = step != 1 ? one : F == 2 && within ? w[(j + 2) % 4] : w[j];
+                    const float v = pick != 4 ? one : F == 2 && within ? w[(j + 2) % 4] : w[j];
                     s.exponent[i] |= exponent_of(v) << (8 * j);
                     s.fraction[4 * i + j] = fraction_of(v);
                 }
@@ -396,42 +413,55 @@ __global__ void __launch_bounds__(kBlock, 1) tile_kernel(const ProductArgs p) {
     const uint32_t begin = (uint32_t)((uint64_t)p.blocks * split / p.splits), end = (uint32_t)((uint64_t)p.blocks * (split + 1) / p.splits);
 
     // Rows beyond the matrix read its last one again.
+    constexpr uint32_t kBack = 4096;  // room for the instructions' offsets
     const uint32_t rows_a = p.m - m0 < TM ? p.m - m0 : TM, rows_b = p.n - n0 < TN ? p.n - n0 : TN;
-    const i32x4 buffer_a = buffer_of(p.a + (uint64_t)m0 * p.row_bytes, (uint64_t)rows_a * p.row_bytes);
-    const i32x4 buffer_b = buffer_of(p.b + (uint64_t)n0 * p.row_bytes, (uint64_t)rows_b * p.row_bytes);
+    const i32x4 buffer_a = buffer_of(p.a + (uint64_t)m0 * p.row_bytes - kBack, (uint64_t)rows_a * p.row_bytes + kBack);
+    const i32x4 buffer_b = buffer_of(p.b + (uint64_t)n0 * p.row_bytes - kBack, (uint64_t)rows_b * p.row_bytes + kBack);
     uint32_t from_a[MF], from_b[NF];
 #pragma unroll
     for (int j = 0; j < MF; ++j) {
         const uint32_t line = (wave * MF + j) * 4 + quarter, logical = (lane % 16) ^ (2 * line / MF % 16);
         const uint32_t row = 2 * line + logical / 8;
-        from_a[j] = (row < rows_a ? row : rows_a - 1) * (uint32_t)p.row_bytes + logical % 8 * 16;
+        from_a[j] = (row < rows_a ? row : rows_a - 1) * (uint32_t)p.row_bytes + logical % 8 * 16 + kBack - j % 4 * 1024;
     }
 #pragma unroll
     for (int j = 0; j < NF; ++j) {
         const uint32_t line = (wave * NF + j) * 4 + quarter, logical = (lane % 16) ^ (2 * line / NF % 16);
         const uint32_t row = 2 * line + logical / 8;
-        from_b[j] = (row < rows_b ? row : rows_b - 1) * (uint32_t)p.row_bytes + logical % 8 * 16;
+        from_b[j] = (row < rows_b ? row : rows_b - 1) * (uint32_t)p.row_bytes + logical % 8 * 16 + kBack - j % 4 * 1024;
     }
-    const Stream stream_a(p.a_scale, p.a_stride, p.a_shift, m0, TM, lane), stream_b(p.b_scale, p.b_stride, p.b_shift, n0, TN, lane);
     // Two waves bring the scales of A, two those of B, so that all have as many loads under way.
     const bool brings_a = wave % 2 == 0;
-    const Stream mine(brings_a ? p.a_scale : p.b_scale, brings_a ? p.a_stride : p.b_stride, brings_a ? p.a_shift : p.b_shift, brings_a ? m0 : n0,
-                      brings_a ? TM : TN, lane);
+    ScaleStream<SCALE> stream(brings_a ? p.a_scale : p.b_scale, brings_a ? p.a_stride : p.b_stride, brings_a ? p.a_shift : p.b_shift,
+                              brings_a ? m0 : n0, brings_a ? TM : TN, lane, begin);
     const uint32_t lds_at = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) uint8_t *)lds;
-    // Block kb of this part of the sum into a stage; beyond its end buffers of no size are asked, so that the count of loads stays
-    // the same without a branch, which would end the compiler's sight of the loop.
-    auto fetch = [&](uint32_t kb, uint32_t stage) {
+    // Load j of the wave's kLoads for block kb of this part of the sum into a stage; beyond its end buffers of no size are asked, which
+    // brings nothing: the count of loads stays the same without a branch, which would end the compiler's sight of the loop.
+    auto fetch = [&](uint32_t kb, uint32_t stage, auto index) {
+        constexpr int J = decltype(index)::value;
         const uint32_t to = lds_at + stage * kStage;
         const bool wanted = kb < end;
-        i32x4 a = buffer_a, b = buffer_b;
-        a[2] = wanted ? a[2] : 0;
-        b[2] = wanted ? b[2] : 0;
-#pragma unroll
-        for (int j = 0; j < MF; ++j) load_to_lds(a, to + (wave * MF + j) * 1024, from_a[j], kb * CNR_BLOCK);
-#pragma unroll
-        for (int j = 0; j < NF; ++j) load_to_lds(b, to + kB + (wave * NF + j) * 1024, from_b[j], kb * CNR_BLOCK);
-        mine.fetch(kb, to + (brings_a ? kScaleA : kScaleB), wanted);
+        if constexpr (J < MF) {
+            i32x4 a = buffer_a;
+            a[2] = wanted ? a[2] : 0;
+            load_to_lds<J % 4 * 1024>(a, to + (wave * MF + J) * 1024, from_a[J], kb * CNR_BLOCK);
+        } else if constexpr (J < MF + NF) {
+            i32x4 b = buffer_b;
+            b[2] = wanted ? b[2] : 0;
+            load_to_lds<(J - MF) % 4 * 1024>(b, to + kB + (wave * NF + J - MF) * 1024, from_b[J - MF], kb * CNR_BLOCK);
+        } else {
+            stream.fetch_next(to + (brings_a ? kScaleA : kScaleB), wanted);
+        }
     };
+    // Which of its word's four a tile's scale is in block kb (see read_scales), 4 where rows have their own; without a branch.
+    auto pick_of = [&](uint32_t kb, uint32_t shift, uint64_t stride, uint32_t row) {
+        const uint32_t at = row >> 7, last = (uint32_t)stride - 1, own = shift / 7 - 1;  // all bits set where rows have their own
+        return (((kb * (uint32_t)stride + (at < last ? at : last)) % 4) & ~own) | (4u & own);
+    };
+    auto pick_a = [&](uint32_t kb) { return pick_of(kb, p.a_shift, p.a_stride, m0 + wave_m); };
+    auto pick_b = [&](uint32_t kb) { return pick_of(kb, p.b_shift, p.b_stride, n0 + wave_n); };
+    auto words_a = [&](uint32_t stage) { return ScaleWords<SCALE, MF>(lds + stage * kStage + kScaleA, wave_m + r * MF); };
+    auto words_b = [&](uint32_t stage) { return ScaleWords<SCALE, NF>(lds + stage * kStage + kScaleB, wave_n + r * NF); };
 
     f32x4 acc[MF][NF];
 #pragma unroll
@@ -454,66 +484,131 @@ __global__ void __launch_bounds__(kBlock, 1) tile_kernel(const ProductArgs p) {
         return __builtin_shufflevector(part[0], part[1], 0, 1, 2, 3, 4, 5, 6, 7);
     };
 
+    // The i-th of `of` even shares of N things to do.
+    auto share = [](auto i, auto of, auto n, const auto &act) {
+        constexpr int I = decltype(i)::value, OF = decltype(of)::value, N = decltype(n)::value, from = I * N / OF, to = (I + 1) * N / OF;
+        unrolled<to - from>([&](auto j) { act(Index<from + decltype(j)::value>()); });
+    };
+    if constexpr (SCALE == CNR_SCALE_E8M0 && !FULL) {
+        // A block's products go by quarters, each half of the wave's rows of A with each half of those of B, so that half of the
+        // operands are in registers while the other half, or the next block's first, are on their way from LDS; a wave alone on its SIMD can
+        // issue about four other instructions for each matrix instruction without holding it up, so loads go between
+        // them.  The last quarter needs nothing more from this stage: before it all waves meet, in it the stage is filled
+        // again.
+        constexpr int HM = MF / 2, HN = NF / 2, kQuarter = HM * HN;
+        unrolled<STAGES>([&](auto i) { unrolled<kLoads>([&](auto j) { fetch(begin + decltype(i)::value, decltype(i)::value, j); }); });
+        wait_for_loads<(STAGES - 1) * kLoads>();
+        barrier();
+        Scales<SCALE, MF> sa = words_a(0).scales(pick_a(begin));
+        Scales<SCALE, NF> sb = words_b(0).scales(pick_b(begin));
+        i32x8 x[2][HM], y[2][HN];
 #pragma unroll
-    for (int i = 0; i < STAGES - 1; ++i) fetch(begin + i, i);
-    wait_for_loads<(STAGES - 2) * kLoads>();
-    barrier();
-    uint32_t stage = 0;
-    for (uint32_t kb = begin; kb < end; ++kb) {
-        fetch(kb + STAGES - 1, stage ? stage - 1 : STAGES - 1);
-        const uint8_t *base = lds + stage * kStage;
-        const Scales<SCALE, MF> sa = stream_a.template read<MF>(base + kScaleA, wave_m + r * MF, kb);
-        const Scales<SCALE, NF> sb = stream_b.template read<NF>(base + kScaleB, wave_n + r * NF, kb);
-        float rows[SCALE == CNR_SCALE_F32 ? MF : 1][4];  // fractions of the rows of the lane's sums
-        if (SCALE == CNR_SCALE_F32) {
+        for (int f = 0; f < HM; ++f) x[0][f] = fragment(lds, piece_a, f);
 #pragma unroll
-            for (int f = 0; f < MF; ++f)
-#pragma unroll
-                for (int i = 0; i < 4; ++i) rows[f][i] = __shfl(sa.fraction[f], (int)(quarter * 4 + i));
-        }
-        typename std::conditional<FULL, Wide, i32x8>::type x[MF];
-#pragma unroll
-        for (int f = 0; f < MF; ++f) {
-            if constexpr (FULL)
-                x[f] = widen(fragment(base, piece_a, f), sa.exponent[f / 4] >> (8 * (f % 4)) & 255u);
-            else
-                x[f] = fragment(base, piece_a, f);
-        }
-        i32x8 ahead = fragment(base, piece_b, 0);
-        unrolled<NF>([&](auto g) {
-            constexpr int G = decltype(g)::value;
-            const i32x8 y = ahead;
-            if constexpr (G + 1 < NF) ahead = fragment(base, piece_b, G + 1);
-            Wide wy;
-            if constexpr (FULL) wy = widen(y, sb.exponent[G / 4] >> (8 * (G % 4)) & 255u);
-            if constexpr (SCALE == CNR_SCALE_E8M0 && FULL) {
-#pragma unroll
-                for (int i = 0; i < 4; ++i)
-#pragma unroll
-                    for (int f = 0; f < MF; ++f) acc[f][G] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(x[f].part[i], wy.part[i], acc[f][G], 0, 0, 0);
-            } else {
-                unrolled<MF>([&](auto f) {
-                    constexpr int F = decltype(f)::value;
-                    if constexpr (SCALE == CNR_SCALE_E8M0) {
-                        acc[F][G] = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(x[F], y, acc[F][G], 0, 0, F % 4, (int)sa.exponent[F / 4], G % 4, (int)sb.exponent[G / 4]);
-                    } else {
-                        f32x4 d = {0.0f, 0.0f, 0.0f, 0.0f};
-                        if constexpr (FULL) {
-#pragma unroll
-                            for (int i = 0; i < 4; ++i) d = __builtin_amdgcn_mfma_f32_16x16x32_bf16(x[F].part[i], wy.part[i], d, 0, 0, 0);
-                        } else {
-                            d = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(x[F], y, d, 0, 0, F % 4, (int)sa.exponent[F / 4], G % 4, (int)sb.exponent[G / 4]);
-                        }
-#pragma unroll
-                        for (int i = 0; i < 4; ++i) acc[F][G][i] = __builtin_fmaf(d[i], rows[F][i] * sb.fraction[G], acc[F][G][i]);
-                    }
+        for (int g = 0; g < HN; ++g) y[0][g] = fragment(lds, piece_b, g);
+        // One quarter; with its i-th product goes beside(i).
+        auto quarter_of = [&](auto half_a, auto half_b, const auto &beside) {
+            constexpr int A = decltype(half_a)::value, B = decltype(half_b)::value;
+            unrolled<kQuarter>([&](auto at) {
+                constexpr int F = decltype(at)::value % HM, G = decltype(at)::value / HM, MA = A * HM + F, NB = B * HN + G;
+                acc[MA][NB] = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(x[A][F], y[B][G], acc[MA][NB], 0, 0, MA % 4, (int)sa.exponent[MA / 4],
+                                                                               NB % 4, (int)sb.exponent[NB / 4]);
+                beside(at);
+                __builtin_amdgcn_sched_barrier(0);
+            });
+        };
+        uint32_t stage = 0;
+        for (uint32_t kb = begin; kb < end; ++kb) {
+            const uint32_t next = stage + 1 < STAGES ? stage + 1 : 0;
+            const uint8_t *base = lds + stage * kStage, *next_base = lds + next * kStage;
+            quarter_of(Index<0>(), Index<0>(), [&](auto at) {
+                share(at, Index<kQuarter>(), Index<HN>(), [&](auto g) { y[1][decltype(g)::value] = fragment(base, piece_b, HN + decltype(g)::value); });
+            });
+            quarter_of(Index<0>(), Index<1>(), [&](auto at) {
+                share(at, Index<kQuarter>(), Index<HM>(), [&](auto f) { x[1][decltype(f)::value] = fragment(base, piece_a, HM + decltype(f)::value); });
+            });
+            quarter_of(Index<1>(), Index<0>(), [&](auto) {});
+            wait_for_loads<(STAGES - 2) * kLoads>();
+            barrier();
+            const ScaleWords<SCALE, MF> next_a = words_a(next);
+            const ScaleWords<SCALE, NF> next_b = words_b(next);
+            quarter_of(Index<1>(), Index<1>(), [&](auto at) {
+                share(at, Index<kQuarter>(), Index<HM + HN>(), [&](auto j) {
+                    constexpr int J = decltype(j)::value;
+                    if constexpr (J < HM)
+                        x[0][J] = fragment(next_base, piece_a, J);
+                    else
+                        y[0][J - HM] = fragment(next_base, piece_b, J - HM);
                 });
-            }
-            __builtin_amdgcn_sched_barrier(0);
-        });
-        stage = stage + 1 < STAGES ? stage + 1 : 0;
+                share(at, Index<kQuarter>(), Index<kLoads>(), [&](auto j) { fetch(kb + STAGES, stage, j); });
+            });
+            sa = next_a.scales(pick_a(kb + 1));
+            sb = next_b.scales(pick_b(kb + 1));
+            stage = next;
+        }
+    } else {
+        // Operands that are converted, or sums that are scaled, keep the ordinary units busy next to the matrix units: a plain order, all of
+        // A's fragments, then B's one ahead.
+        unrolled<STAGES - 1>([&](auto i) { unrolled<kLoads>([&](auto j) { fetch(begin + decltype(i)::value, decltype(i)::value, j); }); });
         wait_for_loads<(STAGES - 2) * kLoads>();
         barrier();
+        uint32_t stage = 0;
+        for (uint32_t kb = begin; kb < end; ++kb) {
+            unrolled<kLoads>([&](auto j) { fetch(kb + STAGES - 1, stage ? stage - 1 : STAGES - 1, j); });
+            const uint8_t *base = lds + stage * kStage;
+            const Scales<SCALE, MF> sa = words_a(stage).scales(pick_a(kb));
+            const Scales<SCALE, NF> sb = words_b(stage).scales(pick_b(kb));
+            float rows[SCALE == CNR_SCALE_F32 ? MF : 1][4];  // fractions of the rows of the lane's sums
+            if constexpr (SCALE == CNR_SCALE_F32) {
+#pragma unroll
+                for (int f = 0; f < MF; ++f)
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) rows[f][i] = __shfl(sa.fraction[f], (int)(quarter * 4 + i));
+            }
+            typename std::conditional<FULL, Wide, i32x8>::type x[MF];
+#pragma unroll
+            for (int f = 0; f < MF; ++f) {
+                if constexpr (FULL)
+                    x[f] = widen(fragment(base, piece_a, f), sa.exponent[f / 4] >> (8 * (f % 4)) & 255u);
+                else
+                    x[f] = fragment(base, piece_a, f);
+            }
+            i32x8 ahead = fragment(base, piece_b, 0);
+            unrolled<NF>([&](auto g) {
+                constexpr int G = decltype(g)::value;
+                const i32x8 y = ahead;
+                if constexpr (G + 1 < NF) ahead = fragment(base, piece_b, G + 1);
+                Wide wy;
+                if constexpr (FULL) wy = widen(y, sb.exponent[G / 4] >> (8 * (G % 4)) & 255u);
+                f32x4 d[MF];
+#pragma unroll
+                for (int f = 0; f < MF; ++f) d[f] = SCALE == CNR_SCALE_F32 ? f32x4{0.0f, 0.0f, 0.0f, 0.0f} : acc[f][G];
+                if constexpr (FULL) {
+#pragma unroll
+                    for (int i = 0; i < 4; ++i)
+#pragma unroll
+                        for (int f = 0; f < MF; ++f) d[f] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(x[f].part[i], wy.part[i], d[f], 0, 0, 0);
+                } else {
+                    unrolled<MF>([&](auto f) {
+                        constexpr int F = decltype(f)::value;
+                        d[F] = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(x[F], y, d[F], 0, 0, F % 4, (int)sa.exponent[F / 4], G % 4, (int)sb.exponent[G / 4]);
+                    });
+                }
+#pragma unroll
+                for (int f = 0; f < MF; ++f) {
+                    if constexpr (SCALE == CNR_SCALE_F32) {
+#pragma unroll
+                        for (int i = 0; i < 4; ++i) acc[f][G][i] = __builtin_fmaf(d[f][i], rows[f][i] * sb.fraction[G], acc[f][G][i]);
+                    } else {
+                        acc[f][G] = d[f];
+                    }
+                }
+                __builtin_amdgcn_sched_barrier(0);
+            });
+            stage = stage + 1 < STAGES ? stage + 1 : 0;
+            wait_for_loads<(STAGES - 2) * kLoads>();
+            barrier();
+        }
     }
     wait_for_loads<0>();
 

@@ -389,16 +389,18 @@ __device__ __forceinline__ void store_row(T *o, uint32_t n, uint32_t n_end, cons
     }
 }
 
-template <int SCALE, bool FULL, int MF, int NF, int STAGES>
-__global__ void __launch_bounds__(kBlock, 1) tile_kernel(const ProductArgs p) {
-    constexpr uint32_t TM = 32 * MF, TN = 32 * NF;
+template <int SCALE, bool FULL, int WM, int WN, int MF, int NF, int STAGES>
+__global__ void __launch_bounds__(WM * WN * kWave, 2) tile_kernel(const ProductArgs p) {
+    constexpr uint32_t TM = WM * 16 * MF, TN = WN * 16 * NF;
+    constexpr int LA = 2 * MF / WN, LB = 2 * NF / WM;  // loads of 1 KB that each wave sends for a block of A and of B
+    static_assert(LA * WN == 2 * MF && LB * WM == 2 * NF, "whole loads");
     typedef ScaleStream<SCALE> Stream;
     constexpr uint32_t kB = TM * CNR_BLOCK, kScaleA = kB + TN * CNR_BLOCK, kScaleB = kScaleA + Stream::kBytes, kStage = kScaleB + Stream::kBytes;
-    constexpr int kLoads = MF + NF + 1;  // of a wave for one block
+    constexpr int kLoads = LA + LB + 1;
     __shared__ __align__(256) uint8_t lds[STAGES * kStage];
     const uint32_t lane = tid_x() % kWave, wave = (uint32_t)__builtin_amdgcn_readfirstlane((int)(tid_x() / kWave));
     const uint32_t r = lane % 16, quarter = lane / 16;
-    const uint32_t wave_m = wave / 2 * 16 * MF, wave_n = wave % 2 * 16 * NF;
+    const uint32_t wave_m = wave / WN * 16 * MF, wave_n = wave % WN * 16 * NF;
 
     // Workgroups go to the eight XCDs in turn: each XCD gets tiles that lie together, in bands of kBand rows of tiles, for its L2.
     constexpr uint32_t kBand = 4;
@@ -417,20 +419,20 @@ __global__ void __launch_bounds__(kBlock, 1) tile_kernel(const ProductArgs p) {
     const uint32_t rows_a = p.m - m0 < TM ? p.m - m0 : TM, rows_b = p.n - n0 < TN ? p.n - n0 : TN;
     const i32x4 buffer_a = buffer_of(p.a + (uint64_t)m0 * p.row_bytes - kBack, (uint64_t)rows_a * p.row_bytes + kBack);
     const i32x4 buffer_b = buffer_of(p.b + (uint64_t)n0 * p.row_bytes - kBack, (uint64_t)rows_b * p.row_bytes + kBack);
-    uint32_t from_a[MF], from_b[NF];
+    uint32_t from_a[LA], from_b[LB];
 #pragma unroll
-    for (int j = 0; j < MF; ++j) {
-        const uint32_t line = (wave * MF + j) * 4 + quarter, logical = (lane % 16) ^ (2 * line / MF % 16);
+    for (int j = 0; j < LA; ++j) {
+        const uint32_t line = (wave * LA + j) * 4 + quarter, logical = (lane % 16) ^ (2 * line / MF % 16);
         const uint32_t row = 2 * line + logical / 8;
         from_a[j] = (row < rows_a ? row : rows_a - 1) * (uint32_t)p.row_bytes + logical % 8 * 16 + kBack - j % 4 * 1024;
     }
 #pragma unroll
-    for (int j = 0; j < NF; ++j) {
-        const uint32_t line = (wave * NF + j) * 4 + quarter, logical = (lane % 16) ^ (2 * line / NF % 16);
+    for (int j = 0; j < LB; ++j) {
+        const uint32_t line = (wave * LB + j) * 4 + quarter, logical = (lane % 16) ^ (2 * line / NF % 16);
         const uint32_t row = 2 * line + logical / 8;
         from_b[j] = (row < rows_b ? row : rows_b - 1) * (uint32_t)p.row_bytes + logical % 8 * 16 + kBack - j % 4 * 1024;
     }
-    // Two waves bring the scales of A, two those of B, so that all have as many loads under way.
+    // Half of the waves bring the scales of A, half those of B: the same ones, so that all have as many loads under way.
     const bool brings_a = wave % 2 == 0;
     ScaleStream<SCALE> stream(brings_a ? p.a_scale : p.b_scale, brings_a ? p.a_stride : p.b_stride, brings_a ? p.a_shift : p.b_shift,
                               brings_a ? m0 : n0, brings_a ? TM : TN, lane, begin);
@@ -441,14 +443,14 @@ __global__ void __launch_bounds__(kBlock, 1) tile_kernel(const ProductArgs p) {
         constexpr int J = decltype(index)::value;
         const uint32_t to = lds_at + stage * kStage;
         const bool wanted = kb < end;
-        if constexpr (J < MF) {
+        if constexpr (J < LA) {
             i32x4 a = buffer_a;
             a[2] = wanted ? a[2] : 0;
-            load_to_lds<J % 4 * 1024>(a, to + (wave * MF + J) * 1024, from_a[J], kb * CNR_BLOCK);
-        } else if constexpr (J < MF + NF) {
+            load_to_lds<J % 4 * 1024>(a, to + (wave * LA + J) * 1024, from_a[J], kb * CNR_BLOCK);
+        } else if constexpr (J < LA + LB) {
             i32x4 b = buffer_b;
             b[2] = wanted ? b[2] : 0;
-            load_to_lds<(J - MF) % 4 * 1024>(b, to + kB + (wave * NF + J - MF) * 1024, from_b[J - MF], kb * CNR_BLOCK);
+            load_to_lds<(J - LA) % 4 * 1024>(b, to + kB + (wave * LB + J - LA) * 1024, from_b[J - LA], kb * CNR_BLOCK);
         } else {
             stream.fetch_next(to + (brings_a ? kScaleA : kScaleB), wanted);
         }
@@ -647,24 +649,13 @@ __global__ void __launch_bounds__(kBlock) join_kernel(const ProductArgs p) {
     store_row<T, 4>(reinterpret_cast<T *>(p.out) + m * p.out_stride + n, n, p.n, v, p.accumulate);
 }
 
-template <int MF, int NF, int STAGES>
-void tiled(const ProductArgs &p, cnr_scale_type scale, hipStream_t s) {
-    const dim3 grid((unsigned)(cnr_ceil_div(p.m, 32 * MF) * cnr_ceil_div(p.n, 32 * NF) * p.splits));
-    const bool full = p.out_type == CNR_FLOAT_F32;
-    if (scale == CNR_SCALE_E8M0) {
-        if (full)
-            hipLaunchKernelGGL((tile_kernel<CNR_SCALE_E8M0, true, MF, NF, STAGES>), grid, dim3(kBlock), 0, s, p);
-        else
-            hipLaunchKernelGGL((tile_kernel<CNR_SCALE_E8M0, false, MF, NF, STAGES>), grid, dim3(kBlock), 0, s, p);
-    } else if constexpr (MF * NF <= 32) {
-        if (full)
-            hipLaunchKernelGGL((tile_kernel<CNR_SCALE_F32, true, MF, NF, STAGES>), grid, dim3(kBlock), 0, s, p);
-        else
-            hipLaunchKernelGGL((tile_kernel<CNR_SCALE_F32, false, MF, NF, STAGES>), grid, dim3(kBlock), 0, s, p);
-    }
+template <bool FULL, int SCALE, int WM, int WN, int MF, int NF, int STAGES>
+void tiled(const ProductArgs &p, hipStream_t s) {
+    const dim3 grid((unsigned)(cnr_ceil_div(p.m, 16 * WM * MF) * cnr_ceil_div(p.n, 16 * WN * NF) * p.splits));
+    hipLaunchKernelGGL((tile_kernel<SCALE, FULL, WM, WN, MF, NF, STAGES>), grid, dim3(WM * WN * kWave), 0, s, p);
     if (p.splits > 1) {
         const dim3 join((unsigned)cnr_ceil_div((uint64_t)p.m * (p.partial_stride / 4), kBlock));
-        if (full)
+        if (FULL)
             hipLaunchKernelGGL((join_kernel<float>), join, dim3(kBlock), 0, s, p);
         else if (p.out_type == CNR_FLOAT_BF16)
             hipLaunchKernelGGL((join_kernel<__bf16>), join, dim3(kBlock), 0, s, p);
@@ -717,10 +708,15 @@ cnr_status cnr_block_product(cnr_ctx *ctx, const uint8_t *a_codes, const void *a
     p.partial = reinterpret_cast<float *>(workspace);
     p.partial_stride = cnr_ceil_div(n, 4) * 4;
     // A tile's offsets are 32 bits: 256 rows of less than 2^24 codes.
-    if (m > 64 && p.row_bytes < 1u << 24)
-        scale_type == CNR_SCALE_E8M0 ? tiled<8, 8, 2>(p, scale_type, as_stream(stream)) : tiled<4, 4, 2>(p, scale_type, as_stream(stream));
-    else
-        narrow<1, 1, 2>(p, scale_type, as_stream(stream));
+    hipStream_t to = as_stream(stream);
+    if (m > 64 && p.row_bytes < 1u << 24) {
+        if (out_type == CNR_FLOAT_F32)
+            scale_type == CNR_SCALE_E8M0 ? tiled<true, CNR_SCALE_E8M0, 2, 4, 4, 4, 2>(p, to) : tiled<true, CNR_SCALE_F32, 2, 4, 4, 4, 2>(p, to);
+        else
+            scale_type == CNR_SCALE_E8M0 ? tiled<false, CNR_SCALE_E8M0, 2, 4, 8, 4, 2>(p, to) : tiled<false, CNR_SCALE_F32, 2, 4, 4, 4, 2>(p, to);
+    } else {
+        narrow<1, 1, 2>(p, scale_type, to);
+    }
     return cnr_launch_status(ctx);
 }
 

@@ -245,12 +245,12 @@ void narrow(const ProductArgs &p, cnr_scale_type scale, hipStream_t s) {
 // read the same piece of their rows find it in sixteen different places, all banks in use.  Memory is read straight
 // into LDS, where a wave's 64 pieces lie in order, so the permutation is in which piece a lane asks for.
 
-__device__ __forceinline__ i32x4 buffer_of(const void *base, uint64_t bytes) {
-    const uint64_t p = reinterpret_cast<uint64_t>(base);
+// Base and size are the same for all lanes.
+__device__ __forceinline__ i32x4 buffer_of(uint64_t base, uint64_t bytes) {
     i32x4 r;
-    r[0] = __builtin_amdgcn_readfirstlane((int)(uint32_t)p);
-    r[1] = __builtin_amdgcn_readfirstlane((int)((uint32_t)(p >> 32) & 0xffffu));
-    r[2] = __builtin_amdgcn_readfirstlane((int)(uint32_t)(bytes < 0xffffffffull ? bytes : 0xffffffffull));
+    r[0] = (int)(uint32_t)base;
+    r[1] = (int)((uint32_t)(base >> 32) & 0xffffu);
+    r[2] = (int)(uint32_t)(bytes < 0xffffffffull ? bytes : 0xffffffffull);
     r[3] = 0x00027000;
     return r;
 }
@@ -293,14 +293,12 @@ template <int SCALE>
 struct ScaleStream {
     static constexpr uint32_t kSize = SCALE == CNR_SCALE_E8M0 ? 1 : 4;  // bytes of a scale
     static constexpr uint32_t kGroup = 4 * kSize, kBytes = kWave * kGroup;  // of four, and of all in LDS
-    bool rows;       // a scale for each row
-    uint64_t base;   // address of the block to fetch next
-    uint64_t step;   // bytes from a block to the next
-    uint32_t block;  // the same within an array of tiles' scales, whose words are not aligned with its blocks
-    uint32_t block_step, in_block;
+    uint64_t base, step;          // address of the block to fetch next, bytes to the one after it
+    uint32_t block, block_step;   // the same within an array of tiles' scales, whose words are not aligned with its blocks
+    uint32_t in_block;
     // `row0`: first row of the tile; four rows to a lane, as far as `n` of them go; rows beyond the matrix take the last scales that there are.
     __device__ __forceinline__ ScaleStream(const void *p, uint64_t stride, uint32_t shift, uint32_t row0, uint32_t n, uint32_t lane, uint32_t kb) {
-        rows = shift == 0;
+        const bool rows = shift == 0;  // a scale for each row
         const uint32_t row = row0 + 4 * (lane < n / 4 ? lane : n / 4 - 1);
         const uint32_t last = (uint32_t)stride - (rows ? 4 : 1), entry = rows ? row : row / CNR_BLOCK;
         const uint32_t low = rows ? row0 : 0;  // goes into the base, so that offsets stay small
@@ -310,16 +308,16 @@ struct ScaleStream {
         block = rows ? 0 : (uint32_t)(kb * stride) * kSize;
         block_step = rows ? 0 : (uint32_t)stride * kSize;
     }
-    // `wanted` false: asks for nothing, but counts as a load.
-    __device__ __forceinline__ void fetch_next(uint32_t lds, bool wanted) {
-        const i32x4 buffer = buffer_of(reinterpret_cast<const void *>(base), wanted ? 0xffffffffull : 0);
+    // `on`: the block is not the last one; there the stream stays.
+    __device__ __forceinline__ void fetch(uint32_t lds, bool on) {
+        const i32x4 buffer = buffer_of(base, 0xffffffffull);
         const uint32_t offset = (block + in_block) & ~(kGroup - 1);
         if constexpr (SCALE == CNR_SCALE_E8M0)
             load_words_to_lds(buffer, lds, offset);
         else
             load_to_lds<0>(buffer, lds, offset, 0);
-        base += step;
-        block += block_step;
+        base += on ? step : 0;
+        block += on ? block_step : 0;
     }
 };
 // The scales of rows [row, row + F) of the tile, in two parts: the words from where they were put, and what they say.  `pick`: which of
@@ -417,8 +415,8 @@ __global__ void __launch_bounds__(WM * WN * kWave, 2) tile_kernel(const ProductA
     // Rows beyond the matrix read its last one again.
     constexpr uint32_t kBack = 4096;  // room for the instructions' offsets
     const uint32_t rows_a = p.m - m0 < TM ? p.m - m0 : TM, rows_b = p.n - n0 < TN ? p.n - n0 : TN;
-    const i32x4 buffer_a = buffer_of(p.a + (uint64_t)m0 * p.row_bytes - kBack, (uint64_t)rows_a * p.row_bytes + kBack);
-    const i32x4 buffer_b = buffer_of(p.b + (uint64_t)n0 * p.row_bytes - kBack, (uint64_t)rows_b * p.row_bytes + kBack);
+    const i32x4 buffer_a = buffer_of(reinterpret_cast<uint64_t>(p.a) + (uint64_t)m0 * p.row_bytes - kBack, (uint64_t)rows_a * p.row_bytes + kBack);
+    const i32x4 buffer_b = buffer_of(reinterpret_cast<uint64_t>(p.b) + (uint64_t)n0 * p.row_bytes - kBack, (uint64_t)rows_b * p.row_bytes + kBack);
     uint32_t from_a[LA], from_b[LB];
 #pragma unroll
     for (int j = 0; j < LA; ++j) {
@@ -437,33 +435,33 @@ __global__ void __launch_bounds__(WM * WN * kWave, 2) tile_kernel(const ProductA
     ScaleStream<SCALE> stream(brings_a ? p.a_scale : p.b_scale, brings_a ? p.a_stride : p.b_stride, brings_a ? p.a_shift : p.b_shift,
                               brings_a ? m0 : n0, brings_a ? TM : TN, lane, begin);
     const uint32_t lds_at = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) uint8_t *)lds;
-    // Load j of the wave's kLoads for block kb of this part of the sum into a stage; beyond its end buffers of no size are asked, which
-    // brings nothing: the count of loads stays the same without a branch, which would end the compiler's sight of the loop.
-    auto fetch = [&](uint32_t kb, uint32_t stage, auto index) {
+    // Load j of the wave's kLoads for block kb of this part of the sum into the stage at `to`; beyond its end the last block once more, which
+    // nobody reads: the count of loads stays the same without a branch, which would end the compiler's sight of the loop.
+    auto fetch = [&](uint32_t kb, uint32_t to, auto index) {
         constexpr int J = decltype(index)::value;
-        const uint32_t to = lds_at + stage * kStage;
-        const bool wanted = kb < end;
-        if constexpr (J < LA) {
-            i32x4 a = buffer_a;
-            a[2] = wanted ? a[2] : 0;
-            load_to_lds<J % 4 * 1024>(a, to + (wave * LA + J) * 1024, from_a[J], kb * CNR_BLOCK);
-        } else if constexpr (J < LA + LB) {
-            i32x4 b = buffer_b;
-            b[2] = wanted ? b[2] : 0;
-            load_to_lds<(J - LA) % 4 * 1024>(b, to + kB + (wave * LB + J - LA) * 1024, from_b[J - LA], kb * CNR_BLOCK);
-        } else {
-            stream.fetch_next(to + (brings_a ? kScaleA : kScaleB), wanted);
+        const uint32_t at = (kb < end - 1 ? kb : end - 1) * CNR_BLOCK;
+        if constexpr (J < LA)
+            load_to_lds<J % 4 * 1024>(buffer_a, lds_at + to + (wave * LA + J) * 1024, from_a[J], at);
+        else if constexpr (J < LA + LB)
+            load_to_lds<(J - LA) % 4 * 1024>(buffer_b, lds_at + to + kB + (wave * LB + J - LA) * 1024, from_b[J - LA], at);
+        else
+            stream.fetch(lds_at + to + (brings_a ? kScaleA : kScaleB), kb < end - 1);
+    };
+    // Which of its word's four a tile's scale is, block by block (see ScaleWords), or 4 where rows have their own.
+    struct Pick {
+        uint32_t now, step, own;
+        __device__ __forceinline__ Pick(uint32_t kb, uint32_t shift, uint64_t stride, uint32_t row) {
+            const uint32_t at = row >> 7, last = (uint32_t)stride - 1;
+            own = shift ? 0 : 4;
+            step = shift ? (uint32_t)stride : 0;
+            now = shift ? kb * step + (at < last ? at : last) : 0;
         }
+        __device__ __forceinline__ uint32_t operator()() const { return (now & 3) | own; }
+        __device__ __forceinline__ void advance() { now += step; }
     };
-    // Which of its word's four a tile's scale is in block kb (see read_scales), 4 where rows have their own; without a branch.
-    auto pick_of = [&](uint32_t kb, uint32_t shift, uint64_t stride, uint32_t row) {
-        const uint32_t at = row >> 7, last = (uint32_t)stride - 1, own = shift / 7 - 1;  // all bits set where rows have their own
-        return (((kb * (uint32_t)stride + (at < last ? at : last)) % 4) & ~own) | (4u & own);
-    };
-    auto pick_a = [&](uint32_t kb) { return pick_of(kb, p.a_shift, p.a_stride, m0 + wave_m); };
-    auto pick_b = [&](uint32_t kb) { return pick_of(kb, p.b_shift, p.b_stride, n0 + wave_n); };
-    auto words_a = [&](uint32_t stage) { return ScaleWords<SCALE, MF>(lds + stage * kStage + kScaleA, wave_m + r * MF); };
-    auto words_b = [&](uint32_t stage) { return ScaleWords<SCALE, NF>(lds + stage * kStage + kScaleB, wave_n + r * NF); };
+    Pick pick_a(begin, p.a_shift, p.a_stride, m0 + wave_m), pick_b(begin, p.b_shift, p.b_stride, n0 + wave_n);
+    auto words_a = [&](uint32_t at) { return ScaleWords<SCALE, MF>(lds + at + kScaleA, wave_m + r * MF); };
+    auto words_b = [&](uint32_t at) { return ScaleWords<SCALE, NF>(lds + at + kScaleB, wave_n + r * NF); };
 
     f32x4 acc[MF][NF];
 #pragma unroll
@@ -472,17 +470,25 @@ __global__ void __launch_bounds__(WM * WN * kWave, 2) tile_kernel(const ProductA
         for (int g = 0; g < NF; ++g) acc[f][g] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
 
     // Where a lane's row of fragment f lies: lines of 256 bytes for each pair of fragments, in them the piece h at one of two places that
-    // depend on the lane alone, in the other half of the line for an odd f.
-    uint32_t piece_a[2], piece_b[2];
+    // depend on the lane alone, in the other half of the line for an odd f.  These addresses move from stage to stage.
+    uint32_t piece_a[2][2], piece_b[2][2];  // [odd][h]
 #pragma unroll
-    for (int h = 0; h < 2; ++h) {
-        piece_a[h] = (wave_m + r * MF) * CNR_BLOCK + ((quarter + 4 * h) ^ r) * 16;
-        piece_b[h] = kB + (wave_n + r * NF) * CNR_BLOCK + ((quarter + 4 * h) ^ r) * 16;
+    for (int i = 0; i < 4; ++i) {
+        const uint32_t at = ((quarter + 4 * (i % 2)) ^ r) * 16 ^ i / 2 * 128;
+        piece_a[i / 2][i % 2] = (wave_m + r * MF) * CNR_BLOCK + at;
+        piece_b[i / 2][i % 2] = kB + (wave_n + r * NF) * CNR_BLOCK + at;
     }
-    auto fragment = [&](const uint8_t *base, const uint32_t (&piece)[2], uint32_t f) {
+    auto move_pieces = [&](uint32_t by) {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            piece_a[i / 2][i % 2] += by;
+            piece_b[i / 2][i % 2] += by;
+        }
+    };
+    auto fragment = [&](const uint32_t (&piece)[2][2], uint32_t f) {
         i32x4 part[2];
 #pragma unroll
-        for (int h = 0; h < 2; ++h) part[h] = *reinterpret_cast<const i32x4 *>(base + (piece[h] ^ (f % 2 * 128)) + f / 2 * 256);
+        for (int h = 0; h < 2; ++h) part[h] = *reinterpret_cast<const i32x4 *>(lds + piece[f % 2][h] + f / 2 * 256);
         return __builtin_shufflevector(part[0], part[1], 0, 1, 2, 3, 4, 5, 6, 7);
     };
 
@@ -498,16 +504,16 @@ __global__ void __launch_bounds__(WM * WN * kWave, 2) tile_kernel(const ProductA
         // them.  The last quarter needs nothing more from this stage: before it all waves meet, in it the stage is filled
         // again.
         constexpr int HM = MF / 2, HN = NF / 2, kQuarter = HM * HN;
-        unrolled<STAGES>([&](auto i) { unrolled<kLoads>([&](auto j) { fetch(begin + decltype(i)::value, decltype(i)::value, j); }); });
+        unrolled<STAGES>([&](auto i) { unrolled<kLoads>([&](auto j) { fetch(begin + decltype(i)::value, decltype(i)::value * kStage, j); }); });
         wait_for_loads<(STAGES - 1) * kLoads>();
         barrier();
-        Scales<SCALE, MF> sa = words_a(0).scales(pick_a(begin));
-        Scales<SCALE, NF> sb = words_b(0).scales(pick_b(begin));
+        Scales<SCALE, MF> sa = words_a(0).scales(pick_a());
+        Scales<SCALE, NF> sb = words_b(0).scales(pick_b());
         i32x8 x[2][HM], y[2][HN];
 #pragma unroll
-        for (int f = 0; f < HM; ++f) x[0][f] = fragment(lds, piece_a, f);
+        for (int f = 0; f < HM; ++f) x[0][f] = fragment(piece_a, f);
 #pragma unroll
-        for (int g = 0; g < HN; ++g) y[0][g] = fragment(lds, piece_b, g);
+        for (int g = 0; g < HN; ++g) y[0][g] = fragment(piece_b, g);
         // One quarter; with its i-th product goes beside(i).
         auto quarter_of = [&](auto half_a, auto half_b, const auto &beside) {
             constexpr int A = decltype(half_a)::value, B = decltype(half_b)::value;
@@ -519,47 +525,48 @@ __global__ void __launch_bounds__(WM * WN * kWave, 2) tile_kernel(const ProductA
                 __builtin_amdgcn_sched_barrier(0);
             });
         };
-        uint32_t stage = 0;
+        uint32_t stage = 0;  // where it begins in LDS
         for (uint32_t kb = begin; kb < end; ++kb) {
-            const uint32_t next = stage + 1 < STAGES ? stage + 1 : 0;
-            const uint8_t *base = lds + stage * kStage, *next_base = lds + next * kStage;
+            const uint32_t next = stage + kStage < STAGES * kStage ? stage + kStage : 0;
             quarter_of(Index<0>(), Index<0>(), [&](auto at) {
-                share(at, Index<kQuarter>(), Index<HN>(), [&](auto g) { y[1][decltype(g)::value] = fragment(base, piece_b, HN + decltype(g)::value); });
+                share(at, Index<kQuarter>(), Index<HN>(), [&](auto g) { y[1][decltype(g)::value] = fragment(piece_b, HN + decltype(g)::value); });
             });
             quarter_of(Index<0>(), Index<1>(), [&](auto at) {
-                share(at, Index<kQuarter>(), Index<HM>(), [&](auto f) { x[1][decltype(f)::value] = fragment(base, piece_a, HM + decltype(f)::value); });
+                share(at, Index<kQuarter>(), Index<HM>(), [&](auto f) { x[1][decltype(f)::value] = fragment(piece_a, HM + decltype(f)::value); });
             });
             quarter_of(Index<1>(), Index<0>(), [&](auto) {});
             wait_for_loads<(STAGES - 2) * kLoads>();
             barrier();
+            move_pieces(next - stage);
             const ScaleWords<SCALE, MF> next_a = words_a(next);
             const ScaleWords<SCALE, NF> next_b = words_b(next);
             quarter_of(Index<1>(), Index<1>(), [&](auto at) {
                 share(at, Index<kQuarter>(), Index<HM + HN>(), [&](auto j) {
                     constexpr int J = decltype(j)::value;
                     if constexpr (J < HM)
-                        x[0][J] = fragment(next_base, piece_a, J);
+                        x[0][J] = fragment(piece_a, J);
                     else
-                        y[0][J - HM] = fragment(next_base, piece_b, J - HM);
+                        y[0][J - HM] = fragment(piece_b, J - HM);
                 });
                 share(at, Index<kQuarter>(), Index<kLoads>(), [&](auto j) { fetch(kb + STAGES, stage, j); });
             });
-            sa = next_a.scales(pick_a(kb + 1));
-            sb = next_b.scales(pick_b(kb + 1));
+            pick_a.advance();
+            pick_b.advance();
+            sa = next_a.scales(pick_a());
+            sb = next_b.scales(pick_b());
             stage = next;
         }
     } else {
         // Operands that are converted, or sums that are scaled, keep the ordinary units busy next to the matrix units: a plain order, all of
         // A's fragments, then B's one ahead.
-        unrolled<STAGES - 1>([&](auto i) { unrolled<kLoads>([&](auto j) { fetch(begin + decltype(i)::value, decltype(i)::value, j); }); });
+        unrolled<STAGES - 1>([&](auto i) { unrolled<kLoads>([&](auto j) { fetch(begin + decltype(i)::value, decltype(i)::value * kStage, j); }); });
         wait_for_loads<(STAGES - 2) * kLoads>();
         barrier();
         uint32_t stage = 0;
         for (uint32_t kb = begin; kb < end; ++kb) {
-            unrolled<kLoads>([&](auto j) { fetch(kb + STAGES - 1, stage ? stage - 1 : STAGES - 1, j); });
-            const uint8_t *base = lds + stage * kStage;
-            const Scales<SCALE, MF> sa = words_a(stage).scales(pick_a(kb));
-            const Scales<SCALE, NF> sb = words_b(stage).scales(pick_b(kb));
+            unrolled<kLoads>([&](auto j) { fetch(kb + STAGES - 1, stage ? stage - kStage : (STAGES - 1) * kStage, j); });
+            const Scales<SCALE, MF> sa = words_a(stage).scales(pick_a());
+            const Scales<SCALE, NF> sb = words_b(stage).scales(pick_b());
             float rows[SCALE == CNR_SCALE_F32 ? MF : 1][4];  // fractions of the rows of the lane's sums
             if constexpr (SCALE == CNR_SCALE_F32) {
 #pragma unroll
@@ -571,15 +578,15 @@ __global__ void __launch_bounds__(WM * WN * kWave, 2) tile_kernel(const ProductA
 #pragma unroll
             for (int f = 0; f < MF; ++f) {
                 if constexpr (FULL)
-                    x[f] = widen(fragment(base, piece_a, f), sa.exponent[f / 4] >> (8 * (f % 4)) & 255u);
+                    x[f] = widen(fragment(piece_a, f), sa.exponent[f / 4] >> (8 * (f % 4)) & 255u);
                 else
-                    x[f] = fragment(base, piece_a, f);
+                    x[f] = fragment(piece_a, f);
             }
-            i32x8 ahead = fragment(base, piece_b, 0);
+            i32x8 ahead = fragment(piece_b, 0);
             unrolled<NF>([&](auto g) {
                 constexpr int G = decltype(g)::value;
                 const i32x8 y = ahead;
-                if constexpr (G + 1 < NF) ahead = fragment(base, piece_b, G + 1);
+                if constexpr (G + 1 < NF) ahead = fragment(piece_b, G + 1);
                 Wide wy;
                 if constexpr (FULL) wy = widen(y, sb.exponent[G / 4] >> (8 * (G % 4)) & 255u);
                 f32x4 d[MF];
@@ -607,32 +614,49 @@ __global__ void __launch_bounds__(WM * WN * kWave, 2) tile_kernel(const ProductA
                 }
                 __builtin_amdgcn_sched_barrier(0);
             });
-            stage = stage + 1 < STAGES ? stage + 1 : 0;
+            const uint32_t next = stage + kStage < STAGES * kStage ? stage + kStage : 0;
+            move_pieces(next - stage);
+            stage = next;
+            pick_a.advance();
+            pick_b.advance();
             wait_for_loads<(STAGES - 2) * kLoads>();
             barrier();
         }
     }
     wait_for_loads<0>();
 
-    const uint32_t n = n0 + wave_n + r * NF;
+    const uint32_t m = m0 + wave_m + quarter * 4 * MF, n = n0 + wave_n + r * NF;
+    auto write = [&](auto *out, uint64_t stride, bool accumulate) {
+        typedef typename std::remove_pointer<decltype(out)>::type T;
+        T *o = out + (uint64_t)m * stride + n;
+        if (m0 + wave_m + 16 * MF <= p.m && n0 + wave_n + 16 * NF <= p.n && !accumulate) {
 #pragma unroll
-    for (int f = 0; f < MF; ++f)
+            for (int i = 0; i < 4 * MF; ++i) {
+                Pack<T, NF> w;
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            const uint32_t m = m0 + wave_m + (quarter * 4 + i) * MF + f;
-            if (m >= p.m || n >= p.n) continue;
-            float v[NF];
+                for (int g = 0; g < NF; ++g) w.v[g] = (T)acc[i % MF][g][i / MF];
+                *reinterpret_cast<Pack<T, NF> *>(o) = w;
+                o += stride;
+            }
+        } else {
 #pragma unroll
-            for (int g = 0; g < NF; ++g) v[g] = acc[f][g][i];
-            if (p.splits > 1)
-                store_row<float, NF>(p.partial + ((uint64_t)split * p.m + m) * p.partial_stride + n, n, p.n, v, false);
-            else if (FULL)
-                store_row<float, NF>(reinterpret_cast<float *>(p.out) + m * p.out_stride + n, n, p.n, v, p.accumulate);
-            else if (p.out_type == CNR_FLOAT_BF16)
-                store_row<__bf16, NF>(reinterpret_cast<__bf16 *>(p.out) + m * p.out_stride + n, n, p.n, v, p.accumulate);
-            else
-                store_row<_Float16, NF>(reinterpret_cast<_Float16 *>(p.out) + m * p.out_stride + n, n, p.n, v, p.accumulate);
+            for (int i = 0; i < 4 * MF; ++i) {
+                float v[NF];
+#pragma unroll
+                for (int g = 0; g < NF; ++g) v[g] = acc[i % MF][g][i / MF];
+                if (m + i < p.m) store_row<T, NF>(o, n, p.n, v, accumulate);
+                o += stride;
+            }
         }
+    };
+    if (p.splits > 1)
+        write(p.partial + (uint64_t)split * p.m * p.partial_stride, p.partial_stride, false);
+    else if constexpr (FULL)
+        write(reinterpret_cast<float *>(p.out), p.out_stride, p.accumulate);
+    else if (p.out_type == CNR_FLOAT_BF16)
+        write(reinterpret_cast<__bf16 *>(p.out), p.out_stride, p.accumulate);
+    else
+        write(reinterpret_cast<_Float16 *>(p.out), p.out_stride, p.accumulate);
 }
 
 // The parts of sums that were split, added up in order: four outputs of a row to a thread.

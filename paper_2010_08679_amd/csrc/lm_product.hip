@@ -14,6 +14,7 @@
 // Scales of any value multiply each block's sum before it is added to the total.
 #include "lm_common.h"
 
+#include <math.h>
 #include <type_traits>
 
 namespace {
@@ -215,21 +216,10 @@ __global__ void __launch_bounds__(kBlock) narrow_kernel(const ProductArgs p) {
     }
 }
 
-template <int MF, int NF, int U>
-void narrow(const ProductArgs &p, cnr_scale_type scale, hipStream_t s) {
+template <bool FULL, int SCALE, int MF, int NF, int U>
+void narrow(const ProductArgs &p, hipStream_t s) {
     const dim3 grid((unsigned)cnr_ceil_div(p.n, 16 * NF), (unsigned)cnr_ceil_div(p.m, 16 * MF));
-    const bool full = p.out_type == CNR_FLOAT_F32;
-    if (scale == CNR_SCALE_E8M0) {
-        if (full)
-            hipLaunchKernelGGL((narrow_kernel<CNR_SCALE_E8M0, true, MF, NF, U>), grid, dim3(kBlock), 0, s, p);
-        else
-            hipLaunchKernelGGL((narrow_kernel<CNR_SCALE_E8M0, false, MF, NF, U>), grid, dim3(kBlock), 0, s, p);
-    } else {
-        if (full)
-            hipLaunchKernelGGL((narrow_kernel<CNR_SCALE_F32, true, MF, NF, U>), grid, dim3(kBlock), 0, s, p);
-        else
-            hipLaunchKernelGGL((narrow_kernel<CNR_SCALE_F32, false, MF, NF, U>), grid, dim3(kBlock), 0, s, p);
-    }
+    hipLaunchKernelGGL((narrow_kernel<SCALE, FULL, MF, NF, U>), grid, dim3(kBlock), 0, s, p);
 }
 
 // ---- many rows: tiles staged in LDS -----------------------------------------------------------------------------
@@ -688,11 +678,89 @@ void tiled(const ProductArgs &p, hipStream_t s) {
     }
 }
 
+// ---- which kernel ---------------------------------------------------------------------------------------------------
+//
+// Each kernel's time for a product is estimated and the shortest taken.  A workgroup's time for a block of 128 columns, by how
+// many share a compute unit, in us; measured with 8-bit instructions; conversion or scaled sums take 1.7 times as long (1.5 to 1.85).
+// 8192^3 with each (bfloat16, powers of two): 424, 1020, 511, 656 and 862 us; 2048^3 26, 14.6, 16.3, 15.9 and 19.8; 512 x 4096 x 4096
+// 44, 20.4, 25, 22.6 and 17.6; 64 x 8192 x 8192 79, 33, 43, 40 and 21.4 (16.6 in two parts).
+struct Tiles {
+    uint32_t rows, columns, resident;  // outputs of a workgroup; workgroups on a compute unit
+    float block[3];
+};
+constexpr Tiles kTiles[] = {
+    {256, 256, 1, {1.65f, 0.0f, 0.0f}},   // eight waves of 128 x 64, 8-bit instructions only
+    {128, 128, 1, {0.54f, 0.0f, 0.0f}},   // eight waves of 64 x 32, four stages: one tile for each compute unit
+    {128, 128, 2, {0.65f, 1.0f, 0.0f}},   // four waves of 64 x 64
+    {64, 128, 3, {0.55f, 0.68f, 0.96f}},  // four waves of 32 x 64
+    {64, 64, 2, {0.28f, 0.42f, 0.0f}},    // four waves of 32 x 32, four stages
+};
+constexpr int kNarrow = (int)(sizeof(kTiles) / sizeof(kTiles[0]));
+constexpr uint32_t kMaxSplits = 8, kMinBlocks = 4;  // parts of a sum, blocks of a part
+
+struct Plan {
+    int kernel;  // of kTiles, or kNarrow
+    uint32_t splits;
+};
+Plan plan_of(const cnr_ctx *ctx, uint64_t m, uint64_t n, uint64_t k, bool plain, bool may_split) {
+    const float units = ctx ? (float)ctx->n_cu : 256.0f, blocks = (float)cnr_ceil_div(k, CNR_BLOCK), outputs = (float)m * (float)n;
+    const float memory = 3.5f + ((float)m * k + (float)n * k + 2.0f * outputs) / 4.7e6f;  // us at what codes are read at
+    // The narrow kernel reads B once for each sixteen rows of A; a lone workgroup takes 0.115 us a block.
+    Plan best = {kNarrow, 1};
+    const float passes = (float)cnr_ceil_div(m, 16);
+    const float read = passes * (float)n * k / 4.2e6f, alone = 0.115f * blocks;
+    float least = 3.5f + (read > alone ? read : alone);
+    if (cnr_block_row_bytes(k) >= 1u << 24) return best;  // a tile's offsets are 32 bits: 256 rows of less than 2^24 codes
+    for (int i = 0; i < kNarrow; ++i) {
+        if (i == 0 && !plain) continue;
+        const Tiles &t = kTiles[i];
+        const float tiles = (float)cnr_ceil_div(m, t.rows) * (float)cnr_ceil_div(n, t.columns), slow = plain ? 1.0f : 1.7f;
+        for (uint32_t s = 1; s == 1 || (may_split && s <= kMaxSplits && blocks >= (float)(s * kMinBlocks)); s *= 2) {
+            const float groups = tiles * (float)s, round = units * (float)t.resident, rounds = floorf(groups / round);
+            const float rest = ceilf((groups - rounds * round) / units);  // workgroups on a unit in the last round
+            float time = ceilf(blocks / (float)s) * slow * (rounds * t.block[t.resident - 1] + (rest > 0.0f ? t.block[(int)rest - 1] : 0.0f));
+            time += 3.5f + 1.5f * (rounds + (rest > 0.0f ? 1.0f : 0.0f));
+            time = (time > memory ? time : memory) + 0.25f * (time < memory ? time : memory);  // one does not quite hide the other
+            if (s > 1) time += 3.5f + (float)(s + 1) * outputs * 4.0f / 3e6f;  // writing the parts, and joining them
+            if (time < least) {
+                least = time;
+                best = {i, s};
+            }
+        }
+    }
+    return best;
+}
+uint64_t partial_bytes(uint64_t m, uint64_t n, uint32_t splits) {
+    return splits > 1 ? (uint64_t)splits * m * (cnr_ceil_div(n, 4) * 4) * sizeof(float) : 0;
+}
+
+template <bool FULL, int SCALE>
+void launch(const ProductArgs &p, const Plan &plan, hipStream_t s) {
+    if constexpr (!FULL && SCALE == CNR_SCALE_E8M0) {
+        if (plan.kernel == 0) return tiled<FULL, SCALE, 2, 4, 8, 4, 2>(p, s);
+    }
+    switch (plan.kernel) {
+        case 1: return tiled<FULL, SCALE, 2, 4, 4, 2, 4>(p, s);
+        case 2: return tiled<FULL, SCALE, 2, 2, 4, 4, 2>(p, s);
+        case 3: return tiled<FULL, SCALE, 2, 2, 2, 4, 2>(p, s);
+        case 4: return tiled<FULL, SCALE, 2, 2, 2, 2, 4>(p, s);
+    }
+    // Two fragments of B to a wave where that still gives every SIMD a wave: A's codes are read half as often (16 x 32000 x 4096 37 -> 31 us).
+    if (p.m > 1 && p.n >= 16384)
+        narrow<FULL, SCALE, 1, 2, 1>(p, s);
+    else
+        narrow<FULL, SCALE, 1, 1, 2>(p, s);
+}
+
 }  // namespace
 
 extern "C" {
 
-size_t cnr_block_product_workspace_bytes(const cnr_ctx *, uint64_t, uint64_t, uint64_t) { return 0; }
+size_t cnr_block_product_workspace_bytes(const cnr_ctx *ctx, uint64_t m, uint64_t n, uint64_t k) {
+    if (m > CNR_LM_MAX_SIZE || n > CNR_LM_MAX_SIZE || k > CNR_LM_MAX_SIZE) return 0;
+    const uint64_t a = partial_bytes(m, n, plan_of(ctx, m, n, k, true, true).splits), b = partial_bytes(m, n, plan_of(ctx, m, n, k, false, true).splits);
+    return (size_t)(a > b ? a : b);
+}
 
 cnr_status cnr_block_product(cnr_ctx *ctx, const uint8_t *a_codes, const void *a_scale, cnr_block_kind a_kind,
                              uint64_t m, const uint8_t *b_codes, const void *b_scale, cnr_block_kind b_kind,
@@ -728,19 +796,17 @@ cnr_status cnr_block_product(cnr_ctx *ctx, const uint8_t *a_codes, const void *a
     p.out_stride = out_stride;
     p.out_type = out_type;
     p.accumulate = accumulate ? 1 : 0;
-    p.splits = 1;
+    const bool full = out_type == CNR_FLOAT_F32, powers = scale_type == CNR_SCALE_E8M0;
+    const Plan plan = plan_of(ctx, m, n, k, powers && !full, workspace != nullptr);
+    if (plan.kernel == kNarrow && cnr_ceil_div(m, 16) > 65535) return CNR_E_TOO_LARGE;
+    p.splits = plan.splits;
     p.partial = reinterpret_cast<float *>(workspace);
     p.partial_stride = cnr_ceil_div(n, 4) * 4;
-    // A tile's offsets are 32 bits: 256 rows of less than 2^24 codes.
     hipStream_t to = as_stream(stream);
-    if (m > 64 && p.row_bytes < 1u << 24) {
-        if (out_type == CNR_FLOAT_F32)
-            scale_type == CNR_SCALE_E8M0 ? tiled<true, CNR_SCALE_E8M0, 2, 4, 4, 4, 2>(p, to) : tiled<true, CNR_SCALE_F32, 2, 4, 4, 4, 2>(p, to);
-        else
-            scale_type == CNR_SCALE_E8M0 ? tiled<false, CNR_SCALE_E8M0, 2, 4, 8, 4, 2>(p, to) : tiled<false, CNR_SCALE_F32, 2, 4, 4, 4, 2>(p, to);
-    } else {
-        narrow<1, 1, 2>(p, scale_type, to);
-    }
+    if (full)
+        powers ? launch<true, CNR_SCALE_E8M0>(p, plan, to) : launch<true, CNR_SCALE_F32>(p, plan, to);
+    else
+        powers ? launch<false, CNR_SCALE_E8M0>(p, plan, to) : launch<false, CNR_SCALE_F32>(p, plan, to);
     return cnr_launch_status(ctx);
 }
 

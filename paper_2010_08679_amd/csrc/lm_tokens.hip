@@ -77,8 +77,12 @@ __global__ void __launch_bounds__(kBlock) count_kernel(const CountArgs a) {
 
 // ---- logits -----------------------------------------------------------------------------------------------------
 
-constexpr uint32_t kTokensPerThread = 8;
-constexpr uint32_t kChunk = kBlock * kTokensPerThread;  // tokens of a workgroup
+// Bound by memory: a logit is read and written once, a bit of each bitmap beside it.  A thread holds 32 bytes of a row, so that enough
+// is under way.  Seen and biased tokens are few and far between: a row's logits are stored as the masks leave them, and then each
+// thread sees to its own special tokens, one after the other.  (Its tokens' counters share a sector, so that the first brings the
+// others; all counters at once and the arithmetic for every token would keep the vector units busy for longer than memory.)
+constexpr uint32_t kLogitBytes = 32;  // of a thread
+constexpr uint32_t kScannedBiases = 4 * kBlock;  // lists up to this are looked through, each workgroup all of it; longer ones searched
 
 struct AdjustArgs {
     const void *logits;
@@ -86,6 +90,10 @@ struct AdjustArgs {
     uint64_t stride, out_stride;
     uint64_t n, vocab, words;
     cnr_adjustments with;
+    // the rows' lists, or words that are there in their place
+    const int32_t *slots, *mask_of;
+    const float *repetition, *frequency, *presence;
+    bool has_slots, has_mask_of, has_repetition, has_frequency, has_presence;
     cnr_dev_errors *err;
 };
 
@@ -101,99 +109,110 @@ __device__ __forceinline__ uint64_t bias_from(const int32_t *tokens, uint64_t lo
     return lo;
 }
 
+// Biases of a chunk of N tokens.
+template <uint32_t N>
+struct Biases {
+    float value[N];
+    uint32_t there[N / 32];
+};
+template <>
+struct Biases<0> {};
+
 // grid.x: chunks of the vocabulary, grid.y: rows.
-template <int TYPE>
+template <int TYPE, bool BIASED>
 __global__ void __launch_bounds__(kBlock) adjust_kernel(const AdjustArgs a) {
     typedef typename Element<TYPE>::type T;
-    __shared__ float bias[kChunk];
+    constexpr uint32_t kPer = kLogitBytes / sizeof(T), kChunk = kBlock * kPer, kBits = (1u << kPer) - 1u;
+    __shared__ Biases<BIASED ? kChunk : 0> lds;
     const cnr_adjustments &w = a.with;
-    const uint32_t begin = wg_x() * kChunk, first = begin + tid_x() * kTokensPerThread;
+    const uint32_t t = tid_x(), own = t * kPer, begin = wg_x() * kChunk, first = begin + own;
     for (uint64_t row = wg_y(); row < a.n; row += 32768) {
-        // 8 tokens' bits lie in one byte of a bitmap, since `first` is a multiple of 8
-        uint32_t allowed = 0xffu, seen = 0u;
-        const bool inside = first < a.vocab;
-        uint64_t slot = 0;
-        if (w.masks) {
-            const int64_t m = w.mask_of ? (int64_t)w.mask_of[row] : (int64_t)row;
-            if (m >= 0 && (uint64_t)m < w.n_masks) {
-                if (inside) allowed = w.masks[(uint64_t)m * a.words + first / 32] >> (first % 32) & 0xffu;
-            } else if (m >= 0 && begin == 0 && tid_x() == 0) {
-                raise_flag(a.err, CNR_FLAG_ROW_ID);
-            }
+        const bool inside = first < a.vocab, whole = first + kPer <= a.vocab;
+        const T *from = reinterpret_cast<const T *>(a.logits) + row * a.stride + first;
+        Pack<T, kPer> v;
+        if (whole) {
+            v = *reinterpret_cast<const Pack<T, kPer> *>(from);
+        } else {
+#pragma unroll
+            for (uint32_t j = 0; j < kPer; ++j) v.v[j] = first + j < a.vocab ? from[j] : (T)0.0f;
         }
-        if (w.seen) {
-            const int64_t s = w.slots ? (int64_t)w.slots[row] : (int64_t)row;
-            if (s >= 0 && (uint64_t)s < w.n_slots) {
-                slot = (uint64_t)s;
-                if (inside) seen = w.seen[slot * a.words + first / 32] >> (first % 32) & 0xffu;
-            } else if (s >= 0 && begin == 0 && tid_x() == 0) {
-                raise_flag(a.err, CNR_FLAG_ROW_ID);
-            }
-        }
-        bool biased = false;
-        if (w.bias_offsets) {
+        // What the row has, all asked for at once: lists that are not given are replaced by words that are there.
+        const int64_t mask = a.mask_of[a.has_mask_of ? row : 0], id = a.slots[a.has_slots ? row : 0];
+        const int64_t m = a.has_mask_of ? mask : (int64_t)row, s = a.has_slots ? id : (int64_t)row;
+        const bool masked = m >= 0 && (uint64_t)m < w.n_masks, counted = s >= 0 && (uint64_t)s < w.n_slots;
+        if (first == 0 && ((w.masks && m >= 0 && !masked) || (w.seen && s >= 0 && !counted))) raise_flag(a.err, CNR_FLAG_ROW_ID);
+        // A thread's tokens' bits lie in one word of a bitmap, since `first` is a multiple of their number.
+        uint32_t allowed = kBits, seen = 0, biased = 0;
+        if (w.masks && masked && inside) allowed = w.masks[(uint64_t)m * a.words + first / 32] >> (first % 32) & kBits;
+        if (w.seen && counted && inside) seen = w.seen[(uint64_t)s * a.words + first / 32] >> (first % 32) & kBits;
+        if constexpr (BIASED) {
             uint64_t lo = w.bias_offsets[row], hi = w.bias_offsets[row + 1];
             hi = hi < w.n_bias ? hi : w.n_bias;
-            if (lo < hi) {
-                lo = bias_from(w.bias_tokens, lo, hi, (int64_t)begin);
-                hi = bias_from(w.bias_tokens, lo, hi, (int64_t)begin + kChunk);
-            }
             if (lo < hi) {  // the same for the whole workgroup
-                biased = true;
+                if (hi - lo > kScannedBiases) {
+                    lo = bias_from(w.bias_tokens, lo, hi, (int64_t)begin);
+                    hi = bias_from(w.bias_tokens, lo, hi, (int64_t)begin + kChunk);
+                }
+                if (t < kChunk / 32) lds.there[t] = 0;
                 __syncthreads();
-#pragma unroll
-                for (uint32_t j = 0; j < kTokensPerThread; ++j) bias[j * kBlock + tid_x()] = 0.0f;
-                __syncthreads();
-                for (uint64_t e = lo + tid_x(); e < hi; e += kBlock) {
-                    const int64_t at = (int64_t)w.bias_tokens[e] - (int64_t)begin;
-                    if (at >= 0 && at < (int64_t)kChunk) bias[at] = w.bias_values[e];
+                for (uint64_t e = lo + t; e < hi; e += kBlock) {
+                    const uint64_t at = (uint64_t)((int64_t)w.bias_tokens[e] - (int64_t)begin);
+                    if (at < kChunk) {
+                        lds.value[at] = w.bias_values[e];
+                        atomicOr(&lds.there[at / 32], 1u << (at % 32));
+                    }
                 }
                 __syncthreads();
+                biased = lds.there[own / 32] >> (own % 32) & kBits;
             }
         }
-        if (!inside) continue;
-        const T *from = reinterpret_cast<const T *>(a.logits) + row * a.stride + first;
-        T *to = reinterpret_cast<T *>(a.out) + row * a.out_stride + first;
-        const bool whole = first + kTokensPerThread <= a.vocab;
-        Pack<T, kTokensPerThread> got;
-        if (whole)
-            got = *reinterpret_cast<const Pack<T, kTokensPerThread> *>(from);
-        else
+        if (inside) {
+            T *to = reinterpret_cast<T *>(a.out) + row * a.out_stride + first;
+            uint32_t special = (seen | biased) & allowed;
 #pragma unroll
-            for (uint32_t j = 0; j < kTokensPerThread; ++j) got.v[j] = first + j < a.vocab ? from[j] : (T)0.0f;
-        float v[kTokensPerThread];
+            for (uint32_t j = 0; j < kPer; ++j) v.v[j] = allowed >> j & 1u ? v.v[j] : (T)(-__builtin_inff());
+            if (whole) {
+                *reinterpret_cast<Pack<T, kPer> *>(to) = v;
+            } else {
 #pragma unroll
-        for (uint32_t j = 0; j < kTokensPerThread; ++j) v[j] = Element<TYPE>::wide(got.v[j]);
-        if (seen) {
-            const float repetition = w.repetition ? w.repetition[row] : 1.0f;
-            const float frequency = w.frequency ? w.frequency[row] : 0.0f, presence = w.presence ? w.presence[row] : 0.0f;
-            const uint32_t *counts = w.counts ? w.counts + slot * a.vocab + first : nullptr;
-#pragma unroll
-            for (uint32_t j = 0; j < kTokensPerThread; ++j) {
-                if (!(seen >> j & 1u) || first + j >= a.vocab) continue;
-                v[j] = v[j] > 0.0f ? v[j] / repetition : v[j] * repetition;
-                if (counts) {
-                    const uint32_t count = counts[j];
-                    v[j] -= frequency * (float)count;
-                    if (count) v[j] -= presence;
-                }
+                for (uint32_t j = 0; j < kPer; ++j)
+                    if (first + j < a.vocab) to[j] = v.v[j];
+                special &= (1u << (uint32_t)(a.vocab - first)) - 1u;
+            }
+            if (special) {
+                const float repetition = a.repetition[a.has_repetition ? row : 0], frequency = a.frequency[a.has_frequency ? row : 0],
+                            presence = a.presence[a.has_presence ? row : 0];
+                const uint32_t *counts = w.counts + (uint64_t)s * a.vocab + first;
+                do {
+                    const uint32_t j = (uint32_t)__ffs((int)special) - 1u;
+                    special &= special - 1u;
+                    float x = Element<TYPE>::wide(from[j]);  // as it was: what is special has been stored unchanged
+                    if (seen >> j & 1u) {
+                        const uint32_t count = w.counts ? counts[j] : 0u;
+                        const float r = a.has_repetition ? repetition : 1.0f;
+                        x = x > 0.0f ? x / r : x * r;
+                        if (w.counts && a.has_frequency) x -= frequency * (float)count;
+                        if (count && a.has_presence) x -= presence;
+                    }
+                    if constexpr (BIASED) {
+                        if (biased >> j & 1u) x += lds.value[own + j];
+                    }
+                    to[j] = Element<TYPE>::narrow(x);
+                } while (special);
             }
         }
-        if (biased) {
-#pragma unroll
-            for (uint32_t j = 0; j < kTokensPerThread; ++j) v[j] += bias[tid_x() * kTokensPerThread + j];
-        }
-        Pack<T, kTokensPerThread> put;
-#pragma unroll
-        for (uint32_t j = 0; j < kTokensPerThread; ++j)
-            put.v[j] = Element<TYPE>::narrow(allowed >> j & 1u ? v[j] : -__builtin_inff());
-        if (whole)
-            *reinterpret_cast<Pack<T, kTokensPerThread> *>(to) = put;
-        else
-#pragma unroll
-            for (uint32_t j = 0; j < kTokensPerThread; ++j)
-                if (first + j < a.vocab) to[j] = put.v[j];
+        if (BIASED && row + 32768 < a.n) __syncthreads();  // the biases are filled again
     }
+}
+
+template <int TYPE>
+void adjust(const AdjustArgs &a, hipStream_t s) {
+    constexpr uint32_t kChunk = kBlock * (kLogitBytes / sizeof(typename Element<TYPE>::type));
+    const dim3 grid((unsigned)cnr_ceil_div(a.vocab, kChunk), (unsigned)(a.n < 32768 ? a.n : 32768));
+    if (a.with.bias_offsets)
+        hipLaunchKernelGGL((adjust_kernel<TYPE, true>), grid, dim3(kBlock), 0, s, a);
+    else
+        hipLaunchKernelGGL((adjust_kernel<TYPE, false>), grid, dim3(kBlock), 0, s, a);
 }
 
 }  // namespace
@@ -270,13 +289,23 @@ cnr_status cnr_adjust_logits(cnr_ctx *ctx, const void *logits, uint64_t stride, 
     a.words = cnr_bitmap_words(vocab);
     a.with = w;
     a.err = ctx->dev_err;
-    const dim3 grid((unsigned)cnr_ceil_div(vocab, kChunk), (unsigned)(n < 32768 ? n : 32768));
+    const void *something = ctx->dev_err;
+    a.has_slots = w.slots != nullptr;
+    a.has_mask_of = w.mask_of != nullptr;
+    a.has_repetition = w.repetition != nullptr;
+    a.has_frequency = w.frequency != nullptr;
+    a.has_presence = w.presence != nullptr;
+    a.slots = w.slots ? w.slots : (const int32_t *)something;
+    a.mask_of = w.mask_of ? w.mask_of : (const int32_t *)something;
+    a.repetition = w.repetition ? w.repetition : (const float *)something;
+    a.frequency = w.frequency ? w.frequency : (const float *)something;
+    a.presence = w.presence ? w.presence : (const float *)something;
     if (type == CNR_FLOAT_F32)
-        hipLaunchKernelGGL((adjust_kernel<CNR_FLOAT_F32>), grid, dim3(kBlock), 0, as_stream(stream), a);
+        adjust<CNR_FLOAT_F32>(a, as_stream(stream));
     else if (type == CNR_FLOAT_BF16)
-        hipLaunchKernelGGL((adjust_kernel<CNR_FLOAT_BF16>), grid, dim3(kBlock), 0, as_stream(stream), a);
+        adjust<CNR_FLOAT_BF16>(a, as_stream(stream));
     else
-        hipLaunchKernelGGL((adjust_kernel<CNR_FLOAT_F16>), grid, dim3(kBlock), 0, as_stream(stream), a);
+        adjust<CNR_FLOAT_F16>(a, as_stream(stream));
     return cnr_launch_status(ctx);
 }
 

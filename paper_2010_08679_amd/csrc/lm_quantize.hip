@@ -25,27 +25,47 @@ struct QuantizeArgs {
     uint64_t scale_stride, scale_stride_t;
 };
 
-// Largest absolute value by its bits (they order like the values); infinities and NaN have none.
-__device__ __forceinline__ uint32_t magnitude(float v) {
-    const uint32_t b = __float_as_uint(v) & 0x7fffffffu;
-    return b < 0x7f800000u ? b : 0u;
-}
-__device__ __forceinline__ uint32_t umax(uint32_t a, uint32_t b) { return a > b ? a : b; }
+// Magnitudes of elements by their bits, which order like the values: a word holds two of a 16-bit type or one float.
+template <int TYPE>
+struct Magnitude {
+    static constexpr int kIn = TYPE == CNR_FLOAT_F32 ? 1 : 2;  // elements in a word
+    static constexpr uint32_t kInfinite = TYPE == CNR_FLOAT_F32 ? 0x7f800000u : TYPE == CNR_FLOAT_BF16 ? 0x7f80u : 0x7c00u;
+    static __device__ __forceinline__ uint32_t of(uint32_t w) { return w & (kIn == 1 ? 0x7fffffffu : 0x7fff7fffu); }
+    static __device__ __forceinline__ uint32_t larger(uint32_t a, uint32_t b) {
+        if constexpr (kIn == 1) return a > b ? a : b;
+        typedef unsigned short u16x2 __attribute__((ext_vector_type(2)));
+        return __builtin_bit_cast(uint32_t, __builtin_elementwise_max(__builtin_bit_cast(u16x2, a), __builtin_bit_cast(u16x2, b)));
+    }
+    static __device__ __forceinline__ uint32_t largest(uint32_t w) { return kIn == 1 ? w : (w & 0xffffu) > (w >> 16) ? w & 0xffffu : w >> 16; }
+    static __device__ __forceinline__ uint32_t part(uint32_t w, int i) { return kIn == 1 ? w : i ? w >> 16 : w & 0xffffu; }
+    static __device__ __forceinline__ bool odd(uint32_t w) { return largest(w) >= kInfinite; }  // one that is infinite or NaN
+    static __device__ __forceinline__ uint32_t without_odd(uint32_t w) {
+        if constexpr (kIn == 1) return w < kInfinite ? w : 0u;
+        return ((w & 0xffffu) < kInfinite ? w & 0xffffu : 0u) | ((w >> 16) < kInfinite ? w & 0xffff0000u : 0u);
+    }
+    static __device__ __forceinline__ uint32_t as_float(uint32_t m) {  // bits
+        if constexpr (TYPE == CNR_FLOAT_F32) return m;
+        if constexpr (TYPE == CNR_FLOAT_BF16) return m << 16;
+        return __float_as_uint((float)__builtin_bit_cast(_Float16, (uint16_t)m));
+    }
+};
 
+template <typename M>
 __device__ __forceinline__ uint32_t max_across(uint32_t m) {  // of the 16 lanes that hold a row
-    m = umax(m, (uint32_t)dpp_i<0xB1>((int)m));
-    m = umax(m, (uint32_t)dpp_i<0x4E>((int)m));
-    m = umax(m, (uint32_t)dpp_i<0x141>((int)m));
-    return umax(m, (uint32_t)dpp_i<0x140>((int)m));
+    m = M::larger(m, (uint32_t)dpp_i<0xB1>((int)m));
+    m = M::larger(m, (uint32_t)dpp_i<0x4E>((int)m));
+    m = M::larger(m, (uint32_t)dpp_i<0x141>((int)m));
+    return M::larger(m, (uint32_t)dpp_i<0x140>((int)m));
 }
+template <typename M>
 __device__ __forceinline__ uint32_t max_down(uint32_t m) {  // of the wave's lanes that hold the same columns
-    m = umax(m, (uint32_t)__shfl_xor((int)m, 16));
-    return umax(m, (uint32_t)__shfl_xor((int)m, 32));
+    m = M::larger(m, (uint32_t)__shfl_xor((int)m, 16));
+    return M::larger(m, (uint32_t)__shfl_xor((int)m, 32));
 }
 
 // A block's scale from the bits of its largest magnitude.  Powers of two: 448 = 1.75 * 2^8, so the exponent is the magnitude's less
 // 8, one more where its fraction is above 1.75.  They divide exactly, a transposed tile's codes are the tile's, and
-// the matrix instructions take them as they are.  code = e4m3(x / scale): `inv` is 1 / scale.
+// the matrix instructions take them as they are.  `inv` is 1 / scale.
 struct Scale {
     float value, inv;
     uint8_t byte;
@@ -69,13 +89,10 @@ __device__ __forceinline__ Scale scale_of(uint32_t amax) {
     return s;
 }
 
-// The quotient whose e4m3 rounding is that of x / scale exactly.  With powers of two that is the quotient itself.
-// Else the rounded quotient could fall on the middle between two codes where the true one lies beside it: a
-// quotient that is not exact gets its last bit set after rounding towards zero, and a middle has that bit clear.
-// The remainder decides both; scaled up by 2^64 where it could leave fp32's range.
-template <int SCALE>
+// The quotient whose e4m3 rounding is that of x / scale exactly, for scales of any value: the rounded quotient could fall on the
+// middle between two codes where the true one lies beside it, so a quotient that is not exact gets its last bit set after rounding towards zero (a
+// middle has that bit clear).  The remainder decides both; scaled up by 2^64 where it could leave fp32's range.
 __device__ __forceinline__ float quotient(float x, const Scale &s, bool tiny) {
-    if (SCALE == CNR_SCALE_E8M0) return x * s.inv;
     float d = s.value, inv = s.inv;
     if (tiny) {
         const float up = d < 0x1p-60f ? 0x1p64f : 1.0f, down = d < 0x1p-60f ? 0x1p-64f : 1.0f;
@@ -91,15 +108,50 @@ __device__ __forceinline__ float quotient(float x, const Scale &s, bool tiny) {
     return __builtin_copysignf(__uint_as_float(rest != 0.0f ? b | 1u : __float_as_uint(q)), x);  // -0 became 0
 }
 
-template <int SCALE>
-__device__ __forceinline__ u32x2 encode8(const float *v, const Scale &s, bool tiny) {
-    u32x2 w;
+// The codes of two elements, in the half HIGH of a word.  Scales of powers of two divide in the conversion itself: its results are the
+// definition's for every 16-bit input, and floats, at scales from 2^-126 to 2^120.
+typedef short s16x2 __attribute__((ext_vector_type(2)));
+template <int TYPE, bool HIGH>
+__device__ __forceinline__ s16x2 encode_pair(s16x2 word, uint32_t pair, float scale) {
+    if constexpr (TYPE == CNR_FLOAT_BF16) {
+        typedef __bf16 pair_of __attribute__((ext_vector_type(2)));
+        return __builtin_amdgcn_cvt_scalef32_pk_fp8_bf16(word, __builtin_bit_cast(pair_of, pair), scale, HIGH);
+    } else {
+        typedef _Float16 pair_of __attribute__((ext_vector_type(2)));
+        return __builtin_amdgcn_cvt_scalef32_pk_fp8_f16(word, __builtin_bit_cast(pair_of, pair), scale, HIGH);
+    }
+}
+// The codes of eight elements, given as words of them.
+template <int TYPE, int SCALE>
+__device__ __forceinline__ u32x2 encode8(const uint32_t *w, const Scale &s, bool tiny) {
+    u32x2 codes;
 #pragma unroll
     for (int i = 0; i < 2; ++i) {
-        int r = __builtin_amdgcn_cvt_pk_fp8_f32(quotient<SCALE>(v[4 * i], s, tiny), quotient<SCALE>(v[4 * i + 1], s, tiny), 0, false);
-        w[i] = (uint32_t)__builtin_amdgcn_cvt_pk_fp8_f32(quotient<SCALE>(v[4 * i + 2], s, tiny), quotient<SCALE>(v[4 * i + 3], s, tiny), r, true);
+        if constexpr (SCALE == CNR_SCALE_E8M0) {
+            s16x2 word = {0, 0};
+            if constexpr (TYPE == CNR_FLOAT_F32) {
+                word = __builtin_amdgcn_cvt_scalef32_pk_fp8_f32(word, __uint_as_float(w[4 * i]), __uint_as_float(w[4 * i + 1]), s.value, false);
+                word = __builtin_amdgcn_cvt_scalef32_pk_fp8_f32(word, __uint_as_float(w[4 * i + 2]), __uint_as_float(w[4 * i + 3]), s.value, true);
+            } else {
+                word = encode_pair<TYPE, false>(word, w[2 * i], s.value);
+                word = encode_pair<TYPE, true>(word, w[2 * i + 1], s.value);
+            }
+            codes[i] = __builtin_bit_cast(uint32_t, word);
+        } else {
+            float q[4];
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                const int e = 4 * i + j;
+                if constexpr (TYPE == CNR_FLOAT_F32)
+                    q[j] = quotient(__uint_as_float(w[e]), s, tiny);
+                else
+                    q[j] = quotient(Element<TYPE>::wide(__builtin_bit_cast(typename Element<TYPE>::type, (uint16_t)(w[e / 2] >> (16 * (e % 2))))), s, tiny);
+            }
+            const int r = __builtin_amdgcn_cvt_pk_fp8_f32(q[0], q[1], 0, false);
+            codes[i] = (uint32_t)__builtin_amdgcn_cvt_pk_fp8_f32(q[2], q[3], r, true);
+        }
     }
-    return w;
+    return codes;
 }
 template <int SCALE>
 __device__ __forceinline__ bool any_tiny(const Scale &s) {
@@ -117,109 +169,154 @@ __device__ __forceinline__ void store_scale(void *to, uint64_t at, const Scale &
 template <int TYPE, int KIND, int SCALE, bool BOTH>
 __global__ void __launch_bounds__(kBlock) quantize_kernel(const QuantizeArgs a) {
     typedef typename Element<TYPE>::type T;
+    typedef Magnitude<TYPE> M;
+    constexpr int kWords = kPer / M::kIn;  // of a thread's part of a row
     __shared__ __align__(16) uint8_t turned[BOTH ? kTile * kPitch : 16];
-    __shared__ uint32_t largest[kWavesPerBlock][kTile];
+    __shared__ __align__(16) uint32_t largest[kWavesPerBlock][kTile / M::kIn];
     const uint32_t tile_row = wg_x() / a.tiles_across, tile_col = wg_x() % a.tiles_across;
     const uint32_t t = tid_x(), wave = t / kWave;
     const uint32_t r0 = tile_row * kTile + t / kAcross * kPer, c0 = tile_col * kTile + t % kAcross * kPer;
     const T *x = reinterpret_cast<const T *>(a.x);
 
-    float v[kPer][kPer];
-    Pack<T, kPer> got[kPer];
-    const bool whole = tile_row * kTile + kTile <= a.n_rows && tile_col * kTile + kTile <= a.dim;
-    if (whole) {
+    // Rows beyond the matrix read its last one, and count as zeros.
+    uint32_t w[kPer][kWords];
+    const uint32_t last = a.n_rows - 1;
+    if (c0 + kPer <= a.dim) {
 #pragma unroll
-        for (int r = 0; r < kPer; ++r) got[r] = *reinterpret_cast<const Pack<T, kPer> *>(x + (uint64_t)(r0 + r) * a.stride + c0);
+        for (int r = 0; r < kPer; ++r)
+#pragma unroll
+            for (int i = 0; i < kWords / 4; ++i) {
+                const u32x4 got = load16(x + (uint64_t)(r0 + r < last ? r0 + r : last) * a.stride + c0 + i * (16 / sizeof(T)));
+#pragma unroll
+                for (int j = 0; j < 4; ++j) w[r][4 * i + j] = got[j];
+            }
     } else {
 #pragma unroll
-        for (int r = 0; r < kPer; ++r)
+        for (int r = 0; r < kPer; ++r) {
+            T part[kPer];
+            const T *from = x + (uint64_t)(r0 + r < last ? r0 + r : last) * a.stride;
 #pragma unroll
-            for (int c = 0; c < kPer; ++c)
-                got[r].v[c] = r0 + r < a.n_rows && c0 + c < a.dim ? x[(uint64_t)(r0 + r) * a.stride + c0 + c] : (T)0.0f;
+            for (int c = 0; c < kPer; ++c) part[c] = c0 + c < a.dim ? from[c0 + c] : (T)0.0f;
+            __builtin_memcpy(w[r], part, sizeof(part));
+        }
     }
-#pragma unroll
-    for (int r = 0; r < kPer; ++r)
-#pragma unroll
-        for (int c = 0; c < kPer; ++c) v[r][c] = Element<TYPE>::wide(got[r].v[c]);
-
-    if (KIND == CNR_BLOCK_TILE) {
-        uint32_t m = 0;
+    if (tile_row * kTile + kTile > a.n_rows) {
 #pragma unroll
         for (int r = 0; r < kPer; ++r)
 #pragma unroll
-            for (int c = 0; c < kPer; ++c) m = umax(m, magnitude(v[r][c]));
-        m = max_down(max_across(m));
-        if (t % kWave == 0) largest[wave][0] = m;
+            for (int i = 0; i < kWords; ++i) w[r][i] = r0 + r <= last ? w[r][i] : 0u;
+    }
+
+    // Magnitudes, and the largest of each column; infinities and NaN, which do not count, are rare.
+    uint32_t mag[kPer][kWords], down[kWords];
+#pragma unroll
+    for (int i = 0; i < kWords; ++i) {
+        down[i] = mag[0][i] = M::of(w[0][i]);
+#pragma unroll
+        for (int r = 1; r < kPer; ++r) {
+            mag[r][i] = M::of(w[r][i]);
+            down[i] = M::larger(down[i], mag[r][i]);
+        }
+    }
+    uint32_t all = down[0];
+#pragma unroll
+    for (int i = 1; i < kWords; ++i) all = M::larger(all, down[i]);
+    if (__any(M::odd(all))) {
+        all = 0;
+#pragma unroll
+        for (int i = 0; i < kWords; ++i) {
+            down[i] = 0;
+#pragma unroll
+            for (int r = 0; r < kPer; ++r) {
+                mag[r][i] = M::without_odd(mag[r][i]);
+                down[i] = M::larger(down[i], mag[r][i]);
+            }
+            all = M::larger(all, down[i]);
+        }
+    }
+
+    if constexpr (KIND == CNR_BLOCK_TILE) {
+        all = max_down<M>(max_across<M>(all));
+        if (t % kWave == 0) largest[wave][0] = all;
         __syncthreads();
 #pragma unroll
-        for (int w = 0; w < kWavesPerBlock; ++w) m = umax(m, largest[w][0]);
-        const Scale s = scale_of<SCALE>(m);
+        for (int i = 0; i < kWavesPerBlock; ++i) all = M::larger(all, largest[i][0]);
+        const Scale s = scale_of<SCALE>(M::as_float(M::largest(all)));
         const bool tiny = any_tiny<SCALE>(s);
         if (t == 0) {
             if (a.codes) store_scale<SCALE>(a.scale, tile_col * a.scale_stride + tile_row, s);
             if (BOTH) store_scale<SCALE>(a.scale_t, tile_row * a.scale_stride_t + tile_col, s);
         }
-        u32x2 w[kPer];
+        u32x2 codes[kPer];
 #pragma unroll
-        for (int r = 0; r < kPer; ++r) w[r] = encode8<SCALE>(v[r], s, tiny);
+        for (int r = 0; r < kPer; ++r) codes[r] = encode8<TYPE, SCALE>(w[r], s, tiny);
         if (a.codes) {
 #pragma unroll
             for (int r = 0; r < kPer; ++r)
-                if (r0 + r < a.n_rows) *reinterpret_cast<u32x2 *>(a.codes + (uint64_t)(r0 + r) * a.row_bytes + c0) = w[r];
+                if (r0 + r < a.n_rows) *reinterpret_cast<u32x2 *>(a.codes + (uint64_t)(r0 + r) * a.row_bytes + c0) = codes[r];
         }
-        if (BOTH) {
+        if constexpr (BOTH) {
+            // eight rows of eight codes, transposed by bytes: pairs of rows, then pairs of pairs
 #pragma unroll
-            for (int c = 0; c < kPer; ++c) {
-                u32x2 o;
+            for (int h = 0; h < 2; ++h) {
+                uint32_t pair[kPer / 2][2];
 #pragma unroll
-                for (int h = 0; h < 2; ++h) {
-                    o[h] = 0;
-#pragma unroll
-                    for (int i = 0; i < 4; ++i) o[h] |= ((w[4 * h + i][c / 4] >> (8 * (c % 4))) & 255u) << (8 * i);
+                for (int r = 0; r < kPer / 2; ++r) {
+                    pair[r][0] = __builtin_amdgcn_perm(codes[2 * r + 1][h], codes[2 * r][h], 0x05010400u);  // columns 0 and 1 of rows 2 r, 2 r + 1
+                    pair[r][1] = __builtin_amdgcn_perm(codes[2 * r + 1][h], codes[2 * r][h], 0x07030602u);
                 }
-                *reinterpret_cast<u32x2 *>(turned + (t % kAcross * kPer + c) * kPitch + t / kAcross * kPer) = o;
+#pragma unroll
+                for (int c = 0; c < 4; ++c) {
+                    const uint32_t pick = c % 2 ? 0x07060302u : 0x05040100u;
+                    const u32x2 column = {__builtin_amdgcn_perm(pair[1][c / 2], pair[0][c / 2], pick), __builtin_amdgcn_perm(pair[3][c / 2], pair[2][c / 2], pick)};
+                    *reinterpret_cast<u32x2 *>(turned + (t % kAcross * kPer + 4 * h + c) * kPitch + t / kAcross * kPer) = column;
+                }
             }
         }
     } else {
         if (a.codes) {
 #pragma unroll
             for (int r = 0; r < kPer; ++r) {
-                uint32_t m = 0;
+                uint32_t m = mag[r][0];
 #pragma unroll
-                for (int c = 0; c < kPer; ++c) m = umax(m, magnitude(v[r][c]));
-                const Scale s = scale_of<SCALE>(max_across(m));
+                for (int i = 1; i < kWords; ++i) m = M::larger(m, mag[r][i]);
+                const Scale s = scale_of<SCALE>(M::as_float(M::largest(max_across<M>(m))));
+                const bool tiny = any_tiny<SCALE>(s);
                 if (r0 + r < a.n_rows) {
-                    *reinterpret_cast<u32x2 *>(a.codes + (uint64_t)(r0 + r) * a.row_bytes + c0) = encode8<SCALE>(v[r], s, any_tiny<SCALE>(s));
+                    *reinterpret_cast<u32x2 *>(a.codes + (uint64_t)(r0 + r) * a.row_bytes + c0) = encode8<TYPE, SCALE>(w[r], s, tiny);
                     if (t % kAcross == 0) store_scale<SCALE>(a.scale, tile_col * a.scale_stride + r0 + r, s);
                 }
             }
         }
-        if (BOTH) {
+        if constexpr (BOTH) {
 #pragma unroll
-            for (int c = 0; c < kPer; ++c) {
-                uint32_t m = 0;
-#pragma unroll
-                for (int r = 0; r < kPer; ++r) m = umax(m, magnitude(v[r][c]));
-                m = max_down(m);
-                if (t % kWave < kAcross) largest[wave][t % kAcross * kPer + c] = m;
+            for (int i = 0; i < kWords; ++i) {
+                down[i] = max_down<M>(down[i]);
+                if (t % kWave < kAcross) largest[wave][t % kAcross * kWords + i] = down[i];
             }
             __syncthreads();
 #pragma unroll
+            for (int i = 0; i < kWords; ++i)
+#pragma unroll
+                for (int v = 0; v < kWavesPerBlock; ++v) down[i] = M::larger(down[i], largest[v][t % kAcross * kWords + i]);
+#pragma unroll
             for (int c = 0; c < kPer; ++c) {
-                uint32_t m = 0;
+                const Scale s = scale_of<SCALE>(M::as_float(M::part(down[c / M::kIn], c % M::kIn)));
+                uint32_t column[kWords];  // the thread's eight rows of column c, side by side
 #pragma unroll
-                for (int w = 0; w < kWavesPerBlock; ++w) m = umax(m, largest[w][t % kAcross * kPer + c]);
-                const Scale s = scale_of<SCALE>(m);
-                float down[kPer];
-#pragma unroll
-                for (int r = 0; r < kPer; ++r) down[r] = v[r][c];
+                for (int i = 0; i < kWords; ++i) {
+                    if constexpr (M::kIn == 1)
+                        column[i] = w[i][c];
+                    else
+                        column[i] = __builtin_amdgcn_perm(w[2 * i + 1][c / 2], w[2 * i][c / 2], c % 2 ? 0x07060302u : 0x05040100u);
+                }
                 *reinterpret_cast<u32x2 *>(turned + (t % kAcross * kPer + c) * kPitch + t / kAcross * kPer) =
-                    encode8<SCALE>(down, s, any_tiny<SCALE>(s));
+                    encode8<TYPE, SCALE>(column, s, any_tiny<SCALE>(s));
                 if (t < kAcross && c0 + c < a.dim) store_scale<SCALE>(a.scale_t, tile_row * a.scale_stride_t + c0 + c, s);
             }
         }
     }
-    if (BOTH) {
+    if constexpr (BOTH) {
         __syncthreads();
 #pragma unroll
         for (int i = 0; i < kTile * kTile / 16 / kBlock; ++i) {

@@ -65,10 +65,11 @@ __device__ __forceinline__ uint32_t max_down(uint32_t m) {  // of the wave's lan
 
 // A block's scale from the bits of its largest magnitude.  Powers of two: 448 = 1.75 * 2^8, so the exponent is the magnitude's less
 // 8, one more where its fraction is above 1.75.  They divide exactly, a transposed tile's codes are the tile's, and
-// the matrix instructions take them as they are.  `inv` is 1 / scale.
+// the matrix instructions take them as they are.
 struct Scale {
-    float value, inv;
-    uint8_t byte;
+    float value;              // the scale
+    uint8_t byte;             // as e8m0
+    float up, divisor, inv;   // for scales of any value: 1 or 2^64, that times the scale, and one divided by that
 };
 template <int SCALE>
 __device__ __forceinline__ Scale scale_of(uint32_t amax) {
@@ -79,27 +80,26 @@ __device__ __forceinline__ Scale scale_of(uint32_t amax) {
         e = amax ? e : 127;
         s.byte = (uint8_t)e;
         s.value = __uint_as_float((uint32_t)e << 23);
-        s.inv = __uint_as_float((uint32_t)(254 - e) << 23);
     } else {
-        const float v = __uint_as_float(amax) / 448.0f;
-        s.value = amax ? (v < 0x1p-126f ? 0x1p-126f : v) : 1.0f;
-        s.inv = 1.0f / s.value;
-        s.byte = 0;
+        // Small blocks are scaled up by 2^64, so that no remainder leaves fp32's range.  amax / 448 correctly rounded is amax / 7 by its
+        // rounded reciprocal and one correction with the exact remainder, times a power of two.
+        s.up = amax < 0x21000000u ? 0x1p64f : 1.0f;  // amax below 2^-61
+        const float m = __uint_as_float(amax) * s.up, seventh = 1.0f / 7.0f, near = m * seventh;
+        const float v = __builtin_fmaf(__builtin_fmaf(-near, 7.0f, m), seventh, near) * 0x1p-6f;
+        const float least = 0x1p-126f * s.up;
+        s.divisor = amax ? (v < least ? least : v) : s.up;
+        s.value = s.divisor * (s.up == 1.0f ? 1.0f : 0x1p-64f);
+        s.inv = __builtin_amdgcn_rcpf(s.divisor);  // the quotient is corrected
     }
     return s;
 }
 
 // The quotient whose e4m3 rounding is that of x / scale exactly, for scales of any value: the rounded quotient could fall on the
 // middle between two codes where the true one lies beside it, so a quotient that is not exact gets its last bit set after rounding towards zero (a
-// middle has that bit clear).  The remainder decides both; scaled up by 2^64 where it could leave fp32's range.
-__device__ __forceinline__ float quotient(float x, const Scale &s, bool tiny) {
-    float d = s.value, inv = s.inv;
-    if (tiny) {
-        const float up = d < 0x1p-60f ? 0x1p64f : 1.0f, down = d < 0x1p-60f ? 0x1p-64f : 1.0f;
-        x *= up;
-        d *= up;
-        inv *= down;
-    }
+// middle has that bit clear).  The remainder decides both.
+__device__ __forceinline__ float quotient(float x, const Scale &s) {
+    const float d = s.divisor, inv = s.inv;
+    x *= s.up;
     float q = x * inv;
     q = __builtin_fmaf(__builtin_fmaf(-q, d, x), inv, q);
     const float rest = __builtin_fmaf(-q, d, x);
@@ -123,7 +123,7 @@ __device__ __forceinline__ s16x2 encode_pair(s16x2 word, uint32_t pair, float sc
 }
 // The codes of eight elements, given as words of them.
 template <int TYPE, int SCALE>
-__device__ __forceinline__ u32x2 encode8(const uint32_t *w, const Scale &s, bool tiny) {
+__device__ __forceinline__ u32x2 encode8(const uint32_t *w, const Scale &s) {
     u32x2 codes;
 #pragma unroll
     for (int i = 0; i < 2; ++i) {
@@ -143,19 +143,15 @@ __device__ __forceinline__ u32x2 encode8(const uint32_t *w, const Scale &s, bool
             for (int j = 0; j < 4; ++j) {
                 const int e = 4 * i + j;
                 if constexpr (TYPE == CNR_FLOAT_F32)
-                    q[j] = quotient(__uint_as_float(w[e]), s, tiny);
+                    q[j] = quotient(__uint_as_float(w[e]), s);
                 else
-                    q[j] = quotient(Element<TYPE>::wide(__builtin_bit_cast(typename Element<TYPE>::type, (uint16_t)(w[e / 2] >> (16 * (e % 2))))), s, tiny);
+                    q[j] = quotient(Element<TYPE>::wide(__builtin_bit_cast(typename Element<TYPE>::type, (uint16_t)(w[e / 2] >> (16 * (e % 2))))), s);
             }
             const int r = __builtin_amdgcn_cvt_pk_fp8_f32(q[0], q[1], 0, false);
             codes[i] = (uint32_t)__builtin_amdgcn_cvt_pk_fp8_f32(q[2], q[3], r, true);
         }
     }
     return codes;
-}
-template <int SCALE>
-__device__ __forceinline__ bool any_tiny(const Scale &s) {
-    return SCALE == CNR_SCALE_F32 && __any(s.value < 0x1p-60f);
 }
 template <int SCALE>
 __device__ __forceinline__ void store_scale(void *to, uint64_t at, const Scale &s) {
@@ -242,14 +238,13 @@ __global__ void __launch_bounds__(kBlock) quantize_kernel(const QuantizeArgs a) 
 #pragma unroll
         for (int i = 0; i < kWavesPerBlock; ++i) all = M::larger(all, largest[i][0]);
         const Scale s = scale_of<SCALE>(M::as_float(M::largest(all)));
-        const bool tiny = any_tiny<SCALE>(s);
         if (t == 0) {
             if (a.codes) store_scale<SCALE>(a.scale, tile_col * a.scale_stride + tile_row, s);
             if (BOTH) store_scale<SCALE>(a.scale_t, tile_row * a.scale_stride_t + tile_col, s);
         }
         u32x2 codes[kPer];
 #pragma unroll
-        for (int r = 0; r < kPer; ++r) codes[r] = encode8<TYPE, SCALE>(w[r], s, tiny);
+        for (int r = 0; r < kPer; ++r) codes[r] = encode8<TYPE, SCALE>(w[r], s);
         if (a.codes) {
 #pragma unroll
             for (int r = 0; r < kPer; ++r)
@@ -281,9 +276,8 @@ __global__ void __launch_bounds__(kBlock) quantize_kernel(const QuantizeArgs a) 
 #pragma unroll
                 for (int i = 1; i < kWords; ++i) m = M::larger(m, mag[r][i]);
                 const Scale s = scale_of<SCALE>(M::as_float(M::largest(max_across<M>(m))));
-                const bool tiny = any_tiny<SCALE>(s);
                 if (r0 + r < a.n_rows) {
-                    *reinterpret_cast<u32x2 *>(a.codes + (uint64_t)(r0 + r) * a.row_bytes + c0) = encode8<TYPE, SCALE>(w[r], s, tiny);
+                    *reinterpret_cast<u32x2 *>(a.codes + (uint64_t)(r0 + r) * a.row_bytes + c0) = encode8<TYPE, SCALE>(w[r], s);
                     if (t % kAcross == 0) store_scale<SCALE>(a.scale, tile_col * a.scale_stride + r0 + r, s);
                 }
             }
@@ -311,7 +305,7 @@ __global__ void __launch_bounds__(kBlock) quantize_kernel(const QuantizeArgs a) 
                         column[i] = __builtin_amdgcn_perm(w[2 * i + 1][c / 2], w[2 * i][c / 2], c % 2 ? 0x07060302u : 0x05040100u);
                 }
                 *reinterpret_cast<u32x2 *>(turned + (t % kAcross * kPer + c) * kPitch + t / kAcross * kPer) =
-                    encode8<TYPE, SCALE>(column, s, any_tiny<SCALE>(s));
+                    encode8<TYPE, SCALE>(column, s);
                 if (t < kAcross && c0 + c < a.dim) store_scale<SCALE>(a.scale_t, tile_row * a.scale_stride_t + c0 + c, s);
             }
         }

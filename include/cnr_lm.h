@@ -86,13 +86,13 @@ cnr_status cnr_block_product(cnr_ctx *ctx, const uint8_t *a_codes, const void *a
  * 0 <= t < vocab: bit t of seen[slot] is set and, for tokens that the model wrote (prompt 0, counts not NULL),
  * counts[slot][t] goes up by one, where slot = slots[i] (i when slots is NULL).  Other tokens (padding) are skipped and counted as
  * cnr_mark_touched counts look-ups outside the table; sequences whose slot is not below n_slots are skipped
- * and raise CNR_FLAG_ROW_ID.
+ * and raise CNR_FLAG_ROW_ID if they have tokens.
  *   seen      uint32 [n_slots][cnr_bitmap_words(vocab)], laid out as a tracking bitmap; 4-byte aligned
  *   counts    uint32 [n_slots][vocab], or NULL: no counts are kept
  *   tokens    int32 or int64 [n_tokens] as `type` says
  *   offsets   uint64 [n + 1], ascending: sequence i has tokens [offsets[i], offsets[i + 1]), as far as they
  *             lie below n_tokens; NULL: n_tokens == n, one token each (a decoding step)
- *   slots     int32 [n] or NULL; sequences may share a slot
+ *   slots     int32 [n] or NULL; sequences may share a slot, which then has the tokens of all
  *   prompt    not 0: the tokens are seen but not counted
  *   restart   not 0: the slots of the call, their counts too, are emptied first */
 cnr_status cnr_count_tokens(cnr_ctx *ctx, uint32_t *seen, uint32_t *counts, uint64_t n_slots, uint64_t vocab,

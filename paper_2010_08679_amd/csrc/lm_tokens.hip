@@ -75,6 +75,130 @@ __global__ void __launch_bounds__(kBlock) count_kernel(const CountArgs a) {
     if (a.counts) atomicAdd(a.counts + slot * a.vocab + (uint64_t)token, 1u);
 }
 
+// ---- counts of prompts ------------------------------------------------------------------------------------------
+
+// A workgroup for each slice of the vocabulary of each sequence: it counts the sequence's tokens of its slice in LDS.  A sequence that
+// begins has its slice of the state written whole, without its old contents or atomics in memory, which is bound by the stores; to one that goes on the
+// counters that are not 0 are added.  The sequence's tokens are read once for each slice, from L2 but for the first.
+// 64 prompts of up to 8192 tokens, 131072 in the vocabulary: 11.0 us, of which the state's 34 MB take 7 at the rate of a copy (with an
+// atomic in memory for each token after the state is emptied 21.5).
+constexpr uint32_t kSlice = 16384;   // tokens: 64 KiB of counters, so that a CU holds two workgroups (16384 with 1024 threads 13.4 us, 8192 with 512 12.5)
+constexpr uint32_t kCounting = 512;  // threads
+constexpr uint32_t kAtOnce = 8;      // tokens that a thread loads before it counts them
+// Which kernels a call takes depends on its average number of tokens a sequence:
+constexpr uint64_t kAddFrom = 8192;       // from here on tokens are added slice by slice: 8192 x 8 9.2 us, by count_kernel 9.0; 131072 x 1 10.8 and 91; 2048 x 1 7.8 and 4.4
+constexpr uint64_t kBeginUpTo = 65536;    // up to here a state that begins is written whole: 65536 x 1 17 us, emptied and added to 17; 131072 x 1 27 and 17; 32768 x 1 11 and 12
+constexpr uint64_t kPart = 8192;          // tokens of a sequence's part where they are added
+
+// Tokens of sequence i.
+struct Range {
+    uint64_t lo, hi;
+};
+__device__ __forceinline__ Range tokens_of(const CountArgs &a, uint64_t i) {
+    Range r = {i, i + 1};
+    if (a.offsets) r = {a.offsets[i], a.offsets[i + 1]};
+    if (r.hi > a.n_tokens) r.hi = a.n_tokens;
+    return r;
+}
+
+// Enters tokens [r.lo, r.hi) that lie in the slice from `begin`; returns how many of the thread's lie outside the vocabulary.
+template <typename Index>
+__device__ __forceinline__ uint32_t count_range(const CountArgs &a, uint32_t *counters, Range r, uint32_t begin) {
+    const Index *tokens = reinterpret_cast<const Index *>(a.tokens);
+    uint32_t bad = 0;
+    for (uint64_t p = r.lo + tid_x(); p < r.hi; p += kAtOnce * kCounting) {
+        int64_t token[kAtOnce];
+#pragma unroll
+        for (uint32_t i = 0; i < kAtOnce; ++i) {
+            const uint64_t at = p + i * kCounting;
+            token[i] = (int64_t)tokens[at < r.hi ? at : p];
+        }
+#pragma unroll
+        for (uint32_t i = 0; i < kAtOnce; ++i) {
+            if (p + i * kCounting >= r.hi) continue;
+            if ((uint64_t)token[i] >= a.vocab)  // negative ones too
+                ++bad;
+            else if ((uint32_t)token[i] - begin < kSlice)
+                atomicAdd(counters + ((uint32_t)token[i] - begin), 1u);
+        }
+    }
+    return bad;
+}
+
+// Bits of `v` of eight lanes side by side, in each of them.
+__device__ __forceinline__ uint32_t or_of_eight(uint32_t v) {
+    v |= (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, 0xb1, 0xf, 0xf, true);   // quads' lanes 1 0 3 2
+    v |= (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, 0x4e, 0xf, 0xf, true);   // quads' lanes 2 3 0 1
+    v |= (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, 0x141, 0xf, 0xf, true);  // eights mirrored
+    return v;
+}
+
+// grid.x: slices, grid.y: sequences, grid.z: parts of a sequence that goes on.
+template <typename Index, bool BEGIN>
+__global__ void __launch_bounds__(kCounting) slice_kernel(const CountArgs a, bool prompt, uint32_t parts) {
+    __shared__ uint32_t counters[kSlice];
+    __shared__ uint32_t before, after;  // sequences of the same slot on either side of this one
+    const uint32_t t = tid_x(), begin = wg_x() * kSlice, vocab = (uint32_t)a.vocab;
+    for (uint64_t i = wg_y(); i < a.n; i += 32768) {
+        const uint64_t slot = slot_of(a.slots, a.n_slots, i);
+        Range own = tokens_of(a, i);
+        if (!BEGIN && own.lo < own.hi) {
+            const uint64_t part = (own.hi - own.lo + parts - 1) / parts;
+            own.lo += part * __builtin_amdgcn_workgroup_id_z();
+            own.hi = own.hi < own.lo + part ? own.hi : own.lo + part;
+        }
+        if (slot == a.n_slots || (!BEGIN && own.lo >= own.hi)) {
+            if (t == 0 && begin == 0 && own.lo < own.hi) raise_flag(a.err, CNR_FLAG_ROW_ID);
+            continue;
+        }
+        if (BEGIN && t == 0) before = after = 0;
+        for (uint32_t at = t * 4; at < kSlice; at += kCounting * 4) *reinterpret_cast<u32x4 *>(counters + at) = u32x4{0, 0, 0, 0};
+        __syncthreads();
+        bool first = true, alone = true;
+        if constexpr (BEGIN) {
+            if (a.slots)
+                for (uint64_t j = t; j < a.n; j += kCounting)
+                    if (j != i && slot_of(a.slots, a.n_slots, j) == slot) atomicAdd(j < i ? &before : &after, 1u);
+            __syncthreads();
+            first = before == 0, alone = after == 0;
+        }
+        if (first) {  // the slot's first sequence enters those that share it too
+            uint32_t bad = count_range<Index>(a, counters, own, begin);
+            if (!alone)
+                for (uint64_t j = i + 1; j < a.n; ++j)
+                    if (slot_of(a.slots, a.n_slots, j) == slot) bad += count_range<Index>(a, counters, tokens_of(a, j), begin);
+            if (begin == 0 && bad) atomicAdd(&a.err->n_bad_indices, (unsigned long long)bad);
+            __syncthreads();
+            uint32_t *counts = a.counts ? a.counts + slot * a.vocab + begin : nullptr, *seen = a.seen + slot * a.words + begin / 32;
+            const uint32_t left = vocab - begin < kSlice ? vocab - begin : kSlice;
+            for (uint32_t at = t * 4; at < kSlice; at += kCounting * 4) {
+                const u32x4 c = *reinterpret_cast<const u32x4 *>(counters + at);
+                const uint32_t bits = (c[0] != 0) | (uint32_t)(c[1] != 0) << 1 | (uint32_t)(c[2] != 0) << 2 | (uint32_t)(c[3] != 0) << 3;
+                const uint32_t word = or_of_eight(bits << (t % 8 * 4));
+                if constexpr (BEGIN) {
+                    if (t % 8 == 0 && at < left) seen[at / 32] = word;
+                    const u32x4 kept = prompt ? u32x4{0, 0, 0, 0} : c;
+                    if (!counts) continue;
+                    if (at + 4 <= left) {
+                        store16(counts + at, kept);
+                    } else {
+#pragma unroll
+                        for (uint32_t e = 0; e < 4; ++e)
+                            if (at + e < left) counts[at + e] = kept[e];
+                    }
+                } else {
+                    if (t % 8 == 0 && word && (seen[at / 32] & word) != word) atomicOr(seen + at / 32, word);
+                    if (!counts || prompt) continue;
+#pragma unroll
+                    for (uint32_t e = 0; e < 4; ++e)
+                        if (c[e]) atomicAdd(counts + at + e, c[e]);
+                }
+            }
+        }
+        __syncthreads();
+    }
+}
+
 // ---- logits -----------------------------------------------------------------------------------------------------
 
 // Bound by memory: a logit is read and written once, a bit of each bitmap beside it.  A thread holds kSegments times 16 bytes of a
@@ -305,19 +429,33 @@ cnr_status cnr_count_tokens(cnr_ctx *ctx, uint32_t *seen, uint32_t *counts, uint
     a.n = n;
     a.err = ctx->dev_err;
     hipStream_t s = as_stream(stream);
-    if (restart && vocab && n_slots) {
+    const bool wide = type == CNR_IDX_I64;
+    if (vocab == 0 || n_slots == 0) restart = 0;  // no state
+    const uint64_t average = n_tokens / n;
+    const unsigned slices = (unsigned)cnr_ceil_div(vocab, kSlice), rows = (unsigned)(n < 32768 ? n : 32768);
+    if (restart && average <= kBeginUpTo) {
+        wide ? slice_kernel<int64_t, true><<<dim3(slices, rows), kCounting, 0, s>>>(a, prompt != 0, 1)
+             : slice_kernel<int32_t, true><<<dim3(slices, rows), kCounting, 0, s>>>(a, prompt != 0, 1);
+        return cnr_launch_status(ctx);
+    }
+    if (restart) {
         const uint32_t shares = (uint32_t)cnr_ceil_div(counts ? vocab : a.words, 16 * kBlock);
-        hipLaunchKernelGGL(restart_kernel, dim3(shares, (unsigned)(n < 32768 ? n : 32768)), dim3(kBlock), 0, s, a, shares);
+        hipLaunchKernelGGL(restart_kernel, dim3(shares, rows), dim3(kBlock), 0, s, a, shares);
         st = cnr_launch_status(ctx);
         if (st != CNR_OK) return st;
     }
     if (n_tokens == 0) return CNR_OK;
+    if (vocab && n_slots && average >= kAddFrom) {
+        const uint64_t wanted = cnr_ceil_div(average, kPart);
+        const unsigned parts = (unsigned)(wanted < 32768 ? wanted : 32768);
+        const dim3 grid(slices, rows, parts);
+        wide ? slice_kernel<int64_t, false><<<grid, kCounting, 0, s>>>(a, prompt != 0, parts)
+             : slice_kernel<int32_t, false><<<grid, kCounting, 0, s>>>(a, prompt != 0, parts);
+        return cnr_launch_status(ctx);
+    }
     if (prompt) a.counts = nullptr;
     const unsigned grid = (unsigned)cnr_ceil_div(n_tokens, kBlock);
-    if (type == CNR_IDX_I64)
-        hipLaunchKernelGGL((count_kernel<int64_t>), dim3(grid), dim3(kBlock), 0, s, a);
-    else
-        hipLaunchKernelGGL((count_kernel<int32_t>), dim3(grid), dim3(kBlock), 0, s, a);
+    wide ? count_kernel<int64_t><<<grid, kBlock, 0, s>>>(a) : count_kernel<int32_t><<<grid, kBlock, 0, s>>>(a);
     return cnr_launch_status(ctx);
 }
 

@@ -42,11 +42,13 @@ def quantize_blocks(ctx, x: torch.Tensor, out: BlockMatrix | None = None, out_t:
     if out is None and out_t is None:
         out = BlockMatrix.empty(*x.shape, device=x.device)
     like = out if out is not None else out_t
-    for m, shape in ((out, tuple(x.shape)), (out_t, tuple(x.shape)[::-1])):
-        if m is not None and ((m.n_rows, m.dim) != shape or m.kind != like.kind or m.scale_type != like.scale_type):
-            raise ValueError("a blocked matrix of another size, kind or scale type")
-    L.cnr_quantize_blocks(ctx, x, like.kind, like.scale_type, *((out.codes, out.scale) if out is not None else (None, None)),
-                          *((out_t.codes, out_t.scale) if out_t is not None else (None, None)), stream)
+    n_rows, dim = x.shape
+    if ((out is not None and (out.n_rows != n_rows or out.dim != dim))
+            or (out_t is not None and (out_t.n_rows != dim or out_t.dim != n_rows or out_t.kind != like.kind or out_t.scale.dtype != like.scale.dtype))):
+        raise ValueError("a blocked matrix of another size, kind or scale type")
+    codes, scale = (out.codes, out.scale) if out is not None else (None, None)
+    codes_t, scale_t = (out_t.codes, out_t.scale) if out_t is not None else (None, None)
+    L.cnr_quantize_blocks(ctx, x, like.kind, like.scale_type, codes, scale, codes_t, scale_t, stream)
     return out
 
 
@@ -65,7 +67,7 @@ def block_product(ctx, a: BlockMatrix, b: BlockMatrix, out: torch.Tensor | None 
         if accumulate:
             raise ValueError("nothing to add to")
         out = torch.empty(a.n_rows, b.n_rows, dtype=torch.bfloat16, device=a.codes.device)
-    elif tuple(out.shape) != (a.n_rows, b.n_rows):
+    elif out.shape != (a.n_rows, b.n_rows):
         raise ValueError("out must be %d x %d" % (a.n_rows, b.n_rows))
     L.cnr_block_product(ctx, a.codes, a.scale, a.kind, a.n_rows, b.codes, b.scale, b.kind, b.n_rows, a.dim, out, accumulate, workspace, stream)
     return out

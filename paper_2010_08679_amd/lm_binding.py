@@ -80,20 +80,20 @@ def cnr_block_scale_count(n_rows: int, dim: int, kind: int) -> int:
 
 
 def _rows(t, name: str):
-    """(address, elements from one row to the next) of a matrix on the GPU whose rows are contiguous."""
+    """(address, rows, columns, elements from one row to the next) of a matrix on the GPU whose rows are contiguous."""
     if not isinstance(t, torch.Tensor) or not t.is_cuda:
         raise TypeError("%s must be a tensor on the GPU" % name)
     if t.dim() != 2:
         raise ValueError("%s must be a matrix" % name)
     rows, cols = t.shape
     step, one = t.stride()
-    if cols > 1 and one != 1:
+    if one != 1 and cols > 1:
         raise ValueError("the rows of %s must be contiguous" % name)
     if rows <= 1:
         step = cols
     elif step < cols:
         raise ValueError("the rows of %s overlap" % name)
-    return t.data_ptr(), step
+    return t.data_ptr(), rows, cols, step
 
 
 def _kind(table, t, name: str, names: str) -> int:
@@ -116,21 +116,22 @@ def _listed(t, n: int, dtype, name: str) -> int:
 
 def _blocked(codes, scale, n_rows: int, dim: int, kind: int, scale_type: int, name: str):
     """Addresses of a blocked matrix's two buffers."""
-    if kind not in (CNR_BLOCK_ROW, CNR_BLOCK_TILE):
+    across, stride = (dim + 127) // CNR_BLOCK, (n_rows + 127) // CNR_BLOCK
+    if kind == CNR_BLOCK_ROW:
+        stride *= CNR_BLOCK
+    elif kind != CNR_BLOCK_TILE:
         raise ValueError("the kind of %s must be CNR_BLOCK_ROW or CNR_BLOCK_TILE" % name)
-    across, down = -(-dim // CNR_BLOCK), -(-n_rows // CNR_BLOCK)
-    return (_listed(codes, n_rows * across * CNR_BLOCK, U8, name + "'s codes"),
-            _listed(scale, across * (down if kind == CNR_BLOCK_TILE else down * CNR_BLOCK), U8 if scale_type == CNR_SCALE_E8M0 else F32,
-                    name + "'s scale"))
+    if codes is None or scale is None or codes.numel() < n_rows * across * CNR_BLOCK or scale.numel() < across * stride:
+        raise ValueError("codes or scale of %s missing or shorter than its size" % name)
+    return B._dev(codes, U8, "the codes of " + name), B._dev(scale, F32 if scale_type else U8, "the scale of " + name)
 
 
 def cnr_quantize_blocks(ctx, x, kind: int, scale_type: int, codes, scale, codes_t=None, scale_t=None, stream=None) -> None:
     """``x``: a matrix of float32, bfloat16 or float16."""
-    at, stride = _rows(x, "x")
-    n_rows, dim = x.shape
-    direct = _blocked(codes, scale, n_rows, dim, kind, scale_type, "the quantized x") if codes is not None else (0, 0)
-    turned = _blocked(codes_t, scale_t, dim, n_rows, kind, scale_type, "x's transpose") if codes_t is not None else (0, 0)
-    _check(load().cnr_quantize_blocks(ctx, at, _float(x, "x"), n_rows, dim, stride, kind, scale_type, *direct, *turned, _stream(stream)),
+    at, n_rows, dim, stride = _rows(x, "x")
+    direct = _blocked(codes, scale, n_rows, dim, kind, scale_type, "the quantized x") if codes is not None or scale is not None else (0, 0)
+    turned = _blocked(codes_t, scale_t, dim, n_rows, kind, scale_type, "x's transpose") if codes_t is not None or scale_t is not None else (0, 0)
+    _check((_lib or load()).cnr_quantize_blocks(ctx, at, _float(x, "x"), n_rows, dim, stride, kind, scale_type, *direct, *turned, _stream(stream)),
            "cnr_quantize_blocks")
 
 
@@ -144,12 +145,12 @@ def cnr_block_product(ctx, a_codes, a_scale, a_kind: int, m: int, b_codes, b_sca
     scale_type = _kind(_SCALES, a_scale, "a_scale", "uint8 or float32")
     a = _blocked(a_codes, a_scale, m, k, a_kind, scale_type, "A")
     b = _blocked(b_codes, b_scale, n, k, b_kind, scale_type, "B")
-    to, stride = _rows(out, "out")
-    if out.shape[0] < m or out.shape[1] < n:
+    to, rows, columns, stride = _rows(out, "out")
+    if rows < m or columns < n:
         raise ValueError("out smaller than m x n")
     if workspace is not None and workspace.numel() * workspace.element_size() < cnr_block_product_workspace_bytes(ctx, m, n, k):
         raise ValueError("workspace smaller than cnr_block_product_workspace_bytes")
-    _check(load().cnr_block_product(ctx, *a, a_kind, m, *b, b_kind, n, k, scale_type, to, _float(out, "out"), stride,
+    _check((_lib or load()).cnr_block_product(ctx, *a, a_kind, m, *b, b_kind, n, k, scale_type, to, _float(out, "out"), stride,
                                     int(accumulate), B._dev(workspace, None, "workspace"), _stream(stream)), "cnr_block_product")
 
 
@@ -159,7 +160,7 @@ def cnr_count_tokens(ctx, seen, counts, n_slots: int, vocab: int, tokens, offset
     n = tokens.numel() if offsets is None else offsets.numel() - 1
     if n < 0:
         raise ValueError("offsets must hold at least one entry")
-    _check(load().cnr_count_tokens(ctx, _listed(seen, n_slots * ((vocab + 31) // 32), U32, "seen"), _listed(counts, n_slots * vocab, U32, "counts"),
+    _check((_lib or load()).cnr_count_tokens(ctx, _listed(seen, n_slots * ((vocab + 31) // 32), U32, "seen"), _listed(counts, n_slots * vocab, U32, "counts"),
                                    n_slots, vocab, B._dev(tokens, None, "tokens"), tokens.numel(),
                                    _kind(_INDICES, tokens, "tokens", "int32 or int64"), B._dev(offsets, U64, "offsets"),
                                    _listed(slots, n, U32, "slots"), n, int(prompt), int(restart), _stream(stream)), "cnr_count_tokens")
@@ -169,10 +170,9 @@ def cnr_adjust_logits(ctx, logits, out, seen=None, counts=None, n_slots: int = 0
                       bias_offsets=None, bias_tokens=None, bias_values=None, masks=None, n_masks: int = 0, mask_of=None,
                       stream=None) -> None:
     """``logits`` and ``out``: matrices of one type and size, or one and the same."""
-    at, stride = _rows(logits, "logits")
-    to, out_stride = _rows(out, "out")
-    n, vocab = logits.shape
-    if out.shape != logits.shape or out.dtype != logits.dtype:
+    at, n, vocab, stride = _rows(logits, "logits")
+    to, rows, columns, out_stride = _rows(out, "out")
+    if rows != n or columns != vocab or out.dtype != logits.dtype:
         raise ValueError("out must have the shape and type of logits")
     if to != at and to < at + ((n - 1) * stride + vocab) * logits.element_size() and at < to + ((n - 1) * out_stride + vocab) * out.element_size():
         raise ValueError("out overlaps logits without being the same")
@@ -187,5 +187,5 @@ def cnr_adjust_logits(ctx, logits, out, seen=None, counts=None, n_slots: int = 0
         _listed(repetition, n, F32, "repetition"), _listed(frequency, n, F32, "frequency"), _listed(presence, n, F32, "presence"),
         _listed(bias_offsets, n + 1, U64, "bias_offsets"), B._dev(bias_tokens, U32, "bias_tokens"), B._dev(bias_values, F32, "bias_values"), n_bias,
         _listed(masks, n_masks * words, U32, "masks"), n_masks, _listed(mask_of, n, U32, "mask_of"))
-    _check(load().cnr_adjust_logits(ctx, at, stride, to, out_stride, _float(logits, "logits"), n, vocab, ctypes.byref(given), _stream(stream)),
+    _check((_lib or load()).cnr_adjust_logits(ctx, at, stride, to, out_stride, _float(logits, "logits"), n, vocab, ctypes.byref(given), _stream(stream)),
            "cnr_adjust_logits")

@@ -711,15 +711,17 @@ Plan plan_of(const cnr_ctx *ctx, uint64_t m, uint64_t n, uint64_t k, bool plain,
     // The narrow kernel reads B once for each sixteen rows of A; a lone workgroup takes 0.115 us a block.
     Plan best = {kNarrow, 1};
     const float passes = (float)cnr_ceil_div(m, 16);
-    const float read = passes * (float)n * k / 4.2e6f, alone = 0.115f * blocks;
+    const float read = passes * (float)(n < 16 ? 16 : n) * k / 4.2e6f, alone = 0.115f * blocks;
     float least = 3.5f + (read > alone ? read : alone);
-    if (cnr_block_row_bytes(k) >= 1u << 24) return best;  // a tile's offsets are 32 bits: 256 rows of less than 2^24 codes
+    if (k == 0 || cnr_block_row_bytes(k) >= 1u << 24) return best;  // tiles have a block at least; a tile's offsets are 32 bits: 256 rows of less than 2^24 codes
     for (int i = 0; i < kNarrow; ++i) {
         if (i == 0 && !plain) continue;
         const Tiles &t = kTiles[i];
         const float tiles = (float)cnr_ceil_div(m, t.rows) * (float)cnr_ceil_div(n, t.columns), slow = plain ? 1.0f : 1.7f;
         for (uint32_t s = 1; s == 1 || (may_split && s <= kMaxSplits && blocks >= (float)(s * kMinBlocks)); s *= 2) {
-            const float groups = tiles * (float)s, round = units * (float)t.resident, rounds = floorf(groups / round);
+            const float groups = tiles * (float)s;
+            if (groups * (float)(i < 2 ? 512 : 256) >= 4.2e9f) continue;  // grids count threads in 32 bits
+            const float round = units * (float)t.resident, rounds = floorf(groups / round);
             const float rest = ceilf((groups - rounds * round) / units);  // workgroups on a unit in the last round
             float time = ceilf(blocks / (float)s) * slow * (rounds * t.block[t.resident - 1] + (rest > 0.0f ? t.block[(int)rest - 1] : 0.0f));
             time += 3.5f + 1.5f * (rounds + (rest > 0.0f ? 1.0f : 0.0f));
@@ -737,6 +739,17 @@ uint64_t partial_bytes(uint64_t m, uint64_t n, uint32_t splits) {
     return splits > 1 ? (uint64_t)splits * m * (cnr_ceil_div(n, 4) * 4) * sizeof(float) : 0;
 }
 
+constexpr uint64_t kNarrowRows = 1u << 19, kNarrowColumns = 1u << 27;
+
+template <bool FULL, int SCALE>
+void narrow_part(const ProductArgs &p, hipStream_t s) {
+    // Two fragments of B to a wave where that still gives every SIMD a wave: A's codes are read half as often (16 x 32000 x 4096 37 -> 30 us).
+    if (p.m > 1 && p.n >= 16384)
+        narrow<FULL, SCALE, 1, 2, 1>(p, s);
+    else
+        narrow<FULL, SCALE, 1, 1, 4>(p, s);
+}
+
 template <bool FULL, int SCALE>
 void launch(const ProductArgs &p, const Plan &plan, hipStream_t s) {
     if constexpr (!FULL && SCALE == CNR_SCALE_E8M0) {
@@ -748,11 +761,20 @@ void launch(const ProductArgs &p, const Plan &plan, hipStream_t s) {
         case 3: return tiled<FULL, SCALE, 2, 2, 2, 4, 2>(p, s);
         case 4: return tiled<FULL, SCALE, 2, 2, 2, 2, 4>(p, s);
     }
-    // Two fragments of B to a wave where that still gives every SIMD a wave: A's codes are read half as often (16 x 32000 x 4096 37 -> 30 us).
-    if (p.m > 1 && p.n >= 16384)
-        narrow<FULL, SCALE, 1, 2, 1>(p, s);
-    else
-        narrow<FULL, SCALE, 1, 1, 4>(p, s);
+    // A grid has fewer than 2^16 workgroups one below the other and 2^32 threads side by side: larger products go by parts, each from a whole tile's scale on.
+    for (uint64_t n0 = 0; n0 < p.n; n0 += kNarrowColumns) {
+        for (uint64_t m0 = 0; m0 < p.m; m0 += kNarrowRows) {
+            ProductArgs q = p;
+            q.m = (uint32_t)(p.m - m0 < kNarrowRows ? p.m - m0 : kNarrowRows);
+            q.n = (uint32_t)(p.n - n0 < kNarrowColumns ? p.n - n0 : kNarrowColumns);
+            q.a += m0 * p.row_bytes;
+            q.b += n0 * p.row_bytes;
+            q.a_scale = reinterpret_cast<const typename ScaleOf<SCALE>::type *>(p.a_scale) + (m0 >> p.a_shift);
+            q.b_scale = reinterpret_cast<const typename ScaleOf<SCALE>::type *>(p.b_scale) + (n0 >> p.b_shift);
+            q.out = reinterpret_cast<uint8_t *>(p.out) + (m0 * p.out_stride + n0) * cnr_float_bytes((cnr_float_type)p.out_type);
+            narrow_part<FULL, SCALE>(q, s);
+        }
+    }
 }
 
 }  // namespace
@@ -774,7 +796,7 @@ cnr_status cnr_block_product(cnr_ctx *ctx, const uint8_t *a_codes, const void *a
         return CNR_E_INVALID;
     if (m > CNR_LM_MAX_SIZE || n > CNR_LM_MAX_SIZE || k > CNR_LM_MAX_SIZE) return CNR_E_TOO_LARGE;
     if (m == 0 || n == 0 || (k == 0 && accumulate)) return CNR_OK;
-    // more outputs than a GPU holds; grids count threads in 32 bits
+    // more outputs or codes than a GPU holds
     if (cnr_ceil_div(m, 128) * cnr_ceil_div(n, 128) >= 1u << 24 || (m > 64 && k >= (1u << 24) - CNR_BLOCK && m > 1u << 19)) return CNR_E_TOO_LARGE;
     if (!out || (k && (!a_codes || !a_scale || !b_codes || !b_scale))) return CNR_E_INVALID;
     if (!cnr_aligned(a_codes, 16) || !cnr_aligned(a_scale, 16) || !cnr_aligned(b_codes, 16) || !cnr_aligned(b_scale, 16) ||
@@ -801,7 +823,6 @@ cnr_status cnr_block_product(cnr_ctx *ctx, const uint8_t *a_codes, const void *a
     p.accumulate = accumulate ? 1 : 0;
     const bool full = out_type == CNR_FLOAT_F32, powers = scale_type == CNR_SCALE_E8M0;
     const Plan plan = plan_of(ctx, m, n, k, powers && !full, workspace != nullptr);
-    if (plan.kernel == kNarrow && cnr_ceil_div(m, 16) > 65535) return CNR_E_TOO_LARGE;
     p.splits = plan.splits;
     p.partial = reinterpret_cast<float *>(workspace);
     p.partial_stride = cnr_ceil_div(n, 4) * 4;

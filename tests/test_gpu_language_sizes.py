@@ -84,6 +84,30 @@ def test_product_with_more_than_4_gib_of_codes(ctx, m, scale):
         assert torch.equal(out[:, i : i + rows], want[:, :rows]), i
 
 
+@pytest.mark.parametrize("scale", [P.CNR_SCALE_E8M0, P.CNR_SCALE_F32])
+@pytest.mark.parametrize("out", ["f32", "bf16"])
+@pytest.mark.parametrize("m,n", [(1_200_000, 10), (2_100_037, 1), (3, 1_500_011)])
+def test_product_of_a_table_with_a_few_rows_either_way(ctx, out, scale, m, n):
+    # more than 2^16 workgroups of 16 rows; in parts that end inside a tile
+    (a, av), (b, bv) = _whole(m, 100, P.CNR_BLOCK_TILE, scale, 1), _whole(n, 100, P.CNR_BLOCK_ROW, scale, 2)
+    got = torch.full((m, n + 1), 3.0, dtype=TYPES[out], device=DEV)
+    P.block_product(ctx, a, b, got[:, :n])
+    assert torch.equal(got[:, :n], (av @ bv.t()).float().to(TYPES[out])) and bool((got[:, n] == 3.0).all())
+
+
+def test_product_with_more_columns_than_a_grid_has_threads(ctx):
+    n = (1 << 28) + 77  # 34 GB of codes, of which one in 128 is in the matrix
+    a, av = _whole(1, 1, P.CNR_BLOCK_ROW, P.CNR_SCALE_E8M0, 1)
+    a.codes[0, 0], a.scale[0, 0] = 0x40, 128  # 2 * 2
+    b = P.BlockMatrix.empty(n, 1, P.CNR_BLOCK_TILE)
+    b.codes.zero_()
+    b.codes[:, 0] = (torch.arange(n, device=DEV) % 9 + 0x38).to(torch.uint8)  # 1, 1.125, ... 2
+    b.scale.copy_((torch.arange(b.scale.shape[1], device=DEV) % 3 + 126).to(torch.uint8))
+    out = P.block_product(ctx, a, b)
+    i = torch.arange(n, device=DEV)
+    assert torch.equal(out[0], (4 * (1 + (i % 9) / 8) * 2.0 ** (i // 128 % 3 - 1)).bfloat16())
+
+
 def test_product_with_more_than_4_gi_outputs(ctx):
     m, n, k = 66_000, 66_000, 130
     a, av = _whole(m, k, P.CNR_BLOCK_ROW, P.CNR_SCALE_E8M0, 1)

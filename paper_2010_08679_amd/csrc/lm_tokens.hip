@@ -85,9 +85,10 @@ __global__ void __launch_bounds__(kBlock) count_kernel(const CountArgs a) {
 constexpr uint32_t kSlice = 16384;   // tokens: 64 KiB of counters, so that a CU holds two workgroups (16384 with 1024 threads 13.4 us, 8192 with 512 12.5)
 constexpr uint32_t kCounting = 512;  // threads
 constexpr uint32_t kAtOnce = 8;      // tokens that a thread loads before it counts them
-// Which kernels a call takes depends on its average number of tokens a sequence:
+// Which kernels a call takes depends on its average number of tokens a sequence and on how many sequences there are:
 constexpr uint64_t kAddFrom = 8192;       // from here on tokens are added slice by slice: 8192 x 8 9.2 us, by count_kernel 9.0; 131072 x 1 10.8 and 91; 2048 x 1 7.8 and 4.4
 constexpr uint64_t kBeginUpTo = 65536;    // up to here a state that begins is written whole: 65536 x 1 17 us, emptied and added to 17; 131072 x 1 27 and 17; 32768 x 1 11 and 12
+constexpr uint64_t kLookedThrough = 4096; // sequences with slots up to which a state that begins is written whole: each workgroup looks through all slots for its own
 constexpr uint64_t kPart = 8192;          // tokens of a sequence's part where they are added
 
 // Tokens of sequence i.
@@ -433,7 +434,7 @@ cnr_status cnr_count_tokens(cnr_ctx *ctx, uint32_t *seen, uint32_t *counts, uint
     if (vocab == 0 || n_slots == 0) restart = 0;  // no state
     const uint64_t average = n_tokens / n;
     const unsigned slices = (unsigned)cnr_ceil_div(vocab, kSlice), rows = (unsigned)(n < 32768 ? n : 32768);
-    if (restart && average <= kBeginUpTo) {
+    if (restart && average <= kBeginUpTo && (!slots || n <= kLookedThrough)) {
         wide ? slice_kernel<int64_t, true><<<dim3(slices, rows), kCounting, 0, s>>>(a, prompt != 0, 1)
              : slice_kernel<int32_t, true><<<dim3(slices, rows), kCounting, 0, s>>>(a, prompt != 0, 1);
         return cnr_launch_status(ctx);

@@ -170,6 +170,23 @@ def test_count_at_every_length(ctx, index, vocab, lengths, prompt, restart):
         assert (n_bad, flags) == (2 * here, 0 if keeps.all() or lengths[-1] == 0 else P.CNR_FLAG_ROW_ID)  # a sequence without tokens needs no slot
 
 
+@pytest.mark.parametrize("n", [4096, 4097, 40_000])
+@pytest.mark.parametrize("prompt", [False, True])
+def test_count_of_many_sequences_that_begin(ctx, n, prompt):
+    g = np.random.default_rng(n)
+    n_slots, vocab = n // 2, 70
+    lengths = g.integers(0, 9, n)
+    offsets = np.concatenate([[0], np.cumsum(lengths)])
+    tokens, slots = g.integers(0, vocab, offsets[-1]), g.integers(0, n_slots, n).astype(np.int32)
+    start = g.integers(0, 3, (n_slots, vocab))
+    seen, counts = start > 0, start.astype(np.int64).copy()
+    ledger = P.TokenLedger(ctx, n_slots, vocab, torch.from_numpy(R.pack_bits(seen)).to(DEV), torch.from_numpy(counts.astype(np.int32)).to(DEV))
+    ledger.count(torch.from_numpy(tokens).to(DEV), torch.from_numpy(offsets).to(DEV), torch.from_numpy(slots).to(DEV), prompt=prompt, restart=True)
+    R.count(seen, counts, vocab, tokens, offsets, slots, prompt, True)
+    assert np.array_equal(ledger.counts.cpu().numpy(), counts) and np.array_equal(ledger.seen.cpu().numpy(), R.pack_bits(seen))
+    assert P.cnr_poll_errors(ctx) == (P.CNR_OK, 0, 0)
+
+
 @pytest.mark.parametrize("restart", [True, False])
 def test_count_of_slots_beyond_4_gib(ctx, restart):
     vocab, n_slots, n = 131_072, 9000, 40  # 4.7 GB of counts

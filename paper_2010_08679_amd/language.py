@@ -88,6 +88,7 @@ class BlockLinear:
         self._dy, self._dy_t = self._buffers(max_tokens, n_out), self._buffers(n_out, max_tokens)
         self._input_t = None
         self._sized = {}
+        self._spaces = []  # workspaces, the last one the largest; earlier ones stay, since captured graphs may hold them
 
     def _buffers(self, n_rows: int, dim: int):
         m = BlockMatrix.empty(n_rows, dim, L.CNR_BLOCK_ROW, self.scale_type, self.device)
@@ -106,9 +107,12 @@ class BlockLinear:
         if tokens not in self._sized:
             space = max(L.cnr_block_product_workspace_bytes(self.ctx, *s) for s in (
                 (tokens, self.n_out, self.n_in), (tokens, self.n_in, self.n_out), (self.n_out, self.n_in, tokens)))
+            had = self._spaces[-1].numel() if self._spaces else 0
+            if space > had:
+                self._spaces.append(torch.empty(max(space, 2 * had), dtype=torch.uint8, device=self.device))
             self._sized = {tokens: (self._of(self._x, tokens, self.n_in), self._of(self._x_t, self.n_in, tokens),
                                     self._of(self._dy, tokens, self.n_out), self._of(self._dy_t, self.n_out, tokens),
-                                    torch.empty(space, dtype=torch.uint8, device=self.device) if space else None)}
+                                    self._spaces[-1] if space else None)}
         return self._sized[tokens]
 
     def load(self, weight: torch.Tensor, stream=None) -> None:

@@ -480,3 +480,27 @@ def test_another_stream_and_a_graph_replayed(ctx):
         graph.replay()
         assert all(torch.equal(a, b) for a, b in zip(results(), want)), k
     assert P.cnr_poll_errors(ctx) == (P.CNR_OK, 0, 0)
+
+
+def test_a_layers_graph_outlives_calls_of_other_sizes(ctx):
+    # the workspace that a graph was captured with stays while the layer lives
+    g = torch.Generator(device=DEV).manual_seed(2)
+    n_in, n_out = 16384, 1024
+    layer = P.BlockLinear(ctx, n_out, n_in, 300)
+    layer.load(torch.randn(n_out, n_in, generator=g, device=DEV))
+    x = torch.randn(64, n_in, generator=g, device=DEV).bfloat16()
+    y = torch.empty(64, n_out, dtype=torch.bfloat16, device=DEV)
+    assert P.block_workspace(ctx, 64, n_out, n_in) is not None
+    want = layer.forward(x, training=False)
+    space = layer._for(64)[4]
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        layer.forward(x, y, training=False)
+    for tokens in (300, 1, 130, 300):
+        layer.forward(torch.randn(tokens, n_in, generator=g, device=DEV).bfloat16(), training=False)
+        assert any(s is space for s in layer._spaces)
+        other = torch.zeros(space.numel(), dtype=torch.uint8, device=DEV)  # takes the memory if it is free
+        y.zero_()
+        graph.replay()
+        torch.cuda.synchronize()
+        assert torch.equal(y, want) and not bool(other.any())

@@ -83,6 +83,7 @@ class cnr_table_job(ctypes.Structure):
 
 _lock = threading.Lock()
 _lib = None
+_extension = None  # csrc/cnr_marshal.cpp, where it is there
 _packed_calls = {}  # the *_batch functions as they take the bytes of a job array
 
 
@@ -160,7 +161,7 @@ def load() -> ctypes.CDLL:
 def _bind_marshal() -> None:
     """From here on the extension checks the tensors of a call and packs job arrays (see csrc/cnr_marshal.cpp).  It is host code, compiled
     against this torch and this interpreter: where it is missing and cannot be built, the general checks stay."""
-    global _dev, _pack_fields, batch_jobs
+    global _dev, _pack_fields, batch_jobs, _extension
     try:
         spec = importlib.util.spec_from_file_location(__package__ + "._marshal", _build.build_marshal(force=False))
         m = importlib.util.module_from_spec(spec)
@@ -169,7 +170,7 @@ def _bind_marshal() -> None:
         warnings.warn("calls are a few microseconds slower, their tensors are checked in Python: %s" % e, RuntimeWarning)
         return
     m.set_general(_general_dev)
-    _dev, _pack_fields, batch_jobs = m.address, m.pack_jobs, m.batch_jobs
+    _dev, _pack_fields, batch_jobs, _extension = m.address, m.pack_jobs, m.batch_jobs, m
 
 
 def status_str(status: int) -> str:

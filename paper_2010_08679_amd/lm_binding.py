@@ -1,5 +1,8 @@
 """ctypes binding of ``include/cnr_lm.h``: argument marshalling only, as in :mod:`binding`.
 
+The calls themselves go through the extension of :mod:`binding` where everything is in order; where it is missing, or
+leaves a call to the general way below, the checks are made and refused here.
+
 Matrices are two-dimensional tensors whose rows may lie further apart than they are long; the sizes, the strides and the
 element type that the C side takes are read off the tensors, everything else has the name and the
 order of the C declaration.
@@ -44,9 +47,16 @@ class cnr_adjustments(ctypes.Structure):
 _lib = None
 
 
+def _no_call(*args):
+    """In place of the extension's calls: the general way has to look."""
+
+
+_quantize = _product = _count = _adjust = _no_call
+
+
 def load() -> ctypes.CDLL:
     """The library of :func:`binding.load`, with this header's functions bound."""
-    global _lib
+    global _lib, _quantize, _product, _count, _adjust
     if _lib is None:
         lib = B.load()
         vp, u64, i32, sz = ctypes.c_void_p, ctypes.c_uint64, ctypes.c_int, ctypes.c_size_t
@@ -63,6 +73,11 @@ def load() -> ctypes.CDLL:
         for name, (res, args) in sig.items():
             fn = getattr(lib, name)
             fn.restype, fn.argtypes = res, args
+        if B._extension is not None:
+            m = B._extension
+            m.set_lm(*(ctypes.cast(getattr(lib, name), vp).value for name in (
+                "cnr_quantize_blocks", "cnr_block_product_workspace_bytes", "cnr_block_product", "cnr_count_tokens", "cnr_adjust_logits")), _stream)
+            _quantize, _product, _count, _adjust = m.quantize_blocks, m.block_product, m.count_tokens, m.adjust_logits
         _lib = lib
     return _lib
 
@@ -128,6 +143,9 @@ def _blocked(codes, scale, n_rows: int, dim: int, kind: int, scale_type: int, na
 
 def cnr_quantize_blocks(ctx, x, kind: int, scale_type: int, codes, scale, codes_t=None, scale_t=None, stream=None) -> None:
     """``x``: a matrix of float32, bfloat16 or float16."""
+    status = _quantize(ctx, x, kind, scale_type, codes, scale, codes_t, scale_t, stream)
+    if status is not None:
+        return _check(status, "cnr_quantize_blocks")
     at, n_rows, dim, stride = _rows(x, "x")
     direct = _blocked(codes, scale, n_rows, dim, kind, scale_type, "the quantized x") if codes is not None or scale is not None else (0, 0)
     turned = _blocked(codes_t, scale_t, dim, n_rows, kind, scale_type, "x's transpose") if codes_t is not None or scale_t is not None else (0, 0)
@@ -142,6 +160,9 @@ def cnr_block_product_workspace_bytes(ctx, m: int, n: int, k: int) -> int:
 def cnr_block_product(ctx, a_codes, a_scale, a_kind: int, m: int, b_codes, b_scale, b_kind: int, n: int, k: int, out,
                       accumulate: bool = False, workspace=None, stream=None) -> None:
     """``out``: a matrix of at least m x n, float32, bfloat16 or float16."""
+    status = _product(ctx, a_codes, a_scale, a_kind, m, b_codes, b_scale, b_kind, n, k, out, accumulate, workspace, stream)
+    if status is not None:
+        return _check(status, "cnr_block_product")
     scale_type = _kind(_SCALES, a_scale, "a_scale", "uint8 or float32")
     a = _blocked(a_codes, a_scale, m, k, a_kind, scale_type, "A")
     b = _blocked(b_codes, b_scale, n, k, b_kind, scale_type, "B")
@@ -157,6 +178,9 @@ def cnr_block_product(ctx, a_codes, a_scale, a_kind: int, m: int, b_codes, b_sca
 def cnr_count_tokens(ctx, seen, counts, n_slots: int, vocab: int, tokens, offsets=None, slots=None, prompt: bool = False,
                      restart: bool = False, stream=None) -> None:
     """The sequences are as many as ``offsets`` has entries, less one; without it, as there are tokens."""
+    status = _count(ctx, seen, counts, n_slots, vocab, tokens, offsets, slots, prompt, restart, stream)
+    if status is not None:
+        return _check(status, "cnr_count_tokens")
     n = tokens.numel() if offsets is None else offsets.numel() - 1
     if n < 0:
         raise ValueError("offsets must hold at least one entry")
@@ -170,6 +194,10 @@ def cnr_adjust_logits(ctx, logits, out, seen=None, counts=None, n_slots: int = 0
                       bias_offsets=None, bias_tokens=None, bias_values=None, masks=None, n_masks: int = 0, mask_of=None,
                       stream=None) -> None:
     """``logits`` and ``out``: matrices of one type and size, or one and the same."""
+    status = _adjust(ctx, logits, out, seen, counts, n_slots, slots, repetition, frequency, presence, bias_offsets, bias_tokens, bias_values, masks, n_masks,
+                     mask_of, stream)
+    if status is not None:
+        return _check(status, "cnr_adjust_logits")
     at, n, vocab, stride = _rows(logits, "logits")
     to, rows, columns, out_stride = _rows(out, "out")
     if rows != n or columns != vocab or out.dtype != logits.dtype:

@@ -5,6 +5,7 @@ import torch
 
 import paper_2010_08679_amd as P
 from oracle import blocks as R
+from paper_2010_08679_amd import lm_binding as L
 
 pytestmark = pytest.mark.gpu
 DEV = "cuda:0"
@@ -504,3 +505,112 @@ def test_a_layers_graph_outlives_calls_of_other_sizes(ctx):
         graph.replay()
         torch.cuda.synchronize()
         assert torch.equal(y, want) and not bool(other.any())
+
+
+# ---- the two ways of the binding ----------------------------------------------------------------------------------------
+
+WAYS = ["extension", "general"]
+
+
+@pytest.fixture(params=WAYS)
+def way(request, monkeypatch):
+    """The calls through the extension, and without it."""
+    L.load()
+    if request.param == "general":
+        for name in ("_quantize", "_product", "_count", "_adjust"):
+            monkeypatch.setattr(L, name, L._no_call)
+    else:
+        assert L._quantize is not L._no_call
+    return request.param
+
+
+def test_both_ways_take_the_same(ctx, way):
+    g = np.random.default_rng(1)
+    m, n, k = 5, 40, 200
+    held = torch.from_numpy(g.normal(0, 1, (m, k + 3))).float().to(DEV)
+    w = torch.from_numpy(g.normal(0, 1, (n, k))).to(torch.float16).to(DEV)
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    for stream in (None, side):
+        x, x_t, y = P.BlockMatrix.empty(m, k), P.BlockMatrix.empty(k, m), P.BlockMatrix.empty(n, k, P.CNR_BLOCK_TILE)
+        torch.cuda.synchronize()
+        P.quantize_blocks(ctx, held[:, :k], x, x_t, stream)
+        P.quantize_blocks(ctx, w, y, stream=stream)
+        out = torch.zeros(m, n + 1, device=DEV)[:, :n]
+        space = torch.empty(1 << 20, dtype=torch.uint8, device=DEV)
+        torch.cuda.synchronize()
+        P.block_product(ctx, x, y, out, workspace=space, stream=stream)
+        P.block_product(ctx, x, y, out, accumulate=True, stream=stream)
+        torch.cuda.synchronize()
+        a, b = (R.values(*R.quantize(_wide(v), kind, "e8m0"), kind) for v, kind in ((held[:, :k], "row"), (w, "tile")))
+        _check(_wide(out), 2 * a @ b.T, 2 * np.abs(a) @ np.abs(b).T, "f32", 2 * k)
+        assert np.array_equal(x_t.codes.cpu().numpy(), R.quantize(_wide(held[:, :k]).T, "row", "e8m0")[0])
+    for index in (torch.int32, torch.int64):
+        ledger, bits = P.TokenLedger(ctx, 4, n), P.TokenLedger(ctx, 4, n, torch.zeros(4, 2, dtype=torch.int32, device=DEV))
+        seen, counts = np.zeros((4, n), bool), np.zeros((4, n), np.int64)
+        tokens, offsets, slots = g.integers(0, n, 9), np.array([0, 3, 3, 9]), np.array([2, 0, 1], np.int32)
+        given = torch.from_numpy(tokens).to(index).to(DEV), torch.from_numpy(offsets).to(DEV), torch.from_numpy(slots).to(DEV)
+        for one in (ledger, bits):
+            one.count(*given, prompt=True, restart=True)
+            one.count(given[0][:4])
+        R.count(seen, counts, n, tokens, offsets, slots, True, True)
+        R.count(seen, counts, n, tokens[:4], np.arange(5), np.arange(4))
+        assert np.array_equal(ledger.counts.cpu().numpy(), counts) and np.array_equal(ledger.seen.cpu().numpy(), R.pack_bits(seen))
+        assert torch.equal(bits.seen, ledger.seen) and bits.counts is None
+    logits = torch.from_numpy(g.normal(0, 3, (3, n))).float().to(DEV)
+    p = [torch.from_numpy(g.random(3).astype(np.float32) + 0.5).to(DEV) for _ in range(3)]
+    allowed = g.random((2, n)) < 0.5
+    biases = [[(1, 2.0)], [], [(0, -1.0), (39, 3.0)]]
+    got = ledger.adjust(logits, torch.empty_like(logits), slots=given[2], repetition=p[0], frequency=p[1], presence=p[2],
+                        bias=(torch.tensor([0, 1, 1, 3], device=DEV), torch.tensor([1, 0, 39], dtype=torch.int32, device=DEV), torch.tensor([2.0, -1.0, 3.0], device=DEV)),
+                        masks=torch.from_numpy(R.pack_bits(allowed)).to(DEV), mask_of=torch.tensor([1, -1, 0], dtype=torch.int32, device=DEV))
+    want = R.adjust(_wide(logits), seen[slots], counts[slots], *(v.cpu().numpy() for v in p), biases, np.where(np.array([1, -1, 0])[:, None] < 0, True, allowed[[1, 0, 0]]))
+    _close(got, want, torch.float32, np.abs(_wide(logits)) * 2 + 40)
+    assert torch.equal(ledger.adjust(logits, torch.empty_like(logits)), logits)
+    assert P.cnr_poll_errors(ctx) == (P.CNR_OK, 0, 0)
+
+
+def test_both_ways_refuse_the_same(ctx, way):
+    x, out = torch.zeros(8, 200, device=DEV), P.BlockMatrix.empty(8, 200)
+    w, y = P.BlockMatrix.empty(6, 200, P.CNR_BLOCK_TILE, P.CNR_SCALE_F32), torch.zeros(8, 6, device=DEV)
+    for error, call in [
+            (TypeError, lambda: L.cnr_quantize_blocks(ctx, x.double(), 0, 0, out.codes, out.scale)),
+            (TypeError, lambda: L.cnr_quantize_blocks(ctx, x.cpu(), 0, 0, out.codes, out.scale)),
+            (ValueError, lambda: L.cnr_quantize_blocks(ctx, x[0], 0, 0, out.codes, out.scale)),
+            (ValueError, lambda: L.cnr_quantize_blocks(ctx, x.t(), 0, 0, out.codes, out.scale)),
+            (ValueError, lambda: L.cnr_quantize_blocks(ctx, x[:, :1].expand(8, 200), 0, 0, out.codes, out.scale)),
+            (ValueError, lambda: L.cnr_quantize_blocks(ctx, x[:1].expand(8, 200), 0, 0, out.codes, out.scale)),
+            (ValueError, lambda: L.cnr_quantize_blocks(ctx, x, 0, 0, out.codes[:7], out.scale)),
+            (ValueError, lambda: L.cnr_quantize_blocks(ctx, x, 0, 0, out.codes, None)),
+            (ValueError, lambda: L.cnr_quantize_blocks(ctx, x, 2, 0, out.codes, out.scale)),
+            (TypeError, lambda: L.cnr_quantize_blocks(ctx, x, 0, 1, out.codes, out.scale)),
+            (ValueError, lambda: L.cnr_quantize_blocks(ctx, x, 0, 0, None, None, out.codes, out.scale)),
+            (P.CnrError, lambda: L.cnr_quantize_blocks(ctx, x, 0, 0, None, None)),
+            (P.CnrError, lambda: L.cnr_quantize_blocks(None, x, 0, 0, out.codes, out.scale)),
+            (P.CnrError, lambda: L.cnr_quantize_blocks(ctx, x, 0, 0, torch.zeros(2049, dtype=torch.uint8, device=DEV)[1:], out.scale)),
+            (TypeError, lambda: P.block_product(ctx, out, w, y)),  # scales of two types
+            (ValueError, lambda: P.block_product(ctx, out, out, y)),
+            (ValueError, lambda: L.cnr_block_product(ctx, out.codes, out.scale, 0, 9, out.codes, out.scale, 0, 6, 200, y)),
+            (ValueError, lambda: L.cnr_block_product(ctx, out.codes, out.scale, 0, 8, out.codes, out.scale, 0, 7, 200, y)),
+            (ValueError, lambda: L.cnr_block_product(ctx, out.codes, out.scale, 0, 8, out.codes, out.scale, 0, 6, 257, y)),
+            (TypeError, lambda: L.cnr_block_product(ctx, out.codes, out.scale, 0, 8, out.codes, out.scale, 0, 6, 200, y.int())),
+            (TypeError, lambda: L.cnr_count_tokens(ctx, out.scale[:1], None, 1, 8, torch.zeros(1, dtype=torch.int64, device=DEV))),
+            (TypeError, lambda: P.TokenLedger(ctx, 2, 40).count(torch.zeros(2, dtype=torch.int16, device=DEV))),
+            (TypeError, lambda: P.TokenLedger(ctx, 2, 40).count(torch.zeros(2, dtype=torch.int64, device=DEV), torch.zeros(2, dtype=torch.int32, device=DEV))),
+            (ValueError, lambda: P.TokenLedger(ctx, 2, 40).count(torch.zeros(2, dtype=torch.int64, device=DEV), torch.zeros(0, dtype=torch.int64, device=DEV))),
+            (ValueError, lambda: P.TokenLedger(ctx, 2, 40).count(torch.zeros(2, dtype=torch.int64, device=DEV), slots=torch.zeros(1, dtype=torch.int32, device=DEV))),
+            (ValueError, lambda: P.TokenLedger(ctx, 2, 40, counts=torch.zeros(79, dtype=torch.int32, device=DEV)).count(torch.zeros(2, dtype=torch.int64, device=DEV))),
+            (ValueError, lambda: L.cnr_adjust_logits(ctx, x, x[:, 1:])),
+            (ValueError, lambda: L.cnr_adjust_logits(ctx, x[:4], x[3:7])),
+            (ValueError, lambda: L.cnr_adjust_logits(ctx, x, x.half())),
+            (ValueError, lambda: L.cnr_adjust_logits(ctx, x, x, repetition=torch.ones(7, device=DEV))),
+            (TypeError, lambda: L.cnr_adjust_logits(ctx, x, x, repetition=torch.ones(8, device=DEV, dtype=torch.float64))),
+            (ValueError, lambda: L.cnr_adjust_logits(ctx, x, x, bias_offsets=torch.zeros(9, dtype=torch.int64, device=DEV))),
+            (ValueError, lambda: L.cnr_adjust_logits(ctx, x, x, bias_offsets=torch.zeros(8, dtype=torch.int64, device=DEV), bias_tokens=torch.zeros(1, dtype=torch.int32, device=DEV),
+                                                     bias_values=torch.zeros(1, device=DEV))),
+            (ValueError, lambda: L.cnr_adjust_logits(ctx, x, x, masks=torch.zeros(8, 6, dtype=torch.int32, device=DEV), n_masks=8)),
+            (P.CnrError, lambda: L.cnr_adjust_logits(None, x, x))]:
+        with pytest.raises(error):
+            call()
+    torch.cuda.synchronize()
+    assert P.cnr_poll_errors(ctx) == (P.CNR_OK, 0, 0)

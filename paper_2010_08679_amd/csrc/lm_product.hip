@@ -632,13 +632,35 @@ __global__ void __launch_bounds__(WM * WN * kWave, 2) tile_kernel(const ProductA
                 o += stride;
             }
         } else {
+            // What is added to is read for eight rows at once: one row after the other would wait for memory each time
+            // (1000 x 1111 x 1100 onto half 11.6 -> 9.1 us).  Rows and columns beyond the matrix read its last ones.
+            const uint32_t rows_left = m < p.m ? p.m - m : 0;
+            const bool whole = n + NF <= p.n;
 #pragma unroll
-            for (int i = 0; i < 4 * MF; ++i) {
-                float v[NF];
+            for (int first = 0; first < 4 * MF; first += 8) {
+                Pack<T, NF> old[8];
+                if (accumulate && rows_left && n < p.n) {
 #pragma unroll
-                for (int g = 0; g < NF; ++g) v[g] = acc[i % MF][g][i / MF];
-                if (m + i < p.m) store_row<T, NF>(o, n, p.n, v, accumulate);
-                o += stride;
+                    for (int u = 0; u < 8; ++u) {
+                        const uint32_t down = (uint32_t)(first + u) < rows_left ? (uint32_t)(first + u) : rows_left - 1;
+                        const T *from = o + (uint64_t)down * stride;
+                        if (whole) {
+                            old[u] = *reinterpret_cast<const Pack<T, NF> *>(from);
+                        } else {
+#pragma unroll
+                            for (int g = 0; g < NF; ++g) old[u].v[g] = from[n + g < p.n ? g : p.n - 1 - n];
+                        }
+                    }
+                }
+#pragma unroll
+                for (int u = 0; u < 8; ++u) {
+                    const int i = first + u;
+                    if ((uint32_t)i >= rows_left) continue;
+                    float v[NF];
+#pragma unroll
+                    for (int g = 0; g < NF; ++g) v[g] = accumulate ? (float)old[u].v[g] + acc[i % MF][g][i / MF] : acc[i % MF][g][i / MF];
+                    store_row<T, NF>(o + (uint64_t)i * stride, n, p.n, v, false);
+                }
             }
         }
     };

@@ -614,3 +614,20 @@ def test_both_ways_refuse_the_same(ctx, way):
             call()
     torch.cuda.synchronize()
     assert P.cnr_poll_errors(ctx) == (P.CNR_OK, 0, 0)
+
+
+def test_the_example_trains_checkpoints_and_decodes():
+    import importlib.util
+    import os
+    path = os.path.join(os.path.dirname(os.path.dirname(os.path.abspath(__file__))), "examples", "train_and_decode.py")
+    spec = importlib.util.spec_from_file_location("train_and_decode", path)
+    example = importlib.util.module_from_spec(spec)
+    spec.loader.exec_module(example)
+    r = example.main()
+    assert r["losses"][0] > 5.0 and r["losses"][-1] < 0.5  # ln 500 = 6.2 to begin with
+    assert r["errors"] == (P.CNR_OK, 0, 0)
+    for way in ("written", "resumed"):
+        for prompt, tokens in zip(r["prompts"], r[way]):
+            assert len(set(prompt + tokens)) == len(prompt) + 12 and 38 not in tokens
+            if prompt != [5]:  # 5 is followed by 38, which the grammar forbids
+                assert tokens[0] == (7 * prompt[-1] + 3) % example.VOCAB

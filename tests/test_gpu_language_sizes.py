@@ -273,3 +273,30 @@ def test_adjust_more_than_4_gi_logits(ctx):
     x[-1, -2] = 0
     x[:, 7 * 32 + 5] = 0
     assert not any(bool(part.any()) for part in x.split(1000))
+
+
+@pytest.mark.parametrize("type", ["f32", "bf16", "f16"])
+@pytest.mark.parametrize("kind", ["row", "tile"])
+def test_quantize_many_quotients_with_scales_of_any_value(ctx, type, kind):
+    # blocks of all magnitudes, the smallest ones among them, with values next to the middles of codes
+    g = torch.Generator().manual_seed(9)
+    rows, dim = 640, 512
+    x = torch.randn(rows, dim, generator=g, dtype=torch.float64)
+    high = 128 if kind == "tile" else 1
+    x *= 2.0 ** torch.randint(-150, 127, (rows // high, dim // 128), generator=g).double().repeat_interleave(high, 0).repeat_interleave(128, 1)
+    x = x.clamp(-3e38, 3e38)
+    whole = x.to(TYPES[type])
+    whole = torch.where(whole.isfinite(), whole, torch.zeros_like(whole))
+    s = R.quantize(whole.double().numpy(), kind, "f32")[1]  # [block][row or tile]
+    each = torch.from_numpy(s if kind == "row" else s.repeat(128, axis=1)).t().repeat_interleave(128, 1)
+    code = torch.randint(0, 126, (rows, dim), generator=g)
+    middle = torch.from_numpy((R.E4M3[1:127] + R.E4M3[:126]) / 2)[code] * each
+    near = torch.nextafter(middle.float(), torch.where(torch.rand(rows, dim, generator=g) < 0.5, 0.0, 3e38)) if type == "f32" else middle
+    take = torch.rand(rows, dim, generator=g) < 0.02
+    limit = whole.abs().reshape(-1, high, dim // 128, 128).amax(dim=(1, 3)).repeat_interleave(high, 0).repeat_interleave(128, 1)
+    whole = torch.where(take & (near.to(TYPES[type]) <= limit), near.to(TYPES[type]), whole)
+    out = P.BlockMatrix.empty(rows, dim, P.CNR_BLOCK_TILE if kind == "tile" else P.CNR_BLOCK_ROW, P.CNR_SCALE_F32)
+    P.quantize_blocks(ctx, whole.to(DEV), out)
+    codes, s = R.quantize(whole.double().numpy(), kind, "f32")
+    assert np.array_equal(out.scale.cpu().numpy().astype(np.float64)[:, : s.shape[1]], s)
+    assert np.array_equal(out.codes.cpu().numpy(), codes)

@@ -21,8 +21,8 @@
  *   scale   [ceil(dim / 128)][cnr_block_scale_stride(n_rows, kind)]: entry [j][i] belongs to columns
  *           [128 j, 128 (j + 1)) of row i (CNR_BLOCK_ROW) or of rows [128 i, 128 (i + 1)) (CNR_BLOCK_TILE);
  *           entries that belong to no row are not read for a result and may hold anything;
- *           uint8 b standing for 2^(b - 127) (CNR_SCALE_E8M0; 255 is not allowed) or float (CNR_SCALE_F32);
- *           16-byte aligned base
+ *           uint8 b from 1 to 254 standing for 2^(b - 127) (CNR_SCALE_E8M0) or float (CNR_SCALE_F32; finite, one
+ *           below 2^-126 counts as 0); 16-byte aligned base
  * and stands for scale * code.
  */
 #ifndef CNR_LM_H
@@ -61,7 +61,7 @@ size_t cnr_block_scale_count(uint64_t n_rows, uint64_t dim, cnr_block_kind kind)
  *   codes_t, scale_t  the transpose of X, dim x n_rows, as a blocked matrix of the same kind, both or neither
  *              NULL: for CNR_BLOCK_TILE the same codes and scales transposed; for CNR_BLOCK_ROW its blocks are
  *              128 rows of one column of X
- * x is read once, whichever are asked for. */
+ * x is read once, whichever are asked for.  CNR_E_TOO_LARGE from 2^24 tiles of 128 x 128 on. */
 cnr_status cnr_quantize_blocks(cnr_ctx *ctx, const void *x, cnr_float_type type, uint64_t n_rows, uint64_t dim,
                                uint64_t stride, cnr_block_kind kind, cnr_scale_type scale_type, uint8_t *codes,
                                void *scale, uint8_t *codes_t, void *scale_t, void *stream);
@@ -70,7 +70,9 @@ cnr_status cnr_quantize_blocks(cnr_ctx *ctx, const void *x, cnr_float_type type,
  * blocked matrix of m x k, B of n x k, both with scales of scale_type.  Sums are held in fp32 and rounded
  * once, to out's type.  For float outputs the products are added up in fp32; for the 16-bit types by the 8-bit
  * matrix instructions, which drop what lies 2^-14 or more below the largest of eight products (about 2^-16 of
- * the result, a fraction of those types' rounding).  The result does not depend on other work on the GPU.
+ * the result, a fraction of those types' rounding).  For float outputs scale * code passes through bfloat16, which holds it
+ * exactly from 2^-126 on (smaller values lose bits below 2^-133).  The result does not depend on other work on the GPU.
+ * CNR_E_TOO_LARGE from 2^24 tiles of 128 x 128 outputs on, and from m > 2^19 with k >= 2^24 - 128 on.
  *   out_stride  elements from one row of out to the next, >= n; out is aligned to its element
  *   workspace   NULL, or cnr_block_product_workspace_bytes(ctx, m, n, k) bytes, 16-byte aligned, contents
  *               irrelevant: with it, products with few outputs and a large k are split over the whole GPU

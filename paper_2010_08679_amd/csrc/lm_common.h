@@ -10,8 +10,6 @@ static inline bool cnr_aligned(const void *p, size_t to) { return (reinterpret_c
 static inline uint64_t cnr_ceil_div(uint64_t a, uint64_t b) { return (a + b - 1) / b; }
 
 #ifdef __HIPCC__
-typedef uint32_t u32x8 __attribute__((ext_vector_type(8)));
-
 // Elements of the three types: to fp32 exactly, from fp32 with one rounding to nearest even.
 template <int TYPE>
 struct Element;
@@ -41,7 +39,7 @@ struct __attribute__((packed, aligned(sizeof(T)))) Pack {
     T v[N];
 };
 
-// 16 bytes of elements that need no more alignment than one of them, in one access, as words; and an element of them.
+// 16 bytes of elements that need no more alignment than one of them, in one access, as words.
 typedef uint32_t u32x4_anywhere __attribute__((ext_vector_type(4), aligned(2)));
 template <typename T>
 __device__ __forceinline__ u32x4 load16(const T *p) {
@@ -50,14 +48,5 @@ __device__ __forceinline__ u32x4 load16(const T *p) {
 template <typename T>
 __device__ __forceinline__ void store16(T *p, const u32x4 &w) {
     *reinterpret_cast<u32x4_anywhere *>(p) = w;
-}
-template <int TYPE>
-__device__ __forceinline__ float element_of(const u32x4 &w, int i) {
-    if constexpr (TYPE == CNR_FLOAT_F32) {
-        return __uint_as_float(w[i]);
-    } else {
-        const uint16_t half = (uint16_t)(w[i / 2] >> (16 * (i % 2)));
-        return Element<TYPE>::wide(__builtin_bit_cast(typename Element<TYPE>::type, half));
-    }
 }
 #endif

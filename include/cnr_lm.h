@@ -71,7 +71,9 @@ cnr_status cnr_quantize_blocks(cnr_ctx *ctx, const void *x, cnr_float_type type,
  * once, to out's type.  For float outputs the products are added up in fp32; for the 16-bit types by the 8-bit
  * matrix instructions, which drop what lies 2^-14 or more below the largest of eight products (about 2^-16 of
  * the result, a fraction of those types' rounding).  For float outputs scale * code passes through bfloat16, which holds it
- * exactly from 2^-126 on (smaller values lose bits below 2^-133).  The result does not depend on other work on the GPU.
+ * exactly from 2^-126 on (smaller values lose bits below 2^-133).  A result is infinite or NaN only where codes are NaN or fp32 cannot
+ * hold a block's sum or the total; tiles of a float output in which one is, or in which scale * code reaches 2^128, take several
+ * times as long.  The result does not depend on other work on the GPU.
  * CNR_E_TOO_LARGE from 2^24 tiles of 128 x 128 outputs on, and from m > 2^19 with k >= 2^24 - 128 on.
  *   out_stride  elements from one row of out to the next, >= n; out is aligned to its element
  *   workspace   NULL, or cnr_block_product_workspace_bytes(ctx, m, n, k) bytes, 16-byte aligned, contents

@@ -10,7 +10,8 @@
 //     step what lies 2^-14 or more below the largest is dropped (measured: normal codes 1.5e-5 of the result, codes
 //     of uniformly spread exponents 7e-5), a small part of a bfloat16's (2^-9) or a half's (2^-12) rounding;
 //   bfloat16 instructions on the codes converted in registers, exact as well (4 of 8 bits of mantissa), their scales
-//     of powers of two applied by the conversion, added up in fp32 (measured 1e-8 to 6e-8): float outputs.
+//     of powers of two applied by the conversion, added up in fp32 (measured 1e-8 to 6e-8): float outputs.  Scales that would
+//     take a code out of bfloat16's range multiply the block's sum instead (sum_any_range).
 // Scales of any value multiply each block's sum before it is added to the total.
 #include "lm_common.h"
 
@@ -88,21 +89,101 @@ __device__ __forceinline__ void store_out(const ProductArgs &p, uint32_t m, uint
     }
 }
 
-// A scale's exponent goes into the matrix instruction and its fraction, from 1 to 2, multiplies the sum: neither leaves fp32's range
-// unless the result does.  (A scale below 2^-126 counts as 0.)
+// A scale's exponent goes into the 8-bit matrix instruction, or into the conversion to bfloat16 (see sum_any_range), and its fraction, from 1 to
+// 2, multiplies the sum: neither leaves fp32's range unless the result does.  (A scale below 2^-126 counts as 0.)
 __device__ __forceinline__ float fraction_of(float s) {
     const uint32_t b = __float_as_uint(s);
     return b & 0x7f800000u ? __uint_as_float((b & 0x807fffffu) | 0x3f800000u) : 0.0f;
 }
 __device__ __forceinline__ uint32_t exponent_of(float s) { return __float_as_uint(s) >> 23 & 255u; }
 
+// Whether a sum that belongs to the matrix is infinite or NaN, for the whole wave.  A code that its scale takes out of bfloat16's range
+// (2^128 and more) becomes infinite, and every sum that it enters infinite or NaN: nothing in the loop has to look for such
+// scales.  Of the lane's rows i * MF + f and columns g the first `rows` and `columns` belong.
+template <int MF, int NF>
+__device__ __forceinline__ bool not_finite(const f32x4 (&acc)[MF][NF], uint32_t rows, uint32_t columns) {
+    float none = 0.0f;
+    if (__all((rows >= 4 * MF) & (columns >= NF))) {
+#pragma unroll
+        for (int f = 0; f < MF; ++f)
+#pragma unroll
+            for (int g = 0; g < NF; ++g)
+#pragma unroll
+                for (int i = 0; i < 4; ++i) none = __builtin_fmaf(acc[f][g][i], 0.0f, none);
+    } else {
+#pragma unroll
+        for (int f = 0; f < MF; ++f)
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                float row = 0.0f;
+#pragma unroll
+                for (uint32_t g = 0; g < NF; ++g) row = __builtin_fmaf(g < columns ? acc[f][g][i] : 0.0f, 0.0f, row);
+                none += (uint32_t)(i * MF + f) < rows ? row : 0.0f;
+            }
+    }
+    return __any(!(none == 0.0f));
+}
+
+// acc[f][g] = the sums over blocks [begin, end) of A's row_a[f] and B's row_b[g] (of each lane), with scales of any range: a block's codes are
+// multiplied as they are and its sum takes fractions and exponents.  Operands come straight from memory, one fragment at a time.
+template <int SCALE, int MF, int NF>
+__device__ __forceinline__ void sum_any_range(const ProductArgs &p, const uint32_t (&row_a)[MF], const uint32_t (&row_b)[NF], uint32_t begin, uint32_t end,
+                                              f32x4 (&acc)[MF][NF]) {
+    typedef typename ScaleOf<SCALE>::type S;
+    const uint32_t quarter = tid_x() % kWave / 16;
+#pragma unroll
+    for (int f = 0; f < MF; ++f)
+#pragma unroll
+        for (int g = 0; g < NF; ++g) acc[f][g] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll 1
+    for (uint32_t kb = begin; kb < end; ++kb) {
+#pragma unroll
+        for (int f = 0; f < MF; ++f) {
+            const i32x8 x = load_codes(p.a + (uint64_t)row_a[f] * p.row_bytes + (uint64_t)kb * CNR_BLOCK + quarter * 16);
+            const S sa = reinterpret_cast<const S *>(p.a_scale)[kb * p.a_stride + (row_a[f] >> p.a_shift)];
+            float fraction[4];  // of the rows of the lane's sums
+            int exponent[4];
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                const S s = __shfl(sa, (int)(quarter * 4 + i));
+                if constexpr (SCALE == CNR_SCALE_E8M0) {
+                    exponent[i] = (int)s - 254;
+                } else {
+                    exponent[i] = (int)exponent_of(s) - 254;
+                    fraction[i] = fraction_of(s);
+                }
+            }
+#pragma unroll
+            for (int g = 0; g < NF; ++g) {
+                const i32x8 y = load_codes(p.b + (uint64_t)row_b[g] * p.row_bytes + (uint64_t)kb * CNR_BLOCK + quarter * 16);
+                const S sb = reinterpret_cast<const S *>(p.b_scale)[kb * p.b_stride + (row_b[g] >> p.b_shift)];
+                f32x4 d = {0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    d = __builtin_amdgcn_mfma_f32_16x16x32_bf16(widen(x, 127).part[i], widen(y, 127).part[i], d, 0, 0, 0);
+                    __builtin_amdgcn_sched_barrier(0);  // no more registers than the caller's own loop
+                }
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    if constexpr (SCALE == CNR_SCALE_E8M0)
+                        acc[f][g][i] += __builtin_ldexpf(d[i], exponent[i] + (int)sb);
+                    else
+                        acc[f][g][i] += __builtin_ldexpf(d[i] * (fraction[i] * fraction_of(sb)), exponent[i] + (int)exponent_of(sb));
+                }
+                __builtin_amdgcn_sched_barrier(0);  // no more registers than the caller's own loop
+            }
+        }
+    }
+}
+
 // ---- few rows or few tiles: operands straight from memory ---------------------------------------------------------
 //
 // A workgroup has 16 MF x 16 NF outputs; each of its waves takes a quarter of the columns, U blocks at a time so that enough loads are
 // under way, straight into the matrix instructions' registers; they add up their sums in LDS at the end.  Bound by reading B: 1 x 131072 x 4096
 // 88 us (6.1 TB/s), 1 x 32000 x 4096 25.5; with every fourth block to a wave 97 and 28.
+// (Waves on a SIMD: as many as the loop leaves room for, which sum_any_range would take from them.)
 template <int SCALE, bool FULL, int MF, int NF, int U>
-__global__ void __launch_bounds__(kBlock) narrow_kernel(const ProductArgs p) {
+__global__ void __launch_bounds__(kBlock, U == 1 ? 6 : 4) narrow_kernel(const ProductArgs p) {
     typedef typename ScaleOf<SCALE>::type S;
     __shared__ f32x4 sums[kWavesPerBlock][MF * NF][kWave];
     const uint32_t lane = tid_x() % kWave, wave = (uint32_t)__builtin_amdgcn_readfirstlane((int)(tid_x() / kWave));
@@ -200,6 +281,16 @@ __global__ void __launch_bounds__(kBlock) narrow_kernel(const ProductArgs p) {
                     }
                 }
             }
+        }
+    }
+    if constexpr (FULL) {
+        if (not_finite(acc, 4 * MF, NF)) {
+            uint32_t row_a[MF], row_b[NF];
+#pragma unroll
+            for (int f = 0; f < MF; ++f) row_a[f] = m0 + 16 * f + lane % 16 < p.m ? m0 + 16 * f + lane % 16 : p.m - 1;
+#pragma unroll
+            for (int f = 0; f < NF; ++f) row_b[f] = n0 + 16 * f + lane % 16 < p.n ? n0 + 16 * f + lane % 16 : p.n - 1;
+            sum_any_range<SCALE, MF, NF>(p, row_a, row_b, begin, end, acc);
         }
     }
 #pragma unroll
@@ -614,6 +705,17 @@ __global__ void __launch_bounds__(WM * WN * kWave, 2) tile_kernel(const ProductA
             pick_b.advance();
             wait_for_loads<(STAGES - 2) * kLoads>();
             barrier();
+        }
+        if constexpr (FULL) {
+            const uint32_t first_m = m0 + wave_m + quarter * 4 * MF, first_n = n0 + wave_n + r * NF;
+            if (not_finite(acc, first_m < p.m ? p.m - first_m : 0, first_n < p.n ? p.n - first_n : 0)) {
+                uint32_t row_a[MF], row_b[NF];
+#pragma unroll
+                for (int f = 0; f < MF; ++f) row_a[f] = m0 + wave_m + r * MF + f < p.m ? m0 + wave_m + r * MF + f : p.m - 1;
+#pragma unroll
+                for (int f = 0; f < NF; ++f) row_b[f] = n0 + wave_n + r * NF + f < p.n ? n0 + wave_n + r * NF + f : p.n - 1;
+                sum_any_range<SCALE, MF, NF>(p, row_a, row_b, begin, end, acc);
+            }
         }
     }
     wait_for_loads<0>();

@@ -1,0 +1,94 @@
+"""Products of blocked matrices at the ends of the scales' range, in every kernel."""
+import numpy as np
+import pytest
+import torch
+
+import paper_2010_08679_amd as P
+from oracle import blocks as R
+
+pytestmark = pytest.mark.gpu
+DEV = "cuda:0"
+TYPES = {"f32": torch.float32, "bf16": torch.bfloat16, "f16": torch.float16}
+SCALES = {"e8m0": P.CNR_SCALE_E8M0, "f32": P.CNR_SCALE_F32}
+ROW, TILE = P.CNR_BLOCK_ROW, P.CNR_BLOCK_TILE
+
+
+@pytest.fixture(scope="module")
+def ctx():
+    c = P.cnr_create(0)
+    yield c
+    torch.cuda.synchronize()
+    P.cnr_destroy(c)
+
+
+def _matrix(values, kind, scale, exponents, fractions=None):
+    """(BlockMatrix, its values in 64 bits) of e4m3 values [rows, k] and exponents [block][row or tile] of the scales; what belongs to no row is rubbish."""
+    rows, k = values.shape
+    m = P.BlockMatrix.empty(rows, k, kind, SCALES[scale])
+    codes = np.zeros(tuple(m.codes.shape), dtype=np.uint8)
+    codes[:, :k] = R.encode(values)
+    m.codes.copy_(torch.from_numpy(codes))
+    s = np.ldexp(1.0 if fractions is None else fractions, exponents)
+    held = np.full(tuple(m.scale.shape), 254.0 if scale == "e8m0" else 3e38)
+    held[:, : s.shape[1]] = exponents + 127 if scale == "e8m0" else s
+    m.scale.copy_(torch.from_numpy(held).to(m.scale.dtype))
+    each = (s if kind == ROW else s.repeat(128, axis=1))[:, :rows].T.repeat(128, axis=1)[:, :k]
+    return m, torch.from_numpy(values * each).to(DEV)
+
+
+# the kernel for few rows, one or two fragments wide, and tiles of each size, in one part and in several
+SIZES = [(3, 140, 256), (5, 16500, 130), (33, 130, 384), (200, 300, 256), (1000, 1000, 300), (500, 2050, 1100), (2049, 4097, 128), (64, 1024, 16384),
+         (100, 1000, 9000), (257, 1000, 9000)]
+
+
+@pytest.mark.parametrize("out", ["f32", "bf16"])
+@pytest.mark.parametrize("scale", ["e8m0", "f32"])
+@pytest.mark.parametrize("m,n,k", SIZES)
+def test_products_at_the_ends_of_the_scales(ctx, m, n, k, scale, out):
+    # one operand's scales from 1 to the largest, the other's near the smallest: every product and every sum is an ordinary float
+    g = np.random.default_rng(m + n + k)
+    for a_kind, b_kind in ((ROW, TILE), (TILE, ROW)):
+        def operand(rows, kind, low, high):
+            v = np.clip(g.normal(0, 100, (rows, k)), -448, 448) * (g.random((rows, k)) < 0.7)  # zeros that meet the largest values
+            v[g.random((rows, k)) < 0.05] = 448.0
+            shape = (-(-k // 128), rows if kind == ROW else -(-rows // 128))
+            e = g.choice([low, low, high, high, (low + high) // 2], shape)
+            return _matrix(R.E4M3[R.encode(v)], kind, scale, e, g.uniform(1, 1.99, shape) if scale == "f32" else None)
+
+        for low, high, other_low, other_high in ((0, 127, -126, -120), (-126, -117, 100, 120)):
+            (a, av), (b, bv) = operand(m, a_kind, low, high), operand(n, b_kind, other_low, other_high)
+            want, sums = av @ bv.t(), av.abs() @ bv.abs().t()
+            space = P.block_workspace(ctx, m, n, k)
+            # fp32 sums of k products, each block's by the scales: off by at most k + 128 roundings of the sum of the magnitudes, and by what lies below the floats
+            # (or the types' smallest values); bfloat16 rounds once more, and its products of eight drop less than 2^-13 of the largest for each of the others
+            bound = (k + 128) * 2.0 ** -23 * sums + (k + 128) * 2.0 ** -149
+            if out == "bf16":
+                bound = bound + 2.0 ** -8 * want.abs() + 7 * 2.0 ** -13 * sums + 2.0 ** -134
+            for workspace in (space, None) if space is not None else (None,):
+                got = torch.full((m, n), 7.0, dtype=TYPES[out], device=DEV)
+                P.block_product(ctx, a, b, got, workspace=workspace)
+                assert bool(((got.double() - want).abs() <= bound).all()), (a_kind, low)
+                P.block_product(ctx, a, b, got, accumulate=True, workspace=workspace)
+                assert bool(((got.double() - 2 * want).abs() <= 2 * bound + (2.0 ** -23 if out == "f32" else 2.0 ** -7) * want.abs()).all()), (a_kind, low)
+
+
+@pytest.mark.parametrize("scale", ["e8m0", "f32"])
+@pytest.mark.parametrize("type", ["f32", "bf16"])
+@pytest.mark.parametrize("m,n", [(4, 50), (300, 500)])
+def test_float_products_of_the_largest_values_quantized(ctx, m, n, type, scale):
+    k, top = 300, float(torch.finfo(TYPES[type]).max)
+    g = torch.Generator().manual_seed(m)
+    x = torch.randn(m, k, generator=g, dtype=torch.float64)
+    x[1] *= top / 4
+    x[2, 130:] = top
+    x[3, 5] = -top
+    w = torch.randn(n, k, generator=g, dtype=torch.float64) * 2.0 ** -100
+    w[:, 5] = 0
+    x, w = x.clamp(-top, top).to(TYPES[type]), w.float()
+    a, b = P.BlockMatrix.empty(m, k, ROW, SCALES[scale]), P.BlockMatrix.empty(n, k, TILE, SCALES[scale])
+    P.quantize_blocks(ctx, x.to(DEV), a)
+    P.quantize_blocks(ctx, w.to(DEV), b)
+    av = torch.from_numpy(R.values(*R.quantize(x.double().numpy(), "row", scale), "row"))[:, :k]
+    bv = torch.from_numpy(R.values(*R.quantize(w.double().numpy(), "tile", scale), "tile"))[:, :k]
+    got = P.block_product(ctx, a, b, torch.empty(m, n, device=DEV)).cpu().double()
+    assert bool(((got - av @ bv.t()).abs() <= (k + 128) * 2.0 ** -23 * (av.abs() @ bv.abs().t())).all())

@@ -21,19 +21,19 @@ def ctx():
     P.cnr_destroy(c)
 
 
-def _matrix(values, kind, scale, exponents, fractions=None):
-    """(BlockMatrix, its values in 64 bits) of e4m3 values [rows, k] and exponents [block][row or tile] of the scales; what belongs to no row is rubbish."""
-    rows, k = values.shape
+def _matrix(given, kind, scale, exponents, fractions=None):
+    """(BlockMatrix, its values in 64 bits) of codes [rows, k] and exponents [block][row or tile] of the scales; what belongs to no row is rubbish."""
+    rows, k = given.shape
     m = P.BlockMatrix.empty(rows, k, kind, SCALES[scale])
     codes = np.zeros(tuple(m.codes.shape), dtype=np.uint8)
-    codes[:, :k] = R.encode(values)
+    codes[:, :k] = given
     m.codes.copy_(torch.from_numpy(codes))
     s = np.ldexp(1.0 if fractions is None else fractions, exponents)
     held = np.full(tuple(m.scale.shape), 254.0 if scale == "e8m0" else 3e38)
     held[:, : s.shape[1]] = exponents + 127 if scale == "e8m0" else s
     m.scale.copy_(torch.from_numpy(held).to(m.scale.dtype))
     each = (s if kind == ROW else s.repeat(128, axis=1))[:, :rows].T.repeat(128, axis=1)[:, :k]
-    return m, torch.from_numpy(values * each).to(DEV)
+    return m, torch.from_numpy(R.E4M3).to(DEV)[torch.from_numpy(given.astype(np.int64)).to(DEV)] * torch.from_numpy(each).to(DEV)
 
 
 # the kernel for few rows, one or two fragments wide, and tiles of each size, in one part and in several
@@ -49,11 +49,11 @@ def test_products_at_the_ends_of_the_scales(ctx, m, n, k, scale, out):
     g = np.random.default_rng(m + n + k)
     for a_kind, b_kind in ((ROW, TILE), (TILE, ROW)):
         def operand(rows, kind, low, high):
-            v = np.clip(g.normal(0, 100, (rows, k)), -448, 448) * (g.random((rows, k)) < 0.7)  # zeros that meet the largest values
-            v[g.random((rows, k)) < 0.05] = 448.0
+            v = g.integers(0x38, 0x7f, (rows, k), dtype=np.uint8) | g.integers(0, 2, (rows, k), dtype=np.uint8) << 7  # magnitudes from 1 to 448
+            v[g.integers(0, 4, (rows, k), dtype=np.uint8) == 0] = 0  # zeros that meet the largest values
             shape = (-(-k // 128), rows if kind == ROW else -(-rows // 128))
             e = g.choice([low, low, high, high, (low + high) // 2], shape)
-            return _matrix(R.E4M3[R.encode(v)], kind, scale, e, g.uniform(1, 1.99, shape) if scale == "f32" else None)
+            return _matrix(v, kind, scale, e, g.uniform(1, 1.99, shape) if scale == "f32" else None)
 
         for low, high, other_low, other_high in ((0, 127, -126, -120), (-126, -117, 100, 120)):
             (a, av), (b, bv) = operand(m, a_kind, low, high), operand(n, b_kind, other_low, other_high)

@@ -3,15 +3,50 @@ a scale for each block of 128, a linear layer trained and served in them, and th
 what follows from them for their logits.
 
 Plumbing only, as in :mod:`checkpoint`: torch allocates the memory and provides the stream, every step runs in libcnr's
-kernels.
+kernels.  A call with ``stream`` is one under ``torch.cuda.stream(stream)``: what it allocates belongs to that stream, what it is
+given has to be ready there.
 """
 from __future__ import annotations
 
+from contextlib import nullcontext
 from dataclasses import dataclass
 
 import torch
 
 from . import lm_binding as L
+
+
+def _on(stream):
+    """Memory that a call allocates comes from the stream that it works on: of the current one's it would be handed out while work queued
+    there still uses it, and again before `stream` is done."""
+    return nullcontext() if stream is None else torch.cuda.stream(stream)
+
+
+class _Holder:
+    """What keeps device memory from one call to the next, made on the current stream and used on the streams that calls name."""
+
+    def _holds(self, device, tensors) -> None:
+        self._held, self._used_on = list(tensors), set()
+        self._made_on = torch.cuda.current_stream(device) if torch.device(device).type == "cuda" else None
+
+    def _hold(self, tensor):
+        """One more, allocated by a call."""
+        self._held.append(tensor)
+        for s in self._used_on:
+            tensor.record_stream(s)
+        return tensor
+
+    def _use(self, stream) -> None:
+        """The first call on a stream lets it wait for what is queued where the memory came from, which that work may still use; freed
+        memory is not handed on before that stream is done with it.  (torch begins a capture on an idle GPU; a stream under capture cannot wait for others.)"""
+        if stream is None or stream in self._used_on or self._made_on is None:
+            return
+        with torch.cuda.stream(stream):
+            if not torch.cuda.is_current_stream_capturing():
+                stream.wait_stream(self._made_on)
+        self._used_on.add(stream)
+        for t in self._held:
+            t.record_stream(stream)
 
 
 @dataclass
@@ -40,7 +75,8 @@ def quantize_blocks(ctx, x: torch.Tensor, out: BlockMatrix | None = None, out_t:
     """Quantizes the matrix ``x`` into ``out`` and its transpose into ``out_t`` (either may be None; a new matrix of rows' blocks
     with scales of powers of two where both are)."""
     if out is None and out_t is None:
-        out = BlockMatrix.empty(*x.shape, device=x.device)
+        with _on(stream):
+            out = BlockMatrix.empty(*x.shape, device=x.device)
     like = out if out is not None else out_t
     n_rows, dim = x.shape
     if ((out is not None and (out.n_rows != n_rows or out.dim != dim))
@@ -66,14 +102,15 @@ def block_product(ctx, a: BlockMatrix, b: BlockMatrix, out: torch.Tensor | None 
     if out is None:
         if accumulate:
             raise ValueError("nothing to add to")
-        out = torch.empty(a.n_rows, b.n_rows, dtype=torch.bfloat16, device=a.codes.device)
+        with _on(stream):
+            out = torch.empty(a.n_rows, b.n_rows, dtype=torch.bfloat16, device=a.codes.device)
     elif out.shape != (a.n_rows, b.n_rows):
         raise ValueError("out must be %d x %d" % (a.n_rows, b.n_rows))
     L.cnr_block_product(ctx, a.codes, a.scale, a.kind, a.n_rows, b.codes, b.scale, b.kind, b.n_rows, a.dim, out, accumulate, workspace, stream)
     return out
 
 
-class BlockLinear:
+class BlockLinear(_Holder):
     """y = x W^T in 8 bits, forward and backward, for up to max_tokens rows of x at a time.
 
     The layer keeps the weight in tiles in both directions (:meth:`load`, after every change of the weight) and, from :meth:`forward` to
@@ -89,6 +126,7 @@ class BlockLinear:
         self._input_t = None
         self._sized = {}
         self._spaces = []  # workspaces, the last one the largest; earlier ones stay, since captured graphs may hold them
+        self._holds(device, (self.weight.codes, self.weight.scale, self.weight_t.codes, self.weight_t.scale, *self._x, *self._x_t, *self._dy, *self._dy_t))
 
     def _buffers(self, n_rows: int, dim: int):
         m = BlockMatrix.empty(n_rows, dim, L.CNR_BLOCK_ROW, self.scale_type, self.device)
@@ -100,7 +138,7 @@ class BlockLinear:
         return BlockMatrix(codes[: n_rows * across * L.CNR_BLOCK].view(n_rows, across * L.CNR_BLOCK), scale[: across * stride].view(across, stride),
                            n_rows, dim, L.CNR_BLOCK_ROW)
 
-    def _for(self, tokens: int):
+    def _for(self, tokens: int, stream=None):
         """Input and output gradient of that many tokens within the layer's buffers, and a workspace for their products."""
         if tokens > self.max_tokens:
             raise ValueError("%d tokens, the layer was made for %d" % (tokens, self.max_tokens))
@@ -109,7 +147,8 @@ class BlockLinear:
                 (tokens, self.n_out, self.n_in), (tokens, self.n_in, self.n_out), (self.n_out, self.n_in, tokens)))
             had = self._spaces[-1].numel() if self._spaces else 0
             if space > had:
-                self._spaces.append(torch.empty(max(space, 2 * had), dtype=torch.uint8, device=self.device))
+                with _on(stream):
+                    self._spaces.append(self._hold(torch.empty(max(space, 2 * had), dtype=torch.uint8, device=self.device)))
             self._sized = {tokens: (self._of(self._x, tokens, self.n_in), self._of(self._x_t, self.n_in, tokens),
                                     self._of(self._dy, tokens, self.n_out), self._of(self._dy_t, self.n_out, tokens),
                                     self._spaces[-1] if space else None)}
@@ -117,15 +156,18 @@ class BlockLinear:
 
     def load(self, weight: torch.Tensor, stream=None) -> None:
         """Takes the weight [n_out, n_in] as it is now."""
+        self._use(stream)
         quantize_blocks(self.ctx, weight, self.weight, self.weight_t, stream)
 
     def forward(self, x: torch.Tensor, out: torch.Tensor | None = None, training: bool = True, stream=None) -> torch.Tensor:
         """x [tokens, n_in] -> [tokens, n_out], of x's type when ``out`` is None; ``training``: :meth:`backward` follows."""
-        qx, qx_t, _, _, space = self._for(x.shape[0])
+        self._use(stream)
+        qx, qx_t, _, _, space = self._for(x.shape[0], stream)
         quantize_blocks(self.ctx, x, qx, qx_t if training else None, stream)
         self._input_t = qx_t if training else None
         if out is None:
-            out = torch.empty(x.shape[0], self.n_out, dtype=x.dtype, device=self.device)
+            with _on(stream):
+                out = torch.empty(x.shape[0], self.n_out, dtype=x.dtype, device=self.device)
         return block_product(self.ctx, qx, self.weight, out, workspace=space, stream=stream)
 
     def backward(self, dy: torch.Tensor, dx: torch.Tensor | None = None, dw: torch.Tensor | None = None, accumulate: bool = False, stream=None):
@@ -133,20 +175,22 @@ class BlockLinear:
         added to ``dw`` where ``accumulate`` is set."""
         if self._input_t is None or self._input_t.dim != dy.shape[0]:
             raise ValueError("no forward pass of %d tokens in training precedes" % dy.shape[0])
-        _, _, qdy, qdy_t, space = self._for(dy.shape[0])
+        if dw is None and accumulate:
+            raise ValueError("nothing to add to")
+        self._use(stream)
+        _, _, qdy, qdy_t, space = self._for(dy.shape[0], stream)
         quantize_blocks(self.ctx, dy, qdy, qdy_t, stream)
-        if dx is None:
-            dx = torch.empty(dy.shape[0], self.n_in, dtype=dy.dtype, device=self.device)
-        if dw is None:
-            if accumulate:
-                raise ValueError("nothing to add to")
-            dw = torch.empty(self.n_out, self.n_in, dtype=torch.float32, device=self.device)
+        with _on(stream):
+            if dx is None:
+                dx = torch.empty(dy.shape[0], self.n_in, dtype=dy.dtype, device=self.device)
+            if dw is None:
+                dw = torch.empty(self.n_out, self.n_in, dtype=torch.float32, device=self.device)
         block_product(self.ctx, qdy, self.weight_t, dx, workspace=space, stream=stream)
         block_product(self.ctx, qdy_t, self._input_t, dw, accumulate, space, stream)
         return dx, dw
 
 
-class TokenLedger:
+class TokenLedger(_Holder):
     """The tokens of up to n_slots sequences: which of the vocabulary each has seen (a bitmap, as a table's tracking bitmap) and
     how often the model wrote each."""
 
@@ -155,10 +199,12 @@ class TokenLedger:
         words = (self.vocab + 31) // 32
         self.seen = torch.zeros(n_slots, words, dtype=torch.int32, device=device) if seen is None else seen
         self.counts = torch.zeros(n_slots, vocab, dtype=torch.int32, device=device) if counts is None and seen is None else counts
+        self._holds(device, [t for t, given in ((self.seen, seen), (self.counts, counts)) if given is None and t is not None])
 
     def count(self, tokens: torch.Tensor, offsets: torch.Tensor | None = None, slots: torch.Tensor | None = None, prompt: bool = False,
               restart: bool = False, stream=None) -> None:
         """Enters one token of each sequence, or those that ``offsets`` gives each; ``restart`` empties the slots first."""
+        self._use(stream)
         L.cnr_count_tokens(self.ctx, self.seen, self.counts, self.n_slots, self.vocab, tokens, offsets, slots, prompt, restart, stream)
 
     def adjust(self, logits: torch.Tensor, out: torch.Tensor | None = None, slots: torch.Tensor | None = None, repetition=None, frequency=None,
@@ -167,6 +213,7 @@ class TokenLedger:
         is None."""
         if logits.shape[1] != self.vocab:
             raise ValueError("logits of %d tokens, a vocabulary of %d" % (logits.shape[1], self.vocab))
+        self._use(stream)
         out = logits if out is None else out
         penalties = repetition is not None or frequency is not None or presence is not None
         seen, counts = (self.seen, self.counts) if penalties else (None, None)

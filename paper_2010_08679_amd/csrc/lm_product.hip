@@ -6,9 +6,10 @@
 // that a load of all lanes reads 64 bytes in a row.
 //
 // Two ways to add up a block's 16 x 16 x 128 products:
-//   8-bit instructions, scales of powers of two applied by them.  Exact products; of each eight that are added in one
-//     step what lies 2^-14 or more below the largest is dropped (measured: normal codes 1.5e-5 of the result, codes
-//     of uniformly spread exponents 7e-5), a small part of a bfloat16's (2^-9) or a half's (2^-12) rounding;
+//   8-bit instructions, scales of powers of two applied by them: the 16-bit outputs.  Exact products; of each eight that are added in
+//     one step what lies 2^-14 or more below the largest is dropped.  Of the sum of the products' magnitudes that is (measured) 1e-5 with
+//     normal codes, 1.4e-4 with codes of evenly spread exponents, 4.3e-4 where one of each eight is 2^14 times the others: less than the
+//     half step of a bfloat16 (2^-8) or a half (2^-11), but not of a result that is small since products cancel.  Chosen for twice the rate;
 //   bfloat16 instructions on the codes converted in registers, exact as well (4 of 8 bits of mantissa), their scales
 //     of powers of two applied by the conversion, added up in fp32 (measured 1e-8 to 6e-8): float outputs.  Scales that would
 //     take a code out of bfloat16's range multiply the block's sum instead (sum_any_range).

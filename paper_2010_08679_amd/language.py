@@ -96,7 +96,10 @@ def block_workspace(ctx, m: int, n: int, k: int, device="cuda:0") -> torch.Tenso
 
 def block_product(ctx, a: BlockMatrix, b: BlockMatrix, out: torch.Tensor | None = None, accumulate: bool = False,
                   workspace: torch.Tensor | None = None, stream=None) -> torch.Tensor:
-    """``a`` times the transpose of ``b``, written to or added to ``out`` (a new bfloat16 matrix when None)."""
+    """``a`` times the transpose of ``b``, written to or added to ``out`` (a new bfloat16 matrix when None).
+
+    A float32 ``out`` holds sums added up in fp32.  16-bit ones are added up by the 8-bit matrix instructions: off by up to 2^-10 of the sum of the
+    products' magnitudes, which is below their rounding unless products cancel."""
     if a.dim != b.dim:
         raise ValueError("rows of %d and of %d columns" % (a.dim, b.dim))
     if out is None:
@@ -114,7 +117,8 @@ class BlockLinear(_Holder):
     """y = x W^T in 8 bits, forward and backward, for up to max_tokens rows of x at a time.
 
     The layer keeps the weight in tiles in both directions (:meth:`load`, after every change of the weight) and, from :meth:`forward` to
-    :meth:`backward`, the transpose of its input.  Calls of one layer belong on one stream."""
+    :meth:`backward`, the transpose of its input.  Outputs and input gradients of 16 bits and float32 ones differ in how they are added up, see
+    :func:`block_product`; the weight's gradient is float32 unless given otherwise.  Calls of one layer belong on one stream."""
 
     def __init__(self, ctx, n_out: int, n_in: int, max_tokens: int, scale_type: int = L.CNR_SCALE_E8M0, device="cuda:0"):
         self.ctx, self.n_out, self.n_in, self.max_tokens, self.scale_type = ctx, int(n_out), int(n_in), int(max_tokens), scale_type

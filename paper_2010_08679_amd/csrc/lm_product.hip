@@ -15,6 +15,7 @@
 //     take a code out of bfloat16's range multiply the block's sum instead (sum_any_range).
 // Scales of any value multiply each block's sum before it is added to the total.
 #include "lm_common.h"
+#include "lm_scale_fetch.h"
 
 #include <math.h>
 #include <type_traits>
@@ -351,8 +352,12 @@ __device__ __forceinline__ void load_to_lds(const i32x4 &buffer, uint32_t lds, u
     else
         asm volatile("buffer_load_dwordx4 %0, %1, %2 offen offset:%3 lds" ::"v"(offset), "s"(buffer), "s"(all), "n"(OFFSET));
 }
-__device__ __forceinline__ void load_words_to_lds(const i32x4 &buffer, uint32_t lds, uint32_t offset) {
-    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dword %1, %2, 0 offen lds" ::"s"(lds), "v"(offset), "s"(buffer));
+// The same of four bytes, or of `one`, which becomes the lowest of four.
+__device__ __forceinline__ void load_bytes_to_lds(const i32x4 &buffer, uint32_t lds, uint32_t offset, uint32_t one) {
+    asm volatile("s_mov_b32 m0, %0\n\ts_cmp_lg_u32 %3, 0\n\ts_cbranch_scc1 .Lone_byte_%=\n\t"
+                 "buffer_load_dword %1, %2, 0 offen lds\n\ts_branch .Lloaded_%=\n"
+                 ".Lone_byte_%=:\n\tbuffer_load_ubyte %1, %2, 0 offen lds\n.Lloaded_%=:" ::"s"(lds), "v"(offset), "s"(buffer), "s"(one)
+                 : "scc");
 }
 template <int LEFT>  // loads that need not have arrived
 __device__ __forceinline__ void wait_for_loads() {
@@ -372,41 +377,24 @@ struct Scales {
     float fraction[SCALE == CNR_SCALE_F32 ? F : 1];
 };
 
-// One operand's scales on their way through LDS: a word (E8M0), or four (F32), for each four rows of the tile.  Rows' scales fill
-// them; where 128 rows share one, each word is the aligned one that it lies in.
+// One operand's scales on their way through LDS: for each four rows of the tile a word (E8M0) or four (F32), which rows' own scales fill.  A
+// scale that 128 rows share is the lowest byte of each word, or one of the aligned four floats that it lies in.
 template <int SCALE>
-struct ScaleStream {
-    static constexpr uint32_t kSize = SCALE == CNR_SCALE_E8M0 ? 1 : 4;  // bytes of a scale
-    static constexpr uint32_t kGroup = 4 * kSize, kBytes = kWave * kGroup;  // of four, and of all in LDS
-    uint64_t base, step;          // address of the block to fetch next, bytes to the one after it
-    uint32_t block, block_step;   // the same within an array of tiles' scales, whose words are not aligned with its blocks
-    uint32_t in_block;
-    // `row0`: first row of the tile; four rows to a lane, as far as `n` of them go; rows beyond the matrix take the last scales that there are.
-    __device__ __forceinline__ ScaleStream(const void *p, uint64_t stride, uint32_t shift, uint32_t row0, uint32_t n, uint32_t lane, uint32_t kb) {
-        const bool rows = shift == 0;  // a scale for each row
-        const uint32_t row = row0 + 4 * (lane < n / 4 ? lane : n / 4 - 1);
-        const uint32_t last = (uint32_t)stride - (rows ? 4 : 1), entry = rows ? row : row / CNR_BLOCK;
-        const uint32_t low = rows ? row0 : 0;  // goes into the base, so that offsets stay small
-        in_block = ((entry < last ? entry : last) - low) * kSize;
-        base = reinterpret_cast<uint64_t>(p) + (rows ? ((uint64_t)kb * stride + low) * kSize : 0);
-        step = rows ? stride * kSize : 0;
-        block = rows ? 0 : (uint32_t)(kb * stride) * kSize;
-        block_step = rows ? 0 : (uint32_t)stride * kSize;
-    }
-    // `on`: the block is not the last one; there the stream stays.
+struct ScaleStream : ScaleFetch<SCALE == CNR_SCALE_E8M0 ? 1 : 4> {
+    typedef ScaleFetch<SCALE == CNR_SCALE_E8M0 ? 1 : 4> Fetch;
+    static constexpr uint32_t kBytes = kWave * 4 * (SCALE == CNR_SCALE_E8M0 ? 1 : 4);  // in LDS
+    using Fetch::Fetch;
     __device__ __forceinline__ void fetch(uint32_t lds, bool on) {
-        const i32x4 buffer = buffer_of(base, 0xffffffffull);
-        const uint32_t offset = (block + in_block) & ~(kGroup - 1);
+        const i32x4 buffer = buffer_of(this->base, this->records);
         if constexpr (SCALE == CNR_SCALE_E8M0)
-            load_words_to_lds(buffer, lds, offset);
+            load_bytes_to_lds(buffer, lds, this->offset(), this->tiles);
         else
-            load_to_lds<0>(buffer, lds, offset, 0);
-        base += on ? step : 0;
-        block += on ? block_step : 0;
+            load_to_lds<0>(buffer, lds, this->offset(), 0);
+        this->advance(on);
     }
 };
 // The scales of rows [row, row + F) of the tile, in two parts: the words from where they were put, and what they say.  `pick`: which of
-// its word's four is the tile's (the wave's rows lie within one); 4: rows have their own.
+// its word's four all rows share (the wave's rows lie within one 128); 4: rows have their own.
 template <int SCALE, int F>
 struct ScaleWords {
     typedef typename std::conditional<SCALE == CNR_SCALE_E8M0, uint32_t, f32x4>::type Word;
@@ -517,7 +505,7 @@ __global__ void __launch_bounds__(WM * WN * kWave, 2) tile_kernel(const ProductA
     }
     // Half of the waves bring the scales of A, half those of B: the same ones, so that all have as many loads under way.
     const bool brings_a = wave % 2 == 0;
-    ScaleStream<SCALE> stream(brings_a ? p.a_scale : p.b_scale, brings_a ? p.a_stride : p.b_stride, brings_a ? p.a_shift : p.b_shift,
+    ScaleStream<SCALE> stream(brings_a ? p.a_scale : p.b_scale, brings_a ? p.a_stride : p.b_stride, p.blocks, brings_a ? p.a_shift : p.b_shift,
                               brings_a ? m0 : n0, brings_a ? TM : TN, lane, begin);
     const uint32_t lds_at = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) uint8_t *)lds;
     // Load j of the wave's kLoads for block kb of this part of the sum into the stage at `to`; beyond its end the last block once more, which
@@ -532,14 +520,14 @@ __global__ void __launch_bounds__(WM * WN * kWave, 2) tile_kernel(const ProductA
         else
             stream.fetch(lds_at + to + (brings_a ? kScaleA : kScaleB), kb < end - 1);
     };
-    // Which of its word's four a tile's scale is, block by block (see ScaleWords), or 4 where rows have their own.
+    // Which of its word's four a shared scale is, block by block (see ScaleWords), or 4 where rows have their own.
     struct Pick {
         uint32_t now, step, own;
         __device__ __forceinline__ Pick(uint32_t kb, uint32_t shift, uint64_t stride, uint32_t row) {
             const uint32_t at = row >> 7, last = (uint32_t)stride - 1;
             own = shift ? 0 : 4;
-            step = shift ? (uint32_t)stride : 0;
-            now = shift ? kb * step + (at < last ? at : last) : 0;
+            step = shift && SCALE == CNR_SCALE_F32 ? (uint32_t)stride : 0;
+            now = step ? kb * step + (at < last ? at : last) : 0;
         }
         __device__ __forceinline__ uint32_t operator()() const { return (now & 3) | own; }
         __device__ __forceinline__ void advance() { now += step; }

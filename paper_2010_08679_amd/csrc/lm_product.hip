@@ -343,22 +343,21 @@ __device__ __forceinline__ i32x4 buffer_of(uint64_t base, uint64_t bytes) {
 
 // 64 pieces of 16 (or 4) bytes, one for each lane, from memory to `lds` and on in lane order.  Written as instructions because the
 // compiler, which cannot tell the stages of the LDS apart, would wait for them before every read of another;
-// wait_for_loads() below does, once a block.  (Nothing else here uses M0, which holds the place in LDS.)  The instruction's own offset
-// OFFSET counts for both addresses, so that four loads in a row need one M0; the buffer and `offset` make up for it.
-template <int OFFSET>
+// wait_for_loads() below does, once a block.  Each sets the place in LDS, M0, for itself.  (The compiler warns that it does not save
+// a reserved register that a statement changes; what counts is that it does not take M0 for unchanged.)
+#pragma clang diagnostic push
+#pragma clang diagnostic ignored "-Winline-asm"
 __device__ __forceinline__ void load_to_lds(const i32x4 &buffer, uint32_t lds, uint32_t offset, uint32_t all) {
-    if constexpr (OFFSET == 0)
-        asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dwordx4 %1, %2, %3 offen lds" ::"s"(lds), "v"(offset), "s"(buffer), "s"(all));
-    else
-        asm volatile("buffer_load_dwordx4 %0, %1, %2 offen offset:%3 lds" ::"v"(offset), "s"(buffer), "s"(all), "n"(OFFSET));
+    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dwordx4 %1, %2, %3 offen lds" ::"s"(lds), "v"(offset), "s"(buffer), "s"(all) : "m0");
 }
 // The same of four bytes, or of `one`, which becomes the lowest of four.
 __device__ __forceinline__ void load_bytes_to_lds(const i32x4 &buffer, uint32_t lds, uint32_t offset, uint32_t one) {
     asm volatile("s_mov_b32 m0, %0\n\ts_cmp_lg_u32 %3, 0\n\ts_cbranch_scc1 .Lone_byte_%=\n\t"
                  "buffer_load_dword %1, %2, 0 offen lds\n\ts_branch .Lloaded_%=\n"
                  ".Lone_byte_%=:\n\tbuffer_load_ubyte %1, %2, 0 offen lds\n.Lloaded_%=:" ::"s"(lds), "v"(offset), "s"(buffer), "s"(one)
-                 : "scc");
+                 : "m0", "scc");
 }
+#pragma clang diagnostic pop
 template <int LEFT>  // loads that need not have arrived
 __device__ __forceinline__ void wait_for_loads() {
     static_assert(LEFT < 64, "the counter's range");
@@ -389,7 +388,7 @@ struct ScaleStream : ScaleFetch<SCALE == CNR_SCALE_E8M0 ? 1 : 4> {
         if constexpr (SCALE == CNR_SCALE_E8M0)
             load_bytes_to_lds(buffer, lds, this->offset(), this->tiles);
         else
-            load_to_lds<0>(buffer, lds, this->offset(), 0);
+            load_to_lds(buffer, lds, this->offset(), 0);
         this->advance(on);
     }
 };
@@ -486,22 +485,21 @@ __global__ void __launch_bounds__(WM * WN * kWave, 2) tile_kernel(const ProductA
     const uint32_t begin = (uint32_t)((uint64_t)p.blocks * split / p.splits), end = (uint32_t)((uint64_t)p.blocks * (split + 1) / p.splits);
 
     // Rows beyond the matrix read its last one again.
-    constexpr uint32_t kBack = 4096;  // room for the instructions' offsets
     const uint32_t rows_a = p.m - m0 < TM ? p.m - m0 : TM, rows_b = p.n - n0 < TN ? p.n - n0 : TN;
-    const i32x4 buffer_a = buffer_of(reinterpret_cast<uint64_t>(p.a) + (uint64_t)m0 * p.row_bytes - kBack, (uint64_t)rows_a * p.row_bytes + kBack);
-    const i32x4 buffer_b = buffer_of(reinterpret_cast<uint64_t>(p.b) + (uint64_t)n0 * p.row_bytes - kBack, (uint64_t)rows_b * p.row_bytes + kBack);
+    const i32x4 buffer_a = buffer_of(reinterpret_cast<uint64_t>(p.a) + (uint64_t)m0 * p.row_bytes, (uint64_t)rows_a * p.row_bytes);
+    const i32x4 buffer_b = buffer_of(reinterpret_cast<uint64_t>(p.b) + (uint64_t)n0 * p.row_bytes, (uint64_t)rows_b * p.row_bytes);
     uint32_t from_a[LA], from_b[LB];
 #pragma unroll
     for (int j = 0; j < LA; ++j) {
         const uint32_t line = (wave * LA + j) * 4 + quarter, logical = (lane % 16) ^ (2 * line / MF % 16);
         const uint32_t row = 2 * line + logical / 8;
-        from_a[j] = (row < rows_a ? row : rows_a - 1) * (uint32_t)p.row_bytes + logical % 8 * 16 + kBack - j % 4 * 1024;
+        from_a[j] = (row < rows_a ? row : rows_a - 1) * (uint32_t)p.row_bytes + logical % 8 * 16;
     }
 #pragma unroll
     for (int j = 0; j < LB; ++j) {
         const uint32_t line = (wave * LB + j) * 4 + quarter, logical = (lane % 16) ^ (2 * line / NF % 16);
         const uint32_t row = 2 * line + logical / 8;
-        from_b[j] = (row < rows_b ? row : rows_b - 1) * (uint32_t)p.row_bytes + logical % 8 * 16 + kBack - j % 4 * 1024;
+        from_b[j] = (row < rows_b ? row : rows_b - 1) * (uint32_t)p.row_bytes + logical % 8 * 16;
     }
     // Half of the waves bring the scales of A, half those of B: the same ones, so that all have as many loads under way.
     const bool brings_a = wave % 2 == 0;
@@ -514,9 +512,9 @@ __global__ void __launch_bounds__(WM * WN * kWave, 2) tile_kernel(const ProductA
         constexpr int J = decltype(index)::value;
         const uint32_t at = (kb < end - 1 ? kb : end - 1) * CNR_BLOCK;
         if constexpr (J < LA)
-            load_to_lds<J % 4 * 1024>(buffer_a, lds_at + to + (wave * LA + J) * 1024, from_a[J], at);
+            load_to_lds(buffer_a, lds_at + to + (wave * LA + J) * 1024, from_a[J], at);
         else if constexpr (J < LA + LB)
-            load_to_lds<(J - LA) % 4 * 1024>(buffer_b, lds_at + to + kB + (wave * LB + J - LA) * 1024, from_b[J - LA], at);
+            load_to_lds(buffer_b, lds_at + to + kB + (wave * LB + J - LA) * 1024, from_b[J - LA], at);
         else
             stream.fetch(lds_at + to + (brings_a ? kScaleA : kScaleB), kb < end - 1);
     };

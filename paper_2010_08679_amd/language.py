@@ -25,9 +25,9 @@ def _on(stream):
 class _Holder:
     """What keeps device memory from one call to the next, made on the current stream and used on the streams that calls name."""
 
-    def _holds(self, device, tensors) -> None:
+    def _holds(self, tensors) -> None:
         self._held, self._used_on = list(tensors), set()
-        self._made_on = torch.cuda.current_stream(device) if torch.device(device).type == "cuda" else None
+        self._made_on = next((torch.cuda.current_stream(t.device) for t in self._held if t.is_cuda), None)
 
     def _hold(self, tensor):
         """One more, allocated by a call."""
@@ -130,7 +130,7 @@ class BlockLinear(_Holder):
         self._input_t = None
         self._sized = {}
         self._spaces = []  # workspaces, the last one the largest; earlier ones stay, since captured graphs may hold them
-        self._holds(device, (self.weight.codes, self.weight.scale, self.weight_t.codes, self.weight_t.scale, *self._x, *self._x_t, *self._dy, *self._dy_t))
+        self._holds((self.weight.codes, self.weight.scale, self.weight_t.codes, self.weight_t.scale, *self._x, *self._x_t, *self._dy, *self._dy_t))
 
     def _buffers(self, n_rows: int, dim: int):
         m = BlockMatrix.empty(n_rows, dim, L.CNR_BLOCK_ROW, self.scale_type, self.device)
@@ -203,7 +203,7 @@ class TokenLedger(_Holder):
         words = (self.vocab + 31) // 32
         self.seen = torch.zeros(n_slots, words, dtype=torch.int32, device=device) if seen is None else seen
         self.counts = torch.zeros(n_slots, vocab, dtype=torch.int32, device=device) if counts is None and seen is None else counts
-        self._holds(device, [t for t, given in ((self.seen, seen), (self.counts, counts)) if given is None and t is not None])
+        self._holds([t for t, given in ((self.seen, seen), (self.counts, counts)) if given is None and t is not None])
 
     def count(self, tokens: torch.Tensor, offsets: torch.Tensor | None = None, slots: torch.Tensor | None = None, prompt: bool = False,
               restart: bool = False, stream=None) -> None:

@@ -95,6 +95,12 @@ def test_a_ledger_waits_for_the_state_that_it_made(monkeypatch):
         assert side.waited_for == [ledger._made_on] and len(seen.recorded) == own
 
 
+def test_a_ledger_of_given_state_has_no_stream_of_its_own():
+    given = torch.zeros(2, 2, dtype=torch.int32)
+    ledger = P.TokenLedger(None, 2, 40, given)  # wherever it is, without a GPU too
+    assert ledger.seen is given and ledger.counts is None and ledger._made_on is None
+
+
 @pytest.mark.gpu
 def test_results_on_another_stream_while_the_current_one_is_busy():
     # memory that work on the current stream still uses is free to that stream's next allocations only

@@ -42,7 +42,7 @@ typedef enum {
 } cnr_block_kind;
 
 #define CNR_BLOCK 128u
-#define CNR_LM_MAX_SIZE 2147483647u /* rows, columns, tokens of a vocabulary: CNR_E_TOO_LARGE beyond */
+#define CNR_LM_MAX_SIZE 2147483647u /* rows, columns, tokens of a vocabulary, slots, masks: CNR_E_TOO_LARGE beyond */
 
 /* Sizes (pure host arithmetic). */
 size_t cnr_block_row_bytes(uint64_t dim);                            /* dim rounded up to a multiple of 128 */

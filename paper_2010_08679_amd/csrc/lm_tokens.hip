@@ -465,7 +465,7 @@ cnr_status cnr_adjust_logits(cnr_ctx *ctx, const void *logits, uint64_t stride, 
                              void *stream) {
     if (!ctx || !adjustments || !cnr_valid_float_type(type) || stride < vocab || out_stride < vocab) return CNR_E_INVALID;
     const cnr_adjustments &w = *adjustments;
-    if (vocab > CNR_LM_MAX_SIZE || n > CNR_LM_MAX_SIZE) return CNR_E_TOO_LARGE;
+    if (vocab > CNR_LM_MAX_SIZE || n > CNR_LM_MAX_SIZE || w.n_slots > CNR_LM_MAX_SIZE || w.n_masks > CNR_LM_MAX_SIZE) return CNR_E_TOO_LARGE;
     if (n == 0 || vocab == 0) return CNR_OK;
     if (!logits || !out || (logits == out && stride != out_stride)) return CNR_E_INVALID;
     if (w.bias_offsets && w.n_bias && (!w.bias_tokens || !w.bias_values)) return CNR_E_INVALID;

@@ -203,6 +203,9 @@ class TokenLedger(_Holder):
         words = (self.vocab + 31) // 32
         self.seen = torch.zeros(n_slots, words, dtype=torch.int32, device=device) if seen is None else seen
         self.counts = torch.zeros(n_slots, vocab, dtype=torch.int32, device=device) if counts is None and seen is None else counts
+        for t, width, name in ((self.seen, words, "seen"), (self.counts, self.vocab, "counts")):
+            if t is not None and t.dim() > 1 and t.shape[-1] != width:
+                raise ValueError("the rows of %s hold %d entries, not %d" % (name, width, t.shape[-1]))
         self._holds([t for t, given in ((self.seen, seen), (self.counts, counts)) if given is None and t is not None])
 
     def count(self, tokens: torch.Tensor, offsets: torch.Tensor | None = None, slots: torch.Tensor | None = None, prompt: bool = False,
@@ -217,6 +220,8 @@ class TokenLedger(_Holder):
         is None."""
         if logits.shape[1] != self.vocab:
             raise ValueError("logits of %d tokens, a vocabulary of %d" % (logits.shape[1], self.vocab))
+        if masks is not None and (masks.dim() != 2 or masks.shape[1] != (self.vocab + 31) // 32):
+            raise ValueError("masks must be [n_masks, %d]" % ((self.vocab + 31) // 32))
         self._use(stream)
         out = logits if out is None else out
         penalties = repetition is not None or frequency is not None or presence is not None

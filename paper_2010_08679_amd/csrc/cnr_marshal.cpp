@@ -9,6 +9,8 @@
 #include <torch/csrc/autograd/python_variable.h>
 #include <torch/csrc/utils/object_ptr.h>
 
+#include <initializer_list>
+
 namespace {
 
 constexpr Py_ssize_t kJobFields = 16;  // of cnr_table_job, each 64 bits
@@ -314,12 +316,19 @@ struct Arguments {
     }
 };
 
+// `written`: the call's results.  Autograd is told, as of torch's operations in place: what a graph has saved of them is not taken for
+// unchanged.
 template <typename Call>
-PyObject *called(const Call &call) {
+PyObject *called(const Call &call, std::initializer_list<PyObject *> written) {
     int status;
     Py_BEGIN_ALLOW_THREADS
     status = call();
     Py_END_ALLOW_THREADS
+    for (PyObject *v : written) {
+        if (status != 0 || !THPVariable_CheckExact(v)) continue;
+        const at::Tensor &t = THPVariable_Unpack(v);
+        if (!t.is_inference()) t.unsafeGetTensorImpl()->bump_version();
+    }
     return PyLong_FromLong(status);
 }
 PyObject *not_taken() {
@@ -347,7 +356,8 @@ PyObject *quantize_blocks(PyObject *, PyObject *const *args, Py_ssize_t n) {
         if (!a.good) return not_taken();
         void *stream = a.stream();
         if (!a.good) return not_taken();
-        return called([&] { return lm.quantize(ctx, pointer(x.at), x.type, x.rows, x.columns, x.stride, kind, scale_type, out.codes, out.scale, out_t.codes, out_t.scale, stream); });
+        return called([&] { return lm.quantize(ctx, pointer(x.at), x.type, x.rows, x.columns, x.stride, kind, scale_type, out.codes, out.scale, out_t.codes, out_t.scale, stream); },
+                      {args[4], args[5], args[6], args[7]});
     } catch (...) {
         return not_taken();
     }
@@ -387,7 +397,7 @@ PyObject *block_product(PyObject *, PyObject *const *args, Py_ssize_t count) {
         if (!a.good) return not_taken();
         return called([&] {
             return lm.product(ctx, x.codes, x.scale, a_kind, m, y.codes, y.scale, b_kind, n, k, scale_type, pointer(out.at), out.type, out.stride, accumulate, workspace, stream);
-        });
+        }, {args[10]});
     } catch (...) {
         return not_taken();
     }
@@ -416,7 +426,7 @@ PyObject *count_tokens(PyObject *, PyObject *const *args, Py_ssize_t count) {
         const int prompt = (int)a.natural(1), restart = (int)a.natural(1);
         void *stream = a.stream();
         if (!a.good) return not_taken();
-        return called([&] { return lm.count(ctx, seen, counts, n_slots, vocab, tokens, n_tokens, type == at::kLong, offsets, slots, n, prompt, restart, stream); });
+        return called([&] { return lm.count(ctx, seen, counts, n_slots, vocab, tokens, n_tokens, type == at::kLong, offsets, slots, n, prompt, restart, stream); }, {args[1], args[2]});
     } catch (...) {
         return not_taken();
     }
@@ -457,7 +467,7 @@ PyObject *adjust_logits(PyObject *, PyObject *const *args, Py_ssize_t count) {
         w[13] = a.list(at::kInt, n);
         void *stream = a.stream();
         if (!a.good) return not_taken();
-        return called([&] { return lm.adjust(ctx, pointer(from.at), from.stride, pointer(to.at), to.stride, from.type, n, vocab, w, stream); });
+        return called([&] { return lm.adjust(ctx, pointer(from.at), from.stride, pointer(to.at), to.stride, from.type, n, vocab, w, stream); }, {args[2]});
     } catch (...) {
         return not_taken();
     }

@@ -118,7 +118,8 @@ class BlockLinear(_Holder):
 
     The layer keeps the weight in tiles in both directions (:meth:`load`, after every change of the weight) and, from :meth:`forward` to
     :meth:`backward`, the transpose of its input.  Outputs and input gradients of 16 bits and float32 ones differ in how they are added up, see
-    :func:`block_product`; the weight's gradient is float32 unless given otherwise.  Calls of one layer belong on one stream."""
+    :func:`block_product`; the weight's gradient is float32 unless given otherwise.  It is no autograd function: its results have no history,
+    gradients are what :meth:`backward` returns.  A second :meth:`forward` takes the place of the first.  Calls of one layer belong on one stream."""
 
     def __init__(self, ctx, n_out: int, n_in: int, max_tokens: int, scale_type: int = L.CNR_SCALE_E8M0, device="cuda:0"):
         self.ctx, self.n_out, self.n_in, self.max_tokens, self.scale_type = ctx, int(n_out), int(n_in), int(max_tokens), scale_type

@@ -122,6 +122,11 @@ def _float(t, name: str) -> int:
     return _kind(_FLOATS, t, name, "float32, bfloat16 or float16")
 
 
+def _written(*tensors) -> None:
+    """Autograd learns that these were written, as of torch's operations in place: what a graph has saved of them is not taken for unchanged."""
+    torch.autograd.graph.increment_version([t for t in tensors if t is not None])
+
+
 def _listed(t, n: int, dtype, name: str) -> int:
     """Address of a list with room for n entries; 0 for None."""
     if t is not None and t.numel() < n:
@@ -151,6 +156,7 @@ def cnr_quantize_blocks(ctx, x, kind: int, scale_type: int, codes, scale, codes_
     turned = _blocked(codes_t, scale_t, dim, n_rows, kind, scale_type, "x's transpose") if codes_t is not None or scale_t is not None else (0, 0)
     _check((_lib or load()).cnr_quantize_blocks(ctx, at, _float(x, "x"), n_rows, dim, stride, kind, scale_type, *direct, *turned, _stream(stream)),
            "cnr_quantize_blocks")
+    _written(codes, scale, codes_t, scale_t)
 
 
 def cnr_block_product_workspace_bytes(ctx, m: int, n: int, k: int) -> int:
@@ -173,6 +179,7 @@ def cnr_block_product(ctx, a_codes, a_scale, a_kind: int, m: int, b_codes, b_sca
         raise ValueError("workspace smaller than cnr_block_product_workspace_bytes")
     _check((_lib or load()).cnr_block_product(ctx, *a, a_kind, m, *b, b_kind, n, k, scale_type, to, _float(out, "out"), stride,
                                     int(accumulate), B._dev(workspace, None, "workspace"), _stream(stream)), "cnr_block_product")
+    _written(out)
 
 
 def cnr_count_tokens(ctx, seen, counts, n_slots: int, vocab: int, tokens, offsets=None, slots=None, prompt: bool = False,
@@ -188,6 +195,7 @@ def cnr_count_tokens(ctx, seen, counts, n_slots: int, vocab: int, tokens, offset
                                    n_slots, vocab, B._dev(tokens, None, "tokens"), tokens.numel(),
                                    _kind(_INDICES, tokens, "tokens", "int32 or int64"), B._dev(offsets, U64, "offsets"),
                                    _listed(slots, n, U32, "slots"), n, int(prompt), int(restart), _stream(stream)), "cnr_count_tokens")
+    _written(seen, counts)
 
 
 def cnr_adjust_logits(ctx, logits, out, seen=None, counts=None, n_slots: int = 0, slots=None, repetition=None, frequency=None, presence=None,
@@ -217,3 +225,4 @@ def cnr_adjust_logits(ctx, logits, out, seen=None, counts=None, n_slots: int = 0
         _listed(masks, n_masks * words, U32, "masks"), n_masks, _listed(mask_of, n, U32, "mask_of"))
     _check((_lib or load()).cnr_adjust_logits(ctx, at, stride, to, out_stride, _float(logits, "logits"), n, vocab, ctypes.byref(given), _stream(stream)),
            "cnr_adjust_logits")
+    _written(out)

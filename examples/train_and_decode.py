@@ -1,5 +1,6 @@
-"""A small language model trained, checkpointed and served: an embedding table whose touched rows are tracked and saved, an output
-layer in 8-bit blocks, and decoding with penalties and a grammar's masks.
+"""A small language model trained, checkpointed and served: an embedding table and the matrix that gives the logits, whose touched rows are
+tracked and saved, an output layer in 8-bit blocks, and decoding with penalties and a grammar's masks, by the model in memory and by one that
+is resumed from nothing but the checkpoints.
 
 The data are chains token -> (7 token + 3) mod vocabulary.  Run on an MI355X:  python examples/train_and_decode.py
 """
@@ -14,13 +15,13 @@ import paper_2010_08679_amd as P  # noqa: E402
 VOCAB, DIM, TOKENS = 500, 128, 1024
 
 
-def train(ctx, table, head, steps, checkpointer, seed=0):
-    """`steps` steps on the cross-entropy of the next token; the losses.  The table's updates are sparse and tracked, the head's dense."""
+def train(ctx, table, head, steps, table_checkpointer, head_checkpointer, seed=0):
+    """`steps` steps on the cross-entropy of the next token; the losses.  The table's updates are sparse, the head's dense; both are tracked."""
     g = torch.Generator(device=table.device).manual_seed(seed)
     layer = P.BlockLinear(ctx, VOCAB, DIM, TOKENS)
     logits = torch.empty(TOKENS, VOCAB, dtype=torch.bfloat16, device=table.device)
     dx, dw = torch.empty(TOKENS, DIM, dtype=torch.bfloat16, device=table.device), torch.empty_like(head)
-    losses = []
+    losses, every_row = [], torch.arange(VOCAB, device=table.device)
     for _ in range(steps):
         now = torch.randint(0, VOCAB, (TOKENS,), generator=g, device=table.device)
         after = (7 * now + 3) % VOCAB
@@ -32,7 +33,8 @@ def train(ctx, table, head, steps, checkpointer, seed=0):
         layer.backward(p.bfloat16(), dx, dw)
         head -= 0.02 * dw
         table.index_add_(0, now, dx.float(), alpha=-0.02)
-        checkpointer.mark(now)
+        table_checkpointer.mark(now)
+        head_checkpointer.mark(every_row)
     return losses
 
 
@@ -69,15 +71,18 @@ def main(device="cuda:0", steps=150):
     g = torch.Generator(device=device).manual_seed(1)
     table = torch.randn(VOCAB, DIM, generator=g, device=device) * 0.1
     head = torch.randn(VOCAB, DIM, generator=g, device=device) * 0.1
-    stale = table.clone()
-    ck = P.TableCheckpointer(ctx, VOCAB, DIM)
-    ck.clear()
-    losses = train(ctx, table, head, steps, ck)
-    ck.compact()
-    ck.restore(stale, ck.encode(table, ck.alloc_output(bits=8)))
+    resumed = [table.clone(), head.clone()]  # as they were before training, when the last full checkpoint was taken
+    checkpointers = [P.TableCheckpointer(ctx, VOCAB, DIM, device=device) for _ in resumed]
+    for ck in checkpointers:
+        ck.clear()
+    losses = train(ctx, table, head, steps, *checkpointers)
+    for ck, trained, stale in zip(checkpointers, (table, head), resumed):
+        ck.compact()
+        ck.restore(stale, ck.encode(trained, ck.alloc_output(bits=8)))
     prompts = [[5], [9, 66], [100, 203, 424]]
     results = {"losses": losses, "written": decode(ctx, table, head, prompts, 12, forbidden=[38]),
-               "resumed": decode(ctx, stale, head, prompts, 12, forbidden=[38]), "prompts": prompts, "errors": P.cnr_poll_errors(ctx)}
+               "resumed": decode(ctx, *resumed, prompts, 12, forbidden=[38]), "prompts": prompts, "errors": P.cnr_poll_errors(ctx),
+               "trained_matrices": (table, head), "resumed_matrices": tuple(resumed)}
     P.cnr_destroy(ctx)
     return results
 

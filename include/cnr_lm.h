@@ -1,7 +1,7 @@
 /*
- * cnr_lm.h -- operators for language models next to the checkpoint path of cnr.h: a token embedding
- * table is also the matrix whose product with the hidden states gives the logits, so the program that
- * tracks and checkpoints the table multiplies with it, in training and in serving.
+ * cnr_lm.h -- operators for language models next to the checkpoint path of cnr.h: a token embedding is a
+ * table like those, and so is the matrix whose product with the hidden states gives the logits (often the same
+ * one); the program that tracks and checkpoints them multiplies with them, in training and in serving.
  *
  *   cnr_quantize_blocks   a matrix to 8-bit floating point with a scale for each block of 128, and its
  *                         transpose for the backward pass

@@ -908,7 +908,7 @@ cnr_status cnr_block_product(cnr_ctx *ctx, const uint8_t *a_codes, const void *a
     if (m > CNR_LM_MAX_SIZE || n > CNR_LM_MAX_SIZE || k > CNR_LM_MAX_SIZE) return CNR_E_TOO_LARGE;
     if (m == 0 || n == 0 || (k == 0 && accumulate)) return CNR_OK;
     // more outputs or codes than a GPU holds
-    if (cnr_ceil_div(m, 128) * cnr_ceil_div(n, 128) >= 1u << 24 || (m > 64 && k >= (1u << 24) - CNR_BLOCK && m > 1u << 19)) return CNR_E_TOO_LARGE;
+    if (cnr_ceil_div(m, 128) * cnr_ceil_div(n, 128) >= 1u << 24 || (k >= (1u << 24) - CNR_BLOCK && m > 1u << 19)) return CNR_E_TOO_LARGE;
     if (!out || (k && (!a_codes || !a_scale || !b_codes || !b_scale))) return CNR_E_INVALID;
     if (!cnr_aligned(a_codes, 16) || !cnr_aligned(a_scale, 16) || !cnr_aligned(b_codes, 16) || !cnr_aligned(b_scale, 16) ||
         !cnr_aligned(out, cnr_float_bytes(out_type)) || !cnr_aligned(workspace, 16))

@@ -182,7 +182,7 @@ __device__ __forceinline__ void sum_any_range(const ProductArgs &p, const uint32
 //
 // A workgroup has 16 MF x 16 NF outputs; each of its waves takes a quarter of the columns, U blocks at a time so that enough loads are
 // under way, straight into the matrix instructions' registers; they add up their sums in LDS at the end.  Bound by reading B: 1 x 131072 x 4096
-// 88 us (6.1 TB/s), 1 x 32000 x 4096 25.5; with every fourth block to a wave 97 and 28.
+// 86 us (6.2 TB/s), 1 x 32000 x 4096 22.4; with every fourth block to a wave a tenth more.
 // (Waves on a SIMD: as many as the loop leaves room for, which sum_any_range would take from them.)
 template <int SCALE, bool FULL, int MF, int NF, int U>
 __global__ void __launch_bounds__(kBlock, U == 1 ? 6 : 4) narrow_kernel(const ProductArgs p) {
@@ -796,8 +796,8 @@ void tiled(const ProductArgs &p, hipStream_t s) {
 //
 // Each kernel's time for a product is estimated and the shortest taken.  A workgroup's time for a block of 128 columns, by how
 // many share a compute unit, in us; measured with 8-bit instructions; conversion or scaled sums take 1.7 times as long (1.5 to 1.85).
-// 8192^3 with each (bfloat16, powers of two): 424, 1020, 511, 656 and 862 us; 2048^3 26, 14.6, 16.3, 15.9 and 19.8; 512 x 4096 x 4096
-// 44, 20.4, 25, 22.6 and 17.6; 64 x 8192 x 8192 79, 33, 43, 40 and 21.4 (16.6 in two parts).
+// 8192^3 with each (bfloat16, powers of two): 401, 593, 492, 627 and 837 us; 2048^3 25.8, 13.4, 13.4, 15.4 and 19.0; 512 x 4096 x 4096
+// 42.9, 19.2, 23.1, 21.6 and 17.0; 64 x 8192 x 8192 82.6, 31.4, 41.7, 38.1 and 18.4 (15.5 in two parts), the narrow kernel 59.9.
 struct Tiles {
     uint32_t rows, columns, resident;  // outputs of a workgroup; workgroups on a compute unit
     float block[3];
@@ -854,7 +854,8 @@ constexpr uint64_t kNarrowRows = 1u << 19, kNarrowColumns = 1u << 27;
 
 template <bool FULL, int SCALE>
 void narrow_part(const ProductArgs &p, hipStream_t s) {
-    // Two fragments of B to a wave where that still gives every SIMD a wave: A's codes are read half as often (16 x 32000 x 4096 37 -> 30 us).
+    // Two fragments of B to a wave where that still gives every SIMD a wave: A's codes are read half as often (16 x 32000 x 4096 to bfloat16 37 -> 30 us
+    // when it was chosen, 24.6 now).
     if (p.m > 1 && p.n >= 16384)
         narrow<FULL, SCALE, 1, 2, 1>(p, s);
     else

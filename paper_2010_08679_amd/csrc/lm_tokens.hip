@@ -80,12 +80,15 @@ __global__ void __launch_bounds__(kBlock) count_kernel(const CountArgs a) {
 // A workgroup for each slice of the vocabulary of each sequence: it counts the sequence's tokens of its slice in LDS.  A sequence that
 // begins has its slice of the state written whole, without its old contents or atomics in memory, which is bound by the stores; to one that goes on the
 // counters that are not 0 are added.  The sequence's tokens are read once for each slice, from L2 but for the first.
-// 64 prompts of up to 8192 tokens, 131072 in the vocabulary: 11.0 us, of which the state's 34 MB take 7 at the rate of a copy (with an
+// 64 prompts of up to 8192 tokens, 131072 in the vocabulary: 10.2 us, of which the state's 34 MB take 7 at the rate of a copy (with an
 // atomic in memory for each token after the state is emptied 21.5).
 constexpr uint32_t kSlice = 16384;   // tokens: 64 KiB of counters, so that a CU holds two workgroups (16384 with 1024 threads 13.4 us, 8192 with 512 12.5)
 constexpr uint32_t kCounting = 512;  // threads
 constexpr uint32_t kAtOnce = 8;      // tokens that a thread loads before it counts them
-// Which kernels a call takes depends on its average number of tokens a sequence and on how many sequences there are:
+// Which kernels a call takes depends on its average number of tokens a sequence, all that the host knows of them without waiting, and on
+// how many sequences there are.  Lengths of one order are meant: a long sequence among short ones goes the short ones' way or is counted by
+// one workgroup a slice (131072 tokens that go on alone 9.6 us, among 63 of one 91; that begin 15 and 33; 2^20 tokens that begin alone 62, among
+// 63 of a hundred 217).
 constexpr uint64_t kAddFrom = 8192;       // from here on tokens are added slice by slice: 8192 x 8 9.2 us, by count_kernel 9.0; 131072 x 1 10.8 and 91; 2048 x 1 7.8 and 4.4
 constexpr uint64_t kBeginUpTo = 65536;    // up to here a state that begins is written whole: 65536 x 1 17 us, emptied and added to 17; 131072 x 1 27 and 17; 32768 x 1 11 and 12
 constexpr uint64_t kLookedThrough = 4096; // sequences with slots up to which a state that begins is written whole: each workgroup looks through all slots for its own
@@ -390,7 +393,7 @@ void adjust(const AdjustArgs &a, hipStream_t s) {
     else
         hipLaunchKernelGGL((adjust_kernel<TYPE, false, kSegments>), grid, dim3(kBlock), 0, s, a);
 }
-// 512 x 131072 bfloat16 with everything: 76 us with four segments, 84 with two; 2048 x 8000, 30 % of the tokens seen, 110 and 79.
+// bfloat16 with everything, four, two and one segments: 512 x 131072 70, 82 and 120 us; 2048 x 8000, 38 % of the tokens seen, 93, 60 and 51.
 template <int TYPE>
 void adjust(const AdjustArgs &a, const cnr_ctx *ctx, hipStream_t s) {
     if (a.vocab >= 32768 && (float)a.n * (float)a.vocab >= 8.0f * (float)ctx->n_cu * 8192.0f)

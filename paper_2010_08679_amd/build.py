@@ -42,7 +42,7 @@ def sources():
 
 
 def dependencies():
-    return sources() + sorted(glob.glob(os.path.join(CSRC, "*.h"))) + [os.path.join(ROOT, "include", h) for h in ("cnr.h", "cnr_lm.h")]
+    return sources() + sorted(glob.glob(os.path.join(CSRC, "*.h"))) + [os.path.join(ROOT, "include", h) for h in ("cnr.h", "cnr_lm.h", "cnr_loss.h")]
 
 
 def source_hash() -> str:

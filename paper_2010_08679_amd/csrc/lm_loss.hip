@@ -1,0 +1,1032 @@
+// Losses of the matrix that gives the logits, z = hidden weight^T, and their gradients, without all logits in memory.
+//
+// The softmax cross entropy of a target is the distillation from a teacher that is certain: both are
+//   loss = sum_j q_j (log q_j - z'[token_j] + lse),  z' = z / T,  lse = log sum_v exp z'_v
+//   dz_v = dloss / T (exp(z'_v - lse) - sum of q_j with token_j = v)
+// with a few (token, share) entries a row, so one machine serves them:
+//   forward   a product whose tiles leave, for each row, the largest logit and the sum of exponentials relative to it (kept to base 2: exp2 is one
+//             instruction), and one workgroup a row that joins them, takes the entries' logits as dot products and writes the loss;
+//   backward  for a piece of the vocabulary at a time, the logits once more, turned into dz in the epilogue (written in both directions, as each of the
+//             two gradients' products wants it along its sum); the entries' own dz, a few a row, are put in by a kernel of its own; then
+//             dhidden += dz weight and dweight = dz^T hidden, plain products with the transposes of the piece and of the hidden states.
+// Rows that are left out, and rows whose dloss is 0, have dz = 0 and a transpose of zeros: whatever they hold reaches no gradient.
+#include "lm_dense.h"
+#include "cnr_loss.h"
+
+#include <type_traits>
+
+namespace {
+
+using dense::i32x4;
+using dense::Place;
+
+constexpr float kLog2e = 1.44269504088896340736f, kLn2 = 0.69314718055994530942f;
+
+__device__ __forceinline__ float exp2_of(float x) { return __builtin_amdgcn_exp2f(x); }
+
+// (largest exponent to base 2, sum of 2^(exponent - largest)) of some of a row's logits; (-infinity, 0) of none.
+struct Stats {
+    float top, sum;
+};
+__device__ __forceinline__ Stats join(const Stats &a, const Stats &b) {
+    const float top = __builtin_fmaxf(a.top, b.top), at = top == -__builtin_inff() ? 0.0f : top;
+    return {top, a.sum * exp2_of(a.top - at) + b.sum * exp2_of(b.top - at)};
+}
+// The same over the sixteen lanes of a row, in all of them.
+__device__ __forceinline__ float max16(float v) {
+    v = __builtin_fmaxf(v, dpp_f<0xB1>(v));
+    v = __builtin_fmaxf(v, dpp_f<0x4E>(v));
+    v = __builtin_fmaxf(v, dpp_f<0x141>(v));
+    return __builtin_fmaxf(v, dpp_f<0x140>(v));
+}
+__device__ __forceinline__ float sum16(float v) {
+    v += dpp_f<0xB1>(v);
+    v += dpp_f<0x4E>(v);
+    v += dpp_f<0x141>(v);
+    return v + dpp_f<0x140>(v);
+}
+__device__ __forceinline__ float wave_max(float v) {
+    v = max16(v);
+    v = __builtin_fmaxf(v, __shfl_xor(v, 16));
+    return __builtin_fmaxf(v, __shfl_xor(v, 32));
+}
+__device__ __forceinline__ float wave_sum(float v) {
+    v = sum16(v);
+    v += __shfl_xor(v, 16);
+    return v + __shfl_xor(v, 32);
+}
+// Stats of N logits of one row in each of sixteen lanes, of those with a set bit in `valid`; c = log2(e) / T.
+template <int N>
+__device__ __forceinline__ Stats stats16(const float (&z)[N], float c, uint32_t valid) {
+    float top = -__builtin_inff();
+#pragma unroll
+    for (int g = 0; g < N; ++g) top = __builtin_fmaxf(top, valid >> g & 1u ? z[g] : -__builtin_inff());
+    top = max16(top) * c;
+    const float at = top == -__builtin_inff() ? 0.0f : top;
+    float sum = 0.0f;
+#pragma unroll
+    for (int g = 0; g < N; ++g) sum += valid >> g & 1u ? exp2_of(__builtin_fmaf(z[g], c, -at)) : 0.0f;
+    return {top, sum16(sum)};
+}
+
+// ---- what the products' tiles do with their outputs ----------------------------------------------------------------
+
+// Stats of each row over the tile's columns.
+struct KeepStats {
+    static constexpr bool kUsesLds = true;
+    Stats *parts;      // [rows][n_parts], from the piece's first part on
+    uint32_t n_parts;
+    float c;
+    template <uint32_t TM, uint32_t TN, int WN, int MF, int NF>
+    __device__ __forceinline__ void finish(const dense::Args &p, const Place &at, const f32x4 (&acc)[MF][NF]) const {
+        Stats *lds = reinterpret_cast<Stats *>(at.lds);  // [WN][TM]
+        const uint32_t lane = tid_x() % 16, wave_n = at.column / (16 * NF);
+        uint32_t valid = 0;
+#pragma unroll
+        for (uint32_t g = 0; g < NF; ++g) valid |= at.n + g < p.n ? 1u << g : 0u;
+#pragma unroll
+        for (int i = 0; i < 4 * MF; ++i) {
+            float z[NF];
+#pragma unroll
+            for (int g = 0; g < NF; ++g) z[g] = acc[i % MF][g][i / MF];
+            const Stats s = stats16(z, c, valid);
+            if (lane == (uint32_t)i % 16) lds[wave_n * TM + at.row + i] = s;
+        }
+        __syncthreads();
+        const uint32_t row = tid_x();
+        if (row < TM && at.m0 + row < p.m) {
+            Stats s = lds[row];
+#pragma unroll
+            for (int w = 1; w < WN; ++w) s = join(s, lds[w * TM + row]);
+            parts[(uint64_t)(at.m0 + row) * n_parts + at.tile_n] = s;
+        }
+    }
+};
+
+// What the backward pass knows of a row: log2 of its sum of exponentials and dloss / T, scaled; 0: the row adds nothing.
+struct RowGradient {
+    float lse2, gradient;
+};
+
+// dz of the tile's rows and columns: [row][column] and [column][row], with zeros up to the next whole block of each.  LOW: also what the 16-bit
+// rounding left, `low` elements further on in the second, for gradients in fp32.
+template <int TYPE, bool LOW>
+struct KeepGradient {
+    static constexpr bool kUsesLds = false;
+    typedef typename Element<TYPE>::type T;
+    T *dz, *dz_t;
+    uint64_t stride, stride_t;  // of whole blocks
+    uint64_t low;
+    const RowGradient *rows;    // up to a multiple of 256
+    float c;
+    template <uint32_t TM, uint32_t TN, int WN, int MF, int NF>
+    __device__ __forceinline__ void finish(const dense::Args &p, const Place &at, f32x4 (&acc)[MF][NF]) const {
+#pragma unroll
+        for (int i = 0; i < 4 * MF; ++i) {
+            const RowGradient row = rows[at.m + i];
+#pragma unroll
+            for (int g = 0; g < NF; ++g) {
+                const float z = acc[i % MF][g][i / MF];
+                acc[i % MF][g][i / MF] = row.gradient == 0.0f || at.n + g >= p.n ? 0.0f : row.gradient * exp2_of(__builtin_fmaf(z, c, -row.lse2));
+            }
+        }
+        if (dz && at.n < stride) {
+            T *to = dz + (uint64_t)at.m * stride + at.n;
+#pragma unroll
+            for (int i = 0; i < 4 * MF; ++i) {
+                Pack<T, NF> w;
+#pragma unroll
+                for (int g = 0; g < NF; ++g) w.v[g] = Element<TYPE>::narrow(acc[i % MF][g][i / MF]);
+                if (at.m + i < p.m) *reinterpret_cast<Pack<T, NF> *>(to + (uint64_t)i * stride) = w;
+            }
+        }
+        if (!dz_t) return;
+        constexpr int kSide = 16 / sizeof(T) < 4 * MF ? 16 / sizeof(T) : 4 * MF;
+#pragma unroll
+        for (int g = 0; g < NF; ++g) {
+            if (at.n + g >= p.n) continue;
+            T *to = dz_t + (uint64_t)(at.n + g) * stride_t + at.m;
+#pragma unroll
+            for (int i = 0; i < 4 * MF; i += kSide) {
+                if (at.m + i >= stride_t) continue;
+                Pack<T, kSide> w, rest;
+#pragma unroll
+                for (int j = 0; j < kSide; ++j) {
+                    const float v = acc[(i + j) % MF][g][(i + j) / MF];
+                    w.v[j] = Element<TYPE>::narrow(v);
+                    if constexpr (LOW) rest.v[j] = Element<TYPE>::narrow(v - Element<TYPE>::wide(w.v[j]));
+                }
+                *reinterpret_cast<Pack<T, kSide> *>(to + i) = w;
+                if constexpr (LOW) *reinterpret_cast<Pack<T, kSide> *>(to + low + i) = rest;
+            }
+        }
+    }
+};
+
+// out = there + scale * product, rounded once; either may be float or TYPE.
+struct Target {
+    void *out;
+    uint64_t stride;
+    int type;
+};
+__device__ __forceinline__ float read(const Target &t, uint64_t m, uint32_t n) {
+    const uint64_t at = m * t.stride + n;
+    if (t.type == CNR_FLOAT_F32) return reinterpret_cast<const float *>(t.out)[at];
+    if (t.type == CNR_FLOAT_BF16) return (float)reinterpret_cast<const __bf16 *>(t.out)[at];
+    return (float)reinterpret_cast<const _Float16 *>(t.out)[at];
+}
+template <int N>
+__device__ __forceinline__ void read_row(const Target &t, uint64_t m, uint32_t n, uint32_t n_end, float (&v)[N]) {
+    if (n + N <= n_end) {
+        const uint64_t at = m * t.stride + n;
+        if (t.type == CNR_FLOAT_F32) {
+            const Pack<float, N> w = *reinterpret_cast<const Pack<float, N> *>(reinterpret_cast<const float *>(t.out) + at);
+#pragma unroll
+            for (int j = 0; j < N; ++j) v[j] = w.v[j];
+        } else if (t.type == CNR_FLOAT_BF16) {
+            const Pack<__bf16, N> w = *reinterpret_cast<const Pack<__bf16, N> *>(reinterpret_cast<const __bf16 *>(t.out) + at);
+#pragma unroll
+            for (int j = 0; j < N; ++j) v[j] = (float)w.v[j];
+        } else {
+            const Pack<_Float16, N> w = *reinterpret_cast<const Pack<_Float16, N> *>(reinterpret_cast<const _Float16 *>(t.out) + at);
+#pragma unroll
+            for (int j = 0; j < N; ++j) v[j] = (float)w.v[j];
+        }
+    } else {
+#pragma unroll
+        for (int j = 0; j < N; ++j) v[j] = n + j < n_end ? read(t, m, n + j) : 0.0f;
+    }
+}
+template <typename T, int N>
+__device__ __forceinline__ void write_as(T *to, uint32_t n, uint32_t n_end, const float (&v)[N]) {
+    if (n + N <= n_end) {
+        Pack<T, N> w;
+#pragma unroll
+        for (int j = 0; j < N; ++j) w.v[j] = (T)v[j];
+        *reinterpret_cast<Pack<T, N> *>(to) = w;
+    } else {
+#pragma unroll
+        for (int j = 0; j < N; ++j)
+            if (n + j < n_end) to[j] = (T)v[j];
+    }
+}
+template <int N>
+__device__ __forceinline__ void write_row(const Target &t, uint64_t m, uint32_t n, uint32_t n_end, const float (&v)[N]) {
+    const uint64_t at = m * t.stride + n;
+    if (t.type == CNR_FLOAT_F32)
+        write_as(reinterpret_cast<float *>(t.out) + at, n, n_end, v);
+    else if (t.type == CNR_FLOAT_BF16)
+        write_as(reinterpret_cast<__bf16 *>(t.out) + at, n, n_end, v);
+    else
+        write_as(reinterpret_cast<_Float16 *>(t.out) + at, n, n_end, v);
+}
+
+struct KeepSum {
+    static constexpr bool kUsesLds = false;
+    Target out, there;      // there.out NULL: nothing is added
+    const float *scale;     // NULL: 1
+    float *partial;         // [splits][m][partial_stride] where sums are split
+    uint64_t partial_stride;
+    template <uint32_t TM, uint32_t TN, int WN, int MF, int NF>
+    __device__ __forceinline__ void finish(const dense::Args &p, const Place &at, const f32x4 (&acc)[MF][NF]) const {
+        if (at.n >= p.n) return;
+        const uint32_t rows = at.m < p.m ? p.m - at.m : 0;
+        if (p.splits > 1) {
+            const Target to = {partial + (uint64_t)at.split * p.m * partial_stride, partial_stride, CNR_FLOAT_F32};
+#pragma unroll
+            for (int i = 0; i < 4 * MF; ++i) {
+                float v[NF];
+#pragma unroll
+                for (int g = 0; g < NF; ++g) v[g] = acc[i % MF][g][i / MF];
+                if ((uint32_t)i < rows) write_as(reinterpret_cast<float *>(to.out) + (uint64_t)(at.m + i) * to.stride + at.n, at.n, p.n, v);
+            }
+            return;
+        }
+        const float by = scale ? *scale : 1.0f;
+        // What is added to is read for eight rows at once: one row after the other would wait for memory each time.
+#pragma unroll
+        for (int first = 0; first < 4 * MF; first += 8) {
+            float old[8][NF];
+#pragma unroll
+            for (int u = 0; u < 8; ++u) {
+#pragma unroll
+                for (int g = 0; g < NF; ++g) old[u][g] = 0.0f;
+                if (there.out && (uint32_t)(first + u) < rows) read_row(there, at.m + first + u, at.n, p.n, old[u]);
+            }
+#pragma unroll
+            for (int u = 0; u < 8; ++u) {
+                const int i = first + u;
+                float v[NF];
+#pragma unroll
+                for (int g = 0; g < NF; ++g) v[g] = __builtin_fmaf(acc[i % MF][g][i / MF], by, old[u][g]);
+                if ((uint32_t)i < rows) write_row(out, at.m + i, at.n, p.n, v);
+            }
+        }
+    }
+};
+
+// The parts of sums that were split, added up in order: four outputs of a row to a thread.
+__global__ void __launch_bounds__(kBlock) join_sums_kernel(const KeepSum k, uint32_t m, uint32_t n, uint32_t splits) {
+    const uint32_t across = (uint32_t)(k.partial_stride / 4);
+    const uint64_t at = (uint64_t)wg_x() * kBlock + tid_x();
+    if (at >= (uint64_t)m * across) return;
+    const uint32_t row = (uint32_t)(at / across), column = (uint32_t)(at % across) * 4;
+    const float *from = k.partial + (uint64_t)row * k.partial_stride + column;
+    f32x4 sum = *reinterpret_cast<const f32x4 *>(from);
+    for (uint32_t s = 1; s < splits; ++s) sum += *reinterpret_cast<const f32x4 *>(from + (uint64_t)s * m * k.partial_stride);
+    const float by = k.scale ? *k.scale : 1.0f;
+    float v[4] = {0.0f, 0.0f, 0.0f, 0.0f};
+    if (k.there.out) read_row(k.there, row, column, n, v);
+#pragma unroll
+    for (int j = 0; j < 4; ++j) v[j] = __builtin_fmaf(sum[j], by, v[j]);
+    write_row(k.out, row, column, n, v);
+}
+
+// ---- operands laid out for the products -----------------------------------------------------------------------
+
+// dst[rows][blocks of 128 bytes] = src, zeros behind it.
+template <typename T>
+__global__ void __launch_bounds__(kBlock) lay_out_kernel(const T *src, uint64_t stride, uint32_t rows, uint32_t dim, T *dst, uint32_t pieces /* of 16 bytes, a row */) {
+    constexpr uint32_t kPer = 16 / sizeof(T);
+    const uint64_t at = (uint64_t)wg_x() * kBlock + tid_x();
+    if (at >= (uint64_t)rows * pieces) return;
+    const uint32_t row = (uint32_t)(at / pieces), column = (uint32_t)(at % pieces) * kPer;
+    const T *from = src + (uint64_t)row * stride + column;
+    Pack<T, kPer> w;
+    if (column + kPer <= dim) {
+        w = *reinterpret_cast<const Pack<T, kPer> *>(from);
+    } else {
+#pragma unroll
+        for (uint32_t j = 0; j < kPer; ++j) w.v[j] = column + j < dim ? from[j] : (T)0.0f;
+    }
+    *reinterpret_cast<Pack<T, kPer> *>(dst + at * kPer) = w;
+}
+
+// dst[columns][to_stride] = the transpose of src[rows][columns], zeros behind it; rows that add nothing are zero.  64 x 64 at a time.
+template <typename T>
+__global__ void __launch_bounds__(kBlock) turn_kernel(const T *src, uint64_t stride, uint32_t rows, uint32_t columns, const RowGradient *keep, T *dst, uint64_t to_stride) {
+    constexpr uint32_t kPer = 16 / sizeof(T), kTile = 64, kAcross = kTile / kPer;
+    __shared__ T lds[kTile][kTile + 4 / sizeof(T)];
+    const uint32_t row0 = wg_x() * kTile, column0 = wg_y() * kTile;
+    for (uint32_t i = tid_x(); i < kTile * kAcross; i += kBlock) {
+        const uint32_t row = i / kAcross, column = i % kAcross * kPer;
+        const bool there = row0 + row < rows && (!keep || keep[row0 + row].gradient != 0.0f);
+        const T *from = src + (uint64_t)(row0 + row) * stride + column0 + column;
+        if (there && column0 + column + kPer <= columns) {
+            const Pack<T, kPer> w = *reinterpret_cast<const Pack<T, kPer> *>(from);
+#pragma unroll
+            for (uint32_t j = 0; j < kPer; ++j) lds[row][column + j] = w.v[j];
+        } else {
+#pragma unroll
+            for (uint32_t j = 0; j < kPer; ++j) lds[row][column + j] = there && column0 + column + j < columns ? from[j] : (T)0.0f;
+        }
+    }
+    __syncthreads();
+    for (uint32_t i = tid_x(); i < kTile * kAcross; i += kBlock) {
+        const uint32_t column = i / kAcross, row = i % kAcross * kPer;
+        if (column0 + column >= columns || row0 + row >= to_stride) continue;
+        Pack<T, kPer> w;
+#pragma unroll
+        for (uint32_t j = 0; j < kPer; ++j) w.v[j] = lds[row + j][column];
+        *reinterpret_cast<Pack<T, kPer> *>(dst + (uint64_t)(column0 + column) * to_stride + row0 + row) = w;
+    }
+}
+
+// ---- forward: few rows, operands straight from memory ------------------------------------------------------------
+//
+// A workgroup has 16 rows by 16 NF columns; each of its waves takes a quarter of the sum, U blocks at a time so that enough loads are under way, straight
+// into the matrix instructions' registers; they add up their sums in LDS.  Bound by reading the weight.
+struct NarrowArgs {
+    const void *hidden, *weight;
+    uint64_t hidden_stride, weight_stride;  // elements
+    uint32_t n, vocab, dim;
+    Stats *parts;
+    uint32_t n_parts;
+    float c;
+};
+template <typename T>
+__device__ __forceinline__ dense::i32x8 load_fragment(const T *row, uint32_t at, uint32_t dim) {
+    constexpr uint32_t kPer = 16 / sizeof(T);
+    i32x4 part[2];
+#pragma unroll
+    for (uint32_t h = 0; h < 2; ++h) {
+        const uint32_t from = at + h * 4 * kPer;
+        if (from + kPer <= dim) {
+            part[h] = __builtin_bit_cast(i32x4, load16(row + from));
+        } else {
+            Pack<T, kPer> w;
+#pragma unroll
+            for (uint32_t j = 0; j < kPer; ++j) w.v[j] = from + j < dim ? row[from + j] : (T)0.0f;
+            part[h] = __builtin_bit_cast(i32x4, w);
+        }
+    }
+    return __builtin_shufflevector(part[0], part[1], 0, 1, 2, 3, 4, 5, 6, 7);
+}
+template <int TYPE, int NF, int U>
+__global__ void __launch_bounds__(kBlock, 4) narrow_kernel(const NarrowArgs p) {
+    typedef typename Element<TYPE>::type T;
+    constexpr uint32_t kPer = 16 / sizeof(T), kColumns = dense::kBlockBytes / sizeof(T);
+    __shared__ f32x4 sums[kWavesPerBlock][NF][kWave];
+    const uint32_t lane = tid_x() % kWave, wave = (uint32_t)__builtin_amdgcn_readfirstlane((int)(tid_x() / kWave));
+    const uint32_t quarter = lane / 16, m0 = wg_y() * 16, n0 = wg_x() * 16 * NF;
+    // Rows beyond the matrix read its last one again.
+    const uint32_t row = m0 + lane % 16 < p.n ? m0 + lane % 16 : p.n - 1;
+    const T *a = reinterpret_cast<const T *>(p.hidden) + row * p.hidden_stride, *b[NF];
+#pragma unroll
+    for (int g = 0; g < NF; ++g) {
+        const uint32_t v = n0 + 16 * g + lane % 16;
+        b[g] = reinterpret_cast<const T *>(p.weight) + (uint64_t)(v < p.vocab ? v : p.vocab - 1) * p.weight_stride;
+    }
+    f32x4 acc[NF];
+#pragma unroll
+    for (int g = 0; g < NF; ++g) acc[g] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+    const uint32_t blocks = (p.dim + kColumns - 1) / kColumns, each = (blocks + kWavesPerBlock - 1) / kWavesPerBlock, begin = wave * each;
+    const uint32_t end = begin + each < blocks ? begin + each : blocks;
+    for (uint32_t first = begin; first < end; first += U) {
+        dense::i32x8 x[U], y[U][NF];
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+            if (u && first + u >= end) break;
+            const uint32_t at = (first + u) * kColumns + quarter * kPer;
+#pragma unroll
+            for (int g = 0; g < NF; ++g) y[u][g] = load_fragment(b[g], at, p.dim);
+            x[u] = load_fragment(a, at, p.dim);
+        }
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+            if (u && first + u >= end) break;
+#pragma unroll
+            for (int g = 0; g < NF; ++g)
+                dense::unrolled<dense::Multiply<TYPE>::kParts>([&](auto h) { acc[g] = dense::Multiply<TYPE>::template part<decltype(h)::value>(x[u], y[u][g], acc[g]); });
+        }
+    }
+#pragma unroll
+    for (int g = 0; g < NF; ++g) sums[wave][g][lane] = acc[g];
+    __syncthreads();
+    // Sixteen threads to a row, each with one column of each sixteen.
+    const uint32_t m = tid_x() / 16, n = tid_x() % 16;
+    float z[NF];
+    uint32_t valid = 0;
+#pragma unroll
+    for (uint32_t g = 0; g < NF; ++g) {
+        z[g] = 0.0f;
+#pragma unroll
+        for (int w = 0; w < kWavesPerBlock; ++w) z[g] += sums[w][g][m / 4 * 16 + n][m % 4];
+        valid |= n0 + 16 * g + n < p.vocab ? 1u << g : 0u;
+    }
+    const Stats s = stats16(z, p.c, valid);
+    if (n == 0 && m0 + m < p.n) p.parts[(uint64_t)(m0 + m) * p.n_parts + wg_x()] = s;
+}
+
+// ---- forward: a row's loss -------------------------------------------------------------------------------------
+
+struct TargetArgs {
+    const void *tokens, *logits;
+    uint64_t token_stride, logit_stride;
+    uint32_t top;
+    int token_type, logit_type;
+    float temperature;
+};
+__device__ __forceinline__ int64_t token_of(const TargetArgs &t, uint64_t row, uint32_t j) {
+    const uint64_t at = row * t.token_stride + j;
+    return t.token_type == CNR_IDX_I64 ? reinterpret_cast<const int64_t *>(t.tokens)[at] : reinterpret_cast<const int32_t *>(t.tokens)[at];
+}
+__device__ __forceinline__ float logit_of(const TargetArgs &t, uint64_t row, uint32_t j) {
+    return read({const_cast<void *>(t.logits), t.logit_stride, t.logit_type}, row, j);
+}
+
+struct LossArgs {
+    const void *hidden, *weight;
+    uint64_t hidden_stride, weight_stride;
+    uint64_t vocab;
+    uint32_t dim;
+    TargetArgs targets;
+    const Stats *parts;
+    uint32_t n_parts;
+    uint64_t row0;      // of this launch
+    float *loss;
+    float *lse2, *picked, *share;  // state, or NULL
+    cnr_dev_errors *err;
+};
+// The product of two rows, over the lanes of a wave.
+template <typename T>
+__device__ __forceinline__ float dot(const T *x, const T *y, uint32_t dim) {
+    constexpr uint32_t kPer = 16 / sizeof(T);
+    float sum = 0.0f;
+    for (uint32_t at = tid_x() % kWave * kPer; at < dim; at += kWave * kPer) {
+        if (at + kPer <= dim) {
+            const Pack<T, kPer> a = *reinterpret_cast<const Pack<T, kPer> *>(x + at), b = *reinterpret_cast<const Pack<T, kPer> *>(y + at);
+#pragma unroll
+            for (uint32_t j = 0; j < kPer; ++j) sum = __builtin_fmaf((float)a.v[j], (float)b.v[j], sum);
+        } else {
+            for (uint32_t j = at; j < dim; ++j) sum = __builtin_fmaf((float)x[j], (float)y[j], sum);
+        }
+    }
+    return wave_sum(sum);
+}
+constexpr uint32_t kMaxTop = 1024;  // entries of a row
+
+template <int TYPE, bool SOFT>
+__global__ void __launch_bounds__(kBlock) loss_kernel(const LossArgs p) {
+    typedef typename Element<TYPE>::type T;
+    __shared__ Stats joined[kWavesPerBlock];
+    __shared__ float sums[kWavesPerBlock][2];
+    __shared__ int32_t token[SOFT ? kMaxTop : 1];
+    __shared__ float share[SOFT ? kMaxTop : 1];
+    const uint32_t lane = tid_x() % kWave, wave = (uint32_t)__builtin_amdgcn_readfirstlane((int)(tid_x() / kWave));
+    const uint64_t row = p.row0 + wg_x();
+    Stats s = {-__builtin_inff(), 0.0f};
+    for (uint32_t i = tid_x(); i < p.n_parts; i += kBlock) s = join(s, p.parts[(uint64_t)wg_x() * p.n_parts + i]);
+#pragma unroll
+    for (int by = 1; by < kWave; by *= 2) s = join(s, Stats{__shfl_xor(s.top, by), __shfl_xor(s.sum, by)});
+    if (lane == 0) joined[wave] = s;
+    const uint32_t top = SOFT ? p.targets.top : 1;
+    const float heat = SOFT ? p.targets.temperature : 1.0f, c = kLog2e / heat;
+    float teacher_top = 0.0f, teacher_sum = 1.0f, negative_entropy = 0.0f;
+    bool counts = true;
+    int64_t only = -1;
+    if constexpr (SOFT) {
+        // The teacher's distribution over the row's entries.
+        float largest = -__builtin_inff();
+        for (uint32_t j = tid_x(); j < top; j += kBlock) {
+            const int64_t t = token_of(p.targets, row, j);
+            const bool there = t >= 0 && (uint64_t)t < p.vocab;
+            if (t >= 0 && !there) atomicAdd(&p.err->n_bad_indices, 1ull);
+            token[j] = there ? (int32_t)t : -1;
+            const float v = there ? logit_of(p.targets, row, j) / heat : -__builtin_inff();
+            share[j] = v;
+            largest = v != v ? __builtin_inff() : __builtin_fmaxf(largest, v);  // NaN, as infinity does, makes the shares NaN
+        }
+        largest = wave_max(largest);
+        if (lane == 0) sums[wave][0] = largest;
+        __syncthreads();
+        teacher_top = sums[0][0];
+        for (int w = 1; w < kWavesPerBlock; ++w) teacher_top = __builtin_fmaxf(teacher_top, sums[w][0]);
+        counts = teacher_top != -__builtin_inff();  // else nothing is left of the row
+        float sum = 0.0f;
+        for (uint32_t j = tid_x(); j < top; j += kBlock) sum += token[j] >= 0 && counts ? expf(share[j] - teacher_top) : 0.0f;
+        sum = wave_sum(sum);
+        if (lane == 0) sums[wave][1] = sum;
+        __syncthreads();
+        teacher_sum = 0.0f;
+        for (int w = 0; w < kWavesPerBlock; ++w) teacher_sum += sums[w][1];
+        const float teacher_log = logf(teacher_sum);
+        for (uint32_t j = tid_x(); j < top; j += kBlock) {
+            const float v = share[j] - teacher_top;
+            const float q = token[j] >= 0 && counts ? expf(v) / teacher_sum : 0.0f;
+            if (q != 0.0f) negative_entropy += q * (v - teacher_log);
+            share[j] = q;
+        }
+        __syncthreads();
+    } else {
+        const int64_t t = token_of(p.targets, row, 0);
+        counts = t >= 0 && (uint64_t)t < p.vocab;
+        if (t >= 0 && !counts && tid_x() == 0) atomicAdd(&p.err->n_bad_indices, 1ull);
+        only = counts ? t : -1;
+        __syncthreads();
+    }
+    s = joined[0];
+    for (int w = 1; w < kWavesPerBlock; ++w) s = join(s, joined[w]);
+    const float lse2 = s.top + __builtin_amdgcn_logf(s.sum);  // to base 2
+    // Logits of the entries, an entry to a wave.
+    const T *x = reinterpret_cast<const T *>(p.hidden) + row * p.hidden_stride;
+    float expected = 0.0f;  // sum of share * logit
+    for (uint32_t j = wave; j < top; j += kWavesPerBlock) {
+        const int64_t t = SOFT ? token[j] : only;
+        const float q = SOFT ? share[j] : 1.0f;
+        float z = 0.0f;
+        if (t >= 0) z = dot(x, reinterpret_cast<const T *>(p.weight) + (uint64_t)t * p.weight_stride, p.dim);
+        if (t >= 0 && q != 0.0f) expected = __builtin_fmaf(q, z, expected);
+        if (p.picked && lane == 0) p.picked[row * top + j] = z;
+    }
+    if constexpr (SOFT) {
+        // For the gradient the shares of a token that comes several times are at the first of them.
+        if (p.share) {
+            for (uint32_t j = tid_x(); j < top; j += kBlock) {
+                const int32_t t = token[j];
+                float all = 0.0f;
+                bool first = t >= 0;
+                for (uint32_t i = 0; i < top; ++i) {
+                    if (token[i] != t) continue;
+                    first = first && i >= j;
+                    all += share[i];
+                }
+                p.share[row * top + j] = first && counts ? all : 0.0f;
+            }
+        }
+        negative_entropy = wave_sum(negative_entropy);
+        __syncthreads();
+        if (lane == 0) {
+            sums[wave][0] = expected;
+            sums[wave][1] = negative_entropy;
+        }
+        __syncthreads();
+        expected = negative_entropy = 0.0f;
+        for (int w = 0; w < kWavesPerBlock; ++w) {
+            expected += sums[w][0];
+            negative_entropy += sums[w][1];
+        }
+    } else if (p.share && tid_x() == 0) {
+        p.share[row] = counts ? 1.0f : 0.0f;
+    }
+    if (tid_x() == 0) {
+        // (the largest logit and the expected one are subtracted first: of a certain token little is left)
+        p.loss[row] = counts ? negative_entropy + ((s.top - expected * c) + __builtin_amdgcn_logf(s.sum)) * kLn2 : 0.0f;
+        if (p.lse2) p.lse2[row] = counts ? lse2 : __builtin_inff();
+    }
+}
+
+// ---- backward: rows and entries ---------------------------------------------------------------------------------
+
+// rows[i] up to a multiple of 256; scale = {by what dz is multiplied, its inverse}: for halves, whose range is small, the power of two that takes the
+// largest |dloss / T| to 2^13 to 2^14; 1 for the others.  One workgroup.
+__global__ void __launch_bounds__(1024) rows_kernel(const float *lse2, const float *dloss, uint64_t n, float temperature, int half, RowGradient *rows, float *scale) {
+    __shared__ float largest[16];
+    float up = 1.0f, down = 1.0f;
+    if (half) {
+        float most = 0.0f;
+        for (uint64_t i = tid_x(); i < n; i += 1024) {
+            const float g = fabsf(dloss[i] / temperature);
+            if (lse2[i] < __builtin_inff() && g < __builtin_inff()) most = __builtin_fmaxf(most, g);
+        }
+        most = wave_max(most);
+        if (tid_x() % kWave == 0) largest[tid_x() / kWave] = most;
+        __syncthreads();
+        most = largest[0];
+        for (int w = 1; w < 16; ++w) most = __builtin_fmaxf(most, largest[w]);
+        if (most > 0.0f) {
+            int e;
+            (void)frexpf(most, &e);  // most = fraction 2^e, fraction from 1/2 to 1
+            e = 14 - e;
+            e = e > 120 ? 120 : e < -120 ? -120 : e;
+            up = ldexpf(1.0f, e);
+            down = ldexpf(1.0f, -e);
+        }
+    }
+    if (tid_x() == 0) {
+        scale[0] = up;
+        scale[1] = down;
+    }
+    const uint64_t padded = (n + 255) / 256 * 256;
+    for (uint64_t i = tid_x(); i < padded; i += 1024) {
+        RowGradient r = {__builtin_inff(), 0.0f};
+        if (i < n && lse2[i] != __builtin_inff()) r = {lse2[i], dloss[i] / temperature * up};
+        rows[i] = r;
+    }
+}
+
+// dz of the entries whose tokens lie in [first, first + width): a thread for each entry.
+template <int TYPE, bool LOW>
+__global__ void __launch_bounds__(kBlock) entries_kernel(const KeepGradient<TYPE, LOW> k, const TargetArgs targets, const float *picked, const float *share, uint64_t n, uint32_t top,
+                                                         uint64_t first, uint32_t width) {
+    const uint64_t at = (uint64_t)wg_x() * kBlock + tid_x();
+    if (at >= n * top) return;
+    const float q = share[at];
+    const uint64_t row = at / top;
+    const RowGradient r = k.rows[row];
+    if (q == 0.0f || r.gradient == 0.0f) return;
+    const int64_t t = token_of(targets, row, (uint32_t)(at % top));
+    if (t < (int64_t)first || t >= (int64_t)(first + width)) return;
+    const float v = r.gradient * (exp2_of(__builtin_fmaf(picked[at], k.c, -r.lse2)) - q);
+    const uint64_t column = (uint64_t)t - first;
+    typedef typename Element<TYPE>::type T;
+    const T high = Element<TYPE>::narrow(v);
+    if (k.dz) k.dz[row * k.stride + column] = high;
+    if (k.dz_t) {
+        k.dz_t[column * k.stride_t + row] = high;
+        if constexpr (LOW) k.dz_t[k.low + column * k.stride_t + row] = Element<TYPE>::narrow(v - Element<TYPE>::wide(high));
+    }
+}
+
+// out = scale-free zeros, or left as it is: what a product over nothing leaves.
+__global__ void __launch_bounds__(kBlock) zero_kernel(const Target out, uint64_t rows, uint32_t columns) {
+    const uint64_t at = (uint64_t)wg_x() * kBlock + tid_x();
+    if (at >= rows * columns) return;
+    const float none[1] = {0.0f};
+    write_row(out, at / columns, (uint32_t)(at % columns), columns, none);
+}
+
+// ---- the host's side ------------------------------------------------------------------------------------------
+
+constexpr uint64_t kMaxRows = 1u << 20, kMaxVocabulary = 1u << 27, kMaxDim = 1u << 20;
+constexpr uint32_t kNarrowRows = 16;            // up to which the weight goes straight from memory to the matrix instructions
+constexpr uint64_t kPieceBytes = 256ull << 20;  // of a piece of the weight, of its dz twice as many
+constexpr uint64_t kStatsBytes = 512ull << 20;  // of the stats of as many rows as go at a time
+constexpr uint64_t kPartBytes = 128ull << 20;   // of sums that are split
+
+uint64_t rounded(uint64_t v, uint64_t to) { return cnr_ceil_div(v, to) * to; }
+uint32_t blocks_of(uint64_t elements, size_t element) { return (uint32_t)cnr_ceil_div(elements * element, dense::kBlockBytes); }
+
+// Whether a product can read rows of dim elements where they are.
+bool whole_rows(const void *base, uint64_t stride, uint64_t dim, uint64_t rows, size_t element) {
+    return dim && dim * element % dense::kBlockBytes == 0 && cnr_aligned(base, 16) && (rows <= 1 || stride * element % 16 == 0) && stride * element < 1u << 23;
+}
+
+// Places in a workspace, in order.
+struct Room {
+    uint64_t used = 0;
+    uint64_t take(uint64_t bytes) {
+        const uint64_t at = used;
+        used += rounded(bytes, 256);
+        return at;
+    }
+};
+
+struct Sizes {
+    uint64_t n, vocab, dim;
+    cnr_float_type type;
+    size_t element;
+    uint64_t row;       // bytes of a laid out row of dim elements, at least one block
+    uint32_t blocks;
+};
+Sizes sizes_of(uint64_t n, uint64_t vocab, uint64_t dim, cnr_float_type type) {
+    Sizes s = {n, vocab, dim, type, cnr_float_bytes(type), 0, 0};
+    s.blocks = blocks_of(dim, s.element);
+    if (s.blocks == 0) s.blocks = 1;
+    s.row = (uint64_t)s.blocks * dense::kBlockBytes;
+    return s;
+}
+
+struct ForwardPlan {
+    bool narrow;
+    uint32_t fragments;    // columns of a narrow workgroup, in sixteens
+    uint64_t rows, piece;  // at a time
+    uint32_t n_parts;      // of a row
+    dense::Plan tiles;
+    uint64_t parts, hidden, weight, bytes;  // in the workspace
+};
+ForwardPlan forward_plan(const cnr_ctx *ctx, const Sizes &s) {
+    ForwardPlan f = {};
+    f.narrow = s.n <= kNarrowRows;
+    // Two fragments of the weight to a wave where that still gives every SIMD a wave.
+    f.fragments = s.n > 1 && s.vocab >= 16384 ? 2 : 1;
+    f.tiles = dense::plan_of(ctx, s.type, s.n, s.vocab, s.blocks, 0);
+    const uint32_t columns = f.narrow ? 16 * f.fragments : dense::kTiles[f.tiles.kind].columns;
+    f.n_parts = (uint32_t)cnr_ceil_div(s.vocab, columns);
+    const uint64_t per_row = (uint64_t)f.n_parts * sizeof(Stats), most = kStatsBytes / (per_row + 1) / 256 * 256;
+    f.rows = most < 256 ? 256 : most;
+    if (f.rows > s.n) f.rows = s.n;
+    f.piece = rounded(kPieceBytes / s.row, 256);
+    if (f.piece > s.vocab) f.piece = s.vocab;
+    Room room;
+    f.parts = room.take(f.rows * per_row);
+    if (!f.narrow) {
+        f.hidden = room.take(f.rows * s.row);
+        f.weight = room.take(f.piece * s.row);
+    }
+    f.bytes = room.used;
+    return f;
+}
+
+struct BackwardPlan {
+    uint64_t piece, width;     // of the vocabulary; columns of dz, whole blocks
+    uint64_t tokens;           // rows of dz^T's rows, whole blocks
+    dense::Plan hidden, weight;
+    uint64_t scale, rows, dz, dz_t, low, hidden_t, weight_t, hidden_at, weight_at, sum, partial, bytes;
+};
+// (low_part: dweight in fp32 from 16-bit operands.)
+BackwardPlan backward_plan(const cnr_ctx *ctx, const Sizes &s, bool low_part) {
+    BackwardPlan b = {};
+    uint64_t piece = 2 * kPieceBytes / (s.n * s.element), by_weight = kPieceBytes / s.row;
+    piece = rounded(piece < by_weight ? piece : by_weight, 256);
+    if (piece == 0) piece = 256;
+    // pieces of one size
+    const uint64_t pieces = cnr_ceil_div(s.vocab, piece);
+    b.piece = rounded(cnr_ceil_div(s.vocab, pieces), 256);
+    if (b.piece > s.vocab) b.piece = s.vocab;
+    const uint64_t per_block = dense::kBlockBytes / s.element;
+    b.width = rounded(b.piece, per_block);
+    b.tokens = rounded(s.n, per_block);
+    b.hidden = dense::plan_of(ctx, s.type, s.n, s.dim, b.width / per_block, kPartBytes);
+    b.weight = dense::plan_of(ctx, s.type, b.piece, s.dim, b.tokens / per_block, kPartBytes);
+    const uint64_t across = rounded(s.dim, 4) * sizeof(float);
+    const uint64_t parts_hidden = b.hidden.splits > 1 ? b.hidden.splits * s.n * across : 0, parts_weight = b.weight.splits > 1 ? b.weight.splits * b.piece * across : 0;
+    Room room;
+    b.scale = room.take(2 * sizeof(float));
+    b.rows = room.take(rounded(s.n, 256) * sizeof(RowGradient));
+    b.dz = room.take(s.n * b.width * s.element);
+    b.low = b.piece * b.tokens;
+    b.dz_t = room.take(b.low * s.element * (low_part ? 2 : 1));
+    b.hidden_t = room.take(s.dim * b.tokens * s.element);
+    b.weight_t = room.take(s.dim * b.width * s.element);
+    b.hidden_at = room.take(s.n * s.row);
+    b.weight_at = room.take(b.piece * s.row);
+    b.sum = room.take(pieces > 1 ? s.n * s.dim * sizeof(float) : 0);
+    b.partial = room.take(parts_hidden > parts_weight ? parts_hidden : parts_weight);
+    b.bytes = room.used;
+    return b;
+}
+
+uint64_t least(uint64_t a, uint64_t b) { return a < b ? a : b; }
+// At least what the plans take for n rows or fewer: each part's largest size.
+uint64_t room_for(const Sizes &s, bool training, bool low_part) {
+    const uint64_t most_weight = least(s.vocab, rounded(kPieceBytes / s.row, 256)), small = least(s.n, 256), per_block = dense::kBlockBytes / s.element;
+    Room f;
+    const uint64_t stats = cnr_ceil_div(s.vocab, 64) * sizeof(Stats), narrow = least(s.n, kNarrowRows) * cnr_ceil_div(s.vocab, 16) * sizeof(Stats);
+    uint64_t parts = least(s.n * stats, kStatsBytes);
+    parts = parts > small * stats ? parts : small * stats;
+    f.take(parts > narrow ? parts : narrow);
+    if (s.n > kNarrowRows) {
+        f.take(s.n * s.row);
+        f.take(most_weight * s.row);
+    }
+    if (!training) return f.used;
+    Room b;
+    const uint64_t tokens = rounded(s.n, per_block), vocab = rounded(s.vocab, per_block), over = 2 * kPieceBytes + 256 * s.n * s.element;
+    b.take(2 * sizeof(float));
+    b.take(rounded(s.n, 256) * sizeof(RowGradient));
+    b.take(least(s.n * vocab * s.element, over));
+    b.take(least(tokens * s.vocab * s.element, over + per_block * most_weight * s.element) * (low_part ? 2 : 1));
+    b.take(s.dim * tokens * s.element);
+    b.take(s.dim * rounded(most_weight, per_block) * s.element);
+    b.take(s.n * s.row);
+    b.take(most_weight * s.row);
+    b.take(s.n * s.dim * sizeof(float));
+    b.take(least(dense::kMaxSplits * (s.n > most_weight ? s.n : most_weight) * rounded(s.dim, 4) * sizeof(float), kPartBytes));
+    return b.used > f.used ? b.used : f.used;
+}
+
+struct Operand {
+    const void *at;
+    uint64_t bytes;  // from row to row
+};
+// Rows as a product can read them: where they are, or laid out in `space`.
+template <typename T>
+Operand laid_out(const T *src, uint64_t stride, uint64_t rows, const Sizes &s, void *space, hipStream_t to) {
+    if (whole_rows(src, stride, s.dim, rows, sizeof(T))) return {src, stride * sizeof(T)};
+    const uint32_t pieces = (uint32_t)(s.row / 16);
+    hipLaunchKernelGGL((lay_out_kernel<T>), dim3((unsigned)cnr_ceil_div(rows * pieces, kBlock)), dim3(kBlock), 0, to, src, stride, (uint32_t)rows, (uint32_t)s.dim, (T *)space,
+                       pieces);
+    return {space, s.row};
+}
+
+template <typename T>
+void turn(const T *src, uint64_t stride, uint64_t rows, uint64_t columns, const RowGradient *keep, T *dst, uint64_t to_stride, hipStream_t to) {
+    hipLaunchKernelGGL((turn_kernel<T>), dim3((unsigned)cnr_ceil_div(to_stride, 64), (unsigned)cnr_ceil_div(columns, 64)), dim3(kBlock), 0, to, src, stride, (uint32_t)rows,
+                       (uint32_t)columns, keep, dst, to_stride);
+}
+
+TargetArgs targets_of(const cnr_targets &t) {
+    TargetArgs a;
+    a.tokens = t.tokens;
+    a.logits = t.logits;
+    a.token_stride = t.token_stride;
+    a.logit_stride = t.logit_stride;
+    a.top = (uint32_t)t.top;
+    a.token_type = t.token_type;
+    a.logit_type = t.logit_type;
+    a.temperature = t.logits ? t.temperature : 1.0f;
+    return a;
+}
+
+template <int TYPE>
+void forward(cnr_ctx *ctx, const cnr_vocabulary &v, const cnr_targets &t, float *loss, float *state, void *workspace, hipStream_t to) {
+    typedef typename Element<TYPE>::type T;
+    const Sizes s = sizes_of(v.n, v.vocab, v.dim, v.type);
+    const ForwardPlan f = forward_plan(ctx, s);
+    uint8_t *space = reinterpret_cast<uint8_t *>(workspace);
+    const T *hidden = reinterpret_cast<const T *>(v.hidden), *weight = reinterpret_cast<const T *>(v.weight);
+    LossArgs l;
+    l.targets = targets_of(t);
+    l.hidden = hidden;
+    l.weight = weight;
+    l.hidden_stride = v.hidden_stride;
+    l.weight_stride = v.weight_stride;
+    l.vocab = v.vocab;
+    l.dim = (uint32_t)v.dim;
+    l.parts = reinterpret_cast<const Stats *>(space + f.parts);
+    l.n_parts = f.n_parts;
+    l.loss = loss;
+    l.lse2 = state;
+    l.picked = state ? state + v.n : nullptr;
+    l.share = state ? state + v.n * (1 + t.top) : nullptr;
+    l.err = ctx->dev_err;
+    const float c = kLog2e / l.targets.temperature;
+    for (uint64_t row0 = 0; row0 < v.n; row0 += f.rows) {
+        const uint64_t rows = v.n - row0 < f.rows ? v.n - row0 : f.rows;
+        Stats *parts = reinterpret_cast<Stats *>(space + f.parts);
+        const T *x = hidden + row0 * v.hidden_stride;
+        if (f.n_parts == 0) {
+        } else if (f.narrow) {
+            NarrowArgs a = {x, weight, v.hidden_stride, v.weight_stride, (uint32_t)rows, (uint32_t)v.vocab, (uint32_t)v.dim, parts, f.n_parts, c};
+            const dim3 grid(f.n_parts, (unsigned)cnr_ceil_div(rows, 16));
+            if (f.fragments == 2)
+                hipLaunchKernelGGL((narrow_kernel<TYPE, 2, 2>), grid, dim3(kBlock), 0, to, a);
+            else
+                hipLaunchKernelGGL((narrow_kernel<TYPE, 1, 4>), grid, dim3(kBlock), 0, to, a);
+        } else {
+            const Operand a = laid_out(x, v.hidden_stride, rows, s, space + f.hidden, to);
+            const uint32_t columns = dense::kTiles[f.tiles.kind].columns;
+            const bool in_place = whole_rows(weight, v.weight_stride, v.dim, v.vocab, s.element);
+            const uint64_t most = in_place ? rounded((1ull << 22) / cnr_ceil_div(rows, 64) * 64, 256) : f.piece;
+            for (uint64_t v0 = 0; v0 < v.vocab; v0 += most) {
+                const uint64_t width = v.vocab - v0 < most ? v.vocab - v0 : most;
+                const Operand b = laid_out(weight + v0 * v.weight_stride, v.weight_stride, width, s, space + f.weight, to);
+                const dense::Args args = {a.at, b.at, a.bytes, b.bytes, (uint32_t)rows, (uint32_t)width, s.blocks, 1};
+                dense::launch<TYPE>(args, f.tiles.kind, KeepStats{parts + v0 / columns, f.n_parts, c}, to);
+            }
+        }
+        l.row0 = row0;
+        if (t.logits)
+            hipLaunchKernelGGL((loss_kernel<TYPE, true>), dim3((unsigned)rows), dim3(kBlock), 0, to, l);
+        else
+            hipLaunchKernelGGL((loss_kernel<TYPE, false>), dim3((unsigned)rows), dim3(kBlock), 0, to, l);
+    }
+}
+
+template <int TYPE>
+void product(const dense::Args &args, const dense::Plan &plan, KeepSum k, hipStream_t to) {
+    dense::Args a = args;
+    a.splits = plan.splits <= a.blocks ? plan.splits : 1;
+    dense::launch<TYPE>(a, plan.kind, k, to);
+    if (a.splits > 1)
+        hipLaunchKernelGGL(join_sums_kernel, dim3((unsigned)cnr_ceil_div((uint64_t)a.m * (k.partial_stride / 4), kBlock)), dim3(kBlock), 0, to, k, a.m, a.n, a.splits);
+}
+
+template <int TYPE, bool LOW>
+void backward(cnr_ctx *ctx, const cnr_vocabulary &v, const cnr_targets &t, const float *state, const float *dloss, void *dhidden, uint64_t dhidden_stride, void *dweight,
+              cnr_float_type dweight_type, uint64_t dweight_stride, bool accumulate, void *workspace, hipStream_t to) {
+    typedef typename Element<TYPE>::type T;
+    const Sizes s = sizes_of(v.n, v.vocab, v.dim, v.type);
+    const BackwardPlan b = backward_plan(ctx, s, LOW);
+    uint8_t *space = reinterpret_cast<uint8_t *>(workspace);
+    const T *hidden = reinterpret_cast<const T *>(v.hidden), *weight = reinterpret_cast<const T *>(v.weight);
+    const TargetArgs targets = targets_of(t);
+    RowGradient *rows = reinterpret_cast<RowGradient *>(space + b.rows);
+    float *scale = reinterpret_cast<float *>(space + b.scale);
+    hipLaunchKernelGGL(rows_kernel, dim3(1), dim3(1024), 0, to, state, dloss, v.n, targets.temperature, TYPE == CNR_FLOAT_F16, rows, scale);
+    T *hidden_t = reinterpret_cast<T *>(space + b.hidden_t), *weight_t = reinterpret_cast<T *>(space + b.weight_t);
+    if (dweight) turn(hidden, v.hidden_stride, v.n, v.dim, rows, hidden_t, b.tokens, to);
+    const Operand x = laid_out(hidden, v.hidden_stride, v.n, s, space + b.hidden_at, to);
+    KeepGradient<TYPE, LOW> k;
+    k.dz = dhidden ? reinterpret_cast<T *>(space + b.dz) : nullptr;
+    k.dz_t = dweight ? reinterpret_cast<T *>(space + b.dz_t) : nullptr;
+    k.stride_t = b.tokens;
+    k.low = b.low;
+    k.rows = rows;
+    k.c = kLog2e / targets.temperature;
+    KeepSum sum;
+    sum.scale = TYPE == CNR_FLOAT_F16 ? scale + 1 : nullptr;
+    sum.partial = reinterpret_cast<float *>(space + b.partial);
+    sum.partial_stride = rounded(v.dim, 4);
+    const Target between = {space + b.sum, v.dim, CNR_FLOAT_F32};
+    for (uint64_t v0 = 0; v0 < v.vocab; v0 += b.piece) {
+        const uint64_t width = v.vocab - v0 < b.piece ? v.vocab - v0 : b.piece;
+        const T *w = weight + v0 * v.weight_stride;
+        const uint32_t blocks = blocks_of(width, s.element);
+        k.stride = (uint64_t)blocks * dense::kBlockBytes / s.element;
+        const Operand y = laid_out(w, v.weight_stride, width, s, space + b.weight_at, to);
+        const dense::Plan tiles = dense::plan_of(ctx, v.type, v.n, width, s.blocks, 0);
+        dense::launch<TYPE>(dense::Args{x.at, y.at, x.bytes, y.bytes, (uint32_t)v.n, (uint32_t)width, s.blocks, 1}, tiles.kind, k, to);
+        hipLaunchKernelGGL((entries_kernel<TYPE, LOW>), dim3((unsigned)cnr_ceil_div(v.n * t.top, kBlock)), dim3(kBlock), 0, to, k, targets, state + v.n, state + v.n * (1 + t.top),
+                           v.n, (uint32_t)t.top, v0, (uint32_t)width);
+        if (dhidden) {
+            turn(w, v.weight_stride, width, v.dim, nullptr, weight_t, k.stride, to);
+            const bool first = v0 == 0, last = v0 + width == v.vocab;
+            sum.there = first ? Target{nullptr, 0, CNR_FLOAT_F32} : between;
+            sum.out = last ? Target{dhidden, dhidden_stride, v.type} : between;
+            product<TYPE>(dense::Args{k.dz, weight_t, k.stride * s.element, k.stride * s.element, (uint32_t)v.n, (uint32_t)v.dim, blocks, 1}, b.hidden, sum, to);
+        }
+        if (dweight) {
+            const Target out = {reinterpret_cast<uint8_t *>(dweight) + v0 * dweight_stride * cnr_float_bytes(dweight_type), dweight_stride, dweight_type};
+            sum.out = out;
+            sum.there = accumulate ? out : Target{nullptr, 0, CNR_FLOAT_F32};
+            const uint64_t bytes = b.tokens * s.element;
+            for (int part = 0; part < (LOW ? 2 : 1); ++part) {
+                product<TYPE>(dense::Args{k.dz_t + part * b.low, hidden_t, bytes, bytes, (uint32_t)width, (uint32_t)v.dim, (uint32_t)(bytes / dense::kBlockBytes), 1}, b.weight,
+                              sum, to);
+                sum.there = out;
+            }
+        }
+    }
+}
+
+void zeros(const Target &out, uint64_t rows, uint64_t columns, hipStream_t to) {
+    if (rows && columns) hipLaunchKernelGGL(zero_kernel, dim3((unsigned)cnr_ceil_div(rows * columns, kBlock)), dim3(kBlock), 0, to, out, rows, (uint32_t)columns);
+}
+
+cnr_status checked(const cnr_vocabulary *v, const cnr_targets *t) {
+    if (!v || !t || !cnr_valid_float_type(v->type) || (t->token_type != CNR_IDX_I32 && t->token_type != CNR_IDX_I64)) return CNR_E_INVALID;
+    if (v->hidden_stride < v->dim || v->weight_stride < v->dim || t->token_stride < t->top) return CNR_E_INVALID;
+    if (t->logits ? !cnr_valid_float_type(t->logit_type) || t->logit_stride < t->top || !(t->temperature > 0.0f) || t->temperature > 3e38f : t->top != 1) return CNR_E_INVALID;
+    if (v->n > kMaxRows || v->vocab > kMaxVocabulary || v->dim > kMaxDim || t->top > kMaxTop) return CNR_E_TOO_LARGE;
+    if (v->n && ((!t->tokens && t->top) || (v->dim && (!v->hidden || (v->vocab && !v->weight))))) return CNR_E_INVALID;
+    const size_t e = cnr_float_bytes(v->type);
+    if (!cnr_aligned(v->hidden, e) || !cnr_aligned(v->weight, e) || !cnr_aligned(t->tokens, t->token_type == CNR_IDX_I64 ? 8 : 4) ||
+        (t->logits && !cnr_aligned(t->logits, cnr_float_bytes(t->logit_type))))
+        return CNR_E_ALIGN;
+    return CNR_OK;
+}
+
+}  // namespace
+
+extern "C" {
+
+size_t cnr_loss_state_floats(uint64_t n, uint64_t top) { return n > kMaxRows || top > kMaxTop ? 0 : (size_t)(n * (1 + 2 * top)); }
+
+size_t cnr_loss_workspace_bytes(uint64_t n, uint64_t vocab, uint64_t dim, cnr_float_type type, int training, cnr_float_type dweight_type) {
+    if (n == 0 || vocab == 0 || n > kMaxRows || vocab > kMaxVocabulary || dim > kMaxDim || !cnr_valid_float_type(type)) return 0;
+    return (size_t)room_for(sizes_of(n, vocab, dim, type), training != 0, type != CNR_FLOAT_F32 && dweight_type == CNR_FLOAT_F32);
+}
+
+cnr_status cnr_vocabulary_loss(cnr_ctx *ctx, const cnr_vocabulary *vocabulary, const cnr_targets *targets, float *loss, float *state, void *workspace, size_t workspace_bytes,
+                               void *stream) {
+    if (!ctx) return CNR_E_INVALID;
+    cnr_status st = checked(vocabulary, targets);
+    if (st != CNR_OK) return st;
+    const cnr_vocabulary &v = *vocabulary;
+    if (v.n == 0) return CNR_OK;
+    if (!loss || workspace_bytes < cnr_loss_workspace_bytes(v.n, v.vocab, v.dim, v.type, 0, v.type) || (workspace_bytes && !workspace)) return CNR_E_INVALID;
+    if (!cnr_aligned(loss, 4) || !cnr_aligned(state, 4) || !cnr_aligned(workspace, 256)) return CNR_E_ALIGN;
+    if (forward_plan(ctx, sizes_of(v.n, v.vocab, v.dim, v.type)).bytes > workspace_bytes) return CNR_E_INVALID;
+    st = cnr_enter(ctx);
+    if (st != CNR_OK) return st;
+    if (v.type == CNR_FLOAT_F32)
+        forward<CNR_FLOAT_F32>(ctx, v, *targets, loss, state, workspace, as_stream(stream));
+    else if (v.type == CNR_FLOAT_BF16)
+        forward<CNR_FLOAT_BF16>(ctx, v, *targets, loss, state, workspace, as_stream(stream));
+    else
+        forward<CNR_FLOAT_F16>(ctx, v, *targets, loss, state, workspace, as_stream(stream));
+    return cnr_launch_status(ctx);
+}
+
+cnr_status cnr_vocabulary_loss_backward(cnr_ctx *ctx, const cnr_vocabulary *vocabulary, const cnr_targets *targets, const float *state, const float *dloss, void *dhidden,
+                                        uint64_t dhidden_stride, void *dweight, cnr_float_type dweight_type, uint64_t dweight_stride, int accumulate, void *workspace,
+                                        size_t workspace_bytes, void *stream) {
+    if (!ctx) return CNR_E_INVALID;
+    cnr_status st = checked(vocabulary, targets);
+    if (st != CNR_OK) return st;
+    const cnr_vocabulary &v = *vocabulary;
+    if (dhidden && dhidden_stride < v.dim) return CNR_E_INVALID;
+    if (dweight && (dweight_stride < v.dim || (dweight_type != v.type && dweight_type != CNR_FLOAT_F32))) return CNR_E_INVALID;
+    if (v.n && (!state || !dloss)) return CNR_E_INVALID;
+    const size_t needed = cnr_loss_workspace_bytes(v.n, v.vocab, v.dim, v.type, 1, dweight ? dweight_type : v.type);
+    if (workspace_bytes < needed || (needed && !workspace)) return CNR_E_INVALID;
+    if (!cnr_aligned(state, 4) || !cnr_aligned(dloss, 4) || !cnr_aligned(dhidden, cnr_float_bytes(v.type)) ||
+        (dweight && !cnr_aligned(dweight, cnr_float_bytes(dweight_type))) || !cnr_aligned(workspace, 256))
+        return CNR_E_ALIGN;
+    if (v.dim == 0 || (!dhidden && !dweight)) return CNR_OK;
+    st = cnr_enter(ctx);
+    if (st != CNR_OK) return st;
+    hipStream_t to = as_stream(stream);
+    if (v.n == 0 || v.vocab == 0) {  // sums over nothing
+        if (dhidden) zeros({dhidden, dhidden_stride, v.type}, v.n, v.dim, to);
+        if (dweight && !accumulate) zeros({dweight, dweight_stride, dweight_type}, v.vocab, v.dim, to);
+        return cnr_launch_status(ctx);
+    }
+    const bool low = dweight && dweight_type == CNR_FLOAT_F32;
+    if (backward_plan(ctx, sizes_of(v.n, v.vocab, v.dim, v.type), low && v.type != CNR_FLOAT_F32).bytes > workspace_bytes) return CNR_E_INVALID;
+    auto call = [&](auto kind, auto part) {
+        backward<decltype(kind)::value, decltype(part)::value>(ctx, v, *targets, state, dloss, dhidden, dhidden_stride, dweight, dweight_type, dweight_stride, accumulate != 0,
+                                                               workspace, to);
+    };
+    if (v.type == CNR_FLOAT_F32)
+        call(std::integral_constant<int, CNR_FLOAT_F32>(), std::false_type());
+    else if (v.type == CNR_FLOAT_BF16)
+        low ? call(std::integral_constant<int, CNR_FLOAT_BF16>(), std::true_type()) : call(std::integral_constant<int, CNR_FLOAT_BF16>(), std::false_type());
+    else
+        low ? call(std::integral_constant<int, CNR_FLOAT_F16>(), std::true_type()) : call(std::integral_constant<int, CNR_FLOAT_F16>(), std::false_type());
+    return cnr_launch_status(ctx);
+}
+
+}  // extern "C"

@@ -1,0 +1,206 @@
+// The largest logits of each row with their tokens, and the logarithm of the sum of all exponentials.
+//
+// One workgroup a row.  The largest of each thread's own elements are found along with the sum of exponentials; the top-th largest of those is at most the
+// top-th largest of all, and hardly more elements reach it than are wanted.  These are collected in LDS, in any order, and each finds its place by counting
+// those before it: keys (the value, then the lower token) are all different, so the order they were collected in does not matter.  Where too many
+// reach it (equal values, or the largest all in one thread's share), the bound is raised digit by digit first.
+#include "cnr_loss.h"
+#include "lm_common.h"
+
+namespace {
+
+constexpr uint32_t kThreads = 1024, kWaves = kThreads / kWave, kRoom = 4096;
+
+struct TopArgs {
+    const void *logits;
+    uint64_t stride;
+    uint32_t vocab, top;
+    uint64_t n;
+    int32_t *tokens;
+    void *values;
+    float *lse;
+};
+
+// In the order of the values, NaN last.
+__device__ __forceinline__ uint32_t key_of(float v) {
+    const uint32_t u = __float_as_uint(v);
+    if (v != v) return 0xffffffffu;
+    if (v == 0.0f) return 0x80000000u;
+    return u ^ ((uint32_t)((int32_t)u >> 31) | 0x80000000u);
+}
+constexpr uint32_t kInfinity = 0xff800000u;
+__device__ __forceinline__ float value_of(uint32_t key) { return __uint_as_float(key ^ (key >> 31 ? 0x80000000u : 0xffffffffu)); }
+// All of a row's keys are different, and larger ones come first.
+__device__ __forceinline__ uint64_t place_of(uint32_t key, uint32_t token) { return (uint64_t)key << 32 | (uint32_t)~token; }
+
+struct Exponentials {
+    float top, sum;
+};
+__device__ __forceinline__ Exponentials join(const Exponentials &a, const Exponentials &b) {
+    const float top = __builtin_fmaxf(a.top, b.top), at = top == -__builtin_inff() ? 0.0f : top;
+    return {top, a.sum * __expf(a.top - at) + b.sum * __expf(b.top - at)};
+}
+
+// each(element's value, token) for all of a row's elements, sixteen bytes to a thread at a time.
+template <int TYPE, typename Each>
+__device__ __forceinline__ void for_row(const typename Element<TYPE>::type *row, uint32_t vocab, const Each &each) {
+    typedef typename Element<TYPE>::type T;
+    constexpr uint32_t kPer = 16 / sizeof(T);
+    for (uint32_t at = tid_x() * kPer; at < vocab; at += kThreads * kPer) {
+        if (at + kPer <= vocab) {
+            const Pack<T, kPer> w = *reinterpret_cast<const Pack<T, kPer> *>(row + at);
+#pragma unroll
+            for (uint32_t j = 0; j < kPer; ++j) each(Element<TYPE>::wide(w.v[j]), at + j);
+        } else {
+            for (uint32_t j = at; j < vocab; ++j) each(Element<TYPE>::wide(row[j]), j);
+        }
+    }
+}
+
+struct Lds {
+    uint64_t found[kRoom];
+    uint32_t largest[kThreads];
+    uint32_t bins[256];
+    Exponentials parts[kWaves];
+    uint32_t n_found, digit, above;
+    uint32_t bound;
+};
+
+template <int TYPE>
+__global__ void __launch_bounds__(kThreads) top_kernel(const TopArgs p) {
+    typedef typename Element<TYPE>::type T;
+    __shared__ Lds lds;
+    const uint32_t lane = tid_x() % kWave, wave = (uint32_t)__builtin_amdgcn_readfirstlane((int)(tid_x() / kWave));
+    const uint64_t row_at = wg_x();
+    const T *row = reinterpret_cast<const T *>(p.logits) + row_at * p.stride;
+    const uint32_t top = p.top < p.vocab ? p.top : p.vocab;
+
+    uint32_t largest = 0;
+    Exponentials e = {-__builtin_inff(), 0.0f};
+    for_row<TYPE>(row, p.vocab, [&](float v, uint32_t) {
+        const uint32_t key = key_of(v);
+        largest = key > largest ? key : largest;
+        if (v > e.top) {
+            e.sum *= __expf(e.top - v);
+            e.top = v;
+        }
+        e.sum += v == -__builtin_inff() ? 0.0f : __expf(v - e.top);
+    });
+    lds.largest[tid_x()] = largest;
+    if (tid_x() == 0) lds.n_found = 0;
+#pragma unroll
+    for (int by = 1; by < kWave; by *= 2) e = join(e, Exponentials{__shfl_xor(e.top, by), __shfl_xor(e.sum, by)});
+    if (lane == 0) lds.parts[wave] = e;
+    __syncthreads();
+    if (wave == 0) {
+        // The largest bound that at least `top` of the threads' largest reach, to 16 bits.
+        uint32_t own[kThreads / kWave], bound = 0;
+#pragma unroll
+        for (uint32_t i = 0; i < kThreads / kWave; ++i) own[i] = lds.largest[i * kWave + lane];
+        for (uint32_t bit = 0x80000000u; bit >= 0x10000u; bit >>= 1) {
+            uint32_t reach = 0;
+#pragma unroll
+            for (uint32_t i = 0; i < kThreads / kWave; ++i) reach += (uint32_t)__popcll(__ballot(own[i] >= (bound | bit)));
+            if (reach >= top) bound |= bit;
+        }
+        if (lane == 0) lds.bound = bound;
+    } else if (wave == 1 && p.lse) {
+        e = lds.parts[0];
+        for (uint32_t w = 1; w < kWaves; ++w) e = join(e, lds.parts[w]);
+        uint32_t most = 0;
+        for (uint32_t i = lane; i < kThreads; i += kWave) most = lds.largest[i] > most ? lds.largest[i] : most;
+#pragma unroll
+        for (int by = 1; by < kWave; by *= 2) {
+            const uint32_t other = (uint32_t)__shfl_xor((int)most, by);
+            most = other > most ? other : most;
+        }
+        if (lane == 0) p.lse[row_at] = most > kInfinity ? __builtin_nanf("") : most == kInfinity ? __builtin_inff() : e.top + __logf(e.sum);
+    }
+    __syncthreads();
+    if (!p.tokens && !p.values) return;
+    uint64_t from = (uint64_t)lds.bound << 32;  // places from here on are collected
+    auto collect = [&]() {
+        for_row<TYPE>(row, p.vocab, [&](float v, uint32_t token) {
+            const uint64_t place = place_of(key_of(v), token);
+            if (place >= from) {
+                const uint32_t at = atomicAdd(&lds.n_found, 1u);
+                if (at < kRoom) lds.found[at] = place;
+            }
+        });
+        __syncthreads();
+    };
+    if (top) collect();
+    if (top && lds.n_found > kRoom) {
+        // Eight bits of the place at a time: how many have each digit behind those that are settled; the digit that the top-th place has.
+        uint64_t settled = 0;
+        uint32_t above = 0;  // places that are larger than any with these digits
+        for (int shift = 56; shift >= 0; shift -= 8) {
+            for (uint32_t i = tid_x(); i < 256; i += kThreads) lds.bins[i] = 0;
+            __syncthreads();
+            for_row<TYPE>(row, p.vocab, [&](float v, uint32_t token) {
+                const uint64_t place = place_of(key_of(v), token);
+                if (shift == 56 || place >> (shift + 8) == settled >> (shift + 8)) atomicAdd(&lds.bins[place >> shift & 255u], 1u);
+            });
+            __syncthreads();
+            if (tid_x() == 0) {
+                uint32_t more = above;
+                int digit = 255;
+                while (more + lds.bins[digit] < top) more += lds.bins[digit--];
+                lds.digit = (uint32_t)digit;
+                lds.above = more;
+                lds.n_found = 0;
+            }
+            __syncthreads();
+            const uint32_t with = lds.bins[lds.digit];
+            settled |= (uint64_t)lds.digit << shift;
+            above = lds.above;
+            __syncthreads();
+            if (above + with <= kRoom) break;
+        }
+        from = settled;
+        collect();
+    }
+    const uint32_t found = top ? lds.n_found : 0;
+    T *values = p.values ? reinterpret_cast<T *>(p.values) + row_at * p.top : nullptr;
+    int32_t *tokens = p.tokens ? p.tokens + row_at * p.top : nullptr;
+    for (uint32_t i = tid_x(); i < found; i += kThreads) {
+        const uint64_t place = lds.found[i];
+        uint32_t before = 0;
+        for (uint32_t j = 0; j < found; ++j) before += lds.found[j] > place ? 1u : 0u;
+        if (before >= top) continue;
+        const uint32_t token = ~(uint32_t)place;
+        if (tokens) tokens[before] = (int32_t)token;
+        if (values) values[before] = row[token];
+    }
+    for (uint32_t i = top + tid_x(); i < p.top; i += kThreads) {
+        if (tokens) tokens[i] = -1;
+        if (values) values[i] = (T)(-__builtin_inff());
+    }
+}
+
+}  // namespace
+
+extern "C" {
+
+cnr_status cnr_top_logits(cnr_ctx *ctx, const void *logits, uint64_t stride, cnr_float_type type, uint64_t n, uint64_t vocab, uint64_t top, int32_t *tokens, void *values,
+                          float *lse, void *stream) {
+    if (!ctx || !cnr_valid_float_type(type) || stride < vocab) return CNR_E_INVALID;
+    if (n > CNR_LM_MAX_SIZE || vocab > CNR_LM_MAX_SIZE || top > CNR_LOSS_MAX_TOP || n * kThreads >= 1ull << 32) return CNR_E_TOO_LARGE;
+    if (n == 0 || ((top == 0 || (!tokens && !values)) && !lse)) return CNR_OK;
+    if (vocab && !logits) return CNR_E_INVALID;
+    const size_t element = cnr_float_bytes(type);
+    if (!cnr_aligned(logits, element) || !cnr_aligned(values, element) || !cnr_aligned(tokens, 4) || !cnr_aligned(lse, 4)) return CNR_E_ALIGN;
+    cnr_status st = cnr_enter(ctx);
+    if (st != CNR_OK) return st;
+    const TopArgs a = {logits, stride, (uint32_t)vocab, (uint32_t)top, n, tokens, values, lse};
+    hipStream_t s = as_stream(stream);
+    if (type == CNR_FLOAT_F32)
+        hipLaunchKernelGGL((top_kernel<CNR_FLOAT_F32>), dim3((unsigned)n), dim3(kThreads), 0, s, a);
+    else if (type == CNR_FLOAT_BF16)
+        hipLaunchKernelGGL((top_kernel<CNR_FLOAT_BF16>), dim3((unsigned)n), dim3(kThreads), 0, s, a);
+    else
+        hipLaunchKernelGGL((top_kernel<CNR_FLOAT_F16>), dim3((unsigned)n), dim3(kThreads), 0, s, a);
+    return cnr_launch_status(ctx);
+}
+
+}  // extern "C"

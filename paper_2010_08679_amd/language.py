@@ -14,6 +14,7 @@ from dataclasses import dataclass
 import torch
 
 from . import lm_binding as L
+from . import loss_binding as S
 
 
 def _on(stream):
@@ -230,3 +231,92 @@ class TokenLedger(_Holder):
         L.cnr_adjust_logits(self.ctx, logits, out, seen, counts, self.n_slots if penalties else 0, slots, repetition, frequency, presence,
                             *(bias if bias is not None else (None, None, None)), masks, 0 if masks is None else masks.shape[0], mask_of, stream)
         return out
+
+
+class VocabularyLoss(_Holder):
+    """Losses of the matrix that gives the logits, ``hidden`` [n, dim] times the transpose of ``weight`` [vocab, dim], for up to max_tokens rows at a time
+    and without all logits in memory: softmax cross entropy, and distillation from up to ``top`` logits a row of a teacher.
+
+    The object keeps a workspace and, from a loss in training to :meth:`backward`, what that loss was made of: its tensors must stay as they are until then.
+    ``gradient_dtype``: the type of the weight's gradient, ``dtype`` or float32 (which costs a second product where ``dtype`` has 16 bits).
+    It is no autograd function: results have no history, gradients are what :meth:`backward` returns.  A second loss in training takes the place of the first.
+    Calls of one object belong on one stream."""
+
+    def __init__(self, ctx, vocab: int, dim: int, max_tokens: int, dtype=torch.bfloat16, top: int = 1, training: bool = True, gradient_dtype=None, device="cuda:0"):
+        self.ctx, self.vocab, self.dim, self.max_tokens, self.top = ctx, int(vocab), int(dim), int(max_tokens), int(top)
+        self.dtype, self.gradient_dtype, self.device = dtype, dtype if gradient_dtype is None else gradient_dtype, torch.device(device)
+        if dtype not in L._FLOATS or self.gradient_dtype not in (dtype, torch.float32):
+            raise TypeError("losses of float32, bfloat16 or float16, gradients of the weight in that type or float32")
+        if not 1 <= self.top <= S.CNR_LOSS_MAX_TOP:
+            raise ValueError("1 to %d entries a row" % S.CNR_LOSS_MAX_TOP)
+        space = S.cnr_loss_workspace_bytes(self.max_tokens, self.vocab, self.dim, L._FLOATS[dtype], training, L._FLOATS[self.gradient_dtype])
+        self._space = torch.empty(space, dtype=torch.uint8, device=self.device)
+        self._state = torch.empty(self.max_tokens * (1 + 2 * self.top), dtype=torch.float32, device=self.device) if training else None
+        self._last = None
+        self._holds([t for t in (self._space, self._state) if t is not None])
+
+    def _loss(self, hidden, weight, tokens, logits, temperature, out, training, stream):
+        if hidden.dim() != 2 or hidden.shape[1] != self.dim or tuple(weight.shape) != (self.vocab, self.dim):
+            raise ValueError("hidden states of %d columns and a weight of %d x %d" % (self.dim, self.vocab, self.dim))
+        if hidden.dtype != self.dtype:
+            raise TypeError("hidden must be %s, got %s" % (self.dtype, hidden.dtype))
+        if hidden.shape[0] > self.max_tokens:
+            raise ValueError("%d tokens, made for %d" % (hidden.shape[0], self.max_tokens))
+        if training and self._state is None:
+            raise ValueError("made without training")
+        self._use(stream)
+        if out is None:
+            with _on(stream):
+                out = torch.empty(hidden.shape[0], dtype=torch.float32, device=hidden.device)
+        if training:
+            self._last = None
+        S.cnr_vocabulary_loss(self.ctx, hidden, weight, tokens, logits, temperature, out, self._state if training else None, self._space, stream)
+        if training:
+            self._last = (hidden, weight, tokens, logits, temperature)
+        return out
+
+    def cross_entropy(self, hidden: torch.Tensor, weight: torch.Tensor, targets: torch.Tensor, out: torch.Tensor | None = None, training: bool = True,
+                      stream=None) -> torch.Tensor:
+        """Each row's loss (float32 [n]) for its target; 0 for negative ones, which are padding.  ``training``: :meth:`backward` follows."""
+        return self._loss(hidden, weight, targets, None, 1.0, out, training, stream)
+
+    def distill(self, hidden: torch.Tensor, weight: torch.Tensor, tokens: torch.Tensor, logits: torch.Tensor, temperature: float = 1.0,
+                out: torch.Tensor | None = None, training: bool = True, stream=None) -> torch.Tensor:
+        """Each row's divergence from a teacher whose top logits are ``logits`` [n, k] of ``tokens`` [n, k] (negative: none), both divided by
+        the temperature.  Gradients shrink with the temperature's square, which ``backward``'s argument can make up for."""
+        if tokens.dim() != 2 or tokens.shape[1] > self.top:
+            raise ValueError("tokens must be a matrix of up to %d columns" % self.top)
+        return self._loss(hidden, weight, tokens, logits, temperature, out, training, stream)
+
+    def backward(self, dloss: torch.Tensor, dhidden: torch.Tensor | None = None, dweight: torch.Tensor | None = None, accumulate: bool = False,
+                 hidden: bool = True, weight: bool = True, stream=None):
+        """The gradients (dhidden, dweight) of the last loss in training, dloss (float32 [n]) times each row's, the weight's added to ``dweight`` where
+        ``accumulate`` is set; None in the place of one that is not wanted."""
+        if self._last is None:
+            raise ValueError("no loss in training precedes")
+        x, w = self._last[:2]
+        if accumulate and (dweight is None or not weight):
+            raise ValueError("nothing to add to")
+        if weight and dweight is not None and dweight.dtype != self.gradient_dtype:
+            raise TypeError("dweight must be %s, got %s" % (self.gradient_dtype, dweight.dtype))
+        self._use(stream)
+        with _on(stream):
+            if hidden and dhidden is None:
+                dhidden = torch.empty(x.shape, dtype=x.dtype, device=x.device)
+            if weight and dweight is None:
+                dweight = torch.empty(w.shape, dtype=self.gradient_dtype, device=w.device)
+        dhidden, dweight = dhidden if hidden else None, dweight if weight else None
+        S.cnr_vocabulary_loss_backward(self.ctx, *self._last, self._state, dloss, dhidden, dweight, accumulate, self._space, stream)
+        return dhidden, dweight
+
+
+def top_logits(ctx, logits: torch.Tensor, top: int, tokens: torch.Tensor | None = None, values: torch.Tensor | None = None, lse: torch.Tensor | None = None, stream=None):
+    """The ``top`` largest of each row of ``logits`` [n, vocab], largest first and the lower token first of equal ones: (tokens int32 [n, top], their logits,
+    float32 [n] the logarithm of the sum of all exponentials).  What they are written to may be given."""
+    n = logits.shape[0]
+    with _on(stream):
+        tokens = torch.empty(n, top, dtype=torch.int32, device=logits.device) if tokens is None else tokens
+        values = torch.empty(n, top, dtype=logits.dtype, device=logits.device) if values is None else values
+        lse = torch.empty(n, dtype=torch.float32, device=logits.device) if lse is None else lse
+    S.cnr_top_logits(ctx, logits, top, tokens, values, lse, stream)
+    return tokens, values, lse

@@ -1,0 +1,151 @@
+"""ctypes binding of ``include/cnr_loss.h``: argument marshalling only, as in :mod:`lm_binding`, whose manner it has: sizes, strides and element types are
+read off the tensors, everything else has the name and the order of the C declaration.
+"""
+from __future__ import annotations
+
+import ctypes
+
+import torch
+
+from . import binding as B
+from . import lm_binding as L
+from .binding import U32, F32, _check, _stream
+
+CNR_LOSS_MAX_TOP = 1024
+
+# Every symbol include/cnr_loss.h declares.
+LOSS_EXPORTS = ("cnr_loss_state_floats", "cnr_loss_workspace_bytes", "cnr_vocabulary_loss", "cnr_vocabulary_loss_backward", "cnr_top_logits")
+
+__all__ = [*LOSS_EXPORTS, "cnr_vocabulary", "cnr_targets", "LOSS_EXPORTS", "CNR_LOSS_MAX_TOP"]
+
+
+class cnr_vocabulary(ctypes.Structure):
+    """Field for field the C struct."""
+    _fields_ = [("hidden", ctypes.c_void_p), ("hidden_stride", ctypes.c_uint64), ("weight", ctypes.c_void_p), ("weight_stride", ctypes.c_uint64),
+                ("type", ctypes.c_int), ("n", ctypes.c_uint64), ("vocab", ctypes.c_uint64), ("dim", ctypes.c_uint64)]
+
+
+class cnr_targets(ctypes.Structure):
+    """Field for field the C struct."""
+    _fields_ = [("tokens", ctypes.c_void_p), ("token_type", ctypes.c_int), ("token_stride", ctypes.c_uint64), ("top", ctypes.c_uint64),
+                ("logits", ctypes.c_void_p), ("logit_type", ctypes.c_int), ("logit_stride", ctypes.c_uint64), ("temperature", ctypes.c_float)]
+
+
+_lib = None
+
+
+def load() -> ctypes.CDLL:
+    """The library of :func:`binding.load`, with this header's functions bound."""
+    global _lib
+    if _lib is None:
+        lib = L.load()
+        vp, u64, i32, sz = ctypes.c_void_p, ctypes.c_uint64, ctypes.c_int, ctypes.c_size_t
+        sig = {
+            "cnr_loss_state_floats": (sz, [u64, u64]),
+            "cnr_loss_workspace_bytes": (sz, [u64, u64, u64, i32, i32, i32]),
+            "cnr_vocabulary_loss": (i32, [vp, ctypes.POINTER(cnr_vocabulary), ctypes.POINTER(cnr_targets), vp, vp, vp, sz, vp]),
+            "cnr_vocabulary_loss_backward": (i32, [vp, ctypes.POINTER(cnr_vocabulary), ctypes.POINTER(cnr_targets), vp, vp, vp, u64, vp, i32, u64, i32, vp, sz,
+                                                   vp]),
+            "cnr_top_logits": (i32, [vp, vp, u64, i32, u64, u64, u64, vp, vp, vp, vp]),
+        }
+        for name, (res, args) in sig.items():
+            fn = getattr(lib, name)
+            fn.restype, fn.argtypes = res, args
+        _lib = lib
+    return _lib
+
+
+def cnr_loss_state_floats(n: int, top: int) -> int:
+    return int(load().cnr_loss_state_floats(n, top))
+
+
+def cnr_loss_workspace_bytes(n: int, vocab: int, dim: int, type: int, training: bool, dweight_type: int) -> int:
+    return int(load().cnr_loss_workspace_bytes(n, vocab, dim, type, int(training), dweight_type))
+
+
+def _loss_arguments(hidden, weight, tokens, logits, temperature: float):
+    """The two structs of a loss."""
+    at, n, dim, stride = L._rows(hidden, "hidden")
+    weight_at, vocab, weight_dim, weight_stride = L._rows(weight, "weight")
+    if weight_dim != dim:
+        raise ValueError("hidden states of %d columns, a weight of %d" % (dim, weight_dim))
+    kind = L._float(hidden, "hidden")
+    if weight.dtype != hidden.dtype:
+        raise TypeError("weight must be of hidden's type, got %s and %s" % (weight.dtype, hidden.dtype))
+    if logits is None and isinstance(tokens, torch.Tensor) and tokens.dim() == 1:
+        tokens = tokens.unsqueeze(1)
+    tokens_at, rows, top, token_stride = L._rows(tokens, "tokens")
+    if rows != n or (logits is None and top != 1):
+        raise ValueError("tokens must hold %s for each of the %d rows" % ("a target" if logits is None else "a list", n))
+    token_type = L._kind(L._INDICES, tokens, "tokens", "int32 or int64")
+    logits_at, logit_type, logit_stride = 0, 0, 0
+    if logits is not None:
+        logits_at, rows, columns, logit_stride = L._rows(logits, "logits")
+        if rows != n or columns != top:
+            raise ValueError("logits must have the shape of tokens")
+        logit_type = L._float(logits, "logits")
+        if not 0.0 < temperature < 3e38:
+            raise ValueError("the temperature must be positive")
+        logits_at = logits_at or 16  # an empty matrix is none that is missing
+    return (cnr_vocabulary(at, stride, weight_at, weight_stride, kind, n, vocab, dim),
+            cnr_targets(tokens_at, token_type, token_stride, top, logits_at, logit_type, logit_stride, temperature))
+
+
+def _bytes(t) -> int:
+    return 0 if t is None else t.numel() * t.element_size()
+
+
+def cnr_vocabulary_loss(ctx, hidden, weight, tokens, logits, temperature: float, loss, state, workspace, stream=None) -> None:
+    """``tokens``: a list of targets with ``logits`` None, else a matrix as ``logits`` is; ``state`` and ``workspace`` may be None where nothing is kept or needed."""
+    v, t = _loss_arguments(hidden, weight, tokens, logits, temperature)
+    n, top = v.n, t.top
+    if top > CNR_LOSS_MAX_TOP:
+        raise ValueError("at most %d entries a row" % CNR_LOSS_MAX_TOP)
+    if loss is None or loss.numel() < n:
+        raise ValueError("loss shorter than %d" % n)
+    if state is not None and state.numel() < n * (1 + 2 * top):
+        raise ValueError("state shorter than cnr_loss_state_floats")
+    if _bytes(workspace) < cnr_loss_workspace_bytes(n, v.vocab, v.dim, v.type, False, v.type):
+        raise ValueError("workspace smaller than cnr_loss_workspace_bytes")
+    _check((_lib or load()).cnr_vocabulary_loss(ctx, ctypes.byref(v), ctypes.byref(t), B._dev(loss, F32, "loss"), B._dev(state, F32, "state"),
+                                                B._dev(workspace, None, "workspace"), _bytes(workspace), _stream(stream)), "cnr_vocabulary_loss")
+    L._written(loss, state)
+
+
+def cnr_vocabulary_loss_backward(ctx, hidden, weight, tokens, logits, temperature: float, state, dloss, dhidden, dweight, accumulate: bool, workspace,
+                                 stream=None) -> None:
+    """``dhidden`` and ``dweight``: matrices of the shapes of ``hidden`` and ``weight``, or None."""
+    v, t = _loss_arguments(hidden, weight, tokens, logits, temperature)
+    n, top = v.n, t.top
+    if top > CNR_LOSS_MAX_TOP:
+        raise ValueError("at most %d entries a row" % CNR_LOSS_MAX_TOP)
+    if state is None or state.numel() < n * (1 + 2 * top):
+        raise ValueError("state missing or shorter than cnr_loss_state_floats")
+    if dloss is None or dloss.numel() < n:
+        raise ValueError("dloss shorter than %d" % n)
+    to_hidden, to_weight, kind = (0, 0, 0, 0), (0, 0, 0, 0), v.type
+    if dhidden is not None:
+        to_hidden = L._rows(dhidden, "dhidden")
+        if dhidden.shape != hidden.shape or dhidden.dtype != hidden.dtype:
+            raise ValueError("dhidden must have the shape and type of hidden")
+    if dweight is not None:
+        to_weight, kind = L._rows(dweight, "dweight"), L._float(dweight, "dweight")
+        if dweight.shape != weight.shape or kind not in (v.type, L.CNR_FLOAT_F32):
+            raise ValueError("dweight must have the shape of weight and its type, or float32")
+    if _bytes(workspace) < cnr_loss_workspace_bytes(n, v.vocab, v.dim, v.type, True, kind):
+        raise ValueError("workspace smaller than cnr_loss_workspace_bytes")
+    _check((_lib or load()).cnr_vocabulary_loss_backward(
+        ctx, ctypes.byref(v), ctypes.byref(t), B._dev(state, F32, "state"), B._dev(dloss, F32, "dloss"), to_hidden[0], to_hidden[3], to_weight[0], kind, to_weight[3],
+        int(accumulate), B._dev(workspace, None, "workspace"), _bytes(workspace), _stream(stream)), "cnr_vocabulary_loss_backward")
+    L._written(dhidden, dweight)
+
+
+def cnr_top_logits(ctx, logits, top: int, tokens=None, values=None, lse=None, stream=None) -> None:
+    """``logits``: a matrix; ``tokens`` and ``values``: room for ``top`` entries of each row, or None."""
+    at, n, vocab, stride = L._rows(logits, "logits")
+    kind = L._float(logits, "logits")
+    if not 0 <= top <= CNR_LOSS_MAX_TOP:
+        raise ValueError("at most %d entries a row" % CNR_LOSS_MAX_TOP)
+    _check((_lib or load()).cnr_top_logits(ctx, at, stride, kind, n, vocab, top, L._listed(tokens, n * top, U32, "tokens"), L._listed(values, n * top, logits.dtype, "values"),
+                                           L._listed(lse, n, F32, "lse"), _stream(stream)), "cnr_top_logits")
+    L._written(tokens, values, lse)

@@ -1,27 +1,41 @@
-// Products of plain matrices, out[m][n] = sum over k of A[m][k] B[n][k], for kernels that do something of their own with the outputs.
+// Products of plain matrices, out[row][column] = sum over k of down[row][k] across[column][k], for kernels that do something of their own with the outputs.
 //
-// Both operands have k along their rows, as multiples of 128 bytes ("blocks"), rows a multiple of 16 bytes apart.  16-bit elements go through the
-// matrix instructions of their type, floats through the fp32 ones: products and sums are fp32's for all three.
+// Elements have 16 bits and go through the matrix instructions of their type: exact products, added up in fp32.  Each operand lies either along k (a row or
+// column of the output in a row of its own, in whole blocks of 64 elements) or across it ([k][row or column], read through the LDS's transposing
+// loads).  An operand may be held in several parts, side by side in its rows, that add up to it (a float in three bfloat16): the sum then goes over
+// pairs of parts ("terms") one after the other.
 #pragma once
 
 #include "lm_common.h"
 
 #include <math.h>
+#include <type_traits>
 
 namespace dense {
 
+typedef int i32x2 __attribute__((ext_vector_type(2)));
 typedef int i32x4 __attribute__((ext_vector_type(4)));
 typedef int i32x8 __attribute__((ext_vector_type(8)));
+typedef short s16x4 __attribute__((ext_vector_type(4)));
 typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
 typedef _Float16 f16x8 __attribute__((ext_vector_type(8)));
 
-constexpr uint32_t kBlockBytes = 128;
+constexpr uint32_t kBlockBytes = 128, kBlockElements = 64;
 
+struct Operand {
+    const void *at;       // 16-byte aligned
+    uint64_t stride;      // bytes from row to row, a multiple of 16; below 2^23 where rows lie along k
+    uint32_t row_bytes;   // of a row with all its parts, a multiple of 16; the last row ends with them
+    uint32_t part_bytes;  // from one part to the next in a row
+    uint32_t parts;       // which part each term takes, four bits a term, the first term lowest
+};
 struct Args {
-    const void *a, *b;
-    uint64_t a_bytes, b_bytes;  // from one row to the next, below 2^23
-    uint32_t m, n, blocks;      // blocks >= 1
-    uint32_t splits;            // parts of the sum, each in its own workgroups
+    Operand across, down;
+    uint32_t columns, rows;  // of the output
+    uint32_t blocks;         // along k, >= 1; operands that lie along k have as many whole blocks, of zeros where they end earlier
+    uint32_t k;              // rows of operands that lie across k; behind them zeros are read
+    uint32_t terms;          // >= 1
+    uint32_t splits;         // parts of the sum, each in its own workgroups
 };
 
 #ifdef __HIPCC__
@@ -37,31 +51,23 @@ __device__ __forceinline__ void unrolled(const Body &body) {
     }
 }
 
-// Part h of kParts of the product of 16 rows of A by 16 of B, 32 bytes of each row: lane l holds bytes of row l % 16, which ones does not matter as
-// long as both operands agree.  Sum i of a lane belongs to A's row 4 (l / 16) + i and B's row l % 16.
-template <int TYPE>
-struct Multiply {
-    static constexpr int kParts = TYPE == CNR_FLOAT_F32 ? 8 : 2;
-    template <int H>
-    static __device__ __forceinline__ f32x4 part(const i32x8 &x, const i32x8 &y, const f32x4 &sum) {
-        if constexpr (TYPE == CNR_FLOAT_F32) {
-            return __builtin_amdgcn_mfma_f32_16x16x4f32(__int_as_float(x[H]), __int_as_float(y[H]), sum, 0, 0, 0);
-        } else {
-            i32x4 a, b;
-            if constexpr (H == 0) {
-                a = __builtin_shufflevector(x, x, 0, 1, 2, 3);
-                b = __builtin_shufflevector(y, y, 0, 1, 2, 3);
-            } else {
-                a = __builtin_shufflevector(x, x, 4, 5, 6, 7);
-                b = __builtin_shufflevector(y, y, 4, 5, 6, 7);
-            }
-            if constexpr (TYPE == CNR_FLOAT_BF16)
-                return __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, a), __builtin_bit_cast(bf16x8, b), sum, 0, 0, 0);
-            else
-                return __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(f16x8, a), __builtin_bit_cast(f16x8, b), sum, 0, 0, 0);
-        }
+// Half h of the products of 16 rows by 16, 32 bytes of each: lane l holds bytes of row l % 16, which ones does not matter as long as both operands agree.
+// Sum i of a lane belongs to row 4 (l / 16) + i of x and row l % 16 of y.
+template <int TYPE, int H>
+__device__ __forceinline__ f32x4 multiply(const i32x8 &x, const i32x8 &y, const f32x4 &sum) {
+    i32x4 a, b;
+    if constexpr (H == 0) {
+        a = __builtin_shufflevector(x, x, 0, 1, 2, 3);
+        b = __builtin_shufflevector(y, y, 0, 1, 2, 3);
+    } else {
+        a = __builtin_shufflevector(x, x, 4, 5, 6, 7);
+        b = __builtin_shufflevector(y, y, 4, 5, 6, 7);
     }
-};
+    if constexpr (TYPE == CNR_FLOAT_BF16)
+        return __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, a), __builtin_bit_cast(bf16x8, b), sum, 0, 0, 0);
+    else
+        return __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(f16x8, a), __builtin_bit_cast(f16x8, b), sum, 0, 0, 0);
+}
 
 // Base and size are the same for all lanes.
 __device__ __forceinline__ i32x4 buffer_of(uint64_t base, uint64_t bytes) {
@@ -91,31 +97,118 @@ __device__ __forceinline__ void barrier() {
     asm volatile("" ::: "memory");
 }
 
-// What a workgroup's outputs are to its epilogue.  A lane holds 4 MF consecutive rows from `m` on by NF consecutive columns from `n` on: row i and
-// column g in acc[i % MF][g][i / MF].
+// What a workgroup's outputs are to its epilogue.  A lane holds 4 MF consecutive columns from `column` on, of NF rows: value(acc, i, g) is that of column
+// column + i and row row(g).
+template <int MF, int NF, bool ACROSS, bool DOWN>
 struct Place {
-    uint32_t m0, n0;        // first output of the workgroup
-    uint32_t m, n;          // of the lane
-    uint32_t row, column;   // the lane's first row and column within the workgroup's
-    uint32_t split, tile_n;
-    uint8_t *lds;           // free, as large as the stages were
+    uint32_t row0, column0;  // first output of the workgroup
+    uint32_t lane_row;       // the lane's first row within the workgroup's
+    uint32_t column;         // of the lane
+    uint32_t split, tile_column;
+    uint32_t wave_column;    // which of the WM parts of the workgroup's columns is the wave's
+    uint8_t *lds;            // free, as large as the stages were
+    // (rows from an operand across k: chunks of four rows, each to four lanes; chunks of odd lanes change places by pairs, see Across)
+    __device__ __forceinline__ uint32_t row_within(uint32_t g) const { return lane_row + (DOWN ? (g ^ (tid_x() / 4 % 2)) * 4 : g); }
+    __device__ __forceinline__ uint32_t row(uint32_t g) const { return row0 + row_within(g); }
+    static __device__ __forceinline__ float value(const f32x4 (&acc)[MF][NF], int i, int g) { return ACROSS ? acc[i / 4][g][i % 4] : acc[i % MF][g][i / MF]; }
 };
 
-// A workgroup of WM x WN waves has 16 WM MF x 16 WN NF outputs, a wave 16 MF x 16 NF of them, and walks along k a block at a time; the next
+// One operand's way from memory through LDS into fragments of 16 of its F * 16 * waves rows (T), a block of k at a time.
+//
+// Along k: fragment f of a wave holds rows F r + f of its part (r = lane % 16), so that a lane's outputs lie side by side.  LDS holds two rows of 128 bytes
+// to a line of 256, its sixteen pieces of 16 bytes permuted by r: sixteen lanes that read the same piece of their rows find it in sixteen different places,
+// all banks in use.  Memory is read straight into LDS, where a wave's 64 pieces lie in order, so the permutation is in which piece a lane asks for.
+template <int F, int T, int LOADS>
+struct Along {
+    static constexpr int kLoads = LOADS;
+    i32x4 buffer;
+    uint32_t from[LOADS];
+    uint32_t piece[2][2];  // [odd][h]
+    // Rows beyond the matrix read its last one again.
+    __device__ __forceinline__ Along(const Operand &o, uint32_t first, uint32_t count, uint32_t, uint32_t wave, uint32_t section, uint32_t region) {
+        const uint32_t lane = tid_x() % kWave, r = lane % 16, quarter = lane / 16, rows = count - first < T ? count - first : T;
+        buffer = buffer_of(reinterpret_cast<uint64_t>(o.at) + (uint64_t)first * o.stride, (uint64_t)(rows - 1) * o.stride + o.row_bytes);
+#pragma unroll
+        for (int j = 0; j < LOADS; ++j) {
+            const uint32_t line = (wave * LOADS + j) * 4 + quarter, logical = r ^ (2 * line / F % 16);
+            const uint32_t row = 2 * line + logical / 8;
+            from[j] = (row < rows ? row : rows - 1) * (uint32_t)o.stride + logical % 8 * 16;
+        }
+#pragma unroll
+        for (int i = 0; i < 4; ++i) piece[i / 2][i % 2] = region + (section + r * F) * kBlockBytes + (((quarter + 4 * (i % 2)) ^ r) * 16 ^ i / 2 * 128);
+    }
+    template <int J>
+    __device__ __forceinline__ void fetch(const Operand &, uint32_t lds, uint32_t part, uint32_t block) const {
+        load_to_lds(buffer, lds, from[J], part + block * kBlockBytes);
+    }
+    __device__ __forceinline__ void move(uint32_t by) {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) piece[i / 2][i % 2] += by;
+    }
+    __device__ __forceinline__ i32x8 fragment(const uint8_t *lds, uint32_t f) const {
+        i32x4 part[2];
+#pragma unroll
+        for (int h = 0; h < 2; ++h) part[h] = *reinterpret_cast<const i32x4 *>(lds + piece[f % 2][h] + f / 2 * 256);
+        return __builtin_shufflevector(part[0], part[1], 0, 1, 2, 3, 4, 5, 6, 7);
+    }
+};
+
+// Across k: LDS holds 64 rows of k with T columns each.  The transposing load gives a lane four rows of one column, sixteen lanes four rows of sixteen columns
+// that are four chunks of four from anywhere: chunk c of fragment f holds columns 4 F c + 4 (f ^ c % 2), so that the lanes of a chunk have 4 F columns
+// side by side between them.  Sixteen lanes thus read four chunks of 8 bytes in each of four rows; that these sixteen lie in different banks takes the other half of a piece
+// of 16 bytes for odd chunks, and pieces permuted by the row (`turned`), on the way in as in the layout along k.
+template <int F, int T, int LOADS>
+struct Across {
+    static constexpr int kLoads = LOADS;
+    static constexpr uint32_t kRow = T * 2, kPieces = T / 8;
+    uint64_t at, left;  // of the first row's first column in bytes, to the end
+    uint32_t from[LOADS];
+    uint32_t chunk;
+    static __device__ __forceinline__ uint32_t turned(uint32_t piece, uint32_t row) {
+        if constexpr (F == 8) return piece ^ 2 * (row % 4) ^ piece / 8 % 2;
+        if constexpr (F == 4) return piece ^ row % 4;
+        return piece ^ row % 2 ^ row / 2 % 2 * 4;
+    }
+    __device__ __forceinline__ Across(const Operand &o, uint32_t first, uint32_t, uint32_t k, uint32_t wave, uint32_t section, uint32_t region) {
+        static_assert(F == 8 || F == 4 || F == 2, "places in LDS");
+        const uint32_t lane = tid_x() % kWave, quarter = lane / 16, c = lane % 4, row = lane % 16 / 4;
+        at = reinterpret_cast<uint64_t>(o.at) + first * 2;
+        left = (uint64_t)(k - 1) * o.stride + o.row_bytes - first * 2;
+#pragma unroll
+        for (int j = 0; j < LOADS; ++j) {
+            const uint32_t i = (wave * LOADS + j) * kWave + lane;
+            from[j] = i / kPieces * (uint32_t)o.stride + turned(i % kPieces, i / kPieces) * 16;
+        }
+        chunk = region + (quarter * 8 + row) * kRow + turned((section + 4 * F * c) / 8, row) * 16 + c % 2 * 8;
+    }
+    // Beyond the end nothing is read, and zeros arrive.
+    template <int J>
+    __device__ __forceinline__ void fetch(const Operand &o, uint32_t lds, uint32_t part, uint32_t block) const {
+        const uint64_t on = part + (uint64_t)block * kBlockElements * o.stride;
+        load_to_lds(buffer_of(at + on, on < left ? left - on : 0), lds, from[J], 0);
+    }
+    __device__ __forceinline__ void move(uint32_t by) { chunk += by; }
+    __device__ __forceinline__ i32x8 fragment(const uint8_t *lds, uint32_t f) const {
+        typedef __attribute__((address_space(3))) s16x4 *Lds;
+        i32x2 part[4];
+        const uint8_t *from = lds + (chunk ^ f * 8);
+#pragma unroll
+        for (int h = 0; h < 4; ++h) part[h] = __builtin_bit_cast(i32x2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((Lds)(from + (h / 2 * 32 + h % 2 * 4) * kRow)));
+        const i32x4 lo = __builtin_shufflevector(part[0], part[1], 0, 1, 2, 3), hi = __builtin_shufflevector(part[2], part[3], 0, 1, 2, 3);
+        return __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7);
+    }
+};
+
+// A workgroup of WM x WN waves has 16 WM MF columns by 16 WN NF rows, a wave 16 MF by 16 NF of them, and walks along k a block at a time; the next
 // STAGES - 1 blocks travel from memory into LDS while this one's are multiplied.
 //
-// Fragment f of a wave holds rows MF r + f of its part of A (r = lane % 16), and likewise of B, so that a lane's outputs lie side by side.  LDS
-// holds two rows of 128 bytes to a line of 256, its sixteen pieces of 16 bytes permuted by r: sixteen lanes that read the same piece of their rows
-// find it in sixteen different places, all banks in use.  Memory is read straight into LDS, where a wave's 64 pieces lie in
-// order, so the permutation is in which piece a lane asks for.
-//
-// A block's products go by quarters, each half of the wave's rows of A with each half of those of B, so that half of the operands are in registers while
+// A block's products go by quarters, each half of the wave's columns with each half of its rows, so that half of the operands are in registers while
 // the other half, or the next block's first, are on their way from LDS; loads go between matrix instructions.  The last quarter needs nothing more
 // from this stage: before it all waves meet, in it the stage is filled again.
-template <int TYPE, int WM, int WN, int MF, int NF, int STAGES, typename Epilogue>
+template <int TYPE, bool ACROSS, bool DOWN, int WM, int WN, int MF, int NF, int STAGES, typename Epilogue>
 __global__ void __launch_bounds__(WM * WN * kWave, 2) tile_kernel(const Args p, const Epilogue epilogue) {
     constexpr uint32_t TM = WM * 16 * MF, TN = WN * 16 * NF;
-    constexpr int LA = 2 * MF / WN, LB = 2 * NF / WM;  // loads of 1 KB that each wave sends for a block of A and of B
+    constexpr int LA = 2 * MF / WN, LB = 2 * NF / WM;  // loads of 1 KB that each wave sends for a block of each operand
     static_assert(LA * WN == 2 * MF && LB * WM == 2 * NF, "whole loads");
     constexpr uint32_t kB = TM * kBlockBytes, kStage = kB + TN * kBlockBytes;
     constexpr int kLoads = LA + LB;
@@ -126,44 +219,36 @@ __global__ void __launch_bounds__(WM * WN * kWave, 2) tile_kernel(const Args p, 
 
     // Workgroups go to the eight XCDs in turn: each XCD gets tiles that lie together, in bands of kBand rows of tiles, for its L2.
     constexpr uint32_t kBand = 4;
-    const uint32_t tiles_m = (p.m + TM - 1) / TM, tiles_n = (p.n + TN - 1) / TN, tiles = tiles_m * tiles_n, all = tiles * p.splits;
+    const uint32_t down = (p.rows + TN - 1) / TN, across = (p.columns + TM - 1) / TM, tiles = down * across, all = tiles * p.splits;
     const uint32_t xcd = wg_x() % 8, each = all / 8, more = all % 8;
     const uint32_t id = xcd * each + (xcd < more ? xcd : more) + wg_x() / 8;
     const uint32_t split = id / tiles, at = id % tiles;
-    const uint32_t band = at / (kBand * tiles_n), band_rows = tiles_m - band * kBand < kBand ? tiles_m - band * kBand : kBand;
-    const uint32_t in_band = at - band * kBand * tiles_n;
-    const uint32_t tile_n = in_band / band_rows, m0 = (band * kBand + in_band % band_rows) * TM, n0 = tile_n * TN;
-    // Blocks of this part of the sum; the host sees to it that there are some.
-    const uint32_t begin = (uint32_t)((uint64_t)p.blocks * split / p.splits), end = (uint32_t)((uint64_t)p.blocks * (split + 1) / p.splits);
+    const uint32_t band = at / (kBand * across), band_rows = down - band * kBand < kBand ? down - band * kBand : kBand;
+    const uint32_t in_band = at - band * kBand * across;
+    const uint32_t tile_column = in_band / band_rows, row0 = (band * kBand + in_band % band_rows) * TN, column0 = tile_column * TM;
+    // Blocks of this part of the sum, over all terms; the host sees to it that there are some.
+    const uint32_t whole = p.blocks * p.terms;
+    const uint32_t begin = (uint32_t)((uint64_t)whole * split / p.splits), end = (uint32_t)((uint64_t)whole * (split + 1) / p.splits);
 
-    // Rows beyond the matrix read its last one again.
-    const uint32_t rows_a = p.m - m0 < TM ? p.m - m0 : TM, rows_b = p.n - n0 < TN ? p.n - n0 : TN;
-    const uint32_t row_bytes = p.blocks * kBlockBytes;
-    const i32x4 buffer_a = buffer_of(reinterpret_cast<uint64_t>(p.a) + (uint64_t)m0 * p.a_bytes, (uint64_t)(rows_a - 1) * p.a_bytes + row_bytes);
-    const i32x4 buffer_b = buffer_of(reinterpret_cast<uint64_t>(p.b) + (uint64_t)n0 * p.b_bytes, (uint64_t)(rows_b - 1) * p.b_bytes + row_bytes);
-    uint32_t from_a[LA], from_b[LB];
-#pragma unroll
-    for (int j = 0; j < LA; ++j) {
-        const uint32_t line = (wave * LA + j) * 4 + quarter, logical = (lane % 16) ^ (2 * line / MF % 16);
-        const uint32_t row = 2 * line + logical / 8;
-        from_a[j] = (row < rows_a ? row : rows_a - 1) * (uint32_t)p.a_bytes + logical % 8 * 16;
-    }
-#pragma unroll
-    for (int j = 0; j < LB; ++j) {
-        const uint32_t line = (wave * LB + j) * 4 + quarter, logical = (lane % 16) ^ (2 * line / NF % 16);
-        const uint32_t row = 2 * line + logical / 8;
-        from_b[j] = (row < rows_b ? row : rows_b - 1) * (uint32_t)p.b_bytes + logical % 8 * 16;
-    }
+    typename std::conditional<ACROSS, Across<MF, TM, LA>, Along<MF, TM, LA>>::type a(p.across, column0, p.columns, p.k, wave, wave_m, 0);
+    typename std::conditional<DOWN, Across<NF, TN, LB>, Along<NF, TN, LB>>::type b(p.down, row0, p.rows, p.k, wave, wave_n, kB);
     const uint32_t lds_at = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) uint8_t *)lds;
-    // Load j of the wave's kLoads for block kb of this part of the sum into the stage at `to`; beyond its end the last block once more, which
-    // nobody reads: the count of loads stays the same without a branch.
-    auto fetch = [&](uint32_t kb, uint32_t to, auto index) {
+    // The block to be fetched next; behind the last one it stays there, and nobody reads what arrives: the count of loads stays the same without a branch.
+    uint32_t ahead = begin, block = begin % p.blocks, term = begin / p.blocks;
+    auto fetch = [&](uint32_t to, auto index) {
         constexpr int J = decltype(index)::value;
-        const uint32_t along = (kb < end - 1 ? kb : end - 1) * kBlockBytes;
         if constexpr (J < LA)
-            load_to_lds(buffer_a, lds_at + to + (wave * LA + J) * 1024, from_a[J], along);
+            a.template fetch<J>(p.across, lds_at + to + (wave * LA + J) * 1024, (p.across.parts >> 4 * term & 15u) * p.across.part_bytes, block);
         else
-            load_to_lds(buffer_b, lds_at + to + kB + (wave * LB + J - LA) * 1024, from_b[J - LA], along);
+            b.template fetch<J - LA>(p.down, lds_at + to + kB + (wave * LB + J - LA) * 1024, (p.down.parts >> 4 * term & 15u) * p.down.part_bytes, block);
+    };
+    auto go_on = [&]() {
+        if (ahead + 1 < end) {
+            ++ahead;
+            const bool over = block + 1 == p.blocks;
+            block = over ? 0 : block + 1;
+            term += over ? 1 : 0;
+        }
     };
 
     f32x4 acc[MF][NF];
@@ -172,50 +257,30 @@ __global__ void __launch_bounds__(WM * WN * kWave, 2) tile_kernel(const Args p, 
 #pragma unroll
         for (int g = 0; g < NF; ++g) acc[f][g] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
 
-    // Where a lane's row of fragment f lies: lines of 256 bytes for each pair of fragments, in them the piece h at one of two places that
-    // depend on the lane alone, in the other half of the line for an odd f.  These addresses move from stage to stage.
-    uint32_t piece_a[2][2], piece_b[2][2];  // [odd][h]
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-        const uint32_t place = ((quarter + 4 * (i % 2)) ^ r) * 16 ^ i / 2 * 128;
-        piece_a[i / 2][i % 2] = (wave_m + r * MF) * kBlockBytes + place;
-        piece_b[i / 2][i % 2] = kB + (wave_n + r * NF) * kBlockBytes + place;
-    }
-    auto move_pieces = [&](uint32_t by) {
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            piece_a[i / 2][i % 2] += by;
-            piece_b[i / 2][i % 2] += by;
-        }
-    };
-    auto fragment = [&](const uint32_t (&piece)[2][2], uint32_t f) {
-        i32x4 part[2];
-#pragma unroll
-        for (int h = 0; h < 2; ++h) part[h] = *reinterpret_cast<const i32x4 *>(lds + piece[f % 2][h] + f / 2 * 256);
-        return __builtin_shufflevector(part[0], part[1], 0, 1, 2, 3, 4, 5, 6, 7);
-    };
     // The i-th of `of` even shares of N things to do.
     auto share = [](auto i, auto of, auto n, const auto &act) {
         constexpr int I = decltype(i)::value, OF = decltype(of)::value, N = decltype(n)::value, from = I * N / OF, to = (I + 1) * N / OF;
         unrolled<to - from>([&](auto j) { act(Index<from + decltype(j)::value>()); });
     };
 
-    typedef Multiply<TYPE> Product;
-    constexpr int HM = MF / 2, HN = NF / 2, kPairs = HM * HN, kSteps = kPairs * Product::kParts;
-    unrolled<STAGES>([&](auto i) { unrolled<kLoads>([&](auto j) { fetch(begin + decltype(i)::value, decltype(i)::value * kStage, j); }); });
+    constexpr int HM = MF / 2, HN = NF / 2, kPairs = HM * HN, kSteps = kPairs * 2;
+    unrolled<STAGES>([&](auto i) {
+        unrolled<kLoads>([&](auto j) { fetch(decltype(i)::value * kStage, j); });
+        go_on();
+    });
     wait_for_loads<(STAGES - 1) * kLoads>();
     barrier();
     i32x8 x[2][HM], y[2][HN];
 #pragma unroll
-    for (int f = 0; f < HM; ++f) x[0][f] = fragment(piece_a, f);
+    for (int f = 0; f < HM; ++f) x[0][f] = a.fragment(lds, f);
 #pragma unroll
-    for (int g = 0; g < HN; ++g) y[0][g] = fragment(piece_b, g);
+    for (int g = 0; g < HN; ++g) y[0][g] = b.fragment(lds, g);
     // One quarter; with its i-th matrix instruction goes beside(i).  Sums take turns, so that none waits for the one before.
     auto quarter_of = [&](auto half_a, auto half_b, const auto &beside) {
         constexpr int A = decltype(half_a)::value, B = decltype(half_b)::value;
         unrolled<kSteps>([&](auto step) {
             constexpr int H = decltype(step)::value / kPairs, PAIR = decltype(step)::value % kPairs, F = PAIR % HM, G = PAIR / HM, MA = A * HM + F, NB = B * HN + G;
-            acc[MA][NB] = Product::template part<H>(x[A][F], y[B][G], acc[MA][NB]);
+            acc[MA][NB] = multiply<TYPE, H>(x[A][F], y[B][G], acc[MA][NB]);
             beside(step);
             __builtin_amdgcn_sched_barrier(0);
         });
@@ -224,57 +289,72 @@ __global__ void __launch_bounds__(WM * WN * kWave, 2) tile_kernel(const Args p, 
     for (uint32_t kb = begin; kb < end; ++kb) {
         const uint32_t next = stage + kStage < STAGES * kStage ? stage + kStage : 0;
         quarter_of(Index<0>(), Index<0>(), [&](auto step) {
-            share(step, Index<kSteps>(), Index<HN>(), [&](auto g) { y[1][decltype(g)::value] = fragment(piece_b, HN + decltype(g)::value); });
+            share(step, Index<kSteps>(), Index<HN>(), [&](auto g) { y[1][decltype(g)::value] = b.fragment(lds, HN + decltype(g)::value); });
         });
         quarter_of(Index<0>(), Index<1>(), [&](auto step) {
-            share(step, Index<kSteps>(), Index<HM>(), [&](auto f) { x[1][decltype(f)::value] = fragment(piece_a, HM + decltype(f)::value); });
+            share(step, Index<kSteps>(), Index<HM>(), [&](auto f) { x[1][decltype(f)::value] = a.fragment(lds, HM + decltype(f)::value); });
         });
         quarter_of(Index<1>(), Index<0>(), [&](auto) {});
         wait_for_loads<(STAGES - 2) * kLoads>();
         barrier();
-        move_pieces(next - stage);
+        a.move(next - stage);
+        b.move(next - stage);
         quarter_of(Index<1>(), Index<1>(), [&](auto step) {
             share(step, Index<kSteps>(), Index<HM + HN>(), [&](auto j) {
                 constexpr int J = decltype(j)::value;
                 if constexpr (J < HM)
-                    x[0][J] = fragment(piece_a, J);
+                    x[0][J] = a.fragment(lds, J);
                 else
-                    y[0][J - HM] = fragment(piece_b, J - HM);
+                    y[0][J - HM] = b.fragment(lds, J - HM);
             });
-            share(step, Index<kSteps>(), Index<kLoads>(), [&](auto j) { fetch(kb + STAGES, stage, j); });
+            share(step, Index<kSteps>(), Index<kLoads>(), [&](auto j) { fetch(stage, j); });
         });
+        go_on();
         stage = next;
     }
     wait_for_loads<0>();
     if constexpr (Epilogue::kUsesLds) __syncthreads();
-    Place place;
-    place.m0 = m0;
-    place.n0 = n0;
-    place.row = wave_m + quarter * 4 * MF;
-    place.column = wave_n + r * NF;
-    place.m = m0 + place.row;
-    place.n = n0 + place.column;
+    if constexpr (ACROSS) {
+        // chunks of odd quarters back in order
+#pragma unroll
+        for (int f = 0; f < MF; f += 2)
+#pragma unroll
+            for (int g = 0; g < NF; ++g)
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    const float v = acc[f][g][i], w = acc[f + 1][g][i];
+                    acc[f][g][i] = quarter % 2 ? w : v;
+                    acc[f + 1][g][i] = quarter % 2 ? v : w;
+                }
+    }
+    Place<MF, NF, ACROSS, DOWN> place;
+    place.row0 = row0;
+    place.column0 = column0;
+    place.lane_row = wave_n + (DOWN ? r / 4 * 4 * NF + r % 4 : r * NF);
+    place.column = column0 + wave_m + quarter * 4 * MF;
     place.split = split;
-    place.tile_n = tile_n;
+    place.tile_column = tile_column;
+    place.wave_column = wave / WN;
     place.lds = lds;
-    epilogue.template finish<TM, TN, WN, MF, NF>(p, place, acc);
+    epilogue.template finish<TM, TN, WM>(p, place, acc);
 }
 #endif
 
 // ---- which tiles ----------------------------------------------------------------------------------------------
 //
-// A workgroup's time for a block by how many share a compute unit, in us, with 16-bit elements; the fp32 instructions take kSlow32 times as long.
+// A workgroup's time for a block by how many share a compute unit, in us.
 struct Tiles {
-    uint32_t rows, columns, resident;
+    uint32_t columns, rows, threads, resident;
     float block[2];
 };
 constexpr Tiles kTiles[] = {
-    {256, 256, 1, {1.65f, 0.0f}},   // eight waves of 128 x 64, two stages
-    {128, 128, 1, {0.54f, 0.0f}},   // eight waves of 64 x 32, four stages
-    {64, 64, 2, {0.28f, 0.42f}},    // four waves of 32 x 32, four stages
+    {256, 256, 512, 1, {1.65f, 0.0f}},  // eight waves of 128 x 64, two stages
+    {128, 128, 512, 1, {0.54f, 0.0f}},  // eight waves of 64 x 32, four stages
+    {128, 128, 256, 2, {0.65f, 1.0f}},  // four waves of 64 x 64, two stages
+    {256, 64, 512, 1, {0.6f, 0.0f}},    // eight waves of 64 x 32, three stages
+    {64, 64, 256, 2, {0.28f, 0.42f}},   // four waves of 32 x 32, four stages
 };
 constexpr int kKinds = (int)(sizeof(kTiles) / sizeof(kTiles[0]));
-constexpr float kSlow32 = 8.0f;
 constexpr uint32_t kMaxSplits = 16, kMinBlocks = 4;  // parts of a sum, blocks of a part
 
 struct Plan {
@@ -282,22 +362,22 @@ struct Plan {
     uint32_t splits;
 };
 // The tiles and parts of the shortest estimated time; parts of up to part_bytes in all, of rows of a multiple of four floats.
-static inline Plan plan_of(const cnr_ctx *ctx, cnr_float_type type, uint64_t m, uint64_t n, uint64_t blocks, uint64_t part_bytes) {
-    const float units = ctx ? (float)ctx->n_cu : 256.0f, slow = type == CNR_FLOAT_F32 ? kSlow32 : 1.0f;
-    const float memory = ((float)m + (float)n) * (float)blocks * (float)kBlockBytes / 4.7e6f;
+static inline Plan plan_of(const cnr_ctx *ctx, uint64_t columns, uint64_t rows, uint64_t blocks, uint64_t part_bytes) {
+    const float units = ctx ? (float)ctx->n_cu : 256.0f;
+    const float memory = ((float)columns + (float)rows) * (float)blocks * (float)kBlockBytes / 4.7e6f;
     Plan best = {0, 1};
     float least = 3e38f;
     for (int i = 0; i < kKinds; ++i) {
         const Tiles &t = kTiles[i];
-        const float tiles = (float)cnr_ceil_div(m, t.rows) * (float)cnr_ceil_div(n, t.columns);
-        for (uint32_t s = 1; s == 1 || (s <= kMaxSplits && blocks >= (uint64_t)s * kMinBlocks && s * m * cnr_ceil_div(n, 4) * 16 <= part_bytes); s *= 2) {
+        const float tiles = (float)cnr_ceil_div(columns, t.columns) * (float)cnr_ceil_div(rows, t.rows);
+        for (uint32_t s = 1; s == 1 || (s <= kMaxSplits && blocks >= (uint64_t)s * kMinBlocks && s * rows * cnr_ceil_div(columns, 4) * 16 <= part_bytes); s *= 2) {
             const float groups = tiles * (float)s, round = units * (float)t.resident, rounds = floorf(groups / round);
-            if (groups * (i < 2 ? 512.0f : 256.0f) >= 4.2e9f) continue;  // grids count threads in 32 bits
+            if (groups * (float)t.threads >= 4.2e9f) continue;  // grids count threads in 32 bits
             const float rest = ceilf((groups - rounds * round) / units);  // workgroups on a unit in the last round
-            float time = ceilf((float)blocks / (float)s) * slow * (rounds * t.block[t.resident - 1] + (rest > 0.0f ? t.block[(int)rest - 1] : 0.0f));
+            float time = ceilf((float)blocks / (float)s) * (rounds * t.block[t.resident - 1] + (rest > 0.0f ? t.block[(int)rest - 1] : 0.0f));
             time += 1.5f * (rounds + (rest > 0.0f ? 1.0f : 0.0f));
             time = (time > memory ? time : memory) + 0.25f * (time < memory ? time : memory);  // one does not quite hide the other
-            if (s > 1) time += 3.5f + (float)(s + 1) * (float)m * (float)n * 4.0f / 3e6f;        // writing the parts, and joining them
+            if (s > 1) time += 3.5f + (float)(s + 1) * (float)rows * (float)columns * 4.0f / 3e6f;  // writing the parts, and joining them
             if (time < least) {
                 least = time;
                 best = {i, s};
@@ -308,14 +388,16 @@ static inline Plan plan_of(const cnr_ctx *ctx, cnr_float_type type, uint64_t m, 
 }
 
 #ifdef __HIPCC__
-template <int TYPE, typename Epilogue>
+template <int TYPE, bool ACROSS, bool DOWN, typename Epilogue>
 void launch(const Args &p, int kind, const Epilogue &e, hipStream_t s) {
     const Tiles &t = kTiles[kind];
-    const dim3 grid((unsigned)(cnr_ceil_div(p.m, t.rows) * cnr_ceil_div(p.n, t.columns) * p.splits));
+    const dim3 grid((unsigned)(cnr_ceil_div(p.columns, t.columns) * cnr_ceil_div(p.rows, t.rows) * p.splits)), threads(t.threads);
     switch (kind) {
-        case 0: hipLaunchKernelGGL((tile_kernel<TYPE, 2, 4, 8, 4, 2, Epilogue>), grid, dim3(512), 0, s, p, e); break;
-        case 1: hipLaunchKernelGGL((tile_kernel<TYPE, 2, 4, 4, 2, 4, Epilogue>), grid, dim3(512), 0, s, p, e); break;
-        default: hipLaunchKernelGGL((tile_kernel<TYPE, 2, 2, 2, 2, 4, Epilogue>), grid, dim3(256), 0, s, p, e); break;
+        case 0: hipLaunchKernelGGL((tile_kernel<TYPE, ACROSS, DOWN, 2, 4, 8, 4, 2, Epilogue>), grid, threads, 0, s, p, e); break;
+        case 1: hipLaunchKernelGGL((tile_kernel<TYPE, ACROSS, DOWN, 2, 4, 4, 2, 4, Epilogue>), grid, threads, 0, s, p, e); break;
+        case 2: hipLaunchKernelGGL((tile_kernel<TYPE, ACROSS, DOWN, 2, 2, 4, 4, 2, Epilogue>), grid, threads, 0, s, p, e); break;
+        case 3: hipLaunchKernelGGL((tile_kernel<TYPE, ACROSS, DOWN, 4, 2, 4, 2, 3, Epilogue>), grid, threads, 0, s, p, e); break;
+        default: hipLaunchKernelGGL((tile_kernel<TYPE, ACROSS, DOWN, 2, 2, 2, 2, 4, Epilogue>), grid, threads, 0, s, p, e); break;
     }
 }
 #endif

@@ -6,10 +6,15 @@
 // with a few (token, share) entries a row, so one machine serves them:
 //   forward   a product whose tiles leave, for each row, the largest logit and the sum of exponentials relative to it (kept to base 2: exp2 is one
 //             instruction), and one workgroup a row that joins them, takes the entries' logits as dot products and writes the loss;
-//   backward  for a piece of the vocabulary at a time, the logits once more, turned into dz in the epilogue (written in both directions, as each of the
-//             two gradients' products wants it along its sum); the entries' own dz, a few a row, are put in by a kernel of its own; then
-//             dhidden += dz weight and dweight = dz^T hidden, plain products with the transposes of the piece and of the hidden states.
-// Rows that are left out, and rows whose dloss is 0, have dz = 0 and a transpose of zeros: whatever they hold reaches no gradient.
+//   backward  for a piece of the vocabulary at a time, the logits once more, turned into dz in the epilogue; the entries' own dz, a few a row, are put in
+//             by a kernel of its own; then dhidden += dz weight and dweight = dz^T hidden, products that read the weight, the hidden states and dz along
+//             whichever side their sum goes, so nothing is transposed in memory.
+// Rows that are left out, and rows whose dloss is 0, have dz = 0 and are zeros in the copy of the hidden states that the backward pass makes: whatever they
+// hold reaches no gradient.
+//
+// The matrix instructions take 16-bit elements.  A float is the sum of three bfloat16, its bits cut in three; of the nine products of two floats' parts
+// six are added up, the rest is below 2^-21 of the product in the worst case (2^-24 on average).  All parts have the float's sign, and a part that is zero of a float that is
+// not, or of an infinite one, is +-2^-126 instead: so an infinity times a float is the infinity that it ought to be in every term.
 #include "lm_dense.h"
 #include "cnr_loss.h"
 
@@ -18,7 +23,6 @@
 namespace {
 
 using dense::i32x4;
-using dense::Place;
 
 constexpr float kLog2e = 1.44269504088896340736f, kLn2 = 0.69314718055994530942f;
 
@@ -77,28 +81,39 @@ struct KeepStats {
     Stats *parts;      // [rows][n_parts], from the piece's first part on
     uint32_t n_parts;
     float c;
-    template <uint32_t TM, uint32_t TN, int WN, int MF, int NF>
+    template <uint32_t TM, uint32_t TN, int WM, typename Place, int MF, int NF>
     __device__ __forceinline__ void finish(const dense::Args &p, const Place &at, const f32x4 (&acc)[MF][NF]) const {
-        Stats *lds = reinterpret_cast<Stats *>(at.lds);  // [WN][TM]
-        const uint32_t lane = tid_x() % 16, wave_n = at.column / (16 * NF);
-        uint32_t valid = 0;
+        if (at.column0 + TM <= p.columns)
+            reduce<TM, TN, WM, true>(p, at, acc);
+        else
+            reduce<TM, TN, WM, false>(p, at, acc);
+    }
+    template <uint32_t TM, uint32_t TN, int WM, bool WHOLE, typename Place, int MF, int NF>
+    __device__ __forceinline__ void reduce(const dense::Args &p, const Place &at, const f32x4 (&acc)[MF][NF]) const {
+        Stats *lds = reinterpret_cast<Stats *>(at.lds);  // [WM][TN]
+        const uint32_t left = at.column < p.columns ? p.columns - at.column : 0;
 #pragma unroll
-        for (uint32_t g = 0; g < NF; ++g) valid |= at.n + g < p.n ? 1u << g : 0u;
+        for (int g = 0; g < NF; ++g) {
+            float top = -__builtin_inff();
 #pragma unroll
-        for (int i = 0; i < 4 * MF; ++i) {
-            float z[NF];
+            for (uint32_t i = 0; i < 4 * MF; ++i) top = __builtin_fmaxf(top, WHOLE || i < left ? at.value(acc, i, g) : -__builtin_inff());
+            top = __builtin_fmaxf(top, __shfl_xor(top, 16));
+            top = __builtin_fmaxf(top, __shfl_xor(top, 32)) * c;
+            const float from = top == -__builtin_inff() ? 0.0f : top;
+            float sum = 0.0f;
 #pragma unroll
-            for (int g = 0; g < NF; ++g) z[g] = acc[i % MF][g][i / MF];
-            const Stats s = stats16(z, c, valid);
-            if (lane == (uint32_t)i % 16) lds[wave_n * TM + at.row + i] = s;
+            for (uint32_t i = 0; i < 4 * MF; ++i) sum += WHOLE || i < left ? exp2_of(__builtin_fmaf(at.value(acc, i, g), c, -from)) : 0.0f;
+            sum += __shfl_xor(sum, 16);
+            sum += __shfl_xor(sum, 32);
+            if (tid_x() % kWave < 16) lds[at.wave_column * TN + at.row_within(g)] = {top, sum};
         }
         __syncthreads();
         const uint32_t row = tid_x();
-        if (row < TM && at.m0 + row < p.m) {
+        if (row < TN && at.row0 + row < p.rows) {
             Stats s = lds[row];
 #pragma unroll
-            for (int w = 1; w < WN; ++w) s = join(s, lds[w * TM + row]);
-            parts[(uint64_t)(at.m0 + row) * n_parts + at.tile_n] = s;
+            for (int w = 1; w < WM; ++w) s = join(s, lds[w * TN + row]);
+            parts[(uint64_t)(at.row0 + row) * n_parts + at.tile_column] = s;
         }
     }
 };
@@ -108,56 +123,47 @@ struct RowGradient {
     float lse2, gradient;
 };
 
-// dz of the tile's rows and columns: [row][column] and [column][row], with zeros up to the next whole block of each.  LOW: also what the 16-bit
-// rounding left, `low` elements further on in the second, for gradients in fp32.
-template <int TYPE, bool LOW>
+// v as PARTS numbers of 16 bits that add up to it.
+template <int TYPE, int PARTS>
+__device__ __forceinline__ void apart(float v, typename Element<TYPE>::type (&part)[PARTS]) {
+#pragma unroll
+    for (int i = 0; i < PARTS; ++i) {
+        part[i] = Element<TYPE>::narrow(v);
+        v -= Element<TYPE>::wide(part[i]);
+    }
+}
+
+// dz of the tile's rows and columns, with zeros up to the next whole block of columns, in PARTS parts side by side.
+template <int TYPE, int PARTS>
 struct KeepGradient {
     static constexpr bool kUsesLds = false;
     typedef typename Element<TYPE>::type T;
-    T *dz, *dz_t;
-    uint64_t stride, stride_t;  // of whole blocks
-    uint64_t low;
-    const RowGradient *rows;    // up to a multiple of 256
+    T *dz;
+    uint64_t width, stride;    // of a part, of a row: PARTS * width, whole blocks
+    const RowGradient *rows;   // up to a multiple of 256
     float c;
-    template <uint32_t TM, uint32_t TN, int WN, int MF, int NF>
-    __device__ __forceinline__ void finish(const dense::Args &p, const Place &at, f32x4 (&acc)[MF][NF]) const {
-#pragma unroll
-        for (int i = 0; i < 4 * MF; ++i) {
-            const RowGradient row = rows[at.m + i];
-#pragma unroll
-            for (int g = 0; g < NF; ++g) {
-                const float z = acc[i % MF][g][i / MF];
-                acc[i % MF][g][i / MF] = row.gradient == 0.0f || at.n + g >= p.n ? 0.0f : row.gradient * exp2_of(__builtin_fmaf(z, c, -row.lse2));
-            }
-        }
-        if (dz && at.n < stride) {
-            T *to = dz + (uint64_t)at.m * stride + at.n;
-#pragma unroll
-            for (int i = 0; i < 4 * MF; ++i) {
-                Pack<T, NF> w;
-#pragma unroll
-                for (int g = 0; g < NF; ++g) w.v[g] = Element<TYPE>::narrow(acc[i % MF][g][i / MF]);
-                if (at.m + i < p.m) *reinterpret_cast<Pack<T, NF> *>(to + (uint64_t)i * stride) = w;
-            }
-        }
-        if (!dz_t) return;
-        constexpr int kSide = 16 / sizeof(T) < 4 * MF ? 16 / sizeof(T) : 4 * MF;
+    template <uint32_t TM, uint32_t TN, int WM, typename Place, int MF, int NF>
+    __device__ __forceinline__ void finish(const dense::Args &p, const Place &at, const f32x4 (&acc)[MF][NF]) const {
 #pragma unroll
         for (int g = 0; g < NF; ++g) {
-            if (at.n + g >= p.n) continue;
-            T *to = dz_t + (uint64_t)(at.n + g) * stride_t + at.m;
+            const uint32_t row = at.row(g);
+            const RowGradient r = rows[row];
+            if (row >= p.rows) continue;
+            T *to = dz + row * stride + at.column;
 #pragma unroll
-            for (int i = 0; i < 4 * MF; i += kSide) {
-                if (at.m + i >= stride_t) continue;
-                Pack<T, kSide> w, rest;
+            for (int first = 0; first < 4 * MF; first += 8) {
+                if (at.column + first >= width) continue;
+                Pack<T, 8> w[PARTS];
 #pragma unroll
-                for (int j = 0; j < kSide; ++j) {
-                    const float v = acc[(i + j) % MF][g][(i + j) / MF];
-                    w.v[j] = Element<TYPE>::narrow(v);
-                    if constexpr (LOW) rest.v[j] = Element<TYPE>::narrow(v - Element<TYPE>::wide(w.v[j]));
+                for (int j = 0; j < 8; ++j) {
+                    const float z = at.value(acc, first + j, g);
+                    T part[PARTS];
+                    apart<TYPE, PARTS>(r.gradient == 0.0f || at.column + first + j >= p.columns ? 0.0f : r.gradient * exp2_of(__builtin_fmaf(z, c, -r.lse2)), part);
+#pragma unroll
+                    for (int i = 0; i < PARTS; ++i) w[i].v[j] = part[i];
                 }
-                *reinterpret_cast<Pack<T, kSide> *>(to + i) = w;
-                if constexpr (LOW) *reinterpret_cast<Pack<T, kSide> *>(to + low + i) = rest;
+#pragma unroll
+                for (int i = 0; i < PARTS; ++i) *reinterpret_cast<Pack<T, 8> *>(to + i * width + first) = w[i];
             }
         }
     }
@@ -227,39 +233,37 @@ struct KeepSum {
     const float *scale;     // NULL: 1
     float *partial;         // [splits][m][partial_stride] where sums are split
     uint64_t partial_stride;
-    template <uint32_t TM, uint32_t TN, int WN, int MF, int NF>
+    template <uint32_t TM, uint32_t TN, int WM, typename Place, int MF, int NF>
     __device__ __forceinline__ void finish(const dense::Args &p, const Place &at, const f32x4 (&acc)[MF][NF]) const {
-        if (at.n >= p.n) return;
-        const uint32_t rows = at.m < p.m ? p.m - at.m : 0;
-        if (p.splits > 1) {
-            const Target to = {partial + (uint64_t)at.split * p.m * partial_stride, partial_stride, CNR_FLOAT_F32};
-#pragma unroll
-            for (int i = 0; i < 4 * MF; ++i) {
-                float v[NF];
-#pragma unroll
-                for (int g = 0; g < NF; ++g) v[g] = acc[i % MF][g][i / MF];
-                if ((uint32_t)i < rows) write_as(reinterpret_cast<float *>(to.out) + (uint64_t)(at.m + i) * to.stride + at.n, at.n, p.n, v);
-            }
-            return;
-        }
         const float by = scale ? *scale : 1.0f;
-        // What is added to is read for eight rows at once: one row after the other would wait for memory each time.
 #pragma unroll
-        for (int first = 0; first < 4 * MF; first += 8) {
-            float old[8][NF];
+        for (int g = 0; g < NF; ++g) {
+            const uint32_t row = at.row(g);
+            if (row >= p.rows || at.column >= p.columns) continue;
+            if (p.splits > 1) {
+                float *to = partial + ((uint64_t)at.split * p.rows + row) * partial_stride;
 #pragma unroll
-            for (int u = 0; u < 8; ++u) {
+                for (int first = 0; first < 4 * MF; first += 4) {
+                    float v[4];
 #pragma unroll
-                for (int g = 0; g < NF; ++g) old[u][g] = 0.0f;
-                if (there.out && (uint32_t)(first + u) < rows) read_row(there, at.m + first + u, at.n, p.n, old[u]);
+                    for (int j = 0; j < 4; ++j) v[j] = at.value(acc, first + j, g);
+                    write_as(to + at.column + first, at.column + first, p.columns, v);
+                }
+                continue;
+            }
+            // What is added to is read for the whole row at once: one piece after the other would wait for memory each time.
+            float old[4 * MF / 8][8];
+#pragma unroll
+            for (int u = 0; u < 4 * MF / 8; ++u) {
+#pragma unroll
+                for (int j = 0; j < 8; ++j) old[u][j] = 0.0f;
+                if (there.out) read_row(there, row, at.column + 8 * u, p.columns, old[u]);
             }
 #pragma unroll
-            for (int u = 0; u < 8; ++u) {
-                const int i = first + u;
-                float v[NF];
+            for (int u = 0; u < 4 * MF / 8; ++u) {
 #pragma unroll
-                for (int g = 0; g < NF; ++g) v[g] = __builtin_fmaf(acc[i % MF][g][i / MF], by, old[u][g]);
-                if ((uint32_t)i < rows) write_row(out, at.m + i, at.n, p.n, v);
+                for (int j = 0; j < 8; ++j) old[u][j] = __builtin_fmaf(at.value(acc, 8 * u + j, g), by, old[u][j]);
+                write_row(out, row, at.column + 8 * u, p.columns, old[u]);
             }
         }
     }
@@ -284,51 +288,50 @@ __global__ void __launch_bounds__(kBlock) join_sums_kernel(const KeepSum k, uint
 
 // ---- operands laid out for the products -----------------------------------------------------------------------
 
-// dst[rows][blocks of 128 bytes] = src, zeros behind it.
+// One of the parts of a float (see above).
+__device__ __forceinline__ __bf16 float_part(float v, int part) {
+    const uint32_t sign = __float_as_uint(v) & 0x80000000u;
+    float rest = v;
+    for (int i = 0; i < part; ++i) rest -= __uint_as_float(__float_as_uint(rest) & 0xffff0000u);
+    uint32_t bits = __float_as_uint(rest) & 0xffff0000u;
+    if (part) {
+        const bool finite = __builtin_fabsf(v) < __builtin_inff();
+        if (!finite || (rest == 0.0f && v != 0.0f)) bits = sign | 0x00800000u;
+    } else if (v != v) {
+        bits = 0x7fc00000u;
+    }
+    return __builtin_bit_cast(__bf16, (unsigned short)(bits >> 16));
+}
+// dst[rows][parts][whole blocks] = src, zeros behind it; rows that add nothing are zeros.  16 bytes of each part to a thread.
 template <typename T>
-__global__ void __launch_bounds__(kBlock) lay_out_kernel(const T *src, uint64_t stride, uint32_t rows, uint32_t dim, T *dst, uint32_t pieces /* of 16 bytes, a row */) {
-    constexpr uint32_t kPer = 16 / sizeof(T);
+__global__ void __launch_bounds__(kBlock) lay_out_kernel(const T *src, uint64_t stride, uint32_t rows, uint32_t dim, const RowGradient *keep, u32x4 *dst,
+                                                         uint32_t pieces /* of a part */) {
+    constexpr int kParts = sizeof(T) == 4 ? 3 : 1;
     const uint64_t at = (uint64_t)wg_x() * kBlock + tid_x();
     if (at >= (uint64_t)rows * pieces) return;
-    const uint32_t row = (uint32_t)(at / pieces), column = (uint32_t)(at % pieces) * kPer;
+    const uint32_t row = (uint32_t)(at / pieces), piece = (uint32_t)(at % pieces), column = piece * 8;
     const T *from = src + (uint64_t)row * stride + column;
-    Pack<T, kPer> w;
-    if (column + kPer <= dim) {
-        w = *reinterpret_cast<const Pack<T, kPer> *>(from);
+    Pack<T, 8> w;
+    if (keep && keep[row].gradient == 0.0f) {
+#pragma unroll
+        for (uint32_t j = 0; j < 8; ++j) w.v[j] = (T)0.0f;
+    } else if (column + 8 <= dim) {
+        w = *reinterpret_cast<const Pack<T, 8> *>(from);
     } else {
 #pragma unroll
-        for (uint32_t j = 0; j < kPer; ++j) w.v[j] = column + j < dim ? from[j] : (T)0.0f;
+        for (uint32_t j = 0; j < 8; ++j) w.v[j] = column + j < dim ? from[j] : (T)0.0f;
     }
-    *reinterpret_cast<Pack<T, kPer> *>(dst + at * kPer) = w;
-}
-
-// dst[columns][to_stride] = the transpose of src[rows][columns], zeros behind it; rows that add nothing are zero.  64 x 64 at a time.
-template <typename T>
-__global__ void __launch_bounds__(kBlock) turn_kernel(const T *src, uint64_t stride, uint32_t rows, uint32_t columns, const RowGradient *keep, T *dst, uint64_t to_stride) {
-    constexpr uint32_t kPer = 16 / sizeof(T), kTile = 64, kAcross = kTile / kPer;
-    __shared__ T lds[kTile][kTile + 4 / sizeof(T)];
-    const uint32_t row0 = wg_x() * kTile, column0 = wg_y() * kTile;
-    for (uint32_t i = tid_x(); i < kTile * kAcross; i += kBlock) {
-        const uint32_t row = i / kAcross, column = i % kAcross * kPer;
-        const bool there = row0 + row < rows && (!keep || keep[row0 + row].gradient != 0.0f);
-        const T *from = src + (uint64_t)(row0 + row) * stride + column0 + column;
-        if (there && column0 + column + kPer <= columns) {
-            const Pack<T, kPer> w = *reinterpret_cast<const Pack<T, kPer> *>(from);
+    u32x4 *to = dst + (uint64_t)row * pieces * kParts + piece;
+    if constexpr (kParts == 1) {
+        *to = __builtin_bit_cast(u32x4, w);
+    } else {
 #pragma unroll
-            for (uint32_t j = 0; j < kPer; ++j) lds[row][column + j] = w.v[j];
-        } else {
+        for (int i = 0; i < kParts; ++i) {
+            Pack<__bf16, 8> part;
 #pragma unroll
-            for (uint32_t j = 0; j < kPer; ++j) lds[row][column + j] = there && column0 + column + j < columns ? from[j] : (T)0.0f;
+            for (int j = 0; j < 8; ++j) part.v[j] = float_part(w.v[j], i);
+            to[(uint64_t)i * pieces] = __builtin_bit_cast(u32x4, part);
         }
-    }
-    __syncthreads();
-    for (uint32_t i = tid_x(); i < kTile * kAcross; i += kBlock) {
-        const uint32_t column = i / kAcross, row = i % kAcross * kPer;
-        if (column0 + column >= columns || row0 + row >= to_stride) continue;
-        Pack<T, kPer> w;
-#pragma unroll
-        for (uint32_t j = 0; j < kPer; ++j) w.v[j] = lds[row + j][column];
-        *reinterpret_cast<Pack<T, kPer> *>(dst + (uint64_t)(column0 + column) * to_stride + row0 + row) = w;
     }
 }
 
@@ -336,6 +339,16 @@ __global__ void __launch_bounds__(kBlock) turn_kernel(const T *src, uint64_t str
 //
 // A workgroup has 16 rows by 16 NF columns; each of its waves takes a quarter of the sum, U blocks at a time so that enough loads are under way, straight
 // into the matrix instructions' registers; they add up their sums in LDS.  Bound by reading the weight.
+template <int TYPE>
+__device__ __forceinline__ f32x4 multiply(const dense::i32x8 &x, const dense::i32x8 &y, f32x4 sum) {
+    if constexpr (TYPE == CNR_FLOAT_F32) {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) sum = __builtin_amdgcn_mfma_f32_16x16x4f32(__int_as_float(x[i]), __int_as_float(y[i]), sum, 0, 0, 0);
+        return sum;
+    } else {
+        return dense::multiply<TYPE, 1>(x, y, dense::multiply<TYPE, 0>(x, y, sum));
+    }
+}
 struct NarrowArgs {
     const void *hidden, *weight;
     uint64_t hidden_stride, weight_stride;  // elements
@@ -396,8 +409,7 @@ __global__ void __launch_bounds__(kBlock, 4) narrow_kernel(const NarrowArgs p) {
         for (int u = 0; u < U; ++u) {
             if (u && first + u >= end) break;
 #pragma unroll
-            for (int g = 0; g < NF; ++g)
-                dense::unrolled<dense::Multiply<TYPE>::kParts>([&](auto h) { acc[g] = dense::Multiply<TYPE>::template part<decltype(h)::value>(x[u], y[u][g], acc[g]); });
+            for (int g = 0; g < NF; ++g) acc[g] = multiply<TYPE>(x[u], y[u][g], acc[g]);
         }
     }
 #pragma unroll
@@ -615,10 +627,11 @@ __global__ void __launch_bounds__(1024) rows_kernel(const float *lse2, const flo
     }
 }
 
-// dz of the entries whose tokens lie in [first, first + width): a thread for each entry.
-template <int TYPE, bool LOW>
-__global__ void __launch_bounds__(kBlock) entries_kernel(const KeepGradient<TYPE, LOW> k, const TargetArgs targets, const float *picked, const float *share, uint64_t n, uint32_t top,
-                                                         uint64_t first, uint32_t width) {
+// dz of the entries whose tokens lie in [first, first + columns): a thread for each entry.
+template <int TYPE, int PARTS>
+__global__ void __launch_bounds__(kBlock) entries_kernel(const KeepGradient<TYPE, PARTS> k, const TargetArgs targets, const float *picked, const float *share, uint64_t n, uint32_t top,
+                                                         uint64_t first, uint32_t columns) {
+    typedef typename Element<TYPE>::type T;
     const uint64_t at = (uint64_t)wg_x() * kBlock + tid_x();
     if (at >= n * top) return;
     const float q = share[at];
@@ -626,19 +639,14 @@ __global__ void __launch_bounds__(kBlock) entries_kernel(const KeepGradient<TYPE
     const RowGradient r = k.rows[row];
     if (q == 0.0f || r.gradient == 0.0f) return;
     const int64_t t = token_of(targets, row, (uint32_t)(at % top));
-    if (t < (int64_t)first || t >= (int64_t)(first + width)) return;
-    const float v = r.gradient * (exp2_of(__builtin_fmaf(picked[at], k.c, -r.lse2)) - q);
-    const uint64_t column = (uint64_t)t - first;
-    typedef typename Element<TYPE>::type T;
-    const T high = Element<TYPE>::narrow(v);
-    if (k.dz) k.dz[row * k.stride + column] = high;
-    if (k.dz_t) {
-        k.dz_t[column * k.stride_t + row] = high;
-        if constexpr (LOW) k.dz_t[k.low + column * k.stride_t + row] = Element<TYPE>::narrow(v - Element<TYPE>::wide(high));
-    }
+    if (t < (int64_t)first || t >= (int64_t)(first + columns)) return;
+    T part[PARTS];
+    apart<TYPE, PARTS>(r.gradient * (exp2_of(__builtin_fmaf(picked[at], k.c, -r.lse2)) - q), part);
+#pragma unroll
+    for (int i = 0; i < PARTS; ++i) k.dz[row * k.stride + i * k.width + ((uint64_t)t - first)] = part[i];
 }
 
-// out = scale-free zeros, or left as it is: what a product over nothing leaves.
+// Zeros: what a sum over nothing is.
 __global__ void __launch_bounds__(kBlock) zero_kernel(const Target out, uint64_t rows, uint32_t columns) {
     const uint64_t at = (uint64_t)wg_x() * kBlock + tid_x();
     if (at >= rows * columns) return;
@@ -655,11 +663,10 @@ constexpr uint64_t kStatsBytes = 512ull << 20;  // of the stats of as many rows 
 constexpr uint64_t kPartBytes = 128ull << 20;   // of sums that are split
 
 uint64_t rounded(uint64_t v, uint64_t to) { return cnr_ceil_div(v, to) * to; }
-uint32_t blocks_of(uint64_t elements, size_t element) { return (uint32_t)cnr_ceil_div(elements * element, dense::kBlockBytes); }
 
 // Whether a product can read rows of dim elements where they are.
-bool whole_rows(const void *base, uint64_t stride, uint64_t dim, uint64_t rows, size_t element) {
-    return dim && dim * element % dense::kBlockBytes == 0 && cnr_aligned(base, 16) && (rows <= 1 || stride * element % 16 == 0) && stride * element < 1u << 23;
+bool whole_rows(const cnr_float_type type, const void *base, uint64_t stride, uint64_t dim, uint64_t rows) {
+    return type != CNR_FLOAT_F32 && dim && dim % dense::kBlockElements == 0 && cnr_aligned(base, 16) && (rows <= 1 || (stride % 8 == 0 && stride < 1u << 22));
 }
 
 // Places in a workspace, in order.
@@ -675,17 +682,20 @@ struct Room {
 struct Sizes {
     uint64_t n, vocab, dim;
     cnr_float_type type;
-    size_t element;
-    uint64_t row;       // bytes of a laid out row of dim elements, at least one block
-    uint32_t blocks;
+    uint32_t parts, blocks;  // of a laid out row: of 16-bit elements each, at least one block
+    uint64_t row;            // its bytes
 };
 Sizes sizes_of(uint64_t n, uint64_t vocab, uint64_t dim, cnr_float_type type) {
-    Sizes s = {n, vocab, dim, type, cnr_float_bytes(type), 0, 0};
-    s.blocks = blocks_of(dim, s.element);
-    if (s.blocks == 0) s.blocks = 1;
-    s.row = (uint64_t)s.blocks * dense::kBlockBytes;
+    Sizes s = {n, vocab, dim, type, type == CNR_FLOAT_F32 ? 3u : 1u, 0, 0};
+    s.blocks = dim ? (uint32_t)cnr_ceil_div(dim, dense::kBlockElements) : 1;
+    s.row = (uint64_t)s.parts * s.blocks * dense::kBlockBytes;
     return s;
 }
+// Pairs of parts, the smallest products first.
+struct Terms {
+    uint32_t number, across, down;
+};
+constexpr Terms kOne = {1, 0, 0}, kOfFloats = {6, 0x001012, 0x010210}, kOfTwoParts = {2, 0, 0x01};
 
 struct ForwardPlan {
     bool narrow;
@@ -700,7 +710,7 @@ ForwardPlan forward_plan(const cnr_ctx *ctx, const Sizes &s) {
     f.narrow = s.n <= kNarrowRows;
     // Two fragments of the weight to a wave where that still gives every SIMD a wave.
     f.fragments = s.n > 1 && s.vocab >= 16384 ? 2 : 1;
-    f.tiles = dense::plan_of(ctx, s.type, s.n, s.vocab, s.blocks, 0);
+    f.tiles = dense::plan_of(ctx, s.vocab, s.n, (uint64_t)s.blocks * (s.parts == 3 ? kOfFloats.number : 1), 0);
     const uint32_t columns = f.narrow ? 16 * f.fragments : dense::kTiles[f.tiles.kind].columns;
     f.n_parts = (uint32_t)cnr_ceil_div(s.vocab, columns);
     const uint64_t per_row = (uint64_t)f.n_parts * sizeof(Stats), most = kStatsBytes / (per_row + 1) / 256 * 256;
@@ -718,39 +728,36 @@ ForwardPlan forward_plan(const cnr_ctx *ctx, const Sizes &s) {
     return f;
 }
 
+uint32_t dz_parts(const Sizes &s, bool two) { return s.parts == 3 ? 3 : two ? 2 : 1; }
 struct BackwardPlan {
-    uint64_t piece, width;     // of the vocabulary; columns of dz, whole blocks
-    uint64_t tokens;           // rows of dz^T's rows, whole blocks
+    uint64_t piece, width;  // of the vocabulary; columns of dz, whole blocks
     dense::Plan hidden, weight;
-    uint64_t scale, rows, dz, dz_t, low, hidden_t, weight_t, hidden_at, weight_at, sum, partial, bytes;
+    uint64_t scale, rows, dz, hidden_at, weight_at, sum, partial, bytes;
 };
-// (low_part: dweight in fp32 from 16-bit operands.)
-BackwardPlan backward_plan(const cnr_ctx *ctx, const Sizes &s, bool low_part) {
+// (two: dweight in fp32 from 16-bit operands, by dz in two parts.  in_place: the weight is read where it is.)
+BackwardPlan backward_plan(const cnr_ctx *ctx, const Sizes &s, bool two, bool in_place) {
     BackwardPlan b = {};
-    uint64_t piece = 2 * kPieceBytes / (s.n * s.element), by_weight = kPieceBytes / s.row;
-    piece = rounded(piece < by_weight ? piece : by_weight, 256);
-    if (piece == 0) piece = 256;
+    const uint32_t parts = dz_parts(s, two);
+    uint64_t piece = 2 * kPieceBytes / (s.n * 2 * parts);
+    const uint64_t by_weight = kPieceBytes / s.row;
+    if (!in_place && piece > by_weight) piece = by_weight;
+    piece = rounded(piece ? piece : 1, 256);
     // pieces of one size
     const uint64_t pieces = cnr_ceil_div(s.vocab, piece);
     b.piece = rounded(cnr_ceil_div(s.vocab, pieces), 256);
     if (b.piece > s.vocab) b.piece = s.vocab;
-    const uint64_t per_block = dense::kBlockBytes / s.element;
-    b.width = rounded(b.piece, per_block);
-    b.tokens = rounded(s.n, per_block);
-    b.hidden = dense::plan_of(ctx, s.type, s.n, s.dim, b.width / per_block, kPartBytes);
-    b.weight = dense::plan_of(ctx, s.type, b.piece, s.dim, b.tokens / per_block, kPartBytes);
+    b.width = rounded(b.piece, dense::kBlockElements);
+    const uint32_t floats = s.parts == 3 ? kOfFloats.number : 1;
+    b.hidden = dense::plan_of(ctx, s.dim, s.n, b.width / dense::kBlockElements * floats, kPartBytes);
+    b.weight = dense::plan_of(ctx, s.dim, b.piece, cnr_ceil_div(s.n, dense::kBlockElements) * (two ? 2 : floats), kPartBytes);
     const uint64_t across = rounded(s.dim, 4) * sizeof(float);
     const uint64_t parts_hidden = b.hidden.splits > 1 ? b.hidden.splits * s.n * across : 0, parts_weight = b.weight.splits > 1 ? b.weight.splits * b.piece * across : 0;
     Room room;
     b.scale = room.take(2 * sizeof(float));
     b.rows = room.take(rounded(s.n, 256) * sizeof(RowGradient));
-    b.dz = room.take(s.n * b.width * s.element);
-    b.low = b.piece * b.tokens;
-    b.dz_t = room.take(b.low * s.element * (low_part ? 2 : 1));
-    b.hidden_t = room.take(s.dim * b.tokens * s.element);
-    b.weight_t = room.take(s.dim * b.width * s.element);
+    b.dz = room.take(s.n * b.width * 2 * parts);
     b.hidden_at = room.take(s.n * s.row);
-    b.weight_at = room.take(b.piece * s.row);
+    b.weight_at = room.take(in_place ? 0 : b.piece * s.row);
     b.sum = room.take(pieces > 1 ? s.n * s.dim * sizeof(float) : 0);
     b.partial = room.take(parts_hidden > parts_weight ? parts_hidden : parts_weight);
     b.bytes = room.used;
@@ -759,8 +766,8 @@ BackwardPlan backward_plan(const cnr_ctx *ctx, const Sizes &s, bool low_part) {
 
 uint64_t least(uint64_t a, uint64_t b) { return a < b ? a : b; }
 // At least what the plans take for n rows or fewer: each part's largest size.
-uint64_t room_for(const Sizes &s, bool training, bool low_part) {
-    const uint64_t most_weight = least(s.vocab, rounded(kPieceBytes / s.row, 256)), small = least(s.n, 256), per_block = dense::kBlockBytes / s.element;
+uint64_t room_for(const Sizes &s, bool training, bool two) {
+    const uint64_t most_weight = least(s.vocab, rounded(kPieceBytes / s.row, 256)), small = least(s.n, 256);
     Room f;
     const uint64_t stats = cnr_ceil_div(s.vocab, 64) * sizeof(Stats), narrow = least(s.n, kNarrowRows) * cnr_ceil_div(s.vocab, 16) * sizeof(Stats);
     uint64_t parts = least(s.n * stats, kStatsBytes);
@@ -772,38 +779,30 @@ uint64_t room_for(const Sizes &s, bool training, bool low_part) {
     }
     if (!training) return f.used;
     Room b;
-    const uint64_t tokens = rounded(s.n, per_block), vocab = rounded(s.vocab, per_block), over = 2 * kPieceBytes + 256 * s.n * s.element;
+    const uint64_t of_dz = s.n * 2 * dz_parts(s, two);
     b.take(2 * sizeof(float));
     b.take(rounded(s.n, 256) * sizeof(RowGradient));
-    b.take(least(s.n * vocab * s.element, over));
-    b.take(least(tokens * s.vocab * s.element, over + per_block * most_weight * s.element) * (low_part ? 2 : 1));
-    b.take(s.dim * tokens * s.element);
-    b.take(s.dim * rounded(most_weight, per_block) * s.element);
+    b.take(least(of_dz * rounded(s.vocab, dense::kBlockElements), 2 * kPieceBytes + 256 * of_dz));
     b.take(s.n * s.row);
     b.take(most_weight * s.row);
     b.take(s.n * s.dim * sizeof(float));
-    b.take(least(dense::kMaxSplits * (s.n > most_weight ? s.n : most_weight) * rounded(s.dim, 4) * sizeof(float), kPartBytes));
+    b.take(kPartBytes);
     return b.used > f.used ? b.used : f.used;
 }
 
-struct Operand {
-    const void *at;
-    uint64_t bytes;  // from row to row
-};
-// Rows as a product can read them: where they are, or laid out in `space`.
+// Rows as a product can read them along k: where they are, or laid out in `space`.
 template <typename T>
-Operand laid_out(const T *src, uint64_t stride, uint64_t rows, const Sizes &s, void *space, hipStream_t to) {
-    if (whole_rows(src, stride, s.dim, rows, sizeof(T))) return {src, stride * sizeof(T)};
-    const uint32_t pieces = (uint32_t)(s.row / 16);
-    hipLaunchKernelGGL((lay_out_kernel<T>), dim3((unsigned)cnr_ceil_div(rows * pieces, kBlock)), dim3(kBlock), 0, to, src, stride, (uint32_t)rows, (uint32_t)s.dim, (T *)space,
-                       pieces);
-    return {space, s.row};
+dense::Operand laid_out(const T *src, uint64_t stride, uint64_t rows, const Sizes &s, const RowGradient *keep, void *space, hipStream_t to) {
+    const uint32_t part = s.blocks * dense::kBlockBytes;
+    if (!keep && whole_rows(s.type, src, stride, s.dim, rows)) return {src, stride * sizeof(T), part, 0, 0};
+    const uint32_t pieces = part / 16;
+    hipLaunchKernelGGL((lay_out_kernel<T>), dim3((unsigned)cnr_ceil_div(rows * pieces, kBlock)), dim3(kBlock), 0, to, src, stride, (uint32_t)rows, (uint32_t)s.dim, keep,
+                       (u32x4 *)space, pieces);
+    return {space, s.row, (uint32_t)s.row, part, 0};
 }
-
-template <typename T>
-void turn(const T *src, uint64_t stride, uint64_t rows, uint64_t columns, const RowGradient *keep, T *dst, uint64_t to_stride, hipStream_t to) {
-    hipLaunchKernelGGL((turn_kernel<T>), dim3((unsigned)cnr_ceil_div(to_stride, 64), (unsigned)cnr_ceil_div(columns, 64)), dim3(kBlock), 0, to, src, stride, (uint32_t)rows,
-                       (uint32_t)columns, keep, dst, to_stride);
+dense::Operand in_terms(dense::Operand o, uint32_t parts) {
+    o.parts = parts;
+    return o;
 }
 
 TargetArgs targets_of(const cnr_targets &t) {
@@ -818,6 +817,10 @@ TargetArgs targets_of(const cnr_targets &t) {
     a.temperature = t.logits ? t.temperature : 1.0f;
     return a;
 }
+
+// The type of the elements that products of a type are made of.
+template <int TYPE>
+constexpr int kOf = TYPE == CNR_FLOAT_F16 ? CNR_FLOAT_F16 : CNR_FLOAT_BF16;
 
 template <int TYPE>
 void forward(cnr_ctx *ctx, const cnr_vocabulary &v, const cnr_targets &t, float *loss, float *state, void *workspace, hipStream_t to) {
@@ -855,15 +858,16 @@ void forward(cnr_ctx *ctx, const cnr_vocabulary &v, const cnr_targets &t, float 
             else
                 hipLaunchKernelGGL((narrow_kernel<TYPE, 1, 4>), grid, dim3(kBlock), 0, to, a);
         } else {
-            const Operand a = laid_out(x, v.hidden_stride, rows, s, space + f.hidden, to);
+            const Terms terms = s.parts == 3 ? kOfFloats : kOne;
+            const dense::Operand x_at = in_terms(laid_out(x, v.hidden_stride, rows, s, nullptr, space + f.hidden, to), terms.down);
             const uint32_t columns = dense::kTiles[f.tiles.kind].columns;
-            const bool in_place = whole_rows(weight, v.weight_stride, v.dim, v.vocab, s.element);
+            const bool in_place = whole_rows(v.type, weight, v.weight_stride, v.dim, v.vocab);
             const uint64_t most = in_place ? rounded((1ull << 22) / cnr_ceil_div(rows, 64) * 64, 256) : f.piece;
             for (uint64_t v0 = 0; v0 < v.vocab; v0 += most) {
                 const uint64_t width = v.vocab - v0 < most ? v.vocab - v0 : most;
-                const Operand b = laid_out(weight + v0 * v.weight_stride, v.weight_stride, width, s, space + f.weight, to);
-                const dense::Args args = {a.at, b.at, a.bytes, b.bytes, (uint32_t)rows, (uint32_t)width, s.blocks, 1};
-                dense::launch<TYPE>(args, f.tiles.kind, KeepStats{parts + v0 / columns, f.n_parts, c}, to);
+                const dense::Operand w_at = in_terms(laid_out(weight + v0 * v.weight_stride, v.weight_stride, width, s, nullptr, space + f.weight, to), terms.across);
+                const dense::Args args = {w_at, x_at, (uint32_t)width, (uint32_t)rows, s.blocks, 0, terms.number, 1};
+                dense::launch<kOf<TYPE>, false, false>(args, f.tiles.kind, KeepStats{parts + v0 / columns, f.n_parts, c}, to);
             }
         }
         l.row0 = row0;
@@ -874,69 +878,60 @@ void forward(cnr_ctx *ctx, const cnr_vocabulary &v, const cnr_targets &t, float 
     }
 }
 
-template <int TYPE>
-void product(const dense::Args &args, const dense::Plan &plan, KeepSum k, hipStream_t to) {
+template <int TYPE, bool DOWN>
+void product(const dense::Args &args, const dense::Plan &plan, const KeepSum &k, hipStream_t to) {
     dense::Args a = args;
     a.splits = plan.splits <= a.blocks ? plan.splits : 1;
-    dense::launch<TYPE>(a, plan.kind, k, to);
+    dense::launch<kOf<TYPE>, true, DOWN>(a, plan.kind, k, to);
     if (a.splits > 1)
-        hipLaunchKernelGGL(join_sums_kernel, dim3((unsigned)cnr_ceil_div((uint64_t)a.m * (k.partial_stride / 4), kBlock)), dim3(kBlock), 0, to, k, a.m, a.n, a.splits);
+        hipLaunchKernelGGL(join_sums_kernel, dim3((unsigned)cnr_ceil_div((uint64_t)a.rows * (k.partial_stride / 4), kBlock)), dim3(kBlock), 0, to, k, a.rows, a.columns, a.splits);
 }
 
-template <int TYPE, bool LOW>
+template <int TYPE, int PARTS>
 void backward(cnr_ctx *ctx, const cnr_vocabulary &v, const cnr_targets &t, const float *state, const float *dloss, void *dhidden, uint64_t dhidden_stride, void *dweight,
               cnr_float_type dweight_type, uint64_t dweight_stride, bool accumulate, void *workspace, hipStream_t to) {
     typedef typename Element<TYPE>::type T;
+    typedef typename Element<kOf<TYPE>>::type Part;
     const Sizes s = sizes_of(v.n, v.vocab, v.dim, v.type);
-    const BackwardPlan b = backward_plan(ctx, s, LOW);
+    const BackwardPlan b = backward_plan(ctx, s, PARTS == 2, whole_rows(v.type, v.weight, v.weight_stride, v.dim, v.vocab));
     uint8_t *space = reinterpret_cast<uint8_t *>(workspace);
-    const T *hidden = reinterpret_cast<const T *>(v.hidden), *weight = reinterpret_cast<const T *>(v.weight);
+    const T *weight = reinterpret_cast<const T *>(v.weight);
     const TargetArgs targets = targets_of(t);
     RowGradient *rows = reinterpret_cast<RowGradient *>(space + b.rows);
     float *scale = reinterpret_cast<float *>(space + b.scale);
     hipLaunchKernelGGL(rows_kernel, dim3(1), dim3(1024), 0, to, state, dloss, v.n, targets.temperature, TYPE == CNR_FLOAT_F16, rows, scale);
-    T *hidden_t = reinterpret_cast<T *>(space + b.hidden_t), *weight_t = reinterpret_cast<T *>(space + b.weight_t);
-    if (dweight) turn(hidden, v.hidden_stride, v.n, v.dim, rows, hidden_t, b.tokens, to);
-    const Operand x = laid_out(hidden, v.hidden_stride, v.n, s, space + b.hidden_at, to);
-    KeepGradient<TYPE, LOW> k;
-    k.dz = dhidden ? reinterpret_cast<T *>(space + b.dz) : nullptr;
-    k.dz_t = dweight ? reinterpret_cast<T *>(space + b.dz_t) : nullptr;
-    k.stride_t = b.tokens;
-    k.low = b.low;
+    const dense::Operand x = laid_out(reinterpret_cast<const T *>(v.hidden), v.hidden_stride, v.n, s, rows, space + b.hidden_at, to);
+    KeepGradient<kOf<TYPE>, PARTS> k;
+    k.dz = reinterpret_cast<Part *>(space + b.dz);
     k.rows = rows;
     k.c = kLog2e / targets.temperature;
     KeepSum sum;
     sum.scale = TYPE == CNR_FLOAT_F16 ? scale + 1 : nullptr;
     sum.partial = reinterpret_cast<float *>(space + b.partial);
     sum.partial_stride = rounded(v.dim, 4);
-    const Target between = {space + b.sum, v.dim, CNR_FLOAT_F32};
+    const Target between = {space + b.sum, v.dim, CNR_FLOAT_F32}, none = {nullptr, 0, CNR_FLOAT_F32};
+    const Terms logits = PARTS == 3 ? kOfFloats : kOne, to_hidden = logits, to_weight = PARTS == 3 ? kOfFloats : PARTS == 2 ? kOfTwoParts : kOne;
+    const uint32_t n = (uint32_t)v.n, dim = (uint32_t)v.dim;
     for (uint64_t v0 = 0; v0 < v.vocab; v0 += b.piece) {
-        const uint64_t width = v.vocab - v0 < b.piece ? v.vocab - v0 : b.piece;
-        const T *w = weight + v0 * v.weight_stride;
-        const uint32_t blocks = blocks_of(width, s.element);
-        k.stride = (uint64_t)blocks * dense::kBlockBytes / s.element;
-        const Operand y = laid_out(w, v.weight_stride, width, s, space + b.weight_at, to);
-        const dense::Plan tiles = dense::plan_of(ctx, v.type, v.n, width, s.blocks, 0);
-        dense::launch<TYPE>(dense::Args{x.at, y.at, x.bytes, y.bytes, (uint32_t)v.n, (uint32_t)width, s.blocks, 1}, tiles.kind, k, to);
-        hipLaunchKernelGGL((entries_kernel<TYPE, LOW>), dim3((unsigned)cnr_ceil_div(v.n * t.top, kBlock)), dim3(kBlock), 0, to, k, targets, state + v.n, state + v.n * (1 + t.top),
-                           v.n, (uint32_t)t.top, v0, (uint32_t)width);
+        const uint32_t width = (uint32_t)(v.vocab - v0 < b.piece ? v.vocab - v0 : b.piece), blocks = (uint32_t)cnr_ceil_div(width, dense::kBlockElements);
+        k.width = (uint64_t)blocks * dense::kBlockElements;
+        k.stride = PARTS * k.width;
+        const dense::Operand w = laid_out(weight + v0 * v.weight_stride, v.weight_stride, width, s, nullptr, space + b.weight_at, to);
+        const dense::Plan tiles = dense::plan_of(ctx, width, v.n, s.blocks * logits.number, 0);
+        dense::launch<kOf<TYPE>, false, false>(dense::Args{in_terms(w, logits.across), in_terms(x, logits.down), width, n, s.blocks, 0, logits.number, 1}, tiles.kind, k, to);
+        hipLaunchKernelGGL((entries_kernel<kOf<TYPE>, PARTS>), dim3((unsigned)cnr_ceil_div(v.n * t.top, kBlock)), dim3(kBlock), 0, to, k, targets, state + v.n,
+                           state + v.n * (1 + t.top), v.n, (uint32_t)t.top, v0, width);
+        const dense::Operand dz = {k.dz, k.stride * 2, (uint32_t)(k.stride * 2), (uint32_t)(k.width * 2), 0};
         if (dhidden) {
-            turn(w, v.weight_stride, width, v.dim, nullptr, weight_t, k.stride, to);
-            const bool first = v0 == 0, last = v0 + width == v.vocab;
-            sum.there = first ? Target{nullptr, 0, CNR_FLOAT_F32} : between;
-            sum.out = last ? Target{dhidden, dhidden_stride, v.type} : between;
-            product<TYPE>(dense::Args{k.dz, weight_t, k.stride * s.element, k.stride * s.element, (uint32_t)v.n, (uint32_t)v.dim, blocks, 1}, b.hidden, sum, to);
+            sum.there = v0 == 0 ? none : between;
+            sum.out = v0 + width == v.vocab ? Target{dhidden, dhidden_stride, v.type} : between;
+            product<TYPE, false>(dense::Args{in_terms(w, to_hidden.across), in_terms(dz, to_hidden.down), dim, n, blocks, width, to_hidden.number, 1}, b.hidden, sum, to);
         }
         if (dweight) {
-            const Target out = {reinterpret_cast<uint8_t *>(dweight) + v0 * dweight_stride * cnr_float_bytes(dweight_type), dweight_stride, dweight_type};
-            sum.out = out;
-            sum.there = accumulate ? out : Target{nullptr, 0, CNR_FLOAT_F32};
-            const uint64_t bytes = b.tokens * s.element;
-            for (int part = 0; part < (LOW ? 2 : 1); ++part) {
-                product<TYPE>(dense::Args{k.dz_t + part * b.low, hidden_t, bytes, bytes, (uint32_t)width, (uint32_t)v.dim, (uint32_t)(bytes / dense::kBlockBytes), 1}, b.weight,
-                              sum, to);
-                sum.there = out;
-            }
+            sum.out = {reinterpret_cast<uint8_t *>(dweight) + v0 * dweight_stride * cnr_float_bytes(dweight_type), dweight_stride, dweight_type};
+            sum.there = accumulate ? sum.out : none;
+            product<TYPE, true>(dense::Args{in_terms(x, to_weight.across), in_terms(dz, to_weight.down), dim, width, (uint32_t)cnr_ceil_div(v.n, dense::kBlockElements), n,
+                                            to_weight.number, 1}, b.weight, sum, to);
         }
     }
 }
@@ -1015,17 +1010,20 @@ cnr_status cnr_vocabulary_loss_backward(cnr_ctx *ctx, const cnr_vocabulary *voca
         return cnr_launch_status(ctx);
     }
     const bool low = dweight && dweight_type == CNR_FLOAT_F32;
-    if (backward_plan(ctx, sizes_of(v.n, v.vocab, v.dim, v.type), low && v.type != CNR_FLOAT_F32).bytes > workspace_bytes) return CNR_E_INVALID;
+    if (backward_plan(ctx, sizes_of(v.n, v.vocab, v.dim, v.type), low && v.type != CNR_FLOAT_F32, whole_rows(v.type, v.weight, v.weight_stride, v.dim, v.vocab)).bytes > workspace_bytes)
+        return CNR_E_INVALID;
     auto call = [&](auto kind, auto part) {
         backward<decltype(kind)::value, decltype(part)::value>(ctx, v, *targets, state, dloss, dhidden, dhidden_stride, dweight, dweight_type, dweight_stride, accumulate != 0,
                                                                workspace, to);
     };
     if (v.type == CNR_FLOAT_F32)
-        call(std::integral_constant<int, CNR_FLOAT_F32>(), std::false_type());
+        call(std::integral_constant<int, CNR_FLOAT_F32>(), std::integral_constant<int, 3>());
     else if (v.type == CNR_FLOAT_BF16)
-        low ? call(std::integral_constant<int, CNR_FLOAT_BF16>(), std::true_type()) : call(std::integral_constant<int, CNR_FLOAT_BF16>(), std::false_type());
+        low ? call(std::integral_constant<int, CNR_FLOAT_BF16>(), std::integral_constant<int, 2>())
+            : call(std::integral_constant<int, CNR_FLOAT_BF16>(), std::integral_constant<int, 1>());
     else
-        low ? call(std::integral_constant<int, CNR_FLOAT_F16>(), std::true_type()) : call(std::integral_constant<int, CNR_FLOAT_F16>(), std::false_type());
+        low ? call(std::integral_constant<int, CNR_FLOAT_F16>(), std::integral_constant<int, 2>())
+            : call(std::integral_constant<int, CNR_FLOAT_F16>(), std::integral_constant<int, 1>());
     return cnr_launch_status(ctx);
 }
 

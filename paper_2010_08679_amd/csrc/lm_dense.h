@@ -342,7 +342,8 @@ __global__ void __launch_bounds__(WM * WN * kWave, 2) tile_kernel(const Args p, 
 
 // ---- which tiles ----------------------------------------------------------------------------------------------
 //
-// A workgroup's time for a block by how many share a compute unit, in us.
+// A workgroup's time for a block by how many share a compute unit, in us, and what it takes besides: until the first block is there, and for its outputs,
+// which a unit writes at its share of what memory takes and which only another workgroup's products hide.
 struct Tiles {
     uint32_t columns, rows, threads, resident;
     float block[2];
@@ -355,35 +356,50 @@ constexpr Tiles kTiles[] = {
     {64, 64, 256, 2, {0.28f, 0.42f}},   // four waves of 32 x 32, four stages
 };
 constexpr int kKinds = (int)(sizeof(kTiles) / sizeof(kTiles[0]));
-constexpr uint32_t kMaxSplits = 16, kMinBlocks = 4;  // parts of a sum, blocks of a part
+constexpr uint32_t kMaxSplits = 32, kMinBlocks = 4;  // parts of a sum, blocks of a part
 
 struct Plan {
     int kind;  // of kTiles
     uint32_t splits;
+    float time;  // estimated, us
 };
 // The tiles and parts of the shortest estimated time; parts of up to part_bytes in all, of rows of a multiple of four floats.
-static inline Plan plan_of(const cnr_ctx *ctx, uint64_t columns, uint64_t rows, uint64_t blocks, uint64_t part_bytes) {
+static inline Plan plan_of(const cnr_ctx *ctx, uint64_t columns, uint64_t rows, uint64_t blocks, float out_bytes, uint64_t part_bytes) {
     const float units = ctx ? (float)ctx->n_cu : 256.0f;
-    const float memory = ((float)columns + (float)rows) * (float)blocks * (float)kBlockBytes / 4.7e6f;
-    Plan best = {0, 1};
-    float least = 3e38f;
+    const float outputs = (float)columns * (float)rows;
+    const float memory = (((float)columns + (float)rows) * (float)blocks * (float)kBlockBytes + outputs * out_bytes) / 4.7e6f;
+    Plan best = {0, 1, 3e38f};
     for (int i = 0; i < kKinds; ++i) {
         const Tiles &t = kTiles[i];
         const float tiles = (float)cnr_ceil_div(columns, t.columns) * (float)cnr_ceil_div(rows, t.rows);
-        for (uint32_t s = 1; s == 1 || (s <= kMaxSplits && blocks >= (uint64_t)s * kMinBlocks && s * rows * cnr_ceil_div(columns, 4) * 16 <= part_bytes); s *= 2) {
+        if (tiles * (float)t.threads >= 4.2e9f) continue;  // grids count threads in 32 bits
+        for (uint32_t s = 1; s == 1 || (s <= kMaxSplits && blocks >= (uint64_t)s * kMinBlocks && tiles * (float)s <= 4.0f * units &&
+                                        s * rows * cnr_ceil_div(columns, 4) * 16 <= part_bytes); ++s) {
             const float groups = tiles * (float)s, round = units * (float)t.resident, rounds = floorf(groups / round);
-            if (groups * (float)t.threads >= 4.2e9f) continue;  // grids count threads in 32 bits
             const float rest = ceilf((groups - rounds * round) / units);  // workgroups on a unit in the last round
-            float time = ceilf((float)blocks / (float)s) * (rounds * t.block[t.resident - 1] + (rest > 0.0f ? t.block[(int)rest - 1] : 0.0f));
-            time += 1.5f * (rounds + (rest > 0.0f ? 1.0f : 0.0f));
+            const float each = 2.5f + (float)(t.columns * t.rows) * (s > 1 ? 4.0f : out_bytes) * units / 4.7e6f;
+            const float some = ceilf((float)blocks / (float)s);
+            float time = rounds * (some * t.block[t.resident - 1] + each) + (rest > 0.0f ? some * t.block[(int)rest - 1] + each : 0.0f);
             time = (time > memory ? time : memory) + 0.25f * (time < memory ? time : memory);  // one does not quite hide the other
-            if (s > 1) time += 3.5f + (float)(s + 1) * (float)rows * (float)columns * 4.0f / 3e6f;  // writing the parts, and joining them
-            if (time < least) {
-                least = time;
-                best = {i, s};
-            }
+            if (s > 1) time += 3.5f + (float)(s + 1) * outputs * 4.0f / 3e6f;  // joining the parts
+            if (time < best.time) best = {i, s, time};
         }
     }
+    return best;
+}
+// Rows [0, first_rows) by one plan and the others by another: whole rounds of workgroups, and what is left in smaller tiles or parts of its sums.
+struct Plans {
+    Plan first, rest;
+    uint64_t first_rows;
+};
+static inline Plans plans_of(const cnr_ctx *ctx, uint64_t columns, uint64_t rows, uint64_t blocks, float out_bytes, uint64_t part_bytes) {
+    Plans best = {plan_of(ctx, columns, rows, blocks, out_bytes, part_bytes), {0, 1, 0.0f}, rows};
+    const Tiles &t = kTiles[0];
+    const uint64_t units = ctx ? (uint64_t)ctx->n_cu : 256, across = cnr_ceil_div(columns, t.columns), rounds = cnr_ceil_div(rows, t.rows) * across / units;
+    const uint64_t first_rows = rounds * units / across * t.rows;
+    if (first_rows == 0 || first_rows >= rows) return best;
+    const Plan first = plan_of(ctx, columns, first_rows, blocks, out_bytes, 0), rest = plan_of(ctx, columns, rows - first_rows, blocks, out_bytes, part_bytes);
+    if (first.time + rest.time + 3.0f < best.first.time) best = {first, rest, first_rows};
     return best;
 }
 

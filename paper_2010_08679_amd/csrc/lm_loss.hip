@@ -118,9 +118,12 @@ struct KeepStats {
     }
 };
 
-// What the backward pass knows of a row: log2 of its sum of exponentials and dloss / T, scaled; 0: the row adds nothing.
-struct RowGradient {
+// What the backward pass knows of a row: log2 of its sum of exponentials and dloss / T, scaled (0: the row adds nothing), and its target where it has
+// one (else kNoTarget).
+constexpr uint32_t kNoTarget = 0xffffffffu;
+struct __attribute__((aligned(16))) RowGradient {
     float lse2, gradient;
+    uint32_t target, unused;
 };
 
 // v as PARTS numbers of 16 bits that add up to it.
@@ -141,7 +144,27 @@ struct KeepGradient {
     T *dz;
     uint64_t width, stride;    // of a part, of a row: PARTS * width, whole blocks
     const RowGradient *rows;   // up to a multiple of 256
+    uint32_t first;            // token of the first column
     float c;
+    template <int MF, int NF, bool TARGET, typename Place>
+    __device__ __forceinline__ void write(const dense::Args &p, const Place &at, const f32x4 (&acc)[MF][NF], int g, const RowGradient &r, uint32_t target, T *to) const {
+#pragma unroll
+        for (int from = 0; from < 4 * MF; from += 8) {
+            if (at.column + from >= width) continue;
+            Pack<T, 8> w[PARTS];
+#pragma unroll
+            for (int j = 0; j < 8; ++j) {
+                float v = exp2_of(__builtin_fmaf(at.value(acc, from + j, g), c, -r.lse2));
+                if (TARGET && target == (uint32_t)(from + j)) v -= 1.0f;
+                T part[PARTS];
+                apart<TYPE, PARTS>(r.gradient == 0.0f || at.column + from + j >= p.columns ? 0.0f : r.gradient * v, part);
+#pragma unroll
+                for (int i = 0; i < PARTS; ++i) w[i].v[j] = part[i];
+            }
+#pragma unroll
+            for (int i = 0; i < PARTS; ++i) *reinterpret_cast<Pack<T, 8> *>(to + i * width + from) = w[i];
+        }
+    }
     template <uint32_t TM, uint32_t TN, int WM, typename Place, int MF, int NF>
     __device__ __forceinline__ void finish(const dense::Args &p, const Place &at, const f32x4 (&acc)[MF][NF]) const {
 #pragma unroll
@@ -150,21 +173,11 @@ struct KeepGradient {
             const RowGradient r = rows[row];
             if (row >= p.rows) continue;
             T *to = dz + row * stride + at.column;
-#pragma unroll
-            for (int first = 0; first < 4 * MF; first += 8) {
-                if (at.column + first >= width) continue;
-                Pack<T, 8> w[PARTS];
-#pragma unroll
-                for (int j = 0; j < 8; ++j) {
-                    const float z = at.value(acc, first + j, g);
-                    T part[PARTS];
-                    apart<TYPE, PARTS>(r.gradient == 0.0f || at.column + first + j >= p.columns ? 0.0f : r.gradient * exp2_of(__builtin_fmaf(z, c, -r.lse2)), part);
-#pragma unroll
-                    for (int i = 0; i < PARTS; ++i) w[i].v[j] = part[i];
-                }
-#pragma unroll
-                for (int i = 0; i < PARTS; ++i) *reinterpret_cast<Pack<T, 8> *>(to + i * width + first) = w[i];
-            }
+            const uint32_t target = r.target - first - at.column;  // among the lane's columns, or large
+            if (__any(target < 4 * MF))
+                write<MF, NF, true>(p, at, acc, g, r, target, to);
+            else
+                write<MF, NF, false>(p, at, acc, g, r, target, to);
         }
     }
 };
@@ -460,12 +473,12 @@ struct LossArgs {
     float *lse2, *picked, *share;  // state, or NULL
     cnr_dev_errors *err;
 };
-// The product of two rows, over the lanes of a wave.
-template <typename T>
+// The product of two rows by THREADS threads: the sum of this wave's.
+template <uint32_t THREADS, typename T>
 __device__ __forceinline__ float dot(const T *x, const T *y, uint32_t dim) {
     constexpr uint32_t kPer = 16 / sizeof(T);
     float sum = 0.0f;
-    for (uint32_t at = tid_x() % kWave * kPer; at < dim; at += kWave * kPer) {
+    for (uint32_t at = tid_x() % THREADS * kPer; at < dim; at += THREADS * kPer) {
         if (at + kPer <= dim) {
             const Pack<T, kPer> a = *reinterpret_cast<const Pack<T, kPer> *>(x + at), b = *reinterpret_cast<const Pack<T, kPer> *>(y + at);
 #pragma unroll
@@ -487,16 +500,33 @@ __global__ void __launch_bounds__(kBlock) loss_kernel(const LossArgs p) {
     __shared__ float share[SOFT ? kMaxTop : 1];
     const uint32_t lane = tid_x() % kWave, wave = (uint32_t)__builtin_amdgcn_readfirstlane((int)(tid_x() / kWave));
     const uint64_t row = p.row0 + wg_x();
+    // eight of the row's parts to a thread at a time, so that their loads and exponentials do not wait for each other
     Stats s = {-__builtin_inff(), 0.0f};
-    for (uint32_t i = tid_x(); i < p.n_parts; i += kBlock) s = join(s, p.parts[(uint64_t)wg_x() * p.n_parts + i]);
+    for (uint32_t first = tid_x(); first < p.n_parts; first += 8 * kBlock) {
+        Stats part[8];
 #pragma unroll
-    for (int by = 1; by < kWave; by *= 2) s = join(s, Stats{__shfl_xor(s.top, by), __shfl_xor(s.sum, by)});
+        for (uint32_t i = 0; i < 8; ++i) {
+            part[i] = {-__builtin_inff(), 0.0f};
+            if (first + i * kBlock < p.n_parts) part[i] = p.parts[(uint64_t)wg_x() * p.n_parts + first + i * kBlock];
+        }
+        float top = s.top;
+#pragma unroll
+        for (uint32_t i = 0; i < 8; ++i) top = __builtin_fmaxf(top, part[i].top);
+        const float at = top == -__builtin_inff() ? 0.0f : top;
+        float sum = s.sum * exp2_of(s.top - at);
+#pragma unroll
+        for (uint32_t i = 0; i < 8; ++i) sum = __builtin_fmaf(part[i].sum, exp2_of(part[i].top - at), sum);
+        s = {top, sum};
+    }
+    {
+        const float top = wave_max(s.top), at = top == -__builtin_inff() ? 0.0f : top;
+        s = {top, wave_sum(s.sum * exp2_of(s.top - at))};
+    }
     if (lane == 0) joined[wave] = s;
     const uint32_t top = SOFT ? p.targets.top : 1;
     const float heat = SOFT ? p.targets.temperature : 1.0f, c = kLog2e / heat;
     float teacher_top = 0.0f, teacher_sum = 1.0f, negative_entropy = 0.0f;
     bool counts = true;
-    int64_t only = -1;
     if constexpr (SOFT) {
         // The teacher's distribution over the row's entries.
         float largest = -__builtin_inff();
@@ -534,22 +564,30 @@ __global__ void __launch_bounds__(kBlock) loss_kernel(const LossArgs p) {
         const int64_t t = token_of(p.targets, row, 0);
         counts = t >= 0 && (uint64_t)t < p.vocab;
         if (t >= 0 && !counts && tid_x() == 0) atomicAdd(&p.err->n_bad_indices, 1ull);
-        only = counts ? t : -1;
+        // its logit, a part of the sum to each wave
+        if (counts) {
+            const float z = dot<kBlock>(reinterpret_cast<const T *>(p.hidden) + row * p.hidden_stride, reinterpret_cast<const T *>(p.weight) + (uint64_t)t * p.weight_stride, p.dim);
+            if (lane == 0) sums[wave][0] = z;
+        }
         __syncthreads();
     }
     s = joined[0];
     for (int w = 1; w < kWavesPerBlock; ++w) s = join(s, joined[w]);
     const float lse2 = s.top + __builtin_amdgcn_logf(s.sum);  // to base 2
-    // Logits of the entries, an entry to a wave.
-    const T *x = reinterpret_cast<const T *>(p.hidden) + row * p.hidden_stride;
     float expected = 0.0f;  // sum of share * logit
-    for (uint32_t j = wave; j < top; j += kWavesPerBlock) {
-        const int64_t t = SOFT ? token[j] : only;
-        const float q = SOFT ? share[j] : 1.0f;
-        float z = 0.0f;
-        if (t >= 0) z = dot(x, reinterpret_cast<const T *>(p.weight) + (uint64_t)t * p.weight_stride, p.dim);
-        if (t >= 0 && q != 0.0f) expected = __builtin_fmaf(q, z, expected);
-        if (p.picked && lane == 0) p.picked[row * top + j] = z;
+    if constexpr (SOFT) {
+        // Logits of the entries, an entry to a wave.
+        const T *x = reinterpret_cast<const T *>(p.hidden) + row * p.hidden_stride;
+        for (uint32_t j = wave; j < top; j += kWavesPerBlock) {
+            const int64_t t = token[j];
+            const float q = share[j];
+            float z = 0.0f;
+            if (t >= 0) z = dot<kWave>(x, reinterpret_cast<const T *>(p.weight) + (uint64_t)t * p.weight_stride, p.dim);
+            if (t >= 0 && q != 0.0f) expected = __builtin_fmaf(q, z, expected);
+            if (p.picked && lane == 0) p.picked[row * top + j] = z;
+        }
+    } else if (counts) {
+        expected = (sums[0][0] + sums[1][0]) + (sums[2][0] + sums[3][0]);
     }
     if constexpr (SOFT) {
         // For the gradient the shares of a token that comes several times are at the first of them.
@@ -578,8 +616,6 @@ __global__ void __launch_bounds__(kBlock) loss_kernel(const LossArgs p) {
             expected += sums[w][0];
             negative_entropy += sums[w][1];
         }
-    } else if (p.share && tid_x() == 0) {
-        p.share[row] = counts ? 1.0f : 0.0f;
     }
     if (tid_x() == 0) {
         // (the largest logit and the expected one are subtracted first: of a certain token little is left)
@@ -591,21 +627,23 @@ __global__ void __launch_bounds__(kBlock) loss_kernel(const LossArgs p) {
 // ---- backward: rows and entries ---------------------------------------------------------------------------------
 
 // rows[i] up to a multiple of 256; scale = {by what dz is multiplied, its inverse}: for halves, whose range is small, the power of two that takes the
-// largest |dloss / T| to 2^13 to 2^14; 1 for the others.  One workgroup.
-__global__ void __launch_bounds__(1024) rows_kernel(const float *lse2, const float *dloss, uint64_t n, float temperature, int half, RowGradient *rows, float *scale) {
-    __shared__ float largest[16];
+// largest |dloss / T| to 2^13 to 2^14; 1 for the others.  Each workgroup looks for the largest itself.
+constexpr uint32_t kRowThreads = 1024, kRowGroups = 16;
+__global__ void __launch_bounds__(kRowThreads) rows_kernel(const float *lse2, const float *dloss, uint64_t n, const TargetArgs targets, uint64_t vocab, int half, RowGradient *rows,
+                                                           float *scale) {
+    __shared__ float largest[kRowThreads / kWave];
     float up = 1.0f, down = 1.0f;
     if (half) {
         float most = 0.0f;
-        for (uint64_t i = tid_x(); i < n; i += 1024) {
-            const float g = fabsf(dloss[i] / temperature);
+        for (uint64_t i = tid_x(); i < n; i += kRowThreads) {
+            const float g = fabsf(dloss[i] / targets.temperature);
             if (lse2[i] < __builtin_inff() && g < __builtin_inff()) most = __builtin_fmaxf(most, g);
         }
         most = wave_max(most);
         if (tid_x() % kWave == 0) largest[tid_x() / kWave] = most;
         __syncthreads();
         most = largest[0];
-        for (int w = 1; w < 16; ++w) most = __builtin_fmaxf(most, largest[w]);
+        for (uint32_t w = 1; w < kRowThreads / kWave; ++w) most = __builtin_fmaxf(most, largest[w]);
         if (most > 0.0f) {
             int e;
             (void)frexpf(most, &e);  // most = fraction 2^e, fraction from 1/2 to 1
@@ -615,14 +653,19 @@ __global__ void __launch_bounds__(1024) rows_kernel(const float *lse2, const flo
             down = ldexpf(1.0f, -e);
         }
     }
-    if (tid_x() == 0) {
+    if (wg_x() == 0 && tid_x() == 0) {
         scale[0] = up;
         scale[1] = down;
     }
     const uint64_t padded = (n + 255) / 256 * 256;
-    for (uint64_t i = tid_x(); i < padded; i += 1024) {
-        RowGradient r = {__builtin_inff(), 0.0f};
-        if (i < n && lse2[i] != __builtin_inff()) r = {lse2[i], dloss[i] / temperature * up};
+    for (uint64_t i = wg_x() * kRowThreads + tid_x(); i < padded; i += kRowGroups * kRowThreads) {
+        RowGradient r = {__builtin_inff(), 0.0f, kNoTarget, 0};
+        if (i < n && lse2[i] != __builtin_inff()) {
+            r.lse2 = lse2[i];
+            r.gradient = dloss[i] / targets.temperature * up;
+            const int64_t t = targets.logits ? -1 : token_of(targets, i, 0);
+            if (t >= 0 && (uint64_t)t < vocab) r.target = (uint32_t)t;
+        }
         rows[i] = r;
     }
 }
@@ -710,7 +753,7 @@ ForwardPlan forward_plan(const cnr_ctx *ctx, const Sizes &s) {
     f.narrow = s.n <= kNarrowRows;
     // Two fragments of the weight to a wave where that still gives every SIMD a wave.
     f.fragments = s.n > 1 && s.vocab >= 16384 ? 2 : 1;
-    f.tiles = dense::plan_of(ctx, s.vocab, s.n, (uint64_t)s.blocks * (s.parts == 3 ? kOfFloats.number : 1), 0);
+    f.tiles = dense::plan_of(ctx, s.vocab, s.n, (uint64_t)s.blocks * (s.parts == 3 ? kOfFloats.number : 1), 0.5f /* time for exponentials */, 0);
     const uint32_t columns = f.narrow ? 16 * f.fragments : dense::kTiles[f.tiles.kind].columns;
     f.n_parts = (uint32_t)cnr_ceil_div(s.vocab, columns);
     const uint64_t per_row = (uint64_t)f.n_parts * sizeof(Stats), most = kStatsBytes / (per_row + 1) / 256 * 256;
@@ -731,7 +774,6 @@ ForwardPlan forward_plan(const cnr_ctx *ctx, const Sizes &s) {
 uint32_t dz_parts(const Sizes &s, bool two) { return s.parts == 3 ? 3 : two ? 2 : 1; }
 struct BackwardPlan {
     uint64_t piece, width;  // of the vocabulary; columns of dz, whole blocks
-    dense::Plan hidden, weight;
     uint64_t scale, rows, dz, hidden_at, weight_at, sum, partial, bytes;
 };
 // (two: dweight in fp32 from 16-bit operands, by dz in two parts.  in_place: the weight is read where it is.)
@@ -747,11 +789,6 @@ BackwardPlan backward_plan(const cnr_ctx *ctx, const Sizes &s, bool two, bool in
     b.piece = rounded(cnr_ceil_div(s.vocab, pieces), 256);
     if (b.piece > s.vocab) b.piece = s.vocab;
     b.width = rounded(b.piece, dense::kBlockElements);
-    const uint32_t floats = s.parts == 3 ? kOfFloats.number : 1;
-    b.hidden = dense::plan_of(ctx, s.dim, s.n, b.width / dense::kBlockElements * floats, kPartBytes);
-    b.weight = dense::plan_of(ctx, s.dim, b.piece, cnr_ceil_div(s.n, dense::kBlockElements) * (two ? 2 : floats), kPartBytes);
-    const uint64_t across = rounded(s.dim, 4) * sizeof(float);
-    const uint64_t parts_hidden = b.hidden.splits > 1 ? b.hidden.splits * s.n * across : 0, parts_weight = b.weight.splits > 1 ? b.weight.splits * b.piece * across : 0;
     Room room;
     b.scale = room.take(2 * sizeof(float));
     b.rows = room.take(rounded(s.n, 256) * sizeof(RowGradient));
@@ -759,7 +796,7 @@ BackwardPlan backward_plan(const cnr_ctx *ctx, const Sizes &s, bool two, bool in
     b.hidden_at = room.take(s.n * s.row);
     b.weight_at = room.take(in_place ? 0 : b.piece * s.row);
     b.sum = room.take(pieces > 1 ? s.n * s.dim * sizeof(float) : 0);
-    b.partial = room.take(parts_hidden > parts_weight ? parts_hidden : parts_weight);
+    b.partial = room.take(kPartBytes);
     b.bytes = room.used;
     return b;
 }
@@ -881,10 +918,31 @@ void forward(cnr_ctx *ctx, const cnr_vocabulary &v, const cnr_targets &t, float 
 template <int TYPE, bool DOWN>
 void product(const dense::Args &args, const dense::Plan &plan, const KeepSum &k, hipStream_t to) {
     dense::Args a = args;
-    a.splits = plan.splits <= a.blocks ? plan.splits : 1;
+    a.splits = plan.splits;
     dense::launch<kOf<TYPE>, true, DOWN>(a, plan.kind, k, to);
     if (a.splits > 1)
         hipLaunchKernelGGL(join_sums_kernel, dim3((unsigned)cnr_ceil_div((uint64_t)a.rows * (k.partial_stride / 4), kBlock)), dim3(kBlock), 0, to, k, a.rows, a.columns, a.splits);
+}
+Target from_row(Target t, uint64_t row) {
+    if (t.out) t.out = reinterpret_cast<uint8_t *>(t.out) + row * t.stride * cnr_float_bytes((cnr_float_type)t.type);
+    return t;
+}
+template <int TYPE, bool DOWN>
+void product(cnr_ctx *ctx, const dense::Args &args, const KeepSum &k, hipStream_t to) {
+    const dense::Plans plans = dense::plans_of(ctx, args.columns, args.rows, (uint64_t)args.blocks * args.terms, (float)cnr_float_bytes((cnr_float_type)k.out.type) * (k.there.out ? 2.0f : 1.0f),
+                                               kPartBytes);
+    dense::Args a = args;
+    a.rows = (uint32_t)plans.first_rows;
+    product<TYPE, DOWN>(a, plans.first, k, to);
+    if (plans.first_rows == args.rows) return;
+    KeepSum rest = k;
+    rest.out = from_row(k.out, plans.first_rows);
+    rest.there = from_row(k.there, plans.first_rows);
+    a.rows = args.rows - a.rows;
+    const uint64_t skipped = plans.first_rows * (DOWN ? 2 : a.down.stride);
+    a.down.at = reinterpret_cast<const uint8_t *>(a.down.at) + skipped;
+    if (DOWN) a.down.row_bytes -= (uint32_t)skipped;
+    product<TYPE, DOWN>(a, plans.rest, rest, to);
 }
 
 template <int TYPE, int PARTS>
@@ -899,7 +957,8 @@ void backward(cnr_ctx *ctx, const cnr_vocabulary &v, const cnr_targets &t, const
     const TargetArgs targets = targets_of(t);
     RowGradient *rows = reinterpret_cast<RowGradient *>(space + b.rows);
     float *scale = reinterpret_cast<float *>(space + b.scale);
-    hipLaunchKernelGGL(rows_kernel, dim3(1), dim3(1024), 0, to, state, dloss, v.n, targets.temperature, TYPE == CNR_FLOAT_F16, rows, scale);
+    hipLaunchKernelGGL(rows_kernel, dim3((unsigned)least(cnr_ceil_div(v.n, kRowThreads), kRowGroups)), dim3(kRowThreads), 0, to, state, dloss, v.n, targets, v.vocab, TYPE == CNR_FLOAT_F16,
+                       rows, scale);
     const dense::Operand x = laid_out(reinterpret_cast<const T *>(v.hidden), v.hidden_stride, v.n, s, rows, space + b.hidden_at, to);
     KeepGradient<kOf<TYPE>, PARTS> k;
     k.dz = reinterpret_cast<Part *>(space + b.dz);
@@ -916,22 +975,24 @@ void backward(cnr_ctx *ctx, const cnr_vocabulary &v, const cnr_targets &t, const
         const uint32_t width = (uint32_t)(v.vocab - v0 < b.piece ? v.vocab - v0 : b.piece), blocks = (uint32_t)cnr_ceil_div(width, dense::kBlockElements);
         k.width = (uint64_t)blocks * dense::kBlockElements;
         k.stride = PARTS * k.width;
+        k.first = (uint32_t)v0;
         const dense::Operand w = laid_out(weight + v0 * v.weight_stride, v.weight_stride, width, s, nullptr, space + b.weight_at, to);
-        const dense::Plan tiles = dense::plan_of(ctx, width, v.n, s.blocks * logits.number, 0);
+        const dense::Plan tiles = dense::plan_of(ctx, width, v.n, s.blocks * logits.number, 2.0f * PARTS, 0);
         dense::launch<kOf<TYPE>, false, false>(dense::Args{in_terms(w, logits.across), in_terms(x, logits.down), width, n, s.blocks, 0, logits.number, 1}, tiles.kind, k, to);
-        hipLaunchKernelGGL((entries_kernel<kOf<TYPE>, PARTS>), dim3((unsigned)cnr_ceil_div(v.n * t.top, kBlock)), dim3(kBlock), 0, to, k, targets, state + v.n,
-                           state + v.n * (1 + t.top), v.n, (uint32_t)t.top, v0, width);
+        if (t.logits)
+            hipLaunchKernelGGL((entries_kernel<kOf<TYPE>, PARTS>), dim3((unsigned)cnr_ceil_div(v.n * t.top, kBlock)), dim3(kBlock), 0, to, k, targets, state + v.n,
+                               state + v.n * (1 + t.top), v.n, (uint32_t)t.top, v0, width);
         const dense::Operand dz = {k.dz, k.stride * 2, (uint32_t)(k.stride * 2), (uint32_t)(k.width * 2), 0};
         if (dhidden) {
             sum.there = v0 == 0 ? none : between;
             sum.out = v0 + width == v.vocab ? Target{dhidden, dhidden_stride, v.type} : between;
-            product<TYPE, false>(dense::Args{in_terms(w, to_hidden.across), in_terms(dz, to_hidden.down), dim, n, blocks, width, to_hidden.number, 1}, b.hidden, sum, to);
+            product<TYPE, false>(ctx, dense::Args{in_terms(w, to_hidden.across), in_terms(dz, to_hidden.down), dim, n, blocks, width, to_hidden.number, 1}, sum, to);
         }
         if (dweight) {
             sum.out = {reinterpret_cast<uint8_t *>(dweight) + v0 * dweight_stride * cnr_float_bytes(dweight_type), dweight_stride, dweight_type};
             sum.there = accumulate ? sum.out : none;
-            product<TYPE, true>(dense::Args{in_terms(x, to_weight.across), in_terms(dz, to_weight.down), dim, width, (uint32_t)cnr_ceil_div(v.n, dense::kBlockElements), n,
-                                            to_weight.number, 1}, b.weight, sum, to);
+            product<TYPE, true>(ctx, dense::Args{in_terms(x, to_weight.across), in_terms(dz, to_weight.down), dim, width, (uint32_t)cnr_ceil_div(v.n, dense::kBlockElements), n,
+                                            to_weight.number, 1}, sum, to);
         }
     }
 }

@@ -28,7 +28,7 @@ __device__ __forceinline__ uint32_t key_of(float v) {
     if (v == 0.0f) return 0x80000000u;
     return u ^ ((uint32_t)((int32_t)u >> 31) | 0x80000000u);
 }
-constexpr uint32_t kInfinity = 0xff800000u;
+constexpr uint32_t kInfinity = 0xff800000u, kMinusInfinity = 0x007fffffu;
 __device__ __forceinline__ float value_of(uint32_t key) { return __uint_as_float(key ^ (key >> 31 ? 0x80000000u : 0xffffffffu)); }
 // All of a row's keys are different, and larger ones come first.
 __device__ __forceinline__ uint64_t place_of(uint32_t key, uint32_t token) { return (uint64_t)key << 32 | (uint32_t)~token; }
@@ -66,33 +66,76 @@ struct Lds {
     uint32_t bound;
 };
 
-template <int TYPE>
-__global__ void __launch_bounds__(kThreads) top_kernel(const TopArgs p) {
+// A row that a workgroup's registers hold, VECTORS times sixteen bytes to a thread, is read from memory once; VECTORS 0: any row, read twice.  Rows with a
+// NaN or an infinity are looked through again by their keys.
+template <int TYPE, int VECTORS>
+__global__ void __launch_bounds__(kThreads, VECTORS <= 8 ? 8 : 4) top_kernel(const TopArgs p) {
     typedef typename Element<TYPE>::type T;
+    constexpr uint32_t kPer = 16 / sizeof(T);
+    typedef Pack<T, kPer> Vector;
     __shared__ Lds lds;
     const uint32_t lane = tid_x() % kWave, wave = (uint32_t)__builtin_amdgcn_readfirstlane((int)(tid_x() / kWave));
     const uint64_t row_at = wg_x();
     const T *row = reinterpret_cast<const T *>(p.logits) + row_at * p.stride;
     const uint32_t top = p.top < p.vocab ? p.top : p.vocab;
 
-    uint32_t largest = 0;
-    Exponentials e = {-__builtin_inff(), 0.0f};
-    for_row<TYPE>(row, p.vocab, [&](float v, uint32_t) {
-        const uint32_t key = key_of(v);
-        largest = key > largest ? key : largest;
-        if (v > e.top) {
-            e.sum *= __expf(e.top - v);
-            e.top = v;
+    // Whole vectors, thread by thread, and an element of what is left for each of the first threads; -infinity beyond the row's end.
+    const uint32_t whole = p.vocab / kPer, left = p.vocab % kPer;
+    u32x4 held[VECTORS ? VECTORS : 1];
+    float most[VECTORS ? (VECTORS + 1) / 2 : 1];  // of each two vectors
+    const float last = tid_x() < left ? Element<TYPE>::wide(row[whole * kPer + tid_x()]) : -__builtin_inff();
+    Exponentials e = {last, last == -__builtin_inff() ? 0.0f : __expf(last - last)};
+    auto add = [&](const u32x4 &words) {
+        const Vector w = __builtin_bit_cast(Vector, words);
+        float largest = Element<TYPE>::wide(w.v[0]);
+#pragma unroll
+        for (uint32_t j = 1; j < kPer; ++j) largest = __builtin_fmaxf(largest, Element<TYPE>::wide(w.v[j]));
+        const float now = __builtin_fmaxf(e.top, largest), from = now == -__builtin_inff() ? 0.0f : now;
+        float sum = 0.0f;
+#pragma unroll
+        for (uint32_t j = 0; j < kPer; ++j) sum += __expf(Element<TYPE>::wide(w.v[j]) - from);
+        e.sum = __builtin_fmaf(e.sum, __expf(e.top - from), sum);
+        e.top = now;
+        return largest;
+    };
+    if constexpr (VECTORS > 0) {
+        const uint32_t none = sizeof(T) == 4 ? 0xff800000u : TYPE == CNR_FLOAT_BF16 ? 0xff80ff80u : 0xfc00fc00u;
+#pragma unroll
+        for (uint32_t i = 0; i < VECTORS; ++i) {
+            held[i] = u32x4{none, none, none, none};
+            if (i * kThreads + tid_x() < whole) held[i] = load16(row + (i * kThreads + tid_x()) * kPer);
         }
-        e.sum += v == -__builtin_inff() ? 0.0f : __expf(v - e.top);
-    });
-    lds.largest[tid_x()] = largest;
+#pragma unroll
+        for (uint32_t i = 0; i < VECTORS; ++i) {
+            const float largest = add(held[i]);
+            most[i / 2] = i % 2 ? __builtin_fmaxf(most[i / 2], largest) : largest;
+            // (the compiler would have the elements of many as floats at once, and keep them until they are looked at again)
+            asm volatile("" : "+v"(held[i]), "+v"(e.sum));
+            __builtin_amdgcn_sched_barrier(0);
+        }
+    } else {
+        for (uint32_t i = tid_x(); i < whole; i += kThreads) add(load16(row + i * kPer));
+    }
+    lds.largest[tid_x()] = key_of(e.top);
     if (tid_x() == 0) lds.n_found = 0;
 #pragma unroll
     for (int by = 1; by < kWave; by *= 2) e = join(e, Exponentials{__shfl_xor(e.top, by), __shfl_xor(e.sum, by)});
     if (lane == 0) lds.parts[wave] = e;
     __syncthreads();
-    if (wave == 0) {
+    e = lds.parts[0];
+    for (uint32_t w = 1; w < kWaves; ++w) e = join(e, lds.parts[w]);
+    // (a NaN, or the difference of two infinities, stays in the sum)
+    const bool odd = e.sum != e.sum;
+    if (odd) {
+        uint32_t largest = 0;
+        for_row<TYPE>(row, p.vocab, [&](float v, uint32_t) {
+            const uint32_t key = key_of(v);
+            largest = key > largest ? key : largest;
+        });
+        lds.largest[tid_x()] = largest;
+        __syncthreads();
+    }
+    if (wave == 0 && top) {
         // The largest bound that at least `top` of the threads' largest reach, to 16 bits.
         uint32_t own[kThreads / kWave], bound = 0;
 #pragma unroll
@@ -105,31 +148,45 @@ __global__ void __launch_bounds__(kThreads) top_kernel(const TopArgs p) {
         }
         if (lane == 0) lds.bound = bound;
     } else if (wave == 1 && p.lse) {
-        e = lds.parts[0];
-        for (uint32_t w = 1; w < kWaves; ++w) e = join(e, lds.parts[w]);
-        uint32_t most = 0;
-        for (uint32_t i = lane; i < kThreads; i += kWave) most = lds.largest[i] > most ? lds.largest[i] : most;
+        uint32_t largest = 0;
+        if (odd)
+            for (uint32_t i = lane; i < kThreads; i += kWave) largest = lds.largest[i] > largest ? lds.largest[i] : largest;
 #pragma unroll
         for (int by = 1; by < kWave; by *= 2) {
-            const uint32_t other = (uint32_t)__shfl_xor((int)most, by);
-            most = other > most ? other : most;
+            const uint32_t other = (uint32_t)__shfl_xor((int)largest, by);
+            largest = other > largest ? other : largest;
         }
-        if (lane == 0) p.lse[row_at] = most > kInfinity ? __builtin_nanf("") : most == kInfinity ? __builtin_inff() : e.top + __logf(e.sum);
+        if (lane == 0) p.lse[row_at] = !odd ? e.top + __logf(e.sum) : largest > kInfinity ? __builtin_nanf("") : __builtin_inff();
     }
-    __syncthreads();
     if (!p.tokens && !p.values) return;
-    uint64_t from = (uint64_t)lds.bound << 32;  // places from here on are collected
-    auto collect = [&]() {
-        for_row<TYPE>(row, p.vocab, [&](float v, uint32_t token) {
+    __syncthreads();
+    auto collect = [&](uint64_t from) {
+        auto take = [&](float v, uint32_t token) {
             const uint64_t place = place_of(key_of(v), token);
-            if (place >= from) {
+            if (place >= from && token < p.vocab) {
                 const uint32_t at = atomicAdd(&lds.n_found, 1u);
                 if (at < kRoom) lds.found[at] = place;
             }
-        });
+        };
+        if (VECTORS > 0 && !odd) {
+            const uint32_t key = (uint32_t)(from >> 32);
+            const float least = key <= kMinusInfinity ? -__builtin_inff() : value_of(key);
+#pragma unroll
+            for (uint32_t i = 0; i < VECTORS; ++i) {
+                if (!(most[i / 2] >= least)) continue;
+                u32x4 words = held[i];
+                asm volatile("" : "+v"(words));  // elements as floats here only
+                const Vector w = __builtin_bit_cast(Vector, words);
+#pragma unroll
+                for (uint32_t j = 0; j < kPer; ++j) take(Element<TYPE>::wide(w.v[j]), (i * kThreads + tid_x()) * kPer + j);
+            }
+            if (tid_x() < left) take(last, whole * kPer + tid_x());
+        } else {
+            for_row<TYPE>(row, p.vocab, take);
+        }
         __syncthreads();
     };
-    if (top) collect();
+    if (top) collect((uint64_t)lds.bound << 32);  // places from there on
     if (top && lds.n_found > kRoom) {
         // Eight bits of the place at a time: how many have each digit behind those that are settled; the digit that the top-th place has.
         uint64_t settled = 0;
@@ -157,8 +214,7 @@ __global__ void __launch_bounds__(kThreads) top_kernel(const TopArgs p) {
             __syncthreads();
             if (above + with <= kRoom) break;
         }
-        from = settled;
-        collect();
+        collect(settled);
     }
     const uint32_t found = top ? lds.n_found : 0;
     T *values = p.values ? reinterpret_cast<T *>(p.values) + row_at * p.top : nullptr;
@@ -166,6 +222,7 @@ __global__ void __launch_bounds__(kThreads) top_kernel(const TopArgs p) {
     for (uint32_t i = tid_x(); i < found; i += kThreads) {
         const uint64_t place = lds.found[i];
         uint32_t before = 0;
+#pragma unroll 8
         for (uint32_t j = 0; j < found; ++j) before += lds.found[j] > place ? 1u : 0u;
         if (before >= top) continue;
         const uint32_t token = ~(uint32_t)place;
@@ -176,6 +233,24 @@ __global__ void __launch_bounds__(kThreads) top_kernel(const TopArgs p) {
         if (tokens) tokens[i] = -1;
         if (values) values[i] = (T)(-__builtin_inff());
     }
+}
+
+template <int TYPE>
+void top_of(const TopArgs &a, hipStream_t s) {
+    const uint64_t vectors = cnr_ceil_div((uint64_t)a.vocab * sizeof(typename Element<TYPE>::type), 16 * kThreads);
+    const dim3 grid((unsigned)a.n), threads(kThreads);
+    if (vectors <= 1)
+        hipLaunchKernelGGL((top_kernel<TYPE, 1>), grid, threads, 0, s, a);
+    else if (vectors <= 2)
+        hipLaunchKernelGGL((top_kernel<TYPE, 2>), grid, threads, 0, s, a);
+    else if (vectors <= 4)
+        hipLaunchKernelGGL((top_kernel<TYPE, 4>), grid, threads, 0, s, a);
+    else if (vectors <= 8)
+        hipLaunchKernelGGL((top_kernel<TYPE, 8>), grid, threads, 0, s, a);
+    else if (vectors <= 16)
+        hipLaunchKernelGGL((top_kernel<TYPE, 16>), grid, threads, 0, s, a);
+    else
+        hipLaunchKernelGGL((top_kernel<TYPE, 0>), grid, threads, 0, s, a);
 }
 
 }  // namespace
@@ -195,11 +270,11 @@ cnr_status cnr_top_logits(cnr_ctx *ctx, const void *logits, uint64_t stride, cnr
     const TopArgs a = {logits, stride, (uint32_t)vocab, (uint32_t)top, n, tokens, values, lse};
     hipStream_t s = as_stream(stream);
     if (type == CNR_FLOAT_F32)
-        hipLaunchKernelGGL((top_kernel<CNR_FLOAT_F32>), dim3((unsigned)n), dim3(kThreads), 0, s, a);
+        top_of<CNR_FLOAT_F32>(a, s);
     else if (type == CNR_FLOAT_BF16)
-        hipLaunchKernelGGL((top_kernel<CNR_FLOAT_BF16>), dim3((unsigned)n), dim3(kThreads), 0, s, a);
+        top_of<CNR_FLOAT_BF16>(a, s);
     else
-        hipLaunchKernelGGL((top_kernel<CNR_FLOAT_F16>), dim3((unsigned)n), dim3(kThreads), 0, s, a);
+        top_of<CNR_FLOAT_F16>(a, s);
     return cnr_launch_status(ctx);
 }
 

@@ -97,80 +97,77 @@ __device__ __forceinline__ void barrier() {
     asm volatile("" ::: "memory");
 }
 
-// What a workgroup's outputs are to its epilogue.  A lane holds 4 MF consecutive columns from `column` on, of NF rows: value(acc, i, g) is that of column
-// column + i and row row(g).
-template <int MF, int NF, bool ACROSS, bool DOWN>
+// What a workgroup's outputs are to its epilogue.  A lane holds MF / 2 times eight columns side by side, 32 apart, of NF rows: value(acc, i, g) is that of
+// column column_of(i) and row row(g).  The four lanes of a row thus write 64 bytes of 16-bit outputs side by side at a time.
+template <int MF, int NF, bool DOWN>
 struct Place {
     uint32_t row0, column0;  // first output of the workgroup
     uint32_t lane_row;       // the lane's first row within the workgroup's
-    uint32_t column;         // of the lane
+    uint32_t column;         // the lane's first
     uint32_t split, tile_column;
     uint32_t wave_column;    // which of the WM parts of the workgroup's columns is the wave's
     uint8_t *lds;            // free, as large as the stages were
-    // (rows from an operand across k: chunks of four rows, each to four lanes; chunks of odd lanes change places by pairs, see Across)
-    __device__ __forceinline__ uint32_t row_within(uint32_t g) const { return lane_row + (DOWN ? (g ^ (tid_x() / 4 % 2)) * 4 : g); }
+    // (rows from an operand across k: chunks of odd lanes change places by pairs, see Across)
+    __device__ __forceinline__ uint32_t row_within(uint32_t g) const { return lane_row + g / 2 * 32 + (DOWN ? (g ^ tid_x() / 4) % 2 : g % 2) * 4; }
     __device__ __forceinline__ uint32_t row(uint32_t g) const { return row0 + row_within(g); }
-    static __device__ __forceinline__ float value(const f32x4 (&acc)[MF][NF], int i, int g) { return ACROSS ? acc[i / 4][g][i % 4] : acc[i % MF][g][i / MF]; }
+    __device__ __forceinline__ uint32_t column_of(uint32_t i) const { return column + i / 8 * 32 + i % 8; }
+    static __device__ __forceinline__ float value(const f32x4 (&acc)[MF][NF], int i, int g) { return acc[i / 4][g][i % 4]; }
 };
 
-// One operand's way from memory through LDS into fragments of 16 of its F * 16 * waves rows (T), a block of k at a time.
+// One operand's way from memory through LDS into fragments of 16 of its F * 16 * waves rows (T), a block of k at a time.  Lane r = lane % 16 of fragment f has
+// row 32 (f / 2) + 8 (r / 4) + 4 (f % 2) + r % 4 of the wave's section: the four sums of a lane of the product, and those of the next fragment, lie side
+// by side.
 //
-// Along k: fragment f of a wave holds rows F r + f of its part (r = lane % 16), so that a lane's outputs lie side by side.  LDS holds two rows of 128 bytes
-// to a line of 256, its sixteen pieces of 16 bytes permuted by r: sixteen lanes that read the same piece of their rows find it in sixteen different places,
-// all banks in use.  Memory is read straight into LDS, where a wave's 64 pieces lie in order, so the permutation is in which piece a lane asks for.
+// Along k: LDS holds two rows of 128 bytes to a line of 256, its sixteen pieces of 16 bytes permuted by r / 2: sixteen lanes that read the same piece of
+// their rows find it in sixteen different places, all banks in use.  Memory is read straight into LDS, where a wave's 64 pieces lie in
+// order, so the permutation is in which piece a lane asks for.
 template <int F, int T, int LOADS>
 struct Along {
-    static constexpr int kLoads = LOADS;
     i32x4 buffer;
     uint32_t from[LOADS];
-    uint32_t piece[2][2];  // [odd][h]
+    uint32_t piece[2];  // of the first fragment's row, by half of the block
     // Rows beyond the matrix read its last one again.
     __device__ __forceinline__ Along(const Operand &o, uint32_t first, uint32_t count, uint32_t, uint32_t wave, uint32_t section, uint32_t region) {
         const uint32_t lane = tid_x() % kWave, r = lane % 16, quarter = lane / 16, rows = count - first < T ? count - first : T;
         buffer = buffer_of(reinterpret_cast<uint64_t>(o.at) + (uint64_t)first * o.stride, (uint64_t)(rows - 1) * o.stride + o.row_bytes);
 #pragma unroll
         for (int j = 0; j < LOADS; ++j) {
-            const uint32_t line = (wave * LOADS + j) * 4 + quarter, logical = r ^ (2 * line / F % 16);
+            const uint32_t line = (wave * LOADS + j) * 4 + quarter, logical = r ^ (line / 4 % 4 * 2 + line % 2);
             const uint32_t row = 2 * line + logical / 8;
             from[j] = (row < rows ? row : rows - 1) * (uint32_t)o.stride + logical % 8 * 16;
         }
 #pragma unroll
-        for (int i = 0; i < 4; ++i) piece[i / 2][i % 2] = region + (section + r * F) * kBlockBytes + (((quarter + 4 * (i % 2)) ^ r) * 16 ^ i / 2 * 128);
+        for (uint32_t h = 0; h < 2; ++h) piece[h] = region + section * kBlockBytes + (r / 4 * 4 + r % 4 / 2) * 256 + ((r % 2 * 8 + quarter + 4 * h) ^ r / 2) * 16;
     }
     template <int J>
     __device__ __forceinline__ void fetch(const Operand &, uint32_t lds, uint32_t part, uint32_t block) const {
         load_to_lds(buffer, lds, from[J], part + block * kBlockBytes);
     }
     __device__ __forceinline__ void move(uint32_t by) {
-#pragma unroll
-        for (int i = 0; i < 4; ++i) piece[i / 2][i % 2] += by;
+        piece[0] += by;
+        piece[1] += by;
     }
     __device__ __forceinline__ i32x8 fragment(const uint8_t *lds, uint32_t f) const {
         i32x4 part[2];
 #pragma unroll
-        for (int h = 0; h < 2; ++h) part[h] = *reinterpret_cast<const i32x4 *>(lds + piece[f % 2][h] + f / 2 * 256);
+        for (int h = 0; h < 2; ++h) part[h] = *reinterpret_cast<const i32x4 *>(lds + piece[h] + f / 2 * 4096 + f % 2 * 512);
         return __builtin_shufflevector(part[0], part[1], 0, 1, 2, 3, 4, 5, 6, 7);
     }
 };
 
 // Across k: LDS holds 64 rows of k with T columns each.  The transposing load gives a lane four rows of one column, sixteen lanes four rows of sixteen columns
-// that are four chunks of four from anywhere: chunk c of fragment f holds columns 4 F c + 4 (f ^ c % 2), so that the lanes of a chunk have 4 F columns
-// side by side between them.  Sixteen lanes thus read four chunks of 8 bytes in each of four rows; that these sixteen lie in different banks takes the other half of a piece
-// of 16 bytes for odd chunks, and pieces permuted by the row (`turned`), on the way in as in the layout along k.
+// that are four chunks of four from anywhere: chunk c = r / 4 of fragment f holds columns 32 (f / 2) + 8 c + 4 (f % 2 ^ c % 2).  Sixteen lanes thus read four
+// chunks of 8 bytes in each of four rows; that these sixteen lie in different banks takes the other half of a piece of 16 bytes for odd chunks, and pieces
+// permuted by the row (`turned`), on the way in as in the layout along k.
 template <int F, int T, int LOADS>
 struct Across {
-    static constexpr int kLoads = LOADS;
     static constexpr uint32_t kRow = T * 2, kPieces = T / 8;
     uint64_t at, left;  // of the first row's first column in bytes, to the end
     uint32_t from[LOADS];
     uint32_t chunk;
-    static __device__ __forceinline__ uint32_t turned(uint32_t piece, uint32_t row) {
-        if constexpr (F == 8) return piece ^ 2 * (row % 4) ^ piece / 8 % 2;
-        if constexpr (F == 4) return piece ^ row % 4;
-        return piece ^ row % 2 ^ row / 2 % 2 * 4;
-    }
+    static __device__ __forceinline__ uint32_t turned(uint32_t piece, uint32_t row) { return piece ^ row % 2 ^ row / 2 % 2 * 4; }
     __device__ __forceinline__ Across(const Operand &o, uint32_t first, uint32_t, uint32_t k, uint32_t wave, uint32_t section, uint32_t region) {
-        static_assert(F == 8 || F == 4 || F == 2, "places in LDS");
+        static_assert(T >= 64, "places in LDS");
         const uint32_t lane = tid_x() % kWave, quarter = lane / 16, c = lane % 4, row = lane % 16 / 4;
         at = reinterpret_cast<uint64_t>(o.at) + first * 2;
         left = (uint64_t)(k - 1) * o.stride + o.row_bytes - first * 2;
@@ -179,7 +176,7 @@ struct Across {
             const uint32_t i = (wave * LOADS + j) * kWave + lane;
             from[j] = i / kPieces * (uint32_t)o.stride + turned(i % kPieces, i / kPieces) * 16;
         }
-        chunk = region + (quarter * 8 + row) * kRow + turned((section + 4 * F * c) / 8, row) * 16 + c % 2 * 8;
+        chunk = region + (quarter * 8 + row) * kRow + turned(section / 8 + c, row) * 16 + c % 2 * 8;
     }
     // Beyond the end nothing is read, and zeros arrive.
     template <int J>
@@ -191,7 +188,7 @@ struct Across {
     __device__ __forceinline__ i32x8 fragment(const uint8_t *lds, uint32_t f) const {
         typedef __attribute__((address_space(3))) s16x4 *Lds;
         i32x2 part[4];
-        const uint8_t *from = lds + (chunk ^ f * 8);
+        const uint8_t *from = lds + (chunk ^ (f / 2 * 64 + f % 2 * 8));  // (these bits of the section's place are 0)
 #pragma unroll
         for (int h = 0; h < 4; ++h) part[h] = __builtin_bit_cast(i32x2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((Lds)(from + (h / 2 * 32 + h % 2 * 4) * kRow)));
         const i32x4 lo = __builtin_shufflevector(part[0], part[1], 0, 1, 2, 3), hi = __builtin_shufflevector(part[2], part[3], 0, 1, 2, 3);
@@ -327,11 +324,11 @@ __global__ void __launch_bounds__(WM * WN * kWave, 2) tile_kernel(const Args p, 
                     acc[f + 1][g][i] = quarter % 2 ? v : w;
                 }
     }
-    Place<MF, NF, ACROSS, DOWN> place;
+    Place<MF, NF, DOWN> place;
     place.row0 = row0;
     place.column0 = column0;
-    place.lane_row = wave_n + (DOWN ? r / 4 * 4 * NF + r % 4 : r * NF);
-    place.column = column0 + wave_m + quarter * 4 * MF;
+    place.lane_row = wave_n + r / 4 * 8 + r % 4;
+    place.column = column0 + wave_m + quarter * 8;
     place.split = split;
     place.tile_column = tile_column;
     place.wave_column = wave / WN;

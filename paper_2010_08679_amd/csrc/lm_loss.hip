@@ -91,18 +91,17 @@ struct KeepStats {
     template <uint32_t TM, uint32_t TN, int WM, bool WHOLE, typename Place, int MF, int NF>
     __device__ __forceinline__ void reduce(const dense::Args &p, const Place &at, const f32x4 (&acc)[MF][NF]) const {
         Stats *lds = reinterpret_cast<Stats *>(at.lds);  // [WM][TN]
-        const uint32_t left = at.column < p.columns ? p.columns - at.column : 0;
 #pragma unroll
         for (int g = 0; g < NF; ++g) {
             float top = -__builtin_inff();
 #pragma unroll
-            for (uint32_t i = 0; i < 4 * MF; ++i) top = __builtin_fmaxf(top, WHOLE || i < left ? at.value(acc, i, g) : -__builtin_inff());
+            for (uint32_t i = 0; i < 4 * MF; ++i) top = __builtin_fmaxf(top, WHOLE || at.column_of(i) < p.columns ? at.value(acc, i, g) : -__builtin_inff());
             top = __builtin_fmaxf(top, __shfl_xor(top, 16));
             top = __builtin_fmaxf(top, __shfl_xor(top, 32)) * c;
             const float from = top == -__builtin_inff() ? 0.0f : top;
             float sum = 0.0f;
 #pragma unroll
-            for (uint32_t i = 0; i < 4 * MF; ++i) sum += WHOLE || i < left ? exp2_of(__builtin_fmaf(at.value(acc, i, g), c, -from)) : 0.0f;
+            for (uint32_t i = 0; i < 4 * MF; ++i) sum += WHOLE || at.column_of(i) < p.columns ? exp2_of(__builtin_fmaf(at.value(acc, i, g), c, -from)) : 0.0f;
             sum += __shfl_xor(sum, 16);
             sum += __shfl_xor(sum, 32);
             if (tid_x() % kWave < 16) lds[at.wave_column * TN + at.row_within(g)] = {top, sum};
@@ -150,19 +149,20 @@ struct KeepGradient {
     __device__ __forceinline__ void write(const dense::Args &p, const Place &at, const f32x4 (&acc)[MF][NF], int g, const RowGradient &r, uint32_t target, T *to) const {
 #pragma unroll
         for (int from = 0; from < 4 * MF; from += 8) {
-            if (at.column + from >= width) continue;
+            const uint32_t column = at.column_of(from);
+            if (column >= width) continue;
             Pack<T, 8> w[PARTS];
 #pragma unroll
             for (int j = 0; j < 8; ++j) {
                 float v = exp2_of(__builtin_fmaf(at.value(acc, from + j, g), c, -r.lse2));
                 if (TARGET && target == (uint32_t)(from + j)) v -= 1.0f;
                 T part[PARTS];
-                apart<TYPE, PARTS>(r.gradient == 0.0f || at.column + from + j >= p.columns ? 0.0f : r.gradient * v, part);
+                apart<TYPE, PARTS>(r.gradient == 0.0f || column + j >= p.columns ? 0.0f : r.gradient * v, part);
 #pragma unroll
                 for (int i = 0; i < PARTS; ++i) w[i].v[j] = part[i];
             }
 #pragma unroll
-            for (int i = 0; i < PARTS; ++i) *reinterpret_cast<Pack<T, 8> *>(to + i * width + from) = w[i];
+            for (int i = 0; i < PARTS; ++i) *reinterpret_cast<Pack<T, 8> *>(to + i * width + column) = w[i];
         }
     }
     template <uint32_t TM, uint32_t TN, int WM, typename Place, int MF, int NF>
@@ -172,9 +172,9 @@ struct KeepGradient {
             const uint32_t row = at.row(g);
             const RowGradient r = rows[row];
             if (row >= p.rows) continue;
-            T *to = dz + row * stride + at.column;
-            const uint32_t target = r.target - first - at.column;  // among the lane's columns, or large
-            if (__any(target < 4 * MF))
+            T *to = dz + row * stride;
+            const uint32_t from = r.target - first - at.column, target = from < 16 * MF && from % 32 < 8 ? from / 32 * 8 + from % 8 : kNoTarget;  // which of the lane's
+            if (__any(target != kNoTarget))
                 write<MF, NF, true>(p, at, acc, g, r, target, to);
             else
                 write<MF, NF, false>(p, at, acc, g, r, target, to);
@@ -252,7 +252,7 @@ struct KeepSum {
 #pragma unroll
         for (int g = 0; g < NF; ++g) {
             const uint32_t row = at.row(g);
-            if (row >= p.rows || at.column >= p.columns) continue;
+            if (row >= p.rows) continue;
             if (p.splits > 1) {
                 float *to = partial + ((uint64_t)at.split * p.rows + row) * partial_stride;
 #pragma unroll
@@ -260,7 +260,7 @@ struct KeepSum {
                     float v[4];
 #pragma unroll
                     for (int j = 0; j < 4; ++j) v[j] = at.value(acc, first + j, g);
-                    write_as(to + at.column + first, at.column + first, p.columns, v);
+                    write_as(to + at.column_of(first), at.column_of(first), p.columns, v);
                 }
                 continue;
             }
@@ -270,13 +270,13 @@ struct KeepSum {
             for (int u = 0; u < 4 * MF / 8; ++u) {
 #pragma unroll
                 for (int j = 0; j < 8; ++j) old[u][j] = 0.0f;
-                if (there.out) read_row(there, row, at.column + 8 * u, p.columns, old[u]);
+                if (there.out) read_row(there, row, at.column_of(8 * u), p.columns, old[u]);
             }
 #pragma unroll
             for (int u = 0; u < 4 * MF / 8; ++u) {
 #pragma unroll
                 for (int j = 0; j < 8; ++j) old[u][j] = __builtin_fmaf(at.value(acc, 8 * u + j, g), by, old[u][j]);
-                write_row(out, row, at.column + 8 * u, p.columns, old[u]);
+                write_row(out, row, at.column_of(8 * u), p.columns, old[u]);
             }
         }
     }
@@ -315,17 +315,28 @@ __device__ __forceinline__ __bf16 float_part(float v, int part) {
     }
     return __builtin_bit_cast(__bf16, (unsigned short)(bits >> 16));
 }
-// dst[rows][parts][whole blocks] = src, zeros behind it; rows that add nothing are zeros.  16 bytes of each part to a thread.
+// dst[rows][parts][whole blocks] = src, zeros behind it; rows that add nothing to a gradient are zeros.
+struct Layout {
+    const void *src;
+    uint64_t stride;
+    uint64_t rows;
+    const float *lse2, *dloss;  // NULL: every row counts
+    u32x4 *dst;
+};
+// Two matrices (either may have no rows), 16 bytes of each part to a thread.
 template <typename T>
-__global__ void __launch_bounds__(kBlock) lay_out_kernel(const T *src, uint64_t stride, uint32_t rows, uint32_t dim, const RowGradient *keep, u32x4 *dst,
-                                                         uint32_t pieces /* of a part */) {
+__global__ void __launch_bounds__(kBlock) lay_out_kernel(const Layout a, const Layout b, uint32_t dim, uint32_t pieces /* of a part */) {
     constexpr int kParts = sizeof(T) == 4 ? 3 : 1;
-    const uint64_t at = (uint64_t)wg_x() * kBlock + tid_x();
-    if (at >= (uint64_t)rows * pieces) return;
-    const uint32_t row = (uint32_t)(at / pieces), piece = (uint32_t)(at % pieces), column = piece * 8;
-    const T *from = src + (uint64_t)row * stride + column;
+    uint64_t at = (uint64_t)wg_x() * kBlock + tid_x();
+    const bool second = at >= a.rows * pieces;
+    const Layout &m = second ? b : a;
+    at -= second ? a.rows * pieces : 0;
+    if (at >= m.rows * pieces) return;
+    const uint64_t row = at / pieces;
+    const uint32_t piece = (uint32_t)(at % pieces), column = piece * 8;
+    const T *from = reinterpret_cast<const T *>(m.src) + row * m.stride + column;
     Pack<T, 8> w;
-    if (keep && keep[row].gradient == 0.0f) {
+    if (m.lse2 && (m.lse2[row] == __builtin_inff() || m.dloss[row] == 0.0f)) {
 #pragma unroll
         for (uint32_t j = 0; j < 8; ++j) w.v[j] = (T)0.0f;
     } else if (column + 8 <= dim) {
@@ -334,7 +345,7 @@ __global__ void __launch_bounds__(kBlock) lay_out_kernel(const T *src, uint64_t 
 #pragma unroll
         for (uint32_t j = 0; j < 8; ++j) w.v[j] = column + j < dim ? from[j] : (T)0.0f;
     }
-    u32x4 *to = dst + (uint64_t)row * pieces * kParts + piece;
+    u32x4 *to = m.dst + row * pieces * kParts + piece;
     if constexpr (kParts == 1) {
         *to = __builtin_bit_cast(u32x4, w);
     } else {
@@ -827,15 +838,18 @@ uint64_t room_for(const Sizes &s, bool training, bool two) {
     return b.used > f.used ? b.used : f.used;
 }
 
-// Rows as a product can read them along k: where they are, or laid out in `space`.
-template <typename T>
-dense::Operand laid_out(const T *src, uint64_t stride, uint64_t rows, const Sizes &s, const RowGradient *keep, void *space, hipStream_t to) {
+// Rows as a product can read them: where they are, or, where `layout` has rows, laid out in `space` by lay_out.
+dense::Operand operand_of(const Sizes &s, const void *src, uint64_t stride, uint64_t rows, bool in_place, void *space, Layout &layout) {
     const uint32_t part = s.blocks * dense::kBlockBytes;
-    if (!keep && whole_rows(s.type, src, stride, s.dim, rows)) return {src, stride * sizeof(T), part, 0, 0};
-    const uint32_t pieces = part / 16;
-    hipLaunchKernelGGL((lay_out_kernel<T>), dim3((unsigned)cnr_ceil_div(rows * pieces, kBlock)), dim3(kBlock), 0, to, src, stride, (uint32_t)rows, (uint32_t)s.dim, keep,
-                       (u32x4 *)space, pieces);
+    layout = {src, stride, in_place ? 0 : rows, nullptr, nullptr, reinterpret_cast<u32x4 *>(space)};
+    if (in_place) return {src, stride * 2, part, 0, 0};
     return {space, s.row, (uint32_t)s.row, part, 0};
+}
+template <typename T>
+void lay_out(const Sizes &s, const Layout &a, const Layout &b, hipStream_t to) {
+    const uint32_t pieces = s.blocks * dense::kBlockBytes / 16;
+    const uint64_t groups = cnr_ceil_div((a.rows + b.rows) * pieces, kBlock);
+    if (groups) hipLaunchKernelGGL((lay_out_kernel<T>), dim3((unsigned)groups), dim3(kBlock), 0, to, a, b, (uint32_t)s.dim, pieces);
 }
 dense::Operand in_terms(dense::Operand o, uint32_t parts) {
     o.parts = parts;
@@ -896,13 +910,16 @@ void forward(cnr_ctx *ctx, const cnr_vocabulary &v, const cnr_targets &t, float 
                 hipLaunchKernelGGL((narrow_kernel<TYPE, 1, 4>), grid, dim3(kBlock), 0, to, a);
         } else {
             const Terms terms = s.parts == 3 ? kOfFloats : kOne;
-            const dense::Operand x_at = in_terms(laid_out(x, v.hidden_stride, rows, s, nullptr, space + f.hidden, to), terms.down);
+            Layout of_x, of_w;
+            const dense::Operand x_at = in_terms(operand_of(s, x, v.hidden_stride, rows, whole_rows(v.type, x, v.hidden_stride, v.dim, rows), space + f.hidden, of_x), terms.down);
             const uint32_t columns = dense::kTiles[f.tiles.kind].columns;
             const bool in_place = whole_rows(v.type, weight, v.weight_stride, v.dim, v.vocab);
             const uint64_t most = in_place ? rounded((1ull << 22) / cnr_ceil_div(rows, 64) * 64, 256) : f.piece;
             for (uint64_t v0 = 0; v0 < v.vocab; v0 += most) {
                 const uint64_t width = v.vocab - v0 < most ? v.vocab - v0 : most;
-                const dense::Operand w_at = in_terms(laid_out(weight + v0 * v.weight_stride, v.weight_stride, width, s, nullptr, space + f.weight, to), terms.across);
+                const dense::Operand w_at = in_terms(operand_of(s, weight + v0 * v.weight_stride, v.weight_stride, width, in_place, space + f.weight, of_w), terms.across);
+                lay_out<T>(s, of_w, of_x, to);
+                of_x.rows = 0;
                 const dense::Args args = {w_at, x_at, (uint32_t)width, (uint32_t)rows, s.blocks, 0, terms.number, 1};
                 dense::launch<kOf<TYPE>, false, false>(args, f.tiles.kind, KeepStats{parts + v0 / columns, f.n_parts, c}, to);
             }
@@ -959,7 +976,11 @@ void backward(cnr_ctx *ctx, const cnr_vocabulary &v, const cnr_targets &t, const
     float *scale = reinterpret_cast<float *>(space + b.scale);
     hipLaunchKernelGGL(rows_kernel, dim3((unsigned)least(cnr_ceil_div(v.n, kRowThreads), kRowGroups)), dim3(kRowThreads), 0, to, state, dloss, v.n, targets, v.vocab, TYPE == CNR_FLOAT_F16,
                        rows, scale);
-    const dense::Operand x = laid_out(reinterpret_cast<const T *>(v.hidden), v.hidden_stride, v.n, s, rows, space + b.hidden_at, to);
+    const bool in_place = whole_rows(v.type, v.weight, v.weight_stride, v.dim, v.vocab);
+    Layout of_x, of_w;
+    const dense::Operand x = operand_of(s, v.hidden, v.hidden_stride, v.n, false, space + b.hidden_at, of_x);
+    of_x.lse2 = state;
+    of_x.dloss = dloss;
     KeepGradient<kOf<TYPE>, PARTS> k;
     k.dz = reinterpret_cast<Part *>(space + b.dz);
     k.rows = rows;
@@ -976,7 +997,9 @@ void backward(cnr_ctx *ctx, const cnr_vocabulary &v, const cnr_targets &t, const
         k.width = (uint64_t)blocks * dense::kBlockElements;
         k.stride = PARTS * k.width;
         k.first = (uint32_t)v0;
-        const dense::Operand w = laid_out(weight + v0 * v.weight_stride, v.weight_stride, width, s, nullptr, space + b.weight_at, to);
+        const dense::Operand w = operand_of(s, weight + v0 * v.weight_stride, v.weight_stride, width, in_place, space + b.weight_at, of_w);
+        lay_out<T>(s, of_w, of_x, to);
+        of_x.rows = 0;
         const dense::Plan tiles = dense::plan_of(ctx, width, v.n, s.blocks * logits.number, 2.0f * PARTS, 0);
         dense::launch<kOf<TYPE>, false, false>(dense::Args{in_terms(w, logits.across), in_terms(x, logits.down), width, n, s.blocks, 0, logits.number, 1}, tiles.kind, k, to);
         if (t.logits)

@@ -9,7 +9,6 @@
 
 namespace {
 
-constexpr uint32_t kThreads = 1024, kWaves = kThreads / kWave, kRoom = 4096;
 
 struct TopArgs {
     const void *logits;
@@ -36,17 +35,32 @@ __device__ __forceinline__ uint64_t place_of(uint32_t key, uint32_t token) { ret
 struct Exponentials {
     float top, sum;
 };
-__device__ __forceinline__ Exponentials join(const Exponentials &a, const Exponentials &b) {
-    const float top = __builtin_fmaxf(a.top, b.top), at = top == -__builtin_inff() ? 0.0f : top;
-    return {top, a.sum * __expf(a.top - at) + b.sum * __expf(b.top - at)};
+// The same of a wave's, in all lanes.
+__device__ __forceinline__ float max_of(float v, float w) { return __builtin_fmaxf(v, w); }
+__device__ __forceinline__ Exponentials over_wave(Exponentials e) {
+    float top = e.top;
+    top = max_of(top, dpp_f<0xB1>(top));
+    top = max_of(top, dpp_f<0x4E>(top));
+    top = max_of(top, dpp_f<0x141>(top));
+    top = max_of(top, dpp_f<0x140>(top));
+    top = max_of(top, __shfl_xor(top, 16));
+    top = max_of(top, __shfl_xor(top, 32));
+    float sum = e.sum * __expf(e.top - (top == -__builtin_inff() ? 0.0f : top));
+    sum += dpp_f<0xB1>(sum);
+    sum += dpp_f<0x4E>(sum);
+    sum += dpp_f<0x141>(sum);
+    sum += dpp_f<0x140>(sum);
+    sum += __shfl_xor(sum, 16);
+    sum += __shfl_xor(sum, 32);
+    return {top, sum};
 }
 
 // each(element's value, token) for all of a row's elements, sixteen bytes to a thread at a time.
-template <int TYPE, typename Each>
+template <int TYPE, uint32_t THREADS, typename Each>
 __device__ __forceinline__ void for_row(const typename Element<TYPE>::type *row, uint32_t vocab, const Each &each) {
     typedef typename Element<TYPE>::type T;
     constexpr uint32_t kPer = 16 / sizeof(T);
-    for (uint32_t at = tid_x() * kPer; at < vocab; at += kThreads * kPer) {
+    for (uint32_t at = tid_x() * kPer; at < vocab; at += THREADS * kPer) {
         if (at + kPer <= vocab) {
             const Pack<T, kPer> w = *reinterpret_cast<const Pack<T, kPer> *>(row + at);
 #pragma unroll
@@ -57,23 +71,26 @@ __device__ __forceinline__ void for_row(const typename Element<TYPE>::type *row,
     }
 }
 
+template <uint32_t THREADS>
 struct Lds {
+    static constexpr uint32_t kRoom = 4 * THREADS;
     uint64_t found[kRoom];
-    uint32_t largest[kThreads];
+    uint32_t largest[THREADS];
     uint32_t bins[256];
-    Exponentials parts[kWaves];
+    Exponentials parts[THREADS / kWave];
     uint32_t n_found, digit, above;
     uint32_t bound;
 };
 
 // A row that a workgroup's registers hold, VECTORS times sixteen bytes to a thread, is read from memory once; VECTORS 0: any row, read twice.  Rows with a
 // NaN or an infinity are looked through again by their keys.
-template <int TYPE, int VECTORS>
-__global__ void __launch_bounds__(kThreads, VECTORS <= 8 ? 8 : 4) top_kernel(const TopArgs p) {
+template <int TYPE, uint32_t THREADS, int VECTORS>
+__global__ void __launch_bounds__(THREADS, VECTORS <= 8 ? 8 : 4) top_kernel(const TopArgs p) {
     typedef typename Element<TYPE>::type T;
     constexpr uint32_t kPer = 16 / sizeof(T);
     typedef Pack<T, kPer> Vector;
-    __shared__ Lds lds;
+    constexpr uint32_t kWaves = THREADS / kWave, kRoom = Lds<THREADS>::kRoom;
+    __shared__ Lds<THREADS> lds;
     const uint32_t lane = tid_x() % kWave, wave = (uint32_t)__builtin_amdgcn_readfirstlane((int)(tid_x() / kWave));
     const uint64_t row_at = wg_x();
     const T *row = reinterpret_cast<const T *>(p.logits) + row_at * p.stride;
@@ -103,7 +120,7 @@ __global__ void __launch_bounds__(kThreads, VECTORS <= 8 ? 8 : 4) top_kernel(con
 #pragma unroll
         for (uint32_t i = 0; i < VECTORS; ++i) {
             held[i] = u32x4{none, none, none, none};
-            if (i * kThreads + tid_x() < whole) held[i] = load16(row + (i * kThreads + tid_x()) * kPer);
+            if (i * THREADS + tid_x() < whole) held[i] = load16(row + (i * THREADS + tid_x()) * kPer);
         }
 #pragma unroll
         for (uint32_t i = 0; i < VECTORS; ++i) {
@@ -114,21 +131,23 @@ __global__ void __launch_bounds__(kThreads, VECTORS <= 8 ? 8 : 4) top_kernel(con
             __builtin_amdgcn_sched_barrier(0);
         }
     } else {
-        for (uint32_t i = tid_x(); i < whole; i += kThreads) add(load16(row + i * kPer));
+        for (uint32_t i = tid_x(); i < whole; i += THREADS) add(load16(row + i * kPer));
     }
     lds.largest[tid_x()] = key_of(e.top);
     if (tid_x() == 0) lds.n_found = 0;
-#pragma unroll
-    for (int by = 1; by < kWave; by *= 2) e = join(e, Exponentials{__shfl_xor(e.top, by), __shfl_xor(e.sum, by)});
+    e = over_wave(e);
     if (lane == 0) lds.parts[wave] = e;
     __syncthreads();
-    e = lds.parts[0];
-    for (uint32_t w = 1; w < kWaves; ++w) e = join(e, lds.parts[w]);
+    e = {lds.parts[0].top, 0.0f};
+#pragma unroll
+    for (uint32_t w = 1; w < kWaves; ++w) e.top = __builtin_fmaxf(e.top, lds.parts[w].top);
+#pragma unroll
+    for (uint32_t w = 0; w < kWaves; ++w) e.sum = __builtin_fmaf(lds.parts[w].sum, __expf(lds.parts[w].top - (e.top == -__builtin_inff() ? 0.0f : e.top)), e.sum);
     // (a NaN, or the difference of two infinities, stays in the sum)
     const bool odd = e.sum != e.sum;
     if (odd) {
         uint32_t largest = 0;
-        for_row<TYPE>(row, p.vocab, [&](float v, uint32_t) {
+        for_row<TYPE, THREADS>(row, p.vocab, [&](float v, uint32_t) {
             const uint32_t key = key_of(v);
             largest = key > largest ? key : largest;
         });
@@ -137,20 +156,20 @@ __global__ void __launch_bounds__(kThreads, VECTORS <= 8 ? 8 : 4) top_kernel(con
     }
     if (wave == 0 && top) {
         // The largest bound that at least `top` of the threads' largest reach, to 16 bits.
-        uint32_t own[kThreads / kWave], bound = 0;
+        uint32_t own[THREADS / kWave], bound = 0;
 #pragma unroll
-        for (uint32_t i = 0; i < kThreads / kWave; ++i) own[i] = lds.largest[i * kWave + lane];
+        for (uint32_t i = 0; i < THREADS / kWave; ++i) own[i] = lds.largest[i * kWave + lane];
         for (uint32_t bit = 0x80000000u; bit >= 0x10000u; bit >>= 1) {
             uint32_t reach = 0;
 #pragma unroll
-            for (uint32_t i = 0; i < kThreads / kWave; ++i) reach += (uint32_t)__popcll(__ballot(own[i] >= (bound | bit)));
+            for (uint32_t i = 0; i < THREADS / kWave; ++i) reach += (uint32_t)__popcll(__ballot(own[i] >= (bound | bit)));
             if (reach >= top) bound |= bit;
         }
         if (lane == 0) lds.bound = bound;
     } else if (wave == 1 && p.lse) {
         uint32_t largest = 0;
         if (odd)
-            for (uint32_t i = lane; i < kThreads; i += kWave) largest = lds.largest[i] > largest ? lds.largest[i] : largest;
+            for (uint32_t i = lane; i < THREADS; i += kWave) largest = lds.largest[i] > largest ? lds.largest[i] : largest;
 #pragma unroll
         for (int by = 1; by < kWave; by *= 2) {
             const uint32_t other = (uint32_t)__shfl_xor((int)largest, by);
@@ -178,11 +197,11 @@ __global__ void __launch_bounds__(kThreads, VECTORS <= 8 ? 8 : 4) top_kernel(con
                 asm volatile("" : "+v"(words));  // elements as floats here only
                 const Vector w = __builtin_bit_cast(Vector, words);
 #pragma unroll
-                for (uint32_t j = 0; j < kPer; ++j) take(Element<TYPE>::wide(w.v[j]), (i * kThreads + tid_x()) * kPer + j);
+                for (uint32_t j = 0; j < kPer; ++j) take(Element<TYPE>::wide(w.v[j]), (i * THREADS + tid_x()) * kPer + j);
             }
             if (tid_x() < left) take(last, whole * kPer + tid_x());
         } else {
-            for_row<TYPE>(row, p.vocab, take);
+            for_row<TYPE, THREADS>(row, p.vocab, take);
         }
         __syncthreads();
     };
@@ -192,9 +211,9 @@ __global__ void __launch_bounds__(kThreads, VECTORS <= 8 ? 8 : 4) top_kernel(con
         uint64_t settled = 0;
         uint32_t above = 0;  // places that are larger than any with these digits
         for (int shift = 56; shift >= 0; shift -= 8) {
-            for (uint32_t i = tid_x(); i < 256; i += kThreads) lds.bins[i] = 0;
+            for (uint32_t i = tid_x(); i < 256; i += THREADS) lds.bins[i] = 0;
             __syncthreads();
-            for_row<TYPE>(row, p.vocab, [&](float v, uint32_t token) {
+            for_row<TYPE, THREADS>(row, p.vocab, [&](float v, uint32_t token) {
                 const uint64_t place = place_of(key_of(v), token);
                 if (shift == 56 || place >> (shift + 8) == settled >> (shift + 8)) atomicAdd(&lds.bins[place >> shift & 255u], 1u);
             });
@@ -219,7 +238,7 @@ __global__ void __launch_bounds__(kThreads, VECTORS <= 8 ? 8 : 4) top_kernel(con
     const uint32_t found = top ? lds.n_found : 0;
     T *values = p.values ? reinterpret_cast<T *>(p.values) + row_at * p.top : nullptr;
     int32_t *tokens = p.tokens ? p.tokens + row_at * p.top : nullptr;
-    for (uint32_t i = tid_x(); i < found; i += kThreads) {
+    for (uint32_t i = tid_x(); i < found; i += THREADS) {
         const uint64_t place = lds.found[i];
         uint32_t before = 0;
 #pragma unroll 8
@@ -227,30 +246,38 @@ __global__ void __launch_bounds__(kThreads, VECTORS <= 8 ? 8 : 4) top_kernel(con
         if (before >= top) continue;
         const uint32_t token = ~(uint32_t)place;
         if (tokens) tokens[before] = (int32_t)token;
-        if (values) values[before] = row[token];
+        if (values) values[before] = Element<TYPE>::narrow(value_of((uint32_t)(place >> 32)));  // exactly what it was
     }
-    for (uint32_t i = top + tid_x(); i < p.top; i += kThreads) {
+    for (uint32_t i = top + tid_x(); i < p.top; i += THREADS) {
         if (tokens) tokens[i] = -1;
         if (values) values[i] = (T)(-__builtin_inff());
     }
 }
 
-template <int TYPE>
-void top_of(const TopArgs &a, hipStream_t s) {
-    const uint64_t vectors = cnr_ceil_div((uint64_t)a.vocab * sizeof(typename Element<TYPE>::type), 16 * kThreads);
-    const dim3 grid((unsigned)a.n), threads(kThreads);
-    if (vectors <= 1)
-        hipLaunchKernelGGL((top_kernel<TYPE, 1>), grid, threads, 0, s, a);
-    else if (vectors <= 2)
-        hipLaunchKernelGGL((top_kernel<TYPE, 2>), grid, threads, 0, s, a);
-    else if (vectors <= 4)
-        hipLaunchKernelGGL((top_kernel<TYPE, 4>), grid, threads, 0, s, a);
+template <int TYPE, uint32_t THREADS>
+void launch(const TopArgs &a, uint64_t vectors, hipStream_t s) {
+    const dim3 grid((unsigned)a.n), threads(THREADS);
+    if (vectors <= 4)
+        hipLaunchKernelGGL((top_kernel<TYPE, THREADS, 4>), grid, threads, 0, s, a);
     else if (vectors <= 8)
-        hipLaunchKernelGGL((top_kernel<TYPE, 8>), grid, threads, 0, s, a);
+        hipLaunchKernelGGL((top_kernel<TYPE, THREADS, 8>), grid, threads, 0, s, a);
     else if (vectors <= 16)
-        hipLaunchKernelGGL((top_kernel<TYPE, 16>), grid, threads, 0, s, a);
+        hipLaunchKernelGGL((top_kernel<TYPE, THREADS, 16>), grid, threads, 0, s, a);
     else
-        hipLaunchKernelGGL((top_kernel<TYPE, 0>), grid, threads, 0, s, a);
+        hipLaunchKernelGGL((top_kernel<TYPE, THREADS, 0>), grid, threads, 0, s, a);
+}
+// The fewer threads hold a row, the more rows share a compute unit and hide each other's steps that have little to do; few rows want many threads.  A bound
+// is of use where clearly more threads than are asked for have elements.
+template <int TYPE>
+void top_of(const TopArgs &a, const cnr_ctx *ctx, hipStream_t s) {
+    const uint64_t vectors = (uint64_t)a.vocab * sizeof(typename Element<TYPE>::type) / 16;
+    const bool many = a.n > 2 * (uint64_t)ctx->n_cu;
+    if (many && vectors <= 16 * 256 && a.top <= 192)
+        launch<TYPE, 256>(a, cnr_ceil_div(vectors, 256), s);
+    else if (many && vectors <= 16 * 512 && a.top <= 384)
+        launch<TYPE, 512>(a, cnr_ceil_div(vectors, 512), s);
+    else
+        launch<TYPE, 1024>(a, cnr_ceil_div(vectors, 1024), s);
 }
 
 }  // namespace
@@ -260,7 +287,7 @@ extern "C" {
 cnr_status cnr_top_logits(cnr_ctx *ctx, const void *logits, uint64_t stride, cnr_float_type type, uint64_t n, uint64_t vocab, uint64_t top, int32_t *tokens, void *values,
                           float *lse, void *stream) {
     if (!ctx || !cnr_valid_float_type(type) || stride < vocab) return CNR_E_INVALID;
-    if (n > CNR_LM_MAX_SIZE || vocab > CNR_LM_MAX_SIZE || top > CNR_LOSS_MAX_TOP || n * kThreads >= 1ull << 32) return CNR_E_TOO_LARGE;
+    if (n > CNR_LM_MAX_SIZE || vocab > CNR_LM_MAX_SIZE || top > CNR_LOSS_MAX_TOP || n * 1024 >= 1ull << 32) return CNR_E_TOO_LARGE;
     if (n == 0 || ((top == 0 || (!tokens && !values)) && !lse)) return CNR_OK;
     if (vocab && !logits) return CNR_E_INVALID;
     const size_t element = cnr_float_bytes(type);
@@ -270,11 +297,11 @@ cnr_status cnr_top_logits(cnr_ctx *ctx, const void *logits, uint64_t stride, cnr
     const TopArgs a = {logits, stride, (uint32_t)vocab, (uint32_t)top, n, tokens, values, lse};
     hipStream_t s = as_stream(stream);
     if (type == CNR_FLOAT_F32)
-        top_of<CNR_FLOAT_F32>(a, s);
+        top_of<CNR_FLOAT_F32>(a, ctx, s);
     else if (type == CNR_FLOAT_BF16)
-        top_of<CNR_FLOAT_BF16>(a, s);
+        top_of<CNR_FLOAT_BF16>(a, ctx, s);
     else
-        top_of<CNR_FLOAT_F16>(a, s);
+        top_of<CNR_FLOAT_F16>(a, ctx, s);
     return cnr_launch_status(ctx);
 }
 

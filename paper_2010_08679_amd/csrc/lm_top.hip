@@ -1,9 +1,10 @@
 // The largest logits of each row with their tokens, and the logarithm of the sum of all exponentials.
 //
-// One workgroup a row.  The largest of each thread's own elements are found along with the sum of exponentials; the top-th largest of those is at most the
-// top-th largest of all, and hardly more elements reach it than are wanted.  These are collected in LDS, in any order, and each finds its place by counting
-// those before it: keys (the value, then the lower token) are all different, so the order they were collected in does not matter.  Where too many
-// reach it (equal values, or the largest all in one thread's share), the bound is raised digit by digit first.
+// One workgroup a row, which it reads once.  The sum of exponentials is taken along, and the largest of every sixteen bytes (of several such vectors, in long
+// rows) stays in a register.  The top-th largest of the threads' own largest is at most the top-th largest of all, and hardly more elements reach it than
+// are wanted: the vectors whose largest does are read again, all at once, and their elements that reach it are collected in LDS, in any order; each finds
+// its place by counting those before it.  Keys (the value, then the lower token) are all different, so the order they were collected in does not matter.
+// Where too many reach the bound (equal values, or the largest all in one thread's share), it is raised digit by digit first.
 #include "cnr_loss.h"
 #include "lm_common.h"
 
@@ -27,6 +28,7 @@ __device__ __forceinline__ uint32_t key_of(float v) {
     if (v == 0.0f) return 0x80000000u;
     return u ^ ((uint32_t)((int32_t)u >> 31) | 0x80000000u);
 }
+constexpr float kLog2e = 1.44269504088896340736f;
 constexpr uint32_t kInfinity = 0xff800000u, kMinusInfinity = 0x007fffffu;
 __device__ __forceinline__ float value_of(uint32_t key) { return __uint_as_float(key ^ (key >> 31 ? 0x80000000u : 0xffffffffu)); }
 // All of a row's keys are different, and larger ones come first.
@@ -75,17 +77,17 @@ template <uint32_t THREADS>
 struct Lds {
     static constexpr uint32_t kRoom = 4 * THREADS;
     uint64_t found[kRoom];
+    uint32_t hits[2 * THREADS];
     uint32_t largest[THREADS];
     uint32_t bins[256];
     Exponentials parts[THREADS / kWave];
-    uint32_t n_found, digit, above;
+    uint32_t n_found, n_hits, digit, above;
     uint32_t bound;
 };
 
-// A row that a workgroup's registers hold, VECTORS times sixteen bytes to a thread, is read from memory once; VECTORS 0: any row, read twice.  Rows with a
-// NaN or an infinity are looked through again by their keys.
-template <int TYPE, uint32_t THREADS, int VECTORS>
-__global__ void __launch_bounds__(THREADS, VECTORS <= 8 ? 8 : 4) top_kernel(const TopArgs p) {
+// GROUPS groups of vectors to a thread, of one vector each unless LONG.  Rows with a NaN or an infinity are looked through again by their keys.
+template <int TYPE, uint32_t THREADS, uint32_t GROUPS, bool LONG>
+__global__ void __launch_bounds__(THREADS) top_kernel(const TopArgs p) {
     typedef typename Element<TYPE>::type T;
     constexpr uint32_t kPer = 16 / sizeof(T);
     typedef Pack<T, kPer> Vector;
@@ -97,44 +99,56 @@ __global__ void __launch_bounds__(THREADS, VECTORS <= 8 ? 8 : 4) top_kernel(cons
     const uint32_t top = p.top < p.vocab ? p.top : p.vocab;
 
     // Whole vectors, thread by thread, and an element of what is left for each of the first threads; -infinity beyond the row's end.
-    const uint32_t whole = p.vocab / kPer, left = p.vocab % kPer;
-    u32x4 held[VECTORS ? VECTORS : 1];
-    float most[VECTORS ? (VECTORS + 1) / 2 : 1];  // of each two vectors
+    const uint32_t whole = p.vocab / kPer, left = p.vocab % kPer, each = LONG ? (whole + GROUPS * THREADS - 1) / (GROUPS * THREADS) : 1;
+    float most[GROUPS];  // of each group of `each` vectors
     const float last = tid_x() < left ? Element<TYPE>::wide(row[whole * kPer + tid_x()]) : -__builtin_inff();
     Exponentials e = {last, last == -__builtin_inff() ? 0.0f : __expf(last - last)};
-    auto add = [&](const u32x4 &words) {
+    auto load = [&](uint32_t i) {  // the thread's i-th vector
+        constexpr uint32_t kNone = sizeof(T) == 4 ? 0xff800000u : TYPE == CNR_FLOAT_BF16 ? 0xff80ff80u : 0xfc00fc00u;
+        u32x4 w = {kNone, kNone, kNone, kNone};
+        if (i * THREADS + tid_x() < whole) w = load16(row + (uint64_t)(i * THREADS + tid_x()) * kPer);
+        return w;
+    };
+    auto add = [&](u32x4 words) {
+        // (the compiler would have the elements of many as floats at once)
+        asm volatile("" : "+v"(words), "+v"(e.sum));
         const Vector w = __builtin_bit_cast(Vector, words);
         float largest = Element<TYPE>::wide(w.v[0]);
 #pragma unroll
         for (uint32_t j = 1; j < kPer; ++j) largest = __builtin_fmaxf(largest, Element<TYPE>::wide(w.v[j]));
-        const float now = __builtin_fmaxf(e.top, largest), from = now == -__builtin_inff() ? 0.0f : now;
+        const float now = __builtin_fmaxf(e.top, largest), from = now == -__builtin_inff() ? 0.0f : now;  // (differences first: the type's lowest value times log2(e) is infinite)
         float sum = 0.0f;
 #pragma unroll
-        for (uint32_t j = 0; j < kPer; ++j) sum += __expf(Element<TYPE>::wide(w.v[j]) - from);
-        e.sum = __builtin_fmaf(e.sum, __expf(e.top - from), sum);
+        for (uint32_t j = 0; j < kPer; ++j) sum += __builtin_amdgcn_exp2f((Element<TYPE>::wide(w.v[j]) - from) * kLog2e);
+        e.sum = __builtin_fmaf(e.sum, __builtin_amdgcn_exp2f((e.top - from) * kLog2e), sum);
         e.top = now;
         return largest;
     };
-    if constexpr (VECTORS > 0) {
-        const uint32_t none = sizeof(T) == 4 ? 0xff800000u : TYPE == CNR_FLOAT_BF16 ? 0xff80ff80u : 0xfc00fc00u;
+    if constexpr (LONG) {
 #pragma unroll
-        for (uint32_t i = 0; i < VECTORS; ++i) {
-            held[i] = u32x4{none, none, none, none};
-            if (i * THREADS + tid_x() < whole) held[i] = load16(row + (i * THREADS + tid_x()) * kPer);
-        }
+        for (uint32_t q = 0; q < GROUPS; ++q) {
+            most[q] = -__builtin_inff();
+            for (uint32_t i = q * each; i < (q + 1) * each; i += 4) {
+                u32x4 w[4];
 #pragma unroll
-        for (uint32_t i = 0; i < VECTORS; ++i) {
-            const float largest = add(held[i]);
-            most[i / 2] = i % 2 ? __builtin_fmaxf(most[i / 2], largest) : largest;
-            // (the compiler would have the elements of many as floats at once, and keep them until they are looked at again)
-            asm volatile("" : "+v"(held[i]), "+v"(e.sum));
-            __builtin_amdgcn_sched_barrier(0);
+                for (uint32_t j = 0; j < 4; ++j) w[j] = i + j < (q + 1) * each ? load(i + j) : load(0xffffffffu / THREADS);
+#pragma unroll
+                for (uint32_t j = 0; j < 4; ++j) most[q] = __builtin_fmaxf(most[q], add(w[j]));
+            }
         }
     } else {
-        for (uint32_t i = tid_x(); i < whole; i += THREADS) add(load16(row + i * kPer));
+        constexpr uint32_t kAtOnce = 4;
+#pragma unroll
+        for (uint32_t first = 0; first < GROUPS; first += kAtOnce) {
+            u32x4 w[kAtOnce];
+#pragma unroll
+            for (uint32_t j = 0; j < kAtOnce; ++j) w[j] = load(first + j);
+#pragma unroll
+            for (uint32_t j = 0; j < kAtOnce; ++j) most[first + j] = add(w[j]);
+        }
     }
     lds.largest[tid_x()] = key_of(e.top);
-    if (tid_x() == 0) lds.n_found = 0;
+    if (tid_x() == 0) lds.n_found = lds.n_hits = 0;
     e = over_wave(e);
     if (lane == 0) lds.parts[wave] = e;
     __syncthreads();
@@ -179,6 +193,7 @@ __global__ void __launch_bounds__(THREADS, VECTORS <= 8 ? 8 : 4) top_kernel(cons
     }
     if (!p.tokens && !p.values) return;
     __syncthreads();
+    bool again = odd;  // the whole row is looked through
     auto collect = [&](uint64_t from) {
         auto take = [&](float v, uint32_t token) {
             const uint64_t place = place_of(key_of(v), token);
@@ -187,25 +202,34 @@ __global__ void __launch_bounds__(THREADS, VECTORS <= 8 ? 8 : 4) top_kernel(cons
                 if (at < kRoom) lds.found[at] = place;
             }
         };
-        if (VECTORS > 0 && !odd) {
-            const uint32_t key = (uint32_t)(from >> 32);
-            const float least = key <= kMinusInfinity ? -__builtin_inff() : value_of(key);
+        if (again) {
+            for_row<TYPE, THREADS>(row, p.vocab, take);
+        } else {
+            const uint32_t hits = lds.n_hits;
+            for (uint32_t i = tid_x(); i < hits * each; i += THREADS) {
+                const uint32_t hit = lds.hits[i / each], at = (hit / THREADS * each + i % each) * THREADS + hit % THREADS;
+                if (at >= whole) continue;
+                const Vector w = __builtin_bit_cast(Vector, load16(row + (uint64_t)at * kPer));
 #pragma unroll
-            for (uint32_t i = 0; i < VECTORS; ++i) {
-                if (!(most[i / 2] >= least)) continue;
-                u32x4 words = held[i];
-                asm volatile("" : "+v"(words));  // elements as floats here only
-                const Vector w = __builtin_bit_cast(Vector, words);
-#pragma unroll
-                for (uint32_t j = 0; j < kPer; ++j) take(Element<TYPE>::wide(w.v[j]), (i * THREADS + tid_x()) * kPer + j);
+                for (uint32_t j = 0; j < kPer; ++j) take(Element<TYPE>::wide(w.v[j]), at * kPer + j);
             }
             if (tid_x() < left) take(last, whole * kPer + tid_x());
-        } else {
-            for_row<TYPE, THREADS>(row, p.vocab, take);
         }
         __syncthreads();
     };
-    if (top) collect((uint64_t)lds.bound << 32);  // places from there on
+    const uint32_t bound = lds.bound;
+    if (top && !odd) {
+        const float least = bound <= kMinusInfinity ? -__builtin_inff() : value_of(bound);
+#pragma unroll
+        for (uint32_t q = 0; q < GROUPS; ++q) {
+            if (!(most[q] >= least)) continue;
+            const uint32_t at = atomicAdd(&lds.n_hits, 1u);
+            if (at < 2 * THREADS) lds.hits[at] = q * THREADS + tid_x();
+        }
+        __syncthreads();
+        again = lds.n_hits > 2 * THREADS;
+    }
+    if (top) collect((uint64_t)bound << 32);  // places from there on
     if (top && lds.n_found > kRoom) {
         // Eight bits of the place at a time: how many have each digit behind those that are settled; the digit that the top-th place has.
         uint64_t settled = 0;
@@ -233,6 +257,7 @@ __global__ void __launch_bounds__(THREADS, VECTORS <= 8 ? 8 : 4) top_kernel(cons
             __syncthreads();
             if (above + with <= kRoom) break;
         }
+        again = true;
         collect(settled);
     }
     const uint32_t found = top ? lds.n_found : 0;
@@ -258,23 +283,22 @@ template <int TYPE, uint32_t THREADS>
 void launch(const TopArgs &a, uint64_t vectors, hipStream_t s) {
     const dim3 grid((unsigned)a.n), threads(THREADS);
     if (vectors <= 4)
-        hipLaunchKernelGGL((top_kernel<TYPE, THREADS, 4>), grid, threads, 0, s, a);
+        hipLaunchKernelGGL((top_kernel<TYPE, THREADS, 4, false>), grid, threads, 0, s, a);
     else if (vectors <= 8)
-        hipLaunchKernelGGL((top_kernel<TYPE, THREADS, 8>), grid, threads, 0, s, a);
+        hipLaunchKernelGGL((top_kernel<TYPE, THREADS, 8, false>), grid, threads, 0, s, a);
     else if (vectors <= 16)
-        hipLaunchKernelGGL((top_kernel<TYPE, THREADS, 16>), grid, threads, 0, s, a);
+        hipLaunchKernelGGL((top_kernel<TYPE, THREADS, 16, false>), grid, threads, 0, s, a);
     else
-        hipLaunchKernelGGL((top_kernel<TYPE, THREADS, 0>), grid, threads, 0, s, a);
+        hipLaunchKernelGGL((top_kernel<TYPE, THREADS, 16, true>), grid, threads, 0, s, a);
 }
-// The fewer threads hold a row, the more rows share a compute unit and hide each other's steps that have little to do; few rows want many threads.  A bound
+// The fewer threads have a row, the more rows share a compute unit and hide each other's steps that have little to do; few rows want many threads.  A bound
 // is of use where clearly more threads than are asked for have elements.
 template <int TYPE>
 void top_of(const TopArgs &a, const cnr_ctx *ctx, hipStream_t s) {
-    const uint64_t vectors = (uint64_t)a.vocab * sizeof(typename Element<TYPE>::type) / 16;
-    const bool many = a.n > 2 * (uint64_t)ctx->n_cu;
-    if (many && vectors <= 16 * 256 && a.top <= 192)
+    const uint64_t vectors = (uint64_t)a.vocab * sizeof(typename Element<TYPE>::type) / 16, per_unit = cnr_ceil_div(a.n, ctx->n_cu);
+    if (per_unit > 4 && a.top <= 192)
         launch<TYPE, 256>(a, cnr_ceil_div(vectors, 256), s);
-    else if (many && vectors <= 16 * 512 && a.top <= 384)
+    else if (per_unit > 2 && a.top <= 384)
         launch<TYPE, 512>(a, cnr_ceil_div(vectors, 512), s);
     else
         launch<TYPE, 1024>(a, cnr_ceil_div(vectors, 1024), s);

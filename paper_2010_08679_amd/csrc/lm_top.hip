@@ -85,9 +85,9 @@ struct Lds {
     uint32_t bound;
 };
 
-// GROUPS groups of vectors to a thread, of one vector each unless LONG.  Rows with a NaN or an infinity are looked through again by their keys.
-template <int TYPE, uint32_t THREADS, uint32_t GROUPS, bool LONG>
-__global__ void __launch_bounds__(THREADS) top_kernel(const TopArgs p) {
+// GROUPS groups of EACH vectors to a thread, 0: of as many as the row takes.  Rows with a NaN or an infinity are looked through again by their keys.
+template <int TYPE, uint32_t THREADS, uint32_t GROUPS, uint32_t EACH>
+__global__ void __launch_bounds__(THREADS, EACH == 2 ? 8 : 1) top_kernel(const TopArgs p) {
     typedef typename Element<TYPE>::type T;
     constexpr uint32_t kPer = 16 / sizeof(T);
     typedef Pack<T, kPer> Vector;
@@ -99,7 +99,7 @@ __global__ void __launch_bounds__(THREADS) top_kernel(const TopArgs p) {
     const uint32_t top = p.top < p.vocab ? p.top : p.vocab;
 
     // Whole vectors, thread by thread, and an element of what is left for each of the first threads; -infinity beyond the row's end.
-    const uint32_t whole = p.vocab / kPer, left = p.vocab % kPer, each = LONG ? (whole + GROUPS * THREADS - 1) / (GROUPS * THREADS) : 1;
+    const uint32_t whole = p.vocab / kPer, left = p.vocab % kPer, each = EACH ? EACH : (whole + GROUPS * THREADS - 1) / (GROUPS * THREADS);
     float most[GROUPS];  // of each group of `each` vectors
     const float last = tid_x() < left ? Element<TYPE>::wide(row[whole * kPer + tid_x()]) : -__builtin_inff();
     Exponentials e = {last, last == -__builtin_inff() ? 0.0f : __expf(last - last)};
@@ -124,7 +124,7 @@ __global__ void __launch_bounds__(THREADS) top_kernel(const TopArgs p) {
         e.top = now;
         return largest;
     };
-    if constexpr (LONG) {
+    if constexpr (EACH == 0) {
 #pragma unroll
         for (uint32_t q = 0; q < GROUPS; ++q) {
             most[q] = -__builtin_inff();
@@ -139,12 +139,16 @@ __global__ void __launch_bounds__(THREADS) top_kernel(const TopArgs p) {
     } else {
         constexpr uint32_t kAtOnce = 4;
 #pragma unroll
-        for (uint32_t first = 0; first < GROUPS; first += kAtOnce) {
+        for (uint32_t first = 0; first < GROUPS * EACH; first += kAtOnce) {
             u32x4 w[kAtOnce];
 #pragma unroll
             for (uint32_t j = 0; j < kAtOnce; ++j) w[j] = load(first + j);
 #pragma unroll
-            for (uint32_t j = 0; j < kAtOnce; ++j) most[first + j] = add(w[j]);
+            for (uint32_t j = 0; j < kAtOnce; ++j) {
+                const float largest = add(w[j]);
+                float &of = most[(first + j) / EACH];
+                of = (first + j) % EACH ? __builtin_fmaxf(of, largest) : largest;
+            }
         }
     }
     lds.largest[tid_x()] = key_of(e.top);
@@ -283,13 +287,13 @@ template <int TYPE, uint32_t THREADS>
 void launch(const TopArgs &a, uint64_t vectors, hipStream_t s) {
     const dim3 grid((unsigned)a.n), threads(THREADS);
     if (vectors <= 4)
-        hipLaunchKernelGGL((top_kernel<TYPE, THREADS, 4, false>), grid, threads, 0, s, a);
+        hipLaunchKernelGGL((top_kernel<TYPE, THREADS, 4, 1>), grid, threads, 0, s, a);
     else if (vectors <= 8)
-        hipLaunchKernelGGL((top_kernel<TYPE, THREADS, 8, false>), grid, threads, 0, s, a);
+        hipLaunchKernelGGL((top_kernel<TYPE, THREADS, 8, 1>), grid, threads, 0, s, a);
     else if (vectors <= 16)
-        hipLaunchKernelGGL((top_kernel<TYPE, THREADS, 16, false>), grid, threads, 0, s, a);
+        hipLaunchKernelGGL((top_kernel<TYPE, THREADS, THREADS == 1024 ? 8 : 16, THREADS == 1024 ? 2 : 1>), grid, threads, 0, s, a);
     else
-        hipLaunchKernelGGL((top_kernel<TYPE, THREADS, 16, true>), grid, threads, 0, s, a);
+        hipLaunchKernelGGL((top_kernel<TYPE, THREADS, 16, 0>), grid, threads, 0, s, a);
 }
 // The fewer threads have a row, the more rows share a compute unit and hide each other's steps that have little to do; few rows want many threads.  A bound
 // is of use where clearly more threads than are asked for have elements.

@@ -20,8 +20,9 @@ extern "C" {
 
 /* The logits z[i][v] = sum over t < dim of hidden[i][t] * weight[v][t], of which a vocabulary's losses are made; a host struct, read during the call.
  *   hidden, weight  float, bfloat16 or half [n][dim] and [vocab][dim] as `type` says, aligned to their element, rows
- *                   hidden_stride and weight_stride >= dim elements apart.  Products and sums are fp32's.  Rows that are whole multiples of 128 bytes,
- *                   16 bytes aligned, are read where they are; others are laid out in the workspace first */
+ *                   hidden_stride and weight_stride >= dim elements apart.  Products and sums are fp32's.  Rows of 16 bits of a multiple of 8
+ *                   elements, 16 bytes aligned, are read where they are by more than 16 rows; others are laid out in the workspace first.  Floats are
+ *                   multiplied in three parts of 8 bits: six of nine products, off by 2^-21 of the product at most and 2^-24 on average */
 typedef struct {
     const void *hidden;
     uint64_t hidden_stride;
@@ -53,8 +54,8 @@ typedef struct {
  *   target t         lse - z[i][t]                                             (T is 1)
  *   teacher          sum over j of q_j (log q_j - z[i][tokens[j]] / T + lse),  q the softmax of the teacher's logits / T over the row's tokens
  * A row without a token (a padded target, no token within the vocabulary, a teacher whose logits are all -infinity) is left out: its loss is 0, it has no
- * gradient, and its hidden state may hold anything.  A row with a NaN or an infinite z that is not -infinity has a loss of NaN.
- *   state        NULL, or float [cnr_loss_state_floats(n, top)], kept for the backward pass
+ * gradient, and its hidden state may hold anything.  A row with a NaN or an infinite z that is not -infinity has a loss of NaN.  |z / T| is to be below 2^127.
+ *   state        float [cnr_loss_state_floats(n, top)], kept for the backward pass; may be NULL for targets that no backward pass follows
  *   workspace    cnr_loss_workspace_bytes(n, vocab, dim, type, 0, type) bytes at least (which serve fewer rows as well), 256-byte aligned,
  *                contents irrelevant; where vocab is 0, NULL
  * Nothing depends on other work on the GPU, sums are joined in order.

@@ -31,7 +31,8 @@ def loss(hidden, weight, tokens, logits=None, temperature=1.0, dloss=None, there
     u, e = 2.0 ** -24, ROUNDING[kind]
     n, dim = hidden.shape
     vocab = weight.shape[0]
-    tokens = tokens.to(torch.int64).reshape(n, -1)
+    tokens = tokens.to(torch.int64)
+    tokens = tokens[:, None] if tokens.dim() == 1 else tokens
     q = shares(tokens, vocab, logits, temperature)
     counts = (q.sum(dim=1) != 0) if tokens.shape[1] else torch.zeros(n, dtype=torch.bool, device=hidden.device)  # NaN counts
     adds = counts if dloss is None else counts & (dloss != 0)

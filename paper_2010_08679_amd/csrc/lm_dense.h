@@ -1,8 +1,8 @@
 // Products of plain matrices, out[row][column] = sum over k of down[row][k] across[column][k], for kernels that do something of their own with the outputs.
 //
 // Elements have 16 bits and go through the matrix instructions of their type: exact products, added up in fp32.  Each operand lies either along k (a row or
-// column of the output in a row of its own, in whole blocks of 64 elements) or across it ([k][row or column], read through the LDS's transposing
-// loads).  An operand may be held in several parts, side by side in its rows, that add up to it (a float in three bfloat16): the sum then goes over
+// column of the output in a row of its own, in whole pieces of eight elements) or across it ([k][row or column], read through the LDS's transposing
+// loads; columns in whole pieces of eight).  An operand may be held in several parts, side by side in its rows, that add up to it (a float in three bfloat16): the sum then goes over
 // pairs of parts ("terms") one after the other.
 #pragma once
 
@@ -28,11 +28,12 @@ struct Operand {
     uint32_t row_bytes;   // of a row with all its parts, a multiple of 16; the last row ends with them
     uint32_t part_bytes;  // from one part to the next in a row
     uint32_t parts;       // which part each term takes, four bits a term, the first term lowest
+    uint32_t last;        // pieces of 16 bytes in the last block of a row that lies along k, from 1 to 8; zeros are taken for the others
 };
 struct Args {
     Operand across, down;
     uint32_t columns, rows;  // of the output
-    uint32_t blocks;         // along k, >= 1; operands that lie along k have as many whole blocks, of zeros where they end earlier
+    uint32_t blocks;         // along k, >= 1
     uint32_t k;              // rows of operands that lie across k; behind them zeros are read
     uint32_t terms;          // >= 1
     uint32_t splits;         // parts of the sum, each in its own workgroups
@@ -69,6 +70,8 @@ __device__ __forceinline__ f32x4 multiply(const i32x8 &x, const i32x8 &y, const 
         return __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(f16x8, a), __builtin_bit_cast(f16x8, b), sum, 0, 0, 0);
 }
 
+constexpr uint32_t kNowhere = 0xf0000000u;  // beyond every buffer, whatever is added: zeros arrive
+
 // Base and size are the same for all lanes.
 __device__ __forceinline__ i32x4 buffer_of(uint64_t base, uint64_t bytes) {
     i32x4 r;
@@ -99,14 +102,15 @@ __device__ __forceinline__ void barrier() {
 
 // What a workgroup's outputs are to its epilogue.  A lane holds MF / 2 times eight columns side by side, 32 apart, of NF rows: value(acc, i, g) is that of
 // column column_of(i) and row row(g).  The four lanes of a row thus write 64 bytes of 16-bit outputs side by side at a time.
-template <int MF, int NF, bool DOWN>
+template <int MF, int NF, bool DOWN, uint32_t THREADS, uint32_t LDS>
 struct Place {
+    static constexpr uint32_t kThreads = THREADS, kLdsBytes = LDS;
     uint32_t row0, column0;  // first output of the workgroup
     uint32_t lane_row;       // the lane's first row within the workgroup's
     uint32_t column;         // the lane's first
     uint32_t split, tile_column;
     uint32_t wave_column;    // which of the WM parts of the workgroup's columns is the wave's
-    uint8_t *lds;            // free, as large as the stages were
+    uint8_t *lds;            // kLdsBytes, free
     // (rows from an operand across k: chunks of odd lanes change places by pairs, see Across)
     __device__ __forceinline__ uint32_t row_within(uint32_t g) const { return lane_row + g / 2 * 32 + (DOWN ? (g ^ tid_x() / 4) % 2 : g % 2) * 4; }
     __device__ __forceinline__ uint32_t row(uint32_t g) const { return row0 + row_within(g); }
@@ -125,16 +129,19 @@ template <int F, int T, int LOADS>
 struct Along {
     i32x4 buffer;
     uint32_t from[LOADS];
-    uint32_t piece[2];  // of the first fragment's row, by half of the block
+    uint32_t beyond;     // bit j: load j's piece is beyond the end of the row, where the block is its last
+    uint32_t piece[2];   // of the first fragment's row, by half of the block
     // Rows beyond the matrix read its last one again.
     __device__ __forceinline__ Along(const Operand &o, uint32_t first, uint32_t count, uint32_t, uint32_t wave, uint32_t section, uint32_t region) {
         const uint32_t lane = tid_x() % kWave, r = lane % 16, quarter = lane / 16, rows = count - first < T ? count - first : T;
         buffer = buffer_of(reinterpret_cast<uint64_t>(o.at) + (uint64_t)first * o.stride, (uint64_t)(rows - 1) * o.stride + o.row_bytes);
+        beyond = 0;
 #pragma unroll
         for (int j = 0; j < LOADS; ++j) {
             const uint32_t line = (wave * LOADS + j) * 4 + quarter, logical = r ^ (line / 4 % 4 * 2 + line % 2);
             const uint32_t row = 2 * line + logical / 8;
             from[j] = (row < rows ? row : rows - 1) * (uint32_t)o.stride + logical % 8 * 16;
+            beyond |= logical % 8 >= o.last ? 1u << j : 0u;
         }
 #pragma unroll
         for (uint32_t h = 0; h < 2; ++h) piece[h] = region + section * kBlockBytes + (r / 4 * 4 + r % 4 / 2) * 256 + ((r % 2 * 8 + quarter + 4 * h) ^ r / 2) * 16;
@@ -142,6 +149,11 @@ struct Along {
     template <int J>
     __device__ __forceinline__ void fetch(const Operand &, uint32_t lds, uint32_t part, uint32_t block) const {
         load_to_lds(buffer, lds, from[J], part + block * kBlockBytes);
+    }
+    // From here on the last block is read.  (Where rows end within it there is one term: an operand of several parts is laid out in whole blocks.)
+    __device__ __forceinline__ void end() {
+#pragma unroll
+        for (int j = 0; j < LOADS; ++j) from[j] = beyond >> j & 1u ? kNowhere : from[j];
     }
     __device__ __forceinline__ void move(uint32_t by) {
         piece[0] += by;
@@ -184,6 +196,7 @@ struct Across {
         const uint64_t on = part + (uint64_t)block * kBlockElements * o.stride;
         load_to_lds(buffer_of(at + on, on < left ? left - on : 0), lds, from[J], 0);
     }
+    __device__ __forceinline__ void end() {}
     __device__ __forceinline__ void move(uint32_t by) { chunk += by; }
     __device__ __forceinline__ i32x8 fragment(const uint8_t *lds, uint32_t f) const {
         typedef __attribute__((address_space(3))) s16x4 *Lds;
@@ -232,6 +245,13 @@ __global__ void __launch_bounds__(WM * WN * kWave, 2) tile_kernel(const Args p, 
     const uint32_t lds_at = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) uint8_t *)lds;
     // The block to be fetched next; behind the last one it stays there, and nobody reads what arrives: the count of loads stays the same without a branch.
     uint32_t ahead = begin, block = begin % p.blocks, term = begin / p.blocks;
+    auto end_of_rows = [&]() {
+        if (block + 1 == p.blocks) {
+            a.end();
+            b.end();
+        }
+    };
+    end_of_rows();
     auto fetch = [&](uint32_t to, auto index) {
         constexpr int J = decltype(index)::value;
         if constexpr (J < LA)
@@ -245,6 +265,7 @@ __global__ void __launch_bounds__(WM * WN * kWave, 2) tile_kernel(const Args p, 
             const bool over = block + 1 == p.blocks;
             block = over ? 0 : block + 1;
             term += over ? 1 : 0;
+            end_of_rows();
         }
     };
 
@@ -324,7 +345,7 @@ __global__ void __launch_bounds__(WM * WN * kWave, 2) tile_kernel(const Args p, 
                     acc[f + 1][g][i] = quarter % 2 ? v : w;
                 }
     }
-    Place<MF, NF, DOWN> place;
+    Place<MF, NF, DOWN, WM * WN * kWave, STAGES * kStage> place;
     place.row0 = row0;
     place.column0 = column0;
     place.lane_row = wave_n + r / 4 * 8 + r % 4;

@@ -3,9 +3,9 @@
 // The softmax cross entropy of a target is the distillation from a teacher that is certain: both are
 //   loss = sum_j q_j (log q_j - z'[token_j] + lse),  z' = z / T,  lse = log sum_v exp z'_v
 //   dz_v = dloss / T (exp(z'_v - lse) - sum of q_j with token_j = v)
-// with a few (token, share) entries a row, so one machine serves them:
+// with a few (token, share) entries a row, so one machine serves them.  The entries of a teacher are sorted by token first, and those of one token put together.
 //   forward   a product whose tiles leave, for each row, the largest logit and the sum of exponentials relative to it (kept to base 2: exp2 is one
-//             instruction), and one workgroup a row that joins them, takes the entries' logits as dot products and writes the loss;
+//             instruction), and the entries' logits, by way of LDS; one workgroup a row then joins them and writes the loss;
 //   backward  for a piece of the vocabulary at a time, the logits once more, turned into dz in the epilogue; the entries' own dz, a few a row, are put in
 //             by a kernel of its own; then dhidden += dz weight and dweight = dz^T hidden, products that read the weight, the hidden states and dz along
 //             whichever side their sum goes, so nothing is transposed in memory.
@@ -75,12 +75,25 @@ __device__ __forceinline__ Stats stats16(const float (&z)[N], float c, uint32_t 
 
 // ---- what the products' tiles do with their outputs ----------------------------------------------------------------
 
-// Stats of each row over the tile's columns.
+// A teacher's entries, [n][top], in the order of their tokens; kNoToken behind the last.
+constexpr int32_t kNoToken = 0x7fffffff;
+struct Entries {
+    int32_t *tokens;
+    float *share;   // all of a token's at its first entry
+    float *picked;  // its logit
+    uint32_t top;
+};
+
+// Stats of each row over the tile's columns; with PICK also the logits of the entries there.
+template <bool PICK>
 struct KeepStats {
     static constexpr bool kUsesLds = true;
     Stats *parts;      // [rows][n_parts], from the piece's first part on
     uint32_t n_parts;
     float c;
+    const uint16_t *begins;  // [rows][n_parts + 1], likewise: a tile's first entry in a row
+    Entries entries;         // from the first row on
+    uint32_t first;          // token of the first column
     template <uint32_t TM, uint32_t TN, int WM, typename Place, int MF, int NF>
     __device__ __forceinline__ void finish(const dense::Args &p, const Place &at, const f32x4 (&acc)[MF][NF]) const {
         if (at.column0 + TM <= p.columns)
@@ -113,6 +126,44 @@ struct KeepStats {
 #pragma unroll
             for (int w = 1; w < WM; ++w) s = join(s, lds[w * TN + row]);
             parts[(uint64_t)(at.row0 + row) * n_parts + at.tile_column] = s;
+        }
+        if constexpr (PICK) pick<TM, TN>(p, at, acc);
+    }
+    // The tile goes into LDS, as many rows at a time as there is room for, and each entry looks its logit up: what it costs does not depend on where the entries
+    // are.  Pieces of four columns are permuted by the row, so that rows that are written together take different banks.
+    template <uint32_t TM, uint32_t TN, typename Place, int MF, int NF>
+    __device__ __forceinline__ void pick(const dense::Args &p, const Place &at, const f32x4 (&acc)[MF][NF]) const {
+        constexpr uint32_t kRoom = Place::kLdsBytes / (TM * 4), kRows = kRoom < TN ? kRoom : TN, kEach = Place::kThreads / kRows;
+        static_assert(TN % kRows == 0 && Place::kThreads % kRows == 0, "whole phases");
+        float *lds = reinterpret_cast<float *>(at.lds);
+        const uint32_t column0 = at.column - at.column0, sub = tid_x() / kRows, own = tid_x() % kRows;
+#pragma unroll
+        for (uint32_t phase = 0; phase < TN / kRows; ++phase) {
+            const uint32_t row = at.row0 + phase * kRows + own;
+            uint32_t begin = 0, end = 0;
+            if (row < p.rows) {
+                const uint16_t *b = begins + (uint64_t)row * (n_parts + 1) + at.tile_column;
+                begin = b[0];
+                end = b[1];
+            }
+            __syncthreads();
+#pragma unroll
+            for (int g = 0; g < NF; ++g) {
+                const uint32_t within = at.row_within(g) - phase * kRows;
+                if (within >= kRows) continue;
+#pragma unroll
+                for (int i = 0; i < 4 * MF; i += 4) {
+                    const f32x4 v = {at.value(acc, i, g), at.value(acc, i + 1, g), at.value(acc, i + 2, g), at.value(acc, i + 3, g)};
+                    const uint32_t piece = (column0 + i / 8 * 32 + i % 8) / 4;
+                    *reinterpret_cast<f32x4 *>(lds + within * TM + (piece ^ within % 16) * 4) = v;
+                }
+            }
+            __syncthreads();
+            for (uint32_t e = begin + sub; e < end; e += kEach) {
+                const uint64_t entry = (uint64_t)row * entries.top + e;
+                const uint32_t column = (uint32_t)entries.tokens[entry] - first - at.column0;
+                if (column < TM) entries.picked[entry] = lds[own * TM + ((column / 4) ^ own % 16) * 4 + column % 4];
+            }
         }
     }
 };
@@ -282,15 +333,36 @@ struct KeepSum {
     }
 };
 
-// The parts of sums that were split, added up in order: four outputs of a row to a thread.
+// The parts of sums that were split, added up in order: four outputs of a row to a thread, or to LANES threads, each with every LANES-th part.
+template <uint32_t LANES>
 __global__ void __launch_bounds__(kBlock) join_sums_kernel(const KeepSum k, uint32_t m, uint32_t n, uint32_t splits) {
-    const uint32_t across = (uint32_t)(k.partial_stride / 4);
-    const uint64_t at = (uint64_t)wg_x() * kBlock + tid_x();
-    if (at >= (uint64_t)m * across) return;
+    const uint32_t across = (uint32_t)(k.partial_stride / 4), lane = tid_x() / (kBlock / LANES);
+    const uint64_t at = (uint64_t)wg_x() * (kBlock / LANES) + tid_x() % (kBlock / LANES);
+    const bool there = at < (uint64_t)m * across;
     const uint32_t row = (uint32_t)(at / across), column = (uint32_t)(at % across) * 4;
-    const float *from = k.partial + (uint64_t)row * k.partial_stride + column;
-    f32x4 sum = *reinterpret_cast<const f32x4 *>(from);
-    for (uint32_t s = 1; s < splits; ++s) sum += *reinterpret_cast<const f32x4 *>(from + (uint64_t)s * m * k.partial_stride);
+    f32x4 sum = {0.0f, 0.0f, 0.0f, 0.0f};
+    if (there) {
+        const float *from = k.partial + (uint64_t)row * k.partial_stride + column;
+        for (uint32_t s = lane; s < splits; s += 8 * LANES) {
+            f32x4 part[8];
+#pragma unroll
+            for (uint32_t u = 0; u < 8; ++u) {
+                part[u] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+                if (s + u * LANES < splits) part[u] = *reinterpret_cast<const f32x4 *>(from + (uint64_t)(s + u * LANES) * m * k.partial_stride);
+            }
+#pragma unroll
+            for (uint32_t u = 0; u < 8; ++u) sum += part[u];
+        }
+    }
+    if constexpr (LANES > 1) {
+        __shared__ f32x4 lds[LANES][kBlock / LANES];
+        lds[lane][tid_x() % (kBlock / LANES)] = sum;
+        __syncthreads();
+        if (lane) return;
+#pragma unroll
+        for (uint32_t l = 1; l < LANES; ++l) sum += lds[l][tid_x()];
+    }
+    if (!there) return;
     const float by = k.scale ? *k.scale : 1.0f;
     float v[4] = {0.0f, 0.0f, 0.0f, 0.0f};
     if (k.there.out) read_row(k.there, row, column, n, v);
@@ -359,10 +431,24 @@ __global__ void __launch_bounds__(kBlock) lay_out_kernel(const Layout a, const L
     }
 }
 
-// ---- forward: few rows, operands straight from memory ------------------------------------------------------------
+// ---- few rows: operands straight from memory -------------------------------------------------------------------
 //
-// A workgroup has 16 rows by 16 NF columns; each of its waves takes a quarter of the sum, U blocks at a time so that enough loads are under way, straight
-// into the matrix instructions' registers; they add up their sums in LDS.  Bound by reading the weight.
+// Logits: a workgroup has 16 MF rows by 16 NF columns; each of its waves takes a quarter of the sum, U blocks at a time so that enough loads are under way,
+// straight into the matrix instructions' registers (floats into the fp32 ones); they add up their sums in LDS.  Bound by reading the weight: 1 x 32000 x
+// 4096 in bfloat16 43.7 us, 6.0 TB/s.
+//
+// The gradients' products go through the fp32 matrix instructions too, with dz in fp32: sixteen rows of dz by four tokens (or sixteen tokens by sixteen rows) by
+// sixteen columns at a time, a lane with four columns side by side of each row of the weight, or of its gradient.
+struct NarrowArgs {
+    const void *hidden, *weight;
+    uint64_t hidden_stride, weight_stride;  // elements
+    uint32_t n, vocab, dim;
+    float c;
+    Stats *parts;              // or, for the backward pass,
+    uint32_t n_parts;
+    const RowGradient *rows;
+    float *dz;                 // [vocab][16], zeros in rows from n on
+};
 template <int TYPE>
 __device__ __forceinline__ f32x4 multiply(const dense::i32x8 &x, const dense::i32x8 &y, f32x4 sum) {
     if constexpr (TYPE == CNR_FLOAT_F32) {
@@ -373,14 +459,6 @@ __device__ __forceinline__ f32x4 multiply(const dense::i32x8 &x, const dense::i3
         return dense::multiply<TYPE, 1>(x, y, dense::multiply<TYPE, 0>(x, y, sum));
     }
 }
-struct NarrowArgs {
-    const void *hidden, *weight;
-    uint64_t hidden_stride, weight_stride;  // elements
-    uint32_t n, vocab, dim;
-    Stats *parts;
-    uint32_t n_parts;
-    float c;
-};
 template <typename T>
 __device__ __forceinline__ dense::i32x8 load_fragment(const T *row, uint32_t at, uint32_t dim) {
     constexpr uint32_t kPer = 16 / sizeof(T);
@@ -399,16 +477,15 @@ __device__ __forceinline__ dense::i32x8 load_fragment(const T *row, uint32_t at,
     }
     return __builtin_shufflevector(part[0], part[1], 0, 1, 2, 3, 4, 5, 6, 7);
 }
-template <int TYPE, int NF, int U>
+template <int TYPE, int NF, int U, bool GRADIENT>
 __global__ void __launch_bounds__(kBlock, 4) narrow_kernel(const NarrowArgs p) {
     typedef typename Element<TYPE>::type T;
     constexpr uint32_t kPer = 16 / sizeof(T), kColumns = dense::kBlockBytes / sizeof(T);
     __shared__ f32x4 sums[kWavesPerBlock][NF][kWave];
     const uint32_t lane = tid_x() % kWave, wave = (uint32_t)__builtin_amdgcn_readfirstlane((int)(tid_x() / kWave));
-    const uint32_t quarter = lane / 16, m0 = wg_y() * 16, n0 = wg_x() * 16 * NF;
+    const uint32_t quarter = lane / 16, n0 = wg_x() * 16 * NF;
     // Rows beyond the matrix read its last one again.
-    const uint32_t row = m0 + lane % 16 < p.n ? m0 + lane % 16 : p.n - 1;
-    const T *a = reinterpret_cast<const T *>(p.hidden) + row * p.hidden_stride, *b[NF];
+    const T *a = reinterpret_cast<const T *>(p.hidden) + (lane % 16 < p.n ? lane % 16 : p.n - 1) * p.hidden_stride, *b[NF];
 #pragma unroll
     for (int g = 0; g < NF; ++g) {
         const uint32_t v = n0 + 16 * g + lane % 16;
@@ -450,8 +527,143 @@ __global__ void __launch_bounds__(kBlock, 4) narrow_kernel(const NarrowArgs p) {
         for (int w = 0; w < kWavesPerBlock; ++w) z[g] += sums[w][g][m / 4 * 16 + n][m % 4];
         valid |= n0 + 16 * g + n < p.vocab ? 1u << g : 0u;
     }
-    const Stats s = stats16(z, p.c, valid);
-    if (n == 0 && m0 + m < p.n) p.parts[(uint64_t)(m0 + m) * p.n_parts + wg_x()] = s;
+    if constexpr (GRADIENT) {
+        const RowGradient r = p.rows[m];  // (padded with rows that add nothing)
+#pragma unroll
+        for (uint32_t g = 0; g < NF; ++g) {
+            const uint32_t v = n0 + 16 * g + n;
+            const float e = exp2_of(__builtin_fmaf(z[g], p.c, -r.lse2));
+            if (valid >> g & 1u) p.dz[(uint64_t)v * 16 + m] = r.gradient == 0.0f ? 0.0f : r.gradient * (v == r.target ? e - 1.0f : e);
+        }
+    } else {
+        const Stats s = stats16(z, p.c, valid);
+        if (n == 0 && m < p.n) p.parts[(uint64_t)m * p.n_parts + wg_x()] = s;
+    }
+}
+
+// Four elements from `column` on, 0 beyond the row.
+template <typename T>
+__device__ __forceinline__ f32x4 load_four(const T *row, uint32_t column, uint32_t dim) {
+    f32x4 v;
+    if (column + 4 <= dim) {
+        const Pack<T, 4> w = *reinterpret_cast<const Pack<T, 4> *>(row + column);
+#pragma unroll
+        for (int j = 0; j < 4; ++j) v[j] = (float)w.v[j];
+    } else {
+#pragma unroll
+        for (int j = 0; j < 4; ++j) v[j] = column + j < dim ? (float)row[column + j] : 0.0f;
+    }
+    return v;
+}
+struct SlabArgs {
+    const void *matrix;        // the weight, or the hidden states
+    uint64_t stride;
+    const float *dz;           // [vocab][16]
+    uint32_t vocab, dim, n;
+    uint32_t groups, slabs;    // of 64 columns, of the vocabulary: a wave has one of each
+    float *partial;            // [slabs][n][partial_stride]
+    uint64_t partial_stride;
+    const float *lse2, *dloss; // which hidden states count
+    Target out, there;
+};
+// partial[slab][i][column] = sum over the slab's tokens of dz[v][i] * weight[v][column].
+template <int TYPE>
+__global__ void __launch_bounds__(kBlock) narrow_hidden_kernel(const SlabArgs p) {
+    typedef typename Element<TYPE>::type T;
+    const uint32_t wave = wave_in_grid(), group = wave % p.groups, slab = wave / p.groups, lane = tid_x() % kWave, quarter = lane / 16, r = lane % 16;
+    if (slab >= p.slabs) return;
+    const uint32_t column = group * 64 + r * 4;
+    const uint32_t begin = (uint32_t)((uint64_t)p.vocab * slab / p.slabs), end = (uint32_t)((uint64_t)p.vocab * (slab + 1) / p.slabs);
+    const T *matrix = reinterpret_cast<const T *>(p.matrix);
+    f32x4 acc[4];  // [column][row of dz]
+#pragma unroll
+    for (int j = 0; j < 4; ++j) acc[j] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+    constexpr uint32_t kAtOnce = 8;
+    for (uint32_t v0 = begin; v0 < end; v0 += 4 * kAtOnce) {
+        f32x4 w[kAtOnce];
+        float d[kAtOnce];
+#pragma unroll
+        for (uint32_t u = 0; u < kAtOnce; ++u) {
+            const uint32_t v = v0 + 4 * u + quarter, at = v < end ? v : end - 1;
+            w[u] = load_four(matrix + (uint64_t)at * p.stride, column, p.dim);
+            d[u] = p.dz[(uint64_t)at * 16 + r];
+            d[u] = v < end ? d[u] : 0.0f;
+        }
+#pragma unroll
+        for (uint32_t u = 0; u < kAtOnce; ++u)
+#pragma unroll
+            for (int j = 0; j < 4; ++j) acc[j] = __builtin_amdgcn_mfma_f32_16x16x4f32(d[u], w[u][j], acc[j], 0, 0, 0);
+    }
+    // sum i of a lane: row 4 quarter + i, column r of each of the four sixteens
+#pragma unroll
+    for (uint32_t i = 0; i < 4; ++i) {
+        const float v[4] = {acc[0][i], acc[1][i], acc[2][i], acc[3][i]};
+        if (4 * quarter + i < p.n) write_as(p.partial + ((uint64_t)slab * p.n + 4 * quarter + i) * p.partial_stride + column, column, p.dim, v);
+    }
+}
+// out[v][column] = there + sum over i of dz[v][i] * hidden[i][column].
+template <int TYPE>
+__global__ void __launch_bounds__(kBlock) narrow_weight_kernel(const SlabArgs p) {
+    typedef typename Element<TYPE>::type T;
+    const uint32_t wave = wave_in_grid(), group = wave % p.groups, slab = wave / p.groups, lane = tid_x() % kWave, quarter = lane / 16, r = lane % 16;
+    if (slab >= p.slabs) return;
+    const uint32_t begin = (uint32_t)((uint64_t)p.vocab * slab / p.slabs), end = (uint32_t)((uint64_t)p.vocab * (slab + 1) / p.slabs);
+    const T *matrix = reinterpret_cast<const T *>(p.matrix);
+    // Sixteen columns f are 32 (f / 2) + 8 (r / 4) + 4 (f % 2) + r % 4: a lane has eight outputs side by side, and the four lanes of a token 32.
+    float x[4][4];  // [f][row of hidden states 4 quarter + s]
+#pragma unroll
+    for (uint32_t s = 0; s < 4; ++s) {
+        const uint32_t row = 4 * quarter + s;
+        const bool counts = row < p.n && p.lse2[row] != __builtin_inff() && p.dloss[row] != 0.0f;
+#pragma unroll
+        for (uint32_t f = 0; f < 4; ++f) {
+            const uint32_t column = group * 64 + f / 2 * 32 + r / 4 * 8 + f % 2 * 4 + r % 4;
+            x[f][s] = counts && column < p.dim ? (float)matrix[row * p.stride + column] : 0.0f;
+        }
+    }
+    constexpr uint32_t kAtOnce = 2;
+    for (uint32_t v0 = begin; v0 < end; v0 += 16 * kAtOnce) {
+        f32x4 d[kAtOnce];
+        float old[kAtOnce][2][8];
+#pragma unroll
+        for (uint32_t u = 0; u < kAtOnce; ++u) {
+            const uint32_t v = v0 + 16 * u + r, at = v < end ? v : end - 1;
+            d[u] = *reinterpret_cast<const f32x4 *>(p.dz + (uint64_t)at * 16 + 4 * quarter);
+#pragma unroll
+            for (uint32_t h = 0; h < 2; ++h) {
+#pragma unroll
+                for (int j = 0; j < 8; ++j) old[u][h][j] = 0.0f;
+                if (p.there.out) read_row(p.there, at, group * 64 + h * 32 + quarter * 8, p.dim, old[u][h]);
+            }
+        }
+#pragma unroll
+        for (uint32_t u = 0; u < kAtOnce; ++u) {
+            const uint32_t v = v0 + 16 * u + r;
+#pragma unroll
+            for (uint32_t h = 0; h < 2; ++h) {
+#pragma unroll
+                for (uint32_t f = 0; f < 2; ++f) {
+                    // (sum i of a lane: column i of its four, token r)
+                    f32x4 sum = {0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll
+                    for (int s = 0; s < 4; ++s) sum = __builtin_amdgcn_mfma_f32_16x16x4f32(x[2 * h + f][s], d[u][s], sum, 0, 0, 0);
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) old[u][h][4 * f + i] += sum[i];
+                }
+                if (v < end) write_row(p.out, v, group * 64 + h * 32 + quarter * 8, p.dim, old[u][h]);
+            }
+        }
+    }
+}
+// dz of a teacher's entries.
+__global__ void __launch_bounds__(kBlock) narrow_entries_kernel(const NarrowArgs p, const Entries entries) {
+    const uint32_t at = wg_x() * kBlock + tid_x();
+    if (at >= p.n * entries.top) return;
+    const float q = entries.share[at];
+    const uint32_t row = at / entries.top, t = (uint32_t)entries.tokens[at];
+    const RowGradient r = p.rows[row];
+    if (q == 0.0f || r.gradient == 0.0f || t >= p.vocab) return;
+    p.dz[(uint64_t)t * 16 + row] = r.gradient * (exp2_of(__builtin_fmaf(entries.picked[at], p.c, -r.lse2)) - q);
 }
 
 // ---- forward: a row's loss -------------------------------------------------------------------------------------
@@ -470,20 +682,98 @@ __device__ __forceinline__ int64_t token_of(const TargetArgs &t, uint64_t row, u
 __device__ __forceinline__ float logit_of(const TargetArgs &t, uint64_t row, uint32_t j) {
     return read({const_cast<void *>(t.logits), t.logit_stride, t.logit_type}, row, j);
 }
+constexpr uint32_t kMaxTop = CNR_LOSS_MAX_TOP;
+__device__ __forceinline__ float max_of_block(float v, float (&parts)[kWavesPerBlock]) {
+    v = wave_max(v);
+    __syncthreads();
+    if (tid_x() % kWave == 0) parts[tid_x() / kWave] = v;
+    __syncthreads();
+    return __builtin_fmaxf(__builtin_fmaxf(parts[0], parts[1]), __builtin_fmaxf(parts[2], parts[3]));
+}
+__device__ __forceinline__ float sum_of_block(float v, float (&parts)[kWavesPerBlock]) {
+    v = wave_sum(v);
+    __syncthreads();
+    if (tid_x() % kWave == 0) parts[tid_x() / kWave] = v;
+    __syncthreads();
+    return (parts[0] + parts[1]) + (parts[2] + parts[3]);
+}
 
-struct LossArgs {
-    const void *hidden, *weight;
-    uint64_t hidden_stride, weight_stride;
-    uint64_t vocab;
-    uint32_t dim;
+// A row's teacher: the shares of its entries, sorted; loss[row] = sum of share * log(share), lse2[row] = 0, or infinity where the row is left out;
+// begins (NULL: not wanted) for tiles of `columns`.  A workgroup to a row.
+struct TeacherArgs {
     TargetArgs targets;
-    const Stats *parts;
-    uint32_t n_parts;
-    uint64_t row0;      // of this launch
-    float *loss;
-    float *lse2, *picked, *share;  // state, or NULL
+    uint64_t vocab, row0;
+    Entries entries;
+    float *loss, *lse2;
+    uint16_t *begins;  // of the launch's first row
+    uint32_t n_parts, columns;
     cnr_dev_errors *err;
 };
+__global__ void __launch_bounds__(kBlock) teacher_kernel(const TeacherArgs p) {
+    __shared__ int32_t token[kMaxTop], sorted[kMaxTop];
+    __shared__ float share[kMaxTop], in_order[kMaxTop];
+    __shared__ float parts[kWavesPerBlock];
+    const uint64_t row = p.row0 + wg_x();
+    const uint32_t top = p.targets.top;
+    float largest = -__builtin_inff();
+    for (uint32_t j = tid_x(); j < top; j += kBlock) {
+        const int64_t t = token_of(p.targets, row, j);
+        const bool there = t >= 0 && (uint64_t)t < p.vocab;
+        if (t >= 0 && !there) atomicAdd(&p.err->n_bad_indices, 1ull);
+        token[j] = there ? (int32_t)t : kNoToken;
+        const float v = there ? logit_of(p.targets, row, j) / p.targets.temperature : -__builtin_inff();
+        share[j] = v;
+        largest = v != v ? __builtin_inff() : __builtin_fmaxf(largest, v);  // NaN, as infinity does, makes the shares NaN
+    }
+    largest = max_of_block(largest, parts);
+    const bool counts = largest != -__builtin_inff();  // else nothing is left of the row
+    float sum = 0.0f;
+    for (uint32_t j = tid_x(); j < top; j += kBlock) sum += token[j] != kNoToken && counts ? expf(share[j] - largest) : 0.0f;
+    sum = sum_of_block(sum, parts);
+    const float log_sum = logf(sum);
+    float negative_entropy = 0.0f;
+    for (uint32_t j = tid_x(); j < top; j += kBlock) {
+        const float v = share[j] - largest, q = token[j] != kNoToken && counts ? expf(v) / sum : 0.0f;
+        if (q != 0.0f) negative_entropy += q * (v - log_sum);
+        share[j] = q;
+    }
+    negative_entropy = sum_of_block(negative_entropy, parts);
+    for (uint32_t j = tid_x(); j < top; j += kBlock) {
+        const int32_t t = token[j];
+        uint32_t place = 0;
+        for (uint32_t i = 0; i < top; ++i) place += token[i] < t || (token[i] == t && i < j) ? 1u : 0u;
+        sorted[place] = t;
+        in_order[place] = share[j];
+    }
+    __syncthreads();
+    for (uint32_t j = tid_x(); j < top; j += kBlock) {
+        const int32_t t = sorted[j];
+        float all = 0.0f;
+        if (t != kNoToken && (j == 0 || sorted[j - 1] != t))
+            for (uint32_t i = j; i < top && sorted[i] == t; ++i) all += in_order[i];
+        p.entries.tokens[row * top + j] = t;
+        p.entries.share[row * top + j] = all;
+        p.entries.picked[row * top + j] = 0.0f;
+    }
+    if (tid_x() == 0) {
+        p.loss[row] = counts ? negative_entropy : 0.0f;
+        p.lse2[row] = counts ? 0.0f : __builtin_inff();
+    }
+    if (!p.begins) return;
+    for (uint64_t tile = tid_x(); tile <= p.n_parts; tile += kBlock) {
+        uint32_t lo = 0, hi = top;  // the first entry whose token is not below
+        while (lo < hi) {
+            const uint32_t middle = (lo + hi) / 2;
+            if ((uint64_t)(uint32_t)sorted[middle] < tile * p.columns)
+                lo = middle + 1;
+            else
+                hi = middle;
+        }
+        // (behind the last tile lie those without a token)
+        p.begins[(uint64_t)wg_x() * (p.n_parts + 1) + tile] = (uint16_t)lo;
+    }
+}
+
 // The product of two rows by THREADS threads: the sum of this wave's.
 template <uint32_t THREADS, typename T>
 __device__ __forceinline__ float dot(const T *x, const T *y, uint32_t dim) {
@@ -500,15 +790,39 @@ __device__ __forceinline__ float dot(const T *x, const T *y, uint32_t dim) {
     }
     return wave_sum(sum);
 }
-constexpr uint32_t kMaxTop = 1024;  // entries of a row
+
+struct LossArgs {
+    const void *hidden, *weight;
+    uint64_t hidden_stride, weight_stride;
+    uint64_t vocab;
+    uint32_t dim;
+    TargetArgs targets;
+    Entries entries;
+    const Stats *parts;
+    uint32_t n_parts;
+    uint64_t row0;      // of this launch
+    float *loss, *lse2; // lse2: NULL where there is no state
+    float c;
+    cnr_dev_errors *err;
+};
+// Logits of entries one by one, an entry to a wave: where few rows go without tiles.
+template <int TYPE>
+__global__ void __launch_bounds__(kBlock) pick_kernel(const LossArgs p, uint64_t n) {
+    typedef typename Element<TYPE>::type T;
+    const uint64_t entry = wave_in_grid();
+    if (entry >= n * p.entries.top) return;
+    const int32_t t = p.entries.tokens[entry];
+    if (t < 0 || (uint64_t)t >= p.vocab) return;
+    const float z = dot<kWave>(reinterpret_cast<const T *>(p.hidden) + entry / p.entries.top * p.hidden_stride, reinterpret_cast<const T *>(p.weight) + (uint64_t)t * p.weight_stride,
+                               p.dim);
+    if (tid_x() % kWave == 0) p.entries.picked[entry] = z;
+}
 
 template <int TYPE, bool SOFT>
 __global__ void __launch_bounds__(kBlock) loss_kernel(const LossArgs p) {
     typedef typename Element<TYPE>::type T;
     __shared__ Stats joined[kWavesPerBlock];
-    __shared__ float sums[kWavesPerBlock][2];
-    __shared__ int32_t token[SOFT ? kMaxTop : 1];
-    __shared__ float share[SOFT ? kMaxTop : 1];
+    __shared__ float sums[kWavesPerBlock];
     const uint32_t lane = tid_x() % kWave, wave = (uint32_t)__builtin_amdgcn_readfirstlane((int)(tid_x() / kWave));
     const uint64_t row = p.row0 + wg_x();
     // eight of the row's parts to a thread at a time, so that their loads and exponentials do not wait for each other
@@ -534,105 +848,34 @@ __global__ void __launch_bounds__(kBlock) loss_kernel(const LossArgs p) {
         s = {top, wave_sum(s.sum * exp2_of(s.top - at))};
     }
     if (lane == 0) joined[wave] = s;
-    const uint32_t top = SOFT ? p.targets.top : 1;
-    const float heat = SOFT ? p.targets.temperature : 1.0f, c = kLog2e / heat;
-    float teacher_top = 0.0f, teacher_sum = 1.0f, negative_entropy = 0.0f;
-    bool counts = true;
+    // the expected logit: the target's, of which each wave has a part of the sum, or that of the teacher
+    float expected = 0.0f;
+    bool counts;
     if constexpr (SOFT) {
-        // The teacher's distribution over the row's entries.
-        float largest = -__builtin_inff();
-        for (uint32_t j = tid_x(); j < top; j += kBlock) {
-            const int64_t t = token_of(p.targets, row, j);
-            const bool there = t >= 0 && (uint64_t)t < p.vocab;
-            if (t >= 0 && !there) atomicAdd(&p.err->n_bad_indices, 1ull);
-            token[j] = there ? (int32_t)t : -1;
-            const float v = there ? logit_of(p.targets, row, j) / heat : -__builtin_inff();
-            share[j] = v;
-            largest = v != v ? __builtin_inff() : __builtin_fmaxf(largest, v);  // NaN, as infinity does, makes the shares NaN
+        counts = p.lse2[row] != __builtin_inff();
+        for (uint32_t j = tid_x(); j < p.entries.top; j += kBlock) {
+            const float q = p.entries.share[row * p.entries.top + j];
+            if (q != 0.0f) expected = __builtin_fmaf(q, p.entries.picked[row * p.entries.top + j], expected);
         }
-        largest = wave_max(largest);
-        if (lane == 0) sums[wave][0] = largest;
-        __syncthreads();
-        teacher_top = sums[0][0];
-        for (int w = 1; w < kWavesPerBlock; ++w) teacher_top = __builtin_fmaxf(teacher_top, sums[w][0]);
-        counts = teacher_top != -__builtin_inff();  // else nothing is left of the row
-        float sum = 0.0f;
-        for (uint32_t j = tid_x(); j < top; j += kBlock) sum += token[j] >= 0 && counts ? expf(share[j] - teacher_top) : 0.0f;
-        sum = wave_sum(sum);
-        if (lane == 0) sums[wave][1] = sum;
-        __syncthreads();
-        teacher_sum = 0.0f;
-        for (int w = 0; w < kWavesPerBlock; ++w) teacher_sum += sums[w][1];
-        const float teacher_log = logf(teacher_sum);
-        for (uint32_t j = tid_x(); j < top; j += kBlock) {
-            const float v = share[j] - teacher_top;
-            const float q = token[j] >= 0 && counts ? expf(v) / teacher_sum : 0.0f;
-            if (q != 0.0f) negative_entropy += q * (v - teacher_log);
-            share[j] = q;
-        }
-        __syncthreads();
+        expected = wave_sum(expected);
     } else {
         const int64_t t = token_of(p.targets, row, 0);
         counts = t >= 0 && (uint64_t)t < p.vocab;
         if (t >= 0 && !counts && tid_x() == 0) atomicAdd(&p.err->n_bad_indices, 1ull);
-        // its logit, a part of the sum to each wave
-        if (counts) {
-            const float z = dot<kBlock>(reinterpret_cast<const T *>(p.hidden) + row * p.hidden_stride, reinterpret_cast<const T *>(p.weight) + (uint64_t)t * p.weight_stride, p.dim);
-            if (lane == 0) sums[wave][0] = z;
-        }
-        __syncthreads();
+        if (counts)
+            expected = dot<kBlock>(reinterpret_cast<const T *>(p.hidden) + row * p.hidden_stride, reinterpret_cast<const T *>(p.weight) + (uint64_t)t * p.weight_stride, p.dim);
     }
+    if (lane == 0) sums[wave] = expected;
+    __syncthreads();
+    if (tid_x() != 0) return;
+    expected = (sums[0] + sums[1]) + (sums[2] + sums[3]);
     s = joined[0];
+#pragma unroll
     for (int w = 1; w < kWavesPerBlock; ++w) s = join(s, joined[w]);
-    const float lse2 = s.top + __builtin_amdgcn_logf(s.sum);  // to base 2
-    float expected = 0.0f;  // sum of share * logit
-    if constexpr (SOFT) {
-        // Logits of the entries, an entry to a wave.
-        const T *x = reinterpret_cast<const T *>(p.hidden) + row * p.hidden_stride;
-        for (uint32_t j = wave; j < top; j += kWavesPerBlock) {
-            const int64_t t = token[j];
-            const float q = share[j];
-            float z = 0.0f;
-            if (t >= 0) z = dot<kWave>(x, reinterpret_cast<const T *>(p.weight) + (uint64_t)t * p.weight_stride, p.dim);
-            if (t >= 0 && q != 0.0f) expected = __builtin_fmaf(q, z, expected);
-            if (p.picked && lane == 0) p.picked[row * top + j] = z;
-        }
-    } else if (counts) {
-        expected = (sums[0][0] + sums[1][0]) + (sums[2][0] + sums[3][0]);
-    }
-    if constexpr (SOFT) {
-        // For the gradient the shares of a token that comes several times are at the first of them.
-        if (p.share) {
-            for (uint32_t j = tid_x(); j < top; j += kBlock) {
-                const int32_t t = token[j];
-                float all = 0.0f;
-                bool first = t >= 0;
-                for (uint32_t i = 0; i < top; ++i) {
-                    if (token[i] != t) continue;
-                    first = first && i >= j;
-                    all += share[i];
-                }
-                p.share[row * top + j] = first && counts ? all : 0.0f;
-            }
-        }
-        negative_entropy = wave_sum(negative_entropy);
-        __syncthreads();
-        if (lane == 0) {
-            sums[wave][0] = expected;
-            sums[wave][1] = negative_entropy;
-        }
-        __syncthreads();
-        expected = negative_entropy = 0.0f;
-        for (int w = 0; w < kWavesPerBlock; ++w) {
-            expected += sums[w][0];
-            negative_entropy += sums[w][1];
-        }
-    }
-    if (tid_x() == 0) {
-        // (the largest logit and the expected one are subtracted first: of a certain token little is left)
-        p.loss[row] = counts ? negative_entropy + ((s.top - expected * c) + __builtin_amdgcn_logf(s.sum)) * kLn2 : 0.0f;
-        if (p.lse2) p.lse2[row] = counts ? lse2 : __builtin_inff();
-    }
+    const float log_sum = __builtin_amdgcn_logf(s.sum);  // to base 2
+    // (the largest logit and the expected one are subtracted first: of a certain token little is left)
+    p.loss[row] = counts ? (SOFT ? p.loss[row] : 0.0f) + ((s.top - expected * p.c) + log_sum) * kLn2 : 0.0f;
+    if (p.lse2) p.lse2[row] = counts ? s.top + log_sum : __builtin_inff();
 }
 
 // ---- backward: rows and entries ---------------------------------------------------------------------------------
@@ -683,21 +926,19 @@ __global__ void __launch_bounds__(kRowThreads) rows_kernel(const float *lse2, co
 
 // dz of the entries whose tokens lie in [first, first + columns): a thread for each entry.
 template <int TYPE, int PARTS>
-__global__ void __launch_bounds__(kBlock) entries_kernel(const KeepGradient<TYPE, PARTS> k, const TargetArgs targets, const float *picked, const float *share, uint64_t n, uint32_t top,
-                                                         uint64_t first, uint32_t columns) {
+__global__ void __launch_bounds__(kBlock) entries_kernel(const KeepGradient<TYPE, PARTS> k, const Entries entries, uint64_t n, uint32_t columns) {
     typedef typename Element<TYPE>::type T;
     const uint64_t at = (uint64_t)wg_x() * kBlock + tid_x();
-    if (at >= n * top) return;
-    const float q = share[at];
-    const uint64_t row = at / top;
+    if (at >= n * entries.top) return;
+    const float q = entries.share[at];
+    const uint64_t row = at / entries.top;
     const RowGradient r = k.rows[row];
-    if (q == 0.0f || r.gradient == 0.0f) return;
-    const int64_t t = token_of(targets, row, (uint32_t)(at % top));
-    if (t < (int64_t)first || t >= (int64_t)(first + columns)) return;
+    const uint32_t column = (uint32_t)entries.tokens[at] - k.first;
+    if (q == 0.0f || r.gradient == 0.0f || column >= columns) return;
     T part[PARTS];
-    apart<TYPE, PARTS>(r.gradient * (exp2_of(__builtin_fmaf(picked[at], k.c, -r.lse2)) - q), part);
+    apart<TYPE, PARTS>(r.gradient * (exp2_of(__builtin_fmaf(entries.picked[at], k.c, -r.lse2)) - q), part);
 #pragma unroll
-    for (int i = 0; i < PARTS; ++i) k.dz[row * k.stride + i * k.width + ((uint64_t)t - first)] = part[i];
+    for (int i = 0; i < PARTS; ++i) k.dz[row * k.stride + i * k.width + column] = part[i];
 }
 
 // Zeros: what a sum over nothing is.
@@ -711,7 +952,12 @@ __global__ void __launch_bounds__(kBlock) zero_kernel(const Target out, uint64_t
 // ---- the host's side ------------------------------------------------------------------------------------------
 
 constexpr uint64_t kMaxRows = 1u << 20, kMaxVocabulary = 1u << 27, kMaxDim = 1u << 20;
-constexpr uint32_t kNarrowRows = 16;            // up to which the weight goes straight from memory to the matrix instructions
+// Up to how many rows the weight goes straight from memory into the products.  With more its rows are better shared through LDS, even where they have to be laid
+// out first: 64 x 54656 x 6026 at an odd stride 608 us by four times as many rows to a workgroup, 534 laid out.
+constexpr uint32_t kNarrowRows = 16;
+// (In the backward pass of larger weights that need not be laid out tiles are faster even then: a step of 16 x 32000 x 1024 85 -> 76 us, of 16 x 131072 x 4096
+// 1300 -> 955, but of 16 x 1249 x 6784 66 against 74.)
+constexpr uint64_t kTiledFrom = 1ull << 24;
 constexpr uint64_t kPieceBytes = 256ull << 20;  // of a piece of the weight, of its dz twice as many
 constexpr uint64_t kStatsBytes = 512ull << 20;  // of the stats of as many rows as go at a time
 constexpr uint64_t kPartBytes = 128ull << 20;   // of sums that are split
@@ -720,7 +966,7 @@ uint64_t rounded(uint64_t v, uint64_t to) { return cnr_ceil_div(v, to) * to; }
 
 // Whether a product can read rows of dim elements where they are.
 bool whole_rows(const cnr_float_type type, const void *base, uint64_t stride, uint64_t dim, uint64_t rows) {
-    return type != CNR_FLOAT_F32 && dim && dim % dense::kBlockElements == 0 && cnr_aligned(base, 16) && (rows <= 1 || (stride % 8 == 0 && stride < 1u << 22));
+    return type != CNR_FLOAT_F32 && dim && dim % 8 == 0 && cnr_aligned(base, 16) && (rows <= 1 || (stride % 8 == 0 && stride < 1u << 22));
 }
 
 // Places in a workspace, in order.
@@ -751,29 +997,38 @@ struct Terms {
 };
 constexpr Terms kOne = {1, 0, 0}, kOfFloats = {6, 0x001012, 0x010210}, kOfTwoParts = {2, 0, 0x01};
 
+// Of a row: its stats, and where the entries of each tile begin.
+uint64_t part_bytes(uint64_t n_parts) { return n_parts * sizeof(Stats) + (n_parts + 1) * sizeof(uint16_t); }
+
 struct ForwardPlan {
     bool narrow;
     uint32_t fragments;    // columns of a narrow workgroup, in sixteens
     uint64_t rows, piece;  // at a time
     uint32_t n_parts;      // of a row
     dense::Plan tiles;
-    uint64_t parts, hidden, weight, bytes;  // in the workspace
+    uint64_t parts, begins, hidden, weight, bytes;  // in the workspace
 };
+uint32_t narrow_fragments(uint64_t n, uint64_t vocab) {
+    // Two fragments of the weight to a wave where that still gives every SIMD a wave.
+    return n > 1 && vocab >= 16384 ? 2 : 1;
+}
 ForwardPlan forward_plan(const cnr_ctx *ctx, const Sizes &s) {
     ForwardPlan f = {};
+    f.rows = s.n;
+    if (s.vocab == 0) return f;
     f.narrow = s.n <= kNarrowRows;
-    // Two fragments of the weight to a wave where that still gives every SIMD a wave.
-    f.fragments = s.n > 1 && s.vocab >= 16384 ? 2 : 1;
+    f.fragments = narrow_fragments(s.n, s.vocab);
     f.tiles = dense::plan_of(ctx, s.vocab, s.n, (uint64_t)s.blocks * (s.parts == 3 ? kOfFloats.number : 1), 0.5f /* time for exponentials */, 0);
     const uint32_t columns = f.narrow ? 16 * f.fragments : dense::kTiles[f.tiles.kind].columns;
     f.n_parts = (uint32_t)cnr_ceil_div(s.vocab, columns);
-    const uint64_t per_row = (uint64_t)f.n_parts * sizeof(Stats), most = kStatsBytes / (per_row + 1) / 256 * 256;
+    const uint64_t per_row = part_bytes(f.n_parts), most = kStatsBytes / (per_row + 1) / 256 * 256;
     f.rows = most < 256 ? 256 : most;
     if (f.rows > s.n) f.rows = s.n;
     f.piece = rounded(kPieceBytes / s.row, 256);
     if (f.piece > s.vocab) f.piece = s.vocab;
     Room room;
-    f.parts = room.take(f.rows * per_row);
+    f.parts = room.take(f.rows * f.n_parts * sizeof(Stats));
+    f.begins = room.take(f.rows * (f.n_parts + 1) * sizeof(uint16_t));
     if (!f.narrow) {
         f.hidden = room.take(f.rows * s.row);
         f.weight = room.take(f.piece * s.row);
@@ -784,6 +1039,7 @@ ForwardPlan forward_plan(const cnr_ctx *ctx, const Sizes &s) {
 
 uint32_t dz_parts(const Sizes &s, bool two) { return s.parts == 3 ? 3 : two ? 2 : 1; }
 struct BackwardPlan {
+    bool narrow;
     uint64_t piece, width;  // of the vocabulary; columns of dz, whole blocks
     uint64_t scale, rows, dz, hidden_at, weight_at, sum, partial, bytes;
 };
@@ -791,6 +1047,16 @@ struct BackwardPlan {
 BackwardPlan backward_plan(const cnr_ctx *ctx, const Sizes &s, bool two, bool in_place) {
     BackwardPlan b = {};
     const uint32_t parts = dz_parts(s, two);
+    b.narrow = s.n <= kNarrowRows && !(in_place && s.vocab * s.dim >= kTiledFrom);
+    if (b.narrow) {
+        Room room;
+        b.scale = room.take(2 * sizeof(float));
+        b.rows = room.take(256 * sizeof(RowGradient));
+        b.dz = room.take(s.vocab * 16 * sizeof(float));
+        b.partial = room.take(kPartBytes);
+        b.bytes = room.used;
+        return b;
+    }
     uint64_t piece = 2 * kPieceBytes / (s.n * 2 * parts);
     const uint64_t by_weight = kPieceBytes / s.row;
     if (!in_place && piece > by_weight) piece = by_weight;
@@ -817,10 +1083,10 @@ uint64_t least(uint64_t a, uint64_t b) { return a < b ? a : b; }
 uint64_t room_for(const Sizes &s, bool training, bool two) {
     const uint64_t most_weight = least(s.vocab, rounded(kPieceBytes / s.row, 256)), small = least(s.n, 256);
     Room f;
-    const uint64_t stats = cnr_ceil_div(s.vocab, 64) * sizeof(Stats), narrow = least(s.n, kNarrowRows) * cnr_ceil_div(s.vocab, 16) * sizeof(Stats);
+    const uint64_t stats = part_bytes(cnr_ceil_div(s.vocab, 64)), narrow = least(s.n, kNarrowRows) * part_bytes(cnr_ceil_div(s.vocab, 16));
     uint64_t parts = least(s.n * stats, kStatsBytes);
     parts = parts > small * stats ? parts : small * stats;
-    f.take(parts > narrow ? parts : narrow);
+    f.take((parts > narrow ? parts : narrow) + 256);
     if (s.n > kNarrowRows) {
         f.take(s.n * s.row);
         f.take(most_weight * s.row);
@@ -830,7 +1096,9 @@ uint64_t room_for(const Sizes &s, bool training, bool two) {
     const uint64_t of_dz = s.n * 2 * dz_parts(s, two);
     b.take(2 * sizeof(float));
     b.take(rounded(s.n, 256) * sizeof(RowGradient));
-    b.take(least(of_dz * rounded(s.vocab, dense::kBlockElements), 2 * kPieceBytes + 256 * of_dz));
+    const uint64_t tiled = least(of_dz * rounded(s.vocab, dense::kBlockElements), 2 * kPieceBytes + 256 * of_dz);
+    const uint64_t narrow_dz = s.vocab * 16 * sizeof(float);
+    b.take(tiled > narrow_dz ? tiled : narrow_dz);
     b.take(s.n * s.row);
     b.take(most_weight * s.row);
     b.take(s.n * s.dim * sizeof(float));
@@ -842,8 +1110,8 @@ uint64_t room_for(const Sizes &s, bool training, bool two) {
 dense::Operand operand_of(const Sizes &s, const void *src, uint64_t stride, uint64_t rows, bool in_place, void *space, Layout &layout) {
     const uint32_t part = s.blocks * dense::kBlockBytes;
     layout = {src, stride, in_place ? 0 : rows, nullptr, nullptr, reinterpret_cast<u32x4 *>(space)};
-    if (in_place) return {src, stride * 2, part, 0, 0};
-    return {space, s.row, (uint32_t)s.row, part, 0};
+    if (in_place) return {src, stride * 2, (uint32_t)s.dim * 2, 0, 0, (uint32_t)((s.dim - 1) % dense::kBlockElements / 8 + 1)};
+    return {space, s.row, (uint32_t)s.row, part, 0, 8};
 }
 template <typename T>
 void lay_out(const Sizes &s, const Layout &a, const Layout &b, hipStream_t to) {
@@ -869,14 +1137,30 @@ TargetArgs targets_of(const cnr_targets &t) {
     return a;
 }
 
+// Where a state holds a teacher's entries, behind a number for each row.
+Entries entries_of(const float *state, uint64_t n, uint64_t top) {
+    float *at = const_cast<float *>(state ? state + n : nullptr);
+    return {reinterpret_cast<int32_t *>(at), at + n * top, at + 2 * n * top, (uint32_t)top};
+}
+
 // The type of the elements that products of a type are made of.
 template <int TYPE>
 constexpr int kOf = TYPE == CNR_FLOAT_F16 ? CNR_FLOAT_F16 : CNR_FLOAT_BF16;
+
+template <int TYPE, bool GRADIENT>
+void narrow(const NarrowArgs &a, uint32_t fragments, hipStream_t to) {
+    const dim3 grid((unsigned)cnr_ceil_div(a.vocab, 16 * fragments)), threads(kBlock);
+    if (fragments == 2)
+        hipLaunchKernelGGL((narrow_kernel<TYPE, 2, 2, GRADIENT>), grid, threads, 0, to, a);
+    else
+        hipLaunchKernelGGL((narrow_kernel<TYPE, 1, 4, GRADIENT>), grid, threads, 0, to, a);
+}
 
 template <int TYPE>
 void forward(cnr_ctx *ctx, const cnr_vocabulary &v, const cnr_targets &t, float *loss, float *state, void *workspace, hipStream_t to) {
     typedef typename Element<TYPE>::type T;
     const Sizes s = sizes_of(v.n, v.vocab, v.dim, v.type);
+    const bool in_place = whole_rows(v.type, v.weight, v.weight_stride, v.dim, v.vocab);
     const ForwardPlan f = forward_plan(ctx, s);
     uint8_t *space = reinterpret_cast<uint8_t *>(workspace);
     const T *hidden = reinterpret_cast<const T *>(v.hidden), *weight = reinterpret_cast<const T *>(v.weight);
@@ -892,28 +1176,27 @@ void forward(cnr_ctx *ctx, const cnr_vocabulary &v, const cnr_targets &t, float 
     l.n_parts = f.n_parts;
     l.loss = loss;
     l.lse2 = state;
-    l.picked = state ? state + v.n : nullptr;
-    l.share = state ? state + v.n * (1 + t.top) : nullptr;
+    l.entries = entries_of(state, v.n, t.top);
     l.err = ctx->dev_err;
-    const float c = kLog2e / l.targets.temperature;
+    const float c = l.c = kLog2e / l.targets.temperature;
+    TeacherArgs teacher = {l.targets, v.vocab, 0, l.entries, loss, state, f.narrow || !v.vocab ? nullptr : reinterpret_cast<uint16_t *>(space + f.begins), f.n_parts,
+                           dense::kTiles[f.tiles.kind].columns, ctx->dev_err};
     for (uint64_t row0 = 0; row0 < v.n; row0 += f.rows) {
         const uint64_t rows = v.n - row0 < f.rows ? v.n - row0 : f.rows;
         Stats *parts = reinterpret_cast<Stats *>(space + f.parts);
         const T *x = hidden + row0 * v.hidden_stride;
+        teacher.row0 = row0;
+        if (t.logits) hipLaunchKernelGGL(teacher_kernel, dim3((unsigned)rows), dim3(kBlock), 0, to, teacher);
         if (f.n_parts == 0) {
         } else if (f.narrow) {
-            NarrowArgs a = {x, weight, v.hidden_stride, v.weight_stride, (uint32_t)rows, (uint32_t)v.vocab, (uint32_t)v.dim, parts, f.n_parts, c};
-            const dim3 grid(f.n_parts, (unsigned)cnr_ceil_div(rows, 16));
-            if (f.fragments == 2)
-                hipLaunchKernelGGL((narrow_kernel<TYPE, 2, 2>), grid, dim3(kBlock), 0, to, a);
-            else
-                hipLaunchKernelGGL((narrow_kernel<TYPE, 1, 4>), grid, dim3(kBlock), 0, to, a);
+            const NarrowArgs a = {x, weight, v.hidden_stride, v.weight_stride, (uint32_t)rows, (uint32_t)v.vocab, (uint32_t)v.dim, c, parts, f.n_parts, nullptr, nullptr};
+            narrow<TYPE, false>(a, f.fragments, to);
+            if (t.logits && t.top) hipLaunchKernelGGL((pick_kernel<TYPE>), dim3((unsigned)cnr_ceil_div(rows * t.top, kWavesPerBlock)), dim3(kBlock), 0, to, l, rows);
         } else {
             const Terms terms = s.parts == 3 ? kOfFloats : kOne;
             Layout of_x, of_w;
             const dense::Operand x_at = in_terms(operand_of(s, x, v.hidden_stride, rows, whole_rows(v.type, x, v.hidden_stride, v.dim, rows), space + f.hidden, of_x), terms.down);
             const uint32_t columns = dense::kTiles[f.tiles.kind].columns;
-            const bool in_place = whole_rows(v.type, weight, v.weight_stride, v.dim, v.vocab);
             const uint64_t most = in_place ? rounded((1ull << 22) / cnr_ceil_div(rows, 64) * 64, 256) : f.piece;
             for (uint64_t v0 = 0; v0 < v.vocab; v0 += most) {
                 const uint64_t width = v.vocab - v0 < most ? v.vocab - v0 : most;
@@ -921,7 +1204,13 @@ void forward(cnr_ctx *ctx, const cnr_vocabulary &v, const cnr_targets &t, float 
                 lay_out<T>(s, of_w, of_x, to);
                 of_x.rows = 0;
                 const dense::Args args = {w_at, x_at, (uint32_t)width, (uint32_t)rows, s.blocks, 0, terms.number, 1};
-                dense::launch<kOf<TYPE>, false, false>(args, f.tiles.kind, KeepStats{parts + v0 / columns, f.n_parts, c}, to);
+                Entries entries = l.entries;
+                entries.tokens += row0 * t.top;
+                entries.picked += row0 * t.top;
+                if (t.logits)
+                    dense::launch<kOf<TYPE>, false, false>(args, f.tiles.kind, KeepStats<true>{parts + v0 / columns, f.n_parts, c, teacher.begins + v0 / columns, entries, (uint32_t)v0}, to);
+                else
+                    dense::launch<kOf<TYPE>, false, false>(args, f.tiles.kind, KeepStats<false>{parts + v0 / columns, f.n_parts, c, nullptr, entries, 0}, to);
             }
         }
         l.row0 = row0;
@@ -938,7 +1227,7 @@ void product(const dense::Args &args, const dense::Plan &plan, const KeepSum &k,
     a.splits = plan.splits;
     dense::launch<kOf<TYPE>, true, DOWN>(a, plan.kind, k, to);
     if (a.splits > 1)
-        hipLaunchKernelGGL(join_sums_kernel, dim3((unsigned)cnr_ceil_div((uint64_t)a.rows * (k.partial_stride / 4), kBlock)), dim3(kBlock), 0, to, k, a.rows, a.columns, a.splits);
+        hipLaunchKernelGGL((join_sums_kernel<1>), dim3((unsigned)cnr_ceil_div((uint64_t)a.rows * (k.partial_stride / 4), kBlock)), dim3(kBlock), 0, to, k, a.rows, a.columns, a.splits);
 }
 Target from_row(Target t, uint64_t row) {
     if (t.out) t.out = reinterpret_cast<uint8_t *>(t.out) + row * t.stride * cnr_float_bytes((cnr_float_type)t.type);
@@ -962,21 +1251,68 @@ void product(cnr_ctx *ctx, const dense::Args &args, const KeepSum &k, hipStream_
     product<TYPE, DOWN>(a, plans.rest, rest, to);
 }
 
+// The backward pass of few rows.
+template <int TYPE>
+void narrow_backward(cnr_ctx *ctx, const cnr_vocabulary &v, const cnr_targets &t, const float *state, const float *dloss, const Target &dhidden, const Target &dweight, bool accumulate,
+                     const BackwardPlan &b, uint8_t *space, hipStream_t to) {
+    const TargetArgs targets = targets_of(t);
+    RowGradient *rows = reinterpret_cast<RowGradient *>(space + b.rows);
+    hipLaunchKernelGGL(rows_kernel, dim3(1), dim3(kRowThreads), 0, to, state, dloss, v.n, targets, v.vocab, 0, rows, reinterpret_cast<float *>(space + b.scale));
+    const uint32_t n = (uint32_t)v.n, vocab = (uint32_t)v.vocab, dim = (uint32_t)v.dim;
+    float *dz = reinterpret_cast<float *>(space + b.dz);
+    const NarrowArgs a = {v.hidden, v.weight, v.hidden_stride, v.weight_stride, n, vocab, dim, kLog2e / targets.temperature, nullptr, 0, rows, dz};
+    narrow<TYPE, true>(a, narrow_fragments(v.n, v.vocab), to);
+    if (t.logits && t.top)
+        hipLaunchKernelGGL(narrow_entries_kernel, dim3((unsigned)cnr_ceil_div(v.n * t.top, kBlock)), dim3(kBlock), 0, to, a, entries_of(state, v.n, t.top));
+    // Sixteen waves to a compute unit, slabs of 64 tokens at least, parts of sums of up to a quarter of the room for them (they are read again).
+    SlabArgs s = {};
+    s.dz = dz;
+    s.vocab = vocab;
+    s.dim = dim;
+    s.n = n;
+    s.groups = (uint32_t)cnr_ceil_div(v.dim, 64);
+    const uint64_t stride = rounded(v.dim, 4), wanted = least(cnr_ceil_div(16ull * ctx->n_cu, s.groups), cnr_ceil_div(v.vocab, 64));
+    const uint64_t by_room = kPartBytes / 4 / (v.n * stride * sizeof(float));
+    if (dhidden.out) {
+        s.slabs = (uint32_t)least(wanted, by_room ? by_room : 1);
+        s.matrix = v.weight;
+        s.stride = v.weight_stride;
+        s.partial = reinterpret_cast<float *>(space + b.partial);
+        s.partial_stride = stride;
+        hipLaunchKernelGGL((narrow_hidden_kernel<TYPE>), dim3((unsigned)cnr_ceil_div((uint64_t)s.groups * s.slabs, kWavesPerBlock)), dim3(kBlock), 0, to, s);
+        const KeepSum sum = {dhidden, {nullptr, 0, CNR_FLOAT_F32}, nullptr, s.partial, stride};
+        hipLaunchKernelGGL((join_sums_kernel<16>), dim3((unsigned)cnr_ceil_div(v.n * (stride / 4), kBlock / 16)), dim3(kBlock), 0, to, sum, n, dim, s.slabs);
+    }
+    if (dweight.out) {
+        s.slabs = (uint32_t)wanted;
+        s.matrix = v.hidden;
+        s.stride = v.hidden_stride;
+        s.lse2 = state;
+        s.dloss = dloss;
+        s.out = dweight;
+        s.there = accumulate ? dweight : Target{nullptr, 0, CNR_FLOAT_F32};
+        hipLaunchKernelGGL((narrow_weight_kernel<TYPE>), dim3((unsigned)cnr_ceil_div((uint64_t)s.groups * s.slabs, kWavesPerBlock)), dim3(kBlock), 0, to, s);
+    }
+}
+
 template <int TYPE, int PARTS>
 void backward(cnr_ctx *ctx, const cnr_vocabulary &v, const cnr_targets &t, const float *state, const float *dloss, void *dhidden, uint64_t dhidden_stride, void *dweight,
               cnr_float_type dweight_type, uint64_t dweight_stride, bool accumulate, void *workspace, hipStream_t to) {
     typedef typename Element<TYPE>::type T;
     typedef typename Element<kOf<TYPE>>::type Part;
     const Sizes s = sizes_of(v.n, v.vocab, v.dim, v.type);
-    const BackwardPlan b = backward_plan(ctx, s, PARTS == 2, whole_rows(v.type, v.weight, v.weight_stride, v.dim, v.vocab));
+    const bool in_place = whole_rows(v.type, v.weight, v.weight_stride, v.dim, v.vocab);
+    const BackwardPlan b = backward_plan(ctx, s, PARTS == 2, in_place);
     uint8_t *space = reinterpret_cast<uint8_t *>(workspace);
+    if (b.narrow)
+        return narrow_backward<TYPE>(ctx, v, t, state, dloss, {dhidden, dhidden_stride, v.type}, {dweight, dweight_stride, dweight_type}, accumulate, b, space, to);
     const T *weight = reinterpret_cast<const T *>(v.weight);
     const TargetArgs targets = targets_of(t);
+    const Entries entries = entries_of(state, v.n, t.top);
     RowGradient *rows = reinterpret_cast<RowGradient *>(space + b.rows);
     float *scale = reinterpret_cast<float *>(space + b.scale);
     hipLaunchKernelGGL(rows_kernel, dim3((unsigned)least(cnr_ceil_div(v.n, kRowThreads), kRowGroups)), dim3(kRowThreads), 0, to, state, dloss, v.n, targets, v.vocab, TYPE == CNR_FLOAT_F16,
                        rows, scale);
-    const bool in_place = whole_rows(v.type, v.weight, v.weight_stride, v.dim, v.vocab);
     Layout of_x, of_w;
     const dense::Operand x = operand_of(s, v.hidden, v.hidden_stride, v.n, false, space + b.hidden_at, of_x);
     of_x.lse2 = state;
@@ -1002,10 +1338,9 @@ void backward(cnr_ctx *ctx, const cnr_vocabulary &v, const cnr_targets &t, const
         of_x.rows = 0;
         const dense::Plan tiles = dense::plan_of(ctx, width, v.n, s.blocks * logits.number, 2.0f * PARTS, 0);
         dense::launch<kOf<TYPE>, false, false>(dense::Args{in_terms(w, logits.across), in_terms(x, logits.down), width, n, s.blocks, 0, logits.number, 1}, tiles.kind, k, to);
-        if (t.logits)
-            hipLaunchKernelGGL((entries_kernel<kOf<TYPE>, PARTS>), dim3((unsigned)cnr_ceil_div(v.n * t.top, kBlock)), dim3(kBlock), 0, to, k, targets, state + v.n,
-                               state + v.n * (1 + t.top), v.n, (uint32_t)t.top, v0, width);
-        const dense::Operand dz = {k.dz, k.stride * 2, (uint32_t)(k.stride * 2), (uint32_t)(k.width * 2), 0};
+        if (t.logits && t.top)
+            hipLaunchKernelGGL((entries_kernel<kOf<TYPE>, PARTS>), dim3((unsigned)cnr_ceil_div(v.n * t.top, kBlock)), dim3(kBlock), 0, to, k, entries, v.n, width);
+        const dense::Operand dz = {k.dz, k.stride * 2, (uint32_t)(k.stride * 2), (uint32_t)(k.width * 2), 0, 8};
         if (dhidden) {
             sum.there = v0 == 0 ? none : between;
             sum.out = v0 + width == v.vocab ? Target{dhidden, dhidden_stride, v.type} : between;
@@ -1041,7 +1376,7 @@ cnr_status checked(const cnr_vocabulary *v, const cnr_targets *t) {
 
 extern "C" {
 
-size_t cnr_loss_state_floats(uint64_t n, uint64_t top) { return n > kMaxRows || top > kMaxTop ? 0 : (size_t)(n * (1 + 2 * top)); }
+size_t cnr_loss_state_floats(uint64_t n, uint64_t top) { return n > kMaxRows || top > kMaxTop ? 0 : (size_t)(n * (1 + 3 * top)); }
 
 size_t cnr_loss_workspace_bytes(uint64_t n, uint64_t vocab, uint64_t dim, cnr_float_type type, int training, cnr_float_type dweight_type) {
     if (n == 0 || vocab == 0 || n > kMaxRows || vocab > kMaxVocabulary || dim > kMaxDim || !cnr_valid_float_type(type)) return 0;
@@ -1055,6 +1390,7 @@ cnr_status cnr_vocabulary_loss(cnr_ctx *ctx, const cnr_vocabulary *vocabulary, c
     if (st != CNR_OK) return st;
     const cnr_vocabulary &v = *vocabulary;
     if (v.n == 0) return CNR_OK;
+    if (targets->logits && !state) return CNR_E_INVALID;
     if (!loss || workspace_bytes < cnr_loss_workspace_bytes(v.n, v.vocab, v.dim, v.type, 0, v.type) || (workspace_bytes && !workspace)) return CNR_E_INVALID;
     if (!cnr_aligned(loss, 4) || !cnr_aligned(state, 4) || !cnr_aligned(workspace, 256)) return CNR_E_ALIGN;
     if (forward_plan(ctx, sizes_of(v.n, v.vocab, v.dim, v.type)).bytes > workspace_bytes) return CNR_E_INVALID;

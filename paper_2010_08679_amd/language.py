@@ -251,9 +251,10 @@ class VocabularyLoss(_Holder):
             raise ValueError("1 to %d entries a row" % S.CNR_LOSS_MAX_TOP)
         space = S.cnr_loss_workspace_bytes(self.max_tokens, self.vocab, self.dim, L._FLOATS[dtype], training, L._FLOATS[self.gradient_dtype])
         self._space = torch.empty(space, dtype=torch.uint8, device=self.device)
-        self._state = torch.empty(self.max_tokens * (1 + 2 * self.top), dtype=torch.float32, device=self.device) if training else None
+        self._state = torch.empty(S.cnr_loss_state_floats(self.max_tokens, self.top), dtype=torch.float32, device=self.device)
+        self.training = bool(training)
         self._last = None
-        self._holds([t for t in (self._space, self._state) if t is not None])
+        self._holds((self._space, self._state))
 
     def _loss(self, hidden, weight, tokens, logits, temperature, out, training, stream):
         if hidden.dim() != 2 or hidden.shape[1] != self.dim or tuple(weight.shape) != (self.vocab, self.dim):
@@ -262,15 +263,16 @@ class VocabularyLoss(_Holder):
             raise TypeError("hidden must be %s, got %s" % (self.dtype, hidden.dtype))
         if hidden.shape[0] > self.max_tokens:
             raise ValueError("%d tokens, made for %d" % (hidden.shape[0], self.max_tokens))
-        if training and self._state is None:
+        if training and not self.training:
             raise ValueError("made without training")
         self._use(stream)
         if out is None:
             with _on(stream):
                 out = torch.empty(hidden.shape[0], dtype=torch.float32, device=hidden.device)
-        if training:
+        if training or logits is not None:  # the state is another's from here on
             self._last = None
-        S.cnr_vocabulary_loss(self.ctx, hidden, weight, tokens, logits, temperature, out, self._state if training else None, self._space, stream)
+        S.cnr_vocabulary_loss(self.ctx, hidden, weight, tokens, logits, temperature, out, self._state if training or logits is not None else None, self._space,
+                              stream)
         if training:
             self._last = (hidden, weight, tokens, logits, temperature)
         return out

@@ -96,14 +96,16 @@ def _bytes(t) -> int:
 
 
 def cnr_vocabulary_loss(ctx, hidden, weight, tokens, logits, temperature: float, loss, state, workspace, stream=None) -> None:
-    """``tokens``: a list of targets with ``logits`` None, else a matrix as ``logits`` is; ``state`` and ``workspace`` may be None where nothing is kept or needed."""
+    """``tokens``: a list of targets with ``logits`` None, else a matrix as ``logits`` is; ``state`` may be None for targets that no backward pass follows."""
     v, t = _loss_arguments(hidden, weight, tokens, logits, temperature)
     n, top = v.n, t.top
     if top > CNR_LOSS_MAX_TOP:
         raise ValueError("at most %d entries a row" % CNR_LOSS_MAX_TOP)
     if loss is None or loss.numel() < n:
         raise ValueError("loss shorter than %d" % n)
-    if state is not None and state.numel() < n * (1 + 2 * top):
+    if state is None and logits is not None:
+        raise ValueError("a teacher's entries need a state")
+    if state is not None and state.numel() < n * (1 + 3 * top):
         raise ValueError("state shorter than cnr_loss_state_floats")
     if _bytes(workspace) < cnr_loss_workspace_bytes(n, v.vocab, v.dim, v.type, False, v.type):
         raise ValueError("workspace smaller than cnr_loss_workspace_bytes")
@@ -119,7 +121,7 @@ def cnr_vocabulary_loss_backward(ctx, hidden, weight, tokens, logits, temperatur
     n, top = v.n, t.top
     if top > CNR_LOSS_MAX_TOP:
         raise ValueError("at most %d entries a row" % CNR_LOSS_MAX_TOP)
-    if state is None or state.numel() < n * (1 + 2 * top):
+    if state is None or state.numel() < n * (1 + 3 * top):
         raise ValueError("state missing or shorter than cnr_loss_state_floats")
     if dloss is None or dloss.numel() < n:
         raise ValueError("dloss shorter than %d" % n)

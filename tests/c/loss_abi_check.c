@@ -16,7 +16,7 @@ int main(void) {
     memset(&v, 0, sizeof v);
     memset(&t, 0, sizeof t);
     t.top = t.token_stride = 1;
-    if (cnr_loss_state_floats(10, 3) != 70 || cnr_loss_state_floats(0, 1) != 0) return 11;
+    if (cnr_loss_state_floats(10, 3) != 100 || cnr_loss_state_floats(0, 1) != 0) return 11;
     if (cnr_loss_workspace_bytes(0, 10, 10, CNR_FLOAT_F32, 1, CNR_FLOAT_F32) != 0) return 12;
     if (cnr_vocabulary_loss(NULL, &v, &t, NULL, NULL, NULL, 0, NULL) != CNR_E_INVALID) return 13;
     if (cnr_vocabulary_loss_backward(NULL, &v, &t, NULL, NULL, NULL, 0, NULL, CNR_FLOAT_F32, 0, 0, NULL, 0, NULL) != CNR_E_INVALID) return 14;

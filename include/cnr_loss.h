@@ -48,7 +48,10 @@ typedef struct {
     float temperature;
 } cnr_targets;
 
-#define CNR_LOSS_MAX_TOP 1024u
+#define CNR_LOSS_MAX_TOP 1024u             /* entries of a row: CNR_E_TOO_LARGE beyond, as of the others */
+#define CNR_LOSS_MAX_ROWS 1048576u
+#define CNR_LOSS_MAX_VOCABULARY 134217728u
+#define CNR_LOSS_MAX_DIM 1048576u
 
 /* loss[i], float [n], with lse = log sum over v of exp(z[i][v] / T):
  *   target t         lse - z[i][t]                                             (T is 1)
@@ -58,8 +61,7 @@ typedef struct {
  *   state        float [cnr_loss_state_floats(n, top)], kept for the backward pass; may be NULL for targets that no backward pass follows
  *   workspace    cnr_loss_workspace_bytes(n, vocab, dim, type, 0, type) bytes at least (which serve fewer rows as well), 256-byte aligned,
  *                contents irrelevant; where vocab is 0, NULL
- * Nothing depends on other work on the GPU, sums are joined in order.
- * CNR_E_TOO_LARGE beyond 2^20 rows, 2^27 tokens, 2^20 columns and CNR_LOSS_MAX_TOP entries. */
+ * Nothing depends on other work on the GPU, sums are joined in order. */
 size_t cnr_loss_state_floats(uint64_t n, uint64_t top);
 size_t cnr_loss_workspace_bytes(uint64_t n, uint64_t vocab, uint64_t dim, cnr_float_type type, int training, cnr_float_type dweight_type);
 cnr_status cnr_vocabulary_loss(cnr_ctx *ctx, const cnr_vocabulary *vocabulary /* host */, const cnr_targets *targets /* host */, float *loss, float *state,
@@ -69,9 +71,10 @@ cnr_status cnr_vocabulary_loss(cnr_ctx *ctx, const cnr_vocabulary *vocabulary /*
  *   dz[i][v] = dloss[i] / T * (exp(z[i][v] / T - lse) - sum of the q_j with tokens[j] = v)
  *   dhidden  NULL, or [n][dim] of `type`: dz weight
  *   dweight  NULL, or [vocab][dim] of dweight_type, `type` or float: dz^T hidden, added to what is there where accumulate is not 0
- * Logits are computed again, a piece of the vocabulary at a time.  dz passes through `type` between the products; for a float dweight of 16-bit operands through
- * two numbers of it (relative 2^-16 for bfloat16, 2^-22 for half).  Halves are scaled by the power of two that takes the largest |dloss / T| to 2^13 to
- * 2^14, so that small gradients are not lost.  Each result is rounded once, after its sum in fp32.  A row with dloss 0 adds nothing, whatever it holds.
+ * Logits are computed again, a piece of the vocabulary at a time.  dz passes through `type` between the products, rounded to it once; through two numbers of it
+ * (relative 2^-16 for bfloat16, 2^-22 for half) where n is at most 64 or dweight is float, through three bfloat16 for floats.  Halves are scaled by
+ * the power of two that takes the largest |dloss / T| to 2^13 to 2^14, so that small gradients are not lost.  Each result is rounded once, after its sum in
+ * fp32.  A row with dloss 0 adds nothing, whatever it holds.
  *   workspace    cnr_loss_workspace_bytes(n, vocab, dim, type, 1, dweight_type) bytes at least (dweight_type: `type` where dweight is NULL) */
 cnr_status cnr_vocabulary_loss_backward(cnr_ctx *ctx, const cnr_vocabulary *vocabulary /* host */, const cnr_targets *targets /* host */, const float *state,
                                         const float *dloss, void *dhidden, uint64_t dhidden_stride, void *dweight, cnr_float_type dweight_type,
@@ -82,7 +85,7 @@ cnr_status cnr_vocabulary_loss_backward(cnr_ctx *ctx, const cnr_vocabulary *voca
  *   tokens   int32 [n][top], or NULL; -1 beyond the vocabulary's size
  *   values   of `type` [n][top], or NULL: the logits of these tokens; -infinity beyond the vocabulary's size
  *   lse      float [n], or NULL: log sum over v of exp(logits[i][v]), summed in fp32; a value minus it is the token's log probability
- * CNR_E_TOO_LARGE from CNR_LOSS_MAX_TOP + 1 on. */
+ * CNR_E_TOO_LARGE beyond CNR_LOSS_MAX_TOP and from n = 2^22 on. */
 cnr_status cnr_top_logits(cnr_ctx *ctx, const void *logits, uint64_t stride, cnr_float_type type, uint64_t n, uint64_t vocab, uint64_t top, int32_t *tokens,
                           void *values, float *lse, void *stream);
 

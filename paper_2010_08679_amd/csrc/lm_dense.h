@@ -3,7 +3,7 @@
 // Elements have 16 bits and go through the matrix instructions of their type: exact products, added up in fp32.  Each operand lies either along k (a row or
 // column of the output in a row of its own, in whole pieces of eight elements) or across it ([k][row or column], read through the LDS's transposing
 // loads; columns in whole pieces of eight).  An operand may be held in several parts, side by side in its rows, that add up to it (a float in three bfloat16): the sum then goes over
-// pairs of parts ("terms") one after the other.
+// pairs of parts ("terms") of each block.
 #pragma once
 
 #include "lm_common.h"
@@ -244,7 +244,7 @@ __global__ void __launch_bounds__(WM * WN * kWave, 2) tile_kernel(const Args p, 
     typename std::conditional<DOWN, Across<NF, TN, LB>, Along<NF, TN, LB>>::type b(p.down, row0, p.rows, p.k, wave, wave_n, kB);
     const uint32_t lds_at = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) uint8_t *)lds;
     // The block to be fetched next; behind the last one it stays there, and nobody reads what arrives: the count of loads stays the same without a branch.
-    uint32_t ahead = begin, block = begin % p.blocks, term = begin / p.blocks;
+    uint32_t ahead = begin, block = begin / p.terms, term = begin % p.terms;
     auto end_of_rows = [&]() {
         if (block + 1 == p.blocks) {
             a.end();
@@ -262,9 +262,9 @@ __global__ void __launch_bounds__(WM * WN * kWave, 2) tile_kernel(const Args p, 
     auto go_on = [&]() {
         if (ahead + 1 < end) {
             ++ahead;
-            const bool over = block + 1 == p.blocks;
-            block = over ? 0 : block + 1;
-            term += over ? 1 : 0;
+            const bool over = term + 1 == p.terms;
+            term = over ? 0 : term + 1;
+            block += over ? 1 : 0;
             end_of_rows();
         }
     };

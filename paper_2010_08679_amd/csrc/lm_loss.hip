@@ -951,10 +951,13 @@ __global__ void __launch_bounds__(kBlock) zero_kernel(const Target out, uint64_t
 
 // ---- the host's side ------------------------------------------------------------------------------------------
 
-constexpr uint64_t kMaxRows = 1u << 20, kMaxVocabulary = 1u << 27, kMaxDim = 1u << 20;
+constexpr uint64_t kMaxRows = CNR_LOSS_MAX_ROWS, kMaxVocabulary = CNR_LOSS_MAX_VOCABULARY, kMaxDim = CNR_LOSS_MAX_DIM;
 // Up to how many rows the weight goes straight from memory into the products.  With more its rows are better shared through LDS, even where they have to be laid
 // out first: 64 x 54656 x 6026 at an odd stride 608 us by four times as many rows to a workgroup, 534 laid out.
 constexpr uint32_t kNarrowRows = 16;
+// Up to how many rows of 16 bits dz is held in two parts, whatever the results' type: products that are bound by reading the weight and by writing its gradient
+// nearly have the time (a step of 32 x 131072 x 4096 941 -> 1013 us), and sums of few rows do not average roundings.
+constexpr uint32_t kTwoPartRows = 64;
 // (In the backward pass of larger weights that need not be laid out tiles are faster even then: a step of 16 x 32000 x 1024 85 -> 76 us, of 16 x 131072 x 4096
 // 1300 -> 955, but of 16 x 1249 x 6784 66 against 74.)
 constexpr uint64_t kTiledFrom = 1ull << 24;
@@ -991,7 +994,7 @@ Sizes sizes_of(uint64_t n, uint64_t vocab, uint64_t dim, cnr_float_type type) {
     s.row = (uint64_t)s.parts * s.blocks * dense::kBlockBytes;
     return s;
 }
-// Pairs of parts, the smallest products first.
+// Pairs of parts, the smallest products of a block first.
 struct Terms {
     uint32_t number, across, down;
 };
@@ -1037,7 +1040,7 @@ ForwardPlan forward_plan(const cnr_ctx *ctx, const Sizes &s) {
     return f;
 }
 
-uint32_t dz_parts(const Sizes &s, bool two) { return s.parts == 3 ? 3 : two ? 2 : 1; }
+uint32_t dz_parts(const Sizes &s, bool two) { return s.parts == 3 ? 3 : two || s.n <= kTwoPartRows ? 2 : 1; }
 struct BackwardPlan {
     bool narrow;
     uint64_t piece, width;  // of the vocabulary; columns of dz, whole blocks
@@ -1096,7 +1099,9 @@ uint64_t room_for(const Sizes &s, bool training, bool two) {
     const uint64_t of_dz = s.n * 2 * dz_parts(s, two);
     b.take(2 * sizeof(float));
     b.take(rounded(s.n, 256) * sizeof(RowGradient));
-    const uint64_t tiled = least(of_dz * rounded(s.vocab, dense::kBlockElements), 2 * kPieceBytes + 256 * of_dz);
+    const uint64_t few = least(s.n, kTwoPartRows) * 2 * (s.parts == 3 ? 3 : 2), vocab = rounded(s.vocab, dense::kBlockElements);
+    uint64_t tiled = least(of_dz * vocab, 2 * kPieceBytes + 256 * of_dz);
+    tiled = tiled > least(few * vocab, 2 * kPieceBytes + 256 * few) ? tiled : least(few * vocab, 2 * kPieceBytes + 256 * few);
     const uint64_t narrow_dz = s.vocab * 16 * sizeof(float);
     b.take(tiled > narrow_dz ? tiled : narrow_dz);
     b.take(s.n * s.row);
@@ -1326,7 +1331,8 @@ void backward(cnr_ctx *ctx, const cnr_vocabulary &v, const cnr_targets &t, const
     sum.partial = reinterpret_cast<float *>(space + b.partial);
     sum.partial_stride = rounded(v.dim, 4);
     const Target between = {space + b.sum, v.dim, CNR_FLOAT_F32}, none = {nullptr, 0, CNR_FLOAT_F32};
-    const Terms logits = PARTS == 3 ? kOfFloats : kOne, to_hidden = logits, to_weight = PARTS == 3 ? kOfFloats : PARTS == 2 ? kOfTwoParts : kOne;
+    // (two parts for the hidden states too where rows are few)
+    const Terms logits = PARTS == 3 ? kOfFloats : kOne, to_hidden = PARTS == 2 && v.n <= kTwoPartRows ? kOfTwoParts : logits, to_weight = PARTS == 3 ? kOfFloats : PARTS == 2 ? kOfTwoParts : kOne;
     const uint32_t n = (uint32_t)v.n, dim = (uint32_t)v.dim;
     for (uint64_t v0 = 0; v0 < v.vocab; v0 += b.piece) {
         const uint32_t width = (uint32_t)(v.vocab - v0 < b.piece ? v.vocab - v0 : b.piece), blocks = (uint32_t)cnr_ceil_div(width, dense::kBlockElements);
@@ -1429,7 +1435,7 @@ cnr_status cnr_vocabulary_loss_backward(cnr_ctx *ctx, const cnr_vocabulary *voca
         if (dweight && !accumulate) zeros({dweight, dweight_stride, dweight_type}, v.vocab, v.dim, to);
         return cnr_launch_status(ctx);
     }
-    const bool low = dweight && dweight_type == CNR_FLOAT_F32;
+    const bool low = (dweight && dweight_type == CNR_FLOAT_F32) || v.n <= kTwoPartRows;
     if (backward_plan(ctx, sizes_of(v.n, v.vocab, v.dim, v.type), low && v.type != CNR_FLOAT_F32, whole_rows(v.type, v.weight, v.weight_stride, v.dim, v.vocab)).bytes > workspace_bytes)
         return CNR_E_INVALID;
     auto call = [&](auto kind, auto part) {

@@ -249,6 +249,9 @@ class VocabularyLoss(_Holder):
             raise TypeError("losses of float32, bfloat16 or float16, gradients of the weight in that type or float32")
         if not 1 <= self.top <= S.CNR_LOSS_MAX_TOP:
             raise ValueError("1 to %d entries a row" % S.CNR_LOSS_MAX_TOP)
+        for size, most, name in ((self.max_tokens, S.CNR_LOSS_MAX_ROWS, "max_tokens"), (self.vocab, S.CNR_LOSS_MAX_VOCABULARY, "vocab"), (self.dim, S.CNR_LOSS_MAX_DIM, "dim")):
+            if not 0 <= size <= most:
+                raise ValueError("%s must be 0 to %d" % (name, most))
         space = S.cnr_loss_workspace_bytes(self.max_tokens, self.vocab, self.dim, L._FLOATS[dtype], training, L._FLOATS[self.gradient_dtype])
         self._space = torch.empty(space, dtype=torch.uint8, device=self.device)
         self._state = torch.empty(S.cnr_loss_state_floats(self.max_tokens, self.top), dtype=torch.float32, device=self.device)

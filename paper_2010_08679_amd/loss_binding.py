@@ -11,12 +11,12 @@ from . import binding as B
 from . import lm_binding as L
 from .binding import U32, F32, _check, _stream
 
-CNR_LOSS_MAX_TOP = 1024
+CNR_LOSS_MAX_TOP, CNR_LOSS_MAX_ROWS, CNR_LOSS_MAX_VOCABULARY, CNR_LOSS_MAX_DIM = 1024, 1048576, 134217728, 1048576
 
 # Every symbol include/cnr_loss.h declares.
 LOSS_EXPORTS = ("cnr_loss_state_floats", "cnr_loss_workspace_bytes", "cnr_vocabulary_loss", "cnr_vocabulary_loss_backward", "cnr_top_logits")
 
-__all__ = [*LOSS_EXPORTS, "cnr_vocabulary", "cnr_targets", "LOSS_EXPORTS", "CNR_LOSS_MAX_TOP"]
+__all__ = [*LOSS_EXPORTS, "cnr_vocabulary", "cnr_targets", "LOSS_EXPORTS", "CNR_LOSS_MAX_TOP", "CNR_LOSS_MAX_ROWS", "CNR_LOSS_MAX_VOCABULARY", "CNR_LOSS_MAX_DIM"]
 
 
 class cnr_vocabulary(ctypes.Structure):

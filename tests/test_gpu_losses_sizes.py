@@ -135,6 +135,54 @@ def test_top_logits_by_few_and_many_threads(ctx, n, vocab, top, kind):
     assert bool(((lse.double() - want[2]).abs() <= (vocab / 256 * 8 + 300) * 2.0 ** -24 * (1 + want[2].abs()))[finite].all()) and torch.equal(lse.isfinite(), finite)
 
 
+@pytest.mark.parametrize("kind", list(TYPES))
+@pytest.mark.parametrize("n,dim,pad", [(7, 72, 8), (7, 71, 9), (100, 72, 8), (100, 200, 56), (100, 71, 9), (100, 8, 8)])
+def test_what_lies_between_rows_is_not_read_for_a_result(ctx, kind, n, dim, pad):
+    """Rows that end within a block of the products, with NaN behind them; before and behind the matrices too."""
+    t, vocab = TYPES[kind], 1500
+    g = torch.Generator(device=DEV).manual_seed(4)
+
+    def held(rows, sigma):
+        whole = torch.full((rows + 2, dim + pad), math.nan, dtype=t, device=DEV)
+        whole[1:-1, :dim] = torch.empty(rows, dim, device=DEV).normal_(0.0, sigma, generator=g).to(t)
+        return whole, whole[1:-1, :dim]
+
+    (_, x), (_, w) = held(n, 2.0), held(vocab, 0.2)
+    targets = torch.randint(0, vocab, (n,), generator=g, device=DEV)
+    dloss = torch.empty(n, device=DEV).uniform_(0.5, 1.0, generator=g)
+    want = R.loss(x, w, targets, dloss=dloss)
+    loss = P.VocabularyLoss(ctx, vocab, dim, n, t)
+    _near(loss.cross_entropy(x, w, targets), want["losses"], "losses")
+    (all_x, dx), (all_w, dw) = held(n, 1.0), held(vocab, 1.0)
+    loss.backward(dloss, dx, dw)
+    _near(dx, want["dhidden"], "dhidden")
+    _near(dw, want["dweight"], "dweight")
+    for whole in (all_x, all_w):
+        assert bool(whole[0].isnan().all()) and bool(whole[-1].isnan().all()) and bool(whole[:, dim:].isnan().all())
+
+
+@pytest.mark.parametrize("kind", list(TYPES))
+@pytest.mark.parametrize("n", [5, 40])
+def test_tokens_whose_logits_are_minus_infinity(ctx, kind, n):
+    """A bias of -infinity as a column of the weight takes tokens out: no probability, a loss of infinity where one is the target."""
+    t, vocab, dim = TYPES[kind], 700, 40
+    g = torch.Generator(device=DEV).manual_seed(6)
+    x, w = _rows(g, n, dim, t, 2.0), _rows(g, vocab, dim, t, 0.2)
+    x[:, -1] = 1.0
+    w[:, -1] = 0.0
+    gone = torch.arange(vocab, device=DEV) % 3 == 1
+    w[gone, -1] = -math.inf
+    targets = torch.randint(0, vocab // 3, (n,), generator=g, device=DEV) * 3
+    targets[3] = 4
+    got = P.VocabularyLoss(ctx, vocab, dim, n, t).cross_entropy(x, w, targets)
+    assert float(got[3]) == math.inf
+    kept = (~gone).nonzero()[:, 0]
+    where = torch.searchsorted(kept, targets)
+    rest = targets != 4
+    want = R.loss(x[rest], w[kept], where[rest])["losses"]
+    _near(got[rest], want, "losses")
+
+
 # ---- fewer rows than it was made for, streams, graphs ------------------------------------------------------------------
 
 def test_one_object_serves_all_numbers_of_rows(ctx):

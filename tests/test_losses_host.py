@@ -31,7 +31,8 @@ def test_binding_names_everything_that_the_header_declares():
     with open(os.path.join(ROOT, "include", "cnr_loss.h")) as f:
         header = re.sub(r"/\*.*?\*/", "", f.read(), flags=re.S)
     assert set(re.findall(r"\b(cnr_[a-z_]+)\(", header)) == set(S.LOSS_EXPORTS)
-    assert int(re.search(r"#define CNR_LOSS_MAX_TOP (\d+)u", header).group(1)) == P.CNR_LOSS_MAX_TOP
+    limits = dict(re.findall(r"#define (CNR_LOSS_MAX_[A-Z]+) (\d+)u", header))
+    assert len(limits) == 4 and all(getattr(P, name) == int(value) for name, value in limits.items())
 
 
 @pytest.mark.parametrize("struct", [P.cnr_vocabulary, P.cnr_targets])
@@ -84,7 +85,7 @@ BOTH = [
 
 
 @pytest.mark.parametrize("name,status,changed", [(name, *b) for name in ("cnr_vocabulary_loss", "cnr_vocabulary_loss_backward") for b in BOTH] + [
-    ("cnr_vocabulary_loss", INVALID, dict(loss=None)), ("cnr_vocabulary_loss", ALIGN, dict(loss=A + 1)), ("cnr_vocabulary_loss", OK, dict(n=0, hidden=None, tokens=None)),
+    ("cnr_vocabulary_loss", INVALID, TEACHER | dict(state=None)), ("cnr_vocabulary_loss", INVALID, dict(loss=None)), ("cnr_vocabulary_loss", ALIGN, dict(loss=A + 1)), ("cnr_vocabulary_loss", OK, dict(n=0, hidden=None, tokens=None)),
     ("cnr_vocabulary_loss_backward", INVALID, dict(state=None)), ("cnr_vocabulary_loss_backward", INVALID, dict(dloss=None)),
     ("cnr_vocabulary_loss_backward", INVALID, dict(dhidden_stride=63)), ("cnr_vocabulary_loss_backward", INVALID, dict(dweight_stride=63)),
     ("cnr_vocabulary_loss_backward", INVALID, dict(dweight_type=F16)), ("cnr_vocabulary_loss_backward", INVALID, dict(dweight_type=BF16, type=F32, dhidden_stride=64)),
@@ -137,6 +138,9 @@ def test_binding_refuses_host_tensors_wrong_types_and_sizes():
     for top in (0, 1025):
         with pytest.raises(ValueError):
             P.VocabularyLoss(None, 10, 8, 4, top=top, device="cpu")
+    for sizes in ((11, 8, (1 << 20) + 1), ((1 << 27) + 1, 8, 4), (10, (1 << 20) + 1, 4), (-1, 8, 4)):
+        with pytest.raises(ValueError):
+            P.VocabularyLoss(None, *sizes, device="cpu")
     with pytest.raises(TypeError):
         P.top_logits(None, x, 2)
     loss._last = (x, w, t, None, 1.0)

@@ -942,11 +942,10 @@ __global__ void __launch_bounds__(kBlock) entries_kernel(const KeepGradient<TYPE
 }
 
 // Zeros: what a sum over nothing is.
+constexpr uint32_t kZeroGroups = 8192;
 __global__ void __launch_bounds__(kBlock) zero_kernel(const Target out, uint64_t rows, uint32_t columns) {
-    const uint64_t at = (uint64_t)wg_x() * kBlock + tid_x();
-    if (at >= rows * columns) return;
     const float none[1] = {0.0f};
-    write_row(out, at / columns, (uint32_t)(at % columns), columns, none);
+    for (uint64_t at = (uint64_t)wg_x() * kBlock + tid_x(); at < rows * columns; at += (uint64_t)kZeroGroups * kBlock) write_row(out, at / columns, (uint32_t)(at % columns), columns, none);
 }
 
 // ---- the host's side ------------------------------------------------------------------------------------------
@@ -962,10 +961,12 @@ constexpr uint32_t kTwoPartRows = 64;
 // 1300 -> 955, but of 16 x 1249 x 6784 66 against 74.)
 constexpr uint64_t kTiledFrom = 1ull << 24;
 constexpr uint64_t kPieceBytes = 256ull << 20;  // of a piece of the weight, of its dz twice as many
+constexpr uint64_t kPieceTokens = 1ull << 20;   // a row of its dz, in up to three parts, is below 2^23 bytes
 constexpr uint64_t kStatsBytes = 512ull << 20;  // of the stats of as many rows as go at a time
 constexpr uint64_t kPartBytes = 128ull << 20;   // of sums that are split
 
 uint64_t rounded(uint64_t v, uint64_t to) { return cnr_ceil_div(v, to) * to; }
+uint64_t least(uint64_t a, uint64_t b) { return a < b ? a : b; }
 
 // Whether a product can read rows of dim elements where they are.
 bool whole_rows(const cnr_float_type type, const void *base, uint64_t stride, uint64_t dim, uint64_t rows) {
@@ -1063,7 +1064,7 @@ BackwardPlan backward_plan(const cnr_ctx *ctx, const Sizes &s, bool two, bool in
     uint64_t piece = 2 * kPieceBytes / (s.n * 2 * parts);
     const uint64_t by_weight = kPieceBytes / s.row;
     if (!in_place && piece > by_weight) piece = by_weight;
-    piece = rounded(piece ? piece : 1, 256);
+    piece = rounded(least(piece ? piece : 1, kPieceTokens), 256);
     // pieces of one size
     const uint64_t pieces = cnr_ceil_div(s.vocab, piece);
     b.piece = rounded(cnr_ceil_div(s.vocab, pieces), 256);
@@ -1081,7 +1082,6 @@ BackwardPlan backward_plan(const cnr_ctx *ctx, const Sizes &s, bool two, bool in
     return b;
 }
 
-uint64_t least(uint64_t a, uint64_t b) { return a < b ? a : b; }
 // At least what the plans take for n rows or fewer: each part's largest size.
 uint64_t room_for(const Sizes &s, bool training, bool two) {
     const uint64_t most_weight = least(s.vocab, rounded(kPieceBytes / s.row, 256)), small = least(s.n, 256);
@@ -1115,7 +1115,7 @@ uint64_t room_for(const Sizes &s, bool training, bool two) {
 dense::Operand operand_of(const Sizes &s, const void *src, uint64_t stride, uint64_t rows, bool in_place, void *space, Layout &layout) {
     const uint32_t part = s.blocks * dense::kBlockBytes;
     layout = {src, stride, in_place ? 0 : rows, nullptr, nullptr, reinterpret_cast<u32x4 *>(space)};
-    if (in_place) return {src, stride * 2, (uint32_t)s.dim * 2, 0, 0, (uint32_t)((s.dim - 1) % dense::kBlockElements / 8 + 1)};
+    if (in_place) return {src, (rows > 1 ? stride : s.dim) * 2, (uint32_t)s.dim * 2, 0, 0, (uint32_t)((s.dim - 1) % dense::kBlockElements / 8 + 1)};
     return {space, s.row, (uint32_t)s.row, part, 0, 8};
 }
 template <typename T>
@@ -1362,7 +1362,7 @@ void backward(cnr_ctx *ctx, const cnr_vocabulary &v, const cnr_targets &t, const
 }
 
 void zeros(const Target &out, uint64_t rows, uint64_t columns, hipStream_t to) {
-    if (rows && columns) hipLaunchKernelGGL(zero_kernel, dim3((unsigned)cnr_ceil_div(rows * columns, kBlock)), dim3(kBlock), 0, to, out, rows, (uint32_t)columns);
+    if (rows && columns) hipLaunchKernelGGL(zero_kernel, dim3(kZeroGroups), dim3(kBlock), 0, to, out, rows, (uint32_t)columns);
 }
 
 cnr_status checked(const cnr_vocabulary *v, const cnr_targets *t) {

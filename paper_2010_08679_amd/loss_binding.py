@@ -91,6 +91,11 @@ def _loss_arguments(hidden, weight, tokens, logits, temperature: float):
             cnr_targets(tokens_at, token_type, token_stride, top, logits_at, logit_type, logit_stride, temperature))
 
 
+def _span(t):
+    """First byte and the one behind the last of a matrix."""
+    return t.data_ptr(), t.data_ptr() + ((t.shape[0] - 1) * t.stride(0) + t.shape[1]) * t.element_size()
+
+
 def _bytes(t) -> int:
     return 0 if t is None else t.numel() * t.element_size()
 
@@ -134,6 +139,10 @@ def cnr_vocabulary_loss_backward(ctx, hidden, weight, tokens, logits, temperatur
         to_weight, kind = L._rows(dweight, "dweight"), L._float(dweight, "dweight")
         if dweight.shape != weight.shape or kind not in (v.type, L.CNR_FLOAT_F32):
             raise ValueError("dweight must have the shape of weight and its type, or float32")
+    spans = [_span(t) for t in (dhidden, dweight, hidden, weight) if t is not None and t.numel()]
+    results = (dhidden is not None and dhidden.numel() > 0) + (dweight is not None and dweight.numel() > 0)
+    if any(a[0] < b[1] and b[0] < a[1] for i, a in enumerate(spans[:results]) for b in spans[i + 1:]):
+        raise ValueError("a result overlaps an operand or the other result")
     if _bytes(workspace) < cnr_loss_workspace_bytes(n, v.vocab, v.dim, v.type, True, kind):
         raise ValueError("workspace smaller than cnr_loss_workspace_bytes")
     _check((_lib or load()).cnr_vocabulary_loss_backward(

@@ -280,6 +280,32 @@ def test_a_graph_replayed_gives_what_eager_calls_give(ctx, kind, n, dim):
                 assert torch.equal(r, v)
 
 
+def test_results_that_overlap_are_refused(ctx):
+    x, w, targets, dloss = _case(20, 300, 64, torch.float32)
+    loss = P.VocabularyLoss(ctx, 300, 64, 20, torch.float32)
+    loss.cross_entropy(x, w, targets)
+    both = torch.zeros(320, 64, device=DEV)
+    for kw in (dict(dhidden=x), dict(dweight=w), dict(dhidden=w[5:25]), dict(dhidden=both[290:310], dweight=both[:300])):
+        with pytest.raises(ValueError, match="overlaps"):
+            loss.backward(dloss, **kw)
+    dx, dw = loss.backward(dloss, both[300:], both[:300])  # side by side is in order
+    want = R.loss(x, w, targets, dloss=dloss)
+    _near(dx, want["dhidden"], "dhidden")
+    _near(dw, want["dweight"], "dweight")
+
+
+def test_a_vocabulary_of_more_tokens_than_a_piece(ctx):
+    n, vocab, dim = 20, (1 << 20) + 700, 8
+    x, w, targets, dloss = _case(n, vocab, dim, torch.bfloat16)
+    targets[0], targets[1] = vocab - 1, 1 << 20
+    want = R.loss(x, w, targets, dloss=dloss, parts=2)
+    loss = P.VocabularyLoss(ctx, vocab, dim, n, gradient_dtype=torch.float32)
+    _near(loss.cross_entropy(x, w, targets), want["losses"], "losses")
+    dx, dw = loss.backward(dloss)
+    _near(dx, want["dhidden"], "dhidden")
+    _near(dw, want["dweight"], "dweight")
+
+
 def test_what_is_written_has_a_new_version(ctx):
     x, w, targets, dloss = _case(20, 300, 64, torch.float32)
     loss = P.VocabularyLoss(ctx, 300, 64, 20, torch.float32)

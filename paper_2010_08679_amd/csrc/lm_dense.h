@@ -215,6 +215,10 @@ struct Across {
 // A block's products go by quarters, each half of the wave's columns with each half of its rows, so that half of the operands are in registers while
 // the other half, or the next block's first, are on their way from LDS; loads go between matrix instructions.  The last quarter needs nothing more
 // from this stage: before it all waves meet, in it the stage is filled again.
+//
+// Bound by the matrix units: 4096 x 131072 x 4096 in bfloat16, both operands along k, 3.18 ms, 1.38 PFLOP/s (on the same card the installed library's plain product
+// of 8192^3 1.14); one or both across k 1.29 to 1.32 (16384 x 16384 x 4096 1.67 to 1.70 ms).  Transposing copies in memory instead took 40 us more for each
+// 134 MB, and dz in both directions.
 template <int TYPE, bool ACROSS, bool DOWN, int WM, int WN, int MF, int NF, int STAGES, typename Epilogue>
 __global__ void __launch_bounds__(WM * WN * kWave, 2) tile_kernel(const Args p, const Epilogue epilogue) {
     constexpr uint32_t TM = WM * 16 * MF, TN = WN * 16 * NF;

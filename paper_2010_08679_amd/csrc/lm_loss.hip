@@ -130,7 +130,8 @@ struct KeepStats {
         if constexpr (PICK) pick<TM, TN>(p, at, acc);
     }
     // The tile goes into LDS, as many rows at a time as there is room for, and each entry looks its logit up: what it costs does not depend on where the entries
-    // are.  Pieces of four columns are permuted by the row, so that rows that are written together take different banks.
+    // are (8192 x 32000 x 4096 with 64 entries a row 1640 -> 1680 us; as dot products of rows from memory they took 680).  Pieces of four columns are permuted by the
+    // row, so that rows that are written together take different banks.
     template <uint32_t TM, uint32_t TN, typename Place, int MF, int NF>
     __device__ __forceinline__ void pick(const dense::Args &p, const Place &at, const f32x4 (&acc)[MF][NF]) const {
         constexpr uint32_t kRoom = Place::kLdsBytes / (TM * 4), kRows = kRoom < TN ? kRoom : TN, kEach = Place::kThreads / kRows;
@@ -186,7 +187,8 @@ __device__ __forceinline__ void apart(float v, typename Element<TYPE>::type (&pa
     }
 }
 
-// dz of the tile's rows and columns, with zeros up to the next whole block of columns, in PARTS parts side by side.
+// dz of the tile's rows and columns, with zeros up to the next whole block of columns, in PARTS parts side by side.  Its stores are not hidden: 8192 x 25344 x 2048
+// 759 us, with the stats alone 675.
 template <int TYPE, int PARTS>
 struct KeepGradient {
     static constexpr bool kUsesLds = false;
@@ -395,7 +397,7 @@ struct Layout {
     const float *lse2, *dloss;  // NULL: every row counts
     u32x4 *dst;
 };
-// Two matrices (either may have no rows), 16 bytes of each part to a thread.
+// Two matrices (either may have no rows), 16 bytes of each part to a thread.  Bound by memory: 34000 rows of 1024 floats 56 us, 6.2 TB/s.
 template <typename T>
 __global__ void __launch_bounds__(kBlock) lay_out_kernel(const Layout a, const Layout b, uint32_t dim, uint32_t pieces /* of a part */) {
     constexpr int kParts = sizeof(T) == 4 ? 3 : 1;
@@ -566,7 +568,8 @@ struct SlabArgs {
     const float *lse2, *dloss; // which hidden states count
     Target out, there;
 };
-// partial[slab][i][column] = sum over the slab's tokens of dz[v][i] * weight[v][column].
+// partial[slab][i][column] = sum over the slab's tokens of dz[v][i] * weight[v][column].  13 x 213243 x 1536 in fp32 254 us, 5.2 TB/s (by the ordinary units,
+// dz as scalars, 850 for 16 x 131072 x 4096 in bfloat16, 444 so).
 template <int TYPE>
 __global__ void __launch_bounds__(kBlock) narrow_hidden_kernel(const SlabArgs p) {
     typedef typename Element<TYPE>::type T;
@@ -601,7 +604,7 @@ __global__ void __launch_bounds__(kBlock) narrow_hidden_kernel(const SlabArgs p)
         if (4 * quarter + i < p.n) write_as(p.partial + ((uint64_t)slab * p.n + 4 * quarter + i) * p.partial_stride + column, column, p.dim, v);
     }
 }
-// out[v][column] = there + sum over i of dz[v][i] * hidden[i][column].
+// out[v][column] = there + sum over i of dz[v][i] * hidden[i][column].  13 x 213243 x 1536 onto an fp32 gradient 650 us, 4.0 TB/s read and written.
 template <int TYPE>
 __global__ void __launch_bounds__(kBlock) narrow_weight_kernel(const SlabArgs p) {
     typedef typename Element<TYPE>::type T;
@@ -699,7 +702,7 @@ __device__ __forceinline__ float sum_of_block(float v, float (&parts)[kWavesPerB
 }
 
 // A row's teacher: the shares of its entries, sorted; loss[row] = sum of share * log(share), lse2[row] = 0, or infinity where the row is left out;
-// begins (NULL: not wanted) for tiles of `columns`.  A workgroup to a row.
+// begins (NULL: not wanted) for tiles of `columns`.  A workgroup to a row; each entry counts those before it: 8192 rows of 64 30 us.
 struct TeacherArgs {
     TargetArgs targets;
     uint64_t vocab, row0;

@@ -5,6 +5,9 @@
 // are wanted: the vectors whose largest does are read again, all at once, and their elements that reach it are collected in LDS, in any order; each finds
 // its place by counting those before it.  Keys (the value, then the lower token) are all different, so the order they were collected in does not matter.
 // Where too many reach the bound (equal values, or the largest all in one thread's share), it is raised digit by digit first.
+//
+// 64 of 8192 x 32000 bfloat16 101 us, 5.2 TB/s, of 512 x 131072 34 us, 3.9 TB/s (177 and 60 with rows held in registers, so that fewer of them share a compute unit; 312
+// and 70 read twice); 50 of 1 x 50257 floats 12 us, one workgroup's latency.
 #include "cnr_loss.h"
 #include "lm_common.h"
 
@@ -295,7 +298,8 @@ void launch(const TopArgs &a, uint64_t vectors, hipStream_t s) {
     else
         hipLaunchKernelGGL((top_kernel<TYPE, THREADS, 16, 0>), grid, threads, 0, s, a);
 }
-// The fewer threads have a row, the more rows share a compute unit and hide each other's steps that have little to do; few rows want many threads.  A bound
+// The fewer threads have a row, the more rows share a compute unit and hide each other's steps that have little to do; few rows want many threads (512 x 131072 by 512
+// threads 46.6 us, by 1024 34.4).  A bound
 // is of use where clearly more threads than are asked for have elements.
 template <int TYPE>
 void top_of(const TopArgs &a, const cnr_ctx *ctx, hipStream_t s) {

@@ -37,7 +37,7 @@ def test_its_gradients_are_the_definitions():
     q = R.shares(tokens.long(), E.VOCAB, logits, E.HEAT)
     soft = (q * (q.log() - torch.log_softmax(z / E.HEAT, dim=1).gather(1, tokens.long()))).sum(dim=1)
     hard = torch.nn.functional.cross_entropy(z, (7 * now + 3) % E.VOCAB, reduction="none")
-    assert abs(losses[0] - float((soft + hard).mean()) / 2) < 1e-5
+    assert abs(losses[0] - float((soft + hard).detach().mean()) / 2) < 1e-5
     dw, dt = torch.autograd.grad((0.5 * E.HEAT ** 2 * soft + 0.5 * hard).mean(), (w, t))
     # sums of up to 512 products in fp32, and the step's rounding of values of up to 2
     assert float((table - before + 4.0 * dw).abs().max()) < 1e-5 and float((turn - turned + 4.0 * dt).abs().max()) < 1e-5

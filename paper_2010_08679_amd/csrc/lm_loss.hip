@@ -435,7 +435,7 @@ __global__ void __launch_bounds__(kBlock) lay_out_kernel(const Layout a, const L
 
 // ---- few rows: operands straight from memory -------------------------------------------------------------------
 //
-// Logits: a workgroup has 16 MF rows by 16 NF columns; each of its waves takes a quarter of the sum, U blocks at a time so that enough loads are under way,
+// Logits: a workgroup has 16 G rows by 16 NF columns; each of its waves takes a quarter of the sum, U blocks at a time so that enough loads are under way,
 // straight into the matrix instructions' registers (floats into the fp32 ones); they add up their sums in LDS.  Bound by reading the weight: 1 x 32000 x
 // 4096 in bfloat16 43.7 us, 6.0 TB/s.
 //
@@ -449,7 +449,7 @@ struct NarrowArgs {
     Stats *parts;              // or, for the backward pass,
     uint32_t n_parts;
     const RowGradient *rows;
-    float *dz;                 // [vocab][16], zeros in rows from n on
+    float *dz;                 // [vocab][16 G], zeros in rows from n on
 };
 template <int TYPE>
 __device__ __forceinline__ f32x4 multiply(const dense::i32x8 &x, const dense::i32x8 &y, f32x4 sum) {
@@ -479,67 +479,83 @@ __device__ __forceinline__ dense::i32x8 load_fragment(const T *row, uint32_t at,
     }
     return __builtin_shufflevector(part[0], part[1], 0, 1, 2, 3, 4, 5, 6, 7);
 }
-template <int TYPE, int NF, int U, bool GRADIENT>
-__global__ void __launch_bounds__(kBlock, 4) narrow_kernel(const NarrowArgs p) {
+template <int TYPE, int G, int NF, int U, bool GRADIENT>
+__global__ void __launch_bounds__(kBlock, G > 2 ? 3 : 4) narrow_kernel(const NarrowArgs p) {
     typedef typename Element<TYPE>::type T;
     constexpr uint32_t kPer = 16 / sizeof(T), kColumns = dense::kBlockBytes / sizeof(T);
-    __shared__ f32x4 sums[kWavesPerBlock][NF][kWave];
+    __shared__ f32x4 sums[kWavesPerBlock][G * NF][kWave];
     const uint32_t lane = tid_x() % kWave, wave = (uint32_t)__builtin_amdgcn_readfirstlane((int)(tid_x() / kWave));
     const uint32_t quarter = lane / 16, n0 = wg_x() * 16 * NF;
     // Rows beyond the matrix read its last one again.
-    const T *a = reinterpret_cast<const T *>(p.hidden) + (lane % 16 < p.n ? lane % 16 : p.n - 1) * p.hidden_stride, *b[NF];
+    const T *a[G], *b[NF];
+#pragma unroll
+    for (int f = 0; f < G; ++f) {
+        const uint32_t row = 16 * f + lane % 16;
+        a[f] = reinterpret_cast<const T *>(p.hidden) + (row < p.n ? row : p.n - 1) * p.hidden_stride;
+    }
 #pragma unroll
     for (int g = 0; g < NF; ++g) {
         const uint32_t v = n0 + 16 * g + lane % 16;
         b[g] = reinterpret_cast<const T *>(p.weight) + (uint64_t)(v < p.vocab ? v : p.vocab - 1) * p.weight_stride;
     }
-    f32x4 acc[NF];
+    f32x4 acc[G][NF];
 #pragma unroll
-    for (int g = 0; g < NF; ++g) acc[g] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+    for (int f = 0; f < G; ++f)
+#pragma unroll
+        for (int g = 0; g < NF; ++g) acc[f][g] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
     const uint32_t blocks = (p.dim + kColumns - 1) / kColumns, each = (blocks + kWavesPerBlock - 1) / kWavesPerBlock, begin = wave * each;
     const uint32_t end = begin + each < blocks ? begin + each : blocks;
     for (uint32_t first = begin; first < end; first += U) {
-        dense::i32x8 x[U], y[U][NF];
+        dense::i32x8 x[U][G], y[U][NF];
 #pragma unroll
         for (int u = 0; u < U; ++u) {
             if (u && first + u >= end) break;
             const uint32_t at = (first + u) * kColumns + quarter * kPer;
 #pragma unroll
             for (int g = 0; g < NF; ++g) y[u][g] = load_fragment(b[g], at, p.dim);
-            x[u] = load_fragment(a, at, p.dim);
+#pragma unroll
+            for (int f = 0; f < G; ++f) x[u][f] = load_fragment(a[f], at, p.dim);
         }
 #pragma unroll
         for (int u = 0; u < U; ++u) {
             if (u && first + u >= end) break;
 #pragma unroll
-            for (int g = 0; g < NF; ++g) acc[g] = multiply<TYPE>(x[u], y[u][g], acc[g]);
+            for (int f = 0; f < G; ++f)
+#pragma unroll
+                for (int g = 0; g < NF; ++g) acc[f][g] = multiply<TYPE>(x[u][f], y[u][g], acc[f][g]);
         }
     }
 #pragma unroll
-    for (int g = 0; g < NF; ++g) sums[wave][g][lane] = acc[g];
+    for (int f = 0; f < G; ++f)
+#pragma unroll
+        for (int g = 0; g < NF; ++g) sums[wave][f * NF + g][lane] = acc[f][g];
     __syncthreads();
     // Sixteen threads to a row, each with one column of each sixteen.
     const uint32_t m = tid_x() / 16, n = tid_x() % 16;
-    float z[NF];
-    uint32_t valid = 0;
 #pragma unroll
-    for (uint32_t g = 0; g < NF; ++g) {
-        z[g] = 0.0f;
-#pragma unroll
-        for (int w = 0; w < kWavesPerBlock; ++w) z[g] += sums[w][g][m / 4 * 16 + n][m % 4];
-        valid |= n0 + 16 * g + n < p.vocab ? 1u << g : 0u;
-    }
-    if constexpr (GRADIENT) {
-        const RowGradient r = p.rows[m];  // (padded with rows that add nothing)
+    for (uint32_t f = 0; f < G; ++f) {
+        const uint32_t row = 16 * f + m;
+        float z[NF];
+        uint32_t valid = 0;
 #pragma unroll
         for (uint32_t g = 0; g < NF; ++g) {
-            const uint32_t v = n0 + 16 * g + n;
-            const float e = exp2_of(__builtin_fmaf(z[g], p.c, -r.lse2));
-            if (valid >> g & 1u) p.dz[(uint64_t)v * 16 + m] = r.gradient == 0.0f ? 0.0f : r.gradient * (v == r.target ? e - 1.0f : e);
+            z[g] = 0.0f;
+#pragma unroll
+            for (int w = 0; w < kWavesPerBlock; ++w) z[g] += sums[w][f * NF + g][m / 4 * 16 + n][m % 4];
+            valid |= n0 + 16 * g + n < p.vocab ? 1u << g : 0u;
         }
-    } else {
-        const Stats s = stats16(z, p.c, valid);
-        if (n == 0 && m < p.n) p.parts[(uint64_t)m * p.n_parts + wg_x()] = s;
+        if constexpr (GRADIENT) {
+            const RowGradient r = p.rows[row];  // (padded with rows that add nothing)
+#pragma unroll
+            for (uint32_t g = 0; g < NF; ++g) {
+                const uint32_t v = n0 + 16 * g + n;
+                const float e = exp2_of(__builtin_fmaf(z[g], p.c, -r.lse2));
+                if (valid >> g & 1u) p.dz[(uint64_t)v * (16 * G) + row] = r.gradient == 0.0f ? 0.0f : r.gradient * (v == r.target ? e - 1.0f : e);
+            }
+        } else {
+            const Stats s = stats16(z, p.c, valid);
+            if (n == 0 && row < p.n) p.parts[(uint64_t)row * p.n_parts + wg_x()] = s;
+        }
     }
 }
 
@@ -560,7 +576,7 @@ __device__ __forceinline__ f32x4 load_four(const T *row, uint32_t column, uint32
 struct SlabArgs {
     const void *matrix;        // the weight, or the hidden states
     uint64_t stride;
-    const float *dz;           // [vocab][16]
+    const float *dz;           // [vocab][16 G]
     uint32_t vocab, dim, n;
     uint32_t groups, slabs;    // of 64 columns, of the vocabulary: a wave has one of each
     float *partial;            // [slabs][n][partial_stride]
@@ -570,7 +586,7 @@ struct SlabArgs {
 };
 // partial[slab][i][column] = sum over the slab's tokens of dz[v][i] * weight[v][column].  13 x 213243 x 1536 in fp32 254 us, 5.2 TB/s (by the ordinary units,
 // dz as scalars, 850 for 16 x 131072 x 4096 in bfloat16, 444 so).
-template <int TYPE>
+template <int TYPE, int G>
 __global__ void __launch_bounds__(kBlock) narrow_hidden_kernel(const SlabArgs p) {
     typedef typename Element<TYPE>::type T;
     const uint32_t wave = wave_in_grid(), group = wave % p.groups, slab = wave / p.groups, lane = tid_x() % kWave, quarter = lane / 16, r = lane % 16;
@@ -578,34 +594,44 @@ __global__ void __launch_bounds__(kBlock) narrow_hidden_kernel(const SlabArgs p)
     const uint32_t column = group * 64 + r * 4;
     const uint32_t begin = (uint32_t)((uint64_t)p.vocab * slab / p.slabs), end = (uint32_t)((uint64_t)p.vocab * (slab + 1) / p.slabs);
     const T *matrix = reinterpret_cast<const T *>(p.matrix);
-    f32x4 acc[4];  // [column][row of dz]
+    f32x4 acc[G][4];  // [sixteen rows][column]
 #pragma unroll
-    for (int j = 0; j < 4; ++j) acc[j] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+    for (int g = 0; g < G; ++g)
+#pragma unroll
+        for (int j = 0; j < 4; ++j) acc[g][j] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
     constexpr uint32_t kAtOnce = 8;
     for (uint32_t v0 = begin; v0 < end; v0 += 4 * kAtOnce) {
         f32x4 w[kAtOnce];
-        float d[kAtOnce];
+        float d[kAtOnce][G];
 #pragma unroll
         for (uint32_t u = 0; u < kAtOnce; ++u) {
             const uint32_t v = v0 + 4 * u + quarter, at = v < end ? v : end - 1;
             w[u] = load_four(matrix + (uint64_t)at * p.stride, column, p.dim);
-            d[u] = p.dz[(uint64_t)at * 16 + r];
-            d[u] = v < end ? d[u] : 0.0f;
+#pragma unroll
+            for (uint32_t g = 0; g < G; ++g) {
+                d[u][g] = p.dz[(uint64_t)at * (16 * G) + 16 * g + r];
+                d[u][g] = v < end ? d[u][g] : 0.0f;
+            }
         }
 #pragma unroll
         for (uint32_t u = 0; u < kAtOnce; ++u)
 #pragma unroll
-            for (int j = 0; j < 4; ++j) acc[j] = __builtin_amdgcn_mfma_f32_16x16x4f32(d[u], w[u][j], acc[j], 0, 0, 0);
-    }
-    // sum i of a lane: row 4 quarter + i, column r of each of the four sixteens
+            for (int g = 0; g < G; ++g)
 #pragma unroll
-    for (uint32_t i = 0; i < 4; ++i) {
-        const float v[4] = {acc[0][i], acc[1][i], acc[2][i], acc[3][i]};
-        if (4 * quarter + i < p.n) write_as(p.partial + ((uint64_t)slab * p.n + 4 * quarter + i) * p.partial_stride + column, column, p.dim, v);
+                for (int j = 0; j < 4; ++j) acc[g][j] = __builtin_amdgcn_mfma_f32_16x16x4f32(d[u][g], w[u][j], acc[g][j], 0, 0, 0);
     }
+    // sum i of a lane: row 4 quarter + i of its sixteen, column r of each of the four sixteens
+#pragma unroll
+    for (uint32_t g = 0; g < G; ++g)
+#pragma unroll
+        for (uint32_t i = 0; i < 4; ++i) {
+            const float v[4] = {acc[g][0][i], acc[g][1][i], acc[g][2][i], acc[g][3][i]};
+            const uint32_t row = 16 * g + 4 * quarter + i;
+            if (row < p.n) write_as(p.partial + ((uint64_t)slab * p.n + row) * p.partial_stride + column, column, p.dim, v);
+        }
 }
 // out[v][column] = there + sum over i of dz[v][i] * hidden[i][column].  13 x 213243 x 1536 onto an fp32 gradient 650 us, 4.0 TB/s read and written.
-template <int TYPE>
+template <int TYPE, int G>
 __global__ void __launch_bounds__(kBlock) narrow_weight_kernel(const SlabArgs p) {
     typedef typename Element<TYPE>::type T;
     const uint32_t wave = wave_in_grid(), group = wave % p.groups, slab = wave / p.groups, lane = tid_x() % kWave, quarter = lane / 16, r = lane % 16;
@@ -613,10 +639,10 @@ __global__ void __launch_bounds__(kBlock) narrow_weight_kernel(const SlabArgs p)
     const uint32_t begin = (uint32_t)((uint64_t)p.vocab * slab / p.slabs), end = (uint32_t)((uint64_t)p.vocab * (slab + 1) / p.slabs);
     const T *matrix = reinterpret_cast<const T *>(p.matrix);
     // Sixteen columns f are 32 (f / 2) + 8 (r / 4) + 4 (f % 2) + r % 4: a lane has eight outputs side by side, and the four lanes of a token 32.
-    float x[4][4];  // [f][row of hidden states 4 quarter + s]
+    float x[4][4 * G];  // [f][row of hidden states 16 (s / 4) + 4 quarter + s % 4]
 #pragma unroll
-    for (uint32_t s = 0; s < 4; ++s) {
-        const uint32_t row = 4 * quarter + s;
+    for (uint32_t s = 0; s < 4 * G; ++s) {
+        const uint32_t row = s / 4 * 16 + 4 * quarter + s % 4;
         const bool counts = row < p.n && p.lse2[row] != __builtin_inff() && p.dloss[row] != 0.0f;
 #pragma unroll
         for (uint32_t f = 0; f < 4; ++f) {
@@ -626,12 +652,13 @@ __global__ void __launch_bounds__(kBlock) narrow_weight_kernel(const SlabArgs p)
     }
     constexpr uint32_t kAtOnce = 2;
     for (uint32_t v0 = begin; v0 < end; v0 += 16 * kAtOnce) {
-        f32x4 d[kAtOnce];
+        f32x4 d[kAtOnce][G];
         float old[kAtOnce][2][8];
 #pragma unroll
         for (uint32_t u = 0; u < kAtOnce; ++u) {
             const uint32_t v = v0 + 16 * u + r, at = v < end ? v : end - 1;
-            d[u] = *reinterpret_cast<const f32x4 *>(p.dz + (uint64_t)at * 16 + 4 * quarter);
+#pragma unroll
+            for (uint32_t g = 0; g < G; ++g) d[u][g] = *reinterpret_cast<const f32x4 *>(p.dz + (uint64_t)at * (16 * G) + 16 * g + 4 * quarter);
 #pragma unroll
             for (uint32_t h = 0; h < 2; ++h) {
 #pragma unroll
@@ -649,7 +676,7 @@ __global__ void __launch_bounds__(kBlock) narrow_weight_kernel(const SlabArgs p)
                     // (sum i of a lane: column i of its four, token r)
                     f32x4 sum = {0.0f, 0.0f, 0.0f, 0.0f};
 #pragma unroll
-                    for (int s = 0; s < 4; ++s) sum = __builtin_amdgcn_mfma_f32_16x16x4f32(x[2 * h + f][s], d[u][s], sum, 0, 0, 0);
+                    for (int s = 0; s < 4 * G; ++s) sum = __builtin_amdgcn_mfma_f32_16x16x4f32(x[2 * h + f][s], d[u][s / 4][s % 4], sum, 0, 0, 0);
 #pragma unroll
                     for (int i = 0; i < 4; ++i) old[u][h][4 * f + i] += sum[i];
                 }
@@ -659,14 +686,14 @@ __global__ void __launch_bounds__(kBlock) narrow_weight_kernel(const SlabArgs p)
     }
 }
 // dz of a teacher's entries.
-__global__ void __launch_bounds__(kBlock) narrow_entries_kernel(const NarrowArgs p, const Entries entries) {
+__global__ void __launch_bounds__(kBlock) narrow_entries_kernel(const NarrowArgs p, const Entries entries, uint32_t padded) {
     const uint32_t at = wg_x() * kBlock + tid_x();
     if (at >= p.n * entries.top) return;
     const float q = entries.share[at];
     const uint32_t row = at / entries.top, t = (uint32_t)entries.tokens[at];
     const RowGradient r = p.rows[row];
     if (q == 0.0f || r.gradient == 0.0f || t >= p.vocab) return;
-    p.dz[(uint64_t)t * 16 + row] = r.gradient * (exp2_of(__builtin_fmaf(entries.picked[at], p.c, -r.lse2)) - q);
+    p.dz[(uint64_t)t * padded + row] = r.gradient * (exp2_of(__builtin_fmaf(entries.picked[at], p.c, -r.lse2)) - q);
 }
 
 // ---- forward: a row's loss -------------------------------------------------------------------------------------
@@ -957,6 +984,9 @@ constexpr uint64_t kMaxRows = CNR_LOSS_MAX_ROWS, kMaxVocabulary = CNR_LOSS_MAX_V
 // Up to how many rows the weight goes straight from memory into the products.  With more its rows are better shared through LDS, even where they have to be laid
 // out first: 64 x 54656 x 6026 at an odd stride 608 us by four times as many rows to a workgroup, 534 laid out.
 constexpr uint32_t kNarrowRows = 16;
+// Floats are laid out in three parts otherwise, and tiles of few rows are few: a step of 32 x 15815 x 5312 1055 -> 500 us, of 64 x 32000 x 1024 351 -> 271; with as many
+// rows again the fp32 instructions would take longer than six bfloat16 ones.
+constexpr uint32_t kNarrowRowsOfFloats = 64;
 // Up to how many rows of 16 bits dz is held in two parts, whatever the results' type: products that are bound by reading the weight and by writing its gradient
 // nearly have the time (a step of 32 x 131072 x 4096 941 -> 1013 us), and sums of few rows do not average roundings.
 constexpr uint32_t kTwoPartRows = 64;
@@ -1015,6 +1045,8 @@ struct ForwardPlan {
     dense::Plan tiles;
     uint64_t parts, begins, hidden, weight, bytes;  // in the workspace
 };
+uint64_t narrow_rows(const Sizes &s) { return s.parts == 3 ? kNarrowRowsOfFloats : kNarrowRows; }
+uint64_t padded_rows(uint64_t n) { return n <= 16 ? 16 : n <= 32 ? 32 : 64; }
 uint32_t narrow_fragments(uint64_t n, uint64_t vocab) {
     // Two fragments of the weight to a wave where that still gives every SIMD a wave.
     return n > 1 && vocab >= 16384 ? 2 : 1;
@@ -1023,7 +1055,7 @@ ForwardPlan forward_plan(const cnr_ctx *ctx, const Sizes &s) {
     ForwardPlan f = {};
     f.rows = s.n;
     if (s.vocab == 0) return f;
-    f.narrow = s.n <= kNarrowRows;
+    f.narrow = s.n <= narrow_rows(s);
     f.fragments = narrow_fragments(s.n, s.vocab);
     f.tiles = dense::plan_of(ctx, s.vocab, s.n, (uint64_t)s.blocks * (s.parts == 3 ? kOfFloats.number : 1), 0.5f /* time for exponentials */, 0);
     const uint32_t columns = f.narrow ? 16 * f.fragments : dense::kTiles[f.tiles.kind].columns;
@@ -1054,12 +1086,12 @@ struct BackwardPlan {
 BackwardPlan backward_plan(const cnr_ctx *ctx, const Sizes &s, bool two, bool in_place) {
     BackwardPlan b = {};
     const uint32_t parts = dz_parts(s, two);
-    b.narrow = s.n <= kNarrowRows && !(in_place && s.vocab * s.dim >= kTiledFrom);
+    b.narrow = s.n <= narrow_rows(s) && !(in_place && s.vocab * s.dim >= kTiledFrom) && s.n * rounded(s.dim, 4) * sizeof(float) <= kPartBytes;
     if (b.narrow) {
         Room room;
         b.scale = room.take(2 * sizeof(float));
         b.rows = room.take(256 * sizeof(RowGradient));
-        b.dz = room.take(s.vocab * 16 * sizeof(float));
+        b.dz = room.take(s.vocab * padded_rows(s.n) * sizeof(float));
         b.partial = room.take(kPartBytes);
         b.bytes = room.used;
         return b;
@@ -1089,11 +1121,11 @@ BackwardPlan backward_plan(const cnr_ctx *ctx, const Sizes &s, bool two, bool in
 uint64_t room_for(const Sizes &s, bool training, bool two) {
     const uint64_t most_weight = least(s.vocab, rounded(kPieceBytes / s.row, 256)), small = least(s.n, 256);
     Room f;
-    const uint64_t stats = part_bytes(cnr_ceil_div(s.vocab, 64)), narrow = least(s.n, kNarrowRows) * part_bytes(cnr_ceil_div(s.vocab, 16));
+    const uint64_t stats = part_bytes(cnr_ceil_div(s.vocab, 64)), narrow = least(s.n, narrow_rows(s)) * part_bytes(cnr_ceil_div(s.vocab, 16));
     uint64_t parts = least(s.n * stats, kStatsBytes);
     parts = parts > small * stats ? parts : small * stats;
     f.take((parts > narrow ? parts : narrow) + 256);
-    if (s.n > kNarrowRows) {
+    if (s.n > narrow_rows(s)) {
         f.take(s.n * s.row);
         f.take(most_weight * s.row);
     }
@@ -1105,7 +1137,7 @@ uint64_t room_for(const Sizes &s, bool training, bool two) {
     const uint64_t few = least(s.n, kTwoPartRows) * 2 * (s.parts == 3 ? 3 : 2), vocab = rounded(s.vocab, dense::kBlockElements);
     uint64_t tiled = least(of_dz * vocab, 2 * kPieceBytes + 256 * of_dz);
     tiled = tiled > least(few * vocab, 2 * kPieceBytes + 256 * few) ? tiled : least(few * vocab, 2 * kPieceBytes + 256 * few);
-    const uint64_t narrow_dz = s.vocab * 16 * sizeof(float);
+    const uint64_t narrow_dz = s.vocab * padded_rows(least(s.n, narrow_rows(s))) * sizeof(float);
     b.take(tiled > narrow_dz ? tiled : narrow_dz);
     b.take(s.n * s.row);
     b.take(most_weight * s.row);
@@ -1158,10 +1190,24 @@ constexpr int kOf = TYPE == CNR_FLOAT_F16 ? CNR_FLOAT_F16 : CNR_FLOAT_BF16;
 template <int TYPE, bool GRADIENT>
 void narrow(const NarrowArgs &a, uint32_t fragments, hipStream_t to) {
     const dim3 grid((unsigned)cnr_ceil_div(a.vocab, 16 * fragments)), threads(kBlock);
-    if (fragments == 2)
-        hipLaunchKernelGGL((narrow_kernel<TYPE, 2, 2, GRADIENT>), grid, threads, 0, to, a);
-    else
-        hipLaunchKernelGGL((narrow_kernel<TYPE, 1, 4, GRADIENT>), grid, threads, 0, to, a);
+    if (a.n <= 16) {
+        if (fragments == 2)
+            hipLaunchKernelGGL((narrow_kernel<TYPE, 1, 2, 2, GRADIENT>), grid, threads, 0, to, a);
+        else
+            hipLaunchKernelGGL((narrow_kernel<TYPE, 1, 1, 4, GRADIENT>), grid, threads, 0, to, a);
+    } else if constexpr (TYPE == CNR_FLOAT_F32) {
+        if (a.n <= 32) {
+            if (fragments == 2)
+                hipLaunchKernelGGL((narrow_kernel<TYPE, 2, 2, 1, GRADIENT>), grid, threads, 0, to, a);
+            else
+                hipLaunchKernelGGL((narrow_kernel<TYPE, 2, 1, 2, GRADIENT>), grid, threads, 0, to, a);
+        } else {
+            if (fragments == 2)
+                hipLaunchKernelGGL((narrow_kernel<TYPE, 4, 2, 1, GRADIENT>), grid, threads, 0, to, a);
+            else
+                hipLaunchKernelGGL((narrow_kernel<TYPE, 4, 1, 1, GRADIENT>), grid, threads, 0, to, a);
+        }
+    }
 }
 
 template <int TYPE>
@@ -1271,8 +1317,12 @@ void narrow_backward(cnr_ctx *ctx, const cnr_vocabulary &v, const cnr_targets &t
     const NarrowArgs a = {v.hidden, v.weight, v.hidden_stride, v.weight_stride, n, vocab, dim, kLog2e / targets.temperature, nullptr, 0, rows, dz};
     narrow<TYPE, true>(a, narrow_fragments(v.n, v.vocab), to);
     if (t.logits && t.top)
-        hipLaunchKernelGGL(narrow_entries_kernel, dim3((unsigned)cnr_ceil_div(v.n * t.top, kBlock)), dim3(kBlock), 0, to, a, entries_of(state, v.n, t.top));
+        hipLaunchKernelGGL(narrow_entries_kernel, dim3((unsigned)cnr_ceil_div(v.n * t.top, kBlock)), dim3(kBlock), 0, to, a, entries_of(state, v.n, t.top), (uint32_t)padded_rows(v.n));
     // Sixteen waves to a compute unit, slabs of 64 tokens at least, parts of sums of up to a quarter of the room for them (they are read again).
+    const auto by_rows = [&](const auto &launch) {
+        if (n <= 16) return launch(std::integral_constant<int, 1>());
+        if constexpr (TYPE == CNR_FLOAT_F32) return n <= 32 ? launch(std::integral_constant<int, 2>()) : launch(std::integral_constant<int, 4>());
+    };
     SlabArgs s = {};
     s.dz = dz;
     s.vocab = vocab;
@@ -1287,7 +1337,9 @@ void narrow_backward(cnr_ctx *ctx, const cnr_vocabulary &v, const cnr_targets &t
         s.stride = v.weight_stride;
         s.partial = reinterpret_cast<float *>(space + b.partial);
         s.partial_stride = stride;
-        hipLaunchKernelGGL((narrow_hidden_kernel<TYPE>), dim3((unsigned)cnr_ceil_div((uint64_t)s.groups * s.slabs, kWavesPerBlock)), dim3(kBlock), 0, to, s);
+        by_rows([&](auto g) {
+            hipLaunchKernelGGL((narrow_hidden_kernel<TYPE, decltype(g)::value>), dim3((unsigned)cnr_ceil_div((uint64_t)s.groups * s.slabs, kWavesPerBlock)), dim3(kBlock), 0, to, s);
+        });
         const KeepSum sum = {dhidden, {nullptr, 0, CNR_FLOAT_F32}, nullptr, s.partial, stride};
         hipLaunchKernelGGL((join_sums_kernel<16>), dim3((unsigned)cnr_ceil_div(v.n * (stride / 4), kBlock / 16)), dim3(kBlock), 0, to, sum, n, dim, s.slabs);
     }
@@ -1299,7 +1351,9 @@ void narrow_backward(cnr_ctx *ctx, const cnr_vocabulary &v, const cnr_targets &t
         s.dloss = dloss;
         s.out = dweight;
         s.there = accumulate ? dweight : Target{nullptr, 0, CNR_FLOAT_F32};
-        hipLaunchKernelGGL((narrow_weight_kernel<TYPE>), dim3((unsigned)cnr_ceil_div((uint64_t)s.groups * s.slabs, kWavesPerBlock)), dim3(kBlock), 0, to, s);
+        by_rows([&](auto g) {
+            hipLaunchKernelGGL((narrow_weight_kernel<TYPE, decltype(g)::value>), dim3((unsigned)cnr_ceil_div((uint64_t)s.groups * s.slabs, kWavesPerBlock)), dim3(kBlock), 0, to, s);
+        });
     }
 }
 

@@ -4,10 +4,11 @@
 // rows) stays in a register.  The top-th largest of the threads' own largest is at most the top-th largest of all, and hardly more elements reach it than
 // are wanted: the vectors whose largest does are read again, all at once, and their elements that reach it are collected in LDS, in any order; each finds
 // its place by counting those before it.  Keys (the value, then the lower token) are all different, so the order they were collected in does not matter.
-// Where too many reach the bound (equal values, or the largest all in one thread's share), it is raised digit by digit first.
+// Where too many reach the bound, they are equal values, of which the first are taken in order, or the largest are all in a few threads' shares, and the bound is raised
+// digit by digit.
 //
 // 64 of 8192 x 32000 bfloat16 101 us, 5.2 TB/s, of 512 x 131072 34 us, 3.9 TB/s (177 and 60 with rows held in registers, so that fewer of them share a compute unit; 312
-// and 70 read twice); 50 of 1 x 50257 floats 12 us, one workgroup's latency.
+// and 70 read twice), 94 where all are equal; 50 of 1 x 50257 floats 12 us, one workgroup's latency.
 #include "cnr_loss.h"
 #include "lm_common.h"
 
@@ -204,7 +205,8 @@ __global__ void __launch_bounds__(THREADS, EACH == 2 ? 8 : 1) top_kernel(const T
     auto collect = [&](uint64_t from) {
         auto take = [&](float v, uint32_t token) {
             const uint64_t place = place_of(key_of(v), token);
-            if (place >= from && token < p.vocab) {
+            // (once there are too many, there is no need to count on)
+            if (place >= from && token < p.vocab && *reinterpret_cast<volatile uint32_t *>(&lds.n_found) <= kRoom) {
                 const uint32_t at = atomicAdd(&lds.n_found, 1u);
                 if (at < kRoom) lds.found[at] = place;
             }
@@ -234,38 +236,90 @@ __global__ void __launch_bounds__(THREADS, EACH == 2 ? 8 : 1) top_kernel(const T
             if (at < 2 * THREADS) lds.hits[at] = q * THREADS + tid_x();
         }
         __syncthreads();
-        again = lds.n_hits > 2 * THREADS;
+        again = lds.n_hits > 2 * THREADS;  // far too many elements
     }
     if (top) collect((uint64_t)bound << 32);  // places from there on
     if (top && lds.n_found > kRoom) {
-        // Eight bits of the place at a time: how many have each digit behind those that are settled; the digit that the top-th place has.
-        uint64_t settled = 0;
-        uint32_t above = 0;  // places that are larger than any with these digits
-        for (int shift = 56; shift >= 0; shift -= 8) {
-            for (uint32_t i = tid_x(); i < 256; i += THREADS) lds.bins[i] = 0;
-            __syncthreads();
-            for_row<TYPE, THREADS>(row, p.vocab, [&](float v, uint32_t token) {
-                const uint64_t place = place_of(key_of(v), token);
-                if (shift == 56 || place >> (shift + 8) == settled >> (shift + 8)) atomicAdd(&lds.bins[place >> shift & 255u], 1u);
-            });
-            __syncthreads();
-            if (tid_x() == 0) {
-                uint32_t more = above;
-                int digit = 255;
-                while (more + lds.bins[digit] < top) more += lds.bins[digit--];
-                lds.digit = (uint32_t)digit;
-                lds.above = more;
+        // Most often that is since many are equal: where fewer than `top` exceed the threads' top-th largest, the others are the first that equal it.
+        __syncthreads();
+        if (wave == 0) {
+            uint32_t own[THREADS / kWave], exact = lds.bound;
+#pragma unroll
+            for (uint32_t i = 0; i < THREADS / kWave; ++i) own[i] = lds.largest[i * kWave + lane];
+            for (uint32_t bit = 0x8000u; bit; bit >>= 1) {
+                uint32_t reach = 0;
+#pragma unroll
+                for (uint32_t i = 0; i < THREADS / kWave; ++i) reach += (uint32_t)__popcll(__ballot(own[i] >= (exact | bit)));
+                if (reach >= top) exact |= bit;
+            }
+            if (lane == 0) {
+                lds.bound = exact;
                 lds.n_found = 0;
             }
-            __syncthreads();
-            const uint32_t with = lds.bins[lds.digit];
-            settled |= (uint64_t)lds.digit << shift;
-            above = lds.above;
-            __syncthreads();
-            if (above + with <= kRoom) break;
         }
+        __syncthreads();
+        const uint32_t exact = lds.bound;
         again = true;
-        collect(settled);
+        if (exact != 0xffffffffu) collect((uint64_t)(exact + 1) << 32);
+        const uint32_t larger = lds.n_found;
+        __syncthreads();
+        if (larger < top) {
+            const uint32_t wanted = top - larger;
+            for (uint32_t base = 0, got = 0; got < wanted && base < p.vocab; base += THREADS) {
+                const uint32_t token = base + tid_x();
+                const bool equal = token < p.vocab && key_of(Element<TYPE>::wide(row[token])) == exact;
+                const uint64_t mask = __ballot(equal);
+                if (lane == 0) lds.bins[wave] = (uint32_t)__popcll(mask);
+                __syncthreads();
+                uint32_t before = got + (uint32_t)__popcll(mask & ((1ull << lane) - 1));
+#pragma unroll
+                for (uint32_t w = 0; w < kWaves; ++w) {
+                    before += w < wave ? lds.bins[w] : 0u;
+                    got += lds.bins[w];
+                }
+                if (equal && before < wanted) lds.found[larger + before] = place_of(exact, token);
+                __syncthreads();
+            }
+            if (tid_x() == 0) lds.n_found = top;
+            __syncthreads();
+        } else {
+            // Eight bits of the place at a time: how many have each digit behind those that are settled; the digit that the top-th place has.
+            uint64_t settled = 0;
+            uint32_t above = 0;  // places that are larger than any with these digits
+            for (int shift = 56; shift >= 0; shift -= 8) {
+                for (uint32_t i = tid_x(); i < 256; i += THREADS) lds.bins[i] = 0;
+                __syncthreads();
+                for_row<TYPE, THREADS>(row, p.vocab, [&](float v, uint32_t token) {
+                    const uint64_t place = place_of(key_of(v), token);
+                    if (shift == 56 || place >> (shift + 8) == settled >> (shift + 8)) {
+                        // what has the first lane's digit is added at once: this way is for rows with many equal ones
+                        const uint32_t digit = (uint32_t)(place >> shift) & 255u, common = (uint32_t)__builtin_amdgcn_readfirstlane((int)digit);
+                        const uint64_t same = __ballot(digit == common);
+                        if (digit != common)
+                            atomicAdd(&lds.bins[digit], 1u);
+                        else if (lane == (uint32_t)__builtin_ctzll(same))
+                            atomicAdd(&lds.bins[common], (uint32_t)__popcll(same));
+                    }
+                });
+                __syncthreads();
+                if (tid_x() == 0) {
+                    uint32_t more = above;
+                    int digit = 255;
+                    while (more + lds.bins[digit] < top) more += lds.bins[digit--];
+                    lds.digit = (uint32_t)digit;
+                    lds.above = more;
+                    lds.n_found = 0;
+                }
+                __syncthreads();
+                const uint32_t with = lds.bins[lds.digit];
+                settled |= (uint64_t)lds.digit << shift;
+                above = lds.above;
+                __syncthreads();
+                if (above + with <= kRoom) break;
+            }
+            again = true;
+            collect(settled);
+        }
     }
     const uint32_t found = top ? lds.n_found : 0;
     T *values = p.values ? reinterpret_cast<T *>(p.values) + row_at * p.top : nullptr;

@@ -183,6 +183,30 @@ def test_tokens_whose_logits_are_minus_infinity(ctx, kind, n):
     _near(got[rest], want, "losses")
 
 
+@pytest.mark.parametrize("kind", list(TYPES))
+@pytest.mark.parametrize("n,threads", [(2, 1024), (1300, 256)])
+def test_top_logits_that_are_in_a_few_threads_shares(ctx, n, threads, kind):
+    """The largest 50 shares hold more than there is room for, their values all different or many the same; ties at the end of the row."""
+    t, vocab, top = TYPES[kind], 200_003 if n == 2 else 30_003, 100
+    x = torch.full((n, vocab), -100.0, dtype=t, device=DEV)
+    share = torch.arange(vocab, device=DEV) // (16 // x.element_size()) % threads < 50
+    count = int(share.sum())
+    x[0, share] = torch.rand(count, generator=torch.Generator(device=DEV).manual_seed(1), device=DEV).to(t)
+    x[1, share] = torch.arange(count, device=DEV).remainder(7).to(t)
+    if n > 2:
+        x[2, -60:] = 1.0
+        x[3] = -math.inf
+        x[3, -130:] = 2.0
+        x[4, ::2] = math.nan
+        x[5, 1::2] = 7.0
+        x[6:] = torch.randint(0, 3, (n - 6, vocab), generator=torch.Generator(device=DEV).manual_seed(2), device=DEV).to(t)
+    tokens, values, lse = P.top_logits(ctx, x, top)
+    want = R.top(x, top)
+    assert torch.equal(tokens, want[0]) and torch.equal(values.nan_to_num(nan=1e4), want[1].nan_to_num(nan=1e4))
+    finite = want[2].isfinite()
+    assert bool(((lse.double() - want[2]).abs() <= (vocab / 256 * 8 + 300) * 2.0 ** -24 * (1 + want[2].abs()))[finite].all()) and bool(lse[~finite].isnan().all())
+
+
 # ---- fewer rows than it was made for, streams, graphs ------------------------------------------------------------------
 
 def test_one_object_serves_all_numbers_of_rows(ctx):

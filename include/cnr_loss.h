@@ -54,7 +54,7 @@ typedef struct {
 #define CNR_LOSS_MAX_DIM 1048576u
 
 /* loss[i], float [n], with lse = log sum over v of exp(z[i][v] / T):
- *   target t         lse - z[i][t]                                             (T is 1)
+ *   target t         lse - z[i][t], by the same sums of products, so never below 0   (T is 1)
  *   teacher          sum over j of q_j (log q_j - z[i][tokens[j]] / T + lse),  q the softmax of the teacher's logits / T over the row's tokens
  * A row without a token (a padded target, no token within the vocabulary, a teacher whose logits are all -infinity) is left out: its loss is 0, it has no
  * gradient, and its hidden state may hold anything.  A row with a NaN or an infinite z that is not -infinity has a loss of NaN.  |z / T| is to be below 2^127.

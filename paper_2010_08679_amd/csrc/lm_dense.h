@@ -100,6 +100,7 @@ __device__ __forceinline__ void barrier() {
     asm volatile("" ::: "memory");
 }
 
+constexpr uint32_t kNoIndex = 0xffffffffu;
 // What a workgroup's outputs are to its epilogue.  A lane holds MF / 2 times eight columns side by side, 32 apart, of NF rows: value(acc, i, g) is that of
 // column column_of(i) and row row(g).  The four lanes of a row thus write 64 bytes of 16-bit outputs side by side at a time.
 template <int MF, int NF, bool DOWN, uint32_t THREADS, uint32_t LDS>
@@ -115,6 +116,8 @@ struct Place {
     __device__ __forceinline__ uint32_t row_within(uint32_t g) const { return lane_row + g / 2 * 32 + (DOWN ? (g ^ tid_x() / 4) % 2 : g % 2) * 4; }
     __device__ __forceinline__ uint32_t row(uint32_t g) const { return row0 + row_within(g); }
     __device__ __forceinline__ uint32_t column_of(uint32_t i) const { return column + i / 8 * 32 + i % 8; }
+    // The i with column_of(i) = column + from, kNoIndex where that is none of the lane's.
+    static __device__ __forceinline__ uint32_t index_of(uint64_t from) { return from < 16 * MF && from % 32 < 8 ? (uint32_t)from / 32 * 8 + (uint32_t)from % 8 : kNoIndex; }
     static __device__ __forceinline__ float value(const f32x4 (&acc)[MF][NF], int i, int g) { return acc[i / 4][g][i % 4]; }
 };
 

@@ -75,6 +75,19 @@ __device__ __forceinline__ Stats stats16(const float (&z)[N], float c, uint32_t 
 
 // ---- what the products' tiles do with their outputs ----------------------------------------------------------------
 
+struct TargetArgs {
+    const void *tokens, *logits;
+    uint64_t token_stride, logit_stride;
+    uint32_t top;
+    int token_type, logit_type;
+    float temperature;
+};
+__device__ __forceinline__ int64_t token_of(const TargetArgs &t, uint64_t row, uint32_t j) {
+    const uint64_t at = row * t.token_stride + j;
+    return t.token_type == CNR_IDX_I64 ? reinterpret_cast<const int64_t *>(t.tokens)[at] : reinterpret_cast<const int32_t *>(t.tokens)[at];
+}
+
+constexpr uint32_t kNoTarget = dense::kNoIndex;
 // A teacher's entries, [n][top], in the order of their tokens; kNoToken behind the last.
 constexpr int32_t kNoToken = 0x7fffffff;
 struct Entries {
@@ -84,16 +97,20 @@ struct Entries {
     uint32_t top;
 };
 
-// Stats of each row over the tile's columns; with PICK also the logits of the entries there.
-template <bool PICK>
+// Stats of each row over the tile's columns, and the logits there of the row's target or, SOFT, of its entries: the same sums that the stats are of, so that of
+// a certain token's loss nothing but the other tokens is left.
+template <bool SOFT>
 struct KeepStats {
     static constexpr bool kUsesLds = true;
     Stats *parts;      // [rows][n_parts], from the piece's first part on
     uint32_t n_parts;
     float c;
-    const uint16_t *begins;  // [rows][n_parts + 1], likewise: a tile's first entry in a row
-    Entries entries;         // from the first row on
     uint32_t first;          // token of the first column
+    TargetArgs targets;      // not SOFT
+    uint64_t row0;           // the first row
+    float *picked;           // [rows]: its target's logit
+    const uint16_t *begins;  // SOFT: [rows][n_parts + 1], as parts: a tile's first entry in a row
+    Entries entries;         // from the first row on
     template <uint32_t TM, uint32_t TN, int WM, typename Place, int MF, int NF>
     __device__ __forceinline__ void finish(const dense::Args &p, const Place &at, const f32x4 (&acc)[MF][NF]) const {
         if (at.column0 + TM <= p.columns)
@@ -104,6 +121,14 @@ struct KeepStats {
     template <uint32_t TM, uint32_t TN, int WM, bool WHOLE, typename Place, int MF, int NF>
     __device__ __forceinline__ void reduce(const dense::Args &p, const Place &at, const f32x4 (&acc)[MF][NF]) const {
         Stats *lds = reinterpret_cast<Stats *>(at.lds);  // [WM][TN]
+        uint32_t target[NF];  // which of the lane's columns
+#pragma unroll
+        for (int g = 0; g < NF; ++g) {
+            target[g] = kNoTarget;
+            // (tokens that are none are below or behind all columns that count)
+            if constexpr (!SOFT)
+                if (at.row(g) < p.rows) target[g] = at.index_of((uint64_t)token_of(targets, row0 + at.row(g), 0) - first - at.column);
+        }
 #pragma unroll
         for (int g = 0; g < NF; ++g) {
             float top = -__builtin_inff();
@@ -118,6 +143,12 @@ struct KeepStats {
             sum += __shfl_xor(sum, 16);
             sum += __shfl_xor(sum, 32);
             if (tid_x() % kWave < 16) lds[at.wave_column * TN + at.row_within(g)] = {top, sum};
+            if (!SOFT && __any(target[g] != kNoTarget)) {
+                float z = 0.0f;
+#pragma unroll
+                for (uint32_t i = 0; i < 4 * MF; ++i) z = target[g] == i ? at.value(acc, i, g) : z;
+                if (target[g] != kNoTarget) picked[at.row(g)] = z;
+            }
         }
         __syncthreads();
         const uint32_t row = tid_x();
@@ -127,7 +158,7 @@ struct KeepStats {
             for (int w = 1; w < WM; ++w) s = join(s, lds[w * TN + row]);
             parts[(uint64_t)(at.row0 + row) * n_parts + at.tile_column] = s;
         }
-        if constexpr (PICK) pick<TM, TN>(p, at, acc);
+        if constexpr (SOFT) pick<TM, TN>(p, at, acc);
     }
     // The tile goes into LDS, as many rows at a time as there is room for, and each entry looks its logit up: what it costs does not depend on where the entries
     // are (8192 x 32000 x 4096 with 64 entries a row 1640 -> 1680 us; as dot products of rows from memory they took 680).  Pieces of four columns are permuted by the
@@ -171,7 +202,6 @@ struct KeepStats {
 
 // What the backward pass knows of a row: log2 of its sum of exponentials and dloss / T, scaled (0: the row adds nothing), and its target where it has
 // one (else kNoTarget).
-constexpr uint32_t kNoTarget = 0xffffffffu;
 struct __attribute__((aligned(16))) RowGradient {
     float lse2, gradient;
     uint32_t target, unused;
@@ -226,7 +256,7 @@ struct KeepGradient {
             const RowGradient r = rows[row];
             if (row >= p.rows) continue;
             T *to = dz + row * stride;
-            const uint32_t from = r.target - first - at.column, target = from < 16 * MF && from % 32 < 8 ? from / 32 * 8 + from % 8 : kNoTarget;  // which of the lane's
+            const uint32_t target = at.index_of(r.target - first - at.column);  // which of the lane's
             if (__any(target != kNoTarget))
                 write<MF, NF, true>(p, at, acc, g, r, target, to);
             else
@@ -446,8 +476,15 @@ struct NarrowArgs {
     uint64_t hidden_stride, weight_stride;  // elements
     uint32_t n, vocab, dim;
     float c;
-    Stats *parts;              // or, for the backward pass,
+    // forward:
+    Stats *parts;
     uint32_t n_parts;
+    bool soft;
+    TargetArgs targets;        // not soft
+    float *picked;
+    const uint16_t *begins;    // soft: of the workgroups, as of tiles
+    Entries entries;
+    // backward:
     const RowGradient *rows;
     float *dz;                 // [vocab][16 G], zeros in rows from n on
 };
@@ -555,6 +592,31 @@ __global__ void __launch_bounds__(kBlock, G > 2 ? 3 : 4) narrow_kernel(const Nar
         } else {
             const Stats s = stats16(z, p.c, valid);
             if (n == 0 && row < p.n) p.parts[(uint64_t)row * p.n_parts + wg_x()] = s;
+            if (p.soft) {
+#pragma unroll
+                for (uint32_t g = 0; g < NF; ++g) sums[0][f * NF + g][m / 4 * 16 + n][m % 4] = z[g];  // (nobody else has read this one)
+            } else if (row < p.n) {
+                const int64_t t = token_of(p.targets, row, 0);
+#pragma unroll
+                for (uint32_t g = 0; g < NF; ++g)
+                    if (t == (int64_t)(n0 + 16 * g + n)) p.picked[row] = z[g];
+            }
+        }
+    }
+    if constexpr (!GRADIENT) {
+        if (!p.soft) return;
+        __syncthreads();
+#pragma unroll
+        for (uint32_t f = 0; f < G; ++f) {
+            const uint32_t row = 16 * f + m;
+            if (row >= p.n) continue;
+            const uint16_t *b = p.begins + (uint64_t)row * (p.n_parts + 1) + wg_x();
+            const uint32_t begin = b[0], end = b[1];
+            for (uint32_t e = begin + n; e < end; e += 16) {
+                const uint64_t entry = (uint64_t)row * p.entries.top + e;
+                const uint32_t column = (uint32_t)p.entries.tokens[entry] - n0;
+                if (column < 16 * NF) p.entries.picked[entry] = sums[0][f * NF + column / 16][m / 4 * 16 + column % 16][m % 4];
+            }
         }
     }
 }
@@ -698,17 +760,6 @@ __global__ void __launch_bounds__(kBlock) narrow_entries_kernel(const NarrowArgs
 
 // ---- forward: a row's loss -------------------------------------------------------------------------------------
 
-struct TargetArgs {
-    const void *tokens, *logits;
-    uint64_t token_stride, logit_stride;
-    uint32_t top;
-    int token_type, logit_type;
-    float temperature;
-};
-__device__ __forceinline__ int64_t token_of(const TargetArgs &t, uint64_t row, uint32_t j) {
-    const uint64_t at = row * t.token_stride + j;
-    return t.token_type == CNR_IDX_I64 ? reinterpret_cast<const int64_t *>(t.tokens)[at] : reinterpret_cast<const int32_t *>(t.tokens)[at];
-}
 __device__ __forceinline__ float logit_of(const TargetArgs &t, uint64_t row, uint32_t j) {
     return read({const_cast<void *>(t.logits), t.logit_stride, t.logit_type}, row, j);
 }
@@ -790,44 +841,29 @@ __global__ void __launch_bounds__(kBlock) teacher_kernel(const TeacherArgs p) {
         p.lse2[row] = counts ? 0.0f : __builtin_inff();
     }
     if (!p.begins) return;
-    for (uint64_t tile = tid_x(); tile <= p.n_parts; tile += kBlock) {
-        uint32_t lo = 0, hi = top;  // the first entry whose token is not below
-        while (lo < hi) {
-            const uint32_t middle = (lo + hi) / 2;
-            if ((uint64_t)(uint32_t)sorted[middle] < tile * p.columns)
-                lo = middle + 1;
-            else
-                hi = middle;
-        }
+    // A share of the tiles to a thread: it looks for the first one's first entry, whose token is not below, and goes on from there.
+    const uint64_t each = (p.n_parts + kBlock) / kBlock, tile0 = tid_x() * each;
+    uint32_t lo = 0, hi = top;
+    while (lo < hi) {
+        const uint32_t middle = (lo + hi) / 2;
+        if ((uint64_t)(uint32_t)sorted[middle] < tile0 * p.columns)
+            lo = middle + 1;
+        else
+            hi = middle;
+    }
+    uint64_t next = lo < top ? (uint32_t)sorted[lo] : ~0ull;
+    for (uint64_t tile = tile0; tile < tile0 + each && tile <= p.n_parts; ++tile) {
+        while (next < tile * p.columns) next = ++lo < top ? (uint32_t)sorted[lo] : ~0ull;
         // (behind the last tile lie those without a token)
         p.begins[(uint64_t)wg_x() * (p.n_parts + 1) + tile] = (uint16_t)lo;
     }
 }
 
-// The product of two rows by THREADS threads: the sum of this wave's.
-template <uint32_t THREADS, typename T>
-__device__ __forceinline__ float dot(const T *x, const T *y, uint32_t dim) {
-    constexpr uint32_t kPer = 16 / sizeof(T);
-    float sum = 0.0f;
-    for (uint32_t at = tid_x() % THREADS * kPer; at < dim; at += THREADS * kPer) {
-        if (at + kPer <= dim) {
-            const Pack<T, kPer> a = *reinterpret_cast<const Pack<T, kPer> *>(x + at), b = *reinterpret_cast<const Pack<T, kPer> *>(y + at);
-#pragma unroll
-            for (uint32_t j = 0; j < kPer; ++j) sum = __builtin_fmaf((float)a.v[j], (float)b.v[j], sum);
-        } else {
-            for (uint32_t j = at; j < dim; ++j) sum = __builtin_fmaf((float)x[j], (float)y[j], sum);
-        }
-    }
-    return wave_sum(sum);
-}
-
 struct LossArgs {
-    const void *hidden, *weight;
-    uint64_t hidden_stride, weight_stride;
     uint64_t vocab;
-    uint32_t dim;
     TargetArgs targets;
     Entries entries;
+    const float *picked;  // of the launch's first row on; without a teacher
     const Stats *parts;
     uint32_t n_parts;
     uint64_t row0;      // of this launch
@@ -835,22 +871,8 @@ struct LossArgs {
     float c;
     cnr_dev_errors *err;
 };
-// Logits of entries one by one, an entry to a wave: where few rows go without tiles.
-template <int TYPE>
-__global__ void __launch_bounds__(kBlock) pick_kernel(const LossArgs p, uint64_t n) {
-    typedef typename Element<TYPE>::type T;
-    const uint64_t entry = wave_in_grid();
-    if (entry >= n * p.entries.top) return;
-    const int32_t t = p.entries.tokens[entry];
-    if (t < 0 || (uint64_t)t >= p.vocab) return;
-    const float z = dot<kWave>(reinterpret_cast<const T *>(p.hidden) + entry / p.entries.top * p.hidden_stride, reinterpret_cast<const T *>(p.weight) + (uint64_t)t * p.weight_stride,
-                               p.dim);
-    if (tid_x() % kWave == 0) p.entries.picked[entry] = z;
-}
-
-template <int TYPE, bool SOFT>
+template <bool SOFT>
 __global__ void __launch_bounds__(kBlock) loss_kernel(const LossArgs p) {
-    typedef typename Element<TYPE>::type T;
     __shared__ Stats joined[kWavesPerBlock];
     __shared__ float sums[kWavesPerBlock];
     const uint32_t lane = tid_x() % kWave, wave = (uint32_t)__builtin_amdgcn_readfirstlane((int)(tid_x() / kWave));
@@ -878,33 +900,36 @@ __global__ void __launch_bounds__(kBlock) loss_kernel(const LossArgs p) {
         s = {top, wave_sum(s.sum * exp2_of(s.top - at))};
     }
     if (lane == 0) joined[wave] = s;
-    // the expected logit: the target's, of which each wave has a part of the sum, or that of the teacher
-    float expected = 0.0f;
+    __syncthreads();
+    s = joined[0];
+#pragma unroll
+    for (int w = 1; w < kWavesPerBlock; ++w) s = join(s, joined[w]);
+    // How far the expected logit, the target's or that of the teacher, is below the largest.  The sum is of powers of exact differences from the largest, which
+    // was rounded: so are these (with the products rounded first, a certain token of |z| = 4000 had a loss of 1.6e-4 below 0).
+    float below = 0.0f;
     bool counts;
     if constexpr (SOFT) {
         counts = p.lse2[row] != __builtin_inff();
         for (uint32_t j = tid_x(); j < p.entries.top; j += kBlock) {
             const float q = p.entries.share[row * p.entries.top + j];
-            if (q != 0.0f) expected = __builtin_fmaf(q, p.entries.picked[row * p.entries.top + j], expected);
+            if (q != 0.0f) below = __builtin_fmaf(q, __builtin_fmaf(-p.entries.picked[row * p.entries.top + j], p.c, s.top), below);
         }
-        expected = wave_sum(expected);
+        below = sum_of_block(below, sums);
+        if (tid_x() != 0) return;
     } else {
+        if (tid_x() != 0) return;
         const int64_t t = token_of(p.targets, row, 0);
         counts = t >= 0 && (uint64_t)t < p.vocab;
-        if (t >= 0 && !counts && tid_x() == 0) atomicAdd(&p.err->n_bad_indices, 1ull);
-        if (counts)
-            expected = dot<kBlock>(reinterpret_cast<const T *>(p.hidden) + row * p.hidden_stride, reinterpret_cast<const T *>(p.weight) + (uint64_t)t * p.weight_stride, p.dim);
+        if (t >= 0 && !counts) atomicAdd(&p.err->n_bad_indices, 1ull);
+        if (counts) below = __builtin_fmaf(-p.picked[wg_x()], p.c, s.top);
     }
-    if (lane == 0) sums[wave] = expected;
-    __syncthreads();
-    if (tid_x() != 0) return;
-    expected = (sums[0] + sums[1]) + (sums[2] + sums[3]);
-    s = joined[0];
-#pragma unroll
-    for (int w = 1; w < kWavesPerBlock; ++w) s = join(s, joined[w]);
     const float log_sum = __builtin_amdgcn_logf(s.sum);  // to base 2
-    // (the largest logit and the expected one are subtracted first: of a certain token little is left)
-    p.loss[row] = counts ? (SOFT ? p.loss[row] : 0.0f) + ((s.top - expected * p.c) + log_sum) * kLn2 : 0.0f;
+    float loss = (below + log_sum) * kLn2;
+    if constexpr (SOFT)
+        loss += p.loss[row];
+    else
+        loss = loss < 0.0f ? 0.0f : loss;  // what roundings leave of a certain token's: a few 2^-24
+    p.loss[row] = counts ? loss : 0.0f;
     if (p.lse2) p.lse2[row] = counts ? s.top + log_sum : __builtin_inff();
 }
 
@@ -1043,7 +1068,7 @@ struct ForwardPlan {
     uint64_t rows, piece;  // at a time
     uint32_t n_parts;      // of a row
     dense::Plan tiles;
-    uint64_t parts, begins, hidden, weight, bytes;  // in the workspace
+    uint64_t parts, begins, picked, hidden, weight, bytes;  // in the workspace
 };
 uint64_t narrow_rows(const Sizes &s) { return s.parts == 3 ? kNarrowRowsOfFloats : kNarrowRows; }
 uint64_t padded_rows(uint64_t n) { return n <= 16 ? 16 : n <= 32 ? 32 : 64; }
@@ -1068,6 +1093,7 @@ ForwardPlan forward_plan(const cnr_ctx *ctx, const Sizes &s) {
     Room room;
     f.parts = room.take(f.rows * f.n_parts * sizeof(Stats));
     f.begins = room.take(f.rows * (f.n_parts + 1) * sizeof(uint16_t));
+    f.picked = room.take(f.rows * sizeof(float));
     if (!f.narrow) {
         f.hidden = room.take(f.rows * s.row);
         f.weight = room.take(f.piece * s.row);
@@ -1125,6 +1151,7 @@ uint64_t room_for(const Sizes &s, bool training, bool two) {
     uint64_t parts = least(s.n * stats, kStatsBytes);
     parts = parts > small * stats ? parts : small * stats;
     f.take((parts > narrow ? parts : narrow) + 256);
+    f.take(s.n * sizeof(float));
     if (s.n > narrow_rows(s)) {
         f.take(s.n * s.row);
         f.take(most_weight * s.row);
@@ -1220,12 +1247,8 @@ void forward(cnr_ctx *ctx, const cnr_vocabulary &v, const cnr_targets &t, float 
     const T *hidden = reinterpret_cast<const T *>(v.hidden), *weight = reinterpret_cast<const T *>(v.weight);
     LossArgs l;
     l.targets = targets_of(t);
-    l.hidden = hidden;
-    l.weight = weight;
-    l.hidden_stride = v.hidden_stride;
-    l.weight_stride = v.weight_stride;
     l.vocab = v.vocab;
-    l.dim = (uint32_t)v.dim;
+    l.picked = reinterpret_cast<const float *>(space + f.picked);
     l.parts = reinterpret_cast<const Stats *>(space + f.parts);
     l.n_parts = f.n_parts;
     l.loss = loss;
@@ -1233,24 +1256,27 @@ void forward(cnr_ctx *ctx, const cnr_vocabulary &v, const cnr_targets &t, float 
     l.entries = entries_of(state, v.n, t.top);
     l.err = ctx->dev_err;
     const float c = l.c = kLog2e / l.targets.temperature;
-    TeacherArgs teacher = {l.targets, v.vocab, 0, l.entries, loss, state, f.narrow || !v.vocab ? nullptr : reinterpret_cast<uint16_t *>(space + f.begins), f.n_parts,
-                           dense::kTiles[f.tiles.kind].columns, ctx->dev_err};
+    const uint32_t columns = f.narrow ? 16 * f.fragments : dense::kTiles[f.tiles.kind].columns;
+    TeacherArgs teacher = {l.targets, v.vocab, 0, l.entries, loss, state, v.vocab ? reinterpret_cast<uint16_t *>(space + f.begins) : nullptr, f.n_parts, columns, ctx->dev_err};
     for (uint64_t row0 = 0; row0 < v.n; row0 += f.rows) {
         const uint64_t rows = v.n - row0 < f.rows ? v.n - row0 : f.rows;
         Stats *parts = reinterpret_cast<Stats *>(space + f.parts);
+        float *picked = reinterpret_cast<float *>(space + f.picked);
         const T *x = hidden + row0 * v.hidden_stride;
         teacher.row0 = row0;
+        Entries entries = l.entries;
+        entries.tokens += row0 * t.top;
+        entries.picked += row0 * t.top;
         if (t.logits) hipLaunchKernelGGL(teacher_kernel, dim3((unsigned)rows), dim3(kBlock), 0, to, teacher);
         if (f.n_parts == 0) {
         } else if (f.narrow) {
-            const NarrowArgs a = {x, weight, v.hidden_stride, v.weight_stride, (uint32_t)rows, (uint32_t)v.vocab, (uint32_t)v.dim, c, parts, f.n_parts, nullptr, nullptr};
+            const NarrowArgs a = {x, weight, v.hidden_stride, v.weight_stride, (uint32_t)rows, (uint32_t)v.vocab, (uint32_t)v.dim, c, parts, f.n_parts, t.logits != nullptr,
+                                  l.targets, picked, teacher.begins, entries, nullptr, nullptr};
             narrow<TYPE, false>(a, f.fragments, to);
-            if (t.logits && t.top) hipLaunchKernelGGL((pick_kernel<TYPE>), dim3((unsigned)cnr_ceil_div(rows * t.top, kWavesPerBlock)), dim3(kBlock), 0, to, l, rows);
         } else {
             const Terms terms = s.parts == 3 ? kOfFloats : kOne;
             Layout of_x, of_w;
             const dense::Operand x_at = in_terms(operand_of(s, x, v.hidden_stride, rows, whole_rows(v.type, x, v.hidden_stride, v.dim, rows), space + f.hidden, of_x), terms.down);
-            const uint32_t columns = dense::kTiles[f.tiles.kind].columns;
             const uint64_t most = in_place ? rounded((1ull << 22) / cnr_ceil_div(rows, 64) * 64, 256) : f.piece;
             for (uint64_t v0 = 0; v0 < v.vocab; v0 += most) {
                 const uint64_t width = v.vocab - v0 < most ? v.vocab - v0 : most;
@@ -1258,20 +1284,19 @@ void forward(cnr_ctx *ctx, const cnr_vocabulary &v, const cnr_targets &t, float 
                 lay_out<T>(s, of_w, of_x, to);
                 of_x.rows = 0;
                 const dense::Args args = {w_at, x_at, (uint32_t)width, (uint32_t)rows, s.blocks, 0, terms.number, 1};
-                Entries entries = l.entries;
-                entries.tokens += row0 * t.top;
-                entries.picked += row0 * t.top;
+                Stats *of_piece = parts + v0 / columns;
                 if (t.logits)
-                    dense::launch<kOf<TYPE>, false, false>(args, f.tiles.kind, KeepStats<true>{parts + v0 / columns, f.n_parts, c, teacher.begins + v0 / columns, entries, (uint32_t)v0}, to);
+                    dense::launch<kOf<TYPE>, false, false>(args, f.tiles.kind,
+                                                           KeepStats<true>{of_piece, f.n_parts, c, (uint32_t)v0, l.targets, row0, nullptr, teacher.begins + v0 / columns, entries}, to);
                 else
-                    dense::launch<kOf<TYPE>, false, false>(args, f.tiles.kind, KeepStats<false>{parts + v0 / columns, f.n_parts, c, nullptr, entries, 0}, to);
+                    dense::launch<kOf<TYPE>, false, false>(args, f.tiles.kind, KeepStats<false>{of_piece, f.n_parts, c, (uint32_t)v0, l.targets, row0, picked, nullptr, entries}, to);
             }
         }
         l.row0 = row0;
         if (t.logits)
-            hipLaunchKernelGGL((loss_kernel<TYPE, true>), dim3((unsigned)rows), dim3(kBlock), 0, to, l);
+            hipLaunchKernelGGL(loss_kernel<true>, dim3((unsigned)rows), dim3(kBlock), 0, to, l);
         else
-            hipLaunchKernelGGL((loss_kernel<TYPE, false>), dim3((unsigned)rows), dim3(kBlock), 0, to, l);
+            hipLaunchKernelGGL(loss_kernel<false>, dim3((unsigned)rows), dim3(kBlock), 0, to, l);
     }
 }
 
@@ -1314,7 +1339,7 @@ void narrow_backward(cnr_ctx *ctx, const cnr_vocabulary &v, const cnr_targets &t
     hipLaunchKernelGGL(rows_kernel, dim3(1), dim3(kRowThreads), 0, to, state, dloss, v.n, targets, v.vocab, 0, rows, reinterpret_cast<float *>(space + b.scale));
     const uint32_t n = (uint32_t)v.n, vocab = (uint32_t)v.vocab, dim = (uint32_t)v.dim;
     float *dz = reinterpret_cast<float *>(space + b.dz);
-    const NarrowArgs a = {v.hidden, v.weight, v.hidden_stride, v.weight_stride, n, vocab, dim, kLog2e / targets.temperature, nullptr, 0, rows, dz};
+    const NarrowArgs a = {v.hidden, v.weight, v.hidden_stride, v.weight_stride, n, vocab, dim, kLog2e / targets.temperature, nullptr, 0, false, targets, nullptr, nullptr, {}, rows, dz};
     narrow<TYPE, true>(a, narrow_fragments(v.n, v.vocab), to);
     if (t.logits && t.top)
         hipLaunchKernelGGL(narrow_entries_kernel, dim3((unsigned)cnr_ceil_div(v.n * t.top, kBlock)), dim3(kBlock), 0, to, a, entries_of(state, v.n, t.top), (uint32_t)padded_rows(v.n));

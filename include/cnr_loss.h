@@ -22,7 +22,8 @@ extern "C" {
  *   hidden, weight  float, bfloat16 or half [n][dim] and [vocab][dim] as `type` says, aligned to their element, rows
  *                   hidden_stride and weight_stride >= dim elements apart.  Products and sums are fp32's.  Rows of 16 bits of a multiple of 8
  *                   elements, 16 bytes aligned, are read where they are by more than 16 rows; others are laid out in the workspace first.  Floats are
- *                   multiplied in three parts of 8 bits: six of nine products, off by 2^-21 of the product at most and 2^-24 on average */
+ *                   multiplied in three parts of 8 bits: six of nine products, off by 2^-21 of the product at most and 2^-24 on average, and by 2^-131
+ *                   of either factor, which is more only next to a float below 2^-110 */
 typedef struct {
     const void *hidden;
     uint64_t hidden_stride;

@@ -40,6 +40,9 @@ def loss(hidden, weight, tokens, logits=None, temperature=1.0, dloss=None, there
     z = x @ w.t() / temperature
     # a sum of dim products, each added with one rounding: at most dim + 1 of them; the scaling to base 2 and its undoing are a few more of |z|
     z_off = ((dim + 8) * u * (x.abs() @ w.abs().t()) / temperature) + 4 * u
+    # a float as three bfloat16: zero parts and what is below bfloat16's smallest number, 2^-133, are held as that number: three parts, each off by 2^-133 at most
+    part = 2.0 ** -131 if kind == torch.float32 else 0.0
+    z_off = z_off + part * (x.abs().sum(dim=1)[:, None] + w.abs().sum(dim=1)[None, :]) / temperature
     lse = torch.logsumexp(z, dim=1) if vocab else torch.full((n,), -math.inf, dtype=torch.float64, device=hidden.device)
     most_off = z_off.max(dim=1).values if vocab else torch.zeros_like(lse)
     at = tokens.clamp(0, max(vocab - 1, 0))
@@ -70,7 +73,9 @@ def loss(hidden, weight, tokens, logits=None, temperature=1.0, dloss=None, there
 
     def sums(a, a_off, b, terms):
         """a b with a off by a_off, added up in fp32 (two sums where a is in two parts; parts of sums joined: 20 more)."""
-        return a @ b, a_off @ b.abs() + (terms + 32) * u * ((a.abs() + a_off) @ b.abs())
+        # below 2^-126 numbers of fp32 are 2^-149 apart: each of up to six additions a term, of the joins and of what follows is off by half of that besides
+        smallest = part * (a.abs().sum(dim=1)[:, None] + b.abs().sum(dim=0)[None, :]) + (6 * terms + 64) * 2.0 ** -150
+        return a @ b, a_off @ b.abs() + (terms + 32) * u * ((a.abs() + a_off) @ b.abs()) + smallest
 
     dh, dh_off = sums(dz, dz_off + e * dz.abs(), w, vocab)
     dw, dw_off = sums(dz.t(), (dz_off + e ** parts * dz.abs()).t(), kept, n)

@@ -14,7 +14,8 @@
 //
 // The matrix instructions take 16-bit elements.  A float is the sum of three bfloat16, its bits cut in three; of the nine products of two floats' parts
 // six are added up, the rest is below 2^-21 of the product in the worst case (2^-24 on average).  All parts have the float's sign, and a part that is zero of a float that is
-// not, or of an infinite one, is +-2^-126 instead: so an infinity times a float is the infinity that it ought to be in every term.
+// not, or of an infinite one, is +-2^-133 instead, bfloat16's smallest, which the matrix instructions keep: so an infinity times a float is the infinity that it ought to be
+// in every term.  A float is thus off by 2^-131 at most, which is more than 2^-21 of it below 2^-110 only.
 #include "lm_dense.h"
 #include "cnr_loss.h"
 
@@ -412,11 +413,11 @@ __device__ __forceinline__ __bf16 float_part(float v, int part) {
     for (int i = 0; i < part; ++i) rest -= __uint_as_float(__float_as_uint(rest) & 0xffff0000u);
     uint32_t bits = __float_as_uint(rest) & 0xffff0000u;
     if (part) {
-        const bool finite = __builtin_fabsf(v) < __builtin_inff();
-        if (!finite || (rest == 0.0f && v != 0.0f)) bits = sign | 0x00800000u;
+        if (!(__builtin_fabsf(v) < __builtin_inff())) bits = 0;
     } else if (v != v) {
         bits = 0x7fc00000u;
     }
+    if ((bits & 0x7fffffffu) == 0 && v != 0.0f) bits = sign | 0x00010000u;
     return __builtin_bit_cast(__bf16, (unsigned short)(bits >> 16));
 }
 // dst[rows][parts][whole blocks] = src, zeros behind it; rows that add nothing to a gradient are zeros.

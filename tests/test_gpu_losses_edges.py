@@ -68,3 +68,36 @@ def test_entries_of_few_rows_are_found_in_the_product(ctx, kind, n, vocab, top):
     dx, dw = loss.backward(dloss)
     _near(dx, want["dhidden"], "dhidden")
     _near(dw, want["dweight"], "dweight")
+
+
+@pytest.mark.parametrize("exponent", [-90, -114, -122])
+@pytest.mark.parametrize("n,vocab,dim", [(100, 300, 64), (300, 2000, 200), (10, 300, 64)])
+def test_small_floats_are_as_exact_as_others(ctx, n, vocab, dim, exponent):
+    """Hidden states of few bits around 2^exponent, whose further parts are zeros, and a weight that makes ordinary logits of them."""
+    g = torch.Generator(device=DEV).manual_seed(n)
+    x = (1.0 + torch.rand(n, dim, generator=g, device=DEV)).bfloat16().float() * 2.0 ** exponent
+    w = _normal(g, vocab, dim) * 2.0 ** (-exponent - 2)
+    targets, dloss = torch.randint(0, vocab, (n,), generator=g, device=DEV), torch.rand(n, generator=g, device=DEV)
+    want = R.loss(x, w, targets, dloss=dloss)
+    loss = P.VocabularyLoss(ctx, vocab, dim, n, torch.float32)
+    _near(loss.cross_entropy(x, w, targets), want["losses"], "losses")
+    dx, dw = loss.backward(dloss)
+    _near(dx, want["dhidden"], "dhidden")
+    _near(dw, want["dweight"], "dweight")
+
+
+@pytest.mark.parametrize("small", [1.0, 2.0 ** -110 * (1 + 2.0 ** -23), 2.0 ** -130, 2.0 ** -140, 2.0 ** -149])
+@pytest.mark.parametrize("n", [5, 100])
+def test_minus_infinity_times_a_small_float(ctx, n, small):
+    """A float of which a part is below bfloat16's smallest number, or all of it: -infinity times it is -infinity, a token without probability."""
+    vocab, dim = 300, 40
+    g = torch.Generator(device=DEV).manual_seed(6)
+    x, w = _normal(g, n, dim, 2.0), _normal(g, vocab, dim, 0.2)
+    x[:, -1] = small
+    w[:, -1] = 0.0
+    gone = torch.arange(vocab, device=DEV) % 3 == 1
+    w[gone, -1] = -math.inf
+    targets = torch.randint(0, vocab // 3, (n,), generator=g, device=DEV) * 3
+    kept = (~gone).nonzero()[:, 0]
+    got = P.VocabularyLoss(ctx, vocab, dim, n, torch.float32).cross_entropy(x, w, targets)
+    _near(got, R.loss(x, w[kept], torch.searchsorted(kept, targets))["losses"], "losses")

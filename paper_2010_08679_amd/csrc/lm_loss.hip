@@ -330,6 +330,8 @@ struct KeepSum {
     const float *scale;     // NULL: 1
     float *partial;         // [splits][m][partial_stride] where sums are split
     uint64_t partial_stride;
+    const RowGradient *rows; // NULL: all count.  The others' outputs are 0, also where the weight holds infinities or NaN
+    __device__ __forceinline__ bool counts(uint32_t row) const { return !rows || rows[row].gradient != 0.0f; }
     template <uint32_t TM, uint32_t TN, int WM, typename Place, int MF, int NF>
     __device__ __forceinline__ void finish(const dense::Args &p, const Place &at, const f32x4 (&acc)[MF][NF]) const {
         const float by = scale ? *scale : 1.0f;
@@ -348,6 +350,7 @@ struct KeepSum {
                 }
                 continue;
             }
+            const bool all = counts(row);
             // What is added to is read for the whole row at once: one piece after the other would wait for memory each time.
             float old[4 * MF / 8][8];
 #pragma unroll
@@ -359,7 +362,7 @@ struct KeepSum {
 #pragma unroll
             for (int u = 0; u < 4 * MF / 8; ++u) {
 #pragma unroll
-                for (int j = 0; j < 8; ++j) old[u][j] = __builtin_fmaf(at.value(acc, 8 * u + j, g), by, old[u][j]);
+                for (int j = 0; j < 8; ++j) old[u][j] = all ? __builtin_fmaf(at.value(acc, 8 * u + j, g), by, old[u][j]) : 0.0f;
                 write_row(out, row, at.column_of(8 * u), p.columns, old[u]);
             }
         }
@@ -399,8 +402,9 @@ __global__ void __launch_bounds__(kBlock) join_sums_kernel(const KeepSum k, uint
     const float by = k.scale ? *k.scale : 1.0f;
     float v[4] = {0.0f, 0.0f, 0.0f, 0.0f};
     if (k.there.out) read_row(k.there, row, column, n, v);
+    const bool all = k.counts(row);
 #pragma unroll
-    for (int j = 0; j < 4; ++j) v[j] = __builtin_fmaf(sum[j], by, v[j]);
+    for (int j = 0; j < 4; ++j) v[j] = all ? __builtin_fmaf(sum[j], by, v[j]) : 0.0f;
     write_row(k.out, row, column, n, v);
 }
 
@@ -1324,6 +1328,7 @@ void product(cnr_ctx *ctx, const dense::Args &args, const KeepSum &k, hipStream_
     KeepSum rest = k;
     rest.out = from_row(k.out, plans.first_rows);
     rest.there = from_row(k.there, plans.first_rows);
+    if (rest.rows) rest.rows += plans.first_rows;
     a.rows = args.rows - a.rows;
     const uint64_t skipped = plans.first_rows * (DOWN ? 2 : a.down.stride);
     a.down.at = reinterpret_cast<const uint8_t *>(a.down.at) + skipped;
@@ -1366,7 +1371,7 @@ void narrow_backward(cnr_ctx *ctx, const cnr_vocabulary &v, const cnr_targets &t
         by_rows([&](auto g) {
             hipLaunchKernelGGL((narrow_hidden_kernel<TYPE, decltype(g)::value>), dim3((unsigned)cnr_ceil_div((uint64_t)s.groups * s.slabs, kWavesPerBlock)), dim3(kBlock), 0, to, s);
         });
-        const KeepSum sum = {dhidden, {nullptr, 0, CNR_FLOAT_F32}, nullptr, s.partial, stride};
+        const KeepSum sum = {dhidden, {nullptr, 0, CNR_FLOAT_F32}, nullptr, s.partial, stride, rows};
         hipLaunchKernelGGL((join_sums_kernel<16>), dim3((unsigned)cnr_ceil_div(v.n * (stride / 4), kBlock / 16)), dim3(kBlock), 0, to, sum, n, dim, s.slabs);
     }
     if (dweight.out) {
@@ -1431,12 +1436,14 @@ void backward(cnr_ctx *ctx, const cnr_vocabulary &v, const cnr_targets &t, const
             hipLaunchKernelGGL((entries_kernel<kOf<TYPE>, PARTS>), dim3((unsigned)cnr_ceil_div(v.n * t.top, kBlock)), dim3(kBlock), 0, to, k, entries, v.n, width);
         const dense::Operand dz = {k.dz, k.stride * 2, (uint32_t)(k.stride * 2), (uint32_t)(k.width * 2), 0, 8};
         if (dhidden) {
+            sum.rows = rows;
             sum.there = v0 == 0 ? none : between;
             sum.out = v0 + width == v.vocab ? Target{dhidden, dhidden_stride, v.type} : between;
             product<TYPE, false>(ctx, dense::Args{in_terms(w, to_hidden.across), in_terms(dz, to_hidden.down), dim, n, blocks, width, to_hidden.number, 1}, sum, to);
         }
         if (dweight) {
             sum.out = {reinterpret_cast<uint8_t *>(dweight) + v0 * dweight_stride * cnr_float_bytes(dweight_type), dweight_stride, dweight_type};
+            sum.rows = nullptr;
             sum.there = accumulate ? sum.out : none;
             product<TYPE, true>(ctx, dense::Args{in_terms(x, to_weight.across), in_terms(dz, to_weight.down), dim, width, (uint32_t)cnr_ceil_div(v.n, dense::kBlockElements), n,
                                             to_weight.number, 1}, sum, to);

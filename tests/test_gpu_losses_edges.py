@@ -101,3 +101,23 @@ def test_minus_infinity_times_a_small_float(ctx, n, small):
     kept = (~gone).nonzero()[:, 0]
     got = P.VocabularyLoss(ctx, vocab, dim, n, torch.float32).cross_entropy(x, w, targets)
     _near(got, R.loss(x, w[kept], torch.searchsorted(kept, targets))["losses"], "losses")
+
+
+@pytest.mark.parametrize("kind", list(TYPES))
+@pytest.mark.parametrize("n,vocab,dim", [(8, 500, 64), (40, 500, 72), (100, 500, 64), (500, 9000, 40), (2100, 40000, 64)])
+def test_rows_that_are_left_out_have_no_gradient_whatever_the_weight_holds(ctx, kind, n, vocab, dim):
+    """Infinities and NaN in the weight make every other row's loss and gradient NaN, and not those of padding, of a teacher without entries or with a dloss of 0."""
+    g, t = torch.Generator(device=DEV).manual_seed(n), TYPES[kind]
+    x, w = _normal(g, n, dim).to(t), _normal(g, vocab, dim, 0.2).to(t)
+    w[7], w[9, 3] = math.inf, math.nan
+    targets = torch.randint(10, vocab, (n,), generator=g, device=DEV)
+    dloss = torch.ones(n, device=DEV)
+    targets[::4], dloss[1::4] = -100, 0.0
+    none = (targets < 0) | (dloss == 0)
+    loss = P.VocabularyLoss(ctx, vocab, dim, n, t, top=2)
+    tokens = torch.stack([targets, torch.where(targets < 0, -1, 11)], dim=1)
+    for losses in (lambda: loss.cross_entropy(x, w, targets), lambda: loss.distill(x, w, tokens, torch.zeros(n, 2, device=DEV))):
+        got = losses()
+        assert bool((got[targets < 0] == 0).all()) and bool(got[targets >= 0].isnan().all())
+        dx, _ = loss.backward(dloss)
+        assert bool((dx[none] == 0).all()) and bool(dx[~none].isnan().any(dim=1).all())

@@ -38,7 +38,7 @@ typedef struct {
  *                counted as cnr_mark_touched counts look-ups outside the table
  *   logits       NULL: top is 1 and each token the row's target; or a teacher's logits of the tokens, [n][top] as logit_type says, rows
  *                logit_stride >= top apart, in any order; a token may come more than once
- *   temperature  > 0; divides the teacher's logits and the row's own.  Not read where logits is NULL */
+ *   temperature  > 0, from 2^-126 to 3e38; divides the teacher's logits and the row's own.  Not read where logits is NULL */
 typedef struct {
     const void *tokens;
     cnr_index_type token_type;

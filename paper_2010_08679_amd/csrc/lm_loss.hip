@@ -1010,6 +1010,7 @@ __global__ void __launch_bounds__(kBlock) zero_kernel(const Target out, uint64_t
 
 // ---- the host's side ------------------------------------------------------------------------------------------
 
+constexpr float kMinTemperature = 0x1p-126f;  // log2(e) / T stays finite: 0 / T is 0
 constexpr uint64_t kMaxRows = CNR_LOSS_MAX_ROWS, kMaxVocabulary = CNR_LOSS_MAX_VOCABULARY, kMaxDim = CNR_LOSS_MAX_DIM;
 // Up to how many rows the weight goes straight from memory into the products.  With more its rows are better shared through LDS, even where they have to be laid
 // out first: 64 x 54656 x 6026 at an odd stride 608 us by four times as many rows to a workgroup, 534 laid out.
@@ -1458,7 +1459,7 @@ void zeros(const Target &out, uint64_t rows, uint64_t columns, hipStream_t to) {
 cnr_status checked(const cnr_vocabulary *v, const cnr_targets *t) {
     if (!v || !t || !cnr_valid_float_type(v->type) || (t->token_type != CNR_IDX_I32 && t->token_type != CNR_IDX_I64)) return CNR_E_INVALID;
     if (v->hidden_stride < v->dim || v->weight_stride < v->dim || t->token_stride < t->top) return CNR_E_INVALID;
-    if (t->logits ? !cnr_valid_float_type(t->logit_type) || t->logit_stride < t->top || !(t->temperature > 0.0f) || t->temperature > 3e38f : t->top != 1) return CNR_E_INVALID;
+    if (t->logits ? !cnr_valid_float_type(t->logit_type) || t->logit_stride < t->top || !(t->temperature >= kMinTemperature) || t->temperature > 3e38f : t->top != 1) return CNR_E_INVALID;
     if (v->n > kMaxRows || v->vocab > kMaxVocabulary || v->dim > kMaxDim || t->top > kMaxTop) return CNR_E_TOO_LARGE;
     if (v->n && ((!t->tokens && t->top) || (v->dim && (!v->hidden || (v->vocab && !v->weight))))) return CNR_E_INVALID;
     const size_t e = cnr_float_bytes(v->type);

@@ -84,8 +84,8 @@ def _loss_arguments(hidden, weight, tokens, logits, temperature: float):
         if rows != n or columns != top:
             raise ValueError("logits must have the shape of tokens")
         logit_type = L._float(logits, "logits")
-        if not 0.0 < temperature < 3e38:
-            raise ValueError("the temperature must be positive")
+        if not 2.0 ** -126 <= temperature < 3e38:
+            raise ValueError("the temperature must be positive, from 2^-126 to 3e38")
         logits_at = logits_at or 16  # an empty matrix is none that is missing
     return (cnr_vocabulary(at, stride, weight_at, weight_stride, kind, n, vocab, dim),
             cnr_targets(tokens_at, token_type, token_stride, top, logits_at, logit_type, logit_stride, temperature))

@@ -184,3 +184,12 @@ def test_oracle_top_by_hand():
     v = torch.tensor([[1.0, math.nan, -0.0, 0.0, math.inf, -math.inf, 1.0]])
     tokens, values, lse = R.top(v, 9)
     assert tokens.tolist() == [[1, 4, 0, 6, 2, 3, 5, -1, -1]] and math.isnan(float(lse)) and values[0, -1] == -math.inf
+
+
+@pytest.mark.parametrize("name", ["cnr_vocabulary_loss", "cnr_vocabulary_loss_backward"])
+@pytest.mark.parametrize("temperature", [2.0 ** -127, 1e-39, 2.0 ** -149, -0.0, 3.2e38])
+def test_temperatures_that_1_cannot_be_divided_by_are_refused(name, temperature):
+    """Below 2^-126 log2(e) / T is infinite, and a logit of 0 would be NaN."""
+    assert _call(name, **(TEACHER | dict(temperature=temperature))) == INVALID
+    # (what comes after the temperature's check)
+    assert _call(name, **(TEACHER | dict(temperature=2.0 ** -126, tokens=A + 2))) == ALIGN

@@ -84,7 +84,7 @@ cnr_status cnr_vocabulary_loss_backward(cnr_ctx *ctx, const cnr_vocabulary *voca
 /* The `top` largest of each row of logits, largest first, of equal ones the lower token first; NaN counts as larger than infinity, -0 as 0.
  *   logits   float, bfloat16 or half [n][vocab] as `type` says, rows stride >= vocab elements apart, aligned to their element
  *   tokens   int32 [n][top], or NULL; -1 beyond the vocabulary's size
- *   values   of `type` [n][top], or NULL: the logits of these tokens; -infinity beyond the vocabulary's size
+ *   values   of `type` [n][top], or NULL: the logits of these tokens, bit for bit; -infinity beyond the vocabulary's size
  *   lse      float [n], or NULL: log sum over v of exp(logits[i][v]), summed in fp32; a value minus it is the token's log probability
  * CNR_E_TOO_LARGE beyond CNR_LOSS_MAX_TOP and from n = 2^22 on. */
 cnr_status cnr_top_logits(cnr_ctx *ctx, const void *logits, uint64_t stride, cnr_float_type type, uint64_t n, uint64_t vocab, uint64_t top, int32_t *tokens,

@@ -25,11 +25,12 @@ struct TopArgs {
     float *lse;
 };
 
+constexpr uint32_t kNan = 0xffffffffu, kZero = 0x80000000u;
 // In the order of the values, NaN last.
 __device__ __forceinline__ uint32_t key_of(float v) {
     const uint32_t u = __float_as_uint(v);
-    if (v != v) return 0xffffffffu;
-    if (v == 0.0f) return 0x80000000u;
+    if (v != v) return kNan;
+    if (v == 0.0f) return kZero;
     return u ^ ((uint32_t)((int32_t)u >> 31) | 0x80000000u);
 }
 constexpr float kLog2e = 1.44269504088896340736f;
@@ -330,9 +331,10 @@ __global__ void __launch_bounds__(THREADS, EACH == 2 ? 8 : 1) top_kernel(const T
 #pragma unroll 8
         for (uint32_t j = 0; j < found; ++j) before += lds.found[j] > place ? 1u : 0u;
         if (before >= top) continue;
-        const uint32_t token = ~(uint32_t)place;
+        const uint32_t token = ~(uint32_t)place, key = (uint32_t)(place >> 32);
         if (tokens) tokens[before] = (int32_t)token;
-        if (values) values[before] = Element<TYPE>::narrow(value_of((uint32_t)(place >> 32)));  // exactly what it was
+        // exactly what it was: a key has neither a zero's sign nor a NaN's bits
+        if (values) values[before] = key == kZero || key == kNan ? row[token] : Element<TYPE>::narrow(value_of(key));
     }
     for (uint32_t i = top + tid_x(); i < p.top; i += THREADS) {
         if (tokens) tokens[i] = -1;

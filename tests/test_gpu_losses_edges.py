@@ -121,3 +121,25 @@ def test_rows_that_are_left_out_have_no_gradient_whatever_the_weight_holds(ctx, 
         assert bool((got[targets < 0] == 0).all()) and bool(got[targets >= 0].isnan().all())
         dx, _ = loss.backward(dloss)
         assert bool((dx[none] == 0).all()) and bool(dx[~none].isnan().any(dim=1).all())
+
+
+@pytest.mark.parametrize("kind", list(TYPES))
+@pytest.mark.parametrize("n,vocab,top", [(3, 900, 50), (1300, 5003, 100), (2, 131_075, 300)])
+def test_top_values_are_the_rows_own_bits(ctx, kind, n, vocab, top):
+    """Zeros keep their signs and NaN their bits, in rows of few and of many such."""
+    t = TYPES[kind]
+    whole = torch.int32 if kind == "f32" else torch.int16
+    g = torch.Generator(device=DEV).manual_seed(vocab)
+    x = -_normal(g, n, vocab).abs().to(t)
+    x[:, torch.randint(0, vocab, (30,), generator=g, device=DEV)] = 0.0
+    x[:, torch.randint(0, vocab, (30,), generator=g, device=DEV)] = -0.0
+    x[1] = -0.0
+    x[1, 5::7] = 0.0
+    exponent = {"f32": 0x7F800000, "bf16": 0x7F80, "f16": 0x7C00}[kind]
+    payload = torch.randint(1, 0x70, (vocab // 9 + 1,), generator=g, device=DEV).to(whole)
+    bits = x.view(whole)
+    bits[0, ::9] = (payload | exponent)[: len(bits[0, ::9])]
+    bits[0, 4::9] = (payload | (exponent - (1 << (31 if kind == "f32" else 15))))[: len(bits[0, 4::9])]  # the same, negative
+    tokens, values, _ = P.top_logits(ctx, x, top)
+    assert torch.equal(tokens, R.top(x, top)[0])
+    assert torch.equal(values.view(whole), bits.gather(1, tokens.long()))

@@ -13,14 +13,8 @@
 
 namespace dense {
 
-typedef int i32x2 __attribute__((ext_vector_type(2)));
-typedef int i32x4 __attribute__((ext_vector_type(4)));
-typedef int i32x8 __attribute__((ext_vector_type(8)));
-typedef short s16x4 __attribute__((ext_vector_type(4)));
-typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
-typedef _Float16 f16x8 __attribute__((ext_vector_type(8)));
-
 constexpr uint32_t kBlockBytes = 128, kBlockElements = 64;
+constexpr uint32_t kNoIndex = 0xffffffffu;
 
 struct Operand {
     const void *at;       // 16-byte aligned
@@ -40,6 +34,13 @@ struct Args {
 };
 
 #ifdef __HIPCC__
+typedef int i32x2 __attribute__((ext_vector_type(2)));
+typedef int i32x4 __attribute__((ext_vector_type(4)));
+typedef int i32x8 __attribute__((ext_vector_type(8)));
+typedef short s16x4 __attribute__((ext_vector_type(4)));
+typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
+typedef _Float16 f16x8 __attribute__((ext_vector_type(8)));
+
 template <int I>
 struct Index {
     static constexpr int value = I;
@@ -100,7 +101,6 @@ __device__ __forceinline__ void barrier() {
     asm volatile("" ::: "memory");
 }
 
-constexpr uint32_t kNoIndex = 0xffffffffu;
 // What a workgroup's outputs are to its epilogue.  A lane holds MF / 2 times eight columns side by side, 32 apart, of NF rows: value(acc, i, g) is that of
 // column column_of(i) and row row(g).  The four lanes of a row thus write 64 bytes of 16-bit outputs side by side at a time.
 template <int MF, int NF, bool DOWN, uint32_t THREADS, uint32_t LDS>

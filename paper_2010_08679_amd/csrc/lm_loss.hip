@@ -16,8 +16,7 @@
 // six are added up, the rest is below 2^-21 of the product in the worst case (2^-24 on average).  All parts have the float's sign, and a part that is zero of a float that is
 // not, or of an infinite one, is +-2^-133 instead, bfloat16's smallest, which the matrix instructions keep: so an infinity times a float is the infinity that it ought to be
 // in every term.  A float is thus off by 2^-131 at most, which is more than 2^-21 of it below 2^-110 only.
-#include "lm_dense.h"
-#include "cnr_loss.h"
+#include "lm_loss_plan.h"
 
 #include <type_traits>
 
@@ -29,10 +28,6 @@ constexpr float kLog2e = 1.44269504088896340736f, kLn2 = 0.69314718055994530942f
 
 __device__ __forceinline__ float exp2_of(float x) { return __builtin_amdgcn_exp2f(x); }
 
-// (largest exponent to base 2, sum of 2^(exponent - largest)) of some of a row's logits; (-infinity, 0) of none.
-struct Stats {
-    float top, sum;
-};
 __device__ __forceinline__ Stats join(const Stats &a, const Stats &b) {
     const float top = __builtin_fmaxf(a.top, b.top), at = top == -__builtin_inff() ? 0.0f : top;
     return {top, a.sum * exp2_of(a.top - at) + b.sum * exp2_of(b.top - at)};
@@ -88,7 +83,6 @@ __device__ __forceinline__ int64_t token_of(const TargetArgs &t, uint64_t row, u
     return t.token_type == CNR_IDX_I64 ? reinterpret_cast<const int64_t *>(t.tokens)[at] : reinterpret_cast<const int32_t *>(t.tokens)[at];
 }
 
-constexpr uint32_t kNoTarget = dense::kNoIndex;
 // A teacher's entries, [n][top], in the order of their tokens; kNoToken behind the last.
 constexpr int32_t kNoToken = 0x7fffffff;
 struct Entries {
@@ -199,13 +193,6 @@ struct KeepStats {
             }
         }
     }
-};
-
-// What the backward pass knows of a row: log2 of its sum of exponentials and dloss / T, scaled (0: the row adds nothing), and its target where it has
-// one (else kNoTarget).
-struct __attribute__((aligned(16))) RowGradient {
-    float lse2, gradient;
-    uint32_t target, unused;
 };
 
 // v as PARTS numbers of 16 bits that add up to it.
@@ -434,9 +421,9 @@ struct Layout {
 };
 // Two matrices (either may have no rows), 16 bytes of each part to a thread.  Bound by memory: 34000 rows of 1024 floats 56 us, 6.2 TB/s.
 template <typename T>
-__global__ void __launch_bounds__(kBlock) lay_out_kernel(const Layout a, const Layout b, uint32_t dim, uint32_t pieces /* of a part */) {
+__global__ void __launch_bounds__(kBlock) lay_out_kernel(const Layout a, const Layout b, uint32_t dim, uint32_t pieces /* of a part */, uint64_t first) {
     constexpr int kParts = sizeof(T) == 4 ? 3 : 1;
-    uint64_t at = (uint64_t)wg_x() * kBlock + tid_x();
+    uint64_t at = first + (uint64_t)wg_x() * kBlock + tid_x();
     const bool second = at >= a.rows * pieces;
     const Layout &m = second ? b : a;
     at -= second ? a.rows * pieces : 0;
@@ -1010,175 +997,6 @@ __global__ void __launch_bounds__(kBlock) zero_kernel(const Target out, uint64_t
 
 // ---- the host's side ------------------------------------------------------------------------------------------
 
-constexpr float kMinTemperature = 0x1p-126f;  // log2(e) / T stays finite: 0 / T is 0
-constexpr uint64_t kMaxRows = CNR_LOSS_MAX_ROWS, kMaxVocabulary = CNR_LOSS_MAX_VOCABULARY, kMaxDim = CNR_LOSS_MAX_DIM;
-// Up to how many rows the weight goes straight from memory into the products.  With more its rows are better shared through LDS, even where they have to be laid
-// out first: 64 x 54656 x 6026 at an odd stride 608 us by four times as many rows to a workgroup, 534 laid out.
-constexpr uint32_t kNarrowRows = 16;
-// Floats are laid out in three parts otherwise, and tiles of few rows are few: a step of 32 x 15815 x 5312 1055 -> 500 us, of 64 x 32000 x 1024 351 -> 271; with as many
-// rows again the fp32 instructions would take longer than six bfloat16 ones.
-constexpr uint32_t kNarrowRowsOfFloats = 64;
-// Up to how many rows of 16 bits dz is held in two parts, whatever the results' type: products that are bound by reading the weight and by writing its gradient
-// nearly have the time (a step of 32 x 131072 x 4096 941 -> 1013 us), and sums of few rows do not average roundings.
-constexpr uint32_t kTwoPartRows = 64;
-// (In the backward pass of larger weights that need not be laid out tiles are faster even then: a step of 16 x 32000 x 1024 85 -> 76 us, of 16 x 131072 x 4096
-// 1300 -> 955, but of 16 x 1249 x 6784 66 against 74.)
-constexpr uint64_t kTiledFrom = 1ull << 24;
-constexpr uint64_t kPieceBytes = 256ull << 20;  // of a piece of the weight, of its dz twice as many
-constexpr uint64_t kPieceTokens = 1ull << 20;   // a row of its dz, in up to three parts, is below 2^23 bytes
-constexpr uint64_t kStatsBytes = 512ull << 20;  // of the stats of as many rows as go at a time
-constexpr uint64_t kPartBytes = 128ull << 20;   // of sums that are split
-
-uint64_t rounded(uint64_t v, uint64_t to) { return cnr_ceil_div(v, to) * to; }
-uint64_t least(uint64_t a, uint64_t b) { return a < b ? a : b; }
-
-// Whether a product can read rows of dim elements where they are.
-bool whole_rows(const cnr_float_type type, const void *base, uint64_t stride, uint64_t dim, uint64_t rows) {
-    return type != CNR_FLOAT_F32 && dim && dim % 8 == 0 && cnr_aligned(base, 16) && (rows <= 1 || (stride % 8 == 0 && stride < 1u << 22));
-}
-
-// Places in a workspace, in order.
-struct Room {
-    uint64_t used = 0;
-    uint64_t take(uint64_t bytes) {
-        const uint64_t at = used;
-        used += rounded(bytes, 256);
-        return at;
-    }
-};
-
-struct Sizes {
-    uint64_t n, vocab, dim;
-    cnr_float_type type;
-    uint32_t parts, blocks;  // of a laid out row: of 16-bit elements each, at least one block
-    uint64_t row;            // its bytes
-};
-Sizes sizes_of(uint64_t n, uint64_t vocab, uint64_t dim, cnr_float_type type) {
-    Sizes s = {n, vocab, dim, type, type == CNR_FLOAT_F32 ? 3u : 1u, 0, 0};
-    s.blocks = dim ? (uint32_t)cnr_ceil_div(dim, dense::kBlockElements) : 1;
-    s.row = (uint64_t)s.parts * s.blocks * dense::kBlockBytes;
-    return s;
-}
-// Pairs of parts, the smallest products of a block first.
-struct Terms {
-    uint32_t number, across, down;
-};
-constexpr Terms kOne = {1, 0, 0}, kOfFloats = {6, 0x001012, 0x010210}, kOfTwoParts = {2, 0, 0x01};
-
-// Of a row: its stats, and where the entries of each tile begin.
-uint64_t part_bytes(uint64_t n_parts) { return n_parts * sizeof(Stats) + (n_parts + 1) * sizeof(uint16_t); }
-
-struct ForwardPlan {
-    bool narrow;
-    uint32_t fragments;    // columns of a narrow workgroup, in sixteens
-    uint64_t rows, piece;  // at a time
-    uint32_t n_parts;      // of a row
-    dense::Plan tiles;
-    uint64_t parts, begins, picked, hidden, weight, bytes;  // in the workspace
-};
-uint64_t narrow_rows(const Sizes &s) { return s.parts == 3 ? kNarrowRowsOfFloats : kNarrowRows; }
-uint64_t padded_rows(uint64_t n) { return n <= 16 ? 16 : n <= 32 ? 32 : 64; }
-uint32_t narrow_fragments(uint64_t n, uint64_t vocab) {
-    // Two fragments of the weight to a wave where that still gives every SIMD a wave.
-    return n > 1 && vocab >= 16384 ? 2 : 1;
-}
-ForwardPlan forward_plan(const cnr_ctx *ctx, const Sizes &s) {
-    ForwardPlan f = {};
-    f.rows = s.n;
-    if (s.vocab == 0) return f;
-    f.narrow = s.n <= narrow_rows(s);
-    f.fragments = narrow_fragments(s.n, s.vocab);
-    f.tiles = dense::plan_of(ctx, s.vocab, s.n, (uint64_t)s.blocks * (s.parts == 3 ? kOfFloats.number : 1), 0.5f /* time for exponentials */, 0);
-    const uint32_t columns = f.narrow ? 16 * f.fragments : dense::kTiles[f.tiles.kind].columns;
-    f.n_parts = (uint32_t)cnr_ceil_div(s.vocab, columns);
-    const uint64_t per_row = part_bytes(f.n_parts), most = kStatsBytes / (per_row + 1) / 256 * 256;
-    f.rows = most < 256 ? 256 : most;
-    if (f.rows > s.n) f.rows = s.n;
-    f.piece = rounded(kPieceBytes / s.row, 256);
-    if (f.piece > s.vocab) f.piece = s.vocab;
-    Room room;
-    f.parts = room.take(f.rows * f.n_parts * sizeof(Stats));
-    f.begins = room.take(f.rows * (f.n_parts + 1) * sizeof(uint16_t));
-    f.picked = room.take(f.rows * sizeof(float));
-    if (!f.narrow) {
-        f.hidden = room.take(f.rows * s.row);
-        f.weight = room.take(f.piece * s.row);
-    }
-    f.bytes = room.used;
-    return f;
-}
-
-uint32_t dz_parts(const Sizes &s, bool two) { return s.parts == 3 ? 3 : two || s.n <= kTwoPartRows ? 2 : 1; }
-struct BackwardPlan {
-    bool narrow;
-    uint64_t piece, width;  // of the vocabulary; columns of dz, whole blocks
-    uint64_t scale, rows, dz, hidden_at, weight_at, sum, partial, bytes;
-};
-// (two: dweight in fp32 from 16-bit operands, by dz in two parts.  in_place: the weight is read where it is.)
-BackwardPlan backward_plan(const cnr_ctx *ctx, const Sizes &s, bool two, bool in_place) {
-    BackwardPlan b = {};
-    const uint32_t parts = dz_parts(s, two);
-    b.narrow = s.n <= narrow_rows(s) && !(in_place && s.vocab * s.dim >= kTiledFrom) && s.n * rounded(s.dim, 4) * sizeof(float) <= kPartBytes;
-    if (b.narrow) {
-        Room room;
-        b.scale = room.take(2 * sizeof(float));
-        b.rows = room.take(256 * sizeof(RowGradient));
-        b.dz = room.take(s.vocab * padded_rows(s.n) * sizeof(float));
-        b.partial = room.take(kPartBytes);
-        b.bytes = room.used;
-        return b;
-    }
-    uint64_t piece = 2 * kPieceBytes / (s.n * 2 * parts);
-    const uint64_t by_weight = kPieceBytes / s.row;
-    if (!in_place && piece > by_weight) piece = by_weight;
-    piece = rounded(least(piece ? piece : 1, kPieceTokens), 256);
-    // pieces of one size
-    const uint64_t pieces = cnr_ceil_div(s.vocab, piece);
-    b.piece = rounded(cnr_ceil_div(s.vocab, pieces), 256);
-    if (b.piece > s.vocab) b.piece = s.vocab;
-    b.width = rounded(b.piece, dense::kBlockElements);
-    Room room;
-    b.scale = room.take(2 * sizeof(float));
-    b.rows = room.take(rounded(s.n, 256) * sizeof(RowGradient));
-    b.dz = room.take(s.n * b.width * 2 * parts);
-    b.hidden_at = room.take(s.n * s.row);
-    b.weight_at = room.take(in_place ? 0 : b.piece * s.row);
-    b.sum = room.take(pieces > 1 ? s.n * s.dim * sizeof(float) : 0);
-    b.partial = room.take(kPartBytes);
-    b.bytes = room.used;
-    return b;
-}
-
-// At least what the plans take for n rows or fewer: each part's largest size.
-uint64_t room_for(const Sizes &s, bool training, bool two) {
-    const uint64_t most_weight = least(s.vocab, rounded(kPieceBytes / s.row, 256)), small = least(s.n, 256);
-    Room f;
-    const uint64_t stats = part_bytes(cnr_ceil_div(s.vocab, 64)), narrow = least(s.n, narrow_rows(s)) * part_bytes(cnr_ceil_div(s.vocab, 16));
-    uint64_t parts = least(s.n * stats, kStatsBytes);
-    parts = parts > small * stats ? parts : small * stats;
-    f.take((parts > narrow ? parts : narrow) + 256);
-    f.take(s.n * sizeof(float));
-    if (s.n > narrow_rows(s)) {
-        f.take(s.n * s.row);
-        f.take(most_weight * s.row);
-    }
-    if (!training) return f.used;
-    Room b;
-    const uint64_t of_dz = s.n * 2 * dz_parts(s, two);
-    b.take(2 * sizeof(float));
-    b.take(rounded(s.n, 256) * sizeof(RowGradient));
-    const uint64_t few = least(s.n, kTwoPartRows) * 2 * (s.parts == 3 ? 3 : 2), vocab = rounded(s.vocab, dense::kBlockElements);
-    uint64_t tiled = least(of_dz * vocab, 2 * kPieceBytes + 256 * of_dz);
-    tiled = tiled > least(few * vocab, 2 * kPieceBytes + 256 * few) ? tiled : least(few * vocab, 2 * kPieceBytes + 256 * few);
-    const uint64_t narrow_dz = s.vocab * padded_rows(least(s.n, narrow_rows(s))) * sizeof(float);
-    b.take(tiled > narrow_dz ? tiled : narrow_dz);
-    b.take(s.n * s.row);
-    b.take(most_weight * s.row);
-    b.take(s.n * s.dim * sizeof(float));
-    b.take(kPartBytes);
-    return b.used > f.used ? b.used : f.used;
-}
-
 // Rows as a product can read them: where they are, or, where `layout` has rows, laid out in `space` by lay_out.
 dense::Operand operand_of(const Sizes &s, const void *src, uint64_t stride, uint64_t rows, bool in_place, void *space, Layout &layout) {
     const uint32_t part = s.blocks * dense::kBlockBytes;
@@ -1189,8 +1007,8 @@ dense::Operand operand_of(const Sizes &s, const void *src, uint64_t stride, uint
 template <typename T>
 void lay_out(const Sizes &s, const Layout &a, const Layout &b, hipStream_t to) {
     const uint32_t pieces = s.blocks * dense::kBlockBytes / 16;
-    const uint64_t groups = cnr_ceil_div((a.rows + b.rows) * pieces, kBlock);
-    if (groups) hipLaunchKernelGGL((lay_out_kernel<T>), dim3((unsigned)groups), dim3(kBlock), 0, to, a, b, (uint32_t)s.dim, pieces);
+    in_launches((a.rows + b.rows) * pieces,
+                [&](uint64_t first, unsigned groups) { hipLaunchKernelGGL((lay_out_kernel<T>), dim3(groups), dim3(kBlock), 0, to, a, b, (uint32_t)s.dim, pieces, first); });
 }
 dense::Operand in_terms(dense::Operand o, uint32_t parts) {
     o.parts = parts;
@@ -1456,6 +1274,7 @@ void zeros(const Target &out, uint64_t rows, uint64_t columns, hipStream_t to) {
     if (rows && columns) hipLaunchKernelGGL(zero_kernel, dim3(kZeroGroups), dim3(kBlock), 0, to, out, rows, (uint32_t)columns);
 }
 
+constexpr float kMinTemperature = 0x1p-126f;  // log2(e) / T stays finite: 0 / T is 0
 cnr_status checked(const cnr_vocabulary *v, const cnr_targets *t) {
     if (!v || !t || !cnr_valid_float_type(v->type) || (t->token_type != CNR_IDX_I32 && t->token_type != CNR_IDX_I64)) return CNR_E_INVALID;
     if (v->hidden_stride < v->dim || v->weight_stride < v->dim || t->token_stride < t->top) return CNR_E_INVALID;

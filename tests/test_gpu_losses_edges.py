@@ -143,3 +143,27 @@ def test_top_values_are_the_rows_own_bits(ctx, kind, n, vocab, top):
     tokens, values, _ = P.top_logits(ctx, x, top)
     assert torch.equal(tokens, R.top(x, top)[0])
     assert torch.equal(values.view(whole), bits.gather(1, tokens.long()))
+
+
+def test_rows_that_are_laid_out_by_several_launches(ctx):
+    """More than 2^28 pieces of 16 bytes, of rows at an odd distance; the rows around the border and behind it are those with a gradient."""
+    n, vocab, dim = 131_200, 100, 16392
+    g = torch.Generator(device=DEV).manual_seed(1)
+    x = torch.empty(n, dim + 1, dtype=torch.bfloat16, device=DEV)[:, :dim]
+    for at in range(0, n, 8200):
+        x[at:at + 8200] = _normal(g, 8200, dim)
+    w = (_normal(g, vocab, dim) / 128.0).bfloat16()
+    targets, dloss = torch.randint(0, vocab, (n,), generator=g, device=DEV), torch.rand(n, generator=g, device=DEV)
+    border = (1 << 28) * 8 // (dim + 56)  # (whole blocks of 64 elements)
+    assert n - 1000 < border < n - 500
+    dloss[: border - 1000] = 0.0
+    loss = P.VocabularyLoss(ctx, vocab, dim, n)
+    losses = loss.cross_entropy(x, w, targets)
+    dx, dw = loss.backward(dloss)
+    for at in range(0, n, 8200):
+        part = slice(at, at + 8200)
+        _near(losses[part], R.loss(x[part], w, targets[part])["losses"], "losses")
+    assert not bool(dx[: border - 1000].any())
+    want = R.loss(x[border - 1000:], w, targets[border - 1000:], dloss=dloss[border - 1000:])
+    _near(dx[border - 1000:], want["dhidden"], "dhidden")
+    _near(dw, want["dweight"], "dweight")

@@ -193,3 +193,12 @@ def test_temperatures_that_1_cannot_be_divided_by_are_refused(name, temperature)
     assert _call(name, **(TEACHER | dict(temperature=temperature))) == INVALID
     # (what comes after the temperature's check)
     assert _call(name, **(TEACHER | dict(temperature=2.0 ** -126, tokens=A + 2))) == ALIGN
+
+
+def test_plans_at_the_limits_of_the_sizes(tmp_path):
+    """What the calls ask for of grids and workspaces, computed on the CPU from their own header."""
+    exe = str(tmp_path / "loss_plan")
+    subprocess.check_call(["g++", "-std=c++17", "-O1", "-Wall", "-D__HIP_PLATFORM_AMD__", "-isystem", "/opt/rocm/include", "-I", os.path.join(ROOT, "include"),
+                           "-I", os.path.join(ROOT, "paper_2010_08679_amd", "csrc"), os.path.join(ROOT, "tests", "c", "loss_plan.cpp"), "-o", exe])
+    out = subprocess.run([exe], capture_output=True, text=True)
+    assert out.returncode == 0, out.stdout + out.stderr

@@ -476,8 +476,9 @@ struct NarrowArgs {
     float *picked;
     const uint16_t *begins;    // soft: of the workgroups, as of tiles
     Entries entries;
-    // backward:
+    // backward, of a piece of the vocabulary:
     const RowGradient *rows;
+    uint32_t first;            // its first token
     float *dz;                 // [vocab][16 G], zeros in rows from n on
 };
 template <int TYPE>
@@ -579,7 +580,7 @@ __global__ void __launch_bounds__(kBlock, G > 2 ? 3 : 4) narrow_kernel(const Nar
             for (uint32_t g = 0; g < NF; ++g) {
                 const uint32_t v = n0 + 16 * g + n;
                 const float e = exp2_of(__builtin_fmaf(z[g], p.c, -r.lse2));
-                if (valid >> g & 1u) p.dz[(uint64_t)v * (16 * G) + row] = r.gradient == 0.0f ? 0.0f : r.gradient * (v == r.target ? e - 1.0f : e);
+                if (valid >> g & 1u) p.dz[(uint64_t)v * (16 * G) + row] = r.gradient == 0.0f ? 0.0f : r.gradient * (p.first + v == r.target ? e - 1.0f : e);
             }
         } else {
             const Stats s = stats16(z, p.c, valid);
@@ -744,7 +745,7 @@ __global__ void __launch_bounds__(kBlock) narrow_entries_kernel(const NarrowArgs
     const uint32_t at = wg_x() * kBlock + tid_x();
     if (at >= p.n * entries.top) return;
     const float q = entries.share[at];
-    const uint32_t row = at / entries.top, t = (uint32_t)entries.tokens[at];
+    const uint32_t row = at / entries.top, t = (uint32_t)entries.tokens[at] - p.first;
     const RowGradient r = p.rows[row];
     if (q == 0.0f || r.gradient == 0.0f || t >= p.vocab) return;
     p.dz[(uint64_t)t * padded + row] = r.gradient * (exp2_of(__builtin_fmaf(entries.picked[at], p.c, -r.lse2)) - q);
@@ -1095,7 +1096,7 @@ void forward(cnr_ctx *ctx, const cnr_vocabulary &v, const cnr_targets &t, float 
         if (f.n_parts == 0) {
         } else if (f.narrow) {
             const NarrowArgs a = {x, weight, v.hidden_stride, v.weight_stride, (uint32_t)rows, (uint32_t)v.vocab, (uint32_t)v.dim, c, parts, f.n_parts, t.logits != nullptr,
-                                  l.targets, picked, teacher.begins, entries, nullptr, nullptr};
+                                  l.targets, picked, teacher.begins, entries, nullptr, 0, nullptr};
             narrow<TYPE, false>(a, f.fragments, to);
         } else {
             const Terms terms = s.parts == 3 ? kOfFloats : kOne;
@@ -1162,48 +1163,53 @@ void narrow_backward(cnr_ctx *ctx, const cnr_vocabulary &v, const cnr_targets &t
     const TargetArgs targets = targets_of(t);
     RowGradient *rows = reinterpret_cast<RowGradient *>(space + b.rows);
     hipLaunchKernelGGL(rows_kernel, dim3(1), dim3(kRowThreads), 0, to, state, dloss, v.n, targets, v.vocab, 0, rows, reinterpret_cast<float *>(space + b.scale));
-    const uint32_t n = (uint32_t)v.n, vocab = (uint32_t)v.vocab, dim = (uint32_t)v.dim;
-    float *dz = reinterpret_cast<float *>(space + b.dz);
-    const NarrowArgs a = {v.hidden, v.weight, v.hidden_stride, v.weight_stride, n, vocab, dim, kLog2e / targets.temperature, nullptr, 0, false, targets, nullptr, nullptr, {}, rows, dz};
-    narrow<TYPE, true>(a, narrow_fragments(v.n, v.vocab), to);
-    if (t.logits && t.top)
-        hipLaunchKernelGGL(narrow_entries_kernel, dim3((unsigned)cnr_ceil_div(v.n * t.top, kBlock)), dim3(kBlock), 0, to, a, entries_of(state, v.n, t.top), (uint32_t)padded_rows(v.n));
-    // Sixteen waves to a compute unit, slabs of 64 tokens at least, parts of sums of up to a quarter of the room for them (they are read again).
+    const uint32_t n = (uint32_t)v.n, dim = (uint32_t)v.dim;
     const auto by_rows = [&](const auto &launch) {
         if (n <= 16) return launch(std::integral_constant<int, 1>());
         if constexpr (TYPE == CNR_FLOAT_F32) return n <= 32 ? launch(std::integral_constant<int, 2>()) : launch(std::integral_constant<int, 4>());
     };
+    const uint64_t stride = rounded(v.dim, 4), by_room = kPartBytes / 4 / (v.n * stride * sizeof(float));
+    const Target between = {space + b.sum, v.dim, CNR_FLOAT_F32}, none = {nullptr, 0, CNR_FLOAT_F32};
     SlabArgs s = {};
-    s.dz = dz;
-    s.vocab = vocab;
+    s.dz = reinterpret_cast<float *>(space + b.dz);
     s.dim = dim;
     s.n = n;
     s.groups = (uint32_t)cnr_ceil_div(v.dim, 64);
-    const uint64_t stride = rounded(v.dim, 4), wanted = least(cnr_ceil_div(16ull * ctx->n_cu, s.groups), cnr_ceil_div(v.vocab, 64));
-    const uint64_t by_room = kPartBytes / 4 / (v.n * stride * sizeof(float));
-    if (dhidden.out) {
-        s.slabs = (uint32_t)least(wanted, by_room ? by_room : 1);
-        s.matrix = v.weight;
-        s.stride = v.weight_stride;
-        s.partial = reinterpret_cast<float *>(space + b.partial);
-        s.partial_stride = stride;
-        by_rows([&](auto g) {
-            hipLaunchKernelGGL((narrow_hidden_kernel<TYPE, decltype(g)::value>), dim3((unsigned)cnr_ceil_div((uint64_t)s.groups * s.slabs, kWavesPerBlock)), dim3(kBlock), 0, to, s);
-        });
-        const KeepSum sum = {dhidden, {nullptr, 0, CNR_FLOAT_F32}, nullptr, s.partial, stride, rows};
-        hipLaunchKernelGGL((join_sums_kernel<16>), dim3((unsigned)cnr_ceil_div(v.n * (stride / 4), kBlock / 16)), dim3(kBlock), 0, to, sum, n, dim, s.slabs);
-    }
-    if (dweight.out) {
-        s.slabs = (uint32_t)wanted;
-        s.matrix = v.hidden;
-        s.stride = v.hidden_stride;
-        s.lse2 = state;
-        s.dloss = dloss;
-        s.out = dweight;
-        s.there = accumulate ? dweight : Target{nullptr, 0, CNR_FLOAT_F32};
-        by_rows([&](auto g) {
-            hipLaunchKernelGGL((narrow_weight_kernel<TYPE, decltype(g)::value>), dim3((unsigned)cnr_ceil_div((uint64_t)s.groups * s.slabs, kWavesPerBlock)), dim3(kBlock), 0, to, s);
-        });
+    for (uint64_t v0 = 0; v0 < v.vocab; v0 += b.piece) {
+        const uint64_t width = least(v.vocab - v0, b.piece);
+        const void *weight = reinterpret_cast<const typename Element<TYPE>::type *>(v.weight) + v0 * v.weight_stride;
+        const NarrowArgs a = {v.hidden, weight, v.hidden_stride, v.weight_stride, n, (uint32_t)width, dim, kLog2e / targets.temperature, nullptr, 0, false, targets, nullptr, nullptr, {},
+                              rows, (uint32_t)v0, reinterpret_cast<float *>(space + b.dz)};
+        narrow<TYPE, true>(a, narrow_fragments(v.n, width), to);
+        if (t.logits && t.top)
+            hipLaunchKernelGGL(narrow_entries_kernel, dim3((unsigned)cnr_ceil_div(v.n * t.top, kBlock)), dim3(kBlock), 0, to, a, entries_of(state, v.n, t.top), (uint32_t)padded_rows(v.n));
+        // Sixteen waves to a compute unit, slabs of 64 tokens at least, parts of sums of up to a quarter of the room for them (they are read again).
+        const uint64_t wanted = least(cnr_ceil_div(16ull * ctx->n_cu, s.groups), cnr_ceil_div(width, 64));
+        s.vocab = (uint32_t)width;
+        if (dhidden.out) {
+            s.slabs = (uint32_t)least(wanted, by_room ? by_room : 1);
+            s.matrix = weight;
+            s.stride = v.weight_stride;
+            s.partial = reinterpret_cast<float *>(space + b.partial);
+            s.partial_stride = stride;
+            by_rows([&](auto g) {
+                hipLaunchKernelGGL((narrow_hidden_kernel<TYPE, decltype(g)::value>), dim3((unsigned)cnr_ceil_div((uint64_t)s.groups * s.slabs, kWavesPerBlock)), dim3(kBlock), 0, to, s);
+            });
+            const KeepSum sum = {v0 + width == v.vocab ? dhidden : between, v0 ? between : none, nullptr, s.partial, stride, rows};
+            hipLaunchKernelGGL((join_sums_kernel<16>), dim3((unsigned)cnr_ceil_div(v.n * (stride / 4), kBlock / 16)), dim3(kBlock), 0, to, sum, n, dim, s.slabs);
+        }
+        if (dweight.out) {
+            s.slabs = (uint32_t)wanted;
+            s.matrix = v.hidden;
+            s.stride = v.hidden_stride;
+            s.lse2 = state;
+            s.dloss = dloss;
+            s.out = from_row(dweight, v0);
+            s.there = accumulate ? s.out : none;
+            by_rows([&](auto g) {
+                hipLaunchKernelGGL((narrow_weight_kernel<TYPE, decltype(g)::value>), dim3((unsigned)cnr_ceil_div((uint64_t)s.groups * s.slabs, kWavesPerBlock)), dim3(kBlock), 0, to, s);
+            });
+        }
     }
 }
 

@@ -31,7 +31,7 @@ constexpr uint32_t kTwoPartRows = 64;
 // (In the backward pass of larger weights that need not be laid out tiles are faster even then: a step of 16 x 32000 x 1024 85 -> 76 us, of 16 x 131072 x 4096
 // 1300 -> 955, but of 16 x 1249 x 6784 66 against 74.)
 constexpr uint64_t kTiledFrom = 1ull << 24;
-constexpr uint64_t kPieceBytes = 256ull << 20;  // of a piece of the weight, of its dz twice as many
+constexpr uint64_t kPieceBytes = 256ull << 20;  // of a piece of the weight, of its dz twice as many, up to the next multiple of 256 tokens
 constexpr uint64_t kPieceTokens = 1ull << 20;   // a row of its dz, in up to three parts, is below 2^23 bytes
 constexpr uint64_t kStatsBytes = 512ull << 20;  // of the stats of as many rows as go at a time
 constexpr uint64_t kPartBytes = 128ull << 20;   // of sums that are split
@@ -121,16 +121,20 @@ struct BackwardPlan {
     uint64_t piece, width;  // of the vocabulary; columns of dz, whole blocks
     uint64_t scale, rows, dz, hidden_at, weight_at, sum, partial, bytes;
 };
+// Tokens of a piece whose dz are held in fp32, for as many rows as the matrix instructions take.
+inline uint64_t narrow_piece(uint64_t n) { return 2 * kPieceBytes / (padded_rows(n) * sizeof(float)); }
 // (two: dweight in fp32 from 16-bit operands, by dz in two parts.  in_place: the weight is read where it is.)
 inline BackwardPlan backward_plan(const cnr_ctx *ctx, const Sizes &s, bool two, bool in_place) {
     BackwardPlan b = {};
     const uint32_t parts = dz_parts(s, two);
     b.narrow = s.n <= narrow_rows(s) && !(in_place && s.vocab * s.dim >= kTiledFrom) && s.n * rounded(s.dim, 4) * sizeof(float) <= kPartBytes;
     if (b.narrow) {
+        b.piece = least(s.vocab, narrow_piece(s.n));
         Room room;
         b.scale = room.take(2 * sizeof(float));
         b.rows = room.take(256 * sizeof(RowGradient));
-        b.dz = room.take(s.vocab * padded_rows(s.n) * sizeof(float));
+        b.dz = room.take(b.piece * padded_rows(s.n) * sizeof(float));
+        b.sum = room.take(b.piece < s.vocab ? s.n * s.dim * sizeof(float) : 0);
         b.partial = room.take(kPartBytes);
         b.bytes = room.used;
         return b;
@@ -177,7 +181,7 @@ inline uint64_t room_for(const Sizes &s, bool training, bool two) {
     const uint64_t few = least(s.n, kTwoPartRows) * 2 * (s.parts == 3 ? 3 : 2), vocab = rounded(s.vocab, dense::kBlockElements);
     uint64_t tiled = least(of_dz * vocab, 2 * kPieceBytes + 256 * of_dz);
     tiled = tiled > least(few * vocab, 2 * kPieceBytes + 256 * few) ? tiled : least(few * vocab, 2 * kPieceBytes + 256 * few);
-    const uint64_t narrow_dz = s.vocab * padded_rows(least(s.n, narrow_rows(s))) * sizeof(float);
+    const uint64_t narrow_dz = least(s.vocab * padded_rows(least(s.n, narrow_rows(s))) * sizeof(float), 2 * kPieceBytes);
     b.take(tiled > narrow_dz ? tiled : narrow_dz);
     b.take(s.n * s.row);
     b.take(most_weight * s.row);

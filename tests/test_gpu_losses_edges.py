@@ -167,3 +167,24 @@ def test_rows_that_are_laid_out_by_several_launches(ctx):
     want = R.loss(x[border - 1000:], w, targets[border - 1000:], dloss=dloss[border - 1000:])
     _near(dx[border - 1000:], want["dhidden"], "dhidden")
     _near(dw, want["dweight"], "dweight")
+
+
+@pytest.mark.parametrize("kind,n,vocab,dim,grad", [("bf16", 3, (1 << 23) + 300, 7, "bf16"), ("f16", 2, (1 << 23) + 17, 5, "f32"), ("f32", 40, (1 << 21) + 100, 8, "f32")])
+def test_few_rows_of_a_vocabulary_of_several_pieces(ctx, kind, n, vocab, dim, grad):
+    """Targets and entries on both sides of the border between the pieces of dz, onto a gradient that is there."""
+    piece = (1 << 23) if n <= 16 else 1 << 21
+    g, t = torch.Generator(device=DEV).manual_seed(n), TYPES[kind]
+    x, w = _normal(g, n, dim, 2.0).to(t), _normal(g, vocab, dim).to(t)
+    targets, dloss = torch.randint(0, vocab, (n,), generator=g, device=DEV), torch.rand(n, generator=g, device=DEV)
+    targets[0], targets[1] = piece, piece - 1
+    there = _normal(g, vocab, dim, 1e-3).to(TYPES[grad])
+    tokens = torch.stack([targets, targets.flip(0), torch.full_like(targets, vocab - 1), torch.full_like(targets, -1)], dim=1)
+    logits = _normal(g, n, 4)
+    loss = P.VocabularyLoss(ctx, vocab, dim, n, t, top=4, gradient_dtype=TYPES[grad])
+    assert loss._space.numel() < 3 << 29
+    for teacher in ((targets,), (tokens, logits, 2.0)):
+        want = R.loss(x, w, *teacher, dloss=dloss, there=there, parts=2 if grad != kind else 1)
+        _near(loss.cross_entropy(x, w, *teacher) if len(teacher) == 1 else loss.distill(x, w, *teacher), want["losses"], "losses")
+        dx, dw = loss.backward(dloss, dweight=there.clone(), accumulate=True)
+        _near(dx, want["dhidden"], "dhidden")
+        _near(dw, want["dweight"], "dweight")

@@ -91,9 +91,32 @@ def _loss_arguments(hidden, weight, tokens, logits, temperature: float):
             cnr_targets(tokens_at, token_type, token_stride, top, logits_at, logit_type, logit_stride, temperature))
 
 
-def _span(t):
-    """First byte and the one behind the last of a matrix."""
-    return t.data_ptr(), t.data_ptr() + ((t.shape[0] - 1) * t.stride(0) + t.shape[1]) * t.element_size()
+def _place(t):
+    """(address, rows, bytes of a row, bytes from one row to the next) of a matrix, None of an empty one."""
+    if t is None or not t.numel():
+        return None
+    size = t.element_size()
+    return t.data_ptr(), t.shape[0], t.shape[1] * size, t.stride(0) * size
+
+
+def _share(a, b) -> bool:
+    """Whether two places have a byte in common.  Column ranges of one matrix have none, though either's rows lie among the other's."""
+    if a is None or b is None:
+        return False
+    (at, n, width, step), (at_b, n_b, width_b, step_b) = a, b
+    by = at_b - at
+    if by >= (n - 1) * step + width or -by >= (n_b - 1) * step_b + width_b:
+        return False
+    if n > n_b:
+        return _share(b, a)
+    if n > 1 and step != step_b:
+        # each of the fewer rows among the other's
+        return any(_share((at + i * step, 1, width, 0), b) for i in range(n))
+    # rows i of a and j of b share bytes where -width_b < by + (j - i) step_b < width: the whole numbers k = j - i for which that holds
+    if n_b == 1:
+        return True
+    first, last = (-width_b - by) // step_b + 1, -((by - width) // step_b) - 1
+    return max(first, 1 - n) <= min(last, n_b - 1)
 
 
 def _bytes(t) -> int:
@@ -139,9 +162,8 @@ def cnr_vocabulary_loss_backward(ctx, hidden, weight, tokens, logits, temperatur
         to_weight, kind = L._rows(dweight, "dweight"), L._float(dweight, "dweight")
         if dweight.shape != weight.shape or kind not in (v.type, L.CNR_FLOAT_F32):
             raise ValueError("dweight must have the shape of weight and its type, or float32")
-    spans = [_span(t) for t in (dhidden, dweight, hidden, weight) if t is not None and t.numel()]
-    results = (dhidden is not None and dhidden.numel() > 0) + (dweight is not None and dweight.numel() > 0)
-    if any(a[0] < b[1] and b[0] < a[1] for i, a in enumerate(spans[:results]) for b in spans[i + 1:]):
+    places = [_place(t) for t in (dhidden, dweight, hidden, weight)]
+    if any(_share(a, b) for i, a in enumerate(places[:2]) for b in places[i + 1:]):
         raise ValueError("a result overlaps an operand or the other result")
     if _bytes(workspace) < cnr_loss_workspace_bytes(n, v.vocab, v.dim, v.type, True, kind):
         raise ValueError("workspace smaller than cnr_loss_workspace_bytes")

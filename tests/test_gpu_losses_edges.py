@@ -188,3 +188,25 @@ def test_few_rows_of_a_vocabulary_of_several_pieces(ctx, kind, n, vocab, dim, gr
         dx, dw = loss.backward(dloss, dweight=there.clone(), accumulate=True)
         _near(dx, want["dhidden"], "dhidden")
         _near(dw, want["dweight"], "dweight")
+
+
+@pytest.mark.parametrize("kind", list(TYPES))
+@pytest.mark.parametrize("n", [10, 200])
+def test_results_that_lie_between_the_operands_rows(ctx, kind, n):
+    """Column ranges of one matrix share nothing, whatever rows they have; one column more and they do."""
+    t, vocab, dim = TYPES[kind], 300, 64
+    g = torch.Generator(device=DEV).manual_seed(n)
+    states, table = _normal(g, n, 3 * dim).to(t), _normal(g, vocab, 2 * dim, 0.2).to(t)
+    x, w, dx, dw = states[:, :dim], table[:, dim:], states[:, dim:2 * dim], table[:, :dim]
+    before = states[:, 2 * dim:].clone()
+    targets, dloss = torch.randint(0, vocab, (n,), generator=g, device=DEV), torch.rand(n, generator=g, device=DEV)
+    want = R.loss(x.clone(), w.clone(), targets, dloss=dloss)
+    loss = P.VocabularyLoss(ctx, vocab, dim, n, t)
+    _near(loss.cross_entropy(x, w, targets), want["losses"], "losses")
+    for kw in (dict(dhidden=states[:, dim - 1:2 * dim - 1]), dict(dweight=table[:, 1:dim + 1]), dict(dhidden=table[:n, dim - 8:2 * dim - 8])):
+        with pytest.raises(ValueError, match="overlaps"):
+            loss.backward(dloss, **kw)
+    loss.backward(dloss, dx, dw)
+    _near(dx, want["dhidden"], "dhidden")
+    _near(dw, want["dweight"], "dweight")
+    assert torch.equal(states[:, 2 * dim:], before)

@@ -202,3 +202,30 @@ def test_plans_at_the_limits_of_the_sizes(tmp_path):
                            "-I", os.path.join(ROOT, "paper_2010_08679_amd", "csrc"), os.path.join(ROOT, "tests", "c", "loss_plan.cpp"), "-o", exe])
     out = subprocess.run([exe], capture_output=True, text=True)
     assert out.returncode == 0, out.stdout + out.stderr
+
+
+def test_places_that_share_bytes():
+    """Matrices in one memory, against the sets of their bytes."""
+    g = torch.Generator().manual_seed(1)
+
+    def place():
+        n, width, gap, at = (int(torch.randint(lo, hi, (), generator=g)) for lo, hi in ((1, 6), (1, 8), (0, 9), (0, 40)))
+        return at, n, width, width + gap if n > 1 else int(torch.randint(0, 9, (), generator=g))
+
+    def held(p):
+        at, n, width, step = p
+        return {at + i * step + j for i in range(n) for j in range(width)}
+
+    same = together = 0
+    for _ in range(4000):
+        a, b = place(), place()
+        if torch.randint(0, 2, (), generator=g) and a[1] > 1 and b[1] > 1 and a[3] >= b[2]:
+            b = (*b[:3], a[3])  # rows of one matrix
+            same += 1
+        share = bool(held(a) & held(b))
+        together += share
+        assert S._share(a, b) == S._share(b, a) == share, (a, b)
+    assert same > 300 and 500 < together < 3500
+    assert not S._share(None, (0, 1, 1, 1)) and not S._share((0, 1, 1, 1), None)
+    # large ones in no more time
+    assert not S._share((0, 1 << 20, 64, 128), (64, 1 << 20, 64, 128)) and S._share((0, 1 << 20, 64, 128), (63, 1 << 20, 64, 128))

@@ -7,7 +7,7 @@
  *   cnr_top_logits        the largest logits of each row, and the logarithm of the sum of all exponentials
  *
  * The general rules of cnr.h and cnr_lm.h hold: device pointers owned by the caller unless a comment says "host", work is only enqueued on `stream`, nothing
- * is allocated, infinities and NaN are ordinary inputs, sizes of zero succeed.
+ * is allocated, infinities and NaN are ordinary inputs, sizes of zero succeed.  Results, states that are written and workspaces overlap neither the operands nor each other.
  */
 #ifndef CNR_LOSS_H
 #define CNR_LOSS_H
@@ -75,7 +75,7 @@ cnr_status cnr_vocabulary_loss(cnr_ctx *ctx, const cnr_vocabulary *vocabulary /*
  * Logits are computed again, a piece of the vocabulary at a time.  dz passes through `type` between the products, rounded to it once; through two numbers of it
  * (relative 2^-16 for bfloat16, 2^-22 for half) where n is at most 64 or dweight is float, through three bfloat16 for floats.  Halves are scaled by
  * the power of two that takes the largest |dloss / T| to 2^13 to 2^14, so that small gradients are not lost.  Each result is rounded once, after its sum in
- * fp32.  A row with dloss 0 adds nothing, whatever it holds.  The results overlap neither the operands nor each other.
+ * fp32.  A row with dloss 0 adds nothing, whatever it holds.
  *   workspace    cnr_loss_workspace_bytes(n, vocab, dim, type, 1, dweight_type) bytes at least (dweight_type: `type` where dweight is NULL) */
 cnr_status cnr_vocabulary_loss_backward(cnr_ctx *ctx, const cnr_vocabulary *vocabulary /* host */, const cnr_targets *targets /* host */, const float *state,
                                         const float *dloss, void *dhidden, uint64_t dhidden_stride, void *dweight, cnr_float_type dweight_type,

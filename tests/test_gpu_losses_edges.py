@@ -210,3 +210,35 @@ def test_results_that_lie_between_the_operands_rows(ctx, kind, n):
     _near(dx, want["dhidden"], "dhidden")
     _near(dw, want["dweight"], "dweight")
     assert torch.equal(states[:, 2 * dim:], before)
+
+
+def test_results_that_overlap_what_is_read_are_refused(ctx):
+    n, vocab, dim = 20, 300, 64
+    g = torch.Generator(device=DEV).manual_seed(1)
+    x, w, targets = _normal(g, n, dim), _normal(g, vocab, dim, 0.2), torch.randint(0, vocab, (n,), generator=g, device=DEV)
+    tokens, logits, dloss = torch.randint(0, vocab, (n, 4), generator=g, device=DEV), _normal(g, n, 4), torch.ones(n, device=DEV)
+    loss = P.VocabularyLoss(ctx, vocab, dim, n, torch.float32, top=4)
+    for call in (lambda: loss.cross_entropy(x, w, targets, out=x.view(-1)[100:120]), lambda: loss.cross_entropy(x, w, targets, out=w.view(-1)[-20:]),
+                 lambda: loss.distill(x, w, tokens, logits, out=logits.view(-1)[3:23]), lambda: loss.cross_entropy(x, w, targets, out=loss._state[:20])):
+        with pytest.raises(ValueError, match="overlaps"):
+            call()
+    loss.cross_entropy(x, w, targets)
+    with pytest.raises(ValueError, match="overlaps"):
+        loss.backward(dloss, loss._space.view(torch.float32)[: n * dim].view(n, dim))
+    many = torch.zeros(n * dim, device=DEV)
+    with pytest.raises(ValueError, match="overlaps"):
+        loss.backward(many[50:50 + n], many.view(n, dim))
+    z = _normal(g, n, vocab)
+    room = torch.zeros(n * 8, device=DEV)
+    for kw in (dict(values=z.view(-1)[:n * 4].view(n, 4)), dict(lse=z[3, 5:5 + n]), dict(tokens=z.view(torch.int32).view(-1)[-n * 4:].view(n, 4)),
+               dict(values=room[: n * 4].view(n, 4), lse=room[n * 4 - 1: n * 5 - 1])):
+        with pytest.raises(ValueError, match="overlaps"):
+            P.top_logits(ctx, z, 4, **kw)
+    # side by side, between the rows, and operands that share memory
+    held = _normal(g, n, vocab + 8)
+    want = R.top(held[:, :vocab], 4)
+    got = P.top_logits(ctx, held[:, :vocab], 4, values=room[: n * 4].view(n, 4), lse=room[n * 4: n * 5])
+    assert torch.equal(got[0], want[0]) and torch.equal(room[: n * 4].view(n, 4), want[1])
+    got = P.top_logits(ctx, held[:1, :vocab], 8, values=held.view(-1)[vocab: vocab + 8].view(1, 8))
+    assert torch.equal(got[1], R.top(held[:1, :vocab], 8)[1])
+    _near(loss.cross_entropy(w[5:5 + n], w, targets), R.loss(w[5:5 + n], w, targets)["losses"], "losses")

@@ -226,6 +226,6 @@ def test_places_that_share_bytes():
         together += share
         assert S._share(a, b) == S._share(b, a) == share, (a, b)
     assert same > 300 and 500 < together < 3500
-    assert not S._share(None, (0, 1, 1, 1)) and not S._share((0, 1, 1, 1), None)
+    assert not S._share((0, 0, 1, 1), (0, 1, 1, 1)) and not S._share((0, 1, 1, 1), (0, 4, 0, 1))
     # large ones in no more time
     assert not S._share((0, 1 << 20, 64, 128), (64, 1 << 20, 64, 128)) and S._share((0, 1 << 20, 64, 128), (63, 1 << 20, 64, 128))

@@ -239,7 +239,8 @@ class VocabularyLoss(_Holder):
 
     The object keeps a workspace and, from a loss in training to :meth:`backward`, what that loss was made of: its tensors must stay as they are until then.
     ``gradient_dtype``: the type of the weight's gradient, ``dtype`` or float32 (which costs a second product where ``dtype`` has 16 bits).
-    It is no autograd function: results have no history, gradients are what :meth:`backward` returns.  A second loss in training takes the place of the first.
+    It is no autograd function: results have no history, gradients are what :meth:`backward` returns.  A second loss in training, or any distillation, takes the
+    place of the first; a call that is refused does not.
     Calls of one object belong on one stream."""
 
     def __init__(self, ctx, vocab: int, dim: int, max_tokens: int, dtype=torch.bfloat16, top: int = 1, training: bool = True, gradient_dtype=None, device="cuda:0"):
@@ -272,10 +273,14 @@ class VocabularyLoss(_Holder):
         if out is None:
             with _on(stream):
                 out = torch.empty(hidden.shape[0], dtype=torch.float32, device=hidden.device)
-        if training or logits is not None:  # the state is another's from here on
+        state, last = self._state if training or logits is not None else None, self._last
+        if state is not None:  # another's from here on
             self._last = None
-        S.cnr_vocabulary_loss(self.ctx, hidden, weight, tokens, logits, temperature, out, self._state if training or logits is not None else None, self._space,
-                              stream)
+        try:
+            S.cnr_vocabulary_loss(self.ctx, hidden, weight, tokens, logits, temperature, out, state, self._space, stream)
+        except (TypeError, ValueError):  # refused: nothing was written
+            self._last = last
+            raise
         if training:
             self._last = (hidden, weight, tokens, logits, temperature)
         return out

@@ -229,3 +229,14 @@ def test_places_that_share_bytes():
     assert not S._share((0, 0, 1, 1), (0, 1, 1, 1)) and not S._share((0, 1, 1, 1), (0, 4, 0, 1))
     # large ones in no more time
     assert not S._share((0, 1 << 20, 64, 128), (64, 1 << 20, 64, 128)) and S._share((0, 1 << 20, 64, 128), (63, 1 << 20, 64, 128))
+
+
+def test_a_refused_loss_leaves_the_one_before_to_its_backward_pass():
+    x, w, t = torch.zeros(4, 8), torch.zeros(10, 8), torch.zeros(4, dtype=torch.int64)
+    loss = P.VocabularyLoss(None, 10, 8, 4, torch.float32, top=3, device="cpu")
+    loss._last = before = (x, w, t, None, 1.0)
+    for call in (lambda: loss.cross_entropy(x, w, t), lambda: loss.distill(x, w, t[:, None], torch.zeros(4, 1)), lambda: loss.cross_entropy(x, w, t, training=False),
+                 lambda: loss.cross_entropy(x.half(), w, t), lambda: loss.cross_entropy(x, w[:9], t)):
+        with pytest.raises((TypeError, ValueError)):
+            call()
+        assert loss._last is before

@@ -1,4 +1,5 @@
-"""Losses over the vocabulary and top logits at the edges of their values: certain tokens."""
+"""Losses over the vocabulary and top logits at the edges of their values, sizes and places: certain tokens, small floats, infinite weights, rows and vocabularies that go by pieces,
+results next to operands."""
 import math
 
 import pytest
@@ -242,3 +243,31 @@ def test_results_that_overlap_what_is_read_are_refused(ctx):
     got = P.top_logits(ctx, held[:1, :vocab], 8, values=held.view(-1)[vocab: vocab + 8].view(1, 8))
     assert torch.equal(got[1], R.top(held[:1, :vocab], 8)[1])
     _near(loss.cross_entropy(w[5:5 + n], w, targets), R.loss(w[5:5 + n], w, targets)["losses"], "losses")
+
+
+# floats of 17 to 64 rows by two fragments of a large vocabulary; weights that are laid out a piece at a time in the forward pass, floats and rows at an odd distance
+PIECES = [("f32", 24, 20000, 136, 0, None), ("f32", 50, 20001, 72, 0, None), ("f32", 17, 16400, 33, 1, None), ("f32", 70, 720_000, 40, 0, 699_136), ("f32", 130, 720_000, 8, 0, 699_136),
+          ("bf16", 20, 2_098_000, 8, 1, 1 << 21), ("f16", 90, 2_098_000, 9, 0, 1 << 21)]
+
+
+@pytest.mark.parametrize("kind,n,vocab,dim,pad,border", PIECES)
+def test_steps_of_few_rows_of_floats_and_of_weights_in_pieces(ctx, kind, n, vocab, dim, pad, border):
+    """Targets and entries on both sides of the border between two pieces."""
+    g, t = torch.Generator(device=DEV).manual_seed(n), TYPES[kind]
+    x, w = _normal(g, n, dim + pad, 2.0).to(t)[:, :dim], _normal(g, vocab, dim + pad, 1.0 / math.sqrt(dim)).to(t)[:, :dim]
+    targets, dloss = torch.randint(0, vocab, (n,), generator=g, device=DEV), torch.rand(n, generator=g, device=DEV)
+    tokens = torch.randint(0, vocab, (n, 20), generator=g, device=DEV)
+    if border is not None:
+        targets[::3], targets[1::3] = border - 1, border
+        tokens[1::2] = border - 10 + torch.arange(20, device=DEV)
+        tokens[::5] = border - 1
+    tokens[-1, 3:] = -1
+    logits = _normal(g, n, 20, 3.0)
+    loss = P.VocabularyLoss(ctx, vocab, dim, n, t, top=20)
+    for teacher in ((targets,), (tokens, logits, 2.0)):
+        losses = loss.cross_entropy(x, w, *teacher) if len(teacher) == 1 else loss.distill(x, w, *teacher)
+        dx, dw = loss.backward(dloss)
+        want = R.loss(x, w, *teacher, dloss=dloss)
+        _near(losses, want["losses"], "losses")
+        _near(dx, want["dhidden"], "dhidden")
+        _near(dw, want["dweight"], "dweight")

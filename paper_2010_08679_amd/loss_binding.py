@@ -117,10 +117,10 @@ def _share(a, b) -> bool:
 def _check_apart(results, operands) -> None:
     """Results' places share no byte with operands' or each other; operands may."""
     last = 0
-    for first, end in sorted([(at, at + (n - 1) * step + width) for at, n, width, step in results + operands]):
-        if first < last:
+    for at, n, width, step in sorted(results + operands):
+        if at < last:
             break
-        last = end if end > last else last
+        last = at + (n - 1) * step + width
     else:
         return
     if any(_share(a, b) for i, a in enumerate(results) for b in results[i + 1:] + operands):

@@ -474,8 +474,7 @@ struct NarrowArgs {
     bool soft;
     TargetArgs targets;        // not soft
     float *picked;
-    const uint16_t *begins;    // soft: of the workgroups, as of tiles
-    Entries entries;
+    Entries entries;           // soft
     // backward, of a piece of the vocabulary:
     const RowGradient *rows;
     uint32_t first;            // its first token
@@ -599,16 +598,20 @@ __global__ void __launch_bounds__(kBlock, G > 2 ? 3 : 4) narrow_kernel(const Nar
     if constexpr (!GRADIENT) {
         if (!p.soft) return;
         __syncthreads();
+        // A row's threads look at every sixteenth part of its entries, which are in order, then go on from the last that begins below these columns.  (With a
+        // list of where each workgroup's entries begin, as tiles have one, a loss of 1 x 262144 x 64 took 33 us instead of 29: one workgroup writes it.)
+        const uint32_t top = p.entries.top, part = (top + 15) / 16;
 #pragma unroll
         for (uint32_t f = 0; f < G; ++f) {
             const uint32_t row = 16 * f + m;
             if (row >= p.n) continue;
-            const uint16_t *b = p.begins + (uint64_t)row * (p.n_parts + 1) + wg_x();
-            const uint32_t begin = b[0], end = b[1];
-            for (uint32_t e = begin + n; e < end; e += 16) {
-                const uint64_t entry = (uint64_t)row * p.entries.top + e;
-                const uint32_t column = (uint32_t)p.entries.tokens[entry] - n0;
-                if (column < 16 * NF) p.entries.picked[entry] = sums[0][f * NF + column / 16][m / 4 * 16 + column % 16][m % 4];
+            const uint64_t entry = (uint64_t)row * top;
+            auto among_row = [&](bool is) { return (uint32_t)(__ballot(is) >> lane / 16 * 16) & 0xffffu; };
+            const uint32_t below = (uint32_t)__popc(among_row(n * part < top && (uint32_t)p.entries.tokens[entry + n * part] < n0));
+            for (uint32_t e = (below ? below - 1 : 0) * part + n;; e += 16) {
+                const uint32_t token = e < top ? (uint32_t)p.entries.tokens[entry + e] : (uint32_t)kNoToken, column = token - n0;
+                if (column < 16 * NF && e < top) p.entries.picked[entry + e] = sums[0][f * NF + column / 16][m / 4 * 16 + column % 16][m % 4];
+                if (among_row(token >= n0 + 16 * NF)) break;
             }
         }
     }
@@ -834,19 +837,15 @@ __global__ void __launch_bounds__(kBlock) teacher_kernel(const TeacherArgs p) {
         p.lse2[row] = counts ? 0.0f : __builtin_inff();
     }
     if (!p.begins) return;
-    // A share of the tiles to a thread: it looks for the first one's first entry, whose token is not below, and goes on from there.
-    const uint64_t each = (p.n_parts + kBlock) / kBlock, tile0 = tid_x() * each;
-    uint32_t lo = 0, hi = top;
-    while (lo < hi) {
-        const uint32_t middle = (lo + hi) / 2;
-        if ((uint64_t)(uint32_t)sorted[middle] < tile0 * p.columns)
-            lo = middle + 1;
-        else
-            hi = middle;
-    }
-    uint64_t next = lo < top ? (uint32_t)sorted[lo] : ~0ull;
-    for (uint64_t tile = tile0; tile < tile0 + each && tile <= p.n_parts; ++tile) {
-        while (next < tile * p.columns) next = ++lo < top ? (uint32_t)sorted[lo] : ~0ull;
+    for (uint64_t tile = tid_x(); tile <= p.n_parts; tile += kBlock) {
+        uint32_t lo = 0, hi = top;  // the first entry whose token is not below
+        while (lo < hi) {
+            const uint32_t middle = (lo + hi) / 2;
+            if ((uint64_t)(uint32_t)sorted[middle] < tile * p.columns)
+                lo = middle + 1;
+            else
+                hi = middle;
+        }
         // (behind the last tile lie those without a token)
         p.begins[(uint64_t)wg_x() * (p.n_parts + 1) + tile] = (uint16_t)lo;
     }
@@ -1082,7 +1081,8 @@ void forward(cnr_ctx *ctx, const cnr_vocabulary &v, const cnr_targets &t, float 
     l.err = ctx->dev_err;
     const float c = l.c = kLog2e / l.targets.temperature;
     const uint32_t columns = f.narrow ? 16 * f.fragments : dense::kTiles[f.tiles.kind].columns;
-    TeacherArgs teacher = {l.targets, v.vocab, 0, l.entries, loss, state, v.vocab ? reinterpret_cast<uint16_t *>(space + f.begins) : nullptr, f.n_parts, columns, ctx->dev_err};
+    TeacherArgs teacher = {l.targets, v.vocab, 0, l.entries, loss, state, f.narrow || !v.vocab ? nullptr : reinterpret_cast<uint16_t *>(space + f.begins), f.n_parts, columns,
+                           ctx->dev_err};
     for (uint64_t row0 = 0; row0 < v.n; row0 += f.rows) {
         const uint64_t rows = v.n - row0 < f.rows ? v.n - row0 : f.rows;
         Stats *parts = reinterpret_cast<Stats *>(space + f.parts);
@@ -1096,7 +1096,7 @@ void forward(cnr_ctx *ctx, const cnr_vocabulary &v, const cnr_targets &t, float 
         if (f.n_parts == 0) {
         } else if (f.narrow) {
             const NarrowArgs a = {x, weight, v.hidden_stride, v.weight_stride, (uint32_t)rows, (uint32_t)v.vocab, (uint32_t)v.dim, c, parts, f.n_parts, t.logits != nullptr,
-                                  l.targets, picked, teacher.begins, entries, nullptr, 0, nullptr};
+                                  l.targets, picked, entries, nullptr, 0, nullptr};
             narrow<TYPE, false>(a, f.fragments, to);
         } else {
             const Terms terms = s.parts == 3 ? kOfFloats : kOne;
@@ -1178,7 +1178,7 @@ void narrow_backward(cnr_ctx *ctx, const cnr_vocabulary &v, const cnr_targets &t
     for (uint64_t v0 = 0; v0 < v.vocab; v0 += b.piece) {
         const uint64_t width = least(v.vocab - v0, b.piece);
         const void *weight = reinterpret_cast<const typename Element<TYPE>::type *>(v.weight) + v0 * v.weight_stride;
-        const NarrowArgs a = {v.hidden, weight, v.hidden_stride, v.weight_stride, n, (uint32_t)width, dim, kLog2e / targets.temperature, nullptr, 0, false, targets, nullptr, nullptr, {},
+        const NarrowArgs a = {v.hidden, weight, v.hidden_stride, v.weight_stride, n, (uint32_t)width, dim, kLog2e / targets.temperature, nullptr, 0, false, targets, nullptr, {},
                               rows, (uint32_t)v0, reinterpret_cast<float *>(space + b.dz)};
         narrow<TYPE, true>(a, narrow_fragments(v.n, width), to);
         if (t.logits && t.top)

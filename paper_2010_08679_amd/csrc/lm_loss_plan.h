@@ -28,9 +28,10 @@ constexpr uint32_t kNarrowRowsOfFloats = 64;
 // Up to how many rows of 16 bits dz is held in two parts, whatever the results' type: products that are bound by reading the weight and by writing its gradient
 // nearly have the time (a step of 32 x 131072 x 4096 941 -> 1013 us), and sums of few rows do not average roundings.
 constexpr uint32_t kTwoPartRows = 64;
-// (In the backward pass of larger weights that need not be laid out tiles are faster even then: a step of 16 x 32000 x 1024 85 -> 76 us, of 16 x 131072 x 4096
-// 1300 -> 955, but of 16 x 1249 x 6784 66 against 74.)
-constexpr uint64_t kTiledFrom = 1ull << 24;
+// In the backward pass of larger weights that need not be laid out tiles are faster even for few rows: a step of 16 x 131072 x 4096 in bfloat16 1249 -> 1022 us, of 1 row
+// 1197 -> 983, of 16 x 32000 x 2048 142 -> 133; 16 x 32000 x 1024 83.8 and 83.0, 16 x 16384 x 1024 55.8 and 55.1; but of 16 x 131072 x 256 89 against 113, of 16 x 131072 x 128
+// 73 against 94, of 16 x 1249 x 6784 62 against 77.
+constexpr uint64_t kTiledFrom = 3ull << 24;
 constexpr uint64_t kPieceBytes = 256ull << 20;  // of a piece of the weight, of its dz twice as many, up to the next multiple of 256 tokens
 constexpr uint64_t kPieceTokens = 1ull << 20;   // a row of its dz, in up to three parts, is below 2^23 bytes
 constexpr uint64_t kStatsBytes = 512ull << 20;  // of the stats of as many rows as go at a time

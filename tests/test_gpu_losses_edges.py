@@ -245,9 +245,9 @@ def test_results_that_overlap_what_is_read_are_refused(ctx):
     _near(loss.cross_entropy(w[5:5 + n], w, targets), R.loss(w[5:5 + n], w, targets)["losses"], "losses")
 
 
-# floats of 17 to 64 rows by two fragments of a large vocabulary; weights that are laid out a piece at a time in the forward pass, floats and rows at an odd distance
+# floats of 17 to 64 rows by two fragments of a large vocabulary, few rows and a large weight; weights that are laid out a piece at a time in the forward pass, floats and rows at an odd distance
 PIECES = [("f32", 24, 20000, 136, 0, None), ("f32", 50, 20001, 72, 0, None), ("f32", 17, 16400, 33, 1, None), ("f32", 70, 720_000, 40, 0, 699_136), ("f32", 130, 720_000, 8, 0, 699_136),
-          ("bf16", 20, 2_098_000, 8, 1, 1 << 21), ("f16", 90, 2_098_000, 9, 0, 1 << 21)]
+          ("bf16", 20, 2_098_000, 8, 1, 1 << 21), ("f16", 90, 2_098_000, 9, 0, 1 << 21), ("bf16", 16, 99_000, 512, 0, None), ("f16", 1, 99_000, 512, 0, None)]
 
 
 @pytest.mark.parametrize("kind,n,vocab,dim,pad,border", PIECES)

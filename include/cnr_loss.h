@@ -21,8 +21,8 @@ extern "C" {
 /* The logits z[i][v] = sum over t < dim of hidden[i][t] * weight[v][t], of which a vocabulary's losses are made; a host struct, read during the call.
  *   hidden, weight  float, bfloat16 or half [n][dim] and [vocab][dim] as `type` says, aligned to their element, rows
  *                   hidden_stride and weight_stride >= dim elements apart.  Products and sums are fp32's.  Rows of 16 bits of a multiple of 8
- *                   elements, 16 bytes aligned, are read where they are by more than 16 rows; others are laid out in the workspace first.  Floats are
- *                   multiplied in three parts of 8 bits: six of nine products, off by 2^-21 of the product at most and 2^-24 on average, and by 2^-131
+ *                   elements, 16 bytes aligned, are read where they are by more than 16 rows; others are laid out in the workspace first.  Floats of
+ *                   more than 64 rows are multiplied in three parts of 8 bits: six of nine products, off by 2^-21 of the product at most and 2^-24 on average, and by 2^-131
  *                   of either factor, which is more only next to a float below 2^-110 */
 typedef struct {
     const void *hidden;
@@ -72,10 +72,11 @@ cnr_status cnr_vocabulary_loss(cnr_ctx *ctx, const cnr_vocabulary *vocabulary /*
  *   dz[i][v] = dloss[i] / T * (exp(z[i][v] / T - lse) - sum of the q_j with tokens[j] = v)
  *   dhidden  NULL, or [n][dim] of `type`: dz weight
  *   dweight  NULL, or [vocab][dim] of dweight_type, `type` or float: dz^T hidden, added to what is there where accumulate is not 0
- * Logits are computed again, a piece of the vocabulary at a time.  dz passes through `type` between the products, rounded to it once; through two numbers of it
- * (relative 2^-16 for bfloat16, 2^-22 for half) where n is at most 64 or dweight is float, through three bfloat16 for floats.  Halves are scaled by
- * the power of two that takes the largest |dloss / T| to 2^13 to 2^14, so that small gradients are not lost.  Each result is rounded once, after its sum in
- * fp32.  A row with dloss 0 adds nothing, whatever it holds.
+ * Logits are computed again, a piece of the vocabulary at a time.  Between the products dz is rounded to `type` once; where n is at most 64 or dweight is float it is two
+ * numbers of `type` (off by 2^-17 of it for bfloat16, 2^-23 for half; dhidden of more than 64 rows takes the first); three bfloat16 for floats, and for bfloat16 up to n = 128 where
+ * dweight is float.  Few rows (up to 16, up to 64 of floats) keep it in fp32, but for bfloat16 and half next to a weight of 3 * 2^24 elements or more that is read where it is.
+ * Halves are scaled by the power of two that takes the largest |dloss / T| to 2^13 to 2^14, so that small gradients are not lost.  Each result is rounded once, after its sum in
+ * fp32.  A row with dloss 0 adds nothing, whatever it holds; a dloss that is infinite or NaN makes gradients infinite or NaN.
  *   workspace    cnr_loss_workspace_bytes(n, vocab, dim, type, 1, dweight_type) bytes at least (dweight_type: `type` where dweight is NULL) */
 cnr_status cnr_vocabulary_loss_backward(cnr_ctx *ctx, const cnr_vocabulary *vocabulary /* host */, const cnr_targets *targets /* host */, const float *state,
                                         const float *dloss, void *dhidden, uint64_t dhidden_stride, void *dweight, cnr_float_type dweight_type,

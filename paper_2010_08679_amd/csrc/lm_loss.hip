@@ -1220,7 +1220,8 @@ void backward(cnr_ctx *ctx, const cnr_vocabulary &v, const cnr_targets &t, const
     typedef typename Element<kOf<TYPE>>::type Part;
     const Sizes s = sizes_of(v.n, v.vocab, v.dim, v.type);
     const bool in_place = whole_rows(v.type, v.weight, v.weight_stride, v.dim, v.vocab);
-    const BackwardPlan b = backward_plan(ctx, s, PARTS == 2, in_place);
+    const bool wide = TYPE != CNR_FLOAT_F32 && dweight && dweight_type == CNR_FLOAT_F32;
+    const BackwardPlan b = backward_plan(ctx, s, wide, in_place);
     uint8_t *space = reinterpret_cast<uint8_t *>(workspace);
     if (b.narrow)
         return narrow_backward<TYPE>(ctx, v, t, state, dloss, {dhidden, dhidden_stride, v.type}, {dweight, dweight_stride, dweight_type}, accumulate, b, space, to);
@@ -1245,7 +1246,8 @@ void backward(cnr_ctx *ctx, const cnr_vocabulary &v, const cnr_targets &t, const
     sum.partial_stride = rounded(v.dim, 4);
     const Target between = {space + b.sum, v.dim, CNR_FLOAT_F32}, none = {nullptr, 0, CNR_FLOAT_F32};
     // (two parts for the hidden states too where rows are few)
-    const Terms logits = PARTS == 3 ? kOfFloats : kOne, to_hidden = PARTS == 2 && v.n <= kTwoPartRows ? kOfTwoParts : logits, to_weight = PARTS == 3 ? kOfFloats : PARTS == 2 ? kOfTwoParts : kOne;
+    const Terms logits = TYPE == CNR_FLOAT_F32 ? kOfFloats : kOne, to_hidden = TYPE != CNR_FLOAT_F32 && v.n <= kTwoPartRows ? kOfTwoParts : logits;
+    const Terms to_weight = TYPE == CNR_FLOAT_F32 ? kOfFloats : PARTS == 3 ? kOfThreeParts : PARTS == 2 ? kOfTwoParts : kOne;
     const uint32_t n = (uint32_t)v.n, dim = (uint32_t)v.dim;
     for (uint64_t v0 = 0; v0 < v.vocab; v0 += b.piece) {
         const uint32_t width = (uint32_t)(v.vocab - v0 < b.piece ? v.vocab - v0 : b.piece), blocks = (uint32_t)cnr_ceil_div(width, dense::kBlockElements);
@@ -1351,8 +1353,10 @@ cnr_status cnr_vocabulary_loss_backward(cnr_ctx *ctx, const cnr_vocabulary *voca
         if (dweight && !accumulate) zeros({dweight, dweight_stride, dweight_type}, v.vocab, v.dim, to);
         return cnr_launch_status(ctx);
     }
-    const bool low = (dweight && dweight_type == CNR_FLOAT_F32) || v.n <= kTwoPartRows;
-    if (backward_plan(ctx, sizes_of(v.n, v.vocab, v.dim, v.type), low && v.type != CNR_FLOAT_F32, whole_rows(v.type, v.weight, v.weight_stride, v.dim, v.vocab)).bytes > workspace_bytes)
+    const bool wide = v.type != CNR_FLOAT_F32 && dweight && dweight_type == CNR_FLOAT_F32;
+    const Sizes sizes = sizes_of(v.n, v.vocab, v.dim, v.type);
+    const uint32_t parts = dz_parts(sizes, wide);
+    if (backward_plan(ctx, sizes, wide, whole_rows(v.type, v.weight, v.weight_stride, v.dim, v.vocab)).bytes > workspace_bytes)
         return CNR_E_INVALID;
     auto call = [&](auto kind, auto part) {
         backward<decltype(kind)::value, decltype(part)::value>(ctx, v, *targets, state, dloss, dhidden, dhidden_stride, dweight, dweight_type, dweight_stride, accumulate != 0,
@@ -1361,11 +1365,12 @@ cnr_status cnr_vocabulary_loss_backward(cnr_ctx *ctx, const cnr_vocabulary *voca
     if (v.type == CNR_FLOAT_F32)
         call(std::integral_constant<int, CNR_FLOAT_F32>(), std::integral_constant<int, 3>());
     else if (v.type == CNR_FLOAT_BF16)
-        low ? call(std::integral_constant<int, CNR_FLOAT_BF16>(), std::integral_constant<int, 2>())
-            : call(std::integral_constant<int, CNR_FLOAT_BF16>(), std::integral_constant<int, 1>());
+        parts == 3   ? call(std::integral_constant<int, CNR_FLOAT_BF16>(), std::integral_constant<int, 3>())
+        : parts == 2 ? call(std::integral_constant<int, CNR_FLOAT_BF16>(), std::integral_constant<int, 2>())
+                     : call(std::integral_constant<int, CNR_FLOAT_BF16>(), std::integral_constant<int, 1>());
     else
-        low ? call(std::integral_constant<int, CNR_FLOAT_F16>(), std::integral_constant<int, 2>())
-            : call(std::integral_constant<int, CNR_FLOAT_F16>(), std::integral_constant<int, 1>());
+        parts == 2 ? call(std::integral_constant<int, CNR_FLOAT_F16>(), std::integral_constant<int, 2>())
+                   : call(std::integral_constant<int, CNR_FLOAT_F16>(), std::integral_constant<int, 1>());
     return cnr_launch_status(ctx);
 }
 

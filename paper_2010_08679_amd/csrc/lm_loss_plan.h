@@ -28,6 +28,9 @@ constexpr uint32_t kNarrowRowsOfFloats = 64;
 // Up to how many rows of 16 bits dz is held in two parts, whatever the results' type: products that are bound by reading the weight and by writing its gradient
 // nearly have the time (a step of 32 x 131072 x 4096 941 -> 1013 us), and sums of few rows do not average roundings.
 constexpr uint32_t kTwoPartRows = 64;
+// And up to how many rows of bfloat16 in three parts for a gradient in fp32, which is then as exact as by dz in fp32 (two parts: off by 2.5e-6, sums in fp32 by 3e-7): a step of
+// 64 x 131072 x 1024 409 -> 431 us, of 128 x 75456 x 602 240 -> 255, but of 333 x 50257 x 1024 286 -> 333, of 8192 x 32000 x 4096 8280 -> 10490.
+constexpr uint32_t kThreePartRows = 128;
 // In the backward pass of larger weights that need not be laid out tiles are faster even for few rows: a step of 16 x 131072 x 4096 in bfloat16 1249 -> 1022 us, of 1 row
 // 1197 -> 983, of 16 x 32000 x 2048 142 -> 133; 16 x 32000 x 1024 83.8 and 83.0, 16 x 16384 x 1024 55.8 and 55.1; but of 16 x 131072 x 256 89 against 113, of 16 x 131072 x 128
 // 73 against 94, of 16 x 1249 x 6784 62 against 77.
@@ -71,7 +74,7 @@ inline Sizes sizes_of(uint64_t n, uint64_t vocab, uint64_t dim, cnr_float_type t
 struct Terms {
     uint32_t number, across, down;
 };
-constexpr Terms kOne = {1, 0, 0}, kOfFloats = {6, 0x001012, 0x010210}, kOfTwoParts = {2, 0, 0x01};
+constexpr Terms kOne = {1, 0, 0}, kOfFloats = {6, 0x001012, 0x010210}, kOfTwoParts = {2, 0, 0x01}, kOfThreeParts = {3, 0, 0x012};
 
 // Of a row: its stats, and where the entries of each tile begin.
 inline uint64_t part_bytes(uint64_t n_parts) { return n_parts * sizeof(Stats) + (n_parts + 1) * sizeof(uint16_t); }
@@ -116,7 +119,11 @@ inline ForwardPlan forward_plan(const cnr_ctx *ctx, const Sizes &s) {
     return f;
 }
 
-inline uint32_t dz_parts(const Sizes &s, bool two) { return s.parts == 3 ? 3 : two || s.n <= kTwoPartRows ? 2 : 1; }
+// (wide: dweight in fp32 from 16-bit operands)
+inline uint32_t dz_parts(const Sizes &s, bool wide) {
+    if (s.parts == 3 || (wide && s.type == CNR_FLOAT_BF16 && s.n <= kThreePartRows)) return 3;
+    return wide || s.n <= kTwoPartRows ? 2 : 1;
+}
 struct BackwardPlan {
     bool narrow;
     uint64_t piece, width;  // of the vocabulary; columns of dz, whole blocks
@@ -124,10 +131,10 @@ struct BackwardPlan {
 };
 // Tokens of a piece whose dz are held in fp32, for as many rows as the matrix instructions take.
 inline uint64_t narrow_piece(uint64_t n) { return 2 * kPieceBytes / (padded_rows(n) * sizeof(float)); }
-// (two: dweight in fp32 from 16-bit operands, by dz in two parts.  in_place: the weight is read where it is.)
-inline BackwardPlan backward_plan(const cnr_ctx *ctx, const Sizes &s, bool two, bool in_place) {
+// (wide: see dz_parts.  in_place: the weight is read where it is.)
+inline BackwardPlan backward_plan(const cnr_ctx *ctx, const Sizes &s, bool wide, bool in_place) {
     BackwardPlan b = {};
-    const uint32_t parts = dz_parts(s, two);
+    const uint32_t parts = dz_parts(s, wide);
     b.narrow = s.n <= narrow_rows(s) && !(in_place && s.vocab * s.dim >= kTiledFrom) && s.n * rounded(s.dim, 4) * sizeof(float) <= kPartBytes;
     if (b.narrow) {
         b.piece = least(s.vocab, narrow_piece(s.n));
@@ -162,7 +169,7 @@ inline BackwardPlan backward_plan(const cnr_ctx *ctx, const Sizes &s, bool two, 
 }
 
 // At least what the plans take for n rows or fewer: each part's largest size.
-inline uint64_t room_for(const Sizes &s, bool training, bool two) {
+inline uint64_t room_for(const Sizes &s, bool training, bool wide) {
     const uint64_t most_weight = least(s.vocab, rounded(kPieceBytes / s.row, 256)), small = least(s.n, 256);
     Room f;
     const uint64_t stats = part_bytes(cnr_ceil_div(s.vocab, 64)), narrow = least(s.n, narrow_rows(s)) * part_bytes(cnr_ceil_div(s.vocab, 16));
@@ -176,10 +183,10 @@ inline uint64_t room_for(const Sizes &s, bool training, bool two) {
     }
     if (!training) return f.used;
     Room b;
-    const uint64_t of_dz = s.n * 2 * dz_parts(s, two);
+    const uint64_t of_dz = s.n * 2 * dz_parts(s, wide);
     b.take(2 * sizeof(float));
     b.take(rounded(s.n, 256) * sizeof(RowGradient));
-    const uint64_t few = least(s.n, kTwoPartRows) * 2 * (s.parts == 3 ? 3 : 2), vocab = rounded(s.vocab, dense::kBlockElements);
+    const uint64_t few = least(s.n, kThreePartRows) * 2 * 3, vocab = rounded(s.vocab, dense::kBlockElements);
     uint64_t tiled = least(of_dz * vocab, 2 * kPieceBytes + 256 * of_dz);
     tiled = tiled > least(few * vocab, 2 * kPieceBytes + 256 * few) ? tiled : least(few * vocab, 2 * kPieceBytes + 256 * few);
     const uint64_t narrow_dz = least(s.vocab * padded_rows(least(s.n, narrow_rows(s))) * sizeof(float), 2 * kPieceBytes);

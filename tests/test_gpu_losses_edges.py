@@ -271,3 +271,22 @@ def test_steps_of_few_rows_of_floats_and_of_weights_in_pieces(ctx, kind, n, voca
         _near(losses, want["losses"], "losses")
         _near(dx, want["dhidden"], "dhidden")
         _near(dw, want["dweight"], "dweight")
+
+
+@pytest.mark.parametrize("n", [5, 17, 64, 100, 128])
+def test_gradients_in_fp32_of_few_rows_are_those_of_fp32(ctx, n):
+    """One row with a gradient, one product in each logit, so dweight is p times dloss times a number.  Roundings on the way, of a logarithm of 30 terms below 8: its own
+    2^-21, its sum 2^-22, the exponent 2^-22, times log(2); the exponential's and the terms' 2^-23 each, the product's 2^-24, four of sums 2^-24: below 1.3e-6 together.
+    A dz of two bfloat16 is off by up to 2^-17 = 7.6e-6."""
+    vocab = 30
+    for seed in range(8):
+        g = torch.Generator(device=DEV).manual_seed(seed)
+        x, w = _normal(g, n, 1).bfloat16(), _normal(g, vocab, 1).bfloat16()
+        targets, dloss = torch.zeros(n, dtype=torch.int64, device=DEV), torch.zeros(n, device=DEV)
+        dloss[n // 2] = 1.0 + seed / 7
+        loss = P.VocabularyLoss(ctx, vocab, 1, n, gradient_dtype=torch.float32)
+        loss.cross_entropy(x, w, targets)
+        _, dw = loss.backward(dloss)
+        a = x[n // 2, 0].double()
+        want = torch.softmax(a * w[:, 0].double(), dim=0) * a * dloss[n // 2].double()
+        assert float(((dw[1:, 0].double() - want[1:]) / want[1:]).abs().max()) < 1.3e-6

@@ -238,7 +238,7 @@ class VocabularyLoss(_Holder):
     and without all logits in memory: softmax cross entropy, and distillation from up to ``top`` logits a row of a teacher.
 
     The object keeps a workspace and, from a loss in training to :meth:`backward`, what that loss was made of: its tensors must stay as they are until then.
-    ``gradient_dtype``: the type of the weight's gradient, ``dtype`` or float32 (which costs a second product where ``dtype`` has 16 bits).
+    ``gradient_dtype``: the type of the weight's gradient, ``dtype`` or float32 (which costs a second product where ``dtype`` has 16 bits, a third for up to 128 rows of bfloat16).
     It is no autograd function: results have no history, gradients are what :meth:`backward` returns.  A second loss in training, or any distillation, takes the
     place of the first; a call that is refused does not.
     Calls of one object belong on one stream."""
